@@ -3,7 +3,8 @@
 `Palsgd` is a thin ctypes binding over the C ABI in `include/palsgd.h`
 (`libpalsgd.so`, built in-tree by `paper_2504_18454_b200.build`).  Every step of
 the path runs in the library's CUDA kernels; this package only marshals
-arguments.  PyTorch supplies device memory and streams.
+arguments.  PyTorch supplies device memory and streams.  `block` binds the
+operators with which the K workers make their gradients (`include/palsgd_block.h`).
 """
 from .binding import (  # noqa: F401
     Palsgd,
@@ -31,4 +32,21 @@ from .binding import (  # noqa: F401
     TUNE_DDP_VARIANT,
     TUNE_OUTER_VARIANT,
     TUNE_OUTER_DYNAMIC,
+)
+from .block import (  # noqa: F401
+    Act8,
+    act8_pack,
+    act8_unpack,
+    ffn_backward,
+    ffn_forward,
+    qk_norm_rope,
+    qk_norm_rope_backward,
+    ACT8_GROUP,
+    ACT_GELU,
+    ACT_GELU_TANH,
+    ACT_RELU,
+    ACT_SILU,
+    SAVE_8BIT,
+    SAVE_FULL,
+    SAVE_NONE,
 )

@@ -87,6 +87,13 @@ class ReplicaArena:
     def views(self, name: str) -> List[List[torch.Tensor]]:
         return self._views[name]
 
+    def worker_tensor(self, name: str, j: int, *shape: int) -> torch.Tensor:
+        """Tensor j of every row of buffer kind `name` as one (rows, *shape) view (packed layouts only): what the block
+        operators take as the K workers' weights and write as their gradients."""
+        rows = self.rows(name)
+        flat = rows[:, self.starts[j]:self.starts[j + 1]]
+        return flat.unflatten(1, shape) if shape else flat
+
     def has(self, name: str) -> bool:
         return name in self._views
 

@@ -14,8 +14,8 @@ from pathlib import Path
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libpalsgd.so"
-SOURCES = [CSRC / "palsgd_api.cu", CSRC / "palsgd_noalloc.cu"]
-DEPS = sorted(CSRC.glob("*.cu*")) + [HERE.parent / "include" / "palsgd.h", Path(__file__)]
+SOURCES = [CSRC / "palsgd_api.cu", CSRC / "palsgd_noalloc.cu", CSRC / "block_api.cu"]
+DEPS = sorted(CSRC.glob("*.cu*")) + sorted(CSRC.glob("*.h")) + sorted((HERE.parent / "include").glob("*.h")) + [Path(__file__)]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

@@ -1,0 +1,443 @@
+// Host side of the block operators (see include/palsgd_block.h): checks of arguments, workspaces, launches.
+#include "block_common.cuh"
+#include "block_matmul.cuh"
+#include "block_rows.cuh"
+
+#include <cmath>
+
+#include "block_host.h"
+
+using namespace palsgd::block;
+
+namespace {
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+inline size_t elem(int32_t prec) { return prec == PALSGD_PREC_BF16_MASTER ? 2 : 4; }
+inline bool prec_ok(int32_t p) { return p == PALSGD_PREC_FP32 || p == PALSGD_PREC_BF16_MASTER; }
+
+constexpr uint64_t kMaxSize = 0x7FFFFFFFull;             // rows, columns, tokens: 31 bits (offsets are 64-bit)
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+
+struct Axis { uint64_t n; int64_t stride; };
+
+// No two of n0*n1*n2 runs of `run` contiguous elements at these strides share an element (sufficient condition: sorted
+// by stride, each axis steps over all of the axes inside it).
+bool disjoint(Axis a, Axis b, Axis c, uint64_t run)
+{
+    Axis v[3] = {a, b, c};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j + 1 < 3; ++j)
+            if (v[j].stride > v[j + 1].stride) { const Axis t = v[j]; v[j] = v[j + 1]; v[j + 1] = t; }
+    uint64_t span = run;
+    for (const Axis& x : v) {
+        if (x.n <= 1) continue;
+        if ((uint64_t)x.stride < span) return false;
+        span += (uint64_t)x.stride * (x.n - 1);
+    }
+    return true;
+}
+
+// A matrix argument: EINVAL / EALIGN / OK.  Nothing is asked of a matrix without elements.
+int check_mat(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, size_t es, bool output)
+{
+    if (!m) return PALSGD_EINVAL;
+    if (m->worker_stride < 0 || m->row_stride < 0 || m->worker_stride > kMaxStride || m->row_stride > kMaxStride) return PALSGD_EINVAL;
+    if (rows == 0 || cols == 0) return PALSGD_OK;
+    if (!m->data) return PALSGD_EINVAL;
+    if (!aligned(m->data, es)) return PALSGD_EALIGN;
+    if (output && !disjoint({K, m->worker_stride}, {rows, m->row_stride}, {1, 0}, cols)) return PALSGD_EINVAL;
+    return PALSGD_OK;
+}
+
+#define BLOCK_TRY(call) do { const int rc_ = (call); if (rc_ != PALSGD_OK) return rc_; } while (0)
+
+int launched(const char* what)
+{
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? PALSGD_OK : palsgd_block_cuda_fail((int)e, what);
+}
+
+int sm_count()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
+    return n;
+}
+
+// ------------------------------------------------------------------------------------------------ 8-bit checkpoints
+
+int check_act8(int32_t prec, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x, const palsgd_mat* q,
+               const palsgd_mat* e, bool pack)
+{
+    if (!prec_ok(prec) || K == 0 || K > PALSGD_MAX_WORKERS || rows > kMaxSize || cols > kMaxSize) return PALSGD_EINVAL;
+    BLOCK_TRY(check_mat(x, K, rows, cols, elem(prec), !pack));
+    BLOCK_TRY(check_mat(q, K, rows, cols, 1, pack));
+    BLOCK_TRY(check_mat(e, K, rows, ceil_div(cols, PALSGD_ACT8_GROUP), 1, pack));
+    return PALSGD_OK;
+}
+
+template <typename T, bool PACK>
+int launch_act8(uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x, const palsgd_mat* q, const palsgd_mat* e,
+                cudaStream_t st)
+{
+    if (rows == 0 || cols == 0) return PALSGD_OK;
+    Act8Args a{x->data, static_cast<int8_t*>(q->data), static_cast<uint8_t*>(e->data), x->worker_stride, x->row_stride,
+               q->worker_stride, q->row_stride, e->worker_stride, e->row_stride, rows, cols, 0, 0};
+    const bool wide = cols % 8 == 0 && aligned(x->data, 16) && (x->row_stride * sizeof(T)) % 16 == 0 && (x->worker_stride * sizeof(T)) % 16 == 0 &&
+                      aligned(q->data, 8) && q->row_stride % 8 == 0 && q->worker_stride % 8 == 0;
+    a.units_per_row = (uint32_t)(ceil_div(cols, 32) * (wide ? 4 : 32));
+    a.units = rows * a.units_per_row;
+    const uint64_t ctas = ceil_div(a.units, 256), most = 64ull * sm_count();
+    const dim3 grid((unsigned)(ctas < most ? ctas : most), K);
+    if (wide) act8_kernel<T, 8, PACK><<<grid, 256, 0, st>>>(a);
+    else act8_kernel<T, 1, PACK><<<grid, 256, 0, st>>>(a);
+    return launched(PACK ? "act8 pack" : "act8 unpack");
+}
+
+// ------------------------------------------------------------------------------------------------ feed-forward block
+
+int check_shape(const palsgd_ffn_shape* s)
+{
+    if (!s || s->K == 0 || s->K > PALSGD_MAX_WORKERS || !prec_ok(s->precision)) return PALSGD_EINVAL;
+    if (s->activation < PALSGD_ACT_SILU || s->activation > PALSGD_ACT_RELU) return PALSGD_EINVAL;
+    if (s->save < PALSGD_SAVE_NONE || s->save > PALSGD_SAVE_8BIT) return PALSGD_EINVAL;
+    if (s->d_model == 0 || s->d_ff == 0 || s->d_model > kMaxSize || s->d_ff > kMaxSize || s->tokens > kMaxSize) return PALSGD_EINVAL;
+    return PALSGD_OK;
+}
+
+int check_saved(const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e,
+                const palsgd_mat* up_e, bool output)
+{
+    const bool eight = s->save == PALSGD_SAVE_8BIT;
+    const size_t es = eight ? 1 : elem(s->precision);
+    BLOCK_TRY(check_mat(gate, s->K, s->tokens, s->d_ff, es, output));
+    BLOCK_TRY(check_mat(up, s->K, s->tokens, s->d_ff, es, output));
+    if (eight) {
+        BLOCK_TRY(check_mat(gate_e, s->K, s->tokens, ceil_div(s->d_ff, PALSGD_ACT8_GROUP), 1, output));
+        BLOCK_TRY(check_mat(up_e, s->K, s->tokens, ceil_div(s->d_ff, PALSGD_ACT8_GROUP), 1, output));
+    }
+    return PALSGD_OK;
+}
+
+// Hands out 256-byte aligned pieces of the workspace; with base = nullptr it only counts.
+struct Arena {
+    char* base;
+    size_t used;
+    void* take(size_t bytes)
+    {
+        void* p = base ? base + used : nullptr;
+        used += (bytes + 255) / 256 * 256;
+        return p;
+    }
+};
+
+int check_workspace(const void* ws, const size_t* bytes)
+{
+    if (!bytes) return PALSGD_EINVAL;
+    if (ws && !aligned(ws, 256)) return PALSGD_EALIGN;
+    return PALSGD_OK;
+}
+
+Operand operand(const palsgd_mat* m, bool mn) { return Operand{m->data, m->worker_stride, m->row_stride, mn}; }
+
+void set_saved(MatArgs& a, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e, const palsgd_mat* up_e)
+{
+    a.save = s->save;
+    if (s->save == PALSGD_SAVE_NONE) return;
+    a.gate = gate->data; a.gw = gate->worker_stride; a.gr = gate->row_stride;
+    a.up = up->data; a.uw = up->worker_stride; a.ur = up->row_stride;
+    if (s->save == PALSGD_SAVE_8BIT) {
+        a.gate_e = static_cast<uint8_t*>(gate_e->data); a.gew = gate_e->worker_stride; a.ger = gate_e->row_stride;
+        a.up_e = static_cast<uint8_t*>(up_e->data); a.uew = up_e->worker_stride; a.uer = up_e->row_stride;
+    }
+}
+
+template <int MODE>
+int launch_mat(int32_t prec, uint32_t K, const MatArgs& a, cudaStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(a.M, 64), (unsigned)ceil_div(a.N, 64), K);
+    if (prec == PALSGD_PREC_FP32) mat_kernel<float, MODE><<<grid, 256, 0, st>>>(a);
+    else mat_kernel<bf16, MODE><<<grid, 256, 0, st>>>(a);
+    return launched("matrix kernel");
+}
+
+int launch_product(const palsgd_ffn_shape* s, uint64_t M, uint64_t N, uint64_t Kd, const palsgd_mat* A0, const palsgd_mat* B0,
+                   const palsgd_mat* A1, const palsgd_mat* B1, bool amn, bool bmn, const palsgd_mat* out, cudaStream_t st)
+{
+    MatArgs a{};
+    a.n_seg = A1 ? 2 : 1;
+    a.A[0] = operand(A0, amn); a.B[0] = operand(B0, bmn);
+    if (A1) { a.A[1] = operand(A1, amn); a.B[1] = operand(B1, bmn); }
+    a.M = (uint32_t)M; a.N = (uint32_t)N; a.Kd = (uint32_t)Kd;
+    a.out[0] = out->data; a.ow = out->worker_stride; a.orow = out->row_stride;
+    return launch_mat<MAT_PLAIN>(s->precision, s->K, a, st);
+}
+
+// ------------------------------------------------------------------------------------------------ q/k norm + rotation
+
+int check_heads(const palsgd_heads* h, const palsgd_qk_shape* s, uint32_t heads, bool output)
+{
+    if (heads == 0) return PALSGD_OK;
+    if (!h || h->worker_stride < 0 || h->token_stride < 0 || h->head_stride < 0) return PALSGD_EINVAL;
+    if (h->worker_stride > kMaxStride || h->token_stride > kMaxStride || h->head_stride > kMaxStride) return PALSGD_EINVAL;
+    if (s->tokens == 0) return PALSGD_OK;
+    if (!h->data) return PALSGD_EINVAL;
+    if (!aligned(h->data, elem(s->precision))) return PALSGD_EALIGN;
+    if (output && !disjoint({s->K, h->worker_stride}, {s->tokens, h->token_stride}, {heads, h->head_stride}, s->head_dim)) return PALSGD_EINVAL;
+    return PALSGD_OK;
+}
+
+int check_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos)
+{
+    if (!s || s->K == 0 || s->K > PALSGD_MAX_WORKERS || !prec_ok(s->precision) || s->reserved_ != 0) return PALSGD_EINVAL;
+    if (s->tokens > kMaxSize || s->heads_q > 65535u || s->heads_k > 65535u) return PALSGD_EINVAL;
+    if (s->head_dim == 0 || s->rotary_dim > s->head_dim || s->rotary_dim % 2) return PALSGD_EINVAL;
+    if (s->interleaved != 0 && s->interleaved != 1) return PALSGD_EINVAL;
+    if (!(std::isfinite(s->eps) && s->eps >= 0.0)) return PALSGD_EINVAL;
+    if (s->pos_worker_stride < 0 || s->pos_worker_stride > kMaxStride || s->table_rows > kMaxSize) return PALSGD_EINVAL;
+    if (s->rotary_dim && s->tokens) {
+        if (!pos || (s->table_rows && (!cos_t || !sin_t))) return PALSGD_EINVAL;
+        if (!aligned(pos, 4) || !aligned(cos_t, 4) || !aligned(sin_t, 4)) return PALSGD_EALIGN;
+    }
+    if (s->head_dim > 512) return PALSGD_EUNSUPPORTED;
+    return PALSGD_OK;
+}
+
+bool heads_wide(const void* p, int64_t w, int64_t t, int64_t h, size_t es)
+{
+    return aligned(p, 16) && (w * es) % 16 == 0 && (t * es) % 16 == 0 && (h * es) % 16 == 0;
+}
+
+struct QkPlan { QkArgs a; int V, NS; unsigned ctas; };
+
+QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos, bool back)
+{
+    QkPlan p{};
+    QkArgs& a = p.a;
+    a.cos_t = cos_t; a.sin_t = sin_t; a.pos = pos; a.pos_w = s->pos_worker_stride;
+    a.tokens = s->tokens; a.table_rows = s->table_rows; a.head_dim = s->head_dim; a.rot = s->rotary_dim;
+    a.interleaved = s->interleaved; a.eps = (float)s->eps;
+    a.side[0].heads = s->heads_q; a.side[1].heads = s->heads_k;
+    const uint64_t per_side = (uint64_t)s->K * ((s->heads_q ? 1 : 0) + (s->heads_k ? 1 : 0));
+    const uint64_t want = ceil_div(s->tokens, 8), most = ceil_div((uint64_t)sm_count() * (back ? 3 : 6), per_side ? per_side : 1);
+    p.ctas = (unsigned)(want < most ? (want ? want : 1) : most);
+    return p;
+}
+
+void finish_qk(QkPlan& p, const palsgd_qk_shape* s, bool back)
+{
+    QkArgs& a = p.a;
+    const size_t es = elem(s->precision);
+    const int v = (int)(16 / es);
+    bool wide = s->head_dim % v == 0 && (s->interleaved || (s->rotary_dim / 2) % v == 0);
+    for (const HeadsArg& h : a.side)
+        if (h.heads)
+            wide = wide && heads_wide(h.x, h.xw, h.xt, h.xh, es) && heads_wide(h.out, h.ow, h.ot, h.oh, es) &&
+                   (!back || heads_wide(h.d, h.dw, h.dt, h.dh, es));
+    p.V = wide ? v : 1;
+    const uint32_t half_vec = s->rotary_dim / 2 / p.V, n_vec = s->head_dim / p.V;
+    a.pair_slots = s->interleaved ? (p.V == 1 ? s->rotary_dim / 2 : 0) : half_vec;
+    a.slots = s->interleaved ? (n_vec + 1) / 2 : half_vec + (n_vec - 2 * half_vec + 1) / 2;
+    a.lanes = 1;
+    while (a.lanes < 32 && a.lanes < a.slots) a.lanes *= 2;
+    p.NS = 1;
+    while ((uint32_t)p.NS * a.lanes < a.slots) p.NS *= 2;
+}
+
+template <typename T, bool BACK>
+int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
+{
+    const dim3 grid(p.ctas, 2, s->K);
+    const size_t sm = BACK ? 8 * (size_t)s->head_dim * sizeof(float) : 0;
+    constexpr int W = 16 / (int)sizeof(T);
+    if (p.V == W && p.NS == 1) qk_kernel<T, W, 1, BACK><<<grid, 256, sm, st>>>(p.a);
+    else if (p.V == W) qk_kernel<T, W, 2, BACK><<<grid, 256, sm, st>>>(p.a);
+    else if (p.NS == 1) qk_kernel<T, 1, 1, BACK><<<grid, 256, sm, st>>>(p.a);
+    else if (p.NS == 2) qk_kernel<T, 1, 2, BACK><<<grid, 256, sm, st>>>(p.a);
+    else if (p.NS == 4) qk_kernel<T, 1, 4, BACK><<<grid, 256, sm, st>>>(p.a);
+    else qk_kernel<T, 1, 8, BACK><<<grid, 256, sm, st>>>(p.a);
+    return launched("q/k norm + rotation");
+}
+
+}  // namespace
+
+extern "C" int palsgd_act8_pack(int32_t precision, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x,
+                                const palsgd_mat* q, const palsgd_mat* e, void* stream)
+{
+    BLOCK_TRY(check_act8(precision, K, rows, cols, x, q, e, true));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return precision == PALSGD_PREC_FP32 ? launch_act8<float, true>(K, rows, cols, x, q, e, st)
+                                         : launch_act8<bf16, true>(K, rows, cols, x, q, e, st);
+}
+
+extern "C" int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* q,
+                                  const palsgd_mat* e, const palsgd_mat* x, void* stream)
+{
+    BLOCK_TRY(check_act8(precision, K, rows, cols, x, q, e, false));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return precision == PALSGD_PREC_FP32 ? launch_act8<float, false>(K, rows, cols, x, q, e, st)
+                                         : launch_act8<bf16, false>(K, rows, cols, x, q, e, st);
+}
+
+extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x, const palsgd_mat* w_gate,
+                                  const palsgd_mat* w_up, const palsgd_mat* w_down, const palsgd_mat* y,
+                                  const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e,
+                                  const palsgd_mat* up_e, void* workspace, size_t* workspace_bytes, void* stream)
+{
+    BLOCK_TRY(check_shape(s));
+    const uint64_t M = s->tokens, D = s->d_model, F = s->d_ff;
+    const size_t es = elem(s->precision);
+    BLOCK_TRY(check_mat(x, s->K, M, D, es, false));
+    BLOCK_TRY(check_mat(w_gate, s->K, F, D, es, false));
+    BLOCK_TRY(check_mat(w_up, s->K, F, D, es, false));
+    BLOCK_TRY(check_mat(w_down, s->K, D, F, es, false));
+    BLOCK_TRY(check_mat(y, s->K, M, D, es, true));
+    if (s->save != PALSGD_SAVE_NONE) BLOCK_TRY(check_saved(s, gate, up, gate_e, up_e, true));
+    BLOCK_TRY(check_workspace(workspace, workspace_bytes));
+    Arena ws{static_cast<char*>(workspace), 0};
+    const palsgd_mat h{ws.take((size_t)s->K * M * F * es), (int64_t)(M * F), (int64_t)F};
+    if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
+    if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
+    if (M == 0) return PALSGD_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    MatArgs a{};
+    a.n_seg = 1;
+    a.A[0] = operand(x, false); a.B[0] = operand(w_gate, false); a.B[1] = operand(w_up, false);
+    a.M = (uint32_t)M; a.N = (uint32_t)F; a.Kd = (uint32_t)D; a.act = s->activation;
+    a.out[0] = h.data; a.ow = h.worker_stride; a.orow = h.row_stride;
+    set_saved(a, s, gate, up, gate_e, up_e);
+    BLOCK_TRY(launch_mat<MAT_GATED>(s->precision, s->K, a, st));
+    return launch_product(s, M, D, F, &h, w_down, nullptr, nullptr, false, false, y, st);
+}
+
+extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* dy, const palsgd_mat* x, const palsgd_mat* x_e,
+                                   const palsgd_mat* w_gate, const palsgd_mat* w_up, const palsgd_mat* w_down,
+                                   const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e,
+                                   const palsgd_mat* up_e, const palsgd_mat* dx, const palsgd_mat* dw_gate,
+                                   const palsgd_mat* dw_up, const palsgd_mat* dw_down, void* workspace,
+                                   size_t* workspace_bytes, void* stream)
+{
+    BLOCK_TRY(check_shape(s));
+    if (s->save == PALSGD_SAVE_NONE || (x_e && s->save != PALSGD_SAVE_8BIT)) return PALSGD_EINVAL;
+    const uint64_t M = s->tokens, D = s->d_model, F = s->d_ff;
+    const size_t es = elem(s->precision);
+    BLOCK_TRY(check_mat(dy, s->K, M, D, es, false));
+    BLOCK_TRY(check_mat(x, s->K, M, D, x_e ? 1 : es, false));
+    if (x_e) BLOCK_TRY(check_mat(x_e, s->K, M, ceil_div(D, PALSGD_ACT8_GROUP), 1, false));
+    BLOCK_TRY(check_mat(w_gate, s->K, F, D, es, false));
+    BLOCK_TRY(check_mat(w_up, s->K, F, D, es, false));
+    BLOCK_TRY(check_mat(w_down, s->K, D, F, es, false));
+    BLOCK_TRY(check_saved(s, gate, up, gate_e, up_e, false));
+    if (dx) BLOCK_TRY(check_mat(dx, s->K, M, D, es, true));
+    BLOCK_TRY(check_mat(dw_gate, s->K, F, D, es, true));
+    BLOCK_TRY(check_mat(dw_up, s->K, F, D, es, true));
+    BLOCK_TRY(check_mat(dw_down, s->K, D, F, es, true));
+    BLOCK_TRY(check_workspace(workspace, workspace_bytes));
+    Arena ws{static_cast<char*>(workspace), 0};
+    palsgd_mat hid[3];                                   // dg, du, h
+    for (palsgd_mat& m : hid) m = palsgd_mat{ws.take((size_t)s->K * M * F * es), (int64_t)(M * F), (int64_t)F};
+    palsgd_mat xs = *x;
+    if (x_e) xs = palsgd_mat{ws.take((size_t)s->K * M * D * es), (int64_t)(M * D), (int64_t)D};
+    if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
+    if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (M) {
+        if (x_e) BLOCK_TRY(palsgd_act8_unpack(s->precision, s->K, M, D, x, x_e, &xs, stream));
+        MatArgs a{};
+        a.n_seg = 1;
+        a.A[0] = operand(dy, false); a.B[0] = operand(w_down, true);
+        a.M = (uint32_t)M; a.N = (uint32_t)F; a.Kd = (uint32_t)D; a.act = s->activation;
+        for (int i = 0; i < 3; ++i) a.out[i] = hid[i].data;
+        a.ow = hid[0].worker_stride; a.orow = hid[0].row_stride;
+        set_saved(a, s, gate, up, gate_e, up_e);
+        BLOCK_TRY(launch_mat<MAT_HIDDEN>(s->precision, s->K, a, st));
+    }
+    BLOCK_TRY(launch_product(s, F, D, M, &hid[0], &xs, nullptr, nullptr, true, true, dw_gate, st));
+    BLOCK_TRY(launch_product(s, F, D, M, &hid[1], &xs, nullptr, nullptr, true, true, dw_up, st));
+    BLOCK_TRY(launch_product(s, D, F, M, dy, &hid[2], nullptr, nullptr, true, true, dw_down, st));
+    if (dx && M) BLOCK_TRY(launch_product(s, M, D, F, &hid[0], w_gate, &hid[1], w_up, false, true, dx, st));
+    return PALSGD_OK;
+}
+
+extern "C" int palsgd_qk_norm_rope_forward(const palsgd_qk_shape* s, const palsgd_heads* q, const palsgd_heads* k,
+                                           const palsgd_mat* w_q, const palsgd_mat* w_k, const float* cos_table,
+                                           const float* sin_table, const int32_t* positions, const palsgd_heads* q_out,
+                                           const palsgd_heads* k_out, void* stream)
+{
+    BLOCK_TRY(check_qk(s, cos_table, sin_table, positions));
+    const palsgd_heads *in[2] = {q, k}, *out[2] = {q_out, k_out};
+    const palsgd_mat* w[2] = {w_q, w_k};
+    const uint32_t heads[2] = {s->heads_q, s->heads_k};
+    for (int i = 0; i < 2; ++i) {
+        BLOCK_TRY(check_heads(in[i], s, heads[i], false));
+        BLOCK_TRY(check_heads(out[i], s, heads[i], true));
+        if (heads[i]) BLOCK_TRY(check_mat(w[i], s->K, 1, s->head_dim, elem(s->precision), false));
+    }
+    if (s->tokens == 0 || (heads[0] | heads[1]) == 0) return PALSGD_OK;
+    QkPlan p = plan_qk(s, cos_table, sin_table, positions, false);
+    for (int i = 0; i < 2; ++i) {
+        if (!heads[i]) continue;
+        HeadsArg& h = p.a.side[i];
+        h.x = in[i]->data; h.xw = in[i]->worker_stride; h.xt = in[i]->token_stride; h.xh = in[i]->head_stride;
+        h.out = out[i]->data; h.ow = out[i]->worker_stride; h.ot = out[i]->token_stride; h.oh = out[i]->head_stride;
+        h.w = w[i]->data; h.ww = w[i]->worker_stride;
+    }
+    finish_qk(p, s, false);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return s->precision == PALSGD_PREC_FP32 ? launch_qk<float, false>(p, s, st) : launch_qk<bf16, false>(p, s, st);
+}
+
+extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const palsgd_heads* dq_out, const palsgd_heads* dk_out,
+                                            const palsgd_heads* q, const palsgd_heads* k, const palsgd_mat* w_q,
+                                            const palsgd_mat* w_k, const float* cos_table, const float* sin_table,
+                                            const int32_t* positions, const palsgd_heads* dq, const palsgd_heads* dk,
+                                            const palsgd_mat* dw_q, const palsgd_mat* dw_k, void* workspace,
+                                            size_t* workspace_bytes, void* stream)
+{
+    BLOCK_TRY(check_qk(s, cos_table, sin_table, positions));
+    const palsgd_heads *in[2] = {q, k}, *grad[2] = {dq_out, dk_out}, *out[2] = {dq, dk};
+    const palsgd_mat *w[2] = {w_q, w_k}, *dw[2] = {dw_q, dw_k};
+    const uint32_t heads[2] = {s->heads_q, s->heads_k};
+    for (int i = 0; i < 2; ++i) {
+        BLOCK_TRY(check_heads(grad[i], s, heads[i], false));
+        BLOCK_TRY(check_heads(in[i], s, heads[i], false));
+        BLOCK_TRY(check_heads(out[i], s, heads[i], true));
+        if (!heads[i]) continue;
+        BLOCK_TRY(check_mat(w[i], s->K, 1, s->head_dim, elem(s->precision), false));
+        BLOCK_TRY(check_mat(dw[i], s->K, 1, s->head_dim, elem(s->precision), true));
+    }
+    BLOCK_TRY(check_workspace(workspace, workspace_bytes));
+    QkPlan p = plan_qk(s, cos_table, sin_table, positions, true);
+    Arena ws{static_cast<char*>(workspace), 0};
+    float* part[2] = {nullptr, nullptr};
+    for (int i = 0; i < 2; ++i)
+        if (heads[i]) part[i] = static_cast<float*>(ws.take((size_t)s->K * p.ctas * s->head_dim * sizeof(float)));
+    if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
+    if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
+    if ((heads[0] | heads[1]) == 0) return PALSGD_OK;
+    QkSumArgs sum{};
+    for (int i = 0; i < 2; ++i) {
+        if (!heads[i]) continue;
+        HeadsArg& h = p.a.side[i];
+        h.x = in[i]->data; h.xw = in[i]->worker_stride; h.xt = in[i]->token_stride; h.xh = in[i]->head_stride;
+        h.d = grad[i]->data; h.dw = grad[i]->worker_stride; h.dt = grad[i]->token_stride; h.dh = grad[i]->head_stride;
+        h.out = out[i]->data; h.ow = out[i]->worker_stride; h.ot = out[i]->token_stride; h.oh = out[i]->head_stride;
+        h.w = w[i]->data; h.ww = w[i]->worker_stride;
+        h.part = part[i];
+        sum.part[i] = part[i]; sum.dw[i] = dw[i]->data; sum.dww[i] = dw[i]->worker_stride; sum.heads[i] = heads[i];
+    }
+    finish_qk(p, s, true);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    sum.parts = s->tokens ? p.ctas : 0;
+    sum.head_dim = s->head_dim;
+    const dim3 grid((unsigned)ceil_div(s->head_dim, 32), 2, s->K);
+    if (s->precision == PALSGD_PREC_FP32) {
+        if (s->tokens) BLOCK_TRY((launch_qk<float, true>(p, s, st)));
+        qk_sum_kernel<float><<<grid, 256, 0, st>>>(sum);
+    } else {
+        if (s->tokens) BLOCK_TRY((launch_qk<bf16, true>(p, s, st)));
+        qk_sum_kernel<bf16><<<grid, 256, 0, st>>>(sum);
+    }
+    return launched("q/k weight gradient");
+}

@@ -1,0 +1,110 @@
+// Pieces that the block operators' kernels share: storage types, 16-byte vectors, the gated activations.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/palsgd_block.h"
+
+namespace palsgd {
+namespace block {
+
+using bf16 = __nv_bfloat16;
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+// V consecutive values of T at p as floats: one 16-byte (or 32-byte, as two) access where V fills it, else one by one.
+template <typename T, int V> struct Vec;
+template <> struct Vec<float, 1> {
+    static __device__ __forceinline__ void load(const float* p, float* v) { v[0] = __ldg(p); }
+    static __device__ __forceinline__ void store(float* p, const float* v) { p[0] = v[0]; }
+};
+template <> struct Vec<bf16, 1> {
+    static __device__ __forceinline__ void load(const bf16* p, float* v) { v[0] = __bfloat162float(p[0]); }
+    static __device__ __forceinline__ void store(bf16* p, const float* v) { p[0] = __float2bfloat16_rn(v[0]); }
+};
+template <> struct Vec<float, 4> {
+    static __device__ __forceinline__ void load(const float* p, float* v)
+    {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(p));
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    }
+    static __device__ __forceinline__ void store(float* p, const float* v)
+    {
+        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+};
+template <> struct Vec<float, 8> {
+    static __device__ __forceinline__ void load(const float* p, float* v) { Vec<float, 4>::load(p, v); Vec<float, 4>::load(p + 4, v + 4); }
+    static __device__ __forceinline__ void store(float* p, const float* v) { Vec<float, 4>::store(p, v); Vec<float, 4>::store(p + 4, v + 4); }
+};
+template <> struct Vec<bf16, 8> {
+    static __device__ __forceinline__ void load(const bf16* p, float* v)
+    {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    }
+    static __device__ __forceinline__ void store(bf16* p, const float* v)
+    {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+// ---- 8-bit checkpoints: the step 2^(E-127) of a group from the largest magnitude in it (as bits: NaN > Inf > finite).
+// Adding 2^16 to the bits carries into the exponent exactly when the mantissa is >= 1.9921875 = 127.5/64, the values
+// that would round to 128 steps; ties (127.5) go to the even 128 and are among them.  A carry out of the largest finite
+// exponent is a value that rounds to 2^128: not representable, like an infinity.
+__device__ __forceinline__ uint32_t act8_exponent(uint32_t amax_bits)
+{
+    const uint32_t b = amax_bits + 0x10000u;
+    const int e = (int)(b >> 23) - 6;
+    return b >= 0x7F800000u ? 255u : (uint32_t)(e < 1 ? 1 : e);
+}
+// 1 / step as a float (0 for a group that is not finite: its q are 0 -- NaN * 0 converts to 0 too)
+__device__ __forceinline__ float act8_inverse(uint32_t E) { return E == 255u ? 0.0f : __uint_as_float((254u - E) << 23); }
+__device__ __forceinline__ float act8_step(uint32_t E) { return E == 255u ? __uint_as_float(0x7FFFFFFFu) : __uint_as_float(E << 23); }
+// x and 1/step as above: |x / step| rounds to at most 127, so the low byte of the integer is the int8
+__device__ __forceinline__ int act8_quant(float x, float inv) { return __float2int_rn(x * inv); }
+
+// ---- gated activations
+// SLOPE: also act'(g).  FAST: exp and division to about 2 units in the last place of binary32, for results that are
+// rounded to bfloat16 anyway.
+template <int ACT, bool SLOPE, bool FAST>
+__device__ __forceinline__ float act(float g, float& slope)
+{
+    if constexpr (ACT == PALSGD_ACT_SILU) {
+        const float s = FAST ? __fdividef(1.0f, 1.0f + __expf(-g)) : 1.0f / (1.0f + expf(-g));
+        const float a = g * s;
+        if constexpr (SLOPE) slope = fmaf(a, 1.0f - s, s);
+        return a;
+    } else if constexpr (ACT == PALSGD_ACT_GELU) {
+        const float cdf = fmaf(0.5f, erff(g * 0.70710678118654752f), 0.5f);
+        if constexpr (SLOPE) slope = fmaf(g * 0.39894228040143268f, FAST ? __expf(-0.5f * g * g) : expf(-0.5f * g * g), cdf);
+        return g * cdf;
+    } else if constexpr (ACT == PALSGD_ACT_GELU_TANH) {
+        // (1 + tanh z) / 2 = 1 / (1 + e^(-2z))
+        const float c = 1.5957691216057308f;                     // 2 sqrt(2/pi)
+        const float z2 = c * g * fmaf(0.044715f * g, g, 1.0f);
+        const float s = FAST ? __fdividef(1.0f, 1.0f + __expf(-z2)) : 1.0f / (1.0f + expf(-z2));
+        if constexpr (SLOPE) slope = fmaf(g * s * (1.0f - s), c * fmaf(0.134145f * g, g, 1.0f), s);
+        return g * s;
+    } else {
+        if constexpr (SLOPE) slope = g > 0.0f ? 1.0f : 0.0f;
+        return g > 0.0f ? g : 0.0f;
+    }
+}
+
+}  // namespace block
+}  // namespace palsgd

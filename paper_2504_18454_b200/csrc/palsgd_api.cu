@@ -17,6 +17,7 @@
 #include <string>
 #include <vector>
 
+#include "block_host.h"
 #include "palsgd_kernels.cuh"
 #include "palsgd_norm.cuh"
 
@@ -1290,6 +1291,8 @@ extern "C" const char* palsgd_strerror(int status)
         default: return "unknown status";
     }
 }
+
+int palsgd_block_cuda_fail(int cuda_error, const char* what) { return cuda_fail(nullptr, (cudaError_t)cuda_error, what); }
 
 extern "C" const char* palsgd_last_cuda_error(palsgd_ctx* ctx)
 {
