@@ -100,6 +100,13 @@ int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* dy, const p
                         const palsgd_mat* dw_down, void* workspace, size_t* workspace_bytes, void* stream);
 
 /*
+ * The matrix kernels' waits for their own copies and products are bounded (a few seconds).  One that gave up -- which
+ * no input should bring about -- leaves its outputs unspecified and a note on the device: this call returns
+ * PALSGD_ECUDA once if there is one, else PALSGD_OK.  SYNCHRONISES the stream.
+ */
+int palsgd_block_status(void* stream);
+
+/*
  * Norm of queries and keys for each head, with the position rotation in the same pass.  For worker k, token t, head h
  * of q (and, with its own weights, of k), x in R^head_dim:
  *   r = 1 / sqrt(mean(x^2) + eps);  n = x r w;   the first rotary_dim values of n are rotated by pairs (a, b):

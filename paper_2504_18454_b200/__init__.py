@@ -37,6 +37,7 @@ from .block import (  # noqa: F401
     Act8,
     act8_pack,
     act8_unpack,
+    block_status,
     ffn_backward,
     ffn_forward,
     qk_norm_rope,

@@ -66,7 +66,8 @@ def lib() -> C.CDLL:
         L.palsgd_qk_norm_rope_forward.argtypes = [C.POINTER(QkShape), H, H, M, M, vp, vp, vp, H, H, vp]
         L.palsgd_qk_norm_rope_backward.argtypes = ([C.POINTER(QkShape), H, H, H, H, M, M, vp, vp, vp, H, H, M, M]
                                                    + [vp, size, vp])
-        for n in ("act8_pack", "act8_unpack", "ffn_forward", "ffn_backward", "qk_norm_rope_forward",
+        L.palsgd_block_status.argtypes = [vp]
+        for n in ("block_status", "act8_pack", "act8_unpack", "ffn_forward", "ffn_backward", "qk_norm_rope_forward",
                   "qk_norm_rope_backward"):
             getattr(L, "palsgd_" + n).restype = C.c_int
         _ready = True
@@ -162,6 +163,13 @@ def _workspace(call, given: Optional[torch.Tensor], device, where: str):
         _refuse(where, f"workspace must be a contiguous uint8 tensor on {device}")
     n.value = given.numel()
     _check(call(C.c_void_p(given.data_ptr()), C.byref(n)), where)
+
+
+def block_status(stream: Optional[int] = None) -> None:
+    """palsgd_block_status: raises PalsgdError if a matrix kernel's bounded wait gave up since the last call (its outputs
+    are then unspecified).  Synchronises the stream."""
+    raw = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    _check(lib().palsgd_block_status(C.c_void_p(raw)), "palsgd_block_status")
 
 
 # ---------------------------------------------------------------------------------------------- 8-bit checkpoints

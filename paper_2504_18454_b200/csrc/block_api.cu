@@ -3,7 +3,10 @@
 #include "block_matmul.cuh"
 #include "block_rows.cuh"
 
+#include <cudaTypedefs.h>
+
 #include <cmath>
+#include <mutex>
 
 #include "block_host.h"
 
@@ -139,39 +142,172 @@ int check_workspace(const void* ws, const size_t* bytes)
     return PALSGD_OK;
 }
 
-Operand operand(const palsgd_mat* m, bool mn) { return Operand{m->data, m->worker_stride, m->row_stride, mn}; }
+// Set by a kernel whose wait gave up (see palsgd_block_status).
+__device__ unsigned int g_gave_up;
 
-void set_saved(MatArgs& a, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e, const palsgd_mat* up_e)
+constexpr int kMaxDevices = 64;
+
+// What the matrix kernels need of a device, looked up on its first call.
+struct Device {
+    bool ready;
+    int sms;
+    unsigned int* gave_up;
+};
+Device g_device[kMaxDevices];
+PFN_cuTensorMapEncodeTiled_v12000 g_encode;
+std::mutex g_mutex;
+
+template <typename T, int MODE>
+cudaError_t allow_smem() { return cudaFuncSetAttribute(mat_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMatSmem); }
+
+int device_of(Device& out)
 {
-    a.save = s->save;
-    if (s->save == PALSGD_SAVE_NONE) return;
-    a.gate = gate->data; a.gw = gate->worker_stride; a.gr = gate->row_stride;
-    a.up = up->data; a.uw = up->worker_stride; a.ur = up->row_stride;
-    if (s->save == PALSGD_SAVE_8BIT) {
-        a.gate_e = static_cast<uint8_t*>(gate_e->data); a.gew = gate_e->worker_stride; a.ger = gate_e->row_stride;
-        a.up_e = static_cast<uint8_t*>(up_e->data); a.uew = up_e->worker_stride; a.uer = up_e->row_stride;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return palsgd_block_cuda_fail((int)e, "cudaGetDevice");
+    if (dev < 0 || dev >= kMaxDevices) return PALSGD_EUNSUPPORTED;
+    std::lock_guard<std::mutex> lock(g_mutex);
+    Device& d = g_device[dev];
+    if (!d.ready) {
+        if (!g_encode) {
+            void* f = nullptr;
+            cudaDriverEntryPointQueryResult found;
+            e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+            if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !f)) e = cudaErrorSymbolNotFound;
+            if (e != cudaSuccess) return palsgd_block_cuda_fail((int)e, "cuTensorMapEncodeTiled");
+            g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+        }
+        void* p = nullptr;
+        e = cudaGetSymbolAddress(&p, g_gave_up);
+        if (e == cudaSuccess) e = allow_smem<float, MAT_PLAIN>();
+        if (e == cudaSuccess) e = allow_smem<float, MAT_GATED>();
+        if (e == cudaSuccess) e = allow_smem<float, MAT_HIDDEN>();
+        if (e == cudaSuccess) e = allow_smem<bf16, MAT_PLAIN>();
+        if (e == cudaSuccess) e = allow_smem<bf16, MAT_GATED>();
+        if (e == cudaSuccess) e = allow_smem<bf16, MAT_HIDDEN>();
+        if (e != cudaSuccess) return palsgd_block_cuda_fail((int)e, "matrix kernel set-up");
+        d.gave_up = static_cast<unsigned int*>(p);
+        d.sms = sm_count();
+        d.ready = true;
     }
+    out = d;
+    return PALSGD_OK;
+}
+
+// An operand as the copy engine reads it: bfloat16 [parts][K][rows][cols], in the caller's memory or the workspace.
+struct Operand {
+    const void* p;
+    int64_t w, r, part;
+    uint64_t rows, cols;
+    uint32_t K, parts;
+    bool one;                                            // all workers read one matrix
+};
+
+struct Stage {
+    StageArgs a{};
+    uint32_t n = 0;
+};
+
+// Rows in the workspace: bfloat16 in rows of a multiple of 16 bytes.
+Operand own_operand(Arena& ws, uint32_t K, uint64_t rows, uint64_t cols, uint32_t parts)
+{
+    const int64_t ld = (int64_t)(ceil_div(cols, 8) * 8);
+    Operand o{nullptr, ld * (int64_t)rows, ld, ld * (int64_t)rows * K, rows, cols, K, parts, false};
+    o.p = ws.take((size_t)parts * o.part * 2);
+    return o;
+}
+
+// Reads m in place where the copy engine can (bfloat16, 16-byte boundaries), else puts it on the list of copies.
+Operand input_operand(Arena& ws, Stage& st, const palsgd_mat* m, const palsgd_mat* e, int32_t prec, uint32_t K, uint64_t rows, uint64_t cols)
+{
+    const bool one = K == 1 || m->worker_stride == 0;
+    const int64_t w = one ? 0 : m->worker_stride, r = rows == 1 ? (int64_t)(ceil_div(cols, 8) * 8) : m->row_stride;
+    if (!e && prec == PALSGD_PREC_BF16_MASTER && aligned(m->data, 16) && r % 8 == 0 && w % 8 == 0 && r >= (int64_t)cols &&
+        r < kMaxStride / 2 && w < kMaxStride / 2)
+        return Operand{m->data, w, r, 0, rows, cols, K, 1, one};
+    const int kind = e ? STAGE_ACT8 : prec == PALSGD_PREC_FP32 ? STAGE_SPLIT : STAGE_BF16;
+    const uint32_t copies = one && (!e || K == 1 || e->worker_stride == 0) ? 1 : K;
+    Operand o = own_operand(ws, copies, rows, cols, kind == STAGE_SPLIT ? 3 : 1);
+    o.K = K;
+    o.one = copies == 1;
+    StageItem& it = st.a.item[st.n++];
+    it = StageItem{m->data, e ? static_cast<const uint8_t*>(e->data) : nullptr, w, m->row_stride, e ? e->worker_stride : 0, e ? e->row_stride : 0,
+                   static_cast<bf16*>(const_cast<void*>(o.p)), o.r, o.part, (uint32_t)rows, (uint32_t)cols, rows * (uint64_t)(o.r / 8), kind, copies};
+    return o;
+}
+
+int run_stage(const Stage& st, uint32_t K, int sms, cudaStream_t stream)
+{
+    if (st.n == 0) return PALSGD_OK;
+    uint64_t most = 1;
+    for (uint32_t i = 0; i < st.n; ++i) most = st.a.item[i].units > most ? st.a.item[i].units : most;
+    const uint64_t want = ceil_div(most, 256), cap = 32ull * sms;
+    stage_kernel<<<dim3((unsigned)(want < cap ? want : cap), st.n, K), 256, 0, stream>>>(st.a);
+    return launched("operand copies");
+}
+
+int encode(CUtensorMap* map, const Operand& o, bool mn)
+{
+    const cuuint64_t dims[4] = {o.cols, o.rows, o.one ? 1u : o.K, o.parts};
+    // a dimension of one element is never stepped over, but its stride has to be a valid one
+    const cuuint64_t row = (cuuint64_t)o.r * 2, w = o.one ? row : (cuuint64_t)o.w * 2, part = o.parts > 1 ? (cuuint64_t)o.part * 2 : row;
+    const cuuint64_t strides[3] = {row, w, part};
+    const cuuint32_t box[4] = {64, mn ? kTileK : 128u, 1, 1}, unit[4] = {1, 1, 1, 1};
+    const CUresult rc = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.p), dims, strides, box, unit,
+                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? PALSGD_OK : palsgd_block_cuda_fail((int)cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+}
+
+MatOut out_of(const palsgd_mat* m, size_t es)
+{
+    MatOut o{m->data, m->worker_stride, m->row_stride, 0, 0};
+    o.wide = aligned(m->data, 16) && (m->worker_stride * es) % 16 == 0 && (m->row_stride * es) % 16 == 0;
+    return o;
+}
+MatOut out_of(const Operand& o) { return MatOut{const_cast<void*>(o.p), o.w, o.r, o.part, 1}; }
+
+// One product appended to a launch; B1/A1: the second segment, or (gate/up) the up weights as B1.
+int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, const Operand* A0, const Operand* A1, bool amn,
+                const Operand* B0, const Operand* B1, bool bmn, uint32_t n_step)
+{
+    MatProblem& p = L.p[L.n_problems++];
+    p.M = (uint32_t)M; p.N = (uint32_t)N; p.Kd = (uint32_t)Kd;
+    p.tiles_m = (uint32_t)ceil_div(M, kTileM); p.tiles_n = (uint32_t)ceil_div(N, n_step);
+    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n * K;
+    if (L.tiles + tiles > 0x7FFFFFFFull) return PALSGD_EUNSUPPORTED;
+    p.tiles = (uint32_t)tiles;
+    L.tiles += p.tiles;
+    p.n_seg = A1 ? 2 : 1;
+    p.a_parts = (uint8_t)A0->parts; p.b_parts = (uint8_t)B0->parts; p.a_mn = amn; p.b_mn = bmn;
+    const Operand *A[2] = {A0, A1}, *B[2] = {B0, B1};
+    for (int i = 0; i < 2; ++i) {
+        if (A[i]) { p.a_one[i] = A[i]->one; BLOCK_TRY(encode(&p.A[i], *A[i], amn)); }
+        if (B[i]) { p.b_one[i] = B[i]->one; BLOCK_TRY(encode(&p.B[i], *B[i], bmn)); }
+    }
+    return PALSGD_OK;
 }
 
 template <int MODE>
-int launch_mat(int32_t prec, uint32_t K, const MatArgs& a, cudaStream_t st)
+int run_mat(MatLaunch& L, int32_t prec, const Device& d, cudaStream_t st)
 {
-    const dim3 grid((unsigned)ceil_div(a.M, 64), (unsigned)ceil_div(a.N, 64), K);
-    if (prec == PALSGD_PREC_FP32) mat_kernel<float, MODE><<<grid, 256, 0, st>>>(a);
-    else mat_kernel<bf16, MODE><<<grid, 256, 0, st>>>(a);
+    if (L.tiles == 0) return PALSGD_OK;
+    L.gave_up = d.gave_up;
+    const uint32_t pairs = (uint32_t)(d.sms / 2) < L.tiles ? (uint32_t)(d.sms / 2) : L.tiles;
+    if (prec == PALSGD_PREC_FP32) mat_kernel<float, MODE><<<2 * pairs, kMatThreads, kMatSmem, st>>>(L);
+    else mat_kernel<bf16, MODE><<<2 * pairs, kMatThreads, kMatSmem, st>>>(L);
     return launched("matrix kernel");
 }
 
-int launch_product(const palsgd_ffn_shape* s, uint64_t M, uint64_t N, uint64_t Kd, const palsgd_mat* A0, const palsgd_mat* B0,
-                   const palsgd_mat* A1, const palsgd_mat* B1, bool amn, bool bmn, const palsgd_mat* out, cudaStream_t st)
+void set_saved(MatLaunch& L, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e, const palsgd_mat* up_e)
 {
-    MatArgs a{};
-    a.n_seg = A1 ? 2 : 1;
-    a.A[0] = operand(A0, amn); a.B[0] = operand(B0, bmn);
-    if (A1) { a.A[1] = operand(A1, amn); a.B[1] = operand(B1, bmn); }
-    a.M = (uint32_t)M; a.N = (uint32_t)N; a.Kd = (uint32_t)Kd;
-    a.out[0] = out->data; a.ow = out->worker_stride; a.orow = out->row_stride;
-    return launch_mat<MAT_PLAIN>(s->precision, s->K, a, st);
+    L.save = s->save;
+    L.act = s->activation;
+    if (s->save == PALSGD_SAVE_NONE) return;
+    const size_t es = s->save == PALSGD_SAVE_8BIT ? 1 : elem(s->precision);
+    L.gate = out_of(gate, es);
+    L.up = out_of(up, es);
+    if (s->save == PALSGD_SAVE_8BIT) { L.gate_e = out_of(gate_e, 1); L.up_e = out_of(up_e, 1); }
 }
 
 // ------------------------------------------------------------------------------------------------ q/k norm + rotation
@@ -296,19 +432,31 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
     if (s->save != PALSGD_SAVE_NONE) BLOCK_TRY(check_saved(s, gate, up, gate_e, up_e, true));
     BLOCK_TRY(check_workspace(workspace, workspace_bytes));
     Arena ws{static_cast<char*>(workspace), 0};
-    const palsgd_mat h{ws.take((size_t)s->K * M * F * es), (int64_t)(M * F), (int64_t)F};
+    Stage stage;
+    const uint32_t parts = s->precision == PALSGD_PREC_FP32 ? 3 : 1;
+    Operand ox, og, ou, od, oh;
+    if (M) {
+        ox = input_operand(ws, stage, x, nullptr, s->precision, s->K, M, D);
+        og = input_operand(ws, stage, w_gate, nullptr, s->precision, s->K, F, D);
+        ou = input_operand(ws, stage, w_up, nullptr, s->precision, s->K, F, D);
+        od = input_operand(ws, stage, w_down, nullptr, s->precision, s->K, D, F);
+        oh = own_operand(ws, s->K, M, F, parts);
+    }
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
     if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
     if (M == 0) return PALSGD_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    MatArgs a{};
-    a.n_seg = 1;
-    a.A[0] = operand(x, false); a.B[0] = operand(w_gate, false); a.B[1] = operand(w_up, false);
-    a.M = (uint32_t)M; a.N = (uint32_t)F; a.Kd = (uint32_t)D; a.act = s->activation;
-    a.out[0] = h.data; a.ow = h.worker_stride; a.orow = h.row_stride;
-    set_saved(a, s, gate, up, gate_e, up_e);
-    BLOCK_TRY(launch_mat<MAT_GATED>(s->precision, s->K, a, st));
-    return launch_product(s, M, D, F, &h, w_down, nullptr, nullptr, false, false, y, st);
+    Device dev{};
+    BLOCK_TRY(device_of(dev));
+    MatLaunch gated{}, down{};
+    BLOCK_TRY(add_problem(gated, M, F, D, s->K, &ox, nullptr, false, &og, &ou, false, kTileN / 2));
+    gated.p[0].out[0] = out_of(oh);
+    set_saved(gated, s, gate, up, gate_e, up_e);
+    BLOCK_TRY(add_problem(down, M, D, F, s->K, &oh, nullptr, false, &od, nullptr, false, kTileN));
+    down.p[0].out[0] = out_of(y, es);
+    BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
+    BLOCK_TRY(run_mat<MAT_GATED>(gated, s->precision, dev, st));
+    return run_mat<MAT_PLAIN>(down, s->precision, dev, st);
 }
 
 extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* dy, const palsgd_mat* x, const palsgd_mat* x_e,
@@ -335,29 +483,67 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     BLOCK_TRY(check_mat(dw_down, s->K, D, F, es, true));
     BLOCK_TRY(check_workspace(workspace, workspace_bytes));
     Arena ws{static_cast<char*>(workspace), 0};
-    palsgd_mat hid[3];                                   // dg, du, h
-    for (palsgd_mat& m : hid) m = palsgd_mat{ws.take((size_t)s->K * M * F * es), (int64_t)(M * F), (int64_t)F};
-    palsgd_mat xs = *x;
-    if (x_e) xs = palsgd_mat{ws.take((size_t)s->K * M * D * es), (int64_t)(M * D), (int64_t)D};
+    Stage stage;
+    const uint32_t parts = s->precision == PALSGD_PREC_FP32 ? 3 : 1;
+    Operand ody, ox, og, ou, od, hid[3];                 // hid: dg, du, h
+    if (M) {
+        ody = input_operand(ws, stage, dy, nullptr, s->precision, s->K, M, D);
+        ox = input_operand(ws, stage, x, x_e, s->precision, s->K, M, D);
+        od = input_operand(ws, stage, w_down, nullptr, s->precision, s->K, D, F);
+        if (dx) {
+            og = input_operand(ws, stage, w_gate, nullptr, s->precision, s->K, F, D);
+            ou = input_operand(ws, stage, w_up, nullptr, s->precision, s->K, F, D);
+        }
+        for (Operand& o : hid) o = own_operand(ws, s->K, M, F, parts);
+    }
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
     if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (M) {
-        if (x_e) BLOCK_TRY(palsgd_act8_unpack(s->precision, s->K, M, D, x, x_e, &xs, stream));
-        MatArgs a{};
-        a.n_seg = 1;
-        a.A[0] = operand(dy, false); a.B[0] = operand(w_down, true);
-        a.M = (uint32_t)M; a.N = (uint32_t)F; a.Kd = (uint32_t)D; a.act = s->activation;
-        for (int i = 0; i < 3; ++i) a.out[i] = hid[i].data;
-        a.ow = hid[0].worker_stride; a.orow = hid[0].row_stride;
-        set_saved(a, s, gate, up, gate_e, up_e);
-        BLOCK_TRY(launch_mat<MAT_HIDDEN>(s->precision, s->K, a, st));
+    if (M == 0) {
+        const palsgd_mat* w[3] = {dw_gate, dw_up, dw_down};
+        ZeroArgs z{};
+        for (int i = 0; i < 3; ++i) {
+            z.p[i] = w[i]->data; z.w[i] = w[i]->worker_stride; z.r[i] = w[i]->row_stride;
+            z.rows[i] = (uint32_t)(i < 2 ? F : D); z.cols[i] = (uint32_t)(i < 2 ? D : F);
+        }
+        const dim3 grid((unsigned)(F > D ? F : D) < 1024u ? (unsigned)(F > D ? F : D) : 1024u, 3, s->K);
+        if (es == 4) zero_kernel<float><<<grid, 256, 0, st>>>(z);
+        else zero_kernel<bf16><<<grid, 256, 0, st>>>(z);
+        return launched("zero weight gradients");
     }
-    BLOCK_TRY(launch_product(s, F, D, M, &hid[0], &xs, nullptr, nullptr, true, true, dw_gate, st));
-    BLOCK_TRY(launch_product(s, F, D, M, &hid[1], &xs, nullptr, nullptr, true, true, dw_up, st));
-    BLOCK_TRY(launch_product(s, D, F, M, dy, &hid[2], nullptr, nullptr, true, true, dw_down, st));
-    if (dx && M) BLOCK_TRY(launch_product(s, M, D, F, &hid[0], w_gate, &hid[1], w_up, false, true, dx, st));
-    return PALSGD_OK;
+    Device dev{};
+    BLOCK_TRY(device_of(dev));
+    MatLaunch hidden{}, grads{};
+    BLOCK_TRY(add_problem(hidden, M, F, D, s->K, &ody, nullptr, false, &od, nullptr, true, kTileN));
+    for (int i = 0; i < 3; ++i) hidden.p[0].out[i] = out_of(hid[i]);
+    set_saved(hidden, s, gate, up, gate_e, up_e);
+    if (dx) {                                            // first: its tiles are the longest
+        BLOCK_TRY(add_problem(grads, M, D, F, s->K, &hid[0], &hid[1], false, &og, &ou, true, kTileN));
+        grads.p[0].out[0] = out_of(dx, es);
+    }
+    BLOCK_TRY(add_problem(grads, F, D, M, s->K, &hid[0], nullptr, true, &ox, nullptr, true, kTileN));
+    grads.p[grads.n_problems - 1].out[0] = out_of(dw_gate, es);
+    BLOCK_TRY(add_problem(grads, F, D, M, s->K, &hid[1], nullptr, true, &ox, nullptr, true, kTileN));
+    grads.p[grads.n_problems - 1].out[0] = out_of(dw_up, es);
+    BLOCK_TRY(add_problem(grads, D, F, M, s->K, &ody, nullptr, true, &hid[2], nullptr, true, kTileN));
+    grads.p[grads.n_problems - 1].out[0] = out_of(dw_down, es);
+    BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
+    BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s->precision, dev, st));
+    return run_mat<MAT_PLAIN>(grads, s->precision, dev, st);
+}
+
+extern "C" int palsgd_block_status(void* stream)
+{
+    Device dev{};
+    BLOCK_TRY(device_of(dev));
+    unsigned int v = 0;
+    cudaError_t e = cudaMemcpyAsync(&v, dev.gave_up, sizeof v, cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess && v) {
+        e = cudaMemsetAsync(dev.gave_up, 0, sizeof v, static_cast<cudaStream_t>(stream));
+        if (e == cudaSuccess) return palsgd_block_cuda_fail((int)cudaErrorLaunchTimeout, "a matrix kernel's wait gave up");
+    }
+    return e == cudaSuccess ? PALSGD_OK : palsgd_block_cuda_fail((int)e, "palsgd_block_status");
 }
 
 extern "C" int palsgd_qk_norm_rope_forward(const palsgd_qk_shape* s, const palsgd_heads* q, const palsgd_heads* k,
