@@ -76,7 +76,8 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
  * products of parts that reach above 2^-24 of the whole, summed in binary32.
  *
  * Workspace: call with workspace = NULL to learn *workspace_bytes (nothing is enqueued; all other arguments as in the
- * call to come); then pass at least that many bytes, 256-byte aligned.  Contents need no preparation.
+ * call to come); then pass at least that many bytes, 256-byte aligned.  Contents need no preparation.  A workspace that
+ * is too small is refused with EINVAL, and *workspace_bytes says what is needed.
  * Errors: EINVAL (NULL, K = 0 or > 64, d_model or d_ff = 0, a size >= 2^31, bad enum, negative or overlapping strides,
  * small workspace); EALIGN; ECUDA.
  */

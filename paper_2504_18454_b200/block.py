@@ -9,7 +9,8 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
-from typing import NamedTuple, Optional, Tuple, Union
+import threading
+from typing import Dict, NamedTuple, Optional, Tuple, Union
 
 import torch
 
@@ -55,18 +56,15 @@ _ready = False
 
 
 def lib() -> C.CDLL:
+    """libpalsgd.so with the argument types of palsgd_block.h (struct pointers as plain addresses)."""
     global _ready
     L = _base_lib()
     if not _ready:
-        vp, u32, u64, i32, M, H = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32, C.POINTER(Mat), C.POINTER(Heads)
-        size = C.POINTER(C.c_size_t)
-        L.palsgd_act8_pack.argtypes = L.palsgd_act8_unpack.argtypes = [i32, u32, u64, u64, M, M, M, vp]
-        L.palsgd_ffn_forward.argtypes = [C.POINTER(FfnShape)] + [M] * 9 + [vp, size, vp]
-        L.palsgd_ffn_backward.argtypes = [C.POINTER(FfnShape)] + [M] * 14 + [vp, size, vp]
-        L.palsgd_qk_norm_rope_forward.argtypes = [C.POINTER(QkShape), H, H, M, M, vp, vp, vp, H, H, vp]
-        L.palsgd_qk_norm_rope_backward.argtypes = ([C.POINTER(QkShape), H, H, H, H, M, M, vp, vp, vp, H, H, M, M]
-                                                   + [vp, size, vp])
-        L.palsgd_block_status.argtypes = [vp]
+        vp, u32, u64, i32 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32
+        L.palsgd_act8_pack.argtypes = L.palsgd_act8_unpack.argtypes = [i32, u32, u64, u64] + [vp] * 4
+        for n, args in (("ffn_forward", 13), ("ffn_backward", 18), ("qk_norm_rope_forward", 11),
+                        ("qk_norm_rope_backward", 17), ("block_status", 1)):
+            getattr(L, "palsgd_" + n).argtypes = [vp] * args
         for n in ("block_status", "act8_pack", "act8_unpack", "ffn_forward", "ffn_backward", "qk_norm_rope_forward",
                   "qk_norm_rope_backward"):
             getattr(L, "palsgd_" + n).restype = C.c_int
@@ -75,6 +73,40 @@ def lib() -> C.CDLL:
 
 
 # ---------------------------------------------------------------------------------------------- argument marshalling
+
+class _Args(threading.local):
+    """The structs of one call, packed into one block of memory a thread: palsgd_mat (3 words), palsgd_heads (4) and the
+    workspace size.  A call fills it from the start and passes addresses into it."""
+    WORDS = 128
+
+    def __init__(self):
+        self.words = (C.c_int64 * self.WORDS)()
+        self.base = C.addressof(self.words)
+        self.size = C.c_size_t(0)
+        self.size_at = C.addressof(self.size)
+
+
+_args = _Args()
+
+
+def _structs(*tensors: Optional[torch.Tensor], skip: int = 0):
+    """The addresses of the structs (palsgd_mat for up to three axes, palsgd_heads for four) of these tensors, None for
+    None.  Strides of axes of length <= 1 do not matter and become 0."""
+    values, at, base = [], [], _args.base
+    for t in tensors:
+        if t is None:
+            at.append(None)
+            continue
+        at.append(base + 8 * len(values))
+        values.append(t.data_ptr())
+        shape, stride, n = t.shape, t.stride(), t.dim()
+        if n == 2:                                        # (K, cols)
+            values += (stride[0] if shape[0] > 1 else 0, 0)
+        else:
+            values += [s if m > 1 else 0 for m, s in zip(shape, stride[:-1])]
+    _args.words[:len(values)] = values
+    return at
+
 
 def _refuse(where: str, why: str):
     raise PalsgdError(EINVAL, where, why)
@@ -86,25 +118,27 @@ def _check(rc: int, where: str) -> None:
 
 
 def _precision(t: torch.Tensor, where: str, name: str) -> int:
-    if t.dtype == torch.float32:
-        return PREC_FP32
-    if t.dtype == torch.bfloat16:
+    dt = t.dtype
+    if dt is torch.bfloat16:
         return PREC_BF16_MASTER
-    _refuse(where, f"{name} must be float32 or bfloat16, not {t.dtype}")
+    if dt is torch.float32:
+        return PREC_FP32
+    _refuse(where, f"{name} must be float32 or bfloat16, not {dt}")
 
 
 def _tensor(t, where: str, name: str, shape, dtype, device) -> torch.Tensor:
+    if (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.device == device
+            and (t.stride()[-1] == 1 or shape[-1] <= 1 or t.numel() == 0)):
+        return t
     if not isinstance(t, torch.Tensor):
         _refuse(where, f"{name} must be a tensor")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         _refuse(where, f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
     if t.dtype != dtype:
         _refuse(where, f"{name} must be {dtype}, not {t.dtype}")
     if t.device != device:
         _refuse(where, f"{name} must be on {device}, not {t.device}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
-        _refuse(where, f"the last axis of {name} must be contiguous")
-    return t
+    _refuse(where, f"the last axis of {name} must be contiguous")
 
 
 def _cuda(t, where: str, name: str, ndim: int) -> torch.device:
@@ -115,33 +149,22 @@ def _cuda(t, where: str, name: str, ndim: int) -> torch.device:
     return t.device
 
 
-def _mat(t: Optional[torch.Tensor]):
-    """(K, rows, cols) or (K, cols) -> palsgd_mat*; strides of axes of length <= 1 do not matter and become 0."""
-    if t is None:
-        return None
-    s = [st if n > 1 else 0 for n, st in zip(t.shape, t.stride())]
-    return C.byref(Mat(t.data_ptr(), s[0], s[1] if t.dim() == 3 else 0))
-
-
-def _heads(t: torch.Tensor):
-    s = [st if n > 1 else 0 for n, st in zip(t.shape, t.stride())]
-    return C.byref(Heads(t.data_ptr(), s[0], s[1], s[2]))
-
-
 class _On:
     """The device and the stream of a call: `raw` is the cudaStream_t; allocations inside the block belong to it."""
+    __slots__ = ("device", "stream", "stack", "raw")
 
     def __init__(self, device: torch.device, stream: Optional[int]):
-        self.device, self.stream = device, stream
-        self.stack = None
+        self.device, self.stream, self.stack = device, stream, None
 
     def __enter__(self) -> "_On":
-        current = torch.cuda.current_stream(self.device).cuda_stream
-        self.raw = C.c_void_p(current if self.stream is None else self.stream)
-        if torch.cuda.current_device() != self.device.index or (self.stream is not None and self.stream != current):
+        index = self.device.index
+        current = torch._C._cuda_getCurrentRawStream(index)
+        other = self.stream is not None and self.stream != current
+        self.raw = self.stream if other else current
+        if other or torch._C._cuda_getDevice() != index:
             self.stack = contextlib.ExitStack()
             self.stack.enter_context(torch.cuda.device(self.device))
-            if self.stream is not None and self.stream != current:
+            if other:
                 # stream 0 is the legacy default stream, which torch knows as its default stream
                 self.stack.enter_context(torch.cuda.stream(
                     torch.cuda.ExternalStream(self.stream, self.device) if self.stream
@@ -153,16 +176,36 @@ class _On:
             self.stack.close()
 
 
-def _workspace(call, given: Optional[torch.Tensor], device, where: str):
-    """call(workspace pointer, bytes pointer) twice: for the size, then with the memory."""
-    n = C.c_size_t(0)
-    _check(call(None, C.byref(n)), where)
-    if given is None:
-        given = torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
-    elif given.dtype != torch.uint8 or given.device != device or not given.is_contiguous():
-        _refuse(where, f"workspace must be a contiguous uint8 tensor on {device}")
-    n.value = given.numel()
-    _check(call(C.c_void_p(given.data_ptr()), C.byref(n)), where)
+_need: Dict[tuple, int] = {}              # workspace bytes by entry point and sizes, as last reported by the library
+
+
+def _workspace(call, key: tuple, given: Optional[torch.Tensor], like: torch.Tensor, where: str):
+    """call(workspace address, address of its size).  Without a workspace of the caller's, one of the size that such a
+    call last asked for is allocated; the library reports the size that it wants where that is too small (operands that
+    are not aligned need more)."""
+    size, at = _args.size, _args.size_at
+    if given is not None:
+        if given.dtype != torch.uint8 or given.device != like.device or not given.is_contiguous():
+            _refuse(where, f"workspace must be a contiguous uint8 tensor on {like.device}")
+        size.value = given.numel()
+        _check(call(given.data_ptr(), at), where)
+        return
+    have = _need.get(key)
+    if have is None:
+        size.value = 0
+        _check(call(None, at), where)
+        have = size.value
+    while True:
+        ws = torch.empty(max(have, 1), dtype=torch.uint8, device=like.device)
+        size.value = have
+        rc = call(ws.data_ptr(), at)
+        if rc != EINVAL or size.value <= have:
+            break
+        have = size.value
+    _check(rc, where)
+    if len(_need) > 4096:
+        _need.clear()
+    _need[key] = have
 
 
 def block_status(stream: Optional[int] = None) -> None:
@@ -174,27 +217,33 @@ def block_status(stream: Optional[int] = None) -> None:
 
 # ---------------------------------------------------------------------------------------------- 8-bit checkpoints
 
+def _groups(cols: int) -> int:
+    return (cols + ACT8_GROUP - 1) // ACT8_GROUP
+
+
 def _three(t: torch.Tensor) -> torch.Tensor:
     return t[None] if t.dim() == 2 else t
+
+
+def _act8(where, a: Act8, name, shape, dev):
+    _tensor(a.q, where, name + ".q", shape, torch.int8, dev)
+    _tensor(a.exponent, where, name + ".exponent", (*shape[:-1], _groups(shape[-1])), torch.uint8, dev)
 
 
 def act8_pack(x: torch.Tensor, *, out: Optional[Act8] = None, stream: Optional[int] = None) -> Act8:
     """palsgd_act8_pack: the 8-bit checkpoint of x (rows, cols) or (K, rows, cols), float32 or bfloat16."""
     where = "palsgd_act8_pack"
     dev = _cuda(x, where, "x", 2 if isinstance(x, torch.Tensor) and x.dim() == 2 else 3)
-    prec = _precision(x, where, "x")
-    _tensor(x, where, "x", x.shape, x.dtype, dev)
-    groups = (x.shape[-1] + ACT8_GROUP - 1) // ACT8_GROUP
+    prec, shape = _precision(x, where, "x"), x.shape
+    _tensor(x, where, "x", shape, x.dtype, dev)
     with _On(dev, stream) as on:
         if out is None:
-            out = Act8(torch.empty(x.shape, dtype=torch.int8, device=dev),
-                       torch.empty(*x.shape[:-1], groups, dtype=torch.uint8, device=dev), x.dtype)
+            out = Act8(torch.empty(shape, dtype=torch.int8, device=dev),
+                       torch.empty((*shape[:-1], _groups(shape[-1])), dtype=torch.uint8, device=dev), x.dtype)
         else:
-            _tensor(out.q, where, "out.q", x.shape, torch.int8, dev)
-            _tensor(out.exponent, where, "out.exponent", (*x.shape[:-1], groups), torch.uint8, dev)
+            _act8(where, out, "out", shape, dev)
         v = _three(x)
-        _check(lib().palsgd_act8_pack(prec, v.shape[0], v.shape[1], v.shape[2], _mat(v), _mat(_three(out.q)),
-                                      _mat(_three(out.exponent)), on.raw), where)
+        _check(lib().palsgd_act8_pack(prec, *v.shape, *_structs(v, _three(out.q), _three(out.exponent)), on.raw), where)
     return out
 
 
@@ -203,19 +252,18 @@ def act8_unpack(a: Act8, *, dtype: Optional[torch.dtype] = None, out: Optional[t
     """palsgd_act8_unpack: the values that a checkpoint stands for, in `dtype` (default: the type it was taken from).
     They have at most eight significant bits: bfloat16 holds them exactly."""
     where = "palsgd_act8_unpack"
-    dev = _cuda(a.q, where, "q", 2 if isinstance(a.q, torch.Tensor) and a.q.dim() == 2 else 3)
-    _tensor(a.q, where, "q", a.q.shape, torch.int8, dev)
-    _tensor(a.exponent, where, "exponent", (*a.q.shape[:-1], (a.q.shape[-1] + ACT8_GROUP - 1) // ACT8_GROUP),
-            torch.uint8, dev)
+    q = a.q
+    dev = _cuda(q, where, "q", 2 if isinstance(q, torch.Tensor) and q.dim() == 2 else 3)
+    shape = q.shape
+    _act8(where, a, "checkpoint", shape, dev)
     dtype = dtype or (out.dtype if out is not None else a.dtype)
     with _On(dev, stream) as on:
         if out is None:
-            out = torch.empty(a.q.shape, dtype=dtype, device=dev)
+            out = torch.empty(shape, dtype=dtype, device=dev)
         prec = _precision(out, where, "out")
-        _tensor(out, where, "out", a.q.shape, dtype, dev)
+        _tensor(out, where, "out", shape, dtype, dev)
         v = _three(out)
-        _check(lib().palsgd_act8_unpack(prec, v.shape[0], v.shape[1], v.shape[2], _mat(_three(a.q)),
-                                        _mat(_three(a.exponent)), _mat(v), on.raw), where)
+        _check(lib().palsgd_act8_unpack(prec, *v.shape, *_structs(_three(q), _three(a.exponent), v), on.raw), where)
     return out
 
 
@@ -229,10 +277,22 @@ def _ffn_weights(where, w_gate, w_up, w_down, K, D, dt, dev):
     return F
 
 
-def _act8_args(where, a: Act8, name, shape, dev):
-    _tensor(a.q, where, name + ".q", shape, torch.int8, dev)
-    _tensor(a.exponent, where, name + ".exponent", (*shape[:-1], (shape[-1] + ACT8_GROUP - 1) // ACT8_GROUP),
-            torch.uint8, dev)
+def _saved(where, save, saved, shape, dt, dev):
+    """gate, up and their exponents as tensors, or None."""
+    if save == SAVE_NONE:
+        return None, None, None, None
+    if not isinstance(saved, (tuple, list)) or len(saved) != 2:
+        _refuse(where, "saved must be the pair (gate, up)")
+    gate, up = saved
+    if save == SAVE_8BIT:
+        if not (isinstance(gate, Act8) and isinstance(up, Act8)):
+            _refuse(where, "gate and up must both be Act8")
+        _act8(where, gate, "gate", shape, dev)
+        _act8(where, up, "up", shape, dev)
+        return gate.q, up.q, gate.exponent, up.exponent
+    _tensor(gate, where, "gate", shape, dt, dev)
+    _tensor(up, where, "up", shape, dt, dev)
+    return gate, up, None, None
 
 
 def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
@@ -251,41 +311,21 @@ def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_dow
     K, M, D = x.shape
     _tensor(x, where, "x", x.shape, dt, dev)
     F = _ffn_weights(where, w_gate, w_up, w_down, K, D, dt, dev)
-    shape = FfnShape(K, prec, int(activation), int(save), M, D, F)
+    shape = FfnShape(K, prec, activation, save, M, D, F)
     with _On(dev, stream) as on:
-        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else _tensor(out, where, "out", x.shape, dt, dev)
+        y = torch.empty((K, M, D), dtype=dt, device=dev) if out is None else _tensor(out, where, "out", (K, M, D), dt, dev)
         if save == SAVE_NONE:
             saved = None
         elif saved is None:
             if save == SAVE_8BIT:
-                G = (F + ACT8_GROUP - 1) // ACT8_GROUP
-                saved = tuple(Act8(torch.empty(K, M, F, dtype=torch.int8, device=dev),
-                                   torch.empty(K, M, G, dtype=torch.uint8, device=dev), dt) for _ in range(2))
+                saved = tuple(Act8(torch.empty((K, M, F), dtype=torch.int8, device=dev),
+                                   torch.empty((K, M, _groups(F)), dtype=torch.uint8, device=dev), dt) for _ in range(2))
             else:
-                saved = tuple(torch.empty(K, M, F, dtype=dt, device=dev) for _ in range(2))
-        mats = _saved_mats(where, save, saved, (K, M, F), dt, dev)
-        call = lambda ws, n: lib().palsgd_ffn_forward(
-            C.byref(shape), _mat(x), _mat(w_gate), _mat(w_up), _mat(w_down), _mat(y), *mats, ws, n, on.raw)
-        _workspace(call, workspace, dev, where)
+                saved = tuple(torch.empty((K, M, F), dtype=dt, device=dev) for _ in range(2))
+        at = _structs(x, w_gate, w_up, w_down, y, *_saved(where, save, saved, (K, M, F), dt, dev))
+        entry, s = lib().palsgd_ffn_forward, C.addressof(shape)
+        _workspace(lambda ws, n: entry(s, *at, ws, n, on.raw), (where, K, M, D, F, prec), workspace, x, where)
     return y, saved
-
-
-def _saved_mats(where, save, saved, shape, dt, dev):
-    """gate, up, gate_e, up_e as palsgd_mat*"""
-    if save == SAVE_NONE:
-        return None, None, None, None
-    if not isinstance(saved, (tuple, list)) or len(saved) != 2:
-        _refuse(where, "saved must be the pair (gate, up)")
-    gate, up = saved
-    if save == SAVE_8BIT:
-        if not (isinstance(gate, Act8) and isinstance(up, Act8)):
-            _refuse(where, "gate and up must both be Act8")
-        _act8_args(where, gate, "gate", shape, dev)
-        _act8_args(where, up, "up", shape, dev)
-        return _mat(gate.q), _mat(up.q), _mat(gate.exponent), _mat(up.exponent)
-    _tensor(gate, where, "gate", shape, dt, dev)
-    _tensor(up, where, "up", shape, dt, dev)
-    return _mat(gate), _mat(up), None, None
 
 
 def ffn_backward(dy: torch.Tensor, x: Saved, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
@@ -307,14 +347,13 @@ def ffn_backward(dy: torch.Tensor, x: Saved, w_gate: torch.Tensor, w_up: torch.T
         _refuse(where, "saved must be the pair (gate, up)")
     save = SAVE_8BIT if isinstance(saved[0], Act8) else SAVE_FULL
     if isinstance(x, Act8):
-        _act8_args(where, x, "x", (K, M, D), dev)
+        _act8(where, x, "x", (K, M, D), dev)
         if save != SAVE_8BIT:
             _refuse(where, "x may be an Act8 only where gate and up are")
-        mx, mxe = _mat(x.q), _mat(x.exponent)
+        xs = (x.q, x.exponent)
     else:
-        _tensor(x, where, "x", (K, M, D), dt, dev)
-        mx, mxe = _mat(x), None
-    shape = FfnShape(K, prec, int(activation), save, M, D, F)
+        xs = (_tensor(x, where, "x", (K, M, D), dt, dev), None)
+    shape = FfnShape(K, prec, activation, save, M, D, F)
     with _On(dev, stream) as on:
         want = ((K, M, D), (K, F, D), (K, F, D), (K, D, F))
         outs = list(out) if out is not None else [None] * 4
@@ -327,11 +366,10 @@ def ffn_backward(dy: torch.Tensor, x: Saved, w_gate: torch.Tensor, w_up: torch.T
                 outs[i] = torch.empty(want[i], dtype=dt, device=dev)
             else:
                 _tensor(outs[i], where, name, want[i], dt, dev)
-        mats = _saved_mats(where, save, saved, (K, M, F), dt, dev)
-        call = lambda ws, n: lib().palsgd_ffn_backward(
-            C.byref(shape), _mat(dy), mx, mxe, _mat(w_gate), _mat(w_up), _mat(w_down), *mats,
-            *(_mat(t) for t in outs), ws, n, on.raw)
-        _workspace(call, workspace, dev, where)
+        at = _structs(dy, *xs, w_gate, w_up, w_down, *_saved(where, save, saved, (K, M, F), dt, dev), *outs)
+        entry, s = lib().palsgd_ffn_backward, C.addressof(shape)
+        _workspace(lambda ws, n: entry(s, *at, ws, n, on.raw), (where, K, M, D, F, prec, need_dx, len(at) - at.count(None)),
+                   workspace, dy, where)
     return tuple(outs)
 
 
@@ -352,10 +390,9 @@ def _qk(where, q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
         if not _tensor(t, where, name, cos.shape, torch.float32, dev).is_contiguous():
             _refuse(where, f"{name} must be contiguous")
     _tensor(positions, where, "positions", (K, M), torch.int32, dev)
-    shape = QkShape(K, prec, M, HQ, HK, DH, 2 * cos.shape[1], int(bool(interleaved)), 0, cos.shape[0],
-                    positions.stride(0) if K > 1 else 0, float(eps))
-    vp = C.c_void_p
-    return dev, shape, (vp(cos.data_ptr()), vp(sin.data_ptr()), vp(positions.data_ptr()))
+    shape = QkShape(K, prec, M, HQ, HK, DH, 2 * cos.shape[1], 1 if interleaved else 0, 0, cos.shape[0],
+                    positions.stride(0) if K > 1 else 0, eps)
+    return dev, shape, (cos.data_ptr(), sin.data_ptr(), positions.data_ptr())
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, w_q: torch.Tensor, w_k: torch.Tensor, cos: torch.Tensor,
@@ -368,12 +405,12 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, w_q: torch.Tensor, w_k: torch
     dev, shape, tables = _qk(where, q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
     with _On(dev, stream) as on:
         if out is None:
-            out = tuple(torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k))
+            out = (torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=q.dtype, device=dev))
         else:
             _tensor(out[0], where, "q_out", q.shape, q.dtype, dev)
             _tensor(out[1], where, "k_out", k.shape, q.dtype, dev)
-        _check(lib().palsgd_qk_norm_rope_forward(C.byref(shape), _heads(q), _heads(k), _mat(w_q), _mat(w_k), *tables,
-                                                 _heads(out[0]), _heads(out[1]), on.raw), where)
+        aq, ak, awq, awk, oq, ok = _structs(q, k, w_q, w_k, *out)
+        _check(lib().palsgd_qk_norm_rope_forward(C.addressof(shape), aq, ak, awq, awk, *tables, oq, ok, on.raw), where)
     return tuple(out)
 
 
@@ -397,8 +434,8 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.T
                 outs[i] = torch.empty(like.shape, dtype=q.dtype, device=dev)
             else:
                 _tensor(outs[i], where, name, like.shape, q.dtype, dev)
-        call = lambda ws, n: lib().palsgd_qk_norm_rope_backward(
-            C.byref(shape), _heads(dq_out), _heads(dk_out), _heads(q), _heads(k), _mat(w_q), _mat(w_k), *tables,
-            _heads(outs[0]), _heads(outs[1]), _mat(outs[2]), _mat(outs[3]), ws, n, on.raw)
-        _workspace(call, workspace, dev, where)
+        at = _structs(dq_out, dk_out, q, k, w_q, w_k, *outs)
+        entry, s = lib().palsgd_qk_norm_rope_backward, C.addressof(shape)
+        _workspace(lambda ws, n: entry(s, *at[:6], *tables, *at[6:], ws, n, on.raw),
+                   (where, *q.shape, k.shape[2]), workspace, q, where)
     return tuple(outs)

@@ -345,19 +345,28 @@ bool heads_wide(const void* p, int64_t w, int64_t t, int64_t h, size_t es)
     return aligned(p, 16) && (w * es) % 16 == 0 && (t * es) % 16 == 0 && (h * es) % 16 == 0;
 }
 
-struct QkPlan { QkArgs a; int V, NS; unsigned ctas; };
+struct QkPlan { QkArgs a; int V, NS; };
 
-QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos, bool back)
+QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos)
 {
     QkPlan p{};
     QkArgs& a = p.a;
     a.cos_t = cos_t; a.sin_t = sin_t; a.pos = pos; a.pos_w = s->pos_worker_stride;
     a.tokens = s->tokens; a.table_rows = s->table_rows; a.head_dim = s->head_dim; a.rot = s->rotary_dim;
     a.interleaved = s->interleaved; a.eps = (float)s->eps;
+    a.table_wide = s->rotary_dim % 8 == 0 && aligned(cos_t, 16) && aligned(sin_t, 16);
     a.side[0].heads = s->heads_q; a.side[1].heads = s->heads_k;
-    const uint64_t per_side = (uint64_t)s->K * ((s->heads_q ? 1 : 0) + (s->heads_k ? 1 : 0));
-    const uint64_t want = ceil_div(s->tokens, 8), most = ceil_div((uint64_t)sm_count() * (back ? 3 : 6), per_side ? per_side : 1);
-    p.ctas = (unsigned)(want < most ? (want ? want : 1) : most);
+    // two CTAs per SM, shared by the workers, and by q and k as their heads are
+    const uint32_t heads[2] = {s->heads_q, s->heads_k}, all = heads[0] + heads[1];
+    const uint64_t slots = 2ull * sm_count() / s->K;
+    uint64_t n[2];
+    for (int i = 0; i < 2; ++i) {
+        n[i] = all ? slots * heads[i] / all : 0;
+        const uint64_t most = ceil_div(s->tokens, 8);
+        if (n[i] > most) n[i] = most;
+        if (heads[i] && n[i] == 0) n[i] = 1;
+        a.ctas[i] = (uint32_t)n[i];
+    }
     return p;
 }
 
@@ -384,7 +393,7 @@ void finish_qk(QkPlan& p, const palsgd_qk_shape* s, bool back)
 template <typename T, bool BACK>
 int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
 {
-    const dim3 grid(p.ctas, 2, s->K);
+    const dim3 grid(p.a.ctas[0] + p.a.ctas[1], s->K);
     const size_t sm = BACK ? 8 * (size_t)s->head_dim * sizeof(float) : 0;
     constexpr int W = 16 / (int)sizeof(T);
     if (p.V == W && p.NS == 1) qk_kernel<T, W, 1, BACK><<<grid, 256, sm, st>>>(p.a);
@@ -443,7 +452,7 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
         oh = own_operand(ws, s->K, M, F, parts);
     }
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
-    if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
+    if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
     if (M == 0) return PALSGD_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Device dev{};
@@ -497,7 +506,7 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
         for (Operand& o : hid) o = own_operand(ws, s->K, M, F, parts);
     }
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
-    if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
+    if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M == 0) {
         const palsgd_mat* w[3] = {dw_gate, dw_up, dw_down};
@@ -561,7 +570,7 @@ extern "C" int palsgd_qk_norm_rope_forward(const palsgd_qk_shape* s, const palsg
         if (heads[i]) BLOCK_TRY(check_mat(w[i], s->K, 1, s->head_dim, elem(s->precision), false));
     }
     if (s->tokens == 0 || (heads[0] | heads[1]) == 0) return PALSGD_OK;
-    QkPlan p = plan_qk(s, cos_table, sin_table, positions, false);
+    QkPlan p = plan_qk(s, cos_table, sin_table, positions);
     for (int i = 0; i < 2; ++i) {
         if (!heads[i]) continue;
         HeadsArg& h = p.a.side[i];
@@ -594,13 +603,13 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
         BLOCK_TRY(check_mat(dw[i], s->K, 1, s->head_dim, elem(s->precision), true));
     }
     BLOCK_TRY(check_workspace(workspace, workspace_bytes));
-    QkPlan p = plan_qk(s, cos_table, sin_table, positions, true);
+    QkPlan p = plan_qk(s, cos_table, sin_table, positions);
     Arena ws{static_cast<char*>(workspace), 0};
     float* part[2] = {nullptr, nullptr};
     for (int i = 0; i < 2; ++i)
-        if (heads[i]) part[i] = static_cast<float*>(ws.take((size_t)s->K * p.ctas * s->head_dim * sizeof(float)));
+        if (heads[i]) part[i] = static_cast<float*>(ws.take((size_t)s->K * p.a.ctas[i] * s->head_dim * sizeof(float)));
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
-    if (*workspace_bytes < ws.used) return PALSGD_EINVAL;
+    if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
     if ((heads[0] | heads[1]) == 0) return PALSGD_OK;
     QkSumArgs sum{};
     for (int i = 0; i < 2; ++i) {
@@ -615,7 +624,7 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
     }
     finish_qk(p, s, true);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    sum.parts = s->tokens ? p.ctas : 0;
+    for (int i = 0; i < 2; ++i) sum.parts[i] = s->tokens ? p.a.ctas[i] : 0;
     sum.head_dim = s->head_dim;
     const dim3 grid((unsigned)ceil_div(s->head_dim, 32), 2, s->K);
     if (s->precision == PALSGD_PREC_FP32) {

@@ -62,6 +62,33 @@ template <> struct Vec<bf16, 8> {
     }
 };
 
+// V values as they lie in memory (16 bytes, or one value), to be kept in registers until they are needed.
+template <typename T, int V> struct Raw { uint4 r; };
+template <typename T> struct Raw<T, 1> { T r; };
+template <typename T, int V> __device__ __forceinline__ void raw_zero(Raw<T, V>& o)
+{
+    if constexpr (V == 1) o.r = from_f<T>(0.0f);
+    else o.r = make_uint4(0, 0, 0, 0);
+}
+template <typename T, int V> __device__ __forceinline__ void raw_load(Raw<T, V>& o, const T* p)
+{
+    if constexpr (V == 1) o.r = *p;
+    else o.r = __ldg(reinterpret_cast<const uint4*>(p));
+}
+template <typename T, int V> __device__ __forceinline__ void raw_get(const Raw<T, V>& o, float* v)
+{
+    if constexpr (V == 1) {
+        v[0] = to_f(o.r);
+    } else {
+        const uint32_t w[4] = {o.r.x, o.r.y, o.r.z, o.r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i]);
+            else { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+        }
+    }
+}
+
 // ---- 8-bit checkpoints: the step 2^(E-127) of a group from the largest magnitude in it (as bits: NaN > Inf > finite).
 // Adding 2^16 to the bits carries into the exponent exactly when the mantissa is >= 1.9921875 = 127.5/64, the values
 // that would round to 128 steps; ties (127.5) go to the even 128 and are among them.  A carry out of the largest finite

@@ -82,11 +82,12 @@ struct HeadsArg {
     const void* w;                // norm weights, one row per worker
     int64_t xw, xt, xh, dw, dt, dh, ow, ot, oh, ww;
     uint32_t heads;
-    float*   part;                // backward: [K][gridDim.x][head_dim] partial sums of the weight gradient
+    float*   part;                // backward: [K][CTAs of this side][head_dim] partial sums of the weight gradient
 };
 
 struct QkArgs {
-    HeadsArg side[2];             // q, k (blockIdx.y)
+    HeadsArg side[2];             // q, k
+    uint32_t ctas[2];             // of one worker, by their shares of the heads: q's first
     const float* cos_t;
     const float* sin_t;
     const int32_t* pos;
@@ -95,24 +96,43 @@ struct QkArgs {
     uint32_t head_dim, rot, pair_slots, slots;   // slots: two vectors of V values each; the first pair_slots hold pairs
     uint32_t lanes;               // lanes of a warp that share one head: a power of two, NS * lanes >= slots
     int      interleaved;
+    int      table_wide;          // the rows of the angle tables start on 16-byte boundaries
     float    eps;
 };
 
-// One warp takes a token and walks its heads, 32/lanes of them at a time; a lane keeps the two vectors of each of its
-// NS slots in registers.  A slot holds both halves of its rotation pairs, so the rotation needs no exchange: for split
-// halves vectors s and s + rot/(2V), for interleaved pairs two neighbouring vectors (V > 1: the pairs lie inside a
-// vector; V = 1: the slot is the pair).  Cosines and sines are read once per token and serve all its heads; the norm
-// weights stay in registers for the whole grid-stride walk.
+// What a lane holds of one head under way: the two vectors of each of its NS slots, as they lie in memory.
 template <typename T, int V, int NS, bool BACK>
-__global__ void __launch_bounds__(256) qk_kernel(const __grid_constant__ QkArgs a)
+struct QkItem {
+    Raw<T, V> x[NS][2], d[BACK ? NS : 1][2];
+    int64_t out;
+    int32_t pos;
+    bool live;
+};
+
+template <bool SECOND, typename A, typename B>
+__device__ __forceinline__ auto& either(A& a, B& b)
 {
-    const HeadsArg& h = a.side[blockIdx.y];
-    const uint32_t k = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (h.heads == 0) return;
+    if constexpr (SECOND) return b;
+    else return a;
+}
+
+// A warp takes a few tokens at a time and walks their heads; `lanes` lanes share a head, and a slot of a lane holds both
+// halves of its rotation pairs, so the rotation needs no exchange: for split halves vectors s and s + rot/(2V), for
+// interleaved pairs two neighbouring vectors (V > 1: the pairs lie inside a vector; V = 1: the slot is the pair).  The
+// only exchanges are the sums over a head.  The next items are under way while one is worked on: two of them forward, one
+// backward (it is twice the size).  Angles are read when their item is due -- all heads of a token read the same ones, so
+// they come from L1 -- and the norm weights stay in registers throughout.
+template <typename T, int V, int NS, bool BACK>
+__global__ void __launch_bounds__(256, NS == 1 ? 2 : 1) qk_kernel(const __grid_constant__ QkArgs a)
+{
+    const uint32_t side = blockIdx.x >= a.ctas[0], cta = blockIdx.x - (side ? a.ctas[0] : 0), ctas = a.ctas[side];
+    const HeadsArg& h = a.side[side];
+    const uint32_t k = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t sub = lane & (a.lanes - 1), group = lane / a.lanes, groups = 32 / a.lanes;
     const uint32_t n_vec = a.head_dim / V;
     uint32_t at[NS][2];           // first element of each vector, or ~0
-    float w[NS][2][V], acc[NS][2][V];
+    T w[NS][2][V];
+    float acc[NS][2][V];
     const T* wp = static_cast<const T*>(h.w) + (int64_t)k * h.ww;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -126,123 +146,155 @@ __global__ void __launch_bounds__(256) qk_kernel(const __grid_constant__ QkArgs 
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) { w[s][p][j] = 0.0f; acc[s][p][j] = 0.0f; }
-            if (at[s][p] != ~0u) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) w[s][p][j] = to_f(wp[at[s][p] + j]);
+            for (int j = 0; j < V; ++j) {
+                w[s][p][j] = at[s][p] != ~0u ? wp[at[s][p] + j] : from_f<T>(0.0f);
+                acc[s][p][j] = 0.0f;
             }
         }
     }
     const float inv_n = 1.0f / (float)a.head_dim;
     const uint32_t half = a.rot / 2;
-    for (uint64_t t = (uint64_t)blockIdx.x * 8 + warp; t < a.tokens; t += (uint64_t)gridDim.x * 8) {
-        // the angle of element j of a slot: split halves (V of them), or pairs inside the two vectors (V/2 each)
-        float c[NS][V], s_[NS][V], bad = 0.0f;
-        if (a.rot) {
-            const int32_t pos = a.pos[(int64_t)k * a.pos_w + (int64_t)t];
-            const bool ok = pos >= 0 && (uint64_t)pos < a.table_rows;
-            const float* ct = a.cos_t + (ok ? (uint64_t)pos * half : 0);
-            const float* st = a.sin_t + (ok ? (uint64_t)pos * half : 0);
-            bad = ok ? 0.0f : __uint_as_float(0x7FFFFFFFu);
+    // the warp's groups: `abreast` heads of each of `tokens` tokens
+    uint32_t abreast = 1;
+    while (abreast < groups && abreast < h.heads) abreast *= 2;
+    const uint32_t tokens = groups / abreast, first = group % abreast, rounds = (h.heads + abreast - 1) / abreast;
+    const uint64_t step = (uint64_t)ctas * 8 * tokens;
+
+    uint64_t t = ((uint64_t)cta * 8 + warp) * tokens;                  // of the item to be fetched
+    uint32_t round = 0;
+    using Item = QkItem<T, V, NS, BACK>;
+    constexpr int kAhead = BACK ? 1 : 2;
+    auto fetch = [&](Item& it) {
+        const uint64_t tk = t + group / abreast;
+        const uint32_t hd = round * abreast + first;
+        it.live = tk < a.tokens && hd < h.heads;
+        it.pos = a.rot && it.live ? __ldg(a.pos + (int64_t)k * a.pos_w + (int64_t)tk) : 0;
+        const int64_t hx = (int64_t)k * h.xw + (int64_t)tk * h.xt + (int64_t)hd * h.xh;
+        const int64_t hg = (int64_t)k * h.dw + (int64_t)tk * h.dt + (int64_t)hd * h.dh;
+        it.out = (int64_t)k * h.ow + (int64_t)tk * h.ot + (int64_t)hd * h.oh;
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const bool on = it.live && at[s][p] != ~0u;
+                raw_zero(it.x[s][p]);
+                if (on) raw_load(it.x[s][p], static_cast<const T*>(h.x) + hx + at[s][p]);
+                if constexpr (BACK) {
+                    raw_zero(it.d[s][p]);
+                    if (on) raw_load(it.d[s][p], static_cast<const T*>(h.d) + hg + at[s][p]);
+                }
+            }
+        if (++round == rounds) { round = 0; t += step; }
+    };
+    auto work = [&](const Item& it) {
+        const bool ok = !a.rot || (it.pos >= 0 && (uint64_t)it.pos < a.table_rows);
+        const float* ct = a.cos_t + (ok ? (uint64_t)it.pos * half : 0);
+        const float* st = a.sin_t + (ok ? (uint64_t)it.pos * half : 0);
+        float c[NS][V], sn[NS][V];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const uint32_t i = (s * a.lanes + sub) * V;                       // first pair of the slot
+            if (V > 1 && a.table_wide && i + V <= half && ok && it.live) {
+                if constexpr (V > 1) {
+#pragma unroll
+                    for (int j = 0; j < V; j += 4) { Vec<float, 4>::load(ct + i + j, c[s] + j); Vec<float, 4>::load(st + i + j, sn[s] + j); }
+                }
+            } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const uint32_t i = (s * a.lanes + sub) * V + j;      // pair index, in either order of the pairs
-                    const bool on = i < half;
-                    c[s][j] = on && ok ? __ldg(ct + i) : 1.0f;
-                    s_[s][j] = on && ok ? __ldg(st + i) : 0.0f;
+                    const bool on = i + j < half && ok && it.live;
+                    c[s][j] = on ? __ldg(ct + i + j) : 1.0f;
+                    sn[s][j] = on ? __ldg(st + i + j) : 0.0f;
                 }
             }
         }
-        for (uint32_t hd = group; hd < (h.heads + groups - 1) / groups * groups; hd += groups) {
-            const bool live = hd < h.heads;
-            const int64_t hx = (int64_t)k * h.xw + (int64_t)t * h.xt + (int64_t)hd * h.xh;
-            float x[NS][2][V], d[NS][2][V];
-            float sq = 0.0f;
+        float x[NS][2][V], d[BACK ? NS : 1][2][V];
+        float sq = 0.0f;
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const bool on = live && at[s][p] != ~0u;
+            for (int p = 0; p < 2; ++p) {
+                raw_get(it.x[s][p], x[s][p]);
+                if constexpr (BACK) raw_get(it.d[s][p], d[s][p]);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) { x[s][p][j] = 0.0f; d[s][p][j] = 0.0f; }
-                    if (on) Vec<T, V>::load(static_cast<const T*>(h.x) + hx + at[s][p], x[s][p]);
-                    if (BACK && on)
-                        Vec<T, V>::load(static_cast<const T*>(h.d) + (int64_t)k * h.dw + (int64_t)t * h.dt + (int64_t)hd * h.dh + at[s][p], d[s][p]);
-                }
+                for (int j = 0; j < V; ++j) sq = fmaf(x[s][p][j], x[s][p][j], sq);
+            }
+        for (uint32_t m = a.lanes / 2; m; m >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, m);
+        const float r = 1.0f / sqrtf(fmaf(sq, inv_n, a.eps)) + (ok ? 0.0f : __uint_as_float(0x7FFFFFFFu));   // outside the table: NaN
+        auto& y = either<BACK>(x, d);
+        if constexpr (!BACK) {
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
                 for (int p = 0; p < 2; ++p)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) sq = fmaf(x[s][p][j], x[s][p][j], sq);
-            for (uint32_t m = a.lanes / 2; m; m >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, m);
-            const float r = 1.0f / sqrtf(fmaf(sq, inv_n, a.eps)) + bad;      // a position outside the table: NaN
-            float (&y)[NS][2][V] = BACK ? d : x;
-            if constexpr (!BACK) {
+                    for (int j = 0; j < V; ++j) x[s][p][j] = x[s][p][j] * r * to_f(w[s][p][j]);
+        }
+        // forward: (a, b) -> (a c - b s, b c + a s); backward: by the opposite angle
 #pragma unroll
-                for (int s = 0; s < NS; ++s)
+        for (int s = 0; s < NS; ++s) {
+            if (V == 1 || !a.interleaved) {
+                if (s * a.lanes + sub < a.pair_slots) {
 #pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int j = 0; j < V; ++j) x[s][p][j] = x[s][p][j] * r * w[s][p][j];
-            }
-            if (a.rot) {
-                // forward: (a, b) -> (a c - b s, b c + a s); backward: by the opposite angle
-#pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const uint32_t slot = s * a.lanes + sub;
-                    if (V == 1 || !a.interleaved) {
-                        if (slot < a.pair_slots) {
-#pragma unroll
-                            for (int j = 0; j < V; ++j) {
-                                const float sn = BACK ? -s_[s][j] : s_[s][j], cs = c[s][j];
-                                const float p0 = y[s][0][j], p1 = y[s][1][j];
-                                y[s][0][j] = fmaf(p0, cs, -(p1 * sn));
-                                y[s][1][j] = fmaf(p1, cs, p0 * sn);
-                            }
-                        }
-                    } else if constexpr (V > 1) {
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {                    // pair j of the slot: element 2j of its 2V values
-                            const float sn = BACK ? -s_[s][j] : s_[s][j], cs = c[s][j];
-                            const float p0 = y[s][2 * j / V][2 * j % V], p1 = y[s][2 * j / V][2 * j % V + 1];
-                            y[s][2 * j / V][2 * j % V] = fmaf(p0, cs, -(p1 * sn));
-                            y[s][2 * j / V][2 * j % V + 1] = fmaf(p1, cs, p0 * sn);
-                        }
+                    for (int j = 0; j < V; ++j) {
+                        const float si = BACK ? -sn[s][j] : sn[s][j], co = c[s][j];
+                        const float p0 = y[s][0][j], p1 = y[s][1][j];
+                        y[s][0][j] = fmaf(p0, co, -(p1 * si));
+                        y[s][1][j] = fmaf(p1, co, p0 * si);
                     }
                 }
+            } else if constexpr (V > 1) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {                                // pair j of the slot: element 2j of its 2V values
+                    const float si = BACK ? -sn[s][j] : sn[s][j], co = c[s][j];
+                    const float p0 = y[s][2 * j / V][2 * j % V], p1 = y[s][2 * j / V][2 * j % V + 1];
+                    y[s][2 * j / V][2 * j % V] = fmaf(p0, co, -(p1 * si));
+                    y[s][2 * j / V][2 * j % V + 1] = fmaf(p1, co, p0 * si);
+                }
             }
-            if constexpr (BACK) {
-                float dot = 0.0f;
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            x[s][p][j] *= r;                              // xh
-                            acc[s][p][j] = fmaf(d[s][p][j], x[s][p][j], acc[s][p][j]);
-                            d[s][p][j] *= w[s][p][j];
-                            dot = fmaf(d[s][p][j], x[s][p][j], dot);
-                        }
-                for (uint32_t m = a.lanes / 2; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
-                dot *= inv_n;
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int j = 0; j < V; ++j) d[s][p][j] = r * fmaf(-x[s][p][j], dot, d[s][p][j]);
-            }
-            const int64_t ho = (int64_t)k * h.ow + (int64_t)t * h.ot + (int64_t)hd * h.oh;
+        }
+        if constexpr (BACK) {
+            float dot = 0.0f;
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
                 for (int p = 0; p < 2; ++p)
-                    if (live && at[s][p] != ~0u) Vec<T, V>::store(static_cast<T*>(h.out) + ho + at[s][p], y[s][p]);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        x[s][p][j] *= r;                                      // xh
+                        acc[s][p][j] = fmaf(d[s][p][j], x[s][p][j], acc[s][p][j]);
+                        d[s][p][j] *= to_f(w[s][p][j]);
+                        dot = fmaf(d[s][p][j], x[s][p][j], dot);
+                    }
+            for (uint32_t m = a.lanes / 2; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
+            dot *= inv_n;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) d[s][p][j] = r * fmaf(-x[s][p][j], dot, d[s][p][j]);
         }
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+                if (it.live && at[s][p] != ~0u) Vec<T, V>::store(static_cast<T*>(h.out) + it.out + at[s][p], y[s][p]);
+    };
+
+    // items of this warp: (token groups) * rounds; all lanes walk the same ones
+    const uint64_t mine = t < a.tokens ? ((a.tokens - 1 - t) / step + 1) * rounds : 0;
+    Item ahead[kAhead];
+    uint64_t fetched = 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (fetched < mine) { fetch(ahead[i]); ++fetched; }
+    for (uint64_t i = 0; i < mine; ++i) {
+        const Item cur = ahead[0];
+#pragma unroll
+        for (int j = 0; j + 1 < kAhead; ++j) ahead[j] = ahead[j + 1];
+        if (fetched < mine) { fetch(ahead[kAhead - 1]); ++fetched; }
+        work(cur);
     }
     if constexpr (BACK) {
         // the CTA's sum in a fixed order: groups of a warp by a butterfly, then the eight warps one after another
@@ -258,7 +310,7 @@ __global__ void __launch_bounds__(256) qk_kernel(const __grid_constant__ QkArgs 
                     if (group == 0 && at[s][p] != ~0u) sum[warp * a.head_dim + at[s][p] + j] = v;
                 }
         __syncthreads();
-        float* const part = h.part + ((uint64_t)k * gridDim.x + blockIdx.x) * a.head_dim;
+        float* const part = h.part + ((uint64_t)k * ctas + cta) * a.head_dim;
         for (uint32_t i = threadIdx.x; i < a.head_dim; i += 256) {
             float v = 0.0f;
 #pragma unroll
@@ -272,7 +324,7 @@ struct QkSumArgs {
     const float* part[2];
     void*    dw[2];
     int64_t  dww[2];
-    uint32_t parts, head_dim;
+    uint32_t parts[2], head_dim;
     uint32_t heads[2];
 };
 
@@ -284,10 +336,11 @@ __global__ void __launch_bounds__(256) qk_sum_kernel(const __grid_constant__ QkS
     const uint32_t side = blockIdx.y, k = blockIdx.z;
     if (a.heads[side] == 0) return;
     const uint32_t i = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
-    const float* p = a.part[side] + (uint64_t)k * a.parts * a.head_dim;
+    const uint32_t parts = a.parts[side];
+    const float* p = a.part[side] + (uint64_t)k * parts * a.head_dim;
     float v = 0.0f;
     if (i < a.head_dim)
-        for (uint32_t b = r; b < a.parts; b += 8) v += p[(uint64_t)b * a.head_dim + i];
+        for (uint32_t b = r; b < parts; b += 8) v += p[(uint64_t)b * a.head_dim + i];
     run[r][threadIdx.x & 31] = v;
     __syncthreads();
     if (r == 0 && i < a.head_dim) {
