@@ -345,7 +345,24 @@ bool heads_wide(const void* p, int64_t w, int64_t t, int64_t h, size_t es)
     return aligned(p, 16) && (w * es) % 16 == 0 && (t * es) % 16 == 0 && (h * es) % 16 == 0;
 }
 
+constexpr int kQkCtasPerSm = 4;                          // resident at the least, of the kernels that the usual sizes take
+
 struct QkPlan { QkArgs a; int V, NS; };
+
+// CTAs by the workers, and by q and k as their heads are.  Needs nothing of the operands: the workspace goes by it.
+void share_out(QkArgs& a, const palsgd_qk_shape* s)
+{
+    const uint32_t heads[2] = {s->heads_q, s->heads_k}, all = heads[0] + heads[1];
+    const uint64_t slots = (uint64_t)kQkCtasPerSm * sm_count() / s->K;
+    for (int i = 0; i < 2; ++i) {
+        uint64_t n = all ? slots * heads[i] / all : 0;
+        const uint64_t most = ceil_div(s->tokens, kQkThreads / 32);
+        if (n > most) n = most;
+        if (heads[i] && n == 0) n = 1;
+        a.ctas[i] = (uint32_t)n;
+    }
+}
+
 
 QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos)
 {
@@ -353,20 +370,10 @@ QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t,
     QkArgs& a = p.a;
     a.cos_t = cos_t; a.sin_t = sin_t; a.pos = pos; a.pos_w = s->pos_worker_stride;
     a.tokens = s->tokens; a.table_rows = s->table_rows; a.head_dim = s->head_dim; a.rot = s->rotary_dim;
-    a.interleaved = s->interleaved; a.eps = (float)s->eps;
+    a.eps = (float)s->eps;
     a.table_wide = s->rotary_dim % 8 == 0 && aligned(cos_t, 16) && aligned(sin_t, 16);
     a.side[0].heads = s->heads_q; a.side[1].heads = s->heads_k;
-    // two CTAs per SM, shared by the workers, and by q and k as their heads are
-    const uint32_t heads[2] = {s->heads_q, s->heads_k}, all = heads[0] + heads[1];
-    const uint64_t slots = 2ull * sm_count() / s->K;
-    uint64_t n[2];
-    for (int i = 0; i < 2; ++i) {
-        n[i] = all ? slots * heads[i] / all : 0;
-        const uint64_t most = ceil_div(s->tokens, 8);
-        if (n[i] > most) n[i] = most;
-        if (heads[i] && n[i] == 0) n[i] = 1;
-        a.ctas[i] = (uint32_t)n[i];
-    }
+    share_out(a, s);
     return p;
 }
 
@@ -388,21 +395,37 @@ void finish_qk(QkPlan& p, const palsgd_qk_shape* s, bool back)
     while (a.lanes < 32 && a.lanes < a.slots) a.lanes *= 2;
     p.NS = 1;
     while ((uint32_t)p.NS * a.lanes < a.slots) p.NS *= 2;
+    // Heads abreast: the most that divide the heads evenly and leave each group four in a row, over which it forms the
+    // token's products once; more where there are too few tokens to keep every warp busy.
+    const uint32_t groups = 32 / a.lanes;
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t heads = a.side[i].heads;
+        uint32_t n = 1;
+        while (n < groups && n < heads &&
+               ((heads % (2 * n) == 0 && heads / (2 * n) >= 4) || s->tokens * s->K * n < (uint64_t)(kQkCtasPerSm * (kQkThreads / 32)) * sm_count() * groups))
+            n *= 2;
+        a.abreast[i] = n;
+    }
 }
 
-template <typename T, bool BACK>
+template <typename T, bool BACK, bool INTER>
 int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
 {
     const dim3 grid(p.a.ctas[0] + p.a.ctas[1], s->K);
-    const size_t sm = BACK ? 8 * (size_t)s->head_dim * sizeof(float) : 0;
+    const size_t sm = BACK ? (kQkThreads / 32) * (size_t)s->head_dim * sizeof(float) : 0;
     constexpr int W = 16 / (int)sizeof(T);
-    if (p.V == W && p.NS == 1) qk_kernel<T, W, 1, BACK><<<grid, 256, sm, st>>>(p.a);
-    else if (p.V == W) qk_kernel<T, W, 2, BACK><<<grid, 256, sm, st>>>(p.a);
-    else if (p.NS == 1) qk_kernel<T, 1, 1, BACK><<<grid, 256, sm, st>>>(p.a);
-    else if (p.NS == 2) qk_kernel<T, 1, 2, BACK><<<grid, 256, sm, st>>>(p.a);
-    else if (p.NS == 4) qk_kernel<T, 1, 4, BACK><<<grid, 256, sm, st>>>(p.a);
-    else qk_kernel<T, 1, 8, BACK><<<grid, 256, sm, st>>>(p.a);
+    if (p.V == W && p.NS == 1) qk_kernel<T, W, 1, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
+    else if (p.V == W) qk_kernel<T, W, 2, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
+    else if (p.NS <= 2) qk_kernel<T, 1, 2, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
+    else qk_kernel<T, 1, 8, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
     return launched("q/k norm + rotation");
+}
+
+template <bool BACK>
+int run_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
+{
+    if (s->precision == PALSGD_PREC_FP32) return s->interleaved ? launch_qk<float, BACK, true>(p, s, st) : launch_qk<float, BACK, false>(p, s, st);
+    return s->interleaved ? launch_qk<bf16, BACK, true>(p, s, st) : launch_qk<bf16, BACK, false>(p, s, st);
 }
 
 }  // namespace
@@ -580,7 +603,7 @@ extern "C" int palsgd_qk_norm_rope_forward(const palsgd_qk_shape* s, const palsg
     }
     finish_qk(p, s, false);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return s->precision == PALSGD_PREC_FP32 ? launch_qk<float, false>(p, s, st) : launch_qk<bf16, false>(p, s, st);
+    return run_qk<false>(p, s, st);
 }
 
 extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const palsgd_heads* dq_out, const palsgd_heads* dk_out,
@@ -627,12 +650,8 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
     for (int i = 0; i < 2; ++i) sum.parts[i] = s->tokens ? p.a.ctas[i] : 0;
     sum.head_dim = s->head_dim;
     const dim3 grid((unsigned)ceil_div(s->head_dim, 32), 2, s->K);
-    if (s->precision == PALSGD_PREC_FP32) {
-        if (s->tokens) BLOCK_TRY((launch_qk<float, true>(p, s, st)));
-        qk_sum_kernel<float><<<grid, 256, 0, st>>>(sum);
-    } else {
-        if (s->tokens) BLOCK_TRY((launch_qk<bf16, true>(p, s, st)));
-        qk_sum_kernel<bf16><<<grid, 256, 0, st>>>(sum);
-    }
+    if (s->tokens) BLOCK_TRY(run_qk<true>(p, s, st));
+    if (s->precision == PALSGD_PREC_FP32) qk_sum_kernel<float><<<grid, 256, 0, st>>>(sum);
+    else qk_sum_kernel<bf16><<<grid, 256, 0, st>>>(sum);
     return launched("q/k weight gradient");
 }

@@ -89,6 +89,24 @@ template <typename T, int V> __device__ __forceinline__ void raw_get(const Raw<T
     }
 }
 
+// ---- two binary32 values in one 64-bit register: multiply and multiply-add of both in one instruction
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 f2_of(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void f2_get(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 f2_mul(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 f2_fma(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f2 f2_swap(f2 v) { float a, b; f2_get(v, a, b); return f2_of(b, a); }
+__device__ __forceinline__ f2 f2_neg(f2 v) { return v ^ 0x8000000080000000ull; }
+// two bfloat16 in a word -> two floats, and back
+__device__ __forceinline__ f2 f2_wide(uint32_t w) { return f2_of(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t f2_narrow(f2 v)
+{
+    float a, b;
+    f2_get(v, a, b);
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+
 // ---- 8-bit checkpoints: the step 2^(E-127) of a group from the largest magnitude in it (as bits: NaN > Inf > finite).
 // Adding 2^16 to the bits carries into the exponent exactly when the mantissa is >= 1.9921875 = 127.5/64, the values
 // that would round to 128 steps; ties (127.5) go to the even 128 and are among them.  A carry out of the largest finite

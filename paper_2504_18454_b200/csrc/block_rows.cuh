@@ -75,6 +75,8 @@ __global__ void __launch_bounds__(256) act8_kernel(const __grid_constant__ Act8A
 
 // ------------------------------------------------------------------------------------------------ q/k norm + rotation
 
+constexpr uint32_t kQkThreads = 128;
+
 struct HeadsArg {
     const void* x;                // input heads
     const void* d;                // backward: gradient of the output heads
@@ -88,6 +90,7 @@ struct HeadsArg {
 struct QkArgs {
     HeadsArg side[2];             // q, k
     uint32_t ctas[2];             // of one worker, by their shares of the heads: q's first
+    uint32_t abreast[2];          // heads of a token that a warp works on at a time: a power of two
     const float* cos_t;
     const float* sin_t;
     const int32_t* pos;
@@ -95,7 +98,6 @@ struct QkArgs {
     uint64_t tokens, table_rows;
     uint32_t head_dim, rot, pair_slots, slots;   // slots: two vectors of V values each; the first pair_slots hold pairs
     uint32_t lanes;               // lanes of a warp that share one head: a power of two, NS * lanes >= slots
-    int      interleaved;
     int      table_wide;          // the rows of the angle tables start on 16-byte boundaries
     float    eps;
 };
@@ -105,219 +107,289 @@ template <typename T, int V, int NS, bool BACK>
 struct QkItem {
     Raw<T, V> x[NS][2], d[BACK ? NS : 1][2];
     int64_t out;
-    int32_t pos;
     bool live;
 };
 
-template <bool SECOND, typename A, typename B>
-__device__ __forceinline__ auto& either(A& a, B& b)
+// The 2V values of a slot as V pairs of floats.
+template <typename T, int V>
+__device__ __forceinline__ void slot_get(const Raw<T, V> (&r)[2], f2 (&v)[V])
 {
-    if constexpr (SECOND) return b;
-    else return a;
+    if constexpr (V == 1) {
+        v[0] = f2_of(to_f(r[0].r), to_f(r[1].r));
+    } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const uint32_t w[4] = {r[p].r.x, r[p].r.y, r[p].r.z, r[p].r.w};
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                if constexpr (sizeof(T) == 2) v[p * (V / 2) + i] = f2_wide(w[i]);
+                else v[p * (V / 2) + i] = f2_of(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+            }
+        }
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void slot_put(T* base, const uint32_t (&at)[2], const f2 (&v)[V])
+{
+    if constexpr (V == 1) {
+        float a, b;
+        f2_get(v[0], a, b);
+        if (at[0] != ~0u) base[at[0]] = from_f<T>(a);
+        if (at[1] != ~0u) base[at[1]] = from_f<T>(b);
+    } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                if constexpr (sizeof(T) == 2) w[i] = f2_narrow(v[p * (V / 2) + i]);
+                else {
+                    float a, b;
+                    f2_get(v[p * (V / 2) + i], a, b);
+                    w[2 * i] = __float_as_uint(a); w[2 * i + 1] = __float_as_uint(b);
+                }
+            }
+            if (at[p] != ~0u) *reinterpret_cast<uint4*>(base + at[p]) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
 }
 
 // A warp takes a few tokens at a time and walks their heads; `lanes` lanes share a head, and a slot of a lane holds both
 // halves of its rotation pairs, so the rotation needs no exchange: for split halves vectors s and s + rot/(2V), for
-// interleaved pairs two neighbouring vectors (V > 1: the pairs lie inside a vector; V = 1: the slot is the pair).  The
-// only exchanges are the sums over a head.  The next items are under way while one is worked on: two of them forward, one
-// backward (it is twice the size).  Angles are read when their item is due -- all heads of a token read the same ones, so
-// they come from L1 -- and the norm weights stay in registers throughout.
-template <typename T, int V, int NS, bool BACK>
-__global__ void __launch_bounds__(256, NS == 1 ? 2 : 1) qk_kernel(const __grid_constant__ QkArgs a)
+// interleaved pairs two neighbouring vectors (V > 1: the pairs lie inside a vector; V = 1: the slot is the pair).  Values
+// that are not rotated are pairs of angle zero.  The only exchanges are the sums over a head.
+// It moves 4 bytes a value forward (bfloat16) and is bound by instructions before it is by memory: the arithmetic is in
+// pairs of floats, and what depends on the token and not on the head is formed once per token (forward the products of
+// weights and angles), so a warp's groups are spread over heads only as far as leaves four heads or so in a row to each.
+// The next item is under way while one is worked on.
+template <typename T, int V, int NS, bool BACK, bool INTER, int SIDE>
+__device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta)
 {
-    const uint32_t side = blockIdx.x >= a.ctas[0], cta = blockIdx.x - (side ? a.ctas[0] : 0), ctas = a.ctas[side];
-    const HeadsArg& h = a.side[side];
+    constexpr bool kInside = INTER || V == 1;                                 // a rotation pair is one f2 (else: f2 i and V/2 + i)
+    constexpr int H = V / 2;
+    constexpr uint32_t kWarps = kQkThreads / 32;
+    const uint32_t ctas = a.ctas[SIDE];
+    const HeadsArg& h = a.side[SIDE];
     const uint32_t k = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t sub = lane & (a.lanes - 1), group = lane / a.lanes, groups = 32 / a.lanes;
-    const uint32_t n_vec = a.head_dim / V;
+    const uint32_t n_vec = a.head_dim / V, half = a.rot / 2;
     uint32_t at[NS][2];           // first element of each vector, or ~0
-    T w[NS][2][V];
-    float acc[NS][2][V];
+    T w[NS][2 * V];               // two to a register where they are bfloat16
+    f2 acc[BACK ? NS : 1][V];
     const T* wp = static_cast<const T*>(h.w) + (int64_t)k * h.ww;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        const uint32_t slot = s * a.lanes + sub;
-        const uint32_t split = a.interleaved ? 0 : a.pair_slots;
+        const uint32_t slot = s * a.lanes + sub, split = INTER ? 0 : a.pair_slots;
         uint32_t v0, v1;
-        if (slot < split) { v0 = slot; v1 = slot + split; }
+        if (!INTER && slot < split) { v0 = slot; v1 = slot + split; }
         else { v0 = 2 * split + 2 * (slot - split); v1 = v0 + 1; }
         at[s][0] = slot < a.slots && v0 < n_vec ? v0 * V : ~0u;
         at[s][1] = slot < a.slots && v1 < n_vec ? v1 * V : ~0u;
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
+        for (int j = 0; j < 2 * V; ++j) {
+            const uint32_t e = at[s][j / V];
+            w[s][j] = e != ~0u ? wp[e + j % V] : from_f<T>(0.0f);
+        }
+        if constexpr (BACK) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                w[s][p][j] = at[s][p] != ~0u ? wp[at[s][p] + j] : from_f<T>(0.0f);
-                acc[s][p][j] = 0.0f;
-            }
+            for (int j = 0; j < V; ++j) acc[s][j] = 0;
         }
     }
     const float inv_n = 1.0f / (float)a.head_dim;
-    const uint32_t half = a.rot / 2;
     // the warp's groups: `abreast` heads of each of `tokens` tokens
-    uint32_t abreast = 1;
-    while (abreast < groups && abreast < h.heads) abreast *= 2;
-    const uint32_t tokens = groups / abreast, first = group % abreast, rounds = (h.heads + abreast - 1) / abreast;
-    const uint64_t step = (uint64_t)ctas * 8 * tokens;
+    const uint32_t abreast = a.abreast[SIDE], tokens = groups / abreast, first = group % abreast, my_token = group / abreast;
+    const uint32_t rounds = (h.heads + abreast - 1) / abreast;
+    const uint64_t step = (uint64_t)ctas * kWarps * tokens, start = ((uint64_t)cta * kWarps + warp) * tokens;
+    const uint64_t turns = start < a.tokens ? (a.tokens - 1 - start) / step + 1 : 0;      // token groups of this warp
 
-    uint64_t t = ((uint64_t)cta * 8 + warp) * tokens;                  // of the item to be fetched
-    uint32_t round = 0;
     using Item = QkItem<T, V, NS, BACK>;
-    constexpr int kAhead = BACK ? 1 : 2;
+    // where the next item to be fetched lies
+    const T* const xb = static_cast<const T*>(h.x) + (int64_t)k * h.xw;
+    const T* const db = static_cast<const T*>(h.d) + (int64_t)k * h.dw;
+    T* const ob = static_cast<T*>(h.out) + (int64_t)k * h.ow;
+    uint64_t ft = start + my_token;
+    uint32_t fh = first;
+    int64_t fx = (int64_t)ft * h.xt + (int64_t)fh * h.xh, fd = (int64_t)ft * h.dt + (int64_t)fh * h.dh, fo = (int64_t)ft * h.ot + (int64_t)fh * h.oh;
+    uint64_t left = turns * rounds;
     auto fetch = [&](Item& it) {
-        const uint64_t tk = t + group / abreast;
-        const uint32_t hd = round * abreast + first;
-        it.live = tk < a.tokens && hd < h.heads;
-        it.pos = a.rot && it.live ? __ldg(a.pos + (int64_t)k * a.pos_w + (int64_t)tk) : 0;
-        const int64_t hx = (int64_t)k * h.xw + (int64_t)tk * h.xt + (int64_t)hd * h.xh;
-        const int64_t hg = (int64_t)k * h.dw + (int64_t)tk * h.dt + (int64_t)hd * h.dh;
-        it.out = (int64_t)k * h.ow + (int64_t)tk * h.ot + (int64_t)hd * h.oh;
+        it.live = ft < a.tokens && fh < h.heads;
+        it.out = fo;
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 const bool on = it.live && at[s][p] != ~0u;
                 raw_zero(it.x[s][p]);
-                if (on) raw_load(it.x[s][p], static_cast<const T*>(h.x) + hx + at[s][p]);
+                if (on) raw_load(it.x[s][p], xb + fx + at[s][p]);
                 if constexpr (BACK) {
                     raw_zero(it.d[s][p]);
-                    if (on) raw_load(it.d[s][p], static_cast<const T*>(h.d) + hg + at[s][p]);
+                    if (on) raw_load(it.d[s][p], db + fd + at[s][p]);
                 }
             }
-        if (++round == rounds) { round = 0; t += step; }
+        --left;
+        fh += abreast;
+        if (fh - first == rounds * abreast) {
+            ft += step;
+            fh = first;
+            fx = (int64_t)ft * h.xt + (int64_t)fh * h.xh; fo = (int64_t)ft * h.ot + (int64_t)fh * h.oh;
+            if constexpr (BACK) fd = (int64_t)ft * h.dt + (int64_t)fh * h.dh;
+        } else {
+            fx += abreast * h.xh; fo += abreast * h.oh;
+            if constexpr (BACK) fd += abreast * h.dh;
+        }
     };
-    auto work = [&](const Item& it) {
-        const bool ok = !a.rot || (it.pos >= 0 && (uint64_t)it.pos < a.table_rows);
-        const float* ct = a.cos_t + (ok ? (uint64_t)it.pos * half : 0);
-        const float* st = a.sin_t + (ok ? (uint64_t)it.pos * half : 0);
-        float c[NS][V], sn[NS][V];
+    auto over_head = [&](f2 v2) {
+        float v, u;
+        f2_get(v2, v, u);
+        v += u;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const uint32_t i = (s * a.lanes + sub) * V;                       // first pair of the slot
-            if (V > 1 && a.table_wide && i + V <= half && ok && it.live) {
-                if constexpr (V > 1) {
+        for (uint32_t m = 1; m < 32; m *= 2)
+            if (m < a.lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);         // (the same branch for the whole grid)
+        return v;
+    };
+    auto position = [&](uint64_t turn) -> int32_t {
+        const uint64_t tk = start + turn * step + my_token;
+        return a.rot && tk < a.tokens ? __ldg(a.pos + (int64_t)k * a.pos_w + (int64_t)tk) : 0;
+    };
+    auto weight = [&](int s, int i) { return f2_of(to_f(w[s][2 * i]), to_f(w[s][2 * i + 1])); };
+
+    Item next;
+    if (left) fetch(next);
+    int32_t pos_next = position(0);
+    for (uint64_t turn = 0; turn < turns; ++turn) {
+        const int32_t pos = pos_next;
+        if (turn + 1 < turns) pos_next = position(turn + 1);
+        const bool ok = !a.rot || (pos >= 0 && (uint64_t)pos < a.table_rows);
+        // of the pairs of each f2: cosines and, with the signs of the rotation, sines; forward: times the weights
+        f2 mc[NS][V], ms[NS][V];
+        {
+            const float* ct = a.cos_t + (ok ? (uint64_t)pos * half : 0);
+            const float* st = a.sin_t + (ok ? (uint64_t)pos * half : 0);
 #pragma unroll
-                    for (int j = 0; j < V; j += 4) { Vec<float, 4>::load(ct + i + j, c[s] + j); Vec<float, 4>::load(st + i + j, sn[s] + j); }
+            for (int s = 0; s < NS; ++s) {
+                float c[V], sn[V];
+                const uint32_t i = (s * a.lanes + sub) * V;                   // first pair of the slot
+                if (V > 1 && a.table_wide && i + V <= half && ok) {
+                    if constexpr (V > 1) {
+#pragma unroll
+                        for (int j = 0; j < V; j += 4) { Vec<float, 4>::load(ct + i + j, c + j); Vec<float, 4>::load(st + i + j, sn + j); }
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const bool on = i + j < half && ok;
+                        c[j] = on ? __ldg(ct + i + j) : 1.0f;
+                        sn[j] = on ? __ldg(st + i + j) : 0.0f;
+                    }
+                }
+                if constexpr (kInside) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        mc[s][j] = f2_of(c[j], c[j]);
+                        ms[s][j] = BACK ? f2_of(sn[j], -sn[j]) : f2_of(-sn[j], sn[j]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < H; ++j) {
+                        mc[s][j] = mc[s][H + j] = f2_of(c[2 * j], c[2 * j + 1]);
+                        const f2 q = f2_of(sn[2 * j], sn[2 * j + 1]);
+                        ms[s][j] = BACK ? q : f2_neg(q);
+                        ms[s][H + j] = BACK ? f2_neg(q) : q;
+                    }
+                }
+                if constexpr (!BACK) {                                        // value times its own weight, partner times the partner's
+                    f2 wf[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) wf[j] = weight(s, j);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        mc[s][j] = f2_mul(mc[s][j], wf[j]);
+                        ms[s][j] = f2_mul(ms[s][j], kInside ? f2_swap(wf[j]) : wf[(j + H) % V]);
+                    }
+                }
+            }
+        }
+        const float bad = ok ? 0.0f : __uint_as_float(0x7FFFFFFFu);           // outside the table: NaN
+        for (uint32_t round = 0; round < rounds; ++round) {
+            const Item it = next;
+            if (left) fetch(next);
+            f2 x[NS][V], sq = 0;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                slot_get<T, V>(it.x[s], x[s]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) sq = f2_fma(x[s][j], x[s][j], sq);
+            }
+            const float r = rsqrtf(fmaf(over_head(sq), inv_n, a.eps)) + bad;
+            const f2 rr = f2_of(r, r);
+            f2 y[NS][V];
+            if constexpr (!BACK) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) x[s][j] = f2_mul(x[s][j], rr);
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        y[s][j] = f2_fma(x[s][j], mc[s][j], f2_mul(kInside ? f2_swap(x[s][j]) : x[s][(j + H) % V], ms[s][j]));
                 }
             } else {
+                f2 dot = 0;
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const bool on = i + j < half && ok && it.live;
-                    c[s][j] = on ? __ldg(ct + i + j) : 1.0f;
-                    sn[s][j] = on ? __ldg(st + i + j) : 0.0f;
-                }
-            }
-        }
-        float x[NS][2][V], d[BACK ? NS : 1][2][V];
-        float sq = 0.0f;
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                raw_get(it.x[s][p], x[s][p]);
-                if constexpr (BACK) raw_get(it.d[s][p], d[s][p]);
-#pragma unroll
-                for (int j = 0; j < V; ++j) sq = fmaf(x[s][p][j], x[s][p][j], sq);
-            }
-        for (uint32_t m = a.lanes / 2; m; m >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, m);
-        const float r = 1.0f / sqrtf(fmaf(sq, inv_n, a.eps)) + (ok ? 0.0f : __uint_as_float(0x7FFFFFFFu));   // outside the table: NaN
-        auto& y = either<BACK>(x, d);
-        if constexpr (!BACK) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) x[s][p][j] = x[s][p][j] * r * to_f(w[s][p][j]);
-        }
-        // forward: (a, b) -> (a c - b s, b c + a s); backward: by the opposite angle
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            if (V == 1 || !a.interleaved) {
-                if (s * a.lanes + sub < a.pair_slots) {
+                for (int s = 0; s < NS; ++s) {
+                    f2 d[V];
+                    slot_get<T, V>(it.d[s], d);
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float si = BACK ? -sn[s][j] : sn[s][j], co = c[s][j];
-                        const float p0 = y[s][0][j], p1 = y[s][1][j];
-                        y[s][0][j] = fmaf(p0, co, -(p1 * si));
-                        y[s][1][j] = fmaf(p1, co, p0 * si);
+                        y[s][j] = f2_fma(d[j], mc[s][j], f2_mul(kInside ? f2_swap(d[j]) : d[(j + H) % V], ms[s][j]));
+                        x[s][j] = f2_mul(x[s][j], rr);                        // xh
+                        acc[s][j] = f2_fma(y[s][j], x[s][j], acc[s][j]);
+                        y[s][j] = f2_mul(y[s][j], weight(s, j));
+                        dot = f2_fma(y[s][j], x[s][j], dot);
                     }
                 }
-            } else if constexpr (V > 1) {
+                const float m = over_head(dot) * -inv_n;
+                const f2 mm = f2_of(m, m);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {                                // pair j of the slot: element 2j of its 2V values
-                    const float si = BACK ? -sn[s][j] : sn[s][j], co = c[s][j];
-                    const float p0 = y[s][2 * j / V][2 * j % V], p1 = y[s][2 * j / V][2 * j % V + 1];
-                    y[s][2 * j / V][2 * j % V] = fmaf(p0, co, -(p1 * si));
-                    y[s][2 * j / V][2 * j % V + 1] = fmaf(p1, co, p0 * si);
-                }
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) y[s][j] = f2_mul(rr, f2_fma(x[s][j], mm, y[s][j]));
+            }
+            if (it.live) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) slot_put<T, V>(ob + it.out, at[s], y[s]);
             }
         }
-        if constexpr (BACK) {
-            float dot = 0.0f;
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        x[s][p][j] *= r;                                      // xh
-                        acc[s][p][j] = fmaf(d[s][p][j], x[s][p][j], acc[s][p][j]);
-                        d[s][p][j] *= to_f(w[s][p][j]);
-                        dot = fmaf(d[s][p][j], x[s][p][j], dot);
-                    }
-            for (uint32_t m = a.lanes / 2; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
-            dot *= inv_n;
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) d[s][p][j] = r * fmaf(-x[s][p][j], dot, d[s][p][j]);
-        }
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-                if (it.live && at[s][p] != ~0u) Vec<T, V>::store(static_cast<T*>(h.out) + it.out + at[s][p], y[s][p]);
-    };
-
-    // items of this warp: (token groups) * rounds; all lanes walk the same ones
-    const uint64_t mine = t < a.tokens ? ((a.tokens - 1 - t) / step + 1) * rounds : 0;
-    Item ahead[kAhead];
-    uint64_t fetched = 0;
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (fetched < mine) { fetch(ahead[i]); ++fetched; }
-    for (uint64_t i = 0; i < mine; ++i) {
-        const Item cur = ahead[0];
-#pragma unroll
-        for (int j = 0; j + 1 < kAhead; ++j) ahead[j] = ahead[j + 1];
-        if (fetched < mine) { fetch(ahead[kAhead - 1]); ++fetched; }
-        work(cur);
     }
     if constexpr (BACK) {
-        // the CTA's sum in a fixed order: groups of a warp by a butterfly, then the eight warps one after another
-        extern __shared__ float sum[];                                    // [8][head_dim]
+        // the CTA's sum in a fixed order: groups of a warp by a butterfly, then the warps one after another
+        extern __shared__ float sum[];                                        // [kWarps][head_dim]
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float v = acc[s][p][j];
-                    for (uint32_t m = 16; m >= a.lanes; m >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
-                    if (group == 0 && at[s][p] != ~0u) sum[warp * a.head_dim + at[s][p] + j] = v;
-                }
+            for (int j = 0; j < 2 * V; ++j) {
+                float v, u;
+                f2_get(acc[s][j / 2], v, u);
+                if (j & 1) v = u;
+                for (uint32_t m = 16; m >= a.lanes; m >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
+                if (group == 0 && at[s][j / V] != ~0u) sum[warp * a.head_dim + at[s][j / V] + j % V] = v;
+            }
         __syncthreads();
         float* const part = h.part + ((uint64_t)k * ctas + cta) * a.head_dim;
-        for (uint32_t i = threadIdx.x; i < a.head_dim; i += 256) {
+        for (uint32_t i = threadIdx.x; i < a.head_dim; i += kQkThreads) {
             float v = 0.0f;
 #pragma unroll
-            for (int wi = 0; wi < 8; ++wi) v += sum[wi * a.head_dim + i];
+            for (uint32_t wi = 0; wi < kWarps; ++wi) v += sum[wi * a.head_dim + i];
             part[i] = v;
         }
     }
+}
+
+// (Two copies of the walk: with the side a constant its strides are constants of the instruction, not loads by index.)
+template <typename T, int V, int NS, bool BACK, bool INTER>
+__global__ void __launch_bounds__(kQkThreads, NS == 1 ? (BACK ? 4 : 5) : 1) qk_kernel(const __grid_constant__ QkArgs a)
+{
+    if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, INTER, 0>(a, blockIdx.x);
+    else qk_walk<T, V, NS, BACK, INTER, 1>(a, blockIdx.x - a.ctas[0]);
 }
 
 struct QkSumArgs {
