@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import struct
 import threading
 from typing import Dict, NamedTuple, Optional, Tuple, Union
 
@@ -74,37 +75,36 @@ def lib() -> C.CDLL:
 
 # ---------------------------------------------------------------------------------------------- argument marshalling
 
+_FFN_SHAPE = struct.Struct("=IiiiQQQ")                   # palsgd_ffn_shape
+_QK_SHAPE = struct.Struct("=IiQIIIIiIQqd")               # palsgd_qk_shape
+_WORDS = [struct.Struct(f"={n}q") for n in range(64)]
+
+
 class _Args(threading.local):
-    """The structs of one call, packed into one block of memory a thread: palsgd_mat (3 words), palsgd_heads (4) and the
-    workspace size.  A call fills it from the start and passes addresses into it."""
-    WORDS = 128
+    """The structs of one call, packed into one block of memory a thread: the shape at 0, matrices or heads from 64 on,
+    the workspace size at the end.  The library reads them before it returns."""
 
     def __init__(self):
-        self.words = (C.c_int64 * self.WORDS)()
-        self.base = C.addressof(self.words)
-        self.size = C.c_size_t(0)
-        self.size_at = C.addressof(self.size)
+        self.mem = bytearray(640)
+        self.keep = (C.c_char * len(self.mem)).from_buffer(self.mem)
+        self.base = C.addressof(self.keep)
+        self.size = C.c_size_t.from_buffer(self.mem, 632)
 
 
 _args = _Args()
 
 
-def _structs(*tensors: Optional[torch.Tensor], skip: int = 0):
-    """The addresses of the structs (palsgd_mat for up to three axes, palsgd_heads for four) of these tensors, None for
-    None.  Strides of axes of length <= 1 do not matter and become 0."""
-    values, at, base = [], [], _args.base
-    for t in tensors:
-        if t is None:
+def _mats(*rows):
+    """Packs operands (pointer and strides) behind the shape; their addresses, None for None."""
+    m, at, words = _args, [], []
+    base = m.base + 64
+    for r in rows:
+        if r is None:
             at.append(None)
-            continue
-        at.append(base + 8 * len(values))
-        values.append(t.data_ptr())
-        shape, stride, n = t.shape, t.stride(), t.dim()
-        if n == 2:                                        # (K, cols)
-            values += (stride[0] if shape[0] > 1 else 0, 0)
         else:
-            values += [s if m > 1 else 0 for m, s in zip(shape, stride[:-1])]
-    _args.words[:len(values)] = values
+            at.append(base + 8 * len(words))
+            words += r
+    _WORDS[len(words)].pack_into(m.mem, 64, *words)
     return at
 
 
@@ -139,6 +139,13 @@ def _tensor(t, where: str, name: str, shape, dtype, device) -> torch.Tensor:
     if t.device != device:
         _refuse(where, f"{name} must be on {device}, not {t.device}")
     _refuse(where, f"the last axis of {name} must be contiguous")
+
+
+def _mat(t, where: str, name: str, shape, dtype, device):
+    """The checked matrix (K, rows, cols) as (pointer, worker stride, row stride)."""
+    _tensor(t, where, name, shape, dtype, device)
+    s = t.stride()
+    return t.data_ptr(), s[0], s[1]
 
 
 def _cuda(t, where: str, name: str, ndim: int) -> torch.device:
@@ -183,7 +190,7 @@ def _workspace(call, key: tuple, given: Optional[torch.Tensor], like: torch.Tens
     """call(workspace address, address of its size).  Without a workspace of the caller's, one of the size that such a
     call last asked for is allocated; the library reports the size that it wants where that is too small (operands that
     are not aligned need more)."""
-    size, at = _args.size, _args.size_at
+    size, at = _args.size, _args.base + 632
     if given is not None:
         if given.dtype != torch.uint8 or given.device != like.device or not given.is_contiguous():
             _refuse(where, f"workspace must be a contiguous uint8 tensor on {like.device}")
@@ -221,13 +228,23 @@ def _groups(cols: int) -> int:
     return (cols + ACT8_GROUP - 1) // ACT8_GROUP
 
 
-def _three(t: torch.Tensor) -> torch.Tensor:
-    return t[None] if t.dim() == 2 else t
+def _rows(t: torch.Tensor):
+    """(rows, cols) or (K, rows, cols) as (pointer, worker stride, row stride)."""
+    s = t.stride()
+    return (t.data_ptr(), s[0], s[1]) if len(s) == 3 else (t.data_ptr(), 0, s[0])
 
 
 def _act8(where, a: Act8, name, shape, dev):
-    _tensor(a.q, where, name + ".q", shape, torch.int8, dev)
-    _tensor(a.exponent, where, name + ".exponent", (*shape[:-1], _groups(shape[-1])), torch.uint8, dev)
+    """The checked checkpoint of a (K, rows, cols) matrix as two triples."""
+    return (_mat(a.q, where, name + ".q", shape, torch.int8, dev),
+            _mat(a.exponent, where, name + ".exponent", (*shape[:-1], _groups(shape[-1])), torch.uint8, dev))
+
+
+def _act8_run(entry: str, prec: int, x: torch.Tensor, a: Act8, raw: int, order) -> None:
+    shape = x.shape
+    at = _mats(_rows(x), _rows(a.q), _rows(a.exponent))
+    k, r = (1, shape[0]) if len(shape) == 2 else (shape[0], shape[1])
+    _check(getattr(lib(), entry)(prec, k, r, shape[-1], at[order[0]], at[order[1]], at[order[2]], raw), entry)
 
 
 def act8_pack(x: torch.Tensor, *, out: Optional[Act8] = None, stream: Optional[int] = None) -> Act8:
@@ -236,14 +253,14 @@ def act8_pack(x: torch.Tensor, *, out: Optional[Act8] = None, stream: Optional[i
     dev = _cuda(x, where, "x", 2 if isinstance(x, torch.Tensor) and x.dim() == 2 else 3)
     prec, shape = _precision(x, where, "x"), x.shape
     _tensor(x, where, "x", shape, x.dtype, dev)
+    groups = (*shape[:-1], _groups(shape[-1]))
     with _On(dev, stream) as on:
         if out is None:
-            out = Act8(torch.empty(shape, dtype=torch.int8, device=dev),
-                       torch.empty((*shape[:-1], _groups(shape[-1])), dtype=torch.uint8, device=dev), x.dtype)
+            out = Act8(x.new_empty(shape, dtype=torch.int8), x.new_empty(groups, dtype=torch.uint8), x.dtype)
         else:
-            _act8(where, out, "out", shape, dev)
-        v = _three(x)
-        _check(lib().palsgd_act8_pack(prec, *v.shape, *_structs(v, _three(out.q), _three(out.exponent)), on.raw), where)
+            _tensor(out.q, where, "out.q", shape, torch.int8, dev)
+            _tensor(out.exponent, where, "out.exponent", groups, torch.uint8, dev)
+        _act8_run(where, prec, x, out, on.raw, (0, 1, 2))
     return out
 
 
@@ -255,15 +272,14 @@ def act8_unpack(a: Act8, *, dtype: Optional[torch.dtype] = None, out: Optional[t
     q = a.q
     dev = _cuda(q, where, "q", 2 if isinstance(q, torch.Tensor) and q.dim() == 2 else 3)
     shape = q.shape
-    _act8(where, a, "checkpoint", shape, dev)
-    dtype = dtype or (out.dtype if out is not None else a.dtype)
+    _tensor(q, where, "q", shape, torch.int8, dev)
+    _tensor(a.exponent, where, "exponent", (*shape[:-1], _groups(shape[-1])), torch.uint8, dev)
     with _On(dev, stream) as on:
         if out is None:
-            out = torch.empty(shape, dtype=dtype, device=dev)
-        prec = _precision(out, where, "out")
-        _tensor(out, where, "out", shape, dtype, dev)
-        v = _three(out)
-        _check(lib().palsgd_act8_unpack(prec, *v.shape, *_structs(_three(q), _three(a.exponent), v), on.raw), where)
+            out = q.new_empty(shape, dtype=dtype or a.dtype)
+        else:
+            _tensor(out, where, "out", shape, dtype or out.dtype, dev)
+        _act8_run(where, _precision(out, where, "out"), out, a, on.raw, (1, 2, 0))
     return out
 
 
@@ -271,14 +287,12 @@ def act8_unpack(a: Act8, *, dtype: Optional[torch.dtype] = None, out: Optional[t
 
 def _ffn_weights(where, w_gate, w_up, w_down, K, D, dt, dev):
     F = w_gate.shape[1] if isinstance(w_gate, torch.Tensor) and w_gate.dim() == 3 else 0
-    _tensor(w_gate, where, "w_gate", (K, F, D), dt, dev)
-    _tensor(w_up, where, "w_up", (K, F, D), dt, dev)
-    _tensor(w_down, where, "w_down", (K, D, F), dt, dev)
-    return F
+    return (F, _mat(w_gate, where, "w_gate", (K, F, D), dt, dev), _mat(w_up, where, "w_up", (K, F, D), dt, dev),
+            _mat(w_down, where, "w_down", (K, D, F), dt, dev))
 
 
 def _saved(where, save, saved, shape, dt, dev):
-    """gate, up and their exponents as tensors, or None."""
+    """gate, up and their exponents as triples, or None."""
     if save == SAVE_NONE:
         return None, None, None, None
     if not isinstance(saved, (tuple, list)) or len(saved) != 2:
@@ -287,12 +301,9 @@ def _saved(where, save, saved, shape, dt, dev):
     if save == SAVE_8BIT:
         if not (isinstance(gate, Act8) and isinstance(up, Act8)):
             _refuse(where, "gate and up must both be Act8")
-        _act8(where, gate, "gate", shape, dev)
-        _act8(where, up, "up", shape, dev)
-        return gate.q, up.q, gate.exponent, up.exponent
-    _tensor(gate, where, "gate", shape, dt, dev)
-    _tensor(up, where, "up", shape, dt, dev)
-    return gate, up, None, None
+        (gq, ge), (uq, ue) = _act8(where, gate, "gate", shape, dev), _act8(where, up, "up", shape, dev)
+        return gq, uq, ge, ue
+    return _mat(gate, where, "gate", shape, dt, dev), _mat(up, where, "up", shape, dt, dev), None, None
 
 
 def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
@@ -308,22 +319,24 @@ def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_dow
     where = "palsgd_ffn_forward"
     dev = _cuda(x, where, "x", 3)
     prec, dt = _precision(x, where, "x"), x.dtype
-    K, M, D = x.shape
-    _tensor(x, where, "x", x.shape, dt, dev)
-    F = _ffn_weights(where, w_gate, w_up, w_down, K, D, dt, dev)
-    shape = FfnShape(K, prec, activation, save, M, D, F)
+    K, M, D = xs = x.shape
+    mx = _mat(x, where, "x", xs, dt, dev)
+    F, mg, mu, md = _ffn_weights(where, w_gate, w_up, w_down, K, D, dt, dev)
     with _On(dev, stream) as on:
-        y = torch.empty((K, M, D), dtype=dt, device=dev) if out is None else _tensor(out, where, "out", (K, M, D), dt, dev)
+        y = x.new_empty(xs) if out is None else out
+        my = _mat(y, where, "out", xs, dt, dev)
         if save == SAVE_NONE:
             saved = None
         elif saved is None:
             if save == SAVE_8BIT:
-                saved = tuple(Act8(torch.empty((K, M, F), dtype=torch.int8, device=dev),
-                                   torch.empty((K, M, _groups(F)), dtype=torch.uint8, device=dev), dt) for _ in range(2))
+                G = _groups(F)
+                saved = tuple([Act8(x.new_empty((K, M, F), dtype=torch.int8), x.new_empty((K, M, G), dtype=torch.uint8), dt)
+                               for _ in range(2)])
             else:
-                saved = tuple(torch.empty((K, M, F), dtype=dt, device=dev) for _ in range(2))
-        at = _structs(x, w_gate, w_up, w_down, y, *_saved(where, save, saved, (K, M, F), dt, dev))
-        entry, s = lib().palsgd_ffn_forward, C.addressof(shape)
+                saved = (x.new_empty((K, M, F)), x.new_empty((K, M, F)))
+        at = _mats(mx, mg, mu, md, my, *_saved(where, save, saved, (K, M, F), dt, dev))
+        _FFN_SHAPE.pack_into(_args.mem, 0, K, prec, activation, save, M, D, F)
+        entry, s = lib().palsgd_ffn_forward, _args.base
         _workspace(lambda ws, n: entry(s, *at, ws, n, on.raw), (where, K, M, D, F, prec), workspace, x, where)
     return y, saved
 
@@ -340,59 +353,68 @@ def ffn_backward(dy: torch.Tensor, x: Saved, w_gate: torch.Tensor, w_up: torch.T
     where = "palsgd_ffn_backward"
     dev = _cuda(dy, where, "dy", 3)
     prec, dt = _precision(dy, where, "dy"), dy.dtype
-    K, M, D = dy.shape
-    _tensor(dy, where, "dy", dy.shape, dt, dev)
-    F = _ffn_weights(where, w_gate, w_up, w_down, K, D, dt, dev)
+    K, M, D = ys = dy.shape
+    mdy = _mat(dy, where, "dy", ys, dt, dev)
+    F, mg, mu, md = _ffn_weights(where, w_gate, w_up, w_down, K, D, dt, dev)
     if not isinstance(saved, (tuple, list)) or len(saved) != 2:
         _refuse(where, "saved must be the pair (gate, up)")
     save = SAVE_8BIT if isinstance(saved[0], Act8) else SAVE_FULL
     if isinstance(x, Act8):
-        _act8(where, x, "x", (K, M, D), dev)
         if save != SAVE_8BIT:
             _refuse(where, "x may be an Act8 only where gate and up are")
-        xs = (x.q, x.exponent)
+        mx, me = _act8(where, x, "x", ys, dev)
     else:
-        xs = (_tensor(x, where, "x", (K, M, D), dt, dev), None)
-    shape = FfnShape(K, prec, activation, save, M, D, F)
+        mx, me = _mat(x, where, "x", ys, dt, dev), None
     with _On(dev, stream) as on:
-        want = ((K, M, D), (K, F, D), (K, F, D), (K, D, F))
+        want = (ys, (K, F, D), (K, F, D), (K, D, F))
         outs = list(out) if out is not None else [None] * 4
         if len(outs) != 4:
             _refuse(where, "out must be (dx, dw_gate, dw_up, dw_down)")
+        mats = [None] * 4
         for i, name in enumerate(("dx", "dw_gate", "dw_up", "dw_down")):
             if i == 0 and not need_dx:
                 outs[0] = None
-            elif outs[i] is None:
-                outs[i] = torch.empty(want[i], dtype=dt, device=dev)
-            else:
-                _tensor(outs[i], where, name, want[i], dt, dev)
-        at = _structs(dy, *xs, w_gate, w_up, w_down, *_saved(where, save, saved, (K, M, F), dt, dev), *outs)
-        entry, s = lib().palsgd_ffn_backward, C.addressof(shape)
-        _workspace(lambda ws, n: entry(s, *at, ws, n, on.raw), (where, K, M, D, F, prec, need_dx, len(at) - at.count(None)),
-                   workspace, dy, where)
+                continue
+            if outs[i] is None:
+                outs[i] = dy.new_empty(want[i])
+            mats[i] = _mat(outs[i], where, name, want[i], dt, dev)
+        at = _mats(mdy, mx, me, mg, mu, md, *_saved(where, save, saved, (K, M, F), dt, dev), *mats)
+        _FFN_SHAPE.pack_into(_args.mem, 0, K, prec, activation, save, M, D, F)
+        entry, s = lib().palsgd_ffn_backward, _args.base
+        _workspace(lambda ws, n: entry(s, *at, ws, n, on.raw), (where, K, M, D, F, prec, need_dx, me is None), workspace,
+                   dy, where)
     return tuple(outs)
 
 
 # ---------------------------------------------------------------------------------------------- q/k norm + rotation
 
+def _heads(t, where: str, name: str, shape, dtype, device):
+    """The checked heads (K, tokens, heads, head_dim) as (pointer, worker, token and head stride)."""
+    _tensor(t, where, name, shape, dtype, device)
+    s = t.stride()
+    return t.data_ptr(), s[0], s[1], s[2]
+
+
 def _qk(where, q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
+    """Checks the arguments and packs the shape; the packed operands, and the addresses of the tables."""
     dev = _cuda(q, where, "q", 4)
     prec, dt = _precision(q, where, "q"), q.dtype
     K, M, HQ, DH = q.shape
     HK = k.shape[2] if isinstance(k, torch.Tensor) and k.dim() == 4 else -1
-    _tensor(q, where, "q", q.shape, dt, dev)
-    _tensor(k, where, "k", (K, M, HK, DH), dt, dev)
-    _tensor(w_q, where, "w_q", (K, DH), dt, dev)
-    _tensor(w_k, where, "w_k", (K, DH), dt, dev)
+    ops = [_heads(q, where, "q", q.shape, dt, dev), _heads(k, where, "k", (K, M, HK, DH), dt, dev)]
+    for name, w in (("w_q", w_q), ("w_k", w_k)):
+        _tensor(w, where, name, (K, DH), dt, dev)
+        ops.append((w.data_ptr(), w.stride(0), 0))
     if not isinstance(cos, torch.Tensor) or cos.dim() != 2:
         _refuse(where, "cos must be a (rows, rotary_dim / 2) tensor")
+    rows, half = shape = cos.shape
     for name, t in (("cos", cos), ("sin", sin)):
-        if not _tensor(t, where, name, cos.shape, torch.float32, dev).is_contiguous():
+        if not _tensor(t, where, name, shape, torch.float32, dev).is_contiguous():
             _refuse(where, f"{name} must be contiguous")
     _tensor(positions, where, "positions", (K, M), torch.int32, dev)
-    shape = QkShape(K, prec, M, HQ, HK, DH, 2 * cos.shape[1], 1 if interleaved else 0, 0, cos.shape[0],
-                    positions.stride(0) if K > 1 else 0, eps)
-    return dev, shape, (cos.data_ptr(), sin.data_ptr(), positions.data_ptr())
+    _QK_SHAPE.pack_into(_args.mem, 0, K, prec, M, HQ, HK, DH, 2 * half, 1 if interleaved else 0, 0, rows,
+                        positions.stride(0) if K > 1 else 0, eps)
+    return dev, ops, (cos.data_ptr(), sin.data_ptr(), positions.data_ptr())
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, w_q: torch.Tensor, w_k: torch.Tensor, cos: torch.Tensor,
@@ -402,16 +424,13 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, w_q: torch.Tensor, w_k: torch
     w_q, w_k (K, head_dim), then the rotation of the first 2*cos.shape[1] values by the angle tables cos, sin
     (rows, rotary_dim / 2) at positions (K, tokens) int32.  Returns (q_out, k_out)."""
     where = "palsgd_qk_norm_rope_forward"
-    dev, shape, tables = _qk(where, q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    dev, ops, tables = _qk(where, q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
     with _On(dev, stream) as on:
-        if out is None:
-            out = (torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=q.dtype, device=dev))
-        else:
-            _tensor(out[0], where, "q_out", q.shape, q.dtype, dev)
-            _tensor(out[1], where, "k_out", k.shape, q.dtype, dev)
-        aq, ak, awq, awk, oq, ok = _structs(q, k, w_q, w_k, *out)
-        _check(lib().palsgd_qk_norm_rope_forward(C.addressof(shape), aq, ak, awq, awk, *tables, oq, ok, on.raw), where)
-    return tuple(out)
+        out = (q.new_empty(q.shape), k.new_empty(k.shape)) if out is None else tuple(out)
+        mq, mk, mwq, mwk, mo, mp = _mats(*ops, _heads(out[0], where, "q_out", q.shape, q.dtype, dev),
+                                         _heads(out[1], where, "k_out", k.shape, q.dtype, dev))
+        _check(lib().palsgd_qk_norm_rope_forward(_args.base, mq, mk, mwq, mwk, *tables, mo, mp, on.raw), where)
+    return out
 
 
 def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
@@ -422,20 +441,24 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.T
     """palsgd_qk_norm_rope_backward: (dq, dk, dw_q, dw_k) from the gradients of qk_norm_rope's results and its inputs.
     `out` gives the memory to write to; entries may be None."""
     where = "palsgd_qk_norm_rope_backward"
-    dev, shape, tables = _qk(where, q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
-    _tensor(dq_out, where, "dq_out", q.shape, q.dtype, dev)
-    _tensor(dk_out, where, "dk_out", k.shape, q.dtype, dev)
+    dev, ops, tables = _qk(where, q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    dt = q.dtype
+    grads = [_heads(dq_out, where, "dq_out", q.shape, dt, dev), _heads(dk_out, where, "dk_out", k.shape, dt, dev)]
     with _On(dev, stream) as on:
         outs = list(out) if out is not None else [None] * 4
         if len(outs) != 4:
             _refuse(where, "out must be (dq, dk, dw_q, dw_k)")
+        mats = []
         for i, (name, like) in enumerate((("dq", q), ("dk", k), ("dw_q", w_q), ("dw_k", w_k))):
             if outs[i] is None:
-                outs[i] = torch.empty(like.shape, dtype=q.dtype, device=dev)
+                outs[i] = like.new_empty(like.shape)
+            if i < 2:
+                mats.append(_heads(outs[i], where, name, like.shape, dt, dev))
             else:
-                _tensor(outs[i], where, name, like.shape, q.dtype, dev)
-        at = _structs(dq_out, dk_out, q, k, w_q, w_k, *outs)
-        entry, s = lib().palsgd_qk_norm_rope_backward, C.addressof(shape)
-        _workspace(lambda ws, n: entry(s, *at[:6], *tables, *at[6:], ws, n, on.raw),
-                   (where, *q.shape, k.shape[2]), workspace, q, where)
+                _tensor(outs[i], where, name, like.shape, dt, dev)
+                mats.append((outs[i].data_ptr(), outs[i].stride(0), 0))
+        at = _mats(*grads, *ops, *mats)
+        entry, s = lib().palsgd_qk_norm_rope_backward, _args.base
+        _workspace(lambda ws, n: entry(s, *at[:6], *tables, *at[6:], ws, n, on.raw), (where, *q.shape, k.shape[2]),
+                   workspace, q, where)
     return tuple(outs)

@@ -41,6 +41,34 @@ bool disjoint(Axis a, Axis b, Axis c, uint64_t run)
     return true;
 }
 
+// A matrix argument with the strides of axes of at most one element, which nothing steps over, as zero.
+struct Mat {
+    palsgd_mat m{};
+    bool given;
+    Mat(const palsgd_mat* p, uint32_t K, uint64_t rows) : given(p != nullptr)
+    {
+        if (!p) return;
+        m = *p;
+        if (K <= 1) m.worker_stride = 0;
+        if (rows <= 1) m.row_stride = 0;
+    }
+    operator const palsgd_mat*() const { return given ? &m : nullptr; }
+};
+
+struct HeadsOf {
+    palsgd_heads m{};
+    bool given;
+    HeadsOf(const palsgd_heads* p, const palsgd_qk_shape* s, uint32_t heads) : given(p != nullptr)
+    {
+        if (!p) return;
+        m = *p;
+        if (s->K <= 1) m.worker_stride = 0;
+        if (s->tokens <= 1) m.token_stride = 0;
+        if (heads <= 1) m.head_stride = 0;
+    }
+    operator const palsgd_heads*() const { return given ? &m : nullptr; }
+};
+
 // A matrix argument: EINVAL / EALIGN / OK.  Nothing is asked of a matrix without elements.
 int check_mat(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, size_t es, bool output)
 {
@@ -430,30 +458,34 @@ int run_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
 
 }  // namespace
 
-extern "C" int palsgd_act8_pack(int32_t precision, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x,
-                                const palsgd_mat* q, const palsgd_mat* e, void* stream)
+extern "C" int palsgd_act8_pack(int32_t precision, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x_,
+                                const palsgd_mat* q_, const palsgd_mat* e_, void* stream)
 {
+    const Mat x(x_, K, rows), q(q_, K, rows), e(e_, K, rows);
     BLOCK_TRY(check_act8(precision, K, rows, cols, x, q, e, true));
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return precision == PALSGD_PREC_FP32 ? launch_act8<float, true>(K, rows, cols, x, q, e, st)
                                          : launch_act8<bf16, true>(K, rows, cols, x, q, e, st);
 }
 
-extern "C" int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* q,
-                                  const palsgd_mat* e, const palsgd_mat* x, void* stream)
+extern "C" int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* q_,
+                                  const palsgd_mat* e_, const palsgd_mat* x_, void* stream)
 {
+    const Mat x(x_, K, rows), q(q_, K, rows), e(e_, K, rows);
     BLOCK_TRY(check_act8(precision, K, rows, cols, x, q, e, false));
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return precision == PALSGD_PREC_FP32 ? launch_act8<float, false>(K, rows, cols, x, q, e, st)
                                          : launch_act8<bf16, false>(K, rows, cols, x, q, e, st);
 }
 
-extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x, const palsgd_mat* w_gate,
-                                  const palsgd_mat* w_up, const palsgd_mat* w_down, const palsgd_mat* y,
-                                  const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e,
-                                  const palsgd_mat* up_e, void* workspace, size_t* workspace_bytes, void* stream)
+extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x_, const palsgd_mat* w_gate_,
+                                  const palsgd_mat* w_up_, const palsgd_mat* w_down_, const palsgd_mat* y_,
+                                  const palsgd_mat* gate_, const palsgd_mat* up_, const palsgd_mat* gate_e_,
+                                  const palsgd_mat* up_e_, void* workspace, size_t* workspace_bytes, void* stream)
 {
     BLOCK_TRY(check_shape(s));
+    const Mat x(x_, s->K, s->tokens), w_gate(w_gate_, s->K, s->d_ff), w_up(w_up_, s->K, s->d_ff), w_down(w_down_, s->K, s->d_model);
+    const Mat y(y_, s->K, s->tokens), gate(gate_, s->K, s->tokens), up(up_, s->K, s->tokens), gate_e(gate_e_, s->K, s->tokens), up_e(up_e_, s->K, s->tokens);
     const uint64_t M = s->tokens, D = s->d_model, F = s->d_ff;
     const size_t es = elem(s->precision);
     BLOCK_TRY(check_mat(x, s->K, M, D, es, false));
@@ -491,14 +523,18 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
     return run_mat<MAT_PLAIN>(down, s->precision, dev, st);
 }
 
-extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* dy, const palsgd_mat* x, const palsgd_mat* x_e,
-                                   const palsgd_mat* w_gate, const palsgd_mat* w_up, const palsgd_mat* w_down,
-                                   const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e,
-                                   const palsgd_mat* up_e, const palsgd_mat* dx, const palsgd_mat* dw_gate,
-                                   const palsgd_mat* dw_up, const palsgd_mat* dw_down, void* workspace,
+extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* dy_, const palsgd_mat* x_, const palsgd_mat* x_e_,
+                                   const palsgd_mat* w_gate_, const palsgd_mat* w_up_, const palsgd_mat* w_down_,
+                                   const palsgd_mat* gate_, const palsgd_mat* up_, const palsgd_mat* gate_e_,
+                                   const palsgd_mat* up_e_, const palsgd_mat* dx_, const palsgd_mat* dw_gate_,
+                                   const palsgd_mat* dw_up_, const palsgd_mat* dw_down_, void* workspace,
                                    size_t* workspace_bytes, void* stream)
 {
     BLOCK_TRY(check_shape(s));
+    const Mat dy(dy_, s->K, s->tokens), x(x_, s->K, s->tokens), x_e(x_e_, s->K, s->tokens), dx(dx_, s->K, s->tokens);
+    const Mat w_gate(w_gate_, s->K, s->d_ff), w_up(w_up_, s->K, s->d_ff), w_down(w_down_, s->K, s->d_model);
+    const Mat gate(gate_, s->K, s->tokens), up(up_, s->K, s->tokens), gate_e(gate_e_, s->K, s->tokens), up_e(up_e_, s->K, s->tokens);
+    const Mat dw_gate(dw_gate_, s->K, s->d_ff), dw_up(dw_up_, s->K, s->d_ff), dw_down(dw_down_, s->K, s->d_model);
     if (s->save == PALSGD_SAVE_NONE || (x_e && s->save != PALSGD_SAVE_8BIT)) return PALSGD_EINVAL;
     const uint64_t M = s->tokens, D = s->d_model, F = s->d_ff;
     const size_t es = elem(s->precision);
@@ -584,9 +620,11 @@ extern "C" int palsgd_qk_norm_rope_forward(const palsgd_qk_shape* s, const palsg
                                            const palsgd_heads* k_out, void* stream)
 {
     BLOCK_TRY(check_qk(s, cos_table, sin_table, positions));
-    const palsgd_heads *in[2] = {q, k}, *out[2] = {q_out, k_out};
-    const palsgd_mat* w[2] = {w_q, w_k};
     const uint32_t heads[2] = {s->heads_q, s->heads_k};
+    const HeadsOf given[4] = {{q, s, heads[0]}, {k, s, heads[1]}, {q_out, s, heads[0]}, {k_out, s, heads[1]}};
+    const Mat weights[2] = {{w_q, s->K, 1}, {w_k, s->K, 1}};
+    const palsgd_heads *in[2] = {given[0], given[1]}, *out[2] = {given[2], given[3]};
+    const palsgd_mat* w[2] = {weights[0], weights[1]};
     for (int i = 0; i < 2; ++i) {
         BLOCK_TRY(check_heads(in[i], s, heads[i], false));
         BLOCK_TRY(check_heads(out[i], s, heads[i], true));
@@ -614,9 +652,11 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
                                             size_t* workspace_bytes, void* stream)
 {
     BLOCK_TRY(check_qk(s, cos_table, sin_table, positions));
-    const palsgd_heads *in[2] = {q, k}, *grad[2] = {dq_out, dk_out}, *out[2] = {dq, dk};
-    const palsgd_mat *w[2] = {w_q, w_k}, *dw[2] = {dw_q, dw_k};
     const uint32_t heads[2] = {s->heads_q, s->heads_k};
+    const HeadsOf given[6] = {{q, s, heads[0]}, {k, s, heads[1]}, {dq_out, s, heads[0]}, {dk_out, s, heads[1]}, {dq, s, heads[0]}, {dk, s, heads[1]}};
+    const Mat weights[4] = {{w_q, s->K, 1}, {w_k, s->K, 1}, {dw_q, s->K, 1}, {dw_k, s->K, 1}};
+    const palsgd_heads *in[2] = {given[0], given[1]}, *grad[2] = {given[2], given[3]}, *out[2] = {given[4], given[5]};
+    const palsgd_mat *w[2] = {weights[0], weights[1]}, *dw[2] = {weights[2], weights[3]};
     for (int i = 0; i < 2; ++i) {
         BLOCK_TRY(check_heads(grad[i], s, heads[i], false));
         BLOCK_TRY(check_heads(in[i], s, heads[i], false));
