@@ -186,7 +186,7 @@ PFN_cuTensorMapEncodeTiled_v12000 g_encode;
 std::mutex g_mutex;
 
 template <typename T, int MODE>
-cudaError_t allow_smem() { return cudaFuncSetAttribute(mat_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMatSmem); }
+cudaError_t allow_smem() { return cudaFuncSetAttribute(mat_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MatShape<T, MODE>::kSmem); }
 
 int device_of(Device& out)
 {
@@ -287,13 +287,13 @@ int encode(CUtensorMap* map, const Operand& o, bool mn)
     return rc == CUDA_SUCCESS ? PALSGD_OK : palsgd_block_cuda_fail((int)cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
 }
 
-MatOut out_of(const palsgd_mat* m, size_t es)
+MatOut out_of(const palsgd_mat* m, uint64_t cols, size_t es)
 {
-    MatOut o{m->data, m->worker_stride, m->row_stride, 0, 0};
+    MatOut o{m->data, m->worker_stride, m->row_stride, 0, 0, (uint32_t)cols};
     o.wide = aligned(m->data, 16) && (m->worker_stride * es) % 16 == 0 && (m->row_stride * es) % 16 == 0;
     return o;
 }
-MatOut out_of(const Operand& o) { return MatOut{const_cast<void*>(o.p), o.w, o.r, o.part, 1}; }
+MatOut out_of(const Operand& o) { return MatOut{const_cast<void*>(o.p), o.w, o.r, o.part, 1, (uint32_t)o.r}; }
 
 // One product appended to a launch; B1/A1: the second segment, or (gate/up) the up weights as B1.
 int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, const Operand* A0, const Operand* A1, bool amn,
@@ -322,8 +322,8 @@ int run_mat(MatLaunch& L, int32_t prec, const Device& d, cudaStream_t st)
     if (L.tiles == 0) return PALSGD_OK;
     L.gave_up = d.gave_up;
     const uint32_t pairs = (uint32_t)(d.sms / 2) < L.tiles ? (uint32_t)(d.sms / 2) : L.tiles;
-    if (prec == PALSGD_PREC_FP32) mat_kernel<float, MODE><<<2 * pairs, kMatThreads, kMatSmem, st>>>(L);
-    else mat_kernel<bf16, MODE><<<2 * pairs, kMatThreads, kMatSmem, st>>>(L);
+    if (prec == PALSGD_PREC_FP32) mat_kernel<float, MODE><<<2 * pairs, MatShape<float, MODE>::kThreads, MatShape<float, MODE>::kSmem, st>>>(L);
+    else mat_kernel<bf16, MODE><<<2 * pairs, MatShape<bf16, MODE>::kThreads, MatShape<bf16, MODE>::kSmem, st>>>(L);
     return launched("matrix kernel");
 }
 
@@ -333,9 +333,9 @@ void set_saved(MatLaunch& L, const palsgd_ffn_shape* s, const palsgd_mat* gate, 
     L.act = s->activation;
     if (s->save == PALSGD_SAVE_NONE) return;
     const size_t es = s->save == PALSGD_SAVE_8BIT ? 1 : elem(s->precision);
-    L.gate = out_of(gate, es);
-    L.up = out_of(up, es);
-    if (s->save == PALSGD_SAVE_8BIT) { L.gate_e = out_of(gate_e, 1); L.up_e = out_of(up_e, 1); }
+    L.gate = out_of(gate, s->d_ff, es);
+    L.up = out_of(up, s->d_ff, es);
+    if (s->save == PALSGD_SAVE_8BIT) { L.gate_e = out_of(gate_e, 0, 1); L.up_e = out_of(up_e, 0, 1); }
 }
 
 // ------------------------------------------------------------------------------------------------ q/k norm + rotation
@@ -517,7 +517,7 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
     gated.p[0].out[0] = out_of(oh);
     set_saved(gated, s, gate, up, gate_e, up_e);
     BLOCK_TRY(add_problem(down, M, D, F, s->K, &oh, nullptr, false, &od, nullptr, false, kTileN));
-    down.p[0].out[0] = out_of(y, es);
+    down.p[0].out[0] = out_of(y, D, es);
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_GATED>(gated, s->precision, dev, st));
     return run_mat<MAT_PLAIN>(down, s->precision, dev, st);
@@ -587,14 +587,14 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     set_saved(hidden, s, gate, up, gate_e, up_e);
     if (dx) {                                            // first: its tiles are the longest
         BLOCK_TRY(add_problem(grads, M, D, F, s->K, &hid[0], &hid[1], false, &og, &ou, true, kTileN));
-        grads.p[0].out[0] = out_of(dx, es);
+        grads.p[0].out[0] = out_of(dx, D, es);
     }
     BLOCK_TRY(add_problem(grads, F, D, M, s->K, &hid[0], nullptr, true, &ox, nullptr, true, kTileN));
-    grads.p[grads.n_problems - 1].out[0] = out_of(dw_gate, es);
+    grads.p[grads.n_problems - 1].out[0] = out_of(dw_gate, D, es);
     BLOCK_TRY(add_problem(grads, F, D, M, s->K, &hid[1], nullptr, true, &ox, nullptr, true, kTileN));
-    grads.p[grads.n_problems - 1].out[0] = out_of(dw_up, es);
+    grads.p[grads.n_problems - 1].out[0] = out_of(dw_up, D, es);
     BLOCK_TRY(add_problem(grads, D, F, M, s->K, &ody, nullptr, true, &hid[2], nullptr, true, kTileN));
-    grads.p[grads.n_problems - 1].out[0] = out_of(dw_down, es);
+    grads.p[grads.n_problems - 1].out[0] = out_of(dw_down, F, es);
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s->precision, dev, st));
     return run_mat<MAT_PLAIN>(grads, s->precision, dev, st);

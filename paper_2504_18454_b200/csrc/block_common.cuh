@@ -120,8 +120,32 @@ __device__ __forceinline__ uint32_t act8_exponent(uint32_t amax_bits)
 // 1 / step as a float (0 for a group that is not finite: its q are 0 -- NaN * 0 converts to 0 too)
 __device__ __forceinline__ float act8_inverse(uint32_t E) { return E == 255u ? 0.0f : __uint_as_float((254u - E) << 23); }
 __device__ __forceinline__ float act8_step(uint32_t E) { return E == 255u ? __uint_as_float(0x7FFFFFFFu) : __uint_as_float(E << 23); }
-// x and 1/step as above: |x / step| rounds to at most 127, so the low byte of the integer is the int8
-__device__ __forceinline__ int act8_quant(float x, float inv) { return __float2int_rn(x * inv); }
+// Four values as the bytes of a word: x / step, rounded to an integer by adding 1.5 * 2^23 (exactly: 1/step is a power of
+// two, so the product is exact), which leaves the int8 in the low byte.  |x / step| rounds to at most 127.
+__device__ __forceinline__ uint32_t act8_quant4(float a, float b, float c, float d, float inv)
+{
+    const float k = 12582912.0f;
+    const uint32_t x = __float_as_uint(fmaf(a, inv, k)), y = __float_as_uint(fmaf(b, inv, k));
+    const uint32_t z = __float_as_uint(fmaf(c, inv, k)), w = __float_as_uint(fmaf(d, inv, k));
+    const uint32_t r = __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
+    return inv == 0.0f ? 0u : r;                          // not finite: every q is 0
+}
+// the larger of m and |x|; a NaN stays
+__device__ __forceinline__ float act8_max(float m, float x)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(x)));
+    return r;
+}
+// m = max |x| of a group, any NaN as the canonical one
+__device__ __forceinline__ uint32_t act8_exponent(float m) { return act8_exponent(__float_as_uint(m)); }
+// the four values of a word of int8: each byte with its sign bit flipped, put behind the exponent of 2^23, is 2^23 + 128 + q
+__device__ __forceinline__ void act8_value4(uint32_t w, float step, float* v)
+{
+    const uint32_t f = w ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (__uint_as_float(__byte_perm(f, 0x4B000000u, 0x7440 | i)) - 8388736.0f) * step;
+}
 
 // ---- gated activations
 // SLOPE: also act'(g).  FAST: exp and division to about 2 units in the last place of binary32, for results that are

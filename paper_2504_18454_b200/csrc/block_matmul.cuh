@@ -9,7 +9,7 @@
 // A pair of CTAs (a cluster, on two SMs) computes a 256 x 256 tile: each CTA stages its 128 rows of A and its half of
 // B by TMA, one thread of the leading CTA issues the pair's tcgen05.mma, and each CTA holds 128 x 256 binary32 sums in
 // its tensor memory, twice, so that the epilogue of one tile overlaps the products of the next.
-//   warp 0: TMA producer   warp 1: MMA issue (leading CTA)   warp 2: tensor memory   warps 4..11: epilogue
+//   warp 0: TMA producer   warp 1: MMA issue (leading CTA)   warp 2: tensor memory   warps 4..: epilogue
 // fp32 operands come as three bfloat16 parts each; the products of parts i, j with i + j <= 2 are summed as so many more
 // steps of the inner axis, the small ones first.
 #pragma once
@@ -23,12 +23,24 @@ namespace block {
 enum { MAT_PLAIN = 0, MAT_GATED = 1, MAT_HIDDEN = 2 };
 
 constexpr uint32_t kTileM = 256, kTileN = 256, kTileK = 64;
-constexpr uint32_t kStages = 6;
 constexpr uint32_t kOperandBytes = 128 * kTileK * 2;                    // a CTA's half of an operand's tile
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
-constexpr uint32_t kMatThreads = 384;
 constexpr uint32_t kBarrierBytes = 256;
-constexpr uint32_t kMatSmem = kStages * kStageBytes + kBarrierBytes + 1024;   // 1024: to start on a swizzle atom
+constexpr uint32_t kPiece = 8;                                          // fp32: steps of kTileK between two roundings to binary32
+
+// Shared memory and warps of a kernel.  bfloat16: 8 epilogue warps of 128 columns each, which pass their results (and, in
+// the hidden pass, gate and up, two blocks ahead) through blocks of 32 x 32 in shared memory.  fp32: 16 epilogue warps
+// of 64 columns, which hold their sums in registers.
+template <typename T, int MODE>
+struct MatShape {
+    static constexpr bool kWide = sizeof(T) == 4;
+    static constexpr uint32_t kEpilogue = kWide ? 16 : 8;
+    static constexpr uint32_t kThreads = 128 + 32 * kEpilogue;
+    static constexpr uint32_t kBlocks = kWide ? 0 : MODE == MAT_PLAIN ? 2 : MODE == MAT_GATED ? 3 : 6;   // of 2048 bytes, a warp
+    static constexpr uint32_t kStages = kWide || MODE == MAT_PLAIN ? 6 : MODE == MAT_GATED ? 5 : 4;
+    static constexpr uint32_t kSmem = kStages * kStageBytes + kEpilogue * kBlocks * 2048 + kBarrierBytes + 1024;   // 1024: to start on a swizzle atom
+    static_assert(kSmem <= 232448, "shared memory of a CTA");
+};
 constexpr uint32_t kMaxProblems = 4;
 constexpr unsigned long long kWaitLimitNs = 4000000000ull;              // how long a wait polls before it gives up
 
@@ -37,6 +49,7 @@ struct MatOut {
     int64_t w, r;                 // worker and row stride, elements
     int64_t part;                 // 0, or the stride between the three bfloat16 parts of an fp32 value
     int     wide;                 // rows start on 16-byte boundaries
+    uint32_t cols;                // columns that may be written: the workspace's rows have room behind their end
 };
 
 struct alignas(64) MatProblem {
@@ -135,6 +148,16 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32])
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16])
+{
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory operand descriptor, 128-byte swizzle.  kk contiguous: rows of 128 bytes, groups of eight 1024 apart.
@@ -152,38 +175,146 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ void lds128(uint32_t at, uint4& v)
+{
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+}
+__device__ __forceinline__ void sts128(uint32_t at, const uint4& v)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 
-// 32 consecutive values of a row, the first `n` of them inside the matrix
-__device__ __forceinline__ void store_row(float* p, const float (&v)[32], uint32_t n, bool wide)
+// A block of 32 rows (one a lane) by 32 columns that a warp passes through shared memory on its way between rows and
+// coalesced accesses.  ROW bytes a row; the 16-byte pieces of a row are permuted so that neither side has bank conflicts.
+template <int ROW>
+__device__ __forceinline__ uint32_t block_at(uint32_t base, uint32_t row, uint32_t piece)
 {
-    if (wide && n >= 32) {
+    constexpr uint32_t kPieces = ROW / 16;                // 8, 4 or 2
+    const uint32_t turn = kPieces == 8 ? row & 7 : kPieces == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
+    return base + row * ROW + ((piece ^ turn) << 4);
+}
+
+// Block -> matrix: `rows` (at most 32) rows and `cols` columns of it are inside.  E: the element type's size.
+template <int ROW, int E>
+__device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
+{
+    constexpr uint32_t kPieces = ROW / 16, kPer = 16 / E;
+    if (wide) {
+        const uint32_t piece = lane % kPieces;
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    } else {
+        for (uint32_t i = 0; i < kPieces; ++i) {
+            const uint32_t row = i * (32 / kPieces) + lane / kPieces;
+            uint4 v;
+            lds128(block_at<ROW>(base, row, piece), v);
+            if (row < rows && piece * kPer < cols) {
+                unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
+                if ((piece + 1) * kPer <= cols) {
+                    *reinterpret_cast<uint4*>(p) = v;
+                } else {                                  // the row ends inside these 16 bytes
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) if (i < n) p[i] = v[i];
+                    for (uint32_t j = 0; j < kPer; ++j)
+                        if (piece * kPer + j < cols) {
+                            if constexpr (E == 4) reinterpret_cast<uint32_t*>(p)[j] = w[j];
+                            else if constexpr (E == 2) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+                            else p[j] = (unsigned char)(w[j / 4] >> (8 * (j & 3)));
+                        }
+                }
+            }
+        }
+    } else if (lane < cols) {                             // one column a lane
+        for (uint32_t row = 0; row < rows; ++row) {
+            const uint32_t at = block_at<ROW>(base, row, lane / kPer) + (lane % kPer) * E;
+            unsigned char* p = to + (int64_t)row * row_bytes + lane * E;
+            if constexpr (E == 2) {
+                uint16_t v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+                *reinterpret_cast<uint16_t*>(p) = v;
+            } else {
+                uint32_t v;
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at));
+                *p = (unsigned char)v;
+            }
+        }
     }
 }
-__device__ __forceinline__ void store_row(bf16* p, const float (&v)[32], uint32_t n, bool wide)
+
+// Matrix -> block, asynchronously where the rows are aligned; zeros outside.  Complete after block_wait and __syncwarp.
+template <int ROW, int E>
+__device__ __forceinline__ void block_in(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
-    if (wide && n >= 32) {
+    constexpr uint32_t kPieces = ROW / 16, kPer = 16 / E;
+    if (wide) {
+        const uint32_t piece = lane % kPieces;
 #pragma unroll
-        for (int i = 0; i < 32; i += 8)
-            *reinterpret_cast<uint4*>(p + i) = make_uint4(pack2(v[i], v[i + 1]), pack2(v[i + 2], v[i + 3]), pack2(v[i + 4], v[i + 5]), pack2(v[i + 6], v[i + 7]));
+        for (uint32_t i = 0; i < kPieces; ++i) {
+            const uint32_t row = i * (32 / kPieces) + lane / kPieces;
+            const uint32_t n = row < rows && piece * kPer < cols ? (cols - piece * kPer < kPer ? cols - piece * kPer : kPer) * E : 0;
+            const unsigned char* p = n ? from + (int64_t)row * row_bytes + piece * 16 : from;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(block_at<ROW>(base, row, piece)), "l"(p), "r"(n) : "memory");
+        }
     } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) if (i < n) p[i] = __float2bfloat16_rn(v[i]);
+        for (uint32_t row = 0; row < 32; ++row) {
+            const uint32_t at = block_at<ROW>(base, row, lane / kPer) + (lane % kPer) * E;
+            const unsigned char* p = from + (int64_t)row * row_bytes + lane * E;
+            const bool on = row < rows && lane < cols;
+            if constexpr (E == 2) {
+                const uint16_t v = on ? *reinterpret_cast<const uint16_t*>(p) : (uint16_t)0;
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory");
+            } else {
+                const uint32_t v = on ? *p : 0u;
+                asm volatile("st.shared.u8 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+            }
+        }
     }
 }
-template <typename T>
-__device__ __forceinline__ void load_row(const T* p, float (&v)[32], uint32_t n, bool wide)
+__device__ __forceinline__ void block_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void block_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// A lane's row of a bfloat16 block
+__device__ __forceinline__ void row_put(uint32_t base, uint32_t lane, const float (&v)[32])
 {
-    if (wide && n >= 32) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 8) Vec<T, 8>::load(p + i, v + i);
-    } else {
+    for (int j = 0; j < 4; ++j)
+        sts128(block_at<64>(base, lane, j), make_uint4(pack2(v[8 * j], v[8 * j + 1]), pack2(v[8 * j + 2], v[8 * j + 3]),
+                                                       pack2(v[8 * j + 4], v[8 * j + 5]), pack2(v[8 * j + 6], v[8 * j + 7])));
+}
+__device__ __forceinline__ void row_get(uint32_t base, uint32_t lane, float (&v)[32])
+{
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = i < n ? to_f(p[i]) : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+        uint4 a;
+        lds128(block_at<64>(base, lane, j), a);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[8 * j + 2 * i] = __uint_as_float(w[i] << 16); v[8 * j + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    }
+}
+// ... of an int8 block: a lane's 32 columns are a group of a checkpoint
+__device__ __forceinline__ uint32_t row_put8(uint32_t base, uint32_t lane, const float (&v)[32])
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = act8_max(m, v[i]);
+    const uint32_t E = act8_exponent(m);
+    const float inv = act8_inverse(E);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = act8_quant4(v[16 * j + 4 * i], v[16 * j + 4 * i + 1], v[16 * j + 4 * i + 2], v[16 * j + 4 * i + 3], inv);
+        sts128(block_at<32>(base, lane, j), make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    return E;
+}
+__device__ __forceinline__ void row_get8(uint32_t base, uint32_t lane, uint32_t E, float (&v)[32])
+{
+    const float s = act8_step(E);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        uint4 a;
+        lds128(block_at<32>(base, lane, j), a);
+        act8_value4(a.x, s, v + 16 * j); act8_value4(a.y, s, v + 16 * j + 4); act8_value4(a.z, s, v + 16 * j + 8); act8_value4(a.w, s, v + 16 * j + 12);
     }
 }
 
@@ -198,83 +329,100 @@ __device__ __forceinline__ float next_part(float& v)
     return hi;
 }
 
-// An operand of the next product: bfloat16, or (part != 0) the three parts of an fp32 value.
-template <typename T>
-__device__ __forceinline__ void store_operand(const MatOut& o, int64_t at, float (&v)[32], uint32_t n)
+// fp32 results go out row by row, eight columns at a time (`n` of them inside): six times the products stand behind each.
+__device__ __forceinline__ void store8(float* p, const float* v, uint32_t n, bool wide)
 {
-    bf16* p = static_cast<bf16*>(o.p) + at;
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int part = 0; part < 3; ++part) {
-            float hi[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) hi[i] = next_part(v[i]);
-            store_row(p + part * o.part, hi, n, o.wide);
-        }
-    } else {
-        store_row(p, v, n, o.wide);
-    }
-}
-
-__device__ __forceinline__ void store_act8(const MatOut& q, const MatOut& e, int64_t qo, int64_t eo, const float (&v)[32], uint32_t n)
-{
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) m = max(m, i < n ? __float_as_uint(v[i]) & 0x7FFFFFFFu : 0u);
-    const uint32_t E = act8_exponent(m);
-    const float inv = act8_inverse(E);
-    int8_t* p = static_cast<int8_t*>(q.p) + qo;
-    if (q.wide && n >= 32) {
-#pragma unroll
-        for (int i = 0; i < 32; i += 16) {
-            uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < 16; ++j) w[j / 4] |= ((uint32_t)act8_quant(v[i + j], inv) & 0xFFu) << (8 * (j & 3));
-            *reinterpret_cast<uint4*>(p + i) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+    if (wide && n >= 8) {
+        Vec<float, 8>::store(p, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) if (i < n) p[i] = (int8_t)act8_quant(v[i], inv);
+        for (int i = 0; i < 8; ++i) if (i < n) p[i] = v[i];
     }
-    static_cast<uint8_t*>(e.p)[eo] = (uint8_t)E;
 }
-
-__device__ __forceinline__ void load_act8(const MatOut& q, const MatOut& e, int64_t qo, int64_t eo, float (&v)[32], uint32_t n)
+__device__ __forceinline__ void load8(const float* p, float* v, uint32_t n, bool wide)
 {
-    const float s = act8_step(static_cast<const uint8_t*>(e.p)[eo]);
-    const int8_t* p = static_cast<const int8_t*>(q.p) + qo;
-    if (q.wide && n >= 32) {
-#pragma unroll
-        for (int i = 0; i < 32; i += 16) {
-            const uint4 a = __ldg(reinterpret_cast<const uint4*>(p + i));
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int j = 0; j < 16; ++j) v[i + j] = (float)(int8_t)(w[j / 4] >> (8 * (j & 3))) * s;
-        }
+    if (wide && n >= 8) {
+        Vec<float, 8>::load(p, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = i < n ? (float)p[i] * s : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
     }
 }
+__device__ __forceinline__ void store8_parts(const MatOut& o, int64_t at, float* v)
+{
+    bf16* p = static_cast<bf16*>(o.p) + at;               // the workspace: rows are padded to eight columns
+#pragma unroll
+    for (int part = 0; part < 3; ++part) {
+        float hi[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) hi[i] = next_part(v[i]);
+        Vec<bf16, 8>::store(p + part * o.part, hi);
+    }
+}
+__device__ __forceinline__ void store8_act8(const MatOut& q, int64_t at, const float* v, float inv, uint32_t n)
+{
+    int8_t* p = static_cast<int8_t*>(q.p) + at;
+    const uint32_t w[2] = {act8_quant4(v[0], v[1], v[2], v[3], inv), act8_quant4(v[4], v[5], v[6], v[7], inv)};
+    if (q.wide && n >= 8) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < n) p[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
+    }
+}
+__device__ __forceinline__ void load8_act8(const MatOut& q, int64_t at, float* v, float step, uint32_t n)
+{
+    const int8_t* p = static_cast<const int8_t*>(q.p) + at;
+    uint32_t w[2] = {0, 0};
+    if (q.wide && n >= 8) {
+        const uint2 a = __ldg(reinterpret_cast<const uint2*>(p));
+        w[0] = a.x; w[1] = a.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < n) w[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+    }
+    act8_value4(w[0], step, v);
+    act8_value4(w[1], step, v + 4);
+}
 
-// v <- act(v) * u  (gate/up);  dh, g, u -> dg, du, h  (hidden).  bfloat16 results take the fast exponential.
-template <int ACT, bool FAST>
-__device__ __forceinline__ void gate_row(float (&g)[32], const float (&u)[32])
+// g <- act(g) * u  (gate/up);  dh, g, u -> h, dg, du  (hidden).  bfloat16 results take the fast exponential.
+template <int ACT, bool FAST, int N>
+__device__ __forceinline__ void gate_row(float* g, const float* u)
 {
     float unused;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) g[i] = act<ACT, false, FAST>(g[i], unused) * u[i];
+    for (int i = 0; i < N; ++i) g[i] = act<ACT, false, FAST>(g[i], unused) * u[i];
 }
-template <int ACT, bool FAST>
-__device__ __forceinline__ void hidden_row(float (&dh)[32], float (&g)[32], float (&u)[32])
+template <int ACT, bool FAST, int N>
+__device__ __forceinline__ void hidden_row(float* dh, float* g, float* u)
 {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
+    for (int i = 0; i < N; ++i) {
         float slope;
         const float a = act<ACT, true, FAST>(g[i], slope), d = dh[i];
         g[i] = d * u[i] * slope;                                        // dg
         dh[i] = a * u[i];                                               // h
         u[i] = d * a;                                                   // du
+    }
+}
+template <bool FAST, int N>
+__device__ __forceinline__ void gate_by(int kind, float* g, const float* u)
+{
+    switch (kind) {
+        case PALSGD_ACT_SILU: gate_row<PALSGD_ACT_SILU, FAST, N>(g, u); break;
+        case PALSGD_ACT_GELU: gate_row<PALSGD_ACT_GELU, FAST, N>(g, u); break;
+        case PALSGD_ACT_GELU_TANH: gate_row<PALSGD_ACT_GELU_TANH, FAST, N>(g, u); break;
+        default: gate_row<PALSGD_ACT_RELU, FAST, N>(g, u);
+    }
+}
+template <bool FAST, int N>
+__device__ __forceinline__ void hidden_by(int kind, float* dh, float* g, float* u)
+{
+    switch (kind) {
+        case PALSGD_ACT_SILU: hidden_row<PALSGD_ACT_SILU, FAST, N>(dh, g, u); break;
+        case PALSGD_ACT_GELU: hidden_row<PALSGD_ACT_GELU, FAST, N>(dh, g, u); break;
+        case PALSGD_ACT_GELU_TANH: hidden_row<PALSGD_ACT_GELU_TANH, FAST, N>(dh, g, u); break;
+        default: hidden_row<PALSGD_ACT_RELU, FAST, N>(dh, g, u);
     }
 }
 
@@ -294,19 +442,35 @@ __device__ __forceinline__ Tile tile_at(const MatLaunch& a, uint32_t t)
 
 __device__ __forceinline__ uint32_t pairs_of(const MatProblem& p) { return p.a_parts == 1 ? p.b_parts : p.b_parts == 1 ? p.a_parts : 6; }
 
-template <typename T, int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatThreads, 1) mat_kernel(const __grid_constant__ MatLaunch a)
+// The inner axis of a tile in pieces, each a sum of its own in tensor memory: f(segment, first step, end, last piece).
+// bfloat16: one piece a segment, joined in tensor memory.  fp32: kPiece steps (with all their parts), joined in registers
+// with rounding to nearest -- the tensor cores cut off what an addition does not hold, which over long sums adds up
+// (measured over 4096 steps of the inner axis in one piece: 4.4e-6 of the result's norm).
+template <typename T, typename F>
+__device__ __forceinline__ bool for_pieces(const MatProblem& p, F&& f)
 {
+    const uint32_t steps = (p.Kd + kTileK - 1) / kTileK, piece = sizeof(T) == 4 ? kPiece : steps;
+    for (uint32_t seg = 0; seg < p.n_seg; ++seg)
+        for (uint32_t k = 0; k < steps; k += piece)
+            if (!f(seg, k, k + piece < steps ? k + piece : steps)) return false;
+    return true;
+}
+
+template <typename T, int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::kThreads, 1) mat_kernel(const __grid_constant__ MatLaunch a)
+{
+    using Shape = MatShape<T, MODE>;
+    constexpr uint32_t kStages = Shape::kStages;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_addr(smem_raw) + 1023) & ~1023u;
-    const uint32_t bars = base + kStages * kStageBytes;
+    const uint32_t blocks = base + kStages * kStageBytes, bars = blocks + Shape::kEpilogue * Shape::kBlocks * 2048;
     const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16, tmem_at = acc_empty + 16;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < kStages; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); }
-        for (uint32_t s = 0; s < 2; ++s) { bar_init(acc_full + 8 * s, 1); bar_init(acc_empty + 8 * s, 16); }
+        for (uint32_t s = 0; s < 2; ++s) { bar_init(acc_full + 8 * s, 1); bar_init(acc_empty + 8 * s, 2 * Shape::kEpilogue); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -327,18 +491,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatThreads, 1) mat_
             for (uint32_t t = pair; ok && t < a.tiles; t += pairs) {
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
-                const uint32_t am = tl.m0 + rank * 128;
-                const uint32_t bn = MODE == MAT_GATED ? tl.n0 : tl.n0 + rank * 128;
-                for (uint32_t seg = 0; ok && seg < p.n_seg; ++seg) {
+                const uint32_t am = tl.m0 + rank * 128, bn = MODE == MAT_GATED ? tl.n0 : tl.n0 + rank * 128;
+                ok = for_pieces<T>(p, [&](uint32_t seg, uint32_t from, uint32_t to) {
                     const uint32_t bi = MODE == MAT_GATED ? rank : seg;
                     const uint32_t aw = p.a_one[seg] ? 0 : tl.worker, bw = p.b_one[bi] ? 0 : tl.worker;
-                    for (int sum = 2; ok && sum >= 0; --sum)
-                        for (int pa = 0; ok && pa <= sum; ++pa) {
+                    for (int sum = sizeof(T) == 4 ? 2 : 0; sum >= 0; --sum)
+                        for (int pa = 0; pa <= sum; ++pa) {
                             const int pb = sum - pa;
                             if (pa >= p.a_parts || pb >= p.b_parts) continue;
-                            for (uint32_t k = 0; k < p.Kd; k += kTileK) {
-                                if (!bar_wait(empty + 8 * s, phase ^ 1, a.gave_up)) { ok = false; break; }
-                                const uint32_t fb = in_cta(full + 8 * s, 0);
+                            for (uint32_t i = from; i < to; ++i) {
+                                if (!bar_wait(empty + 8 * s, phase ^ 1, a.gave_up)) return false;
+                                const uint32_t k = i * kTileK, fb = in_cta(full + 8 * s, 0);
                                 if (rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);
                                 const uint32_t da = base + s * kStageBytes, db = da + kOperandBytes;
                                 if (p.a_mn) {
@@ -357,7 +520,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatThreads, 1) mat_
                                 if (++s == kStages) { s = 0; phase ^= 1; }
                             }
                         }
-                }
+                    return true;
+                });
             }
             // every stage that was filled is drained before the CTA may leave: no copy or arrival is under way then
             for (uint32_t i = 0; i < used; ++i) {
@@ -370,102 +534,243 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatThreads, 1) mat_
         if (rank == 0 && lane == 0) {
             uint32_t s = 0, phase = 0, it = 0;
             bool ok = true;
-            for (uint32_t t = pair; ok && t < a.tiles; t += pairs, ++it) {
+            for (uint32_t t = pair; ok && t < a.tiles; t += pairs) {
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
-                const uint32_t steps = p.n_seg * pairs_of(p) * ((p.Kd + kTileK - 1) / kTileK);
+                const uint32_t n_pairs = pairs_of(p);
                 // binary32 sums; bfloat16 operands; majors; N / 8; M / 16
                 const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((kTileN / 8) << 17) | ((kTileM / 16) << 24);
-                const uint32_t acc = it & 1, d = tmem + acc * kTileN;
                 const uint64_t da = operand_desc(base, p.a_mn), db = operand_desc(base + kOperandBytes, p.b_mn);
                 const uint32_t sa = p.a_mn ? 2048 / 16 : 32 / 16, sb = p.b_mn ? 2048 / 16 : 32 / 16;
-                if (!bar_wait(acc_empty + 8 * acc, (it >> 1 & 1) ^ 1, a.gave_up)) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (uint32_t k = 0; k < steps; ++k) {
-                    if (!bar_wait(full + 8 * s, phase, a.gave_up)) { ok = false; break; }
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                ok = for_pieces<T>(p, [&](uint32_t seg, uint32_t from, uint32_t to) {
+                    const uint32_t acc = it & 1, d = tmem + acc * kTileN;
+                    const bool begins = sizeof(T) == 4 || seg == 0, ends = sizeof(T) == 4 || seg + 1 == p.n_seg;
+                    if (begins) {
+                        if (!bar_wait(acc_empty + 8 * acc, (it >> 1 & 1) ^ 1, a.gave_up)) return false;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    }
+                    const uint32_t steps = n_pairs * (to - from);
+                    for (uint32_t k = 0; k < steps; ++k) {
+                        if (!bar_wait(full + 8 * s, phase, a.gave_up)) return false;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                    for (uint32_t j = 0; j < kTileK / 16; ++j)
-                        mma(d, da + s * (kStageBytes / 16) + j * sa, db + s * (kStageBytes / 16) + j * sb, idesc, k > 0 || j > 0);
-                    mma_commit(empty + 8 * s);
-                    if (++s == kStages) { s = 0; phase ^= 1; }
-                }
-                if (ok) mma_commit(acc_full + 8 * acc);
+                        for (uint32_t j = 0; j < kTileK / 16; ++j)
+                            mma(d, da + s * (kStageBytes / 16) + j * sa, db + s * (kStageBytes / 16) + j * sb, idesc, !begins || k > 0 || j > 0);
+                        mma_commit(empty + 8 * s);
+                        if (++s == kStages) { s = 0; phase ^= 1; }
+                    }
+                    if (ends) { mma_commit(acc_full + 8 * acc); ++it; }
+                    return true;
+                });
             }
         }
     } else if (warp >= 4) {
-        const uint32_t quad = warp & 3, half = (warp - 4) >> 2;           // tensor memory rows of 32; half of the columns
+        const uint32_t quad = warp & 3, part = (warp - 4) >> 2;           // tensor memory rows of 32; share of the columns
         uint32_t it = 0;
-        for (uint32_t t = pair; t < a.tiles; t += pairs, ++it) {
-            const Tile tl = tile_at<MODE>(a, t);
-            const MatProblem& p = *tl.p;
-            const uint32_t acc = it & 1, src = tmem + acc * kTileN + (quad << 21);
-            const uint32_t m = tl.m0 + rank * 128 + quad * 32 + lane;
-            const bool row = m < p.M;
-            const bool ok = bar_wait(acc_full + 8 * acc, it >> 1 & 1, a.gave_up);
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+        auto acc_wait = [&]() {                                           // the next sum is complete
+            __syncwarp();
+            const bool ok = bar_wait(acc_full + 8 * (it & 1), it >> 1 & 1, a.gave_up);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            constexpr uint32_t kChunks = MODE == MAT_GATED ? 2 : 4;
-#pragma unroll 1
-            for (uint32_t c = 0; c < kChunks; ++c) {
-                const uint32_t col = (half * kChunks + c) * 32, n = tl.n0 + col;
-                const bool on = row && n < p.N;
-                const uint32_t left = p.N - n;
-                float v[32], u[32];
-                tmem_load32(src + col, v);
-                if constexpr (MODE == MAT_GATED) tmem_load32(src + kTileN / 2 + col, u);
-                tmem_load_wait();
-                if (on) {
-                const int64_t w = tl.worker;
-                const int64_t at = w * p.out[0].w + (int64_t)m * p.out[0].r + n;
-                if constexpr (MODE == MAT_PLAIN) {
-                    store_row(static_cast<T*>(p.out[0].p) + at, v, left, p.out[0].wide);
-                } else {
-                    const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
-                    const int64_t geo = w * a.gate_e.w + (int64_t)m * a.gate_e.r + n / 32, ueo = w * a.up_e.w + (int64_t)m * a.up_e.r + n / 32;
-                    constexpr bool kFast = sizeof(T) == 2;
-                    if constexpr (MODE == MAT_GATED) {
-                        if (a.save == PALSGD_SAVE_FULL) {
-                            store_row(static_cast<T*>(a.gate.p) + go, v, left, a.gate.wide);
-                            store_row(static_cast<T*>(a.up.p) + uo, u, left, a.up.wide);
-                        } else if (a.save == PALSGD_SAVE_8BIT) {
-                            store_act8(a.gate, a.gate_e, go, geo, v, left);
-                            store_act8(a.up, a.up_e, uo, ueo, u, left);
-                        }
-                        switch (a.act) {
-                            case PALSGD_ACT_SILU: gate_row<PALSGD_ACT_SILU, kFast>(v, u); break;
-                            case PALSGD_ACT_GELU: gate_row<PALSGD_ACT_GELU, kFast>(v, u); break;
-                            case PALSGD_ACT_GELU_TANH: gate_row<PALSGD_ACT_GELU_TANH, kFast>(v, u); break;
-                            default: gate_row<PALSGD_ACT_RELU, kFast>(v, u);
-                        }
-                        store_operand<T>(p.out[0], at, v, left);
-                    } else {
-                        float g[32];
-                        if (a.save == PALSGD_SAVE_FULL) {
-                            load_row(static_cast<const T*>(a.gate.p) + go, g, left, a.gate.wide);
-                            load_row(static_cast<const T*>(a.up.p) + uo, u, left, a.up.wide);
-                        } else {
-                            load_act8(a.gate, a.gate_e, go, geo, g, left);
-                            load_act8(a.up, a.up_e, uo, ueo, u, left);
-                        }
-                        switch (a.act) {
-                            case PALSGD_ACT_SILU: hidden_row<PALSGD_ACT_SILU, kFast>(v, g, u); break;
-                            case PALSGD_ACT_GELU: hidden_row<PALSGD_ACT_GELU, kFast>(v, g, u); break;
-                            case PALSGD_ACT_GELU_TANH: hidden_row<PALSGD_ACT_GELU_TANH, kFast>(v, g, u); break;
-                            default: hidden_row<PALSGD_ACT_RELU, kFast>(v, g, u);
-                        }
-                        store_operand<T>(p.out[0], at, g, left);
-                        store_operand<T>(p.out[1], at, u, left);
-                        store_operand<T>(p.out[2], at, v, left);
-                    }
-                }
-                }
-                __syncwarp();                                             // the next load from tensor memory is the whole warp's
-            }
+            return __all_sync(0xFFFFFFFFu, ok);
+        };
+        auto acc_read = [&]() {                                           // ... and has been read
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive_at(in_cta(acc_empty + 8 * acc, 0));
+            if (lane == 0) bar_arrive_at(in_cta(acc_empty + 8 * (it & 1), 0));
+            ++it;
+        };
+        const int64_t gate_e_r = a.gate_e.r, up_e_r = a.up_e.r;
+        if constexpr (!Shape::kWide) {
+            // ---- bfloat16: blocks of 32 columns
+            constexpr uint32_t kChunks = MODE == MAT_GATED ? 2 : 4;
+            const uint32_t mine = blocks + (warp - 4) * Shape::kBlocks * 2048;
+            uint32_t ge = 0, ue = 0;                                      // hidden, 8 bits: exponents of the block under way
+            // hidden: gate and up of block c of a tile into block set `set`
+            auto fetch = [&](const Tile& tl, uint32_t c, uint32_t set) {
+                const uint32_t m = tl.m0 + rank * 128 + quad * 32, n = tl.n0 + (part * kChunks + c) * 32;
+                const uint32_t M = tl.p->M, N = tl.p->N;
+                const uint32_t rows = m < M ? min(M - m, 32u) : 0, cols = n < N ? N - n : 0;
+                const int64_t w = tl.worker;
+                const uint32_t gb = mine + set * 3 * 2048, ub = gb + 2048;
+                const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
+                if (a.save == PALSGD_SAVE_8BIT) {
+                    block_in<32, 1>(gb, static_cast<const unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
+                    block_in<32, 1>(ub, static_cast<const unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
+                    const bool on = lane < rows && cols;
+                    ge = on ? static_cast<const uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * gate_e_r + n / 32] : 0u;
+                    ue = on ? static_cast<const uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] : 0u;
+                } else {
+                    block_in<64, 2>(gb, static_cast<const unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
+                    block_in<64, 2>(ub, static_cast<const unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
+                }
+                block_commit();
+            };
+            uint32_t set = 0;
+            if constexpr (MODE == MAT_HIDDEN) { if (pair < a.tiles) fetch(tile_at<MODE>(a, pair), 0, 0); }
+            for (uint32_t t = pair; t < a.tiles; t += pairs) {
+                const Tile tl = tile_at<MODE>(a, t);
+                const MatProblem& p = *tl.p;
+                const uint32_t src = tmem + (it & 1) * kTileN + (quad << 21);
+                const uint32_t m = tl.m0 + rank * 128 + quad * 32, rows = m < p.M ? min(p.M - m, 32u) : 0;
+                const int64_t w = tl.worker;
+                if (!acc_wait()) break;
+#pragma unroll 1
+                for (uint32_t c = 0; c < kChunks; ++c) {
+                    const uint32_t col = (part * kChunks + c) * 32, n = tl.n0 + col;
+                    const uint32_t cols = n < p.N ? p.N - n : 0;
+                    float v[32], u[32];
+                    tmem_load32(src + col, v);
+                    if constexpr (MODE == MAT_GATED) tmem_load32(src + kTileN / 2 + col, u);
+                    tmem_load_wait();
+                    if (c + 1 == kChunks) acc_read();
+                    const int64_t at = 2 * (w * p.out[0].w + (int64_t)m * p.out[0].r + n), step = 2 * p.out[0].r;
+                    const uint32_t room = n < p.out[0].cols ? p.out[0].cols - n : 0;
+                    if constexpr (MODE == MAT_PLAIN) {
+                        const uint32_t b = mine + (c & 1) * 2048;
+                        row_put(b, lane, v);
+                        __syncwarp();
+                        block_out<64, 2>(b, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, p.out[0].wide, lane);
+                        __syncwarp();
+                    } else if constexpr (MODE == MAT_GATED) {
+                        const uint32_t gb = mine, ub = mine + 2048, hb = mine + 4096;
+                        const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
+                        if (a.save == PALSGD_SAVE_FULL) {
+                            row_put(gb, lane, v);
+                            row_put(ub, lane, u);
+                        } else if (a.save == PALSGD_SAVE_8BIT) {
+                            const uint32_t eg = row_put8(gb, lane, v), eu = row_put8(ub, lane, u);
+                            if (lane < rows && cols) {
+                                static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * gate_e_r + n / 32] = (uint8_t)eg;
+                                static_cast<uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] = (uint8_t)eu;
+                            }
+                        }
+                        gate_by<true, 32>(a.act, v, u);
+                        row_put(hb, lane, v);
+                        __syncwarp();
+                        if (a.save == PALSGD_SAVE_FULL) {
+                            block_out<64, 2>(gb, static_cast<unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
+                            block_out<64, 2>(ub, static_cast<unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
+                        } else if (a.save == PALSGD_SAVE_8BIT) {
+                            block_out<32, 1>(gb, static_cast<unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
+                            block_out<32, 1>(ub, static_cast<unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
+                        }
+                        block_out<64, 2>(hb, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
+                        __syncwarp();
+                    } else {
+                        const uint32_t gb = mine + set * 3 * 2048, ub = gb + 2048, hb = ub + 2048;
+                        const uint32_t eg = ge, eu = ue;
+                        // the next block: of this tile, or the first of the warp's next tile
+                        if (c + 1 < kChunks) fetch(tl, c + 1, set ^ 1);
+                        else if (t + pairs < a.tiles) fetch(tile_at<MODE>(a, t + pairs), 0, set ^ 1);
+                        else block_commit();
+                        block_wait<1>();                                  // all but the next block's
+                        __syncwarp();
+                        float g[32];
+                        if (a.save == PALSGD_SAVE_8BIT) { row_get8(gb, lane, eg, g); row_get8(ub, lane, eu, u); }
+                        else { row_get(gb, lane, g); row_get(ub, lane, u); }
+                        __syncwarp();
+                        hidden_by<true, 32>(a.act, v, g, u);
+                        row_put(gb, lane, g);
+                        row_put(ub, lane, u);
+                        row_put(hb, lane, v);
+                        __syncwarp();
+                        block_out<64, 2>(gb, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
+                        block_out<64, 2>(ub, static_cast<unsigned char*>(p.out[1].p) + at, step, rows, room, 1, lane);
+                        block_out<64, 2>(hb, static_cast<unsigned char*>(p.out[2].p) + at, step, rows, room, 1, lane);
+                        __syncwarp();
+                        set ^= 1;
+                    }
+                }
+            }
+        } else {
+            // ---- fp32: sums of 64 columns in registers (gate/up: 32 of each)
+            for (uint32_t t = pair; t < a.tiles; t += pairs) {
+                const Tile tl = tile_at<MODE>(a, t);
+                const MatProblem& p = *tl.p;
+                const uint32_t m = tl.m0 + rank * 128 + quad * 32 + lane;
+                const int64_t w = tl.worker;
+                const uint32_t col[2] = {MODE == MAT_GATED ? part * 32 : part * 64, MODE == MAT_GATED ? kTileN / 2 + part * 32 : part * 64 + 32};
+                float sum[64];
+#pragma unroll
+                for (int i = 0; i < 64; ++i) sum[i] = 0.0f;
+                const bool ok = for_pieces<T>(p, [&](uint32_t, uint32_t, uint32_t) {
+                    const uint32_t src = tmem + (it & 1) * kTileN + (quad << 21);
+                    if (!acc_wait()) return false;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float v[16];
+                        tmem_load16(src + col[q / 2] + (q & 1) * 16, v);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[q * 16 + i] += v[i];
+                    }
+                    acc_read();
+                    return true;
+                });
+                if (!ok) break;
+                // (nothing below is a whole warp's: rows outside have no columns, and no thread leaves the common path)
+#pragma unroll
+                for (int c = 0; c < (MODE == MAT_GATED ? 1 : 2); ++c) {
+                    const uint32_t n = tl.n0 + col[c];
+                    if (m >= p.M || n >= p.N) continue;
+                    const int64_t at = w * p.out[0].w + (int64_t)m * p.out[0].r + n;
+                    const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
+                    const int64_t geo = w * a.gate_e.w + (int64_t)m * gate_e_r + n / 32, ueo = w * a.up_e.w + (int64_t)m * up_e_r + n / 32;
+                    const bool eight = a.save == PALSGD_SAVE_8BIT;
+                    float gs = 0.0f, us = 0.0f;                           // steps of the groups, or one over them
+                    if constexpr (MODE == MAT_GATED) {
+                        if (eight) {
+                            float gm = 0.0f, um = 0.0f;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) { gm = act8_max(gm, sum[i]); um = act8_max(um, sum[32 + i]); }
+                            const uint32_t eg = act8_exponent(gm), eu = act8_exponent(um);
+                            static_cast<uint8_t*>(a.gate_e.p)[geo] = (uint8_t)eg;
+                            static_cast<uint8_t*>(a.up_e.p)[ueo] = (uint8_t)eu;
+                            gs = act8_inverse(eg); us = act8_inverse(eu);
+                        }
+                    } else if constexpr (MODE == MAT_HIDDEN) {
+                        if (eight) {
+                            gs = act8_step(static_cast<const uint8_t*>(a.gate_e.p)[geo]);
+                            us = act8_step(static_cast<const uint8_t*>(a.up_e.p)[ueo]);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        if (n + j >= p.N) continue;
+                        const uint32_t left = p.N - n - j;
+                        float* v = sum + 32 * c + j;
+                        if constexpr (MODE == MAT_PLAIN) {
+                            store8(static_cast<float*>(p.out[0].p) + at + j, v, left, p.out[0].wide);
+                        } else if constexpr (MODE == MAT_GATED) {
+                            float* u = sum + 32 + j;
+                            if (a.save == PALSGD_SAVE_FULL) {
+                                store8(static_cast<float*>(a.gate.p) + go + j, v, left, a.gate.wide);
+                                store8(static_cast<float*>(a.up.p) + uo + j, u, left, a.up.wide);
+                            } else if (eight) {
+                                store8_act8(a.gate, go + j, v, gs, left);
+                                store8_act8(a.up, uo + j, u, us, left);
+                            }
+                            gate_by<false, 8>(a.act, v, u);
+                            store8_parts(p.out[0], at + j, v);
+                        } else {
+                            float g[8], u[8];
+                            if (eight) {
+                                load8_act8(a.gate, go + j, g, gs, left);
+                                load8_act8(a.up, uo + j, u, us, left);
+                            } else {
+                                load8(static_cast<const float*>(a.gate.p) + go + j, g, left, a.gate.wide);
+                                load8(static_cast<const float*>(a.up.p) + uo + j, u, left, a.up.wide);
+                            }
+                            hidden_by<false, 8>(a.act, v, g, u);
+                            store8_parts(p.out[0], at + j, g);
+                            store8_parts(p.out[1], at + j, u);
+                            store8_parts(p.out[2], at + j, v);
+                        }
+                    }
+                }
+            }
         }
+        if constexpr (MODE == MAT_HIDDEN && !Shape::kWide) block_wait<0>();
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

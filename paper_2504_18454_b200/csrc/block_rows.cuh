@@ -41,21 +41,18 @@ __global__ void __launch_bounds__(256) act8_kernel(const __grid_constant__ Act8A
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = 0.0f;
             if (on) Vec<T, V>::load(x + xo, v);
-            uint32_t m = 0;
+            float m = 0.0f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+            for (int j = 0; j < V; ++j) m = act8_max(m, v[j]);
 #pragma unroll
-            for (int s = kLanes / 2; s; s >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, s));
+            for (int s = kLanes / 2; s; s >>= 1) m = act8_max(m, __shfl_xor_sync(0xFFFFFFFFu, m, s));
             const uint32_t E = act8_exponent(m);
             const float inv = act8_inverse(E);
             if (on) {
                 if constexpr (V == 8) {
-                    uint32_t w[2] = {0, 0};
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j / 4] |= ((uint32_t)act8_quant(v[j], inv) & 0xFFu) << (8 * (j & 3));
-                    *reinterpret_cast<uint2*>(q + qo) = make_uint2(w[0], w[1]);
+                    *reinterpret_cast<uint2*>(q + qo) = make_uint2(act8_quant4(v[0], v[1], v[2], v[3], inv), act8_quant4(v[4], v[5], v[6], v[7], inv));
                 } else {
-                    q[qo] = (int8_t)act8_quant(v[0], inv);
+                    q[qo] = (int8_t)act8_quant4(v[0], 0.0f, 0.0f, 0.0f, inv);
                 }
                 if (threadIdx.x % kLanes == 0) e[eo] = (uint8_t)E;
             }
@@ -63,8 +60,8 @@ __global__ void __launch_bounds__(256) act8_kernel(const __grid_constant__ Act8A
             const float s = act8_step(e[eo]);
             if constexpr (V == 8) {
                 const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + qo));
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3))) * s;
+                act8_value4(w.x, s, v);
+                act8_value4(w.y, s, v + 4);
             } else {
                 v[0] = (float)q[qo] * s;
             }
