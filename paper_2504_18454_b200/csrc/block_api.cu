@@ -185,8 +185,18 @@ Device g_device[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_encode;
 std::mutex g_mutex;
 
-template <typename T, int MODE>
-cudaError_t allow_smem() { return cudaFuncSetAttribute(mat_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MatShape<T, MODE>::kSmem); }
+template <typename T, int MODE, int ACT>
+cudaError_t allow_smem() { return cudaFuncSetAttribute(mat_kernel<T, MODE, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MatShape<T, MODE>::kSmem); }
+
+template <typename T>
+cudaError_t allow_smem_all()
+{
+    const cudaError_t e[9] = {allow_smem<T, MAT_PLAIN, 0>(),
+                              allow_smem<T, MAT_GATED, 0>(), allow_smem<T, MAT_GATED, 1>(), allow_smem<T, MAT_GATED, 2>(), allow_smem<T, MAT_GATED, 3>(),
+                              allow_smem<T, MAT_HIDDEN, 0>(), allow_smem<T, MAT_HIDDEN, 1>(), allow_smem<T, MAT_HIDDEN, 2>(), allow_smem<T, MAT_HIDDEN, 3>()};
+    for (cudaError_t r : e) if (r != cudaSuccess) return r;
+    return cudaSuccess;
+}
 
 int device_of(Device& out)
 {
@@ -207,12 +217,8 @@ int device_of(Device& out)
         }
         void* p = nullptr;
         e = cudaGetSymbolAddress(&p, g_gave_up);
-        if (e == cudaSuccess) e = allow_smem<float, MAT_PLAIN>();
-        if (e == cudaSuccess) e = allow_smem<float, MAT_GATED>();
-        if (e == cudaSuccess) e = allow_smem<float, MAT_HIDDEN>();
-        if (e == cudaSuccess) e = allow_smem<bf16, MAT_PLAIN>();
-        if (e == cudaSuccess) e = allow_smem<bf16, MAT_GATED>();
-        if (e == cudaSuccess) e = allow_smem<bf16, MAT_HIDDEN>();
+        if (e == cudaSuccess) e = allow_smem_all<float>();
+        if (e == cudaSuccess) e = allow_smem_all<bf16>();
         if (e != cudaSuccess) return palsgd_block_cuda_fail((int)e, "matrix kernel set-up");
         d.gave_up = static_cast<unsigned int*>(p);
         d.sms = sm_count();
@@ -316,21 +322,41 @@ int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, c
     return PALSGD_OK;
 }
 
+template <typename T, int MODE, int ACT>
+void launch_mat(const MatLaunch& L, uint32_t pairs, cudaStream_t st)
+{
+    mat_kernel<T, MODE, ACT><<<2 * pairs, MatShape<T, MODE>::kThreads, MatShape<T, MODE>::kSmem, st>>>(L);
+}
+
+template <typename T, int MODE>
+void launch_mat(const MatLaunch& L, int act, uint32_t pairs, cudaStream_t st)
+{
+    if constexpr (MODE == MAT_PLAIN) {
+        launch_mat<T, MODE, 0>(L, pairs, st);
+    } else {
+        switch (act) {
+            case PALSGD_ACT_SILU: launch_mat<T, MODE, PALSGD_ACT_SILU>(L, pairs, st); break;
+            case PALSGD_ACT_GELU: launch_mat<T, MODE, PALSGD_ACT_GELU>(L, pairs, st); break;
+            case PALSGD_ACT_GELU_TANH: launch_mat<T, MODE, PALSGD_ACT_GELU_TANH>(L, pairs, st); break;
+            default: launch_mat<T, MODE, PALSGD_ACT_RELU>(L, pairs, st);
+        }
+    }
+}
+
 template <int MODE>
-int run_mat(MatLaunch& L, int32_t prec, const Device& d, cudaStream_t st)
+int run_mat(MatLaunch& L, const palsgd_ffn_shape* s, const Device& d, cudaStream_t st)
 {
     if (L.tiles == 0) return PALSGD_OK;
     L.gave_up = d.gave_up;
     const uint32_t pairs = (uint32_t)(d.sms / 2) < L.tiles ? (uint32_t)(d.sms / 2) : L.tiles;
-    if (prec == PALSGD_PREC_FP32) mat_kernel<float, MODE><<<2 * pairs, MatShape<float, MODE>::kThreads, MatShape<float, MODE>::kSmem, st>>>(L);
-    else mat_kernel<bf16, MODE><<<2 * pairs, MatShape<bf16, MODE>::kThreads, MatShape<bf16, MODE>::kSmem, st>>>(L);
+    if (s->precision == PALSGD_PREC_FP32) launch_mat<float, MODE>(L, s->activation, pairs, st);
+    else launch_mat<bf16, MODE>(L, s->activation, pairs, st);
     return launched("matrix kernel");
 }
 
 void set_saved(MatLaunch& L, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e, const palsgd_mat* up_e)
 {
     L.save = s->save;
-    L.act = s->activation;
     if (s->save == PALSGD_SAVE_NONE) return;
     const size_t es = s->save == PALSGD_SAVE_8BIT ? 1 : elem(s->precision);
     L.gate = out_of(gate, s->d_ff, es);
@@ -519,8 +545,8 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
     BLOCK_TRY(add_problem(down, M, D, F, s->K, &oh, nullptr, false, &od, nullptr, false, kTileN));
     down.p[0].out[0] = out_of(y, D, es);
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
-    BLOCK_TRY(run_mat<MAT_GATED>(gated, s->precision, dev, st));
-    return run_mat<MAT_PLAIN>(down, s->precision, dev, st);
+    BLOCK_TRY(run_mat<MAT_GATED>(gated, s, dev, st));
+    return run_mat<MAT_PLAIN>(down, s, dev, st);
 }
 
 extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* dy_, const palsgd_mat* x_, const palsgd_mat* x_e_,
@@ -596,8 +622,8 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     BLOCK_TRY(add_problem(grads, D, F, M, s->K, &ody, nullptr, true, &hid[2], nullptr, true, kTileN));
     grads.p[grads.n_problems - 1].out[0] = out_of(dw_down, F, es);
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
-    BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s->precision, dev, st));
-    return run_mat<MAT_PLAIN>(grads, s->precision, dev, st);
+    BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s, dev, st));
+    return run_mat<MAT_PLAIN>(grads, s, dev, st);
 }
 
 extern "C" int palsgd_block_status(void* stream)

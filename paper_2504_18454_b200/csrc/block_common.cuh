@@ -175,5 +175,44 @@ __device__ __forceinline__ float act(float g, float& slope)
     }
 }
 
+// The same for two values at a time, to a few units in the last place of binary32: for results that are rounded to
+// bfloat16.  2^x and 1/x are the units' own approximations, subnormal results flushed to zero.
+__device__ __forceinline__ float fast_exp2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float fast_inverse(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ f2 f2_same(float v) { return f2_of(v, v); }
+__device__ __forceinline__ f2 f2_add(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+// 1 / (1 + 2^z)
+__device__ __forceinline__ f2 f2_logistic(f2 z)
+{
+    float a, b;
+    f2_get(z, a, b);
+    f2_get(f2_add(f2_of(fast_exp2(a), fast_exp2(b)), f2_same(1.0f)), a, b);
+    return f2_of(fast_inverse(a), fast_inverse(b));
+}
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ f2 act2(f2 g, f2& slope)
+{
+    if constexpr (ACT == PALSGD_ACT_SILU) {
+        const f2 s = f2_logistic(f2_mul(g, f2_same(-1.4426950408889634f)));
+        const f2 a = f2_mul(g, s);
+        if constexpr (SLOPE) slope = f2_fma(a, f2_fma(s, f2_same(-1.0f), f2_same(1.0f)), s);
+        return a;
+    } else if constexpr (ACT == PALSGD_ACT_GELU_TANH) {
+        const float c = 1.5957691216057308f;                     // 2 sqrt(2/pi)
+        const f2 gg = f2_mul(g, g);
+        const f2 s = f2_logistic(f2_mul(f2_mul(g, f2_same(-1.4426950408889634f * c)), f2_fma(gg, f2_same(0.044715f), f2_same(1.0f))));
+        const f2 a = f2_mul(g, s);
+        if constexpr (SLOPE)
+            slope = f2_fma(f2_mul(a, f2_fma(s, f2_same(-1.0f), f2_same(1.0f))), f2_fma(gg, f2_same(0.134145f * c), f2_same(c)), s);
+        return a;
+    } else {
+        float x, y, sx = 0.0f, sy = 0.0f;
+        f2_get(g, x, y);
+        const float ax = act<ACT, SLOPE, true>(x, sx), ay = act<ACT, SLOPE, true>(y, sy);
+        if constexpr (SLOPE) slope = f2_of(sx, sy);
+        return f2_of(ax, ay);
+    }
+}
+
 }  // namespace block
 }  // namespace palsgd

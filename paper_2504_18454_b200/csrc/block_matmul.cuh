@@ -63,7 +63,7 @@ struct alignas(64) MatProblem {
 struct MatLaunch {
     MatProblem p[kMaxProblems];
     uint32_t n_problems, tiles;
-    int      act, save;
+    int      save;
     MatOut   gate, up;            // saved (gate/up pass) or read (hidden pass)
     MatOut   gate_e, up_e;
     unsigned int* gave_up;
@@ -279,19 +279,19 @@ __device__ __forceinline__ void row_put(uint32_t base, uint32_t lane, const floa
         sts128(block_at<64>(base, lane, j), make_uint4(pack2(v[8 * j], v[8 * j + 1]), pack2(v[8 * j + 2], v[8 * j + 3]),
                                                        pack2(v[8 * j + 4], v[8 * j + 5]), pack2(v[8 * j + 6], v[8 * j + 7])));
 }
-__device__ __forceinline__ void row_get(uint32_t base, uint32_t lane, float (&v)[32])
+// ... as pairs of floats, eight columns of it
+__device__ __forceinline__ void row_put8(uint32_t base, uint32_t lane, int j, const f2 (&v)[4])
 {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint4 a;
-        lds128(block_at<64>(base, lane, j), a);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[8 * j + 2 * i] = __uint_as_float(w[i] << 16); v[8 * j + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-    }
+    sts128(block_at<64>(base, lane, j), make_uint4(f2_narrow(v[0]), f2_narrow(v[1]), f2_narrow(v[2]), f2_narrow(v[3])));
+}
+__device__ __forceinline__ void row_get8(uint32_t base, uint32_t lane, int j, f2 (&v)[4])
+{
+    uint4 a;
+    lds128(block_at<64>(base, lane, j), a);
+    v[0] = f2_wide(a.x); v[1] = f2_wide(a.y); v[2] = f2_wide(a.z); v[3] = f2_wide(a.w);
 }
 // ... of an int8 block: a lane's 32 columns are a group of a checkpoint
-__device__ __forceinline__ uint32_t row_put8(uint32_t base, uint32_t lane, const float (&v)[32])
+__device__ __forceinline__ uint32_t row_put_act8(uint32_t base, uint32_t lane, const float (&v)[32])
 {
     float m = 0.0f;
 #pragma unroll
@@ -307,15 +307,15 @@ __device__ __forceinline__ uint32_t row_put8(uint32_t base, uint32_t lane, const
     }
     return E;
 }
-__device__ __forceinline__ void row_get8(uint32_t base, uint32_t lane, uint32_t E, float (&v)[32])
+__device__ __forceinline__ void row_get_act8(uint32_t base, uint32_t lane, int j, float step, f2 (&v)[4])
 {
-    const float s = act8_step(E);
+    uint2 a;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a.x), "=r"(a.y) : "r"(block_at<32>(base, lane, j >> 1) + (j & 1) * 8));
+    float f[8];
+    act8_value4(a.x, step, f);
+    act8_value4(a.y, step, f + 4);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        uint4 a;
-        lds128(block_at<32>(base, lane, j), a);
-        act8_value4(a.x, s, v + 16 * j); act8_value4(a.y, s, v + 16 * j + 4); act8_value4(a.z, s, v + 16 * j + 8); act8_value4(a.w, s, v + 16 * j + 12);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = f2_of(f[2 * i], f[2 * i + 1]);
 }
 
 // The next of the three bfloat16 parts of an fp32 value; v becomes the rest, exactly.  A finite value past the largest
@@ -385,44 +385,24 @@ __device__ __forceinline__ void load8_act8(const MatOut& q, int64_t at, float* v
     act8_value4(w[1], step, v + 4);
 }
 
-// g <- act(g) * u  (gate/up);  dh, g, u -> h, dg, du  (hidden).  bfloat16 results take the fast exponential.
-template <int ACT, bool FAST, int N>
-__device__ __forceinline__ void gate_row(float* g, const float* u)
+// fp32, eight columns: g <- act(g) * u  (gate/up);  dh, g, u -> h, dg, du  (hidden)
+template <int ACT>
+__device__ __forceinline__ void gate8(float* g, const float* u)
 {
     float unused;
 #pragma unroll
-    for (int i = 0; i < N; ++i) g[i] = act<ACT, false, FAST>(g[i], unused) * u[i];
+    for (int i = 0; i < 8; ++i) g[i] = act<ACT, false, false>(g[i], unused) * u[i];
 }
-template <int ACT, bool FAST, int N>
-__device__ __forceinline__ void hidden_row(float* dh, float* g, float* u)
+template <int ACT>
+__device__ __forceinline__ void hidden8(float* dh, float* g, float* u)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < 8; ++i) {
         float slope;
-        const float a = act<ACT, true, FAST>(g[i], slope), d = dh[i];
+        const float a = act<ACT, true, false>(g[i], slope), d = dh[i];
         g[i] = d * u[i] * slope;                                        // dg
         dh[i] = a * u[i];                                               // h
         u[i] = d * a;                                                   // du
-    }
-}
-template <bool FAST, int N>
-__device__ __forceinline__ void gate_by(int kind, float* g, const float* u)
-{
-    switch (kind) {
-        case PALSGD_ACT_SILU: gate_row<PALSGD_ACT_SILU, FAST, N>(g, u); break;
-        case PALSGD_ACT_GELU: gate_row<PALSGD_ACT_GELU, FAST, N>(g, u); break;
-        case PALSGD_ACT_GELU_TANH: gate_row<PALSGD_ACT_GELU_TANH, FAST, N>(g, u); break;
-        default: gate_row<PALSGD_ACT_RELU, FAST, N>(g, u);
-    }
-}
-template <bool FAST, int N>
-__device__ __forceinline__ void hidden_by(int kind, float* dh, float* g, float* u)
-{
-    switch (kind) {
-        case PALSGD_ACT_SILU: hidden_row<PALSGD_ACT_SILU, FAST, N>(dh, g, u); break;
-        case PALSGD_ACT_GELU: hidden_row<PALSGD_ACT_GELU, FAST, N>(dh, g, u); break;
-        case PALSGD_ACT_GELU_TANH: hidden_row<PALSGD_ACT_GELU_TANH, FAST, N>(dh, g, u); break;
-        default: hidden_row<PALSGD_ACT_RELU, FAST, N>(dh, g, u);
     }
 }
 
@@ -456,7 +436,8 @@ __device__ __forceinline__ bool for_pieces(const MatProblem& p, F&& f)
     return true;
 }
 
-template <typename T, int MODE>
+// (The activation is a parameter of the template: with all four in one kernel the epilogue outgrew the instruction cache.)
+template <typename T, int MODE, int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::kThreads, 1) mat_kernel(const __grid_constant__ MatLaunch a)
 {
     using Shape = MatShape<T, MODE>;
@@ -638,14 +619,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                             row_put(gb, lane, v);
                             row_put(ub, lane, u);
                         } else if (a.save == PALSGD_SAVE_8BIT) {
-                            const uint32_t eg = row_put8(gb, lane, v), eu = row_put8(ub, lane, u);
+                            const uint32_t eg = row_put_act8(gb, lane, v), eu = row_put_act8(ub, lane, u);
                             if (lane < rows && cols) {
                                 static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * gate_e_r + n / 32] = (uint8_t)eg;
                                 static_cast<uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] = (uint8_t)eu;
                             }
                         }
-                        gate_by<true, 32>(a.act, v, u);
-                        row_put(hb, lane, v);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            f2 h[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                f2 unused;
+                                h[i] = f2_mul(act2<ACT, false>(f2_of(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]), unused), f2_of(u[8 * j + 2 * i], u[8 * j + 2 * i + 1]));
+                            }
+                            row_put8(hb, lane, j, h);
+                        }
                         __syncwarp();
                         if (a.save == PALSGD_SAVE_FULL) {
                             block_out<64, 2>(gb, static_cast<unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
@@ -665,14 +654,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                         else block_commit();
                         block_wait<1>();                                  // all but the next block's
                         __syncwarp();
-                        float g[32];
-                        if (a.save == PALSGD_SAVE_8BIT) { row_get8(gb, lane, eg, g); row_get8(ub, lane, eu, u); }
-                        else { row_get(gb, lane, g); row_get(ub, lane, u); }
-                        __syncwarp();
-                        hidden_by<true, 32>(a.act, v, g, u);
-                        row_put(gb, lane, g);
-                        row_put(ub, lane, u);
-                        row_put(hb, lane, v);
+                        const bool eight = a.save == PALSGD_SAVE_8BIT;
+                        const float gs = act8_step(eg), us = act8_step(eu);
+                        f2 g[4][4], q[4][4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (eight) { row_get_act8(gb, lane, j, gs, g[j]); row_get_act8(ub, lane, j, us, q[j]); }
+                            else { row_get8(gb, lane, j, g[j]); row_get8(ub, lane, j, q[j]); }
+                        }
+                        if (eight) __syncwarp();                          // rows of 8-bit blocks lie elsewhere than those written below
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            f2 dg[4], du[4], h[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                f2 slope;
+                                const f2 act = act2<ACT, true>(g[j][i], slope), d = f2_of(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]);
+                                dg[i] = f2_mul(f2_mul(d, q[j][i]), slope);
+                                du[i] = f2_mul(d, act);
+                                h[i] = f2_mul(act, q[j][i]);
+                            }
+                            row_put8(gb, lane, j, dg);
+                            row_put8(ub, lane, j, du);
+                            row_put8(hb, lane, j, h);
+                        }
                         __syncwarp();
                         block_out<64, 2>(gb, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
                         block_out<64, 2>(ub, static_cast<unsigned char*>(p.out[1].p) + at, step, rows, room, 1, lane);
@@ -750,7 +755,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                                 store8_act8(a.gate, go + j, v, gs, left);
                                 store8_act8(a.up, uo + j, u, us, left);
                             }
-                            gate_by<false, 8>(a.act, v, u);
+                            gate8<ACT>(v, u);
                             store8_parts(p.out[0], at + j, v);
                         } else {
                             float g[8], u[8];
@@ -761,7 +766,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                                 load8(static_cast<const float*>(a.gate.p) + go + j, g, left, a.gate.wide);
                                 load8(static_cast<const float*>(a.up.p) + uo + j, u, left, a.up.wide);
                             }
-                            hidden_by<false, 8>(a.act, v, g, u);
+                            hidden8<ACT>(v, g, u);
                             store8_parts(p.out[0], at + j, g);
                             store8_parts(p.out[1], at + j, u);
                             store8_parts(p.out[2], at + j, v);
