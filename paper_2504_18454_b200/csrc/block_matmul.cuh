@@ -9,7 +9,7 @@
 // A pair of CTAs (a cluster, on two SMs) computes a 256 x 256 tile: each CTA stages its 128 rows of A and its half of
 // B by TMA, one thread of the leading CTA issues the pair's tcgen05.mma, and each CTA holds 128 x 256 binary32 sums in
 // its tensor memory, twice, so that the epilogue of one tile overlaps the products of the next.
-//   warp 0: TMA producer   warp 1: MMA issue (leading CTA)   warp 2: tensor memory   warps 4..: epilogue
+//   warps 0, 3: TMA producers   warp 1: MMA issue (leading CTA)   warp 2: tensor memory   warps 4..: epilogue
 // fp32 operands come as three bfloat16 parts each; the products of parts i, j with i + j <= 2 are summed as so many more
 // steps of the inner axis, the small ones first.
 #pragma once
@@ -83,7 +83,7 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 }
 __device__ __forceinline__ void bar_arrive_at(uint32_t cluster_bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // A wait that always ends: false, and the device-wide note, if the barrier's phase does not complete.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, unsigned int* gave_up)
@@ -91,7 +91,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, unsigned
     unsigned long long start = 0;
     for (uint32_t i = 0;; ++i) {
         uint32_t done;
-        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
                      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
         if (done) return true;
         if ((i & 63) == 63) {                                           // the clock is slow to read: not at every poll
@@ -465,37 +465,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at));
 
-    if (warp == 0) {
+    if (warp == 0 || warp == 3) {
+        // producers: warp 0 brings A, warp 3 brings B (one thread that did both held the copy engine up: 410 ns a step of
+        // 32 KB, of which 120 its own)
         if (lane == 0) {
+            const bool is_b = warp == 3;
+            const uint32_t dst = base + (is_b ? kOperandBytes : 0), signal = in_cta(full, 0);
             uint32_t s = 0, phase = 0, used = 0;
             bool ok = true;
             for (uint32_t t = pair; ok && t < a.tiles; t += pairs) {
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
-                const uint32_t am = tl.m0 + rank * 128, bn = MODE == MAT_GATED ? tl.n0 : tl.n0 + rank * 128;
+                const uint32_t mn = is_b ? (MODE == MAT_GATED ? tl.n0 : tl.n0 + rank * 128) : tl.m0 + rank * 128;
+                const bool across = is_b ? p.b_mn : p.a_mn;
+                const int parts_a = p.a_parts, parts_b = p.b_parts;
                 ok = for_pieces<T>(p, [&](uint32_t seg, uint32_t from, uint32_t to) {
-                    const uint32_t bi = MODE == MAT_GATED ? rank : seg;
-                    const uint32_t aw = p.a_one[seg] ? 0 : tl.worker, bw = p.b_one[bi] ? 0 : tl.worker;
+                    const uint32_t i = is_b && MODE == MAT_GATED ? rank : seg;
+                    const CUtensorMap* const map = is_b ? &p.B[i] : &p.A[i];
+                    const uint32_t w = (is_b ? p.b_one[i] : p.a_one[i]) ? 0 : tl.worker;
                     for (int sum = sizeof(T) == 4 ? 2 : 0; sum >= 0; --sum)
                         for (int pa = 0; pa <= sum; ++pa) {
-                            const int pb = sum - pa;
-                            if (pa >= p.a_parts || pb >= p.b_parts) continue;
-                            for (uint32_t i = from; i < to; ++i) {
+                            if (pa >= parts_a || sum - pa >= parts_b) continue;
+                            const uint32_t part = is_b ? sum - pa : pa;
+                            for (uint32_t k = from * kTileK; k < to * kTileK; k += kTileK) {
                                 if (!bar_wait(empty + 8 * s, phase ^ 1, a.gave_up)) return false;
-                                const uint32_t k = i * kTileK, fb = in_cta(full + 8 * s, 0);
-                                if (rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);
-                                const uint32_t da = base + s * kStageBytes, db = da + kOperandBytes;
-                                if (p.a_mn) {
-                                    tma_load(&p.A[seg], da, fb, am, k, aw, pa);
-                                    tma_load(&p.A[seg], da + 8192, fb, am + 64, k, aw, pa);
+                                if (!is_b && rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);
+                                const uint32_t to_s = dst + s * kStageBytes, bar = signal + 8 * s;
+                                if (across) {
+                                    tma_load(map, to_s, bar, mn, k, w, part);
+                                    tma_load(map, to_s + 8192, bar, mn + 64, k, w, part);
                                 } else {
-                                    tma_load(&p.A[seg], da, fb, k, am, aw, pa);
-                                }
-                                if (p.b_mn) {
-                                    tma_load(&p.B[bi], db, fb, bn, k, bw, pb);
-                                    tma_load(&p.B[bi], db + 8192, fb, bn + 64, k, bw, pb);
-                                } else {
-                                    tma_load(&p.B[bi], db, fb, k, bn, bw, pb);
+                                    tma_load(map, to_s, bar, k, mn, w, part);
                                 }
                                 if (used < kStages) ++used;
                                 if (++s == kStages) { s = 0; phase ^= 1; }
