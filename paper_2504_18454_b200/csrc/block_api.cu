@@ -301,15 +301,23 @@ MatOut out_of(const palsgd_mat* m, uint64_t cols, size_t es)
 }
 MatOut out_of(const Operand& o) { return MatOut{const_cast<void*>(o.p), o.w, o.r, o.part, 1, (uint32_t)o.r}; }
 
+Divisor divisor(uint32_t d)
+{
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+}
+
 // One product appended to a launch; B1/A1: the second segment, or (gate/up) the up weights as B1.
 int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, const Operand* A0, const Operand* A1, bool amn,
                 const Operand* B0, const Operand* B1, bool bmn, uint32_t n_step)
 {
     MatProblem& p = L.p[L.n_problems++];
     p.M = (uint32_t)M; p.N = (uint32_t)N; p.Kd = (uint32_t)Kd;
-    p.tiles_m = (uint32_t)ceil_div(M, kTileM); p.tiles_n = (uint32_t)ceil_div(N, n_step);
-    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n * K;
-    if (L.tiles + tiles > 0x7FFFFFFFull) return PALSGD_EUNSUPPORTED;
+    const uint64_t down = ceil_div(M, kTileM), across = ceil_div(N, n_step), tiles = down * across * K;
+    if (down * across > 0x7FFFFFFFull || L.tiles + tiles > 0x7FFFFFFFull) return PALSGD_EUNSUPPORTED;
+    p.tiles_m = divisor((uint32_t)down);
+    p.per_worker = divisor((uint32_t)(down * across));
     p.tiles = (uint32_t)tiles;
     L.tiles += p.tiles;
     p.n_seg = A1 ? 2 : 1;

@@ -28,16 +28,16 @@ constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr uint32_t kBarrierBytes = 256;
 constexpr uint32_t kPiece = 8;                                          // fp32: steps of kTileK between two roundings to binary32
 
-// Shared memory and warps of a kernel.  bfloat16: 8 epilogue warps of 128 columns each, which pass their results (and, in
-// the hidden pass, gate and up, two blocks ahead) through blocks of 32 x 32 in shared memory.  fp32: 16 epilogue warps
-// of 64 columns, which hold their sums in registers.
+// Shared memory and warps of a kernel: 16 epilogue warps of 64 columns each (8 of 128 took three times as long in the
+// hidden pass: two warps a scheduler do not cover each other's latencies).  bfloat16: they pass their results (and, in
+// the hidden pass, gate and up) through blocks of 32 x 32 in shared memory.  fp32: they hold their sums in registers.
 template <typename T, int MODE>
 struct MatShape {
     static constexpr bool kWide = sizeof(T) == 4;
-    static constexpr uint32_t kEpilogue = kWide ? 16 : 8;
+    static constexpr uint32_t kEpilogue = 16;
     static constexpr uint32_t kThreads = 128 + 32 * kEpilogue;
-    static constexpr uint32_t kBlocks = kWide ? 0 : MODE == MAT_PLAIN ? 2 : MODE == MAT_GATED ? 3 : 6;   // of 2048 bytes, a warp
-    static constexpr uint32_t kStages = kWide || MODE == MAT_PLAIN ? 6 : MODE == MAT_GATED ? 5 : 4;
+    static constexpr uint32_t kBlocks = kWide ? 0 : MODE == MAT_PLAIN ? 1 : 3;   // of 2048 bytes, a warp
+    static constexpr uint32_t kStages = kWide || MODE == MAT_PLAIN ? 6 : 4;
     static constexpr uint32_t kSmem = kStages * kStageBytes + kEpilogue * kBlocks * 2048 + kBarrierBytes + 1024;   // 1024: to start on a swizzle atom
     static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
@@ -52,9 +52,17 @@ struct MatOut {
     uint32_t cols;                // columns that may be written: the workspace's rows have room behind their end
 };
 
+// Division of t < 2^31 by a divisor d known on the host: with s = ceil(log2 d) and m = ceil(2^(31+s) / d) < 2^32, the
+// quotient is t m >> (31 + s) (m d exceeds 2^(31+s) by less than 2^s, and t times that stays below 2^(31+s)).
+struct Divisor {
+    uint32_t d, m, s;
+    __device__ __forceinline__ uint32_t of(uint32_t t) const { return (uint32_t)(((uint64_t)t * m) >> (31 + s)); }
+};
+
 struct alignas(64) MatProblem {
     CUtensorMap A[2], B[2];       // by segment; the gate/up pass: B[0] gate, B[1] up
-    uint32_t M, N, Kd, tiles_m, tiles_n, tiles;
+    uint32_t M, N, Kd, tiles;
+    Divisor  tiles_m, per_worker; // tiles down, tiles of one worker
     uint8_t  n_seg, a_parts, b_parts, a_mn, b_mn;
     uint8_t  a_one[2], b_one[2];  // all workers read one matrix
     MatOut   out[3];              // plain: the product; gate/up: h; hidden: dg, du, h
@@ -135,19 +143,6 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
     asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32])
-{
-    uint32_t r[32];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-                   "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-                   "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(addr));
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-}
 __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16])
 {
     uint32_t r[16];
@@ -157,6 +152,14 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16])
                  : "r"(addr));
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8])
+{
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -170,11 +173,6 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn)
 
 // ---------------------------------------------------------------------------------------------- epilogue memory access
 
-__device__ __forceinline__ uint32_t pack2(float a, float b)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
 __device__ __forceinline__ void lds128(uint32_t at, uint4& v)
 {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
@@ -196,33 +194,31 @@ __device__ __forceinline__ uint32_t block_at(uint32_t base, uint32_t row, uint32
 
 // Block -> matrix: `rows` (at most 32) rows and `cols` columns of it are inside.  E: the element type's size.
 template <int ROW, int E>
-__device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
+__device__ __noinline__ void block_out_edge(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
-    constexpr uint32_t kPieces = ROW / 16, kPer = 16 / E;
+    constexpr uint32_t kPer = 16 / E;
     if (wide) {
+        constexpr uint32_t kPieces = ROW / 16;
         const uint32_t piece = lane % kPieces;
-#pragma unroll
-        for (uint32_t i = 0; i < kPieces; ++i) {
-            const uint32_t row = i * (32 / kPieces) + lane / kPieces;
+#pragma unroll 1
+        for (uint32_t row = lane / kPieces; row < rows; row += 32 / kPieces) {
             uint4 v;
             lds128(block_at<ROW>(base, row, piece), v);
-            if (row < rows && piece * kPer < cols) {
-                unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
-                if ((piece + 1) * kPer <= cols) {
-                    *reinterpret_cast<uint4*>(p) = v;
-                } else {                                  // the row ends inside these 16 bytes
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
+            if ((piece + 1) * kPer <= cols) {
+                *reinterpret_cast<uint4*>(p) = v;
+            } else {                                      // the row ends inside these 16 bytes, or before them
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (uint32_t j = 0; j < kPer; ++j)
-                        if (piece * kPer + j < cols) {
-                            if constexpr (E == 4) reinterpret_cast<uint32_t*>(p)[j] = w[j];
-                            else if constexpr (E == 2) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-                            else p[j] = (unsigned char)(w[j / 4] >> (8 * (j & 3)));
-                        }
-                }
+                for (uint32_t j = 0; j < kPer; ++j)
+                    if (piece * kPer + j < cols) {
+                        if constexpr (E == 2) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+                        else p[j] = (unsigned char)(w[j / 4] >> (8 * (j & 3)));
+                    }
             }
         }
     } else if (lane < cols) {                             // one column a lane
+#pragma unroll 1
         for (uint32_t row = 0; row < rows; ++row) {
             const uint32_t at = block_at<ROW>(base, row, lane / kPer) + (lane % kPer) * E;
             unsigned char* p = to + (int64_t)row * row_bytes + lane * E;
@@ -238,24 +234,44 @@ __device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int6
         }
     }
 }
-
-// Matrix -> block, asynchronously where the rows are aligned; zeros outside.  Complete after block_wait and __syncwarp.
 template <int ROW, int E>
-__device__ __forceinline__ void block_in(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
+__device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
-    constexpr uint32_t kPieces = ROW / 16, kPer = 16 / E;
+    constexpr uint32_t kPieces = ROW / 16;
+    if (rows == 32 && cols >= 32 && wide) {               // the same for the whole warp
+        const uint32_t piece = lane % kPieces, row = lane / kPieces;
+        unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
+        const int64_t step = row_bytes * (32 / kPieces);
+        uint4 v[kPieces];
+#pragma unroll
+        for (uint32_t i = 0; i < kPieces; ++i) lds128(block_at<ROW>(base, i * (32 / kPieces) + row, piece), v[i]);
+#pragma unroll
+        for (uint32_t i = 0; i < kPieces; ++i) { *reinterpret_cast<uint4*>(p) = v[i]; p += step; }
+    } else if (rows && cols) {
+        block_out_edge<ROW, E>(base, to, row_bytes, rows, cols, wide, lane);
+    }
+}
+
+// Matrix -> block of 64-byte rows, asynchronously where the rows are aligned; zeros outside.  Complete after block_wait and
+// __syncwarp.  bfloat16 fills a row; int8 its second half, so that a lane can write its bfloat16 results over its row from
+// the front while it still reads.
+template <int E>
+__device__ __noinline__ void block_in_edge(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
+{
+    constexpr uint32_t kPieces = 2 * E, kPer = 16 / E, kFirst = E == 1 ? 2 : 0;
     if (wide) {
         const uint32_t piece = lane % kPieces;
-#pragma unroll
-        for (uint32_t i = 0; i < kPieces; ++i) {
-            const uint32_t row = i * (32 / kPieces) + lane / kPieces;
-            const uint32_t n = row < rows && piece * kPer < cols ? (cols - piece * kPer < kPer ? cols - piece * kPer : kPer) * E : 0;
+        const uint32_t inside = piece * kPer < cols ? (cols - piece * kPer < kPer ? cols - piece * kPer : kPer) * E : 0;
+#pragma unroll 1
+        for (uint32_t row = lane / kPieces; row < 32; row += 32 / kPieces) {
+            const uint32_t n = row < rows ? inside : 0;
             const unsigned char* p = n ? from + (int64_t)row * row_bytes + piece * 16 : from;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(block_at<ROW>(base, row, piece)), "l"(p), "r"(n) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(block_at<64>(base, row, kFirst + piece)), "l"(p), "r"(n) : "memory");
         }
     } else {
+#pragma unroll 1
         for (uint32_t row = 0; row < 32; ++row) {
-            const uint32_t at = block_at<ROW>(base, row, lane / kPer) + (lane % kPer) * E;
+            const uint32_t at = block_at<64>(base, row, kFirst + lane / kPer) + (lane % kPer) * E;
             const unsigned char* p = from + (int64_t)row * row_bytes + lane * E;
             const bool on = row < rows && lane < cols;
             if constexpr (E == 2) {
@@ -268,49 +284,46 @@ __device__ __forceinline__ void block_in(uint32_t base, const unsigned char* fro
         }
     }
 }
-__device__ __forceinline__ void block_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT> __device__ __forceinline__ void block_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-
-// A lane's row of a bfloat16 block
-__device__ __forceinline__ void row_put(uint32_t base, uint32_t lane, const float (&v)[32])
+template <int E>
+__device__ __forceinline__ void block_in(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
+    constexpr uint32_t kPieces = 2 * E, kFirst = E == 1 ? 2 : 0;
+    if (rows == 32 && cols >= 32 && wide) {
+        const uint32_t piece = lane % kPieces, row = lane / kPieces;
+        const unsigned char* p = from + (int64_t)row * row_bytes + piece * 16;
+        const int64_t step = row_bytes * (32 / kPieces);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        sts128(block_at<64>(base, lane, j), make_uint4(pack2(v[8 * j], v[8 * j + 1]), pack2(v[8 * j + 2], v[8 * j + 3]),
-                                                       pack2(v[8 * j + 4], v[8 * j + 5]), pack2(v[8 * j + 6], v[8 * j + 7])));
+        for (uint32_t i = 0; i < kPieces; ++i) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(block_at<64>(base, i * (32 / kPieces) + row, kFirst + piece)), "l"(p) : "memory");
+            p += step;
+        }
+    } else if (rows && cols) {                            // (a block that is all outside is not read)
+        block_in_edge<E>(base, from, row_bytes, rows, cols, wide, lane);
+    }
 }
-// ... as pairs of floats, eight columns of it
-__device__ __forceinline__ void row_put8(uint32_t base, uint32_t lane, int j, const f2 (&v)[4])
+__device__ __forceinline__ void block_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Eight columns of a lane's row of a bfloat16 block, as pairs of floats
+__device__ __forceinline__ void row_put(uint32_t base, uint32_t lane, uint32_t j, const f2 (&v)[4])
 {
     sts128(block_at<64>(base, lane, j), make_uint4(f2_narrow(v[0]), f2_narrow(v[1]), f2_narrow(v[2]), f2_narrow(v[3])));
 }
-__device__ __forceinline__ void row_get8(uint32_t base, uint32_t lane, int j, f2 (&v)[4])
+__device__ __forceinline__ void row_get(uint32_t base, uint32_t lane, uint32_t j, f2 (&v)[4])
 {
     uint4 a;
     lds128(block_at<64>(base, lane, j), a);
     v[0] = f2_wide(a.x); v[1] = f2_wide(a.y); v[2] = f2_wide(a.z); v[3] = f2_wide(a.w);
 }
-// ... of an int8 block: a lane's 32 columns are a group of a checkpoint
-__device__ __forceinline__ uint32_t row_put_act8(uint32_t base, uint32_t lane, const float (&v)[32])
+// ... of an 8-bit block: written in rows of 32 bytes, read where block_in puts it
+__device__ __forceinline__ void row_put_act8(uint32_t base, uint32_t lane, uint32_t j, float inv, const float (&v)[8])
 {
-    float m = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) m = act8_max(m, v[i]);
-    const uint32_t E = act8_exponent(m);
-    const float inv = act8_inverse(E);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = act8_quant4(v[16 * j + 4 * i], v[16 * j + 4 * i + 1], v[16 * j + 4 * i + 2], v[16 * j + 4 * i + 3], inv);
-        sts128(block_at<32>(base, lane, j), make_uint4(w[0], w[1], w[2], w[3]));
-    }
-    return E;
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(block_at<32>(base, lane, j >> 1) + (j & 1) * 8),
+                 "r"(act8_quant4(v[0], v[1], v[2], v[3], inv)), "r"(act8_quant4(v[4], v[5], v[6], v[7], inv)) : "memory");
 }
-__device__ __forceinline__ void row_get_act8(uint32_t base, uint32_t lane, int j, float step, f2 (&v)[4])
+__device__ __forceinline__ void row_get_act8(uint32_t base, uint32_t lane, uint32_t j, float step, f2 (&v)[4])
 {
     uint2 a;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a.x), "=r"(a.y) : "r"(block_at<32>(base, lane, j >> 1) + (j & 1) * 8));
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a.x), "=r"(a.y) : "r"(block_at<64>(base, lane, 2 + (j >> 1)) + (j & 1) * 8));
     float f[8];
     act8_value4(a.x, step, f);
     act8_value4(a.y, step, f + 4);
@@ -416,7 +429,7 @@ __device__ __forceinline__ Tile tile_at(const MatLaunch& a, uint32_t t)
     uint32_t i = 0;
     while (i + 1 < a.n_problems && t >= a.p[i].tiles) { t -= a.p[i].tiles; ++i; }
     const MatProblem& p = a.p[i];
-    const uint32_t per = p.tiles_m * p.tiles_n, w = t / per, r = t - w * per, m = r % p.tiles_m, n = r / p.tiles_m;
+    const uint32_t w = p.per_worker.of(t), r = t - w * p.per_worker.d, n = p.tiles_m.of(r), m = r - n * p.tiles_m.d;
     return Tile{w, m * kTileM, n * (MODE == MAT_GATED ? kTileN / 2 : kTileN), &p};
 }
 
@@ -562,32 +575,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
         };
         const int64_t gate_e_r = a.gate_e.r, up_e_r = a.up_e.r;
         if constexpr (!Shape::kWide) {
-            // ---- bfloat16: blocks of 32 columns
-            constexpr uint32_t kChunks = MODE == MAT_GATED ? 2 : 4;
+            // ---- bfloat16: blocks of 32 columns, eight at a time (in a loop: unrolled, they outgrow the instruction cache)
+            constexpr uint32_t kChunks = MODE == MAT_GATED ? 1 : 2;
             const uint32_t mine = blocks + (warp - 4) * Shape::kBlocks * 2048;
+            const bool eight = a.save == PALSGD_SAVE_8BIT;
             uint32_t ge = 0, ue = 0;                                      // hidden, 8 bits: exponents of the block under way
-            // hidden: gate and up of block c of a tile into block set `set`
-            auto fetch = [&](const Tile& tl, uint32_t c, uint32_t set) {
+            // hidden: gate and up of block c of a tile into the warp's first two blocks
+            auto fetch = [&](const Tile& tl, uint32_t c) {
                 const uint32_t m = tl.m0 + rank * 128 + quad * 32, n = tl.n0 + (part * kChunks + c) * 32;
                 const uint32_t M = tl.p->M, N = tl.p->N;
                 const uint32_t rows = m < M ? min(M - m, 32u) : 0, cols = n < N ? N - n : 0;
                 const int64_t w = tl.worker;
-                const uint32_t gb = mine + set * 3 * 2048, ub = gb + 2048;
                 const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
-                if (a.save == PALSGD_SAVE_8BIT) {
-                    block_in<32, 1>(gb, static_cast<const unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
-                    block_in<32, 1>(ub, static_cast<const unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
+                if (eight) {
+                    block_in<1>(mine, static_cast<const unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
+                    block_in<1>(mine + 2048, static_cast<const unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
                     const bool on = lane < rows && cols;
                     ge = on ? static_cast<const uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * gate_e_r + n / 32] : 0u;
                     ue = on ? static_cast<const uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] : 0u;
                 } else {
-                    block_in<64, 2>(gb, static_cast<const unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
-                    block_in<64, 2>(ub, static_cast<const unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
+                    block_in<2>(mine, static_cast<const unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
+                    block_in<2>(mine + 2048, static_cast<const unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
                 }
-                block_commit();
             };
-            uint32_t set = 0;
-            if constexpr (MODE == MAT_HIDDEN) { if (pair < a.tiles) fetch(tile_at<MODE>(a, pair), 0, 0); }
+            if constexpr (MODE == MAT_HIDDEN) { if (pair < a.tiles) fetch(tile_at<MODE>(a, pair), 0); }
             for (uint32_t t = pair; t < a.tiles; t += pairs) {
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
@@ -598,92 +609,107 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
 #pragma unroll 1
                 for (uint32_t c = 0; c < kChunks; ++c) {
                     const uint32_t col = (part * kChunks + c) * 32, n = tl.n0 + col;
-                    const uint32_t cols = n < p.N ? p.N - n : 0;
-                    float v[32], u[32];
-                    tmem_load32(src + col, v);
-                    if constexpr (MODE == MAT_GATED) tmem_load32(src + kTileN / 2 + col, u);
-                    tmem_load_wait();
-                    if (c + 1 == kChunks) acc_read();
+                    const uint32_t cols = n < p.N ? p.N - n : 0, room = n < p.out[0].cols ? p.out[0].cols - n : 0;
                     const int64_t at = 2 * (w * p.out[0].w + (int64_t)m * p.out[0].r + n), step = 2 * p.out[0].r;
-                    const uint32_t room = n < p.out[0].cols ? p.out[0].cols - n : 0;
+                    const uint32_t b0 = mine, b1 = mine + 2048, b2 = mine + 4096;
                     if constexpr (MODE == MAT_PLAIN) {
-                        const uint32_t b = mine + (c & 1) * 2048;
-                        row_put(b, lane, v);
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; j += 2) {
+                            float v[16];
+                            tmem_load16(src + col + 8 * j, v);
+                            tmem_load_wait();
+                            f2 y[2][4];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) y[i / 4][i % 4] = f2_of(v[2 * i], v[2 * i + 1]);
+                            row_put(b0, lane, j, y[0]);
+                            row_put(b0, lane, j + 1, y[1]);
+                        }
+                        if (c + 1 == kChunks) acc_read();
                         __syncwarp();
-                        block_out<64, 2>(b, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, p.out[0].wide, lane);
+                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, p.out[0].wide, lane);
                         __syncwarp();
                     } else if constexpr (MODE == MAT_GATED) {
-                        const uint32_t gb = mine, ub = mine + 2048, hb = mine + 4096;
-                        const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
-                        if (a.save == PALSGD_SAVE_FULL) {
-                            row_put(gb, lane, v);
-                            row_put(ub, lane, u);
-                        } else if (a.save == PALSGD_SAVE_8BIT) {
-                            const uint32_t eg = row_put_act8(gb, lane, v), eu = row_put_act8(ub, lane, u);
+                        float gi = 0.0f, ui = 0.0f;                       // one over the steps of the groups
+                        if (eight) {
+                            float gm = 0.0f, um = 0.0f;
+#pragma unroll 1
+                            for (uint32_t j = 0; j < 4; ++j) {
+                                float v[8], u[8];
+                                tmem_load8(src + col + 8 * j, v);
+                                tmem_load8(src + kTileN / 2 + col + 8 * j, u);
+                                tmem_load_wait();
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) { gm = act8_max(gm, v[i]); um = act8_max(um, u[i]); }
+                            }
+                            const uint32_t eg = act8_exponent(gm), eu = act8_exponent(um);
+                            gi = act8_inverse(eg); ui = act8_inverse(eu);
                             if (lane < rows && cols) {
                                 static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * gate_e_r + n / 32] = (uint8_t)eg;
                                 static_cast<uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] = (uint8_t)eu;
                             }
                         }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            f2 h[4];
+#pragma unroll 1
+                        for (uint32_t j = 0; j < 4; ++j) {
+                            float v[8], u[8];
+                            tmem_load8(src + col + 8 * j, v);
+                            tmem_load8(src + kTileN / 2 + col + 8 * j, u);
+                            tmem_load_wait();
+                            f2 g[4], q[4], h[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 f2 unused;
-                                h[i] = f2_mul(act2<ACT, false>(f2_of(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]), unused), f2_of(u[8 * j + 2 * i], u[8 * j + 2 * i + 1]));
+                                g[i] = f2_of(v[2 * i], v[2 * i + 1]);
+                                q[i] = f2_of(u[2 * i], u[2 * i + 1]);
+                                h[i] = f2_mul(act2<ACT, false>(g[i], unused), q[i]);
                             }
-                            row_put8(hb, lane, j, h);
+                            if (eight) { row_put_act8(b0, lane, j, gi, v); row_put_act8(b1, lane, j, ui, u); }
+                            else if (a.save == PALSGD_SAVE_FULL) { row_put(b0, lane, j, g); row_put(b1, lane, j, q); }
+                            row_put(b2, lane, j, h);
                         }
-                        __syncwarp();
-                        if (a.save == PALSGD_SAVE_FULL) {
-                            block_out<64, 2>(gb, static_cast<unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
-                            block_out<64, 2>(ub, static_cast<unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
-                        } else if (a.save == PALSGD_SAVE_8BIT) {
-                            block_out<32, 1>(gb, static_cast<unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
-                            block_out<32, 1>(ub, static_cast<unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
+                        acc_read();
+                        const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
+                        if (eight) {
+                            block_out<32, 1>(b0, static_cast<unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
+                            block_out<32, 1>(b1, static_cast<unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
+                        } else if (a.save == PALSGD_SAVE_FULL) {
+                            block_out<64, 2>(b0, static_cast<unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
+                            block_out<64, 2>(b1, static_cast<unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
                         }
-                        block_out<64, 2>(hb, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
+                        block_out<64, 2>(b2, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
                         __syncwarp();
                     } else {
-                        const uint32_t gb = mine + set * 3 * 2048, ub = gb + 2048, hb = ub + 2048;
-                        const uint32_t eg = ge, eu = ue;
-                        // the next block: of this tile, or the first of the warp's next tile
-                        if (c + 1 < kChunks) fetch(tl, c + 1, set ^ 1);
-                        else if (t + pairs < a.tiles) fetch(tile_at<MODE>(a, t + pairs), 0, set ^ 1);
-                        else block_commit();
-                        block_wait<1>();                                  // all but the next block's
+                        block_wait();
                         __syncwarp();
-                        const bool eight = a.save == PALSGD_SAVE_8BIT;
-                        const float gs = act8_step(eg), us = act8_step(eu);
-                        f2 g[4][4], q[4][4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (eight) { row_get_act8(gb, lane, j, gs, g[j]); row_get_act8(ub, lane, j, us, q[j]); }
-                            else { row_get8(gb, lane, j, g[j]); row_get8(ub, lane, j, q[j]); }
-                        }
-                        if (eight) __syncwarp();                          // rows of 8-bit blocks lie elsewhere than those written below
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            f2 dg[4], du[4], h[4];
+                        const float gs = act8_step(ge), us = act8_step(ue);
+#pragma unroll 1
+                        for (uint32_t j = 0; j < 4; ++j) {
+                            float v[8];
+                            f2 g[4], q[4], dg[4], du[4], h[4];
+                            tmem_load8(src + col + 8 * j, v);
+                            if (eight) { row_get_act8(b0, lane, j, gs, g); row_get_act8(b1, lane, j, us, q); }
+                            else { row_get(b0, lane, j, g); row_get(b1, lane, j, q); }
+                            tmem_load_wait();
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 f2 slope;
-                                const f2 act = act2<ACT, true>(g[j][i], slope), d = f2_of(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]);
-                                dg[i] = f2_mul(f2_mul(d, q[j][i]), slope);
-                                du[i] = f2_mul(d, act);
-                                h[i] = f2_mul(act, q[j][i]);
+                                const f2 ag = act2<ACT, true>(g[i], slope), d = f2_of(v[2 * i], v[2 * i + 1]);
+                                dg[i] = f2_mul(f2_mul(d, q[i]), slope);
+                                du[i] = f2_mul(d, ag);
+                                h[i] = f2_mul(ag, q[i]);
                             }
-                            row_put8(gb, lane, j, dg);
-                            row_put8(ub, lane, j, du);
-                            row_put8(hb, lane, j, h);
+                            row_put(b0, lane, j, dg);
+                            row_put(b1, lane, j, du);
+                            row_put(b2, lane, j, h);
                         }
+                        if (c + 1 == kChunks) acc_read();
                         __syncwarp();
-                        block_out<64, 2>(gb, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
-                        block_out<64, 2>(ub, static_cast<unsigned char*>(p.out[1].p) + at, step, rows, room, 1, lane);
-                        block_out<64, 2>(hb, static_cast<unsigned char*>(p.out[2].p) + at, step, rows, room, 1, lane);
+                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
+                        block_out<64, 2>(b1, static_cast<unsigned char*>(p.out[1].p) + at, step, rows, room, 1, lane);
+                        block_out<64, 2>(b2, static_cast<unsigned char*>(p.out[2].p) + at, step, rows, room, 1, lane);
                         __syncwarp();
-                        set ^= 1;
+                        // the next block: of this tile, or the first of the warp's next tile
+                        if (c + 1 < kChunks) fetch(tl, c + 1);
+                        else if (t + pairs < a.tiles) fetch(tile_at<MODE>(a, t + pairs), 0);
                     }
                 }
             }
@@ -775,7 +801,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 }
             }
         }
-        if constexpr (MODE == MAT_HIDDEN && !Shape::kWide) block_wait<0>();
+        if constexpr (MODE == MAT_HIDDEN && !Shape::kWide) block_wait();
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
