@@ -619,16 +619,27 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     BLOCK_TRY(add_problem(hidden, M, F, D, s->K, &ody, nullptr, false, &od, nullptr, true, kTileN));
     for (int i = 0; i < 3; ++i) hidden.p[0].out[i] = out_of(hid[i]);
     set_saved(hidden, s, gate, up, gate_e, up_e);
-    if (dx) {                                            // first: its tiles are the longest
+    // dx contracts over both halves of the hidden axis, the weight gradients over the tokens: the longer tiles first
+    const uint64_t long_x = 2 * ceil_div(F, kTileK) + kTileEnd, long_w = ceil_div(M, kTileK) + kTileEnd;
+    const bool x_first = long_x >= long_w;
+    auto add_x = [&]() -> int {
+        if (!dx) return PALSGD_OK;
         BLOCK_TRY(add_problem(grads, M, D, F, s->K, &hid[0], &hid[1], false, &og, &ou, true, kTileN));
-        grads.p[0].out[0] = out_of(dx, D, es);
-    }
-    BLOCK_TRY(add_problem(grads, F, D, M, s->K, &hid[0], nullptr, true, &ox, nullptr, true, kTileN));
-    grads.p[grads.n_problems - 1].out[0] = out_of(dw_gate, D, es);
-    BLOCK_TRY(add_problem(grads, F, D, M, s->K, &hid[1], nullptr, true, &ox, nullptr, true, kTileN));
-    grads.p[grads.n_problems - 1].out[0] = out_of(dw_up, D, es);
-    BLOCK_TRY(add_problem(grads, D, F, M, s->K, &ody, nullptr, true, &hid[2], nullptr, true, kTileN));
-    grads.p[grads.n_problems - 1].out[0] = out_of(dw_down, F, es);
+        grads.p[grads.n_problems - 1].out[0] = out_of(dx, D, es);
+        return PALSGD_OK;
+    };
+    auto add_w = [&]() -> int {
+        const palsgd_mat* w[3] = {dw_gate, dw_up, dw_down};
+        for (int i = 0; i < 3; ++i) {
+            BLOCK_TRY(add_problem(grads, i < 2 ? F : D, i < 2 ? D : F, M, s->K, i < 2 ? &hid[i] : &ody, nullptr, true, i < 2 ? &ox : &hid[2], nullptr, true, kTileN));
+            grads.p[grads.n_problems - 1].out[0] = out_of(w[i], i < 2 ? D : F, es);
+        }
+        return PALSGD_OK;
+    };
+    BLOCK_TRY(x_first ? add_x() : add_w());
+    grads.heavy = grads.tiles;
+    grads.lag = (uint32_t)(x_first ? long_x / long_w : long_w / long_x);
+    BLOCK_TRY(x_first ? add_w() : add_x());
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s, dev, st));
     return run_mat<MAT_PLAIN>(grads, s, dev, st);

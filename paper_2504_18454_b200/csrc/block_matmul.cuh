@@ -36,12 +36,13 @@ struct MatShape {
     static constexpr bool kWide = sizeof(T) == 4;
     static constexpr uint32_t kEpilogue = 16;
     static constexpr uint32_t kThreads = 128 + 32 * kEpilogue;
-    static constexpr uint32_t kBlocks = kWide ? 0 : MODE == MAT_PLAIN ? 1 : 3;   // of 2048 bytes, a warp
-    static constexpr uint32_t kStages = kWide || MODE == MAT_PLAIN ? 6 : 4;
+    static constexpr uint32_t kBlocks = kWide ? 0 : MODE == MAT_HIDDEN ? 2 : 1;   // of 2048 bytes, a warp
+    static constexpr uint32_t kStages = !kWide && MODE == MAT_HIDDEN ? 5 : 6;
     static constexpr uint32_t kSmem = kStages * kStageBytes + kEpilogue * kBlocks * 2048 + kBarrierBytes + 1024;   // 1024: to start on a swizzle atom
     static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
 constexpr uint32_t kMaxProblems = 4;
+constexpr uint32_t kTileEnd = 3;                                        // what a tile costs beside its steps, in steps
 constexpr unsigned long long kWaitLimitNs = 4000000000ull;              // how long a wait polls before it gives up
 
 struct MatOut {
@@ -70,7 +71,7 @@ struct alignas(64) MatProblem {
 
 struct MatLaunch {
     MatProblem p[kMaxProblems];
-    uint32_t n_problems, tiles;
+    uint32_t n_problems, tiles, heavy, lag;   // see Order
     int      save;
     MatOut   gate, up;            // saved (gate/up pass) or read (hidden pass)
     MatOut   gate_e, up_e;
@@ -161,6 +162,11 @@ __device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8])
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_store4(uint32_t addr, const uint32_t (&r)[4])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory operand descriptor, 128-byte swizzle.  kk contiguous: rows of 128 bytes, groups of eight 1024 apart.
@@ -315,7 +321,7 @@ __device__ __forceinline__ void row_get(uint32_t base, uint32_t lane, uint32_t j
     v[0] = f2_wide(a.x); v[1] = f2_wide(a.y); v[2] = f2_wide(a.z); v[3] = f2_wide(a.w);
 }
 // ... of an 8-bit block: written in rows of 32 bytes, read where block_in puts it
-__device__ __forceinline__ void row_put_act8(uint32_t base, uint32_t lane, uint32_t j, float inv, const float (&v)[8])
+__device__ __forceinline__ void row_put_act8(uint32_t base, uint32_t lane, uint32_t j, float inv, const float* v)
 {
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(block_at<32>(base, lane, j >> 1) + (j & 1) * 8),
                  "r"(act8_quant4(v[0], v[1], v[2], v[3], inv)), "r"(act8_quant4(v[4], v[5], v[6], v[7], inv)) : "memory");
@@ -421,6 +427,35 @@ __device__ __forceinline__ void hidden8(float* dh, float* g, float* u)
 
 // ---------------------------------------------------------------------------------------------- the kernel
 
+// The tiles of a launch in the order in which its pairs of CTAs take them up: first the `heavy` ones, then the rest.  The
+// heavy ones go round the pairs; where they do not come out even, the pairs that have one less take up light ones for as
+// long (`lag` of them fit beside a heavy one), so that all pairs end within a light tile of each other.  Every pair works
+// out its own tiles: a pair's step `j` among the light ones is preceded by those that the others take up before that time.
+// (Round and round alone left the tensor cores idle for a fifth of the backward pass of 8 workers, 768 x 2048.)
+struct Order {
+    uint32_t heavy, tiles, lag, pair, pairs, mine, more, j;
+    __device__ __forceinline__ Order(const MatLaunch& a, uint32_t pair_, uint32_t pairs_)
+        : heavy(a.heavy), tiles(a.tiles), lag(a.lag), pair(pair_), pairs(pairs_), j(0)
+    {
+        mine = heavy / pairs;
+        more = heavy - mine * pairs;                      // this many pairs have one more
+        mine += pair < more;
+    }
+    __device__ __forceinline__ uint32_t at(uint32_t i) const    // the pair's i-th tile; `tiles`: none
+    {
+        uint64_t t;
+        const uint64_t k = i - mine;
+        if (i < mine) t = pair + (uint64_t)i * pairs;
+        else if (more == 0) t = heavy + pair + k * pairs;
+        else if (pair >= more) t = heavy + (pairs - more) * k + (pair - more) + more * (k > lag ? k - lag : 0);
+        else t = heavy + more * k + pair + (pairs - more) * (k + lag + 1);
+        return t < tiles ? (uint32_t)t : tiles;
+    }
+    __device__ __forceinline__ uint32_t now() const { return at(j); }
+    __device__ __forceinline__ uint32_t then() const { return at(j + 1); }
+    __device__ __forceinline__ void next() { ++j; }
+};
+
 struct Tile { uint32_t worker, m0, n0; const MatProblem* p; };
 
 template <int MODE>
@@ -486,7 +521,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             const uint32_t dst = base + (is_b ? kOperandBytes : 0), signal = in_cta(full, 0);
             uint32_t s = 0, phase = 0, used = 0;
             bool ok = true;
-            for (uint32_t t = pair; ok && t < a.tiles; t += pairs) {
+            for (Order o(a, pair, pairs); ok && o.now() < a.tiles; o.next()) {
+                const uint32_t t = o.now();
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
                 const uint32_t mn = is_b ? (MODE == MAT_GATED ? tl.n0 : tl.n0 + rank * 128) : tl.m0 + rank * 128;
@@ -528,7 +564,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
         if (rank == 0 && lane == 0) {
             uint32_t s = 0, phase = 0, it = 0;
             bool ok = true;
-            for (uint32_t t = pair; ok && t < a.tiles; t += pairs) {
+            for (Order o(a, pair, pairs); ok && o.now() < a.tiles; o.next()) {
+                const uint32_t t = o.now();
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
                 const uint32_t n_pairs = pairs_of(p);
@@ -598,8 +635,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     block_in<2>(mine + 2048, static_cast<const unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
                 }
             };
-            if constexpr (MODE == MAT_HIDDEN) { if (pair < a.tiles) fetch(tile_at<MODE>(a, pair), 0); }
-            for (uint32_t t = pair; t < a.tiles; t += pairs) {
+            if constexpr (MODE == MAT_HIDDEN) { fetch(tile_at<MODE>(a, Order(a, pair, pairs).now()), 0); }
+            for (Order o(a, pair, pairs); o.now() < a.tiles; o.next()) {
+                const uint32_t t = o.now();
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
                 const uint32_t src = tmem + (it & 1) * kTileN + (quad << 21);
@@ -611,7 +649,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     const uint32_t col = (part * kChunks + c) * 32, n = tl.n0 + col;
                     const uint32_t cols = n < p.N ? p.N - n : 0, room = n < p.out[0].cols ? p.out[0].cols - n : 0;
                     const int64_t at = 2 * (w * p.out[0].w + (int64_t)m * p.out[0].r + n), step = 2 * p.out[0].r;
-                    const uint32_t b0 = mine, b1 = mine + 2048, b2 = mine + 4096;
+                    const uint32_t b0 = mine;
                     if constexpr (MODE == MAT_PLAIN) {
 #pragma unroll
                         for (uint32_t j = 0; j < 4; j += 2) {
@@ -648,38 +686,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                                 static_cast<uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] = (uint8_t)eu;
                             }
                         }
+                        // gate, up and h pass through one block, one after another (tensor memory is read again for each)
+                        if (a.save != PALSGD_SAVE_NONE) {
+#pragma unroll 1
+                            for (uint32_t which = 0; which < 2; ++which) {
+                                const MatOut& s = which ? a.up : a.gate;
+                                const float inv = which ? ui : gi;
+#pragma unroll
+                                for (uint32_t j = 0; j < 4; j += 2) {
+                                    float v[16];
+                                    tmem_load16(src + which * (kTileN / 2) + col + 8 * j, v);
+                                    tmem_load_wait();
+                                    if (eight) {
+                                        row_put_act8(b0, lane, j, inv, v);
+                                        row_put_act8(b0, lane, j + 1, inv, v + 8);
+                                    } else {
+                                        f2 y[2][4];
+#pragma unroll
+                                        for (int i = 0; i < 8; ++i) y[i / 4][i % 4] = f2_of(v[2 * i], v[2 * i + 1]);
+                                        row_put(b0, lane, j, y[0]);
+                                        row_put(b0, lane, j + 1, y[1]);
+                                    }
+                                }
+                                __syncwarp();
+                                const int64_t to = w * s.w + (int64_t)m * s.r + n;
+                                if (eight) block_out<32, 1>(b0, static_cast<unsigned char*>(s.p) + to, s.r, rows, cols, s.wide, lane);
+                                else block_out<64, 2>(b0, static_cast<unsigned char*>(s.p) + 2 * to, 2 * s.r, rows, cols, s.wide, lane);
+                                __syncwarp();
+                            }
+                        }
 #pragma unroll 1
                         for (uint32_t j = 0; j < 4; ++j) {
                             float v[8], u[8];
                             tmem_load8(src + col + 8 * j, v);
                             tmem_load8(src + kTileN / 2 + col + 8 * j, u);
                             tmem_load_wait();
-                            f2 g[4], q[4], h[4];
+                            f2 h[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 f2 unused;
-                                g[i] = f2_of(v[2 * i], v[2 * i + 1]);
-                                q[i] = f2_of(u[2 * i], u[2 * i + 1]);
-                                h[i] = f2_mul(act2<ACT, false>(g[i], unused), q[i]);
+                                h[i] = f2_mul(act2<ACT, false>(f2_of(v[2 * i], v[2 * i + 1]), unused), f2_of(u[2 * i], u[2 * i + 1]));
                             }
-                            if (eight) { row_put_act8(b0, lane, j, gi, v); row_put_act8(b1, lane, j, ui, u); }
-                            else if (a.save == PALSGD_SAVE_FULL) { row_put(b0, lane, j, g); row_put(b1, lane, j, q); }
-                            row_put(b2, lane, j, h);
+                            row_put(b0, lane, j, h);
                         }
                         acc_read();
-                        const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
-                        if (eight) {
-                            block_out<32, 1>(b0, static_cast<unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
-                            block_out<32, 1>(b1, static_cast<unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
-                        } else if (a.save == PALSGD_SAVE_FULL) {
-                            block_out<64, 2>(b0, static_cast<unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
-                            block_out<64, 2>(b1, static_cast<unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
-                        }
-                        block_out<64, 2>(b2, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
+                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
                         __syncwarp();
                     } else {
                         block_wait();
                         __syncwarp();
+                        const uint32_t b1 = mine + 2048;
                         const float gs = act8_step(ge), us = act8_step(ue);
 #pragma unroll 1
                         for (uint32_t j = 0; j < 4; ++j) {
@@ -699,23 +755,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                             }
                             row_put(b0, lane, j, dg);
                             row_put(b1, lane, j, du);
-                            row_put(b2, lane, j, h);
+                            // h waits its turn in tensor memory, over sums that have been read
+                            const uint32_t hw[4] = {f2_narrow(h[0]), f2_narrow(h[1]), f2_narrow(h[2]), f2_narrow(h[3])};
+                            tmem_store4(src + col + 4 * j, hw);
                         }
-                        if (c + 1 == kChunks) acc_read();
+                        tmem_store_wait();
                         __syncwarp();
                         block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
                         block_out<64, 2>(b1, static_cast<unsigned char*>(p.out[1].p) + at, step, rows, room, 1, lane);
-                        block_out<64, 2>(b2, static_cast<unsigned char*>(p.out[2].p) + at, step, rows, room, 1, lane);
+                        __syncwarp();
+                        {
+                            float h[16];
+                            tmem_load16(src + col, h);
+                            tmem_load_wait();
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                sts128(block_at<64>(b0, lane, j), make_uint4(__float_as_uint(h[4 * j]), __float_as_uint(h[4 * j + 1]), __float_as_uint(h[4 * j + 2]), __float_as_uint(h[4 * j + 3])));
+                        }
+                        if (c + 1 == kChunks) acc_read();
+                        __syncwarp();
+                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[2].p) + at, step, rows, room, 1, lane);
                         __syncwarp();
                         // the next block: of this tile, or the first of the warp's next tile
                         if (c + 1 < kChunks) fetch(tl, c + 1);
-                        else if (t + pairs < a.tiles) fetch(tile_at<MODE>(a, t + pairs), 0);
+                        else if (o.then() < a.tiles) fetch(tile_at<MODE>(a, o.then()), 0);
                     }
                 }
             }
         } else {
             // ---- fp32: sums of 64 columns in registers (gate/up: 32 of each)
-            for (uint32_t t = pair; t < a.tiles; t += pairs) {
+            for (Order o(a, pair, pairs); o.now() < a.tiles; o.next()) {
+                const uint32_t t = o.now();
                 const Tile tl = tile_at<MODE>(a, t);
                 const MatProblem& p = *tl.p;
                 const uint32_t m = tl.m0 + rank * 128 + quad * 32 + lane;
