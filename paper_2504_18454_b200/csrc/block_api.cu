@@ -266,7 +266,9 @@ Operand input_operand(Arena& ws, Stage& st, const palsgd_mat* m, const palsgd_ma
     o.one = copies == 1;
     StageItem& it = st.a.item[st.n++];
     it = StageItem{m->data, e ? static_cast<const uint8_t*>(e->data) : nullptr, w, m->row_stride, e ? e->worker_stride : 0, e ? e->row_stride : 0,
-                   static_cast<bf16*>(const_cast<void*>(o.p)), o.r, o.part, (uint32_t)rows, (uint32_t)cols, rows * (uint64_t)(o.r / 8), kind, copies};
+                   static_cast<bf16*>(const_cast<void*>(o.p)), o.r, o.part, (uint32_t)rows, (uint32_t)cols, rows * (uint64_t)(o.r / 8), kind, copies, 0};
+    const int unit = kind == STAGE_ACT8 ? 8 : 4;         // elements in the 8 or 16 bytes of a load
+    it.wide = aligned(m->data, kind == STAGE_ACT8 ? 8 : 16) && m->row_stride % unit == 0 && w % unit == 0;
     return o;
 }
 

@@ -29,18 +29,19 @@ constexpr uint32_t kBarrierBytes = 256;
 constexpr uint32_t kPiece = 8;                                          // fp32: steps of kTileK between two roundings to binary32
 
 // Shared memory and warps of a kernel: 16 epilogue warps of 64 columns each (8 of 128 took three times as long in the
-// hidden pass: two warps a scheduler do not cover each other's latencies).  bfloat16: they pass their results (and, in
-// the hidden pass, gate and up) through blocks of 32 x 32 in shared memory.  fp32: they hold their sums in registers.
+// hidden pass: two warps a scheduler do not cover each other's latencies).  They pass their results (and, in the hidden
+// pass, gate and up) through blocks of 32 rows of 64 bytes in shared memory: 32 columns of bfloat16, 16 of fp32.
 template <typename T, int MODE>
 struct MatShape {
     static constexpr bool kWide = sizeof(T) == 4;
     static constexpr uint32_t kEpilogue = 16;
     static constexpr uint32_t kThreads = 128 + 32 * kEpilogue;
-    static constexpr uint32_t kBlocks = kWide ? 0 : MODE == MAT_HIDDEN ? 2 : 1;   // of 2048 bytes, a warp
-    static constexpr uint32_t kStages = !kWide && MODE == MAT_HIDDEN ? 5 : 6;
+    static constexpr uint32_t kBlocks = MODE == MAT_HIDDEN ? 2 : 1;       // a warp's
+    static constexpr uint32_t kStages = MODE == MAT_HIDDEN ? 5 : 6;
     static constexpr uint32_t kSmem = kStages * kStageBytes + kEpilogue * kBlocks * 2048 + kBarrierBytes + 1024;   // 1024: to start on a swizzle atom
     static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
+
 constexpr uint32_t kMaxProblems = 4;
 constexpr uint32_t kTileEnd = 3;                                        // what a tile costs beside its steps, in steps
 constexpr unsigned long long kWaitLimitNs = 4000000000ull;              // how long a wait polls before it gives up
@@ -166,6 +167,11 @@ __device__ __forceinline__ void tmem_store4(uint32_t addr, const uint32_t (&r)[4
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
+__device__ __forceinline__ void tmem_store8(uint32_t addr, const float* v)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -188,63 +194,63 @@ __device__ __forceinline__ void sts128(uint32_t at, const uint4& v)
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-// A block of 32 rows (one a lane) by 32 columns that a warp passes through shared memory on its way between rows and
-// coalesced accesses.  ROW bytes a row; the 16-byte pieces of a row are permuted so that neither side has bank conflicts.
+// A block of 32 rows (one a lane) that a warp passes through shared memory on its way between rows and coalesced accesses.
+// ROW bytes a row: 64, or 32 / 16 for the 8-bit form; the 16-byte pieces of a row are permuted so that neither side has
+// bank conflicts.
 template <int ROW>
 __device__ __forceinline__ uint32_t block_at(uint32_t base, uint32_t row, uint32_t piece)
 {
-    constexpr uint32_t kPieces = ROW / 16;                // 8, 4 or 2
-    const uint32_t turn = kPieces == 8 ? row & 7 : kPieces == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
+    constexpr uint32_t kPieces = ROW / 16;
+    const uint32_t turn = kPieces == 4 ? (row >> 1) & 3 : kPieces == 2 ? (row >> 2) & 1 : 0;
     return base + row * ROW + ((piece ^ turn) << 4);
+}
+
+// One element of E bytes between a block and memory.
+template <int E> __device__ __forceinline__ void element_out(uint32_t at, unsigned char* p)
+{
+    uint32_t v;
+    if constexpr (E == 4) { asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at)); *reinterpret_cast<uint32_t*>(p) = v; }
+    else if constexpr (E == 2) { asm volatile("{\n .reg .b16 h;\n ld.shared.b16 h, [%1];\n cvt.u32.u16 %0, h;\n}" : "=r"(v) : "r"(at)); *reinterpret_cast<uint16_t*>(p) = (uint16_t)v; }
+    else { asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at)); *p = (unsigned char)v; }
+}
+template <int E> __device__ __forceinline__ void element_in(uint32_t at, const unsigned char* p, bool on)
+{
+    if constexpr (E == 4) { const uint32_t v = on ? *reinterpret_cast<const uint32_t*>(p) : 0u; asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+    else if constexpr (E == 2) { const uint16_t v = on ? *reinterpret_cast<const uint16_t*>(p) : (uint16_t)0; asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(v) : "memory"); }
+    else { const uint32_t v = on ? *p : 0u; asm volatile("st.shared.u8 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 }
 
 // Block -> matrix: `rows` (at most 32) rows and `cols` columns of it are inside.  E: the element type's size.
 template <int ROW, int E>
 __device__ __noinline__ void block_out_edge(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
-    constexpr uint32_t kPer = 16 / E;
+    constexpr uint32_t kPieces = ROW / 16, kPer = 16 / E, kCols = ROW / E;
     if (wide) {
-        constexpr uint32_t kPieces = ROW / 16;
-        const uint32_t piece = lane % kPieces;
+        const uint32_t piece = lane % kPieces, first = piece * kPer;
 #pragma unroll 1
         for (uint32_t row = lane / kPieces; row < rows; row += 32 / kPieces) {
-            uint4 v;
-            lds128(block_at<ROW>(base, row, piece), v);
+            const uint32_t at = block_at<ROW>(base, row, piece);
             unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
-            if ((piece + 1) * kPer <= cols) {
+            if (first + kPer <= cols) {
+                uint4 v;
+                lds128(at, v);
                 *reinterpret_cast<uint4*>(p) = v;
             } else {                                      // the row ends inside these 16 bytes, or before them
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (uint32_t j = 0; j < kPer; ++j)
-                    if (piece * kPer + j < cols) {
-                        if constexpr (E == 2) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-                        else p[j] = (unsigned char)(w[j / 4] >> (8 * (j & 3)));
-                    }
-            }
-        }
-    } else if (lane < cols) {                             // one column a lane
 #pragma unroll 1
-        for (uint32_t row = 0; row < rows; ++row) {
-            const uint32_t at = block_at<ROW>(base, row, lane / kPer) + (lane % kPer) * E;
-            unsigned char* p = to + (int64_t)row * row_bytes + lane * E;
-            if constexpr (E == 2) {
-                uint16_t v;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
-                *reinterpret_cast<uint16_t*>(p) = v;
-            } else {
-                uint32_t v;
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at));
-                *p = (unsigned char)v;
+                for (uint32_t j = 0; first + j < cols; ++j) element_out<E>(at + j * E, p + j * E);
             }
         }
+    } else if (lane < min(cols, kCols)) {                 // one column a lane
+#pragma unroll 1
+        for (uint32_t row = 0; row < rows; ++row)
+            element_out<E>(block_at<ROW>(base, row, lane / kPer) + (lane % kPer) * E, to + (int64_t)row * row_bytes + lane * E);
     }
 }
 template <int ROW, int E>
 __device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
     constexpr uint32_t kPieces = ROW / 16;
-    if (rows == 32 && cols >= 32 && wide) {               // the same for the whole warp
+    if (rows == 32 && cols >= ROW / E && wide) {          // the same for the whole warp
         const uint32_t piece = lane % kPieces, row = lane / kPieces;
         unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
         const int64_t step = row_bytes * (32 / kPieces);
@@ -259,77 +265,84 @@ __device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int6
 }
 
 // Matrix -> block of 64-byte rows, asynchronously where the rows are aligned; zeros outside.  Complete after block_wait and
-// __syncwarp.  bfloat16 fills a row; int8 its second half, so that a lane can write its bfloat16 results over its row from
-// the front while it still reads.
-template <int E>
+// __syncwarp.  PIECES 16-byte pieces a row, the last ones of the row: int8 fills its end, so that a lane can write its
+// results over its row from the front while it still reads.
+template <int E, int PIECES>
 __device__ __noinline__ void block_in_edge(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
-    constexpr uint32_t kPieces = 2 * E, kPer = 16 / E, kFirst = E == 1 ? 2 : 0;
+    constexpr uint32_t kPer = 16 / E, kFirst = 4 - PIECES;
     if (wide) {
-        const uint32_t piece = lane % kPieces;
-        const uint32_t inside = piece * kPer < cols ? (cols - piece * kPer < kPer ? cols - piece * kPer : kPer) * E : 0;
+        const uint32_t piece = lane % PIECES, first = piece * kPer;
+        const uint32_t inside = first < cols ? min(cols - first, kPer) * E : 0;
 #pragma unroll 1
-        for (uint32_t row = lane / kPieces; row < 32; row += 32 / kPieces) {
+        for (uint32_t row = lane / PIECES; row < 32; row += 32 / PIECES) {
             const uint32_t n = row < rows ? inside : 0;
             const unsigned char* p = n ? from + (int64_t)row * row_bytes + piece * 16 : from;
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(block_at<64>(base, row, kFirst + piece)), "l"(p), "r"(n) : "memory");
         }
-    } else {
+    } else if (lane < PIECES * kPer) {
 #pragma unroll 1
-        for (uint32_t row = 0; row < 32; ++row) {
-            const uint32_t at = block_at<64>(base, row, kFirst + lane / kPer) + (lane % kPer) * E;
-            const unsigned char* p = from + (int64_t)row * row_bytes + lane * E;
-            const bool on = row < rows && lane < cols;
-            if constexpr (E == 2) {
-                const uint16_t v = on ? *reinterpret_cast<const uint16_t*>(p) : (uint16_t)0;
-                asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory");
-            } else {
-                const uint32_t v = on ? *p : 0u;
-                asm volatile("st.shared.u8 [%0], %1;" ::"r"(at), "r"(v) : "memory");
-            }
-        }
+        for (uint32_t row = 0; row < 32; ++row)
+            element_in<E>(block_at<64>(base, row, kFirst + lane / kPer) + (lane % kPer) * E, from + (int64_t)row * row_bytes + lane * E, row < rows && lane < cols);
     }
 }
-template <int E>
+template <int E, int PIECES>
 __device__ __forceinline__ void block_in(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
-    constexpr uint32_t kPieces = 2 * E, kFirst = E == 1 ? 2 : 0;
-    if (rows == 32 && cols >= 32 && wide) {
-        const uint32_t piece = lane % kPieces, row = lane / kPieces;
+    constexpr uint32_t kFirst = 4 - PIECES;
+    if (rows == 32 && cols >= PIECES * 16 / E && wide) {
+        const uint32_t piece = lane % PIECES, row = lane / PIECES;
         const unsigned char* p = from + (int64_t)row * row_bytes + piece * 16;
-        const int64_t step = row_bytes * (32 / kPieces);
+        const int64_t step = row_bytes * (32 / PIECES);
 #pragma unroll
-        for (uint32_t i = 0; i < kPieces; ++i) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(block_at<64>(base, i * (32 / kPieces) + row, kFirst + piece)), "l"(p) : "memory");
+        for (uint32_t i = 0; i < PIECES; ++i) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(block_at<64>(base, i * (32 / PIECES) + row, kFirst + piece)), "l"(p) : "memory");
             p += step;
         }
     } else if (rows && cols) {                            // (a block that is all outside is not read)
-        block_in_edge<E>(base, from, row_bytes, rows, cols, wide, lane);
+        block_in_edge<E, PIECES>(base, from, row_bytes, rows, cols, wide, lane);
     }
 }
 __device__ __forceinline__ void block_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Eight columns of a lane's row of a bfloat16 block, as pairs of floats
+// Eight columns of a lane's row of a block, as pairs of floats
+template <typename T>
 __device__ __forceinline__ void row_put(uint32_t base, uint32_t lane, uint32_t j, const f2 (&v)[4])
 {
-    sts128(block_at<64>(base, lane, j), make_uint4(f2_narrow(v[0]), f2_narrow(v[1]), f2_narrow(v[2]), f2_narrow(v[3])));
+    if constexpr (sizeof(T) == 2) {
+        sts128(block_at<64>(base, lane, j), make_uint4(f2_narrow(v[0]), f2_narrow(v[1]), f2_narrow(v[2]), f2_narrow(v[3])));
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i)
+            asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(block_at<64>(base, lane, 2 * j + i)), "l"(v[2 * i]), "l"(v[2 * i + 1]) : "memory");
+    }
 }
+template <typename T>
 __device__ __forceinline__ void row_get(uint32_t base, uint32_t lane, uint32_t j, f2 (&v)[4])
 {
-    uint4 a;
-    lds128(block_at<64>(base, lane, j), a);
-    v[0] = f2_wide(a.x); v[1] = f2_wide(a.y); v[2] = f2_wide(a.z); v[3] = f2_wide(a.w);
+    if constexpr (sizeof(T) == 2) {
+        uint4 a;
+        lds128(block_at<64>(base, lane, j), a);
+        v[0] = f2_wide(a.x); v[1] = f2_wide(a.y); v[2] = f2_wide(a.z); v[3] = f2_wide(a.w);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i)
+            asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[2 * i]), "=l"(v[2 * i + 1]) : "r"(block_at<64>(base, lane, 2 * j + i)));
+    }
 }
-// ... of an 8-bit block: written in rows of 32 bytes, read where block_in puts it
+// ... of an 8-bit block: written in rows of as many bytes as columns, read where block_in puts it
+template <typename T>
 __device__ __forceinline__ void row_put_act8(uint32_t base, uint32_t lane, uint32_t j, float inv, const float* v)
 {
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(block_at<32>(base, lane, j >> 1) + (j & 1) * 8),
-                 "r"(act8_quant4(v[0], v[1], v[2], v[3], inv)), "r"(act8_quant4(v[4], v[5], v[6], v[7], inv)) : "memory");
+    const uint32_t at = sizeof(T) == 2 ? block_at<32>(base, lane, j >> 1) + (j & 1) * 8 : block_at<16>(base, lane, 0) + j * 8;
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(act8_quant4(v[0], v[1], v[2], v[3], inv)), "r"(act8_quant4(v[4], v[5], v[6], v[7], inv)) : "memory");
 }
+template <typename T>
 __device__ __forceinline__ void row_get_act8(uint32_t base, uint32_t lane, uint32_t j, float step, f2 (&v)[4])
 {
+    const uint32_t at = sizeof(T) == 2 ? block_at<64>(base, lane, 2 + (j >> 1)) + (j & 1) * 8 : block_at<64>(base, lane, 3) + j * 8;
     uint2 a;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a.x), "=r"(a.y) : "r"(block_at<64>(base, lane, 2 + (j >> 1)) + (j & 1) * 8));
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(a.x), "=r"(a.y) : "r"(at));
     float f[8];
     act8_value4(a.x, step, f);
     act8_value4(a.y, step, f + 4);
@@ -348,80 +361,45 @@ __device__ __forceinline__ float next_part(float& v)
     return hi;
 }
 
-// fp32 results go out row by row, eight columns at a time (`n` of them inside): six times the products stand behind each.
-__device__ __forceinline__ void store8(float* p, const float* v, uint32_t n, bool wide)
+// A block of an operand of the next product -> workspace: bfloat16, or the three parts of 16 fp32 columns.
+template <typename T>
+__device__ __forceinline__ void operand_out(uint32_t base, const MatOut& o, int64_t at, uint32_t rows, uint32_t room, uint32_t lane)
 {
-    if (wide && n >= 8) {
-        Vec<float, 8>::store(p, v);
+    if constexpr (sizeof(T) == 2) {
+        block_out<64, 2>(base, static_cast<unsigned char*>(o.p) + 2 * at, 2 * o.r, rows, room, true, lane);
     } else {
+        const uint32_t piece = lane & 3;
+        bf16* p = static_cast<bf16*>(o.p) + at + (int64_t)(lane >> 2) * o.r + piece * 4;
+#pragma unroll 1
+        for (uint32_t row = lane >> 2; row < 32; row += 8) {
+            float v[4];
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(block_at<64>(base, row, piece)));
+            if (row < rows && piece * 4 < room) {         // (the workspace's rows hold a multiple of eight columns)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) p[i] = v[i];
+                for (int part = 0; part < 3; ++part) {
+                    float hi[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) hi[i] = next_part(v[i]);
+                    *reinterpret_cast<uint2*>(p + part * o.part) = make_uint2(f2_narrow(f2_of(hi[0], hi[1])), f2_narrow(f2_of(hi[2], hi[3])));
+                }
+            }
+            p += 8 * o.r;
+        }
     }
-}
-__device__ __forceinline__ void load8(const float* p, float* v, uint32_t n, bool wide)
-{
-    if (wide && n >= 8) {
-        Vec<float, 8>::load(p, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
-    }
-}
-__device__ __forceinline__ void store8_parts(const MatOut& o, int64_t at, float* v)
-{
-    bf16* p = static_cast<bf16*>(o.p) + at;               // the workspace: rows are padded to eight columns
-#pragma unroll
-    for (int part = 0; part < 3; ++part) {
-        float hi[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) hi[i] = next_part(v[i]);
-        Vec<bf16, 8>::store(p + part * o.part, hi);
-    }
-}
-__device__ __forceinline__ void store8_act8(const MatOut& q, int64_t at, const float* v, float inv, uint32_t n)
-{
-    int8_t* p = static_cast<int8_t*>(q.p) + at;
-    const uint32_t w[2] = {act8_quant4(v[0], v[1], v[2], v[3], inv), act8_quant4(v[4], v[5], v[6], v[7], inv)};
-    if (q.wide && n >= 8) {
-        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) p[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
-    }
-}
-__device__ __forceinline__ void load8_act8(const MatOut& q, int64_t at, float* v, float step, uint32_t n)
-{
-    const int8_t* p = static_cast<const int8_t*>(q.p) + at;
-    uint32_t w[2] = {0, 0};
-    if (q.wide && n >= 8) {
-        const uint2 a = __ldg(reinterpret_cast<const uint2*>(p));
-        w[0] = a.x; w[1] = a.y;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) w[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
-    }
-    act8_value4(w[0], step, v);
-    act8_value4(w[1], step, v + 4);
 }
 
-// fp32, eight columns: g <- act(g) * u  (gate/up);  dh, g, u -> h, dg, du  (hidden)
-template <int ACT>
-__device__ __forceinline__ void gate8(float* g, const float* u)
+// The activation of a pair: fast for results that are rounded to bfloat16, accurate for fp32.
+template <typename T, int ACT, bool SLOPE>
+__device__ __forceinline__ f2 act_pair(f2 g, f2& slope)
 {
-    float unused;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = act<ACT, false, false>(g[i], unused) * u[i];
-}
-template <int ACT>
-__device__ __forceinline__ void hidden8(float* dh, float* g, float* u)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float slope;
-        const float a = act<ACT, true, false>(g[i], slope), d = dh[i];
-        g[i] = d * u[i] * slope;                                        // dg
-        dh[i] = a * u[i];                                               // h
-        u[i] = d * a;                                                   // du
+    if constexpr (sizeof(T) == 2) {
+        return act2<ACT, SLOPE>(g, slope);
+    } else {
+        float x, y, sx = 0.0f, sy = 0.0f;
+        f2_get(g, x, y);
+        const float ax = act<ACT, SLOPE, false>(x, sx), ay = act<ACT, SLOPE, false>(y, sy);
+        if constexpr (SLOPE) slope = f2_of(sx, sy);
+        return f2_of(ax, ay);
     }
 }
 
@@ -610,268 +588,212 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             if (lane == 0) bar_arrive_at(in_cta(acc_empty + 8 * (it & 1), 0));
             ++it;
         };
-        const int64_t gate_e_r = a.gate_e.r, up_e_r = a.up_e.r;
-        if constexpr (!Shape::kWide) {
-            // ---- bfloat16: blocks of 32 columns, eight at a time (in a loop: unrolled, they outgrow the instruction cache)
-            constexpr uint32_t kChunks = MODE == MAT_GATED ? 1 : 2;
-            const uint32_t mine = blocks + (warp - 4) * Shape::kBlocks * 2048;
-            const bool eight = a.save == PALSGD_SAVE_8BIT;
-            uint32_t ge = 0, ue = 0;                                      // hidden, 8 bits: exponents of the block under way
-            // hidden: gate and up of block c of a tile into the warp's first two blocks
-            auto fetch = [&](const Tile& tl, uint32_t c) {
-                const uint32_t m = tl.m0 + rank * 128 + quad * 32, n = tl.n0 + (part * kChunks + c) * 32;
-                const uint32_t M = tl.p->M, N = tl.p->N;
-                const uint32_t rows = m < M ? min(M - m, 32u) : 0, cols = n < N ? N - n : 0;
-                const int64_t w = tl.worker;
-                const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
-                if (eight) {
-                    block_in<1>(mine, static_cast<const unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
-                    block_in<1>(mine + 2048, static_cast<const unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
-                    const bool on = lane < rows && cols;
-                    ge = on ? static_cast<const uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * gate_e_r + n / 32] : 0u;
-                    ue = on ? static_cast<const uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] : 0u;
-                } else {
-                    block_in<2>(mine, static_cast<const unsigned char*>(a.gate.p) + 2 * go, 2 * a.gate.r, rows, cols, a.gate.wide, lane);
-                    block_in<2>(mine + 2048, static_cast<const unsigned char*>(a.up.p) + 2 * uo, 2 * a.up.r, rows, cols, a.up.wide, lane);
-                }
-            };
-            if constexpr (MODE == MAT_HIDDEN) { fetch(tile_at<MODE>(a, Order(a, pair, pairs).now()), 0); }
-            for (Order o(a, pair, pairs); o.now() < a.tiles; o.next()) {
-                const uint32_t t = o.now();
-                const Tile tl = tile_at<MODE>(a, t);
-                const MatProblem& p = *tl.p;
-                const uint32_t src = tmem + (it & 1) * kTileN + (quad << 21);
-                const uint32_t m = tl.m0 + rank * 128 + quad * 32, rows = m < p.M ? min(p.M - m, 32u) : 0;
-                const int64_t w = tl.worker;
-                if (!acc_wait()) break;
-#pragma unroll 1
-                for (uint32_t c = 0; c < kChunks; ++c) {
-                    const uint32_t col = (part * kChunks + c) * 32, n = tl.n0 + col;
-                    const uint32_t cols = n < p.N ? p.N - n : 0, room = n < p.out[0].cols ? p.out[0].cols - n : 0;
-                    const int64_t at = 2 * (w * p.out[0].w + (int64_t)m * p.out[0].r + n), step = 2 * p.out[0].r;
-                    const uint32_t b0 = mine;
-                    if constexpr (MODE == MAT_PLAIN) {
-#pragma unroll
-                        for (uint32_t j = 0; j < 4; j += 2) {
-                            float v[16];
-                            tmem_load16(src + col + 8 * j, v);
-                            tmem_load_wait();
-                            f2 y[2][4];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) y[i / 4][i % 4] = f2_of(v[2 * i], v[2 * i + 1]);
-                            row_put(b0, lane, j, y[0]);
-                            row_put(b0, lane, j + 1, y[1]);
-                        }
-                        if (c + 1 == kChunks) acc_read();
-                        __syncwarp();
-                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, p.out[0].wide, lane);
-                        __syncwarp();
-                    } else if constexpr (MODE == MAT_GATED) {
-                        float gi = 0.0f, ui = 0.0f;                       // one over the steps of the groups
-                        if (eight) {
-                            float gm = 0.0f, um = 0.0f;
-#pragma unroll 1
-                            for (uint32_t j = 0; j < 4; ++j) {
-                                float v[8], u[8];
-                                tmem_load8(src + col + 8 * j, v);
-                                tmem_load8(src + kTileN / 2 + col + 8 * j, u);
-                                tmem_load_wait();
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) { gm = act8_max(gm, v[i]); um = act8_max(um, u[i]); }
-                            }
-                            const uint32_t eg = act8_exponent(gm), eu = act8_exponent(um);
-                            gi = act8_inverse(eg); ui = act8_inverse(eu);
-                            if (lane < rows && cols) {
-                                static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * gate_e_r + n / 32] = (uint8_t)eg;
-                                static_cast<uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * up_e_r + n / 32] = (uint8_t)eu;
-                            }
-                        }
-                        // gate, up and h pass through one block, one after another (tensor memory is read again for each)
-                        if (a.save != PALSGD_SAVE_NONE) {
-#pragma unroll 1
-                            for (uint32_t which = 0; which < 2; ++which) {
-                                const MatOut& s = which ? a.up : a.gate;
-                                const float inv = which ? ui : gi;
-#pragma unroll
-                                for (uint32_t j = 0; j < 4; j += 2) {
-                                    float v[16];
-                                    tmem_load16(src + which * (kTileN / 2) + col + 8 * j, v);
-                                    tmem_load_wait();
-                                    if (eight) {
-                                        row_put_act8(b0, lane, j, inv, v);
-                                        row_put_act8(b0, lane, j + 1, inv, v + 8);
-                                    } else {
-                                        f2 y[2][4];
-#pragma unroll
-                                        for (int i = 0; i < 8; ++i) y[i / 4][i % 4] = f2_of(v[2 * i], v[2 * i + 1]);
-                                        row_put(b0, lane, j, y[0]);
-                                        row_put(b0, lane, j + 1, y[1]);
-                                    }
-                                }
-                                __syncwarp();
-                                const int64_t to = w * s.w + (int64_t)m * s.r + n;
-                                if (eight) block_out<32, 1>(b0, static_cast<unsigned char*>(s.p) + to, s.r, rows, cols, s.wide, lane);
-                                else block_out<64, 2>(b0, static_cast<unsigned char*>(s.p) + 2 * to, 2 * s.r, rows, cols, s.wide, lane);
-                                __syncwarp();
-                            }
-                        }
-#pragma unroll 1
-                        for (uint32_t j = 0; j < 4; ++j) {
-                            float v[8], u[8];
-                            tmem_load8(src + col + 8 * j, v);
-                            tmem_load8(src + kTileN / 2 + col + 8 * j, u);
-                            tmem_load_wait();
-                            f2 h[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                f2 unused;
-                                h[i] = f2_mul(act2<ACT, false>(f2_of(v[2 * i], v[2 * i + 1]), unused), f2_of(u[2 * i], u[2 * i + 1]));
-                            }
-                            row_put(b0, lane, j, h);
-                        }
-                        acc_read();
-                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
-                        __syncwarp();
-                    } else {
-                        block_wait();
-                        __syncwarp();
-                        const uint32_t b1 = mine + 2048;
-                        const float gs = act8_step(ge), us = act8_step(ue);
-#pragma unroll 1
-                        for (uint32_t j = 0; j < 4; ++j) {
-                            float v[8];
-                            f2 g[4], q[4], dg[4], du[4], h[4];
-                            tmem_load8(src + col + 8 * j, v);
-                            if (eight) { row_get_act8(b0, lane, j, gs, g); row_get_act8(b1, lane, j, us, q); }
-                            else { row_get(b0, lane, j, g); row_get(b1, lane, j, q); }
-                            tmem_load_wait();
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                f2 slope;
-                                const f2 ag = act2<ACT, true>(g[i], slope), d = f2_of(v[2 * i], v[2 * i + 1]);
-                                dg[i] = f2_mul(f2_mul(d, q[i]), slope);
-                                du[i] = f2_mul(d, ag);
-                                h[i] = f2_mul(ag, q[i]);
-                            }
-                            row_put(b0, lane, j, dg);
-                            row_put(b1, lane, j, du);
-                            // h waits its turn in tensor memory, over sums that have been read
-                            const uint32_t hw[4] = {f2_narrow(h[0]), f2_narrow(h[1]), f2_narrow(h[2]), f2_narrow(h[3])};
-                            tmem_store4(src + col + 4 * j, hw);
-                        }
-                        tmem_store_wait();
-                        __syncwarp();
-                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[0].p) + at, step, rows, room, 1, lane);
-                        block_out<64, 2>(b1, static_cast<unsigned char*>(p.out[1].p) + at, step, rows, room, 1, lane);
-                        __syncwarp();
-                        {
-                            float h[16];
-                            tmem_load16(src + col, h);
-                            tmem_load_wait();
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                sts128(block_at<64>(b0, lane, j), make_uint4(__float_as_uint(h[4 * j]), __float_as_uint(h[4 * j + 1]), __float_as_uint(h[4 * j + 2]), __float_as_uint(h[4 * j + 3])));
-                        }
-                        if (c + 1 == kChunks) acc_read();
-                        __syncwarp();
-                        block_out<64, 2>(b0, static_cast<unsigned char*>(p.out[2].p) + at, step, rows, room, 1, lane);
-                        __syncwarp();
-                        // the next block: of this tile, or the first of the warp's next tile
-                        if (c + 1 < kChunks) fetch(tl, c + 1);
-                        else if (o.then() < a.tiles) fetch(tile_at<MODE>(a, o.then()), 0);
-                    }
-                }
+        // blocks of kCols columns, eight columns at a time in a loop (unrolled, they outgrow the instruction cache)
+        constexpr uint32_t E = sizeof(T), kCols = 64 / E, kOcts = kCols / 8, kMine = MODE == MAT_GATED ? 32 : 64, kChunks = kMine / kCols;
+        const uint32_t b0 = blocks + (warp - 4) * Shape::kBlocks * 2048, b1 = b0 + 2048;
+        const bool eight = a.save == PALSGD_SAVE_8BIT;
+        uint32_t ge = 0, ue = 0;                                          // hidden, 8 bits: exponents of the block under way
+        // hidden: gate and up of block c of a tile into the warp's two blocks
+        auto fetch = [&](const Tile& tl, uint32_t c) {
+            const uint32_t m = tl.m0 + rank * 128 + quad * 32, n = tl.n0 + part * kMine + c * kCols;
+            const uint32_t M = tl.p->M, N = tl.p->N;
+            const uint32_t rows = m < M ? min(M - m, 32u) : 0, cols = n < N ? N - n : 0;
+            const int64_t w = tl.worker;
+            const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
+            if (eight) {
+                block_in<1, kCols / 16>(b0, static_cast<const unsigned char*>(a.gate.p) + go, a.gate.r, rows, cols, a.gate.wide, lane);
+                block_in<1, kCols / 16>(b1, static_cast<const unsigned char*>(a.up.p) + uo, a.up.r, rows, cols, a.up.wide, lane);
+                const bool on = lane < rows && cols;
+                ge = on ? static_cast<const uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * a.gate_e.r + n / 32] : 0u;
+                ue = on ? static_cast<const uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * a.up_e.r + n / 32] : 0u;
+            } else {
+                block_in<E, 4>(b0, static_cast<const unsigned char*>(a.gate.p) + E * go, E * a.gate.r, rows, cols, a.gate.wide, lane);
+                block_in<E, 4>(b1, static_cast<const unsigned char*>(a.up.p) + E * uo, E * a.up.r, rows, cols, a.up.wide, lane);
             }
-        } else {
-            // ---- fp32: sums of 64 columns in registers (gate/up: 32 of each)
-            for (Order o(a, pair, pairs); o.now() < a.tiles; o.next()) {
-                const uint32_t t = o.now();
-                const Tile tl = tile_at<MODE>(a, t);
-                const MatProblem& p = *tl.p;
-                const uint32_t m = tl.m0 + rank * 128 + quad * 32 + lane;
-                const int64_t w = tl.worker;
-                const uint32_t col[2] = {MODE == MAT_GATED ? part * 32 : part * 64, MODE == MAT_GATED ? kTileN / 2 + part * 32 : part * 64 + 32};
+        };
+        if constexpr (MODE == MAT_HIDDEN) fetch(tile_at<MODE>(a, Order(a, pair, pairs).now()), 0);
+        for (Order o(a, pair, pairs); o.now() < a.tiles; o.next()) {
+            const Tile tl = tile_at<MODE>(a, o.now());
+            const MatProblem& p = *tl.p;
+            const uint32_t m = tl.m0 + rank * 128 + quad * 32, rows = m < p.M ? min(p.M - m, 32u) : 0;
+            const int64_t w = tl.worker;
+            uint32_t src = tmem + (it & 1) * kTileN + (quad << 21) + part * kMine;
+            if constexpr (!Shape::kWide) {
+                if (!acc_wait()) break;
+            } else {
+                // fp32: the pieces' sums joined in registers, and put back for what follows
                 float sum[64];
 #pragma unroll
                 for (int i = 0; i < 64; ++i) sum[i] = 0.0f;
-                const bool ok = for_pieces<T>(p, [&](uint32_t, uint32_t, uint32_t) {
-                    const uint32_t src = tmem + (it & 1) * kTileN + (quad << 21);
-                    if (!acc_wait()) return false;
+                uint32_t pieces = p.n_seg * ((p.Kd + kPiece * kTileK - 1) / (kPiece * kTileK));
+                bool ok = true;
+                for (;;) {
+                    src = tmem + (it & 1) * kTileN + (quad << 21) + part * kMine;
+                    if (!acc_wait()) { ok = false; break; }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         float v[16];
-                        tmem_load16(src + col[q / 2] + (q & 1) * 16, v);
+                        tmem_load16(src + (MODE == MAT_GATED && q >= 2 ? kTileN / 2 + (q - 2) * 16 : q * 16), v);
                         tmem_load_wait();
 #pragma unroll
                         for (int i = 0; i < 16; ++i) sum[q * 16 + i] += v[i];
                     }
+                    if (--pieces == 0) break;
                     acc_read();
-                    return true;
-                });
+                }
                 if (!ok) break;
-                // (nothing below is a whole warp's: rows outside have no columns, and no thread leaves the common path)
 #pragma unroll
-                for (int c = 0; c < (MODE == MAT_GATED ? 1 : 2); ++c) {
-                    const uint32_t n = tl.n0 + col[c];
-                    if (m >= p.M || n >= p.N) continue;
-                    const int64_t at = w * p.out[0].w + (int64_t)m * p.out[0].r + n;
-                    const int64_t go = w * a.gate.w + (int64_t)m * a.gate.r + n, uo = w * a.up.w + (int64_t)m * a.up.r + n;
-                    const int64_t geo = w * a.gate_e.w + (int64_t)m * gate_e_r + n / 32, ueo = w * a.up_e.w + (int64_t)m * up_e_r + n / 32;
-                    const bool eight = a.save == PALSGD_SAVE_8BIT;
-                    float gs = 0.0f, us = 0.0f;                           // steps of the groups, or one over them
-                    if constexpr (MODE == MAT_GATED) {
-                        if (eight) {
-                            float gm = 0.0f, um = 0.0f;
+                for (int q = 0; q < 8; ++q) tmem_store8(src + (MODE == MAT_GATED && q >= 4 ? kTileN / 2 + (q - 4) * 8 : q * 8), sum + 8 * q);
+                tmem_store_wait();
+            }
+            float gi = 0.0f, ui = 0.0f;                                   // gate/up, 8 bits: one over the steps of the groups
+            if constexpr (MODE == MAT_GATED) {
+                const uint32_t n = tl.n0 + part * kMine;
+                if (eight) {
+                    float gm = 0.0f, um = 0.0f;
+#pragma unroll 1
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        float v[8], u[8];
+                        tmem_load8(src + 8 * j, v);
+                        tmem_load8(src + kTileN / 2 + 8 * j, u);
+                        tmem_load_wait();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) { gm = act8_max(gm, sum[i]); um = act8_max(um, sum[32 + i]); }
-                            const uint32_t eg = act8_exponent(gm), eu = act8_exponent(um);
-                            static_cast<uint8_t*>(a.gate_e.p)[geo] = (uint8_t)eg;
-                            static_cast<uint8_t*>(a.up_e.p)[ueo] = (uint8_t)eu;
-                            gs = act8_inverse(eg); us = act8_inverse(eu);
-                        }
-                    } else if constexpr (MODE == MAT_HIDDEN) {
-                        if (eight) {
-                            gs = act8_step(static_cast<const uint8_t*>(a.gate_e.p)[geo]);
-                            us = act8_step(static_cast<const uint8_t*>(a.up_e.p)[ueo]);
-                        }
+                        for (int i = 0; i < 8; ++i) { gm = act8_max(gm, v[i]); um = act8_max(um, u[i]); }
                     }
-#pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        if (n + j >= p.N) continue;
-                        const uint32_t left = p.N - n - j;
-                        float* v = sum + 32 * c + j;
-                        if constexpr (MODE == MAT_PLAIN) {
-                            store8(static_cast<float*>(p.out[0].p) + at + j, v, left, p.out[0].wide);
-                        } else if constexpr (MODE == MAT_GATED) {
-                            float* u = sum + 32 + j;
-                            if (a.save == PALSGD_SAVE_FULL) {
-                                store8(static_cast<float*>(a.gate.p) + go + j, v, left, a.gate.wide);
-                                store8(static_cast<float*>(a.up.p) + uo + j, u, left, a.up.wide);
-                            } else if (eight) {
-                                store8_act8(a.gate, go + j, v, gs, left);
-                                store8_act8(a.up, uo + j, u, us, left);
-                            }
-                            gate8<ACT>(v, u);
-                            store8_parts(p.out[0], at + j, v);
-                        } else {
-                            float g[8], u[8];
-                            if (eight) {
-                                load8_act8(a.gate, go + j, g, gs, left);
-                                load8_act8(a.up, uo + j, u, us, left);
-                            } else {
-                                load8(static_cast<const float*>(a.gate.p) + go + j, g, left, a.gate.wide);
-                                load8(static_cast<const float*>(a.up.p) + uo + j, u, left, a.up.wide);
-                            }
-                            hidden8<ACT>(v, g, u);
-                            store8_parts(p.out[0], at + j, g);
-                            store8_parts(p.out[1], at + j, u);
-                            store8_parts(p.out[2], at + j, v);
-                        }
+                    const uint32_t eg = act8_exponent(gm), eu = act8_exponent(um);
+                    gi = act8_inverse(eg); ui = act8_inverse(eu);
+                    if (lane < rows && n < p.N) {
+                        static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * a.gate_e.r + n / 32] = (uint8_t)eg;
+                        static_cast<uint8_t*>(a.up_e.p)[w * a.up_e.w + (int64_t)(m + lane) * a.up_e.r + n / 32] = (uint8_t)eu;
                     }
                 }
             }
+#pragma unroll 1
+            for (uint32_t c = 0; c < kChunks; ++c) {
+                const uint32_t from = src + c * kCols, n = tl.n0 + part * kMine + c * kCols;
+                const uint32_t cols = n < p.N ? p.N - n : 0, room = n < p.out[0].cols ? p.out[0].cols - n : 0;
+                const int64_t at = w * p.out[0].w + (int64_t)m * p.out[0].r + n;
+                if constexpr (MODE == MAT_PLAIN) {
+#pragma unroll
+                    for (uint32_t j = 0; j < kOcts; j += 2) {
+                        float v[16];
+                        tmem_load16(from + 8 * j, v);
+                        tmem_load_wait();
+                        f2 y[2][4];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i / 4][i % 4] = f2_of(v[2 * i], v[2 * i + 1]);
+                        row_put<T>(b0, lane, j, y[0]);
+                        row_put<T>(b0, lane, j + 1, y[1]);
+                    }
+                    if (c + 1 == kChunks) acc_read();
+                    __syncwarp();
+                    block_out<64, E>(b0, static_cast<unsigned char*>(p.out[0].p) + E * at, E * p.out[0].r, rows, room, p.out[0].wide, lane);
+                    __syncwarp();
+                } else if constexpr (MODE == MAT_GATED) {
+                    // gate, up and h pass through one block, one after another (tensor memory is read again for each)
+                    if (a.save != PALSGD_SAVE_NONE) {
+#pragma unroll 1
+                        for (uint32_t which = 0; which < 2; ++which) {
+                            const MatOut& s = which ? a.up : a.gate;
+                            const float inv = which ? ui : gi;
+#pragma unroll
+                            for (uint32_t j = 0; j < kOcts; j += 2) {
+                                float v[16];
+                                tmem_load16(from + which * (kTileN / 2) + 8 * j, v);
+                                tmem_load_wait();
+                                if (eight) {
+                                    row_put_act8<T>(b0, lane, j, inv, v);
+                                    row_put_act8<T>(b0, lane, j + 1, inv, v + 8);
+                                } else {
+                                    f2 y[2][4];
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) y[i / 4][i % 4] = f2_of(v[2 * i], v[2 * i + 1]);
+                                    row_put<T>(b0, lane, j, y[0]);
+                                    row_put<T>(b0, lane, j + 1, y[1]);
+                                }
+                            }
+                            __syncwarp();
+                            const int64_t to = w * s.w + (int64_t)m * s.r + n;
+                            if (eight) block_out<kCols, 1>(b0, static_cast<unsigned char*>(s.p) + to, s.r, rows, cols, s.wide, lane);
+                            else block_out<64, E>(b0, static_cast<unsigned char*>(s.p) + E * to, E * s.r, rows, cols, s.wide, lane);
+                            __syncwarp();
+                        }
+                    }
+#pragma unroll 1
+                    for (uint32_t j = 0; j < kOcts; ++j) {
+                        float v[8], u[8];
+                        tmem_load8(from + 8 * j, v);
+                        tmem_load8(from + kTileN / 2 + 8 * j, u);
+                        tmem_load_wait();
+                        f2 h[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            f2 unused;
+                            h[i] = f2_mul(act_pair<T, ACT, false>(f2_of(v[2 * i], v[2 * i + 1]), unused), f2_of(u[2 * i], u[2 * i + 1]));
+                        }
+                        row_put<T>(b0, lane, j, h);
+                    }
+                    if (c + 1 == kChunks) acc_read();
+                    __syncwarp();
+                    operand_out<T>(b0, p.out[0], at, rows, room, lane);
+                    __syncwarp();
+                } else {
+                    block_wait();
+                    __syncwarp();
+                    const float gs = act8_step(ge), us = act8_step(ue);
+#pragma unroll 1
+                    for (uint32_t j = 0; j < kOcts; ++j) {
+                        float v[8];
+                        f2 g[4], q[4], dg[4], du[4], h[4];
+                        tmem_load8(from + 8 * j, v);
+                        if (eight) { row_get_act8<T>(b0, lane, j, gs, g); row_get_act8<T>(b1, lane, j, us, q); }
+                        else { row_get<T>(b0, lane, j, g); row_get<T>(b1, lane, j, q); }
+                        tmem_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            f2 slope;
+                            const f2 ag = act_pair<T, ACT, true>(g[i], slope), d = f2_of(v[2 * i], v[2 * i + 1]);
+                            dg[i] = f2_mul(f2_mul(d, q[i]), slope);
+                            du[i] = f2_mul(d, ag);
+                            h[i] = f2_mul(ag, q[i]);
+                        }
+                        row_put<T>(b0, lane, j, dg);
+                        row_put<T>(b1, lane, j, du);
+                        // h waits its turn in tensor memory, over sums that have been read
+                        if constexpr (E == 2) {
+                            const uint32_t hw[4] = {f2_narrow(h[0]), f2_narrow(h[1]), f2_narrow(h[2]), f2_narrow(h[3])};
+                            tmem_store4(from + 4 * j, hw);
+                        } else {
+                            float hv[8];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) f2_get(h[i], hv[2 * i], hv[2 * i + 1]);
+                            tmem_store8(from + 8 * j, hv);
+                        }
+                    }
+                    tmem_store_wait();
+                    __syncwarp();
+                    operand_out<T>(b0, p.out[0], at, rows, room, lane);
+                    operand_out<T>(b1, p.out[1], at, rows, room, lane);
+                    __syncwarp();
+                    {
+                        float h[16];                                      // 64 bytes of a row in either type
+                        tmem_load16(from, h);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            sts128(block_at<64>(b0, lane, j), make_uint4(__float_as_uint(h[4 * j]), __float_as_uint(h[4 * j + 1]), __float_as_uint(h[4 * j + 2]), __float_as_uint(h[4 * j + 3])));
+                    }
+                    if (c + 1 == kChunks) acc_read();
+                    __syncwarp();
+                    operand_out<T>(b0, p.out[2], at, rows, room, lane);
+                    __syncwarp();
+                    // the next block: of this tile, or the first of the warp's next tile
+                    if (c + 1 < kChunks) fetch(tl, c + 1);
+                    else if (o.then() < a.tiles) fetch(tile_at<MODE>(a, o.then()), 0);
+                }
+            }
         }
-        if constexpr (MODE == MAT_HIDDEN && !Shape::kWide) block_wait();
+        if constexpr (MODE == MAT_HIDDEN) block_wait();
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -898,6 +820,7 @@ struct StageItem {
     uint64_t units;               // of 8 columns, one worker
     int      kind;
     uint32_t K;                   // workers to copy: 1 if all read one matrix
+    int      wide;                // eight columns can be read at a time (fp32, 8 bits)
 };
 struct StageArgs { StageItem item[kMaxStaged]; };
 
@@ -912,19 +835,28 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
         const uint32_t c = (uint32_t)(i - row * per) * 8;
         const int64_t from = k * it.w + (int64_t)row * it.r + c;
         float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = 0.0f;
-            if (c + j < it.cols) {
-                if (it.kind == STAGE_BF16) v[j] = to_f(static_cast<const bf16*>(it.src)[from + j]);
-                else if (it.kind == STAGE_SPLIT) v[j] = static_cast<const float*>(it.src)[from + j];
-                else v[j] = (float)static_cast<const int8_t*>(it.src)[from + j];
-            }
-        }
+        const bool whole = it.wide && c + 8 <= it.cols;
         if (it.kind == STAGE_ACT8) {
-            const float s = act8_step(it.e[k * it.ew + (int64_t)row * it.er + c / 32]);
+            uint2 q = make_uint2(0, 0);
+            const int8_t* p = static_cast<const int8_t*>(it.src) + from;
+            if (whole) {
+                q = __ldg(reinterpret_cast<const uint2*>(p));
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= s;
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < it.cols) (j < 4 ? q.x : q.y) |= (uint32_t)(uint8_t)p[j] << (8 * (j & 3));
+            }
+            const float s = act8_step(it.e[k * it.ew + (int64_t)row * it.er + c / 32]);
+            act8_value4(q.x, s, v);
+            act8_value4(q.y, s, v + 4);
+        } else if (it.kind == STAGE_SPLIT && whole) {
+            Vec<float, 8>::load(static_cast<const float*>(it.src) + from, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = 0.0f;
+                if (c + j < it.cols) v[j] = it.kind == STAGE_BF16 ? to_f(static_cast<const bf16*>(it.src)[from + j]) : static_cast<const float*>(it.src)[from + j];
+            }
         }
         bf16* to = it.dst + (k * it.rows + (int64_t)row) * it.ld + c;
         if (it.kind == STAGE_SPLIT) {
