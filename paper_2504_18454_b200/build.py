@@ -1,4 +1,5 @@
-"""Compile the CUDA library in-tree: paper_2504_18454_b200/libpalsgd.so (sm_100a).
+"""Compile the CUDA library in-tree: paper_2504_18454_b200/libpalsgd.so (sm_100a), and the native part of the
+block operators' Python binding, paper_2504_18454_b200/_block.so (g++, against the installed torch).
 
 nvcc cross-compiles without a GPU.  The runtime is linked statically, so the
 library loads (and its pure-host entry points work) on a machine without a
@@ -14,6 +15,8 @@ from pathlib import Path
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libpalsgd.so"
+EXT = HERE / "_block.so"
+EXT_SOURCE = CSRC / "block_torch.cpp"
 SOURCES = [CSRC / "palsgd_api.cu", CSRC / "palsgd_noalloc.cu", CSRC / "block_api.cu"]
 DEPS = sorted(CSRC.glob("*.cu*")) + sorted(CSRC.glob("*.h")) + sorted((HERE.parent / "include").glob("*.h")) + [Path(__file__)]
 
@@ -37,7 +40,29 @@ def needs_build() -> bool:
     return LIB.stat().st_mtime < max(p.stat().st_mtime for p in DEPS)
 
 
+def build_extension(force: bool = False) -> Path:
+    """_block.so: it is bound to the loaded libpalsgd.so at run time and links torch only."""
+    newest = max(p.stat().st_mtime for p in (EXT_SOURCE, HERE.parent / "include" / "palsgd_block.h", Path(__file__)))
+    if not force and EXT.exists() and EXT.stat().st_mtime >= newest:
+        return EXT
+    import sysconfig
+
+    import torch
+    home = Path(torch.__file__).resolve().parent
+    cuda = Path(nvcc_path()).resolve().parent.parent
+    tmp = HERE / f"_block.{os.getpid()}.tmp.so"
+    subprocess.check_call([
+        os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+        f"-I{home}/include", f"-I{home}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}",
+        f"-I{cuda}/include", str(EXT_SOURCE), "-o", str(tmp),
+        f"-L{home}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(tmp, EXT)
+    return EXT
+
+
 def build(force: bool = False, verbose: bool = False) -> Path:
+    build_extension(force)
     if not force and not needs_build():
         return LIB
     tmp = HERE / f"libpalsgd.{os.getpid()}.tmp.so"
