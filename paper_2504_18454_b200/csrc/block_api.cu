@@ -83,10 +83,20 @@ int check_mat(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, siz
 
 #define BLOCK_TRY(call) do { const int rc_ = (call); if (rc_ != PALSGD_OK) return rc_; } while (0)
 
-int launched(const char* what)
+// A launch that may start up while the stream's previous kernel still runs (the kernels wait for it: block_common.cuh).
+template <typename... A, typename... B>
+int launch(const char* what, void (*kernel)(A...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const B&... args)
 {
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? PALSGD_OK : palsgd_block_cuda_fail((int)e, what);
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid; c.blockDim = dim3(threads); c.dynamicSmemBytes = smem; c.stream = st;
+    c.attrs = &early; c.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&c, kernel, args...);
+    if (e == cudaSuccess) return PALSGD_OK;
+    (void)cudaGetLastError();
+    return palsgd_block_cuda_fail((int)e, what);
 }
 
 int sm_count()
@@ -121,9 +131,7 @@ int launch_act8(uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x, c
     a.units = rows * a.units_per_row;
     const uint64_t ctas = ceil_div(a.units, 256), most = 64ull * sm_count();
     const dim3 grid((unsigned)(ctas < most ? ctas : most), K);
-    if (wide) act8_kernel<T, 8, PACK><<<grid, 256, 0, st>>>(a);
-    else act8_kernel<T, 1, PACK><<<grid, 256, 0, st>>>(a);
-    return launched(PACK ? "act8 pack" : "act8 unpack");
+    return launch(PACK ? "act8 pack" : "act8 unpack", wide ? act8_kernel<T, 8, PACK> : act8_kernel<T, 1, PACK>, grid, 256, 0, st, a);
 }
 
 // ------------------------------------------------------------------------------------------------ feed-forward block
@@ -278,8 +286,7 @@ int run_stage(const Stage& st, uint32_t K, int sms, cudaStream_t stream)
     uint64_t most = 1;
     for (uint32_t i = 0; i < st.n; ++i) most = st.a.item[i].units > most ? st.a.item[i].units : most;
     const uint64_t want = ceil_div(most, 256), cap = 32ull * sms;
-    stage_kernel<<<dim3((unsigned)(want < cap ? want : cap), st.n, K), 256, 0, stream>>>(st.a);
-    return launched("operand copies");
+    return launch("operand copies", stage_kernel, dim3((unsigned)(want < cap ? want : cap), st.n, K), 256, 0, stream, st.a);
 }
 
 int encode(CUtensorMap* map, const Operand& o, bool mn)
@@ -333,22 +340,22 @@ int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, c
 }
 
 template <typename T, int MODE, int ACT>
-void launch_mat(const MatLaunch& L, uint32_t pairs, cudaStream_t st)
+int launch_mat(const MatLaunch& L, uint32_t pairs, cudaStream_t st)
 {
-    mat_kernel<T, MODE, ACT><<<2 * pairs, MatShape<T, MODE>::kThreads, MatShape<T, MODE>::kSmem, st>>>(L);
+    return launch("matrix kernel", mat_kernel<T, MODE, ACT>, dim3(2 * pairs), MatShape<T, MODE>::kThreads, MatShape<T, MODE>::kSmem, st, L);
 }
 
 template <typename T, int MODE>
-void launch_mat(const MatLaunch& L, int act, uint32_t pairs, cudaStream_t st)
+int launch_mat(const MatLaunch& L, int act, uint32_t pairs, cudaStream_t st)
 {
     if constexpr (MODE == MAT_PLAIN) {
-        launch_mat<T, MODE, 0>(L, pairs, st);
+        return launch_mat<T, MODE, 0>(L, pairs, st);
     } else {
         switch (act) {
-            case PALSGD_ACT_SILU: launch_mat<T, MODE, PALSGD_ACT_SILU>(L, pairs, st); break;
-            case PALSGD_ACT_GELU: launch_mat<T, MODE, PALSGD_ACT_GELU>(L, pairs, st); break;
-            case PALSGD_ACT_GELU_TANH: launch_mat<T, MODE, PALSGD_ACT_GELU_TANH>(L, pairs, st); break;
-            default: launch_mat<T, MODE, PALSGD_ACT_RELU>(L, pairs, st);
+            case PALSGD_ACT_SILU: return launch_mat<T, MODE, PALSGD_ACT_SILU>(L, pairs, st);
+            case PALSGD_ACT_GELU: return launch_mat<T, MODE, PALSGD_ACT_GELU>(L, pairs, st);
+            case PALSGD_ACT_GELU_TANH: return launch_mat<T, MODE, PALSGD_ACT_GELU_TANH>(L, pairs, st);
+            default: return launch_mat<T, MODE, PALSGD_ACT_RELU>(L, pairs, st);
         }
     }
 }
@@ -359,9 +366,7 @@ int run_mat(MatLaunch& L, const palsgd_ffn_shape* s, const Device& d, cudaStream
     if (L.tiles == 0) return PALSGD_OK;
     L.gave_up = d.gave_up;
     const uint32_t pairs = (uint32_t)(d.sms / 2) < L.tiles ? (uint32_t)(d.sms / 2) : L.tiles;
-    if (s->precision == PALSGD_PREC_FP32) launch_mat<float, MODE>(L, s->activation, pairs, st);
-    else launch_mat<bf16, MODE>(L, s->activation, pairs, st);
-    return launched("matrix kernel");
+    return s->precision == PALSGD_PREC_FP32 ? launch_mat<float, MODE>(L, s->activation, pairs, st) : launch_mat<bf16, MODE>(L, s->activation, pairs, st);
 }
 
 void set_saved(MatLaunch& L, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e, const palsgd_mat* up_e)
@@ -478,11 +483,11 @@ int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
     const dim3 grid(p.a.ctas[0] + p.a.ctas[1], s->K);
     const size_t sm = BACK ? (kQkThreads / 32) * (size_t)s->head_dim * sizeof(float) : 0;
     constexpr int W = 16 / (int)sizeof(T);
-    if (p.V == W && p.NS == 1) qk_kernel<T, W, 1, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
-    else if (p.V == W) qk_kernel<T, W, 2, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
-    else if (p.NS <= 2) qk_kernel<T, 1, 2, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
-    else qk_kernel<T, 1, 8, BACK, INTER><<<grid, kQkThreads, sm, st>>>(p.a);
-    return launched("q/k norm + rotation");
+    const char* what = "q/k norm + rotation";
+    if (p.V == W && p.NS == 1) return launch(what, qk_kernel<T, W, 1, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
+    if (p.V == W) return launch(what, qk_kernel<T, W, 2, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
+    if (p.NS <= 2) return launch(what, qk_kernel<T, 1, 2, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
+    return launch(what, qk_kernel<T, 1, 8, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
 }
 
 template <bool BACK>
@@ -611,9 +616,7 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
             z.rows[i] = (uint32_t)(i < 2 ? F : D); z.cols[i] = (uint32_t)(i < 2 ? D : F);
         }
         const dim3 grid((unsigned)(F > D ? F : D) < 1024u ? (unsigned)(F > D ? F : D) : 1024u, 3, s->K);
-        if (es == 4) zero_kernel<float><<<grid, 256, 0, st>>>(z);
-        else zero_kernel<bf16><<<grid, 256, 0, st>>>(z);
-        return launched("zero weight gradients");
+        return launch("zero weight gradients", es == 4 ? zero_kernel<float> : zero_kernel<bf16>, grid, 256, 0, st, z);
     }
     Device dev{};
     BLOCK_TRY(device_of(dev));
@@ -738,7 +741,5 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
     sum.head_dim = s->head_dim;
     const dim3 grid((unsigned)ceil_div(s->head_dim, 32), 2, s->K);
     if (s->tokens) BLOCK_TRY(run_qk<true>(p, s, st));
-    if (s->precision == PALSGD_PREC_FP32) qk_sum_kernel<float><<<grid, 256, 0, st>>>(sum);
-    else qk_sum_kernel<bf16><<<grid, 256, 0, st>>>(sum);
-    return launched("q/k weight gradient");
+    return launch("q/k weight gradient", s->precision == PALSGD_PREC_FP32 ? qk_sum_kernel<float> : qk_sum_kernel<bf16>, grid, 256, 0, st, sum);
 }

@@ -11,6 +11,12 @@ namespace block {
 
 using bf16 = __nv_bfloat16;
 
+// Kernels of this library are launched so that one may start up while the kernel before it in the stream is still
+// running (launch() in the host file): each lets the next one start at once, and touches no memory of others' before
+// that kernel is complete.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
 template <typename T> __device__ __forceinline__ T from_f(float v);

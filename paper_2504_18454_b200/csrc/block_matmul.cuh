@@ -475,6 +475,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
+    let_next_start();
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < kStages; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); }
         for (uint32_t s = 0; s < 2; ++s) { bar_init(acc_full + 8 * s, 1); bar_init(acc_empty + 8 * s, 2 * Shape::kEpilogue); }
@@ -490,6 +491,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at));
+    wait_for_previous();
 
     if (warp == 0 || warp == 3) {
         // producers: warp 0 brings A, warp 3 brings B (one thread that did both held the copy engine up: 410 ns a step of
@@ -826,6 +828,8 @@ struct StageArgs { StageItem item[kMaxStaged]; };
 
 __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ StageArgs a)
 {
+    let_next_start();
+    wait_for_previous();
     const StageItem& it = a.item[blockIdx.y];
     const uint32_t per = (uint32_t)(it.ld / 8);
     const int64_t k = blockIdx.z;
@@ -878,6 +882,8 @@ struct ZeroArgs { void* p[3]; int64_t w[3], r[3]; uint32_t rows[3], cols[3]; };
 template <typename T>
 __global__ void __launch_bounds__(256) zero_kernel(const __grid_constant__ ZeroArgs a)
 {
+    let_next_start();
+    wait_for_previous();
     const uint32_t i = blockIdx.y;
     T* p = static_cast<T*>(a.p[i]) + (int64_t)blockIdx.z * a.w[i];
     for (uint32_t r = blockIdx.x; r < a.rows[i]; r += gridDim.x)

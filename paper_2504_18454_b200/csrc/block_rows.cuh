@@ -23,6 +23,8 @@ struct Act8Args {
 template <typename T, int V, bool PACK>
 __global__ void __launch_bounds__(256) act8_kernel(const __grid_constant__ Act8Args a)
 {
+    let_next_start();
+    wait_for_previous();
     constexpr int kLanes = 32 / V;
     T* const x = static_cast<T*>(a.x) + (int64_t)blockIdx.y * a.xw;
     int8_t* const q = a.q + (int64_t)blockIdx.y * a.qw;
@@ -385,6 +387,8 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta)
 template <typename T, int V, int NS, bool BACK, bool INTER>
 __global__ void __launch_bounds__(kQkThreads, NS == 1 ? (BACK ? 4 : 5) : 1) qk_kernel(const __grid_constant__ QkArgs a)
 {
+    let_next_start();
+    wait_for_previous();
     if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, INTER, 0>(a, blockIdx.x);
     else qk_walk<T, V, NS, BACK, INTER, 1>(a, blockIdx.x - a.ctas[0]);
 }
@@ -402,6 +406,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) qk_sum_kernel(const __grid_constant__ QkSumArgs a)
 {
     __shared__ float run[8][32];
+    let_next_start();
+    wait_for_previous();
     const uint32_t side = blockIdx.y, k = blockIdx.z;
     if (a.heads[side] == 0) return;
     const uint32_t i = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
