@@ -106,6 +106,13 @@ int sm_count()
     return n;
 }
 
+Divisor divisor(uint32_t d)
+{
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+}
+
 // ------------------------------------------------------------------------------------------------ 8-bit checkpoints
 
 int check_act8(int32_t prec, uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x, const palsgd_mat* q,
@@ -124,12 +131,14 @@ int launch_act8(uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x, c
 {
     if (rows == 0 || cols == 0) return PALSGD_OK;
     Act8Args a{x->data, static_cast<int8_t*>(q->data), static_cast<uint8_t*>(e->data), x->worker_stride, x->row_stride,
-               q->worker_stride, q->row_stride, e->worker_stride, e->row_stride, rows, cols, 0, 0};
+               q->worker_stride, q->row_stride, e->worker_stride, e->row_stride, rows, cols, 0, {}, 0};
     const bool wide = cols % 8 == 0 && aligned(x->data, 16) && (x->row_stride * sizeof(T)) % 16 == 0 && (x->worker_stride * sizeof(T)) % 16 == 0 &&
                       aligned(q->data, 8) && q->row_stride % 8 == 0 && q->worker_stride % 8 == 0;
-    a.units_per_row = (uint32_t)(ceil_div(cols, 32) * (wide ? 4 : 32));
-    a.units = rows * a.units_per_row;
-    const uint64_t ctas = ceil_div(a.units, 256), most = 64ull * sm_count();
+    const uint64_t per_row = ceil_div(cols, 32) * (wide ? 4 : 32);
+    a.units = rows * per_row;
+    a.per_row = per_row < 0x80000000ull ? divisor((uint32_t)per_row) : Divisor{(uint32_t)per_row, 0, 0};
+    a.flat = cols % 32 == 0 && (rows == 1 || (x->row_stride == (int64_t)cols && q->row_stride == (int64_t)cols && e->row_stride == (int64_t)(cols / 32)));
+    const uint64_t ctas = ceil_div(a.units, 1024), most = 8ull * sm_count();
     const dim3 grid((unsigned)(ctas < most ? ctas : most), K);
     return launch(PACK ? "act8 pack" : "act8 unpack", wide ? act8_kernel<T, 8, PACK> : act8_kernel<T, 1, PACK>, grid, 256, 0, st, a);
 }
@@ -310,13 +319,6 @@ MatOut out_of(const palsgd_mat* m, uint64_t cols, size_t es)
 }
 MatOut out_of(const Operand& o) { return MatOut{const_cast<void*>(o.p), o.w, o.r, o.part, 1, (uint32_t)o.r}; }
 
-Divisor divisor(uint32_t d)
-{
-    uint32_t s = 0;
-    while ((1ull << s) < d) ++s;
-    return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
-}
-
 // One product appended to a launch; B1/A1: the second segment, or (gate/up) the up weights as B1.
 int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, const Operand* A0, const Operand* A1, bool amn,
                 const Operand* B0, const Operand* B1, bool bmn, uint32_t n_step)
@@ -481,13 +483,12 @@ template <typename T, bool BACK, bool INTER>
 int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
 {
     const dim3 grid(p.a.ctas[0] + p.a.ctas[1], s->K);
-    const size_t sm = BACK ? (kQkThreads / 32) * (size_t)s->head_dim * sizeof(float) : 0;
     constexpr int W = 16 / (int)sizeof(T);
     const char* what = "q/k norm + rotation";
-    if (p.V == W && p.NS == 1) return launch(what, qk_kernel<T, W, 1, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
-    if (p.V == W) return launch(what, qk_kernel<T, W, 2, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
-    if (p.NS <= 2) return launch(what, qk_kernel<T, 1, 2, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
-    return launch(what, qk_kernel<T, 1, 8, BACK, INTER>, grid, kQkThreads, sm, st, p.a);
+    if (p.V == W && p.NS == 1) return launch(what, qk_kernel<T, W, 1, BACK, INTER>, grid, kQkThreads, qk_smem(W, 1, BACK, s->head_dim), st, p.a);
+    if (p.V == W) return launch(what, qk_kernel<T, W, 2, BACK, INTER>, grid, kQkThreads, qk_smem(W, 2, BACK, s->head_dim), st, p.a);
+    if (p.NS <= 2) return launch(what, qk_kernel<T, 1, 2, BACK, INTER>, grid, kQkThreads, qk_smem(1, 2, BACK, s->head_dim), st, p.a);
+    return launch(what, qk_kernel<T, 1, 8, BACK, INTER>, grid, kQkThreads, qk_smem(1, 8, BACK, s->head_dim), st, p.a);
 }
 
 template <bool BACK>

@@ -68,32 +68,12 @@ template <> struct Vec<bf16, 8> {
     }
 };
 
-// V values as they lie in memory (16 bytes, or one value), to be kept in registers until they are needed.
-template <typename T, int V> struct Raw { uint4 r; };
-template <typename T> struct Raw<T, 1> { T r; };
-template <typename T, int V> __device__ __forceinline__ void raw_zero(Raw<T, V>& o)
-{
-    if constexpr (V == 1) o.r = from_f<T>(0.0f);
-    else o.r = make_uint4(0, 0, 0, 0);
-}
-template <typename T, int V> __device__ __forceinline__ void raw_load(Raw<T, V>& o, const T* p)
-{
-    if constexpr (V == 1) o.r = *p;
-    else o.r = __ldg(reinterpret_cast<const uint4*>(p));
-}
-template <typename T, int V> __device__ __forceinline__ void raw_get(const Raw<T, V>& o, float* v)
-{
-    if constexpr (V == 1) {
-        v[0] = to_f(o.r);
-    } else {
-        const uint32_t w[4] = {o.r.x, o.r.y, o.r.z, o.r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i]);
-            else { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-        }
-    }
-}
+// Division of t < 2^31 by a divisor d known on the host: with s = ceil(log2 d) and m = ceil(2^(31+s) / d) < 2^32, the
+// quotient is t m >> (31 + s) (m d exceeds 2^(31+s) by less than 2^s, and t times that stays below 2^(31+s)).
+struct Divisor {
+    uint32_t d, m, s;
+    __device__ __forceinline__ uint32_t of(uint32_t t) const { return (uint32_t)(((uint64_t)t * m) >> (31 + s)); }
+};
 
 // ---- two binary32 values in one 64-bit register: multiply and multiply-add of both in one instruction
 using f2 = unsigned long long;

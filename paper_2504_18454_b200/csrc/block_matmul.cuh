@@ -54,13 +54,6 @@ struct MatOut {
     uint32_t cols;                // columns that may be written: the workspace's rows have room behind their end
 };
 
-// Division of t < 2^31 by a divisor d known on the host: with s = ceil(log2 d) and m = ceil(2^(31+s) / d) < 2^32, the
-// quotient is t m >> (31 + s) (m d exceeds 2^(31+s) by less than 2^s, and t times that stays below 2^(31+s)).
-struct Divisor {
-    uint32_t d, m, s;
-    __device__ __forceinline__ uint32_t of(uint32_t t) const { return (uint32_t)(((uint64_t)t * m) >> (31 + s)); }
-};
-
 struct alignas(64) MatProblem {
     CUtensorMap A[2], B[2];       // by segment; the gate/up pass: B[0] gate, B[1] up
     uint32_t M, N, Kd, tiles;

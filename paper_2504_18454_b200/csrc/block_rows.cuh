@@ -14,60 +14,82 @@ struct Act8Args {
     uint8_t* e;
     int64_t  xw, xr, qw, qr, ew, er;
     uint64_t rows, cols;
-    uint32_t units_per_row;       // pieces of V values, padded to whole groups
-    uint64_t units;               // rows * units_per_row
+    uint64_t units;               // rows * (pieces of V values of a row, padded to whole groups)
+    Divisor  per_row;             // those pieces (units < 2^31)
+    int      flat;                // rows follow one another in x, q and e without gaps: one long row
 };
 
-// A unit is V consecutive values, 32/V lanes share a group, and a thread takes one unit: 16 (bf16) or 32 (fp32) bytes
-// of x and 8 of q a lane where the layout allows (V = 8), else one value (V = 1, a warp is a group).
+// A unit is V consecutive values, 32/V lanes share a group, and a thread takes four units 256 apart: 16 (bf16) or 32 (fp32)
+// bytes of x and 8 of q each where the layout allows (V = 8), else one value (V = 1, a warp is a group).  Four units in
+// flight a thread: with one, the loads that a full SM has under way do not cover the memory's latency.
 template <typename T, int V, bool PACK>
 __global__ void __launch_bounds__(256) act8_kernel(const __grid_constant__ Act8Args a)
 {
     let_next_start();
     wait_for_previous();
-    constexpr int kLanes = 32 / V;
+    constexpr int kLanes = 32 / V, U = 4;
     T* const x = static_cast<T*>(a.x) + (int64_t)blockIdx.y * a.xw;
     int8_t* const q = a.q + (int64_t)blockIdx.y * a.qw;
     uint8_t* const e = a.e + (int64_t)blockIdx.y * a.ew;
-    const uint64_t step = (uint64_t)gridDim.x * blockDim.x;
-    const uint64_t end = (a.units + 31) / 32 * 32;       // whole warps take part in the exchange below
-    for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < end; i += step) {
-        uint64_t row = a.units < 0x80000000ull ? (uint32_t)i / a.units_per_row : i / a.units_per_row;
-        const uint64_t c = (i - row * a.units_per_row) * V;
-        const bool on = row < a.rows && c < a.cols;
-        if (!on) row = 0;
-        const int64_t xo = (int64_t)row * a.xr + (int64_t)c, qo = (int64_t)row * a.qr + (int64_t)c;
-        const int64_t eo = (int64_t)row * a.er + (int64_t)(c / 32);
-        float v[V];
-        if constexpr (PACK) {
+    const uint64_t step = (uint64_t)gridDim.x * (256 * U);
+    for (uint64_t base = (uint64_t)blockIdx.x * (256 * U); base < a.units; base += step) {
+        int64_t xo[U], qo[U], eo[U];
+        bool on[U];
+        float v[U][V];
+        uint2 w[U];
+        uint8_t E[U];
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = 0.0f;
-            if (on) Vec<T, V>::load(x + xo, v);
-            float m = 0.0f;
-#pragma unroll
-            for (int j = 0; j < V; ++j) m = act8_max(m, v[j]);
-#pragma unroll
-            for (int s = kLanes / 2; s; s >>= 1) m = act8_max(m, __shfl_xor_sync(0xFFFFFFFFu, m, s));
-            const uint32_t E = act8_exponent(m);
-            const float inv = act8_inverse(E);
-            if (on) {
-                if constexpr (V == 8) {
-                    *reinterpret_cast<uint2*>(q + qo) = make_uint2(act8_quant4(v[0], v[1], v[2], v[3], inv), act8_quant4(v[4], v[5], v[6], v[7], inv));
-                } else {
-                    q[qo] = (int8_t)act8_quant4(v[0], 0.0f, 0.0f, 0.0f, inv);
-                }
-                if (threadIdx.x % kLanes == 0) e[eo] = (uint8_t)E;
-            }
-        } else if (on) {
-            const float s = act8_step(e[eo]);
-            if constexpr (V == 8) {
-                const uint2 w = __ldg(reinterpret_cast<const uint2*>(q + qo));
-                act8_value4(w.x, s, v);
-                act8_value4(w.y, s, v + 4);
+        for (int u = 0; u < U; ++u) {
+            const uint64_t i = base + u * 256 + threadIdx.x;
+            if (a.flat) {
+                on[u] = i < a.units;
+                xo[u] = qo[u] = (int64_t)i * V;
+                eo[u] = (int64_t)(i / kLanes);
             } else {
-                v[0] = (float)q[qo] * s;
+                const uint64_t row = a.units < 0x80000000ull ? a.per_row.of((uint32_t)i) : i / a.per_row.d;
+                const uint64_t c = (i - row * a.per_row.d) * V;
+                on[u] = i < a.units && c < a.cols;
+                xo[u] = (int64_t)row * a.xr + (int64_t)c;
+                qo[u] = (int64_t)row * a.qr + (int64_t)c;
+                eo[u] = (int64_t)row * a.er + (int64_t)(c / 32);
             }
-            Vec<T, V>::store(x + xo, v);
+            if constexpr (PACK) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[u][j] = 0.0f;
+                if (on[u]) Vec<T, V>::load(x + xo[u], v[u]);
+            } else if (on[u]) {
+                E[u] = __ldg(e + eo[u]);
+                if constexpr (V == 8) w[u] = __ldg(reinterpret_cast<const uint2*>(q + qo[u]));
+                else w[u].x = (uint8_t)q[qo[u]];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (PACK) {
+                float m = 0.0f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) m = act8_max(m, v[u][j]);
+#pragma unroll
+                for (int s = kLanes / 2; s; s >>= 1) m = act8_max(m, __shfl_xor_sync(0xFFFFFFFFu, m, s));
+                const uint32_t ex = act8_exponent(m);
+                const float inv = act8_inverse(ex);
+                if (on[u]) {
+                    if constexpr (V == 8)
+                        *reinterpret_cast<uint2*>(q + qo[u]) = make_uint2(act8_quant4(v[u][0], v[u][1], v[u][2], v[u][3], inv), act8_quant4(v[u][4], v[u][5], v[u][6], v[u][7], inv));
+                    else
+                        q[qo[u]] = (int8_t)act8_quant4(v[u][0], 0.0f, 0.0f, 0.0f, inv);
+                    if (threadIdx.x % kLanes == 0) e[eo[u]] = (uint8_t)ex;
+                }
+            } else if (on[u]) {
+                const float s = act8_step(E[u]);
+                if constexpr (V == 8) {
+                    act8_value4(w[u].x, s, v[u]);
+                    act8_value4(w[u].y, s, v[u] + 4);
+                } else {
+                    v[u][0] = (float)(int8_t)w[u].x * s;
+                }
+                Vec<T, V>::store(x + xo[u], v[u]);
+            }
         }
     }
 }
@@ -75,6 +97,13 @@ __global__ void __launch_bounds__(256) act8_kernel(const __grid_constant__ Act8A
 // ------------------------------------------------------------------------------------------------ q/k norm + rotation
 
 constexpr uint32_t kQkThreads = 128;
+// items of a warp under way at a time, and a CTA's shared memory: the ring, or the warps' sums of the weight gradient
+__host__ __device__ constexpr int qk_ring(int V, int NS) { return V == 1 ? 1 : NS == 1 ? 4 : 2; }
+__host__ __device__ constexpr uint32_t qk_smem(int V, int NS, bool back, uint32_t head_dim)
+{
+    const uint32_t ring = V == 1 ? 0 : qk_ring(V, NS) * NS * 2 * (back ? 2 : 1) * 16 * kQkThreads, sums = back ? kQkThreads / 32 * head_dim * 4 : 0;
+    return ring > sums ? ring : sums;
+}
 
 struct HeadsArg {
     const void* x;                // input heads
@@ -101,29 +130,17 @@ struct QkArgs {
     float    eps;
 };
 
-// What a lane holds of one head under way: the two vectors of each of its NS slots, as they lie in memory.
-template <typename T, int V, int NS, bool BACK>
-struct QkItem {
-    Raw<T, V> x[NS][2], d[BACK ? NS : 1][2];
-    int64_t out;
-    bool live;
-};
-
-// The 2V values of a slot as V pairs of floats.
+// The 2V values of a slot as V pairs of floats, from the two vectors as they lie in memory.
 template <typename T, int V>
-__device__ __forceinline__ void slot_get(const Raw<T, V> (&r)[2], f2 (&v)[V])
+__device__ __forceinline__ void slot_get(const uint4 (&r)[2], f2 (&v)[V])
 {
-    if constexpr (V == 1) {
-        v[0] = f2_of(to_f(r[0].r), to_f(r[1].r));
-    } else {
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const uint32_t w[4] = {r[p].r.x, r[p].r.y, r[p].r.z, r[p].r.w};
+    for (int p = 0; p < 2; ++p) {
+        const uint32_t w[4] = {r[p].x, r[p].y, r[p].z, r[p].w};
 #pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                if constexpr (sizeof(T) == 2) v[p * (V / 2) + i] = f2_wide(w[i]);
-                else v[p * (V / 2) + i] = f2_of(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-            }
+        for (int i = 0; i < V / 2; ++i) {
+            if constexpr (sizeof(T) == 2) v[p * (V / 2) + i] = f2_wide(w[i]);
+            else v[p * (V / 2) + i] = f2_of(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
         }
     }
 }
@@ -157,12 +174,13 @@ __device__ __forceinline__ void slot_put(T* base, const uint32_t (&at)[2], const
 // halves of its rotation pairs, so the rotation needs no exchange: for split halves vectors s and s + rot/(2V), for
 // interleaved pairs two neighbouring vectors (V > 1: the pairs lie inside a vector; V = 1: the slot is the pair).  Values
 // that are not rotated are pairs of angle zero.  The only exchanges are the sums over a head.
-// It moves 4 bytes a value forward (bfloat16) and is bound by instructions before it is by memory: the arithmetic is in
-// pairs of floats, and what depends on the token and not on the head is formed once per token (forward the products of
-// weights and angles), so a warp's groups are spread over heads only as far as leaves four heads or so in a row to each.
-// The next item is under way while one is worked on.
+// It moves 4 bytes a value forward (bfloat16), and instructions weigh as much as memory: the arithmetic is in pairs of
+// floats, and what depends on the token and not on the head is formed once per token (forward the products of weights and
+// angles), so a warp's groups are spread over heads only as far as leaves four heads or so in a row to each.  Each lane
+// brings what it will work on into shared memory by asynchronous copies, kRing items ahead (held in registers, one item
+// ahead was all there was room for).  V = 1, for layouts without 16-byte boundaries, reads directly.
 template <typename T, int V, int NS, bool BACK, bool INTER, int SIDE>
-__device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta)
+__device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, unsigned char* smem)
 {
     constexpr bool kInside = INTER || V == 1;                                 // a rotation pair is one f2 (else: f2 i and V/2 + i)
     constexpr int H = V / 2;
@@ -201,40 +219,57 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta)
     const uint64_t step = (uint64_t)ctas * kWarps * tokens, start = ((uint64_t)cta * kWarps + warp) * tokens;
     const uint64_t turns = start < a.tokens ? (a.tokens - 1 - start) / step + 1 : 0;      // token groups of this warp
 
-    using Item = QkItem<T, V, NS, BACK>;
     // where the next item to be fetched lies
+    constexpr int kRing = qk_ring(V, NS), kVecs = NS * 2 * (BACK ? 2 : 1);    // items under way; 16-byte pieces of one a lane
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(smem) + (warp * (kRing * kVecs) * 32 + lane) * 16;
     const T* const xb = static_cast<const T*>(h.x) + (int64_t)k * h.xw;
     const T* const db = static_cast<const T*>(h.d) + (int64_t)k * h.dw;
     T* const ob = static_cast<T*>(h.out) + (int64_t)k * h.ow;
     uint64_t ft = start + my_token;
     uint32_t fh = first;
-    int64_t fx = (int64_t)ft * h.xt + (int64_t)fh * h.xh, fd = (int64_t)ft * h.dt + (int64_t)fh * h.dh, fo = (int64_t)ft * h.ot + (int64_t)fh * h.oh;
+    int64_t fx = (int64_t)ft * h.xt + (int64_t)fh * h.xh, fd = (int64_t)ft * h.dt + (int64_t)fh * h.dh;
     uint64_t left = turns * rounds;
-    auto fetch = [&](Item& it) {
-        it.live = ft < a.tokens && fh < h.heads;
-        it.out = fo;
+    auto fetch = [&](uint32_t slot) {
+        if constexpr (V > 1) {
+            if (left) {
+                if (ft < a.tokens && fh < h.heads) {
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+                    for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const bool on = it.live && at[s][p] != ~0u;
-                raw_zero(it.x[s][p]);
-                if (on) raw_load(it.x[s][p], xb + fx + at[s][p]);
-                if constexpr (BACK) {
-                    raw_zero(it.d[s][p]);
-                    if (on) raw_load(it.d[s][p], db + fd + at[s][p]);
+                        for (int p = 0; p < 2; ++p)
+                            if (at[s][p] != ~0u) {
+                                const uint32_t to = mine + (slot * kVecs + s * 2 + p) * 512;
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(xb + fx + at[s][p]) : "memory");
+                                if constexpr (BACK)
+                                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + NS * 2 * 512), "l"(db + fd + at[s][p]) : "memory");
+                            }
+                }
+                --left;
+                fh += abreast;
+                if (fh - first == rounds * abreast) {
+                    ft += step;
+                    fh = first;
+                    fx = (int64_t)ft * h.xt + (int64_t)fh * h.xh;
+                    if constexpr (BACK) fd = (int64_t)ft * h.dt + (int64_t)fh * h.dh;
+                } else {
+                    fx += abreast * h.xh;
+                    if constexpr (BACK) fd += abreast * h.dh;
                 }
             }
-        --left;
-        fh += abreast;
-        if (fh - first == rounds * abreast) {
-            ft += step;
-            fh = first;
-            fx = (int64_t)ft * h.xt + (int64_t)fh * h.xh; fo = (int64_t)ft * h.ot + (int64_t)fh * h.oh;
-            if constexpr (BACK) fd = (int64_t)ft * h.dt + (int64_t)fh * h.dh;
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    // an item's values: from its place in the ring, or (V = 1) from memory
+    auto values = [&](uint32_t slot, bool second, int s, const T* from, f2 (&v)[V]) {
+        if constexpr (V > 1) {
+            uint4 r[2];
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[p].x), "=r"(r[p].y), "=r"(r[p].z), "=r"(r[p].w)
+                             : "r"(mine + (slot * kVecs + (second ? NS * 2 : 0) + s * 2 + p) * 512));
+            slot_get<T, V>(r, v);
         } else {
-            fx += abreast * h.xh; fo += abreast * h.oh;
-            if constexpr (BACK) fd += abreast * h.dh;
+            v[0] = f2_of(from && at[s][0] != ~0u ? to_f(from[at[s][0]]) : 0.0f, from && at[s][1] != ~0u ? to_f(from[at[s][1]]) : 0.0f);
         }
     };
     auto over_head = [&](f2 v2) {
@@ -252,116 +287,136 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta)
     };
     auto weight = [&](int s, int i) { return f2_of(to_f(w[s][2 * i]), to_f(w[s][2 * i + 1])); };
 
-    Item next;
-    if (left) fetch(next);
-    int32_t pos_next = position(0);
-    for (uint64_t turn = 0; turn < turns; ++turn) {
-        const int32_t pos = pos_next;
-        if (turn + 1 < turns) pos_next = position(turn + 1);
+    // of the pairs of each f2 of the token: cosines and, with the signs of the rotation, sines; forward: times the weights
+    f2 mc[NS][V], ms[NS][V];
+    float bad = 0.0f;
+    auto token = [&](int32_t pos) {
         const bool ok = !a.rot || (pos >= 0 && (uint64_t)pos < a.table_rows);
-        // of the pairs of each f2: cosines and, with the signs of the rotation, sines; forward: times the weights
-        f2 mc[NS][V], ms[NS][V];
-        {
-            const float* ct = a.cos_t + (ok ? (uint64_t)pos * half : 0);
-            const float* st = a.sin_t + (ok ? (uint64_t)pos * half : 0);
+        const float* ct = a.cos_t + (ok ? (uint64_t)pos * half : 0);
+        const float* st = a.sin_t + (ok ? (uint64_t)pos * half : 0);
+        bad = ok ? 0.0f : __uint_as_float(0x7FFFFFFFu);                       // outside the table: NaN
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                float c[V], sn[V];
-                const uint32_t i = (s * a.lanes + sub) * V;                   // first pair of the slot
-                if (V > 1 && a.table_wide && i + V <= half && ok) {
-                    if constexpr (V > 1) {
+        for (int s = 0; s < NS; ++s) {
+            float c[V], sn[V];
+            const uint32_t i = (s * a.lanes + sub) * V;                       // first pair of the slot
+            if (V > 1 && a.table_wide && i + V <= half && ok) {
+                if constexpr (V > 1) {
 #pragma unroll
-                        for (int j = 0; j < V; j += 4) { Vec<float, 4>::load(ct + i + j, c + j); Vec<float, 4>::load(st + i + j, sn + j); }
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const bool on = i + j < half && ok;
-                        c[j] = on ? __ldg(ct + i + j) : 1.0f;
-                        sn[j] = on ? __ldg(st + i + j) : 0.0f;
-                    }
+                    for (int j = 0; j < V; j += 4) { Vec<float, 4>::load(ct + i + j, c + j); Vec<float, 4>::load(st + i + j, sn + j); }
                 }
-                if constexpr (kInside) {
+            } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        mc[s][j] = f2_of(c[j], c[j]);
-                        ms[s][j] = BACK ? f2_of(sn[j], -sn[j]) : f2_of(-sn[j], sn[j]);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < H; ++j) {
-                        mc[s][j] = mc[s][H + j] = f2_of(c[2 * j], c[2 * j + 1]);
-                        const f2 q = f2_of(sn[2 * j], sn[2 * j + 1]);
-                        ms[s][j] = BACK ? q : f2_neg(q);
-                        ms[s][H + j] = BACK ? f2_neg(q) : q;
-                    }
+                for (int j = 0; j < V; ++j) {
+                    const bool on = i + j < half && ok;
+                    c[j] = on ? __ldg(ct + i + j) : 1.0f;
+                    sn[j] = on ? __ldg(st + i + j) : 0.0f;
                 }
-                if constexpr (!BACK) {                                        // value times its own weight, partner times the partner's
-                    f2 wf[V];
+            }
+            if constexpr (kInside) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) wf[j] = weight(s, j);
+                for (int j = 0; j < V; ++j) {
+                    mc[s][j] = f2_of(c[j], c[j]);
+                    ms[s][j] = BACK ? f2_of(sn[j], -sn[j]) : f2_of(-sn[j], sn[j]);
+                }
+            } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        mc[s][j] = f2_mul(mc[s][j], wf[j]);
-                        ms[s][j] = f2_mul(ms[s][j], kInside ? f2_swap(wf[j]) : wf[(j + H) % V]);
-                    }
+                for (int j = 0; j < H; ++j) {
+                    mc[s][j] = mc[s][H + j] = f2_of(c[2 * j], c[2 * j + 1]);
+                    const f2 q = f2_of(sn[2 * j], sn[2 * j + 1]);
+                    ms[s][j] = BACK ? q : f2_neg(q);
+                    ms[s][H + j] = BACK ? f2_neg(q) : q;
+                }
+            }
+            if constexpr (!BACK) {                                            // value times its own weight, partner times the partner's
+                f2 wf[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) wf[j] = weight(s, j);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    mc[s][j] = f2_mul(mc[s][j], wf[j]);
+                    ms[s][j] = f2_mul(ms[s][j], kInside ? f2_swap(wf[j]) : wf[(j + H) % V]);
                 }
             }
         }
-        const float bad = ok ? 0.0f : __uint_as_float(0x7FFFFFFFu);           // outside the table: NaN
-        for (uint32_t round = 0; round < rounds; ++round) {
-            const Item it = next;
-            if (left) fetch(next);
-            f2 x[NS][V], sq = 0;
+    };
+    auto work = [&](uint32_t slot, bool live, int64_t xo, int64_t go, int64_t oo) {
+        f2 x[NS][V], sq = 0;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            values(slot, false, s, live ? xb + xo : nullptr, x[s]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sq = f2_fma(x[s][j], x[s][j], sq);
+        }
+        // (a head that is not there: 0, so that what its place in the ring still holds adds nothing to the weight gradient)
+        const float mean = fmaf(over_head(sq), inv_n, a.eps), r = live ? rsqrtf(mean) + bad : 0.0f;
+        const f2 rr = f2_of(r, r);
+        f2 y[NS][V];
+        if constexpr (!BACK) {
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                slot_get<T, V>(it.x[s], x[s]);
 #pragma unroll
-                for (int j = 0; j < V; ++j) sq = f2_fma(x[s][j], x[s][j], sq);
+                for (int j = 0; j < V; ++j) x[s][j] = f2_mul(x[s][j], rr);
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    y[s][j] = f2_fma(x[s][j], mc[s][j], f2_mul(kInside ? f2_swap(x[s][j]) : x[s][(j + H) % V], ms[s][j]));
             }
-            const float r = rsqrtf(fmaf(over_head(sq), inv_n, a.eps)) + bad;
-            const f2 rr = f2_of(r, r);
-            f2 y[NS][V];
-            if constexpr (!BACK) {
+        } else {
+            f2 dot = 0;
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
+            for (int s = 0; s < NS; ++s) {
+                f2 d[V];
+                values(slot, true, s, live ? db + go : nullptr, d);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) x[s][j] = f2_mul(x[s][j], rr);
-#pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        y[s][j] = f2_fma(x[s][j], mc[s][j], f2_mul(kInside ? f2_swap(x[s][j]) : x[s][(j + H) % V], ms[s][j]));
+                for (int j = 0; j < V; ++j) {
+                    y[s][j] = f2_fma(d[j], mc[s][j], f2_mul(kInside ? f2_swap(d[j]) : d[(j + H) % V], ms[s][j]));
+                    x[s][j] = f2_mul(x[s][j], rr);                            // xh
+                    acc[s][j] = f2_fma(y[s][j], x[s][j], acc[s][j]);
+                    y[s][j] = f2_mul(y[s][j], weight(s, j));
+                    dot = f2_fma(y[s][j], x[s][j], dot);
                 }
-            } else {
-                f2 dot = 0;
-#pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    f2 d[V];
-                    slot_get<T, V>(it.d[s], d);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        y[s][j] = f2_fma(d[j], mc[s][j], f2_mul(kInside ? f2_swap(d[j]) : d[(j + H) % V], ms[s][j]));
-                        x[s][j] = f2_mul(x[s][j], rr);                        // xh
-                        acc[s][j] = f2_fma(y[s][j], x[s][j], acc[s][j]);
-                        y[s][j] = f2_mul(y[s][j], weight(s, j));
-                        dot = f2_fma(y[s][j], x[s][j], dot);
-                    }
-                }
-                const float m = over_head(dot) * -inv_n;
-                const f2 mm = f2_of(m, m);
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) y[s][j] = f2_mul(rr, f2_fma(x[s][j], mm, y[s][j]));
             }
-            if (it.live) {
+            const float m = over_head(dot) * -inv_n;
+            const f2 mm = f2_of(m, m);
 #pragma unroll
-                for (int s = 0; s < NS; ++s) slot_put<T, V>(ob + it.out, at[s], y[s]);
-            }
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int j = 0; j < V; ++j) y[s][j] = f2_mul(rr, f2_fma(x[s][j], mm, y[s][j]));
+        }
+        if (live) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) slot_put<T, V>(ob + oo, at[s], y[s]);
+        }
+    };
+
+    if constexpr (V > 1) {                                                    // a lane without a vector reads zeros
+#pragma unroll
+        for (int i = 0; i < kRing * kVecs; ++i)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(mine + i * 512), "r"(0) : "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) fetch(i);
+    int32_t pos_next = position(0);
+    uint32_t slot = 0;
+    for (uint64_t turn = 0; turn < turns; ++turn) {
+        const int32_t pos = pos_next;
+        if (turn + 1 < turns) pos_next = position(turn + 1);
+        token(pos);
+        const uint64_t tk = start + turn * step + my_token;
+        const bool in = tk < a.tokens;
+        int64_t xo = (int64_t)tk * h.xt + (int64_t)first * h.xh, go = (int64_t)tk * h.dt + (int64_t)first * h.dh, oo = (int64_t)tk * h.ot + (int64_t)first * h.oh;
+        for (uint32_t hd = first; hd - first < rounds * abreast; hd += abreast) {
+            fetch(slot == 0 ? kRing - 1 : slot - 1);                          // into the place of the item before this one
+            if constexpr (V > 1) asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+            work(slot, in && hd < h.heads, xo, go, oo);
+            slot = slot + 1 == kRing ? 0 : slot + 1;
+            if constexpr (V == 1) { xo += abreast * h.xh; go += abreast * h.dh; }
+            oo += abreast * h.oh;
         }
     }
     if constexpr (BACK) {
         // the CTA's sum in a fixed order: groups of a warp by a butterfly, then the warps one after another
-        extern __shared__ float sum[];                                        // [kWarps][head_dim]
+        __syncthreads();                                                      // (the ring is done with)
+        float* const sum = reinterpret_cast<float*>(smem);                    // [kWarps][head_dim]
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -385,12 +440,13 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta)
 
 // (Two copies of the walk: with the side a constant its strides are constants of the instruction, not loads by index.)
 template <typename T, int V, int NS, bool BACK, bool INTER>
-__global__ void __launch_bounds__(kQkThreads, NS == 1 ? (BACK ? 4 : 5) : 1) qk_kernel(const __grid_constant__ QkArgs a)
+__global__ void __launch_bounds__(kQkThreads, NS == 1 ? 4 : 1) qk_kernel(const __grid_constant__ QkArgs a)
 {
     let_next_start();
     wait_for_previous();
-    if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, INTER, 0>(a, blockIdx.x);
-    else qk_walk<T, V, NS, BACK, INTER, 1>(a, blockIdx.x - a.ctas[0]);
+    extern __shared__ __align__(16) unsigned char smem[];
+    if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, INTER, 0>(a, blockIdx.x, smem);
+    else qk_walk<T, V, NS, BACK, INTER, 1>(a, blockIdx.x - a.ctas[0], smem);
 }
 
 struct QkSumArgs {
