@@ -131,16 +131,20 @@ int launch_act8(uint32_t K, uint64_t rows, uint64_t cols, const palsgd_mat* x, c
 {
     if (rows == 0 || cols == 0) return PALSGD_OK;
     Act8Args a{x->data, static_cast<int8_t*>(q->data), static_cast<uint8_t*>(e->data), x->worker_stride, x->row_stride,
-               q->worker_stride, q->row_stride, e->worker_stride, e->row_stride, rows, cols, 0, {}, 0};
+               q->worker_stride, q->row_stride, e->worker_stride, e->row_stride, rows, cols, 0, {}};
     const bool wide = cols % 8 == 0 && aligned(x->data, 16) && (x->row_stride * sizeof(T)) % 16 == 0 && (x->worker_stride * sizeof(T)) % 16 == 0 &&
                       aligned(q->data, 8) && q->row_stride % 8 == 0 && q->worker_stride % 8 == 0;
-    const uint64_t per_row = ceil_div(cols, 32) * (wide ? 4 : 32);
+    // rows that follow one another without gaps and end with a group: one long row
+    const bool flat = wide && cols % 32 == 0 &&
+                      (rows == 1 || (x->row_stride == (int64_t)cols && q->row_stride == (int64_t)cols && e->row_stride == (int64_t)(cols / 32)));
+    const uint64_t per_row = ceil_div(cols, 32) * 4;
     a.units = rows * per_row;
-    a.per_row = per_row < 0x80000000ull ? divisor((uint32_t)per_row) : Divisor{(uint32_t)per_row, 0, 0};
-    a.flat = cols % 32 == 0 && (rows == 1 || (x->row_stride == (int64_t)cols && q->row_stride == (int64_t)cols && e->row_stride == (int64_t)(cols / 32)));
-    const uint64_t ctas = ceil_div(a.units, 1024), most = 8ull * sm_count();
-    const dim3 grid((unsigned)(ctas < most ? ctas : most), K);
-    return launch(PACK ? "act8 pack" : "act8 unpack", wide ? act8_kernel<T, 8, PACK> : act8_kernel<T, 1, PACK>, grid, 256, 0, st, a);
+    a.per_row = divisor((uint32_t)per_row);
+    const uint64_t ctas = ceil_div(a.units, 256 * (sizeof(T) == 4 ? 2 : 4));
+    if (ctas > 0x7FFFFFFFull) return PALSGD_EUNSUPPORTED;
+    const dim3 grid((unsigned)ctas, K);
+    return launch(PACK ? "act8 pack" : "act8 unpack",
+                  flat ? act8_kernel<T, PACK, ACT8_FLAT> : wide ? act8_kernel<T, PACK, ACT8_WIDE> : act8_kernel<T, PACK, ACT8_LOOSE>, grid, 256, 0, st, a);
 }
 
 // ------------------------------------------------------------------------------------------------ feed-forward block
@@ -283,9 +287,7 @@ Operand input_operand(Arena& ws, Stage& st, const palsgd_mat* m, const palsgd_ma
     o.one = copies == 1;
     StageItem& it = st.a.item[st.n++];
     it = StageItem{m->data, e ? static_cast<const uint8_t*>(e->data) : nullptr, w, m->row_stride, e ? e->worker_stride : 0, e ? e->row_stride : 0,
-                   static_cast<bf16*>(const_cast<void*>(o.p)), o.r, o.part, (uint32_t)rows, (uint32_t)cols, rows * (uint64_t)(o.r / 8), kind, copies, 0};
-    const int unit = kind == STAGE_ACT8 ? 8 : 4;         // elements in the 8 or 16 bytes of a load
-    it.wide = aligned(m->data, kind == STAGE_ACT8 ? 8 : 16) && m->row_stride % unit == 0 && w % unit == 0;
+                   static_cast<bf16*>(const_cast<void*>(o.p)), o.r, o.part, (uint32_t)rows, (uint32_t)cols, rows * (uint64_t)(o.r / 8), kind, copies};
     return o;
 }
 

@@ -93,6 +93,56 @@ __device__ __forceinline__ uint32_t f2_narrow(f2 v)
     return *reinterpret_cast<const uint32_t*>(&t);
 }
 
+// ---- 16 bytes at any address, the first `bytes` of them inside a row (the others read as 0 and are not written).
+// Reads are of whole aligned 16-byte blocks that hold a byte of the row, shifted into place; such a block lies inside the
+// row's allocation, which starts and ends on a multiple of 16 bytes.  Writes are as wide as the address allows; ELEM: the
+// size of the elements, on a multiple of which the address lies.
+__device__ __forceinline__ uint4 get16(const unsigned char* p, uint32_t bytes)
+{
+    const uint32_t o = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15, s = 8 * (o & 3);
+    const uint4* base = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+    const uint4 a = bytes ? __ldg(base) : make_uint4(0, 0, 0, 0), b = bytes && o + bytes > 16 ? __ldg(base + 1) : make_uint4(0, 0, 0, 0);
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = o & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = o & 4 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], s);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)                      // what lies behind the row's end is not of it
+        if (4 * i + 4 > bytes) w[i] = 4 * i >= bytes ? 0u : w[i] & ((1u << (8 * (bytes & 3))) - 1u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int ELEM>
+__device__ __forceinline__ void put16(unsigned char* p, uint32_t bytes, const uint4& v)
+{
+    const uint32_t o = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if (bytes == 16 && o == 0) {
+        *reinterpret_cast<uint4*>(p) = v;
+    } else if (bytes == 16 && (o & 7) == 0) {
+        reinterpret_cast<uint2*>(p)[0] = make_uint2(w[0], w[1]);
+        reinterpret_cast<uint2*>(p)[1] = make_uint2(w[2], w[3]);
+    } else if (bytes == 16 && (ELEM == 4 || (o & 3) == 0)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+    } else if (bytes == 16 && ELEM < 4 && (ELEM == 2 || (o & 1) == 0)) {
+        *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) reinterpret_cast<uint32_t*>(p + 2)[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        *reinterpret_cast<uint16_t*>(p + 14) = (uint16_t)(w[3] >> 16);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 16 / ELEM; ++j)
+            if (j * ELEM < bytes) {
+                if constexpr (ELEM == 4) reinterpret_cast<uint32_t*>(p)[j] = w[j];
+                else if constexpr (ELEM == 2) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+                else p[j] = (unsigned char)(w[j / 4] >> (8 * (j & 3)));
+            }
+    }
+}
+
 // ---- 8-bit checkpoints: the step 2^(E-127) of a group from the largest magnitude in it (as bits: NaN > Inf > finite).
 // Adding 2^16 to the bits carries into the exponent exactly when the mantissa is >= 1.9921875 = 127.5/64, the values
 // that would round to 128 steps; ties (127.5) go to the even 128 and are among them.  A carry out of the largest finite

@@ -198,45 +198,18 @@ __device__ __forceinline__ uint32_t block_at(uint32_t base, uint32_t row, uint32
     return base + row * ROW + ((piece ^ turn) << 4);
 }
 
-// One element of E bytes between a block and memory.
-template <int E> __device__ __forceinline__ void element_out(uint32_t at, unsigned char* p)
-{
-    uint32_t v;
-    if constexpr (E == 4) { asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at)); *reinterpret_cast<uint32_t*>(p) = v; }
-    else if constexpr (E == 2) { asm volatile("{\n .reg .b16 h;\n ld.shared.b16 h, [%1];\n cvt.u32.u16 %0, h;\n}" : "=r"(v) : "r"(at)); *reinterpret_cast<uint16_t*>(p) = (uint16_t)v; }
-    else { asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at)); *p = (unsigned char)v; }
-}
-template <int E> __device__ __forceinline__ void element_in(uint32_t at, const unsigned char* p, bool on)
-{
-    if constexpr (E == 4) { const uint32_t v = on ? *reinterpret_cast<const uint32_t*>(p) : 0u; asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
-    else if constexpr (E == 2) { const uint16_t v = on ? *reinterpret_cast<const uint16_t*>(p) : (uint16_t)0; asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(v) : "memory"); }
-    else { const uint32_t v = on ? *p : 0u; asm volatile("st.shared.u8 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
-}
-
 // Block -> matrix: `rows` (at most 32) rows and `cols` columns of it are inside.  E: the element type's size.
 template <int ROW, int E>
-__device__ __noinline__ void block_out_edge(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
+__device__ __noinline__ void block_out_edge(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, uint32_t lane)
 {
-    constexpr uint32_t kPieces = ROW / 16, kPer = 16 / E, kCols = ROW / E;
-    if (wide) {
-        const uint32_t piece = lane % kPieces, first = piece * kPer;
+    constexpr uint32_t kPieces = ROW / 16;
+    const uint32_t piece = lane % kPieces, bytes = cols * E > piece * 16 ? min(cols * E - piece * 16, 16u) : 0;
+    if (bytes == 0) return;
 #pragma unroll 1
-        for (uint32_t row = lane / kPieces; row < rows; row += 32 / kPieces) {
-            const uint32_t at = block_at<ROW>(base, row, piece);
-            unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
-            if (first + kPer <= cols) {
-                uint4 v;
-                lds128(at, v);
-                *reinterpret_cast<uint4*>(p) = v;
-            } else {                                      // the row ends inside these 16 bytes, or before them
-#pragma unroll 1
-                for (uint32_t j = 0; first + j < cols; ++j) element_out<E>(at + j * E, p + j * E);
-            }
-        }
-    } else if (lane < min(cols, kCols)) {                 // one column a lane
-#pragma unroll 1
-        for (uint32_t row = 0; row < rows; ++row)
-            element_out<E>(block_at<ROW>(base, row, lane / kPer) + (lane % kPer) * E, to + (int64_t)row * row_bytes + lane * E);
+    for (uint32_t row = lane / kPieces; row < rows; row += 32 / kPieces) {
+        uint4 v;
+        lds128(block_at<ROW>(base, row, piece), v);
+        put16<E>(to + (int64_t)row * row_bytes + piece * 16, bytes, v);
     }
 }
 template <int ROW, int E>
@@ -253,7 +226,7 @@ __device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int6
 #pragma unroll
         for (uint32_t i = 0; i < kPieces; ++i) { *reinterpret_cast<uint4*>(p) = v[i]; p += step; }
     } else if (rows && cols) {
-        block_out_edge<ROW, E>(base, to, row_bytes, rows, cols, wide, lane);
+        block_out_edge<ROW, E>(base, to, row_bytes, rows, min(cols, (uint32_t)(ROW / E)), lane);
     }
 }
 
@@ -261,23 +234,12 @@ __device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int6
 // __syncwarp.  PIECES 16-byte pieces a row, the last ones of the row: int8 fills its end, so that a lane can write its
 // results over its row from the front while it still reads.
 template <int E, int PIECES>
-__device__ __noinline__ void block_in_edge(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
+__device__ __noinline__ void block_in_edge(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, uint32_t lane)
 {
-    constexpr uint32_t kPer = 16 / E, kFirst = 4 - PIECES;
-    if (wide) {
-        const uint32_t piece = lane % PIECES, first = piece * kPer;
-        const uint32_t inside = first < cols ? min(cols - first, kPer) * E : 0;
-#pragma unroll 1
-        for (uint32_t row = lane / PIECES; row < 32; row += 32 / PIECES) {
-            const uint32_t n = row < rows ? inside : 0;
-            const unsigned char* p = n ? from + (int64_t)row * row_bytes + piece * 16 : from;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(block_at<64>(base, row, kFirst + piece)), "l"(p), "r"(n) : "memory");
-        }
-    } else if (lane < PIECES * kPer) {
-#pragma unroll 1
-        for (uint32_t row = 0; row < 32; ++row)
-            element_in<E>(block_at<64>(base, row, kFirst + lane / kPer) + (lane % kPer) * E, from + (int64_t)row * row_bytes + lane * E, row < rows && lane < cols);
-    }
+    const uint32_t piece = lane % PIECES, bytes = cols * E > piece * 16 ? min(cols * E - piece * 16, 16u) : 0;
+#pragma unroll 4
+    for (uint32_t row = lane / PIECES; row < 32; row += 32 / PIECES)
+        sts128(block_at<64>(base, row, 4 - PIECES + piece), get16(from + (int64_t)row * row_bytes + piece * 16, row < rows ? bytes : 0));
 }
 template <int E, int PIECES>
 __device__ __forceinline__ void block_in(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
@@ -293,7 +255,7 @@ __device__ __forceinline__ void block_in(uint32_t base, const unsigned char* fro
             p += step;
         }
     } else if (rows && cols) {                            // (a block that is all outside is not read)
-        block_in_edge<E, PIECES>(base, from, row_bytes, rows, cols, wide, lane);
+        block_in_edge<E, PIECES>(base, from, row_bytes, rows, min(cols, (uint32_t)(PIECES * 16 / E)), lane);
     }
 }
 __device__ __forceinline__ void block_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
@@ -815,7 +777,6 @@ struct StageItem {
     uint64_t units;               // of 8 columns, one worker
     int      kind;
     uint32_t K;                   // workers to copy: 1 if all read one matrix
-    int      wide;                // eight columns can be read at a time (fp32, 8 bits)
 };
 struct StageArgs { StageItem item[kMaxStaged]; };
 
@@ -832,27 +793,21 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
         const uint32_t c = (uint32_t)(i - row * per) * 8;
         const int64_t from = k * it.w + (int64_t)row * it.r + c;
         float v[8];
-        const bool whole = it.wide && c + 8 <= it.cols;
-        if (it.kind == STAGE_ACT8) {
-            uint2 q = make_uint2(0, 0);
-            const int8_t* p = static_cast<const int8_t*>(it.src) + from;
-            if (whole) {
-                q = __ldg(reinterpret_cast<const uint2*>(p));
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < it.cols) (j < 4 ? q.x : q.y) |= (uint32_t)(uint8_t)p[j] << (8 * (j & 3));
-            }
+        const uint32_t n = c < it.cols ? min(it.cols - c, 8u) : 0;
+        if (it.kind == STAGE_BF16) {
+            const uint4 q = get16(static_cast<const unsigned char*>(it.src) + 2 * from, 2 * n);
+            *reinterpret_cast<uint4*>(it.dst + (k * it.rows + (int64_t)row) * it.ld + c) = q;
+            continue;
+        } else if (it.kind == STAGE_ACT8) {
+            const uint4 q = get16(static_cast<const unsigned char*>(it.src) + from, n);
             const float s = act8_step(it.e[k * it.ew + (int64_t)row * it.er + c / 32]);
             act8_value4(q.x, s, v);
             act8_value4(q.y, s, v + 4);
-        } else if (it.kind == STAGE_SPLIT && whole) {
-            Vec<float, 8>::load(static_cast<const float*>(it.src) + from, v);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = 0.0f;
-                if (c + j < it.cols) v[j] = it.kind == STAGE_BF16 ? to_f(static_cast<const bf16*>(it.src)[from + j]) : static_cast<const float*>(it.src)[from + j];
+            for (uint32_t j = 0; j < 2; ++j) {
+                const uint4 q = get16(static_cast<const unsigned char*>(it.src) + 4 * (from + 4 * j), n > 4 * j ? 4 * min(n - 4 * j, 4u) : 0);
+                v[4 * j] = __uint_as_float(q.x); v[4 * j + 1] = __uint_as_float(q.y); v[4 * j + 2] = __uint_as_float(q.z); v[4 * j + 3] = __uint_as_float(q.w);
             }
         }
         bf16* to = it.dst + (k * it.rows + (int64_t)row) * it.ld + c;
