@@ -330,7 +330,8 @@ int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, c
     const uint64_t down = ceil_div(M, kTileM), across = ceil_div(N, n_step), tiles = down * across * K;
     if (down * across > 0x7FFFFFFFull || L.tiles + tiles > 0x7FFFFFFFull) return PALSGD_EUNSUPPORTED;
     p.tiles_m = divisor((uint32_t)down);
-    p.per_worker = divisor((uint32_t)(down * across));
+    p.per_split = p.per_worker = divisor((uint32_t)(down * across));
+    p.splits = 1;
     p.tiles = (uint32_t)tiles;
     L.tiles += p.tiles;
     p.n_seg = A1 ? 2 : 1;
@@ -341,6 +342,65 @@ int add_problem(MatLaunch& L, uint64_t M, uint64_t N, uint64_t Kd, uint32_t K, c
         if (B[i]) { p.b_one[i] = B[i]->one; BLOCK_TRY(encode(&p.B[i], *B[i], bmn)); }
     }
     return PALSGD_OK;
+}
+
+// One product of a plain launch as the host plans it.
+struct Product {
+    uint64_t M, N, Kd;
+    const Operand *A0, *A1, *B0, *B1;
+    bool amn, bmn;
+    const palsgd_mat* out;
+    uint32_t splits;
+    const float* part;
+    uint64_t tiles(uint32_t K) const { return ceil_div(M, kTileM) * ceil_div(N, kTileN) * K; }
+    uint64_t steps(uint32_t parts) const { return (A1 ? 2 : 1) * ceil_div(Kd, kTileK) * (parts == 3 ? 6 : 1); }
+    static uint64_t length_of(uint64_t steps) { return (steps > kTileLeast ? steps : kTileLeast) + 1; }
+    uint64_t length(uint32_t parts) const { return length_of(ceil_div(steps(parts), splits)); }
+    int64_t ld() const { return (int64_t)(ceil_div(N, 8) * 8); }
+};
+
+// Cuts long inner axes into shares where a launch has too few tiles for the pairs of CTAs: the shares' binary32 sums go
+// to the workspace and one more small kernel joins them (kJoin: what that costs, in steps of 0.43 us; kStepBytes: the
+// sums that are written and read again in a step's time).  Of a few cuts -- shares of the average load of a pair, or up to
+// three times that -- the one that should end first, if it ends before no cut at all.  (One worker, one token, 2048 x
+// 5632: the second product is 8 tiles of 88 steps, the forward call 68 us uncut and 48 us cut.)
+constexpr uint64_t kJoin = 20, kStepBytes = 4000000;
+constexpr uint32_t kMaxSplits = 32;
+
+void plan_splits(Product* p, int n, uint32_t K, uint32_t parts, uint64_t pairs)
+{
+    uint64_t work = 0;
+    for (int i = 0; i < n; ++i) { p[i].splits = 1; work += p[i].tiles(K) * p[i].length(parts); }
+    const uint64_t least = work / pairs > 8 ? work / pairs : 8;
+    // when the last tile ends, the longer tiles being taken up first
+    auto end_of = [&](uint64_t share) {
+        uint64_t tiles = 0, all = 0, longest = 0, shortest = ~0ull, rounds = 0, bytes = 0;
+        bool joins = false;
+        for (int i = 0; i < n; ++i) {
+            const uint64_t s = p[i].steps(parts), c = share ? ceil_div(s, share) : 1, split = c > kMaxSplits ? kMaxSplits : c;
+            const uint64_t len = Product::length_of(ceil_div(s, split)), count = p[i].tiles(K) * split;
+            tiles += count; all += count * len;
+            rounds = ceil_div(tiles, pairs) * len;       // (of products that are alike)
+            longest = len > longest ? len : longest;
+            shortest = len < shortest ? len : shortest;
+            if (split > 1) { joins = true; bytes += 8 * split * K * p[i].M * (uint64_t)p[i].ld(); }
+        }
+        uint64_t e = longest == shortest ? rounds : all / pairs + shortest;
+        if (e < longest) e = longest;
+        return e + (joins ? kJoin + bytes / kStepBytes : 0);
+    };
+    uint64_t best = end_of(0), share = 0;
+    for (uint64_t quarter = 4; quarter <= 12; ++quarter) {
+        const uint64_t s = least * quarter / 4, e = end_of(s);
+        if (e < best) { best = e; share = s; }
+    }
+    for (int i = 0; share && i < n; ++i) {
+        const uint64_t c = ceil_div(p[i].steps(parts), share);
+        // (fp32: a share is of whole steps of the inner axis, each six products)
+        const uint64_t most = p[i].steps(1);
+        p[i].splits = (uint32_t)(c > kMaxSplits ? kMaxSplits : c);
+        if (p[i].splits > most) p[i].splits = (uint32_t)most;
+    }
 }
 
 template <typename T, int MODE, int ACT>
@@ -371,6 +431,59 @@ int run_mat(MatLaunch& L, const palsgd_ffn_shape* s, const Device& d, cudaStream
     L.gave_up = d.gave_up;
     const uint32_t pairs = (uint32_t)(d.sms / 2) < L.tiles ? (uint32_t)(d.sms / 2) : L.tiles;
     return s->precision == PALSGD_PREC_FP32 ? launch_mat<float, MODE>(L, s->activation, pairs, st) : launch_mat<bf16, MODE>(L, s->activation, pairs, st);
+}
+
+// Decides on the shares and takes the workspace for their sums (the same decision in both calls of an entry point: it
+// goes by sizes alone, for the device's pairs of CTAs).
+void take_shares(Arena& ws, Product* p, int n, uint32_t K, uint32_t parts)
+{
+    plan_splits(p, n, K, parts, (uint64_t)sm_count() / 2);
+    for (int i = 0; i < n; ++i)
+        if (p[i].splits > 1) p[i].part = static_cast<const float*>(ws.take((size_t)p[i].splits * K * p[i].M * (size_t)p[i].ld() * sizeof(float)));
+}
+
+// The products of a call in one launch, the longer ones first, and the kernel that joins what was cut.
+int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, size_t es, uint32_t parts, cudaStream_t st)
+{
+    MatLaunch L{};
+    JoinArgs join{};
+    uint32_t joins = 0;
+    uint64_t units = 0;
+    int heavy = 0;                                       // products whose tiles are the longer ones (Order)
+    if (n == 4) {                                        // dx and the three weight gradients, which are alike
+        heavy = 1;
+        if (p[0].length(parts) < p[1].length(parts)) {
+            const Product x = p[0];
+            for (int i = 0; i < 3; ++i) p[i] = p[i + 1];
+            p[3] = x;
+            heavy = 3;
+        }
+    }
+    for (int i = 0; i < n; ++i) {
+        BLOCK_TRY(add_problem(L, p[i].M, p[i].N, p[i].Kd, s->K, p[i].A0, p[i].A1, p[i].amn, p[i].B0, p[i].B1, p[i].bmn, kTileN));
+        MatProblem& q = L.p[i];
+        q.out[0] = out_of(p[i].out, p[i].N, es);
+        if (p[i].splits > 1) {
+            JoinItem& j = join.item[joins++];
+            const int64_t ld = p[i].ld(), w = ld * (int64_t)p[i].M;
+            j = JoinItem{p[i].part, w, w * s->K, p[i].splits, (uint32_t)ld, (uint32_t)p[i].M, (uint32_t)p[i].N, p[i].M * (uint64_t)(ld / 8), divisor((uint32_t)(ld / 8)), q.out[0]};
+            if (j.units > units) units = j.units;
+            q.out[0] = MatOut{const_cast<float*>(p[i].part), w, ld, w * s->K, 1, (uint32_t)ld};
+            q.splits = p[i].splits;
+            const uint64_t per = (uint64_t)q.per_split.d * q.splits, tiles = per * s->K;
+            if (per > 0x7FFFFFFFull || L.tiles - q.tiles + tiles > 0x7FFFFFFFull) return PALSGD_EUNSUPPORTED;
+            q.per_worker = divisor((uint32_t)per);
+            L.tiles += (uint32_t)tiles - q.tiles;
+            q.tiles = (uint32_t)tiles;
+        }
+        if (i + 1 == heavy) L.heavy = L.tiles;
+    }
+    if (heavy) L.lag = (uint32_t)(p[0].length(parts) / p[n - 1].length(parts));
+    BLOCK_TRY(run_mat<MAT_PLAIN>(L, s, d, st));
+    if (joins == 0) return PALSGD_OK;
+    const uint64_t want = ceil_div(units, 256), cap = 16ull * d.sms;
+    const dim3 grid((unsigned)(want < cap ? want : cap), joins, s->K);
+    return launch("joined shares", es == 4 ? join_kernel<float> : join_kernel<bf16>, grid, 256, 0, st, join);
 }
 
 void set_saved(MatLaunch& L, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e, const palsgd_mat* up_e)
@@ -550,21 +663,21 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
         od = input_operand(ws, stage, w_down, nullptr, s->precision, s->K, D, F);
         oh = own_operand(ws, s->K, M, F, parts);
     }
+    Product down{M, D, F, &oh, nullptr, &od, nullptr, false, false, y, 1, nullptr};
+    if (M) take_shares(ws, &down, 1, s->K, parts);
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
     if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
     if (M == 0) return PALSGD_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Device dev{};
     BLOCK_TRY(device_of(dev));
-    MatLaunch gated{}, down{};
+    MatLaunch gated{};
     BLOCK_TRY(add_problem(gated, M, F, D, s->K, &ox, nullptr, false, &og, &ou, false, kTileN / 2));
     gated.p[0].out[0] = out_of(oh);
     set_saved(gated, s, gate, up, gate_e, up_e);
-    BLOCK_TRY(add_problem(down, M, D, F, s->K, &oh, nullptr, false, &od, nullptr, false, kTileN));
-    down.p[0].out[0] = out_of(y, D, es);
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_GATED>(gated, s, dev, st));
-    return run_mat<MAT_PLAIN>(down, s, dev, st);
+    return run_products(&down, 1, s, dev, es, parts, st);
 }
 
 extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* dy_, const palsgd_mat* x_, const palsgd_mat* x_e_,
@@ -608,6 +721,15 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
         }
         for (Operand& o : hid) o = own_operand(ws, s->K, M, F, parts);
     }
+    // dx contracts over both halves of the hidden axis, the weight gradients over the tokens
+    const Product all[4] = {{M, D, F, &hid[0], &hid[1], &og, &ou, false, true, dx, 1, nullptr},
+                            {F, D, M, &hid[0], nullptr, &ox, nullptr, true, true, dw_gate, 1, nullptr},
+                            {F, D, M, &hid[1], nullptr, &ox, nullptr, true, true, dw_up, 1, nullptr},
+                            {D, F, M, &ody, nullptr, &hid[2], nullptr, true, true, dw_down, 1, nullptr}};
+    Product products[4];
+    const int n_products = dx ? 4 : 3;
+    for (int i = 0; i < n_products; ++i) products[i] = all[dx ? i : i + 1];
+    if (M) take_shares(ws, products, n_products, s->K, parts);
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
     if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -623,34 +745,13 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     }
     Device dev{};
     BLOCK_TRY(device_of(dev));
-    MatLaunch hidden{}, grads{};
+    MatLaunch hidden{};
     BLOCK_TRY(add_problem(hidden, M, F, D, s->K, &ody, nullptr, false, &od, nullptr, true, kTileN));
     for (int i = 0; i < 3; ++i) hidden.p[0].out[i] = out_of(hid[i]);
     set_saved(hidden, s, gate, up, gate_e, up_e);
-    // dx contracts over both halves of the hidden axis, the weight gradients over the tokens: the longer tiles first
-    const uint64_t long_x = 2 * ceil_div(F, kTileK) + kTileEnd, long_w = ceil_div(M, kTileK) + kTileEnd;
-    const bool x_first = long_x >= long_w;
-    auto add_x = [&]() -> int {
-        if (!dx) return PALSGD_OK;
-        BLOCK_TRY(add_problem(grads, M, D, F, s->K, &hid[0], &hid[1], false, &og, &ou, true, kTileN));
-        grads.p[grads.n_problems - 1].out[0] = out_of(dx, D, es);
-        return PALSGD_OK;
-    };
-    auto add_w = [&]() -> int {
-        const palsgd_mat* w[3] = {dw_gate, dw_up, dw_down};
-        for (int i = 0; i < 3; ++i) {
-            BLOCK_TRY(add_problem(grads, i < 2 ? F : D, i < 2 ? D : F, M, s->K, i < 2 ? &hid[i] : &ody, nullptr, true, i < 2 ? &ox : &hid[2], nullptr, true, kTileN));
-            grads.p[grads.n_problems - 1].out[0] = out_of(w[i], i < 2 ? D : F, es);
-        }
-        return PALSGD_OK;
-    };
-    BLOCK_TRY(x_first ? add_x() : add_w());
-    grads.heavy = grads.tiles;
-    grads.lag = (uint32_t)(x_first ? long_x / long_w : long_w / long_x);
-    BLOCK_TRY(x_first ? add_w() : add_x());
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s, dev, st));
-    return run_mat<MAT_PLAIN>(grads, s, dev, st);
+    return run_products(products, n_products, s, dev, es, parts, st);
 }
 
 extern "C" int palsgd_block_status(void* stream)

@@ -127,11 +127,15 @@ __device__ __forceinline__ void put16(unsigned char* p, uint32_t bytes, const ui
     } else if (bytes == 16 && (ELEM == 4 || (o & 3) == 0)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
-    } else if (bytes == 16 && ELEM < 4 && (ELEM == 2 || (o & 1) == 0)) {
-        *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    } else if (bytes == 16 && ELEM < 4) {                 // up to the next word, three words, the rest
+        const uint32_t head = 4 - (o & 3), rest = w[3] >> (8 * head);
+        if (ELEM == 1 && (head & 1)) *p = (unsigned char)w[0];
+        if (head >= 2) *reinterpret_cast<uint16_t*>(p + (head & 1)) = (uint16_t)(w[0] >> (8 * (head & 1)));
 #pragma unroll
-        for (int i = 0; i < 3; ++i) reinterpret_cast<uint32_t*>(p + 2)[i] = __funnelshift_r(w[i], w[i + 1], 16);
-        *reinterpret_cast<uint16_t*>(p + 14) = (uint16_t)(w[3] >> 16);
+        for (int i = 0; i < 3; ++i) reinterpret_cast<uint32_t*>(p + head)[i] = __funnelshift_r(w[i], w[i + 1], 8 * head);
+        unsigned char* q = p + head + 12;
+        if (head <= 2) *reinterpret_cast<uint16_t*>(q) = (uint16_t)rest;
+        if (ELEM == 1 && (head & 1)) q[head == 1 ? 2 : 0] = (unsigned char)(head == 1 ? rest >> 16 : rest);
     } else {
 #pragma unroll
         for (uint32_t j = 0; j < 16 / ELEM; ++j)

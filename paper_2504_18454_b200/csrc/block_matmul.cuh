@@ -43,13 +43,13 @@ struct MatShape {
 };
 
 constexpr uint32_t kMaxProblems = 4;
-constexpr uint32_t kTileEnd = 3;                                        // what a tile costs beside its steps, in steps
+constexpr uint32_t kTileLeast = 6;                                      // steps that a tile's results take to leave: a shorter tile ends no sooner
 constexpr unsigned long long kWaitLimitNs = 4000000000ull;              // how long a wait polls before it gives up
 
 struct MatOut {
     void*   p;
     int64_t w, r;                 // worker and row stride, elements
-    int64_t part;                 // 0, or the stride between the three bfloat16 parts of an fp32 value
+    int64_t part;                 // the stride between the three bfloat16 parts of an fp32 value, or between shares' sums
     int     wide;                 // rows start on 16-byte boundaries
     uint32_t cols;                // columns that may be written: the workspace's rows have room behind their end
 };
@@ -57,7 +57,8 @@ struct MatOut {
 struct alignas(64) MatProblem {
     CUtensorMap A[2], B[2];       // by segment; the gate/up pass: B[0] gate, B[1] up
     uint32_t M, N, Kd, tiles;
-    Divisor  tiles_m, per_worker; // tiles down, tiles of one worker
+    Divisor  tiles_m, per_split, per_worker; // tiles down, of one share of the inner axis, of one worker
+    uint32_t splits;              // shares of the inner axis (plain): above one, out[0] takes each share's binary32 sums
     uint8_t  n_seg, a_parts, b_parts, a_mn, b_mn;
     uint8_t  a_one[2], b_one[2];  // all workers read one matrix
     MatOut   out[3];              // plain: the product; gate/up: h; hidden: dg, du, h
@@ -389,7 +390,7 @@ struct Order {
     __device__ __forceinline__ void next() { ++j; }
 };
 
-struct Tile { uint32_t worker, m0, n0; const MatProblem* p; };
+struct Tile { uint32_t worker, m0, n0, split; const MatProblem* p; };
 
 template <int MODE>
 __device__ __forceinline__ Tile tile_at(const MatLaunch& a, uint32_t t)
@@ -397,23 +398,35 @@ __device__ __forceinline__ Tile tile_at(const MatLaunch& a, uint32_t t)
     uint32_t i = 0;
     while (i + 1 < a.n_problems && t >= a.p[i].tiles) { t -= a.p[i].tiles; ++i; }
     const MatProblem& p = a.p[i];
-    const uint32_t w = p.per_worker.of(t), r = t - w * p.per_worker.d, n = p.tiles_m.of(r), m = r - n * p.tiles_m.d;
-    return Tile{w, m * kTileM, n * (MODE == MAT_GATED ? kTileN / 2 : kTileN), &p};
+    const uint32_t w = p.per_worker.of(t), i_w = t - w * p.per_worker.d, s = MODE == MAT_PLAIN ? p.per_split.of(i_w) : 0, r = i_w - s * p.per_split.d;
+    const uint32_t n = p.tiles_m.of(r), m = r - n * p.tiles_m.d;
+    return Tile{w, m * kTileM, n * (MODE == MAT_GATED ? kTileN / 2 : kTileN), s, &p};
 }
 
 __device__ __forceinline__ uint32_t pairs_of(const MatProblem& p) { return p.a_parts == 1 ? p.b_parts : p.b_parts == 1 ? p.a_parts : 6; }
 
-// The inner axis of a tile in pieces, each a sum of its own in tensor memory: f(segment, first step, end, last piece).
-// bfloat16: one piece a segment, joined in tensor memory.  fp32: kPiece steps (with all their parts), joined in registers
-// with rounding to nearest -- the tensor cores cut off what an addition does not hold, which over long sums adds up
-// (measured over 4096 steps of the inner axis in one piece: 4.4e-6 of the result's norm).
+// The inner axis of a tile -- its share of all segments' steps -- in pieces of one segment each:
+// f(segment, first step, end, begins a sum, ends it).  bfloat16: the pieces of a tile are one sum.  fp32: kPiece steps (with
+// all their parts) are a sum of their own, and the sums are joined in registers with rounding to nearest -- the tensor
+// cores cut off what an addition does not hold, which over long sums adds up (measured over 4096 steps of the inner axis
+// in one sum: 4.4e-6 of the result's norm; in pieces: 5e-7).
 template <typename T, typename F>
-__device__ __forceinline__ bool for_pieces(const MatProblem& p, F&& f)
+__device__ __forceinline__ bool for_pieces(const Tile& tl, F&& f)
 {
-    const uint32_t steps = (p.Kd + kTileK - 1) / kTileK, piece = sizeof(T) == 4 ? kPiece : steps;
-    for (uint32_t seg = 0; seg < p.n_seg; ++seg)
-        for (uint32_t k = 0; k < steps; k += piece)
-            if (!f(seg, k, k + piece < steps ? k + piece : steps)) return false;
+    const MatProblem& p = *tl.p;
+    const uint32_t steps = (p.Kd + kTileK - 1) / kTileK, all = p.n_seg * steps;
+    uint32_t g = 0, last = all;
+    if (p.splits > 1) {
+        g = (uint32_t)((uint64_t)all * tl.split / p.splits);
+        last = (uint32_t)((uint64_t)all * (tl.split + 1) / p.splits);
+    }
+    for (bool first = true; g < last; first = false) {
+        const uint32_t seg = g >= steps, k = g - seg * steps;
+        uint32_t n = min(steps - k, last - g);
+        if (sizeof(T) == 4) n = min(n, kPiece);
+        g += n;
+        if (!f(seg, k, k + n, sizeof(T) == 4 || first, sizeof(T) == 4 || g == last)) return false;
+    }
     return true;
 }
 
@@ -463,7 +476,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 const uint32_t mn = is_b ? (MODE == MAT_GATED ? tl.n0 : tl.n0 + rank * 128) : tl.m0 + rank * 128;
                 const bool across = is_b ? p.b_mn : p.a_mn;
                 const int parts_a = p.a_parts, parts_b = p.b_parts;
-                ok = for_pieces<T>(p, [&](uint32_t seg, uint32_t from, uint32_t to) {
+                ok = for_pieces<T>(tl, [&](uint32_t seg, uint32_t from, uint32_t to, bool, bool) {
                     const uint32_t i = is_b && MODE == MAT_GATED ? rank : seg;
                     const CUtensorMap* const map = is_b ? &p.B[i] : &p.A[i];
                     const uint32_t w = (is_b ? p.b_one[i] : p.a_one[i]) ? 0 : tl.worker;
@@ -508,9 +521,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((kTileN / 8) << 17) | ((kTileM / 16) << 24);
                 const uint64_t da = operand_desc(base, p.a_mn), db = operand_desc(base + kOperandBytes, p.b_mn);
                 const uint32_t sa = p.a_mn ? 2048 / 16 : 32 / 16, sb = p.b_mn ? 2048 / 16 : 32 / 16;
-                ok = for_pieces<T>(p, [&](uint32_t seg, uint32_t from, uint32_t to) {
+                ok = for_pieces<T>(tl, [&](uint32_t, uint32_t from, uint32_t to, bool begins, bool ends) {
                     const uint32_t acc = it & 1, d = tmem + acc * kTileN;
-                    const bool begins = sizeof(T) == 4 || seg == 0, ends = sizeof(T) == 4 || seg + 1 == p.n_seg;
                     if (begins) {
                         if (!bar_wait(acc_empty + 8 * acc, (it >> 1 & 1) ^ 1, a.gave_up)) return false;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -582,7 +594,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 float sum[64];
 #pragma unroll
                 for (int i = 0; i < 64; ++i) sum[i] = 0.0f;
-                uint32_t pieces = p.n_seg * ((p.Kd + kPiece * kTileK - 1) / (kPiece * kTileK));
+                uint32_t pieces = 0;
+                for_pieces<T>(tl, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
                 bool ok = true;
                 for (;;) {
                     src = tmem + (it & 1) * kTileN + (quad << 21) + part * kMine;
@@ -631,6 +644,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 const uint32_t cols = n < p.N ? p.N - n : 0, room = n < p.out[0].cols ? p.out[0].cols - n : 0;
                 const int64_t at = w * p.out[0].w + (int64_t)m * p.out[0].r + n;
                 if constexpr (MODE == MAT_PLAIN) {
+                    if (E == 2 && p.splits > 1) {                         // binary32 sums of a share: 16 columns a block
+                        float* to = static_cast<float*>(p.out[0].p) + (int64_t)tl.split * p.out[0].part + at;
+#pragma unroll 1
+                        for (uint32_t half = 0; half < 2; ++half) {
+                            float v[16];
+                            tmem_load16(from + 16 * half, v);
+                            tmem_load_wait();
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                sts128(block_at<64>(b0, lane, j), make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
+                            __syncwarp();
+                            block_out<64, 4>(b0, reinterpret_cast<unsigned char*>(to + 16 * half), 4 * p.out[0].r, rows, room > 16 * half ? room - 16 * half : 0, true, lane);
+                            __syncwarp();
+                        }
+                        if (c + 1 == kChunks) acc_read();
+                        continue;
+                    }
 #pragma unroll
                     for (uint32_t j = 0; j < kOcts; j += 2) {
                         float v[16];
@@ -644,7 +674,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     }
                     if (c + 1 == kChunks) acc_read();
                     __syncwarp();
-                    block_out<64, E>(b0, static_cast<unsigned char*>(p.out[0].p) + E * at, E * p.out[0].r, rows, room, p.out[0].wide, lane);
+                    const int64_t to = E == 4 && p.splits > 1 ? at + (int64_t)tl.split * p.out[0].part : at;
+                    block_out<64, E>(b0, static_cast<unsigned char*>(p.out[0].p) + E * to, E * p.out[0].r, rows, room, p.out[0].wide, lane);
                     __syncwarp();
                 } else if constexpr (MODE == MAT_GATED) {
                     // gate, up and h pass through one block, one after another (tensor memory is read again for each)
@@ -821,6 +852,48 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
             }
         } else {
             Vec<bf16, 8>::store(to, v);
+        }
+    }
+}
+
+// The shares' sums of a product, joined in a fixed order.
+struct JoinItem {
+    const float* part;            // [splits][K][M][ld]
+    int64_t  w, share;            // strides of a worker and of a share
+    uint32_t splits, ld, M, N;
+    uint64_t units;               // of 8 columns, one worker
+    Divisor  per_row;             // ld / 8
+    MatOut   out;
+};
+struct JoinArgs { JoinItem item[kMaxProblems]; };
+
+template <typename T>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinArgs a)
+{
+    let_next_start();
+    wait_for_previous();
+    const JoinItem& it = a.item[blockIdx.y];
+    const int64_t k = blockIdx.z;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < it.units; i += (uint64_t)gridDim.x * 256) {
+        const uint32_t row = it.units < 0x80000000ull ? it.per_row.of((uint32_t)i) : (uint32_t)(i / it.per_row.d);
+        const uint32_t c = (uint32_t)(i - (uint64_t)row * it.per_row.d) * 8;
+        if (c >= it.N) continue;
+        const float* p = it.part + k * it.w + (int64_t)row * it.ld + c;
+        float sum[8];
+        Vec<float, 8>::load(p, sum);
+        for (uint32_t s = 1; s < it.splits; ++s) {
+            float v[8];
+            Vec<float, 8>::load(p + s * it.share, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += v[j];
+        }
+        T* to = static_cast<T*>(it.out.p) + k * it.out.w + (int64_t)row * it.out.r + c;
+        const uint32_t n = min(it.N - c, 8u);
+        if (it.out.wide && n == 8) {
+            Vec<T, 8>::store(to, sum);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) if (j < n) to[j] = from_f<T>(sum[j]);
         }
     }
 }

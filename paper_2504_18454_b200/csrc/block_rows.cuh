@@ -144,6 +144,12 @@ __global__ void __launch_bounds__(256, LAYOUT == ACT8_LOOSE ? 4 : 6) act8_kernel
                     Vec<T, 8>::store(x + xo, v);
                 } else if constexpr (sizeof(T) == 2) {
                     put16<2>(reinterpret_cast<unsigned char*>(x + xo), 2 * n, make_uint4(f2_narrow(f2_of(v[0], v[1])), f2_narrow(f2_of(v[2], v[3])), f2_narrow(f2_of(v[4], v[5])), f2_narrow(f2_of(v[6], v[7]))));
+                } else if (n == 8 && (reinterpret_cast<uintptr_t>(x + xo) & 7)) {
+                    T* p = x + xo;
+                    p[0] = v[0];
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) reinterpret_cast<float2*>(p + 1)[i] = make_float2(v[2 * i + 1], v[2 * i + 2]);
+                    p[7] = v[7];
                 } else {
 #pragma unroll
                     for (uint32_t j = 0; j < 2; ++j)
