@@ -225,6 +225,10 @@ int device_of(Device& out)
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return palsgd_block_cuda_fail((int)e, "cudaGetDevice");
     if (dev < 0 || dev >= kMaxDevices) return PALSGD_EUNSUPPORTED;
+    // The device's context has to be current in this thread before the driver is asked for tensor maps: a thread that has
+    // made no call of the runtime's yet (autograd's, say) has none.
+    e = cudaSetDevice(dev);
+    if (e != cudaSuccess) return palsgd_block_cuda_fail((int)e, "cudaSetDevice");
     std::lock_guard<std::mutex> lock(g_mutex);
     Device& d = g_device[dev];
     if (!d.ready) {
@@ -310,7 +314,8 @@ int encode(CUtensorMap* map, const Operand& o, bool mn)
     const CUresult rc = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.p), dims, strides, box, unit,
                                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return rc == CUDA_SUCCESS ? PALSGD_OK : palsgd_block_cuda_fail((int)cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    if (rc == CUDA_SUCCESS) return PALSGD_OK;
+    return palsgd_block_cuda_fail((int)rc, "cuTensorMapEncodeTiled");   // (the runtime's codes are the driver's)
 }
 
 MatOut out_of(const palsgd_mat* m, uint64_t cols, size_t es)

@@ -232,3 +232,66 @@ def test_python_refusals():
     for call in bad:
         with pytest.raises(P.PalsgdError):
             call()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size", [(1, 1, 64, 4096), (1, 5, 33, 3001), (2, 3000, 72, 40), (1, 7000, 16, 264)], ids=str)
+def test_long_inner_axes_with_few_tiles(dtype, size):
+    """The products' inner axes are cut into shares here: few tiles, up to 110 steps of 64 each."""
+    K, M, D, F = size
+    x, wg, wu, wd, dy = _inputs(K, M, D, F, DT[dtype], seed=12)
+    y, saved = P.ffn_forward(x, wg, wu, wd, activation=P.ACT_GELU)
+    want = ffn_forward64(x, wg, wu, wd, P.ACT_GELU, dtype == "bf16")
+    within(y, *want["y"], "y")
+    got = P.ffn_backward(dy, x, wg, wu, wd, saved, activation=P.ACT_GELU)
+    ref = ffn_backward64(dy, x, wg, wu, wd, saved[0], saved[1], P.ACT_GELU, dtype == "bf16")
+    for t, name in zip(got, ("dx", "dw_gate", "dw_up", "dw_down")):
+        within(t, *ref[name], name)
+    for a, b in zip(got, P.ffn_backward(dy, x, wg, wu, wd, saved, activation=P.ACT_GELU)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shift", range(1, 8))
+def test_every_alignment_of_outputs_and_saved_checkpoints(shift):
+    """Rows at every offset from a 16-byte boundary: forward writes to them, backward reads from them."""
+    K, M, D, F = 2, 45, 50, 83
+    x, wg, wu, wd, dy = _inputs(K, M, D, F, torch.bfloat16, seed=13)
+    wide = lambda n, dt, v: torch.full((K, M, n + 19), v, device="cuda", dtype=dt)
+    yb, gb, ub = wide(D, torch.bfloat16, 1536.0), wide(F, torch.int8, 99), wide(F, torch.int8, 99)
+    ge, ue = (torch.empty(K, M, 3, device="cuda", dtype=torch.uint8) for _ in range(2))
+    cut = lambda t, n: t[:, :, shift:shift + n]
+    saved = (P.Act8(cut(gb, F), ge, x.dtype), P.Act8(cut(ub, F), ue, x.dtype))
+    P.ffn_forward(x, wg, wu, wd, save=P.SAVE_8BIT, out=cut(yb, D), saved=saved)
+    y0, saved0 = P.ffn_forward(x, wg, wu, wd, save=P.SAVE_8BIT)
+    assert torch.equal(cut(yb, D), y0)
+    for a, b in zip(saved, saved0):
+        assert torch.equal(a.q, b.q) and torch.equal(a.exponent, b.exponent)
+    for t, n, v in ((yb, D, 1536), (gb, F, 99), (ub, F, 99)):
+        assert bool((t[:, :, :shift] == v).all()) and bool((t[:, :, shift + n:] == v).all())
+    xb = wide(D, torch.int8, 99)
+    px = P.act8_pack(x)
+    cut(xb, D).copy_(px.q)
+    for a, b in zip(P.ffn_backward(dy, P.Act8(cut(xb, D), px.exponent, x.dtype), wg, wu, wd, saved),
+                    P.ffn_backward(dy, px, wg, wu, wd, saved0)):
+        assert torch.equal(a, b)
+
+
+def test_a_thread_that_has_not_used_the_gpu_yet():
+    import threading
+    K, M, D, F = 1, 40, 64, 96
+    x, wg, wu, wd, dy = _inputs(K, M, D, F, torch.bfloat16, seed=14)
+    y, saved = P.ffn_forward(x, wg, wu, wd)
+    want, got = P.ffn_backward(dy, x, wg, wu, wd, saved), []
+    torch.cuda.synchronize()
+
+    def call():
+        try:
+            got.extend(P.ffn_backward(dy, x, wg, wu, wd, saved))
+        except Exception as e:                           # noqa: BLE001 -- reported below, in the test's thread
+            got.append(e)
+
+    t = threading.Thread(target=call)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert len(got) == 4 and all(torch.equal(a, b) for a, b in zip(got, want)), got

@@ -198,3 +198,22 @@ def test_python_refusals():
     for call in bad:
         with pytest.raises(P.PalsgdError):
             call()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", [24, 33, 64, 77])
+@pytest.mark.parametrize("shift", range(8))
+def test_act8_at_every_alignment(dtype, cols, shift):
+    R = 13
+    base = torch.randn(R, cols + 11, device="cuda").to(DT[dtype])
+    x = base[:, shift:shift + cols]
+    q = torch.full((R, cols + 9), 99, dtype=torch.int8, device="cuda")
+    e = torch.empty(R, (cols + 31) // 32, dtype=torch.uint8, device="cuda")
+    a = P.act8_pack(x, out=P.Act8(q[:, shift:shift + cols], e, x.dtype))
+    wq, we, wv = act8_numpy(x.float().cpu().numpy())
+    assert np.array_equal(a.q.cpu().numpy(), wq) and np.array_equal(a.exponent.cpu().numpy(), we)
+    assert bool((q[:, :shift] == 99).all()) and bool((q[:, shift + cols:] == 99).all())
+    out = torch.full_like(base, 5.0)
+    P.act8_unpack(a, out=out[:, shift:shift + cols])
+    assert np.array_equal(out[:, shift:shift + cols].double().cpu().numpy(), wv)
+    assert bool((out[:, :shift] == 5).all()) and bool((out[:, shift + cols:] == 5).all())
