@@ -605,10 +605,18 @@ int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
     const dim3 grid(p.a.ctas[0] + p.a.ctas[1], s->K);
     constexpr int W = 16 / (int)sizeof(T);
     const char* what = "q/k norm + rotation";
-    if (p.V == W && p.NS == 1) return launch(what, qk_kernel<T, W, 1, BACK, INTER>, grid, kQkThreads, qk_smem(W, 1, BACK, s->head_dim), st, p.a);
-    if (p.V == W) return launch(what, qk_kernel<T, W, 2, BACK, INTER>, grid, kQkThreads, qk_smem(W, 2, BACK, s->head_dim), st, p.a);
-    if (p.NS <= 2) return launch(what, qk_kernel<T, 1, 2, BACK, INTER>, grid, kQkThreads, qk_smem(1, 2, BACK, s->head_dim), st, p.a);
-    return launch(what, qk_kernel<T, 1, 8, BACK, INTER>, grid, kQkThreads, qk_smem(1, 8, BACK, s->head_dim), st, p.a);
+    auto run = [&](void (*kernel)(const QkArgs), int V, int NS) { return launch(what, kernel, grid, kQkThreads, qk_smem(V, NS, BACK, s->head_dim), st, p.a); };
+    if (p.V == W && p.NS == 1) {
+        switch (p.a.lanes) {
+            case 4: return run(qk_kernel<T, W, 1, BACK, INTER, 4>, W, 1);
+            case 8: return run(qk_kernel<T, W, 1, BACK, INTER, 8>, W, 1);
+            case 16: return run(qk_kernel<T, W, 1, BACK, INTER, 16>, W, 1);
+            default: return run(qk_kernel<T, W, 1, BACK, INTER, 0>, W, 1);
+        }
+    }
+    if (p.V == W) return run(qk_kernel<T, W, 2, BACK, INTER, 32>, W, 2);
+    if (p.NS <= 2) return run(qk_kernel<T, 1, 2, BACK, INTER, 0>, 1, 2);
+    return run(qk_kernel<T, 1, 8, BACK, INTER, 32>, 1, 8);
 }
 
 template <bool BACK>

@@ -246,16 +246,17 @@ __device__ __forceinline__ void slot_put(T* base, const uint32_t (&at)[2], const
 // angles), so a warp's groups are spread over heads only as far as leaves four heads or so in a row to each.  Each lane
 // brings what it will work on into shared memory by asynchronous copies, kRing items ahead (held in registers, one item
 // ahead was all there was room for).  V = 1, for layouts without 16-byte boundaries, reads directly.
-template <typename T, int V, int NS, bool BACK, bool INTER, int SIDE>
+template <typename T, int V, int NS, bool BACK, bool INTER, int LANES, int SIDE>
 __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, unsigned char* smem)
 {
     constexpr bool kInside = INTER || V == 1;                                 // a rotation pair is one f2 (else: f2 i and V/2 + i)
     constexpr int H = V / 2;
     constexpr uint32_t kWarps = kQkThreads / 32;
+    const uint32_t lanes = LANES ? LANES : a.lanes;
     const uint32_t ctas = a.ctas[SIDE];
     const HeadsArg& h = a.side[SIDE];
     const uint32_t k = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t sub = lane & (a.lanes - 1), group = lane / a.lanes, groups = 32 / a.lanes;
+    const uint32_t sub = lane & (lanes - 1), group = lane / lanes, groups = 32 / lanes;
     const uint32_t n_vec = a.head_dim / V, half = a.rot / 2;
     uint32_t at[NS][2];           // first element of each vector, or ~0
     T w[NS][2 * V];               // two to a register where they are bfloat16
@@ -263,7 +264,7 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
     const T* wp = static_cast<const T*>(h.w) + (int64_t)k * h.ww;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        const uint32_t slot = s * a.lanes + sub, split = INTER ? 0 : a.pair_slots;
+        const uint32_t slot = s * lanes + sub, split = INTER ? 0 : a.pair_slots;
         uint32_t v0, v1;
         if (!INTER && slot < split) { v0 = slot; v1 = slot + split; }
         else { v0 = 2 * split + 2 * (slot - split); v1 = v0 + 1; }
@@ -345,7 +346,7 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
         v += u;
 #pragma unroll
         for (uint32_t m = 1; m < 32; m *= 2)
-            if (m < a.lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);         // (the same branch for the whole grid)
+            if (m < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);         // (the same branch for the whole grid)
         return v;
     };
     auto position = [&](uint64_t turn) -> int32_t {
@@ -365,7 +366,7 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             float c[V], sn[V];
-            const uint32_t i = (s * a.lanes + sub) * V;                       // first pair of the slot
+            const uint32_t i = (s * lanes + sub) * V;                       // first pair of the slot
             if (V > 1 && a.table_wide && i + V <= half && ok) {
                 if constexpr (V > 1) {
 #pragma unroll
@@ -491,7 +492,7 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
                 float v, u;
                 f2_get(acc[s][j / 2], v, u);
                 if (j & 1) v = u;
-                for (uint32_t m = 16; m >= a.lanes; m >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
+                for (uint32_t m = 16; m >= lanes; m >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
                 if (group == 0 && at[s][j / V] != ~0u) sum[warp * a.head_dim + at[s][j / V] + j % V] = v;
             }
         __syncthreads();
@@ -506,14 +507,16 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
 }
 
 // (Two copies of the walk: with the side a constant its strides are constants of the instruction, not loads by index.)
-template <typename T, int V, int NS, bool BACK, bool INTER>
+// LANES: the lanes that share a head where the host picks a copy made for them (0: any; the sum over a head is then a
+// chain of branches, which take a tenth of the time).
+template <typename T, int V, int NS, bool BACK, bool INTER, int LANES>
 __global__ void __launch_bounds__(kQkThreads, NS == 1 ? 4 : 1) qk_kernel(const __grid_constant__ QkArgs a)
 {
     let_next_start();
     wait_for_previous();
     extern __shared__ __align__(16) unsigned char smem[];
-    if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, INTER, 0>(a, blockIdx.x, smem);
-    else qk_walk<T, V, NS, BACK, INTER, 1>(a, blockIdx.x - a.ctas[0], smem);
+    if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, INTER, LANES, 0>(a, blockIdx.x, smem);
+    else qk_walk<T, V, NS, BACK, INTER, LANES, 1>(a, blockIdx.x - a.ctas[0], smem);
 }
 
 struct QkSumArgs {
