@@ -108,6 +108,12 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, unsigned
     atomicExch(gave_up, 1u);
     return false;
 }
+__device__ __forceinline__ bool elect_one()                              // one thread of the warp, the same each time
+{
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p;
+}
 __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank)
 {
     uint32_t r;
@@ -440,7 +446,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
     const uint32_t base = (smem_addr(smem_raw) + 1023) & ~1023u;
     const uint32_t blocks = base + kStages * kStageBytes, bars = blocks + Shape::kEpilogue * Shape::kBlocks * 2048;
     const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16, tmem_at = acc_empty + 16;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
+    const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     let_next_start();
@@ -463,9 +469,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
 
     if (warp == 0 || warp == 3) {
         // producers: warp 0 brings A, warp 3 brings B (one thread that did both held the copy engine up: 410 ns a step of
-        // 32 KB, of which 120 its own)
-        if (lane == 0) {
-            const bool is_b = warp == 3;
+        // 32 KB, of which 120 its own).  The whole warp walks the loop and one thread of it issues: what it walks with stays
+        // in the warp's shared registers, from where the copy engine takes it.
+        {
+            const bool is_b = warp == 3, one = elect_one();
             const uint32_t dst = base + (is_b ? kOperandBytes : 0), signal = in_cta(full, 0);
             uint32_t s = 0, phase = 0, used = 0;
             bool ok = true;
@@ -485,15 +492,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                             if (pa >= parts_a || sum - pa >= parts_b) continue;
                             const uint32_t part = is_b ? sum - pa : pa;
                             for (uint32_t k = from * kTileK; k < to * kTileK; k += kTileK) {
-                                if (!bar_wait(empty + 8 * s, phase ^ 1, a.gave_up)) return false;
-                                if (!is_b && rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);
+                                if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * s, phase ^ 1, a.gave_up))) return false;
                                 const uint32_t to_s = dst + s * kStageBytes, bar = signal + 8 * s;
-                                if (across) {
-                                    tma_load(map, to_s, bar, mn, k, w, part);
-                                    tma_load(map, to_s + 8192, bar, mn + 64, k, w, part);
-                                } else {
-                                    tma_load(map, to_s, bar, k, mn, w, part);
+                                if (one) {
+                                    if (!is_b && rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);
+                                    if (across) {
+                                        tma_load(map, to_s, bar, mn, k, w, part);
+                                        tma_load(map, to_s + 8192, bar, mn + 64, k, w, part);
+                                    } else {
+                                        tma_load(map, to_s, bar, k, mn, w, part);
+                                    }
                                 }
+                                __syncwarp();
                                 if (used < kStages) ++used;
                                 if (++s == kStages) { s = 0; phase ^= 1; }
                             }
@@ -509,7 +519,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             }
         }
     } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
+        if (rank == 0) {
+            const bool one = elect_one();
             uint32_t s = 0, phase = 0, it = 0;
             bool ok = true;
             for (Order o(a, pair, pairs); ok && o.now() < a.tiles; o.next()) {
@@ -524,20 +535,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 ok = for_pieces<T>(tl, [&](uint32_t, uint32_t from, uint32_t to, bool begins, bool ends) {
                     const uint32_t acc = it & 1, d = tmem + acc * kTileN;
                     if (begins) {
-                        if (!bar_wait(acc_empty + 8 * acc, (it >> 1 & 1) ^ 1, a.gave_up)) return false;
+                        if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_empty + 8 * acc, (it >> 1 & 1) ^ 1, a.gave_up))) return false;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     }
                     const uint32_t steps = n_pairs * (to - from);
                     for (uint32_t k = 0; k < steps; ++k) {
-                        if (!bar_wait(full + 8 * s, phase, a.gave_up)) return false;
+                        if (!__all_sync(0xFFFFFFFFu, bar_wait(full + 8 * s, phase, a.gave_up))) return false;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        if (one) {
 #pragma unroll
-                        for (uint32_t j = 0; j < kTileK / 16; ++j)
-                            mma(d, da + s * (kStageBytes / 16) + j * sa, db + s * (kStageBytes / 16) + j * sb, idesc, !begins || k > 0 || j > 0);
-                        mma_commit(empty + 8 * s);
+                            for (uint32_t j = 0; j < kTileK / 16; ++j)
+                                mma(d, da + s * (kStageBytes / 16) + j * sa, db + s * (kStageBytes / 16) + j * sb, idesc, !begins || k > 0 || j > 0);
+                            mma_commit(empty + 8 * s);
+                        }
+                        __syncwarp();
                         if (++s == kStages) { s = 0; phase ^= 1; }
                     }
-                    if (ends) { mma_commit(acc_full + 8 * acc); ++it; }
+                    if (ends) {
+                        if (one) mma_commit(acc_full + 8 * acc);
+                        __syncwarp();
+                        ++it;
+                    }
                     return true;
                 });
             }
