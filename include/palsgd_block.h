@@ -57,7 +57,7 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
 /*
  * Gated feed-forward block of worker k, x [tokens, d_model], w_gate and w_up [d_ff, d_model], w_down [d_model, d_ff]:
  *   g = x w_gate^T;  u = x w_up^T;  h = act(g) * u;  y = h w_down^T
- * act: SILU g/(1+e^-g);  GELU g Phi(g);  GELU_TANH g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)));  RELU max(g, 0).
+ * act: SILU g/(1+e^-g);  GELU g Phi(g);  GELU_TANH g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)));  RELU g > 0 ? g : 0.
  * g and u stay in binary32 up to h.  BF16: h is rounded to bfloat16 once, for the second product.
  *
  * `save` names what the forward call keeps for the backward call (and the form the backward call finds it in):
@@ -73,7 +73,9 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
  * Outputs are overwritten.  tokens = 0: the weight gradients are zero.  dx may be NULL (first layer).
  *
  * FP32 products are formed on the tensor cores from three bfloat16 parts of each operand (24 bits together), all six
- * products of parts that reach above 2^-24 of the whole, summed in binary32.
+ * products of parts that reach above 2^-24 of the whole, summed in binary32 with a rounding to nearest every 256 terms.
+ * An infinite operand gives NaN there where a product of binary32 would be infinite.  Results do not depend on timing:
+ * the same call gives the same bits.
  *
  * Workspace: call with workspace = NULL to learn *workspace_bytes (nothing is enqueued; all other arguments as in the
  * call to come); then pass at least that many bytes, 256-byte aligned.  Contents need no preparation.  A workspace that

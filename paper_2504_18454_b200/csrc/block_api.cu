@@ -369,7 +369,7 @@ struct Product {
 // sums that are written and read again in a step's time).  Of a few cuts -- shares of the average load of a pair, or up to
 // three times that -- the one that should end first, if it ends before no cut at all.  (One worker, one token, 2048 x
 // 5632: the second product is 8 tiles of 88 steps, the forward call 68 us uncut and 48 us cut.)
-constexpr uint64_t kJoin = 20, kStepBytes = 4000000;
+constexpr uint64_t kJoin = 26, kStepBytes = 4000000;
 constexpr uint32_t kMaxSplits = 32;
 
 void plan_splits(Product* p, int n, uint32_t K, uint32_t parts, uint64_t pairs)
@@ -401,7 +401,7 @@ void plan_splits(Product* p, int n, uint32_t K, uint32_t parts, uint64_t pairs)
     }
     for (int i = 0; share && i < n; ++i) {
         const uint64_t c = ceil_div(p[i].steps(parts), share);
-        // (fp32: a share is of whole steps of the inner axis, each six products)
+        // (fp32: a share is of whole steps of the inner axis)
         const uint64_t most = p[i].steps(1);
         p[i].splits = (uint32_t)(c > kMaxSplits ? kMaxSplits : c);
         if (p[i].splits > most) p[i].splits = (uint32_t)most;

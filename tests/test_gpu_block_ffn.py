@@ -295,3 +295,22 @@ def test_a_thread_that_has_not_used_the_gpu_yet():
     t.join()
     torch.cuda.synchronize()
     assert len(got) == 4 and all(torch.equal(a, b) for a, b in zip(got, want)), got
+
+
+def test_offsets_beyond_31_bits():
+    """One worker, a million tokens: gate, up and the hidden rows pass 2^31 elements.  The last rows are compared with the
+    64-bit statement, and so are the weight gradients of a batch whose gradient is zero but for them."""
+    M, D, F, tail = 1_000_037, 16, 2200, 300
+    x, wg, wu, wd, dy = _inputs(1, M, D, F, torch.bfloat16, seed=15)
+    dy[:, :-tail] = 0
+    y, saved = P.ffn_forward(x, wg, wu, wd)
+    xt, dyt = x[:, -tail:], dy[:, -tail:]
+    want = ffn_forward64(xt, wg, wu, wd, 0, True)
+    within(y[:, -tail:], *want["y"], "y")
+    _check_saved([s[:, -tail:] for s in saved], want, P.SAVE_FULL, torch.bfloat16, 1, tail, F)
+    got = P.ffn_backward(dy, x, wg, wu, wd, saved)
+    ref = ffn_backward64(dyt, xt, wg, wu, wd, *(s[:, -tail:] for s in saved), 0, True)
+    within(got[0][:, -tail:], *ref["dx"], "dx")
+    assert bool((got[0][:, :-tail] == 0).all())
+    for t, name in zip(got[1:], ("dw_gate", "dw_up", "dw_down")):
+        within(t, *ref[name], name)
