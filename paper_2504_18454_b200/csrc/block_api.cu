@@ -538,7 +538,7 @@ bool heads_wide(const void* p, int64_t w, int64_t t, int64_t h, size_t es)
 
 constexpr int kQkCtasPerSm = 4;                          // resident at the least, of the kernels that the usual sizes take
 
-struct QkPlan { QkArgs a; int V, NS; };
+struct QkPlan { QkArgs a; int V, NS, pairs; };
 
 // CTAs by the workers, and by q and k as their heads are.  Needs nothing of the operands: the workspace goes by it.
 void share_out(QkArgs& a, const palsgd_qk_shape* s)
@@ -573,15 +573,16 @@ void finish_qk(QkPlan& p, const palsgd_qk_shape* s, bool back)
     QkArgs& a = p.a;
     const size_t es = elem(s->precision);
     const int v = (int)(16 / es);
-    bool wide = s->head_dim % v == 0 && (s->interleaved || (s->rotary_dim / 2) % v == 0);
+    bool wide = s->head_dim % v == 0;
     for (const HeadsArg& h : a.side)
         if (h.heads)
             wide = wide && heads_wide(h.x, h.xw, h.xt, h.xh, es) && heads_wide(h.out, h.ow, h.ot, h.oh, es) &&
                    (!back || heads_wide(h.d, h.dw, h.dt, h.dh, es));
     p.V = wide ? v : 1;
-    const uint32_t half_vec = s->rotary_dim / 2 / p.V, n_vec = s->head_dim / p.V;
-    a.pair_slots = s->interleaved ? (p.V == 1 ? s->rotary_dim / 2 : 0) : half_vec;
-    a.slots = s->interleaved ? (n_vec + 1) / 2 : half_vec + (n_vec - 2 * half_vec + 1) / 2;
+    const uint32_t half = s->rotary_dim / 2, n_vec = s->head_dim / p.V;
+    p.pairs = s->interleaved ? QK_INTER : half % p.V ? QK_CROSS : QK_SPLIT;
+    a.pair_slots = p.pairs == QK_SPLIT || p.V == 1 ? half / p.V : 0;
+    a.slots = p.pairs == QK_SPLIT ? half / p.V + (n_vec - 2 * (half / p.V) + 1) / 2 : (n_vec + 1) / 2;
     a.lanes = 1;
     while (a.lanes < 32 && a.lanes < a.slots) a.lanes *= 2;
     p.NS = 1;
@@ -599,7 +600,7 @@ void finish_qk(QkPlan& p, const palsgd_qk_shape* s, bool back)
     }
 }
 
-template <typename T, bool BACK, bool INTER>
+template <typename T, bool BACK, int PAIRS>
 int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
 {
     const dim3 grid(p.a.ctas[0] + p.a.ctas[1], s->K);
@@ -608,22 +609,30 @@ int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
     auto run = [&](void (*kernel)(const QkArgs), int V, int NS) { return launch(what, kernel, grid, kQkThreads, qk_smem(V, NS, BACK, s->head_dim), st, p.a); };
     if (p.V == W && p.NS == 1) {
         switch (p.a.lanes) {
-            case 4: return run(qk_kernel<T, W, 1, BACK, INTER, 4>, W, 1);
-            case 8: return run(qk_kernel<T, W, 1, BACK, INTER, 8>, W, 1);
-            case 16: return run(qk_kernel<T, W, 1, BACK, INTER, 16>, W, 1);
-            default: return run(qk_kernel<T, W, 1, BACK, INTER, 0>, W, 1);
+            case 4: return run(qk_kernel<T, W, 1, BACK, PAIRS, 4>, W, 1);
+            case 8: return run(qk_kernel<T, W, 1, BACK, PAIRS, 8>, W, 1);
+            case 16: return run(qk_kernel<T, W, 1, BACK, PAIRS, 16>, W, 1);
+            default: return run(qk_kernel<T, W, 1, BACK, PAIRS, 0>, W, 1);
         }
     }
-    if (p.V == W) return run(qk_kernel<T, W, 2, BACK, INTER, 32>, W, 2);
-    if (p.NS <= 2) return run(qk_kernel<T, 1, 2, BACK, INTER, 0>, 1, 2);
-    return run(qk_kernel<T, 1, 8, BACK, INTER, 32>, 1, 8);
+    if (p.V == W) return run(qk_kernel<T, W, 2, BACK, PAIRS, 32>, W, 2);
+    if constexpr (PAIRS != QK_CROSS) {                   // (one value a vector is never across)
+        if (p.NS <= 2) return run(qk_kernel<T, 1, 2, BACK, PAIRS, 0>, 1, 2);
+        return run(qk_kernel<T, 1, 8, BACK, PAIRS, 32>, 1, 8);
+    }
+    return PALSGD_EUNSUPPORTED;
+}
+
+template <typename T, bool BACK>
+int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
+{
+    return p.pairs == QK_INTER ? launch_qk<T, BACK, QK_INTER>(p, s, st) : p.pairs == QK_CROSS ? launch_qk<T, BACK, QK_CROSS>(p, s, st) : launch_qk<T, BACK, QK_SPLIT>(p, s, st);
 }
 
 template <bool BACK>
 int run_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
 {
-    if (s->precision == PALSGD_PREC_FP32) return s->interleaved ? launch_qk<float, BACK, true>(p, s, st) : launch_qk<float, BACK, false>(p, s, st);
-    return s->interleaved ? launch_qk<bf16, BACK, true>(p, s, st) : launch_qk<bf16, BACK, false>(p, s, st);
+    return s->precision == PALSGD_PREC_FP32 ? launch_qk<float, BACK>(p, s, st) : launch_qk<bf16, BACK>(p, s, st);
 }
 
 }  // namespace

@@ -237,6 +237,10 @@ __device__ __forceinline__ void slot_put(T* base, const uint32_t (&at)[2], const
     }
 }
 
+// Where a value's partner of the rotation is: SPLIT the same place of another vector of the lane (halves of whole vectors);
+// INTER the next value; CROSS (halves of other sizes) any place of the head, read from the ring's other lanes.
+enum { QK_SPLIT = 0, QK_INTER = 1, QK_CROSS = 2 };
+
 // A warp takes a few tokens at a time and walks their heads; `lanes` lanes share a head, and a slot of a lane holds both
 // halves of its rotation pairs, so the rotation needs no exchange: for split halves vectors s and s + rot/(2V), for
 // interleaved pairs two neighbouring vectors (V > 1: the pairs lie inside a vector; V = 1: the slot is the pair).  Values
@@ -246,10 +250,11 @@ __device__ __forceinline__ void slot_put(T* base, const uint32_t (&at)[2], const
 // angles), so a warp's groups are spread over heads only as far as leaves four heads or so in a row to each.  Each lane
 // brings what it will work on into shared memory by asynchronous copies, kRing items ahead (held in registers, one item
 // ahead was all there was room for).  V = 1, for layouts without 16-byte boundaries, reads directly.
-template <typename T, int V, int NS, bool BACK, bool INTER, int LANES, int SIDE>
+template <typename T, int V, int NS, bool BACK, int PAIRS, int LANES, int SIDE>
 __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, unsigned char* smem)
 {
-    constexpr bool kInside = INTER || V == 1;                                 // a rotation pair is one f2 (else: f2 i and V/2 + i)
+    constexpr bool kCross = PAIRS == QK_CROSS;
+    constexpr bool kInside = PAIRS == QK_INTER || V == 1;                     // a rotation pair is one f2 (else: f2 i and V/2 + i)
     constexpr int H = V / 2;
     constexpr uint32_t kWarps = kQkThreads / 32;
     const uint32_t lanes = LANES ? LANES : a.lanes;
@@ -264,9 +269,9 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
     const T* wp = static_cast<const T*>(h.w) + (int64_t)k * h.ww;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        const uint32_t slot = s * lanes + sub, split = INTER ? 0 : a.pair_slots;
+        const uint32_t slot = s * lanes + sub, split = PAIRS == QK_SPLIT ? a.pair_slots : 0;
         uint32_t v0, v1;
-        if (!INTER && slot < split) { v0 = slot; v1 = slot + split; }
+        if (PAIRS == QK_SPLIT && slot < split) { v0 = slot; v1 = slot + split; }
         else { v0 = 2 * split + 2 * (slot - split); v1 = v0 + 1; }
         at[s][0] = slot < a.slots && v0 < n_vec ? v0 * V : ~0u;
         at[s][1] = slot < a.slots && v1 < n_vec ? v1 * V : ~0u;
@@ -279,6 +284,20 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[s][j] = 0;
         }
+    }
+    // CROSS: the partner of each value -- its weight, and where it lies in an item of the ring
+    T w_of[kCross ? NS : 1][2 * V];
+    uint32_t lies[kCross ? NS : 1][2 * V];
+    if constexpr (kCross) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int j = 0; j < 2 * V; ++j) {
+                const uint32_t e = at[s][j / V] == ~0u ? 0 : at[s][j / V] + j % V;
+                const uint32_t q = e < half ? e + half : e < a.rot ? e - half : e, v = q / V, sl = v / 2;
+                w_of[s][j] = wp[q];
+                lies[s][j] = ((sl / lanes) * 2 + (v & 1)) * 512 + (sl % lanes) * 16 + q % V * (uint32_t)sizeof(T) - sub * 16;
+            }
     }
     const float inv_n = 1.0f / (float)a.head_dim;
     // the warp's groups: `abreast` heads of each of `tokens` tokens
@@ -340,6 +359,27 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
             v[0] = f2_of(from && at[s][0] != ~0u ? to_f(from[at[s][0]]) : 0.0f, from && at[s][1] != ~0u ? to_f(from[at[s][1]]) : 0.0f);
         }
     };
+    // CROSS: the partners of a slot's values in an item
+    auto partners = [&](uint32_t slot, bool second, int s, f2 (&v)[V]) {
+        if constexpr (kCross) {
+            const uint32_t from = mine + (slot * kVecs + (second ? NS * 2 : 0)) * 512;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float f[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (sizeof(T) == 4) {
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[i]) : "r"(from + lies[s][2 * j + i]));
+                    } else {
+                        uint32_t h;
+                        asm volatile("{\n .reg .b16 t;\n ld.shared.b16 t, [%1];\n cvt.u32.u16 %0, t;\n}" : "=r"(h) : "r"(from + lies[s][2 * j + i]));
+                        f[i] = __uint_as_float(h << 16);
+                    }
+                }
+                v[j] = f2_of(f[0], f[1]);
+            }
+        }
+    };
     auto over_head = [&](f2 v2) {
         float v, u;
         f2_get(v2, v, u);
@@ -365,6 +405,26 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
         bad = ok ? 0.0f : __uint_as_float(0x7FFFFFFFu);                       // outside the table: NaN
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
+            if constexpr (kCross) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float c[2], sn[2], w0[2], w1[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int k2 = 2 * j + i;
+                        const uint32_t e = at[s][k2 / V] == ~0u ? a.rot : at[s][k2 / V] + k2 % V, n = e < half ? e : e - half;
+                        const bool on = e < a.rot && ok;
+                        c[i] = on ? __ldg(ct + n) : 1.0f;
+                        sn[i] = on ? __ldg(st + n) : 0.0f;
+                        if ((e < half) != BACK) sn[i] = -sn[i];               // (a, b) -> (a c - b s, b c + a s), or back
+                        w0[i] = to_f(w[s][k2]);
+                        w1[i] = to_f(w_of[s][k2]);
+                    }
+                    mc[s][j] = BACK ? f2_of(c[0], c[1]) : f2_of(c[0] * w0[0], c[1] * w0[1]);
+                    ms[s][j] = BACK ? f2_of(sn[0], sn[1]) : f2_of(sn[0] * w1[0], sn[1] * w1[1]);
+                }
+                continue;
+            }
             float c[V], sn[V];
             const uint32_t i = (s * lanes + sub) * V;                       // first pair of the slot
             if (V > 1 && a.table_wide && i + V <= half && ok) {
@@ -424,19 +484,22 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
             for (int s = 0; s < NS; ++s) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) x[s][j] = f2_mul(x[s][j], rr);
+                f2 q[V];
+                partners(slot, false, s, q);
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    y[s][j] = f2_fma(x[s][j], mc[s][j], f2_mul(kInside ? f2_swap(x[s][j]) : x[s][(j + H) % V], ms[s][j]));
+                    y[s][j] = f2_fma(x[s][j], mc[s][j], f2_mul(kCross ? f2_mul(q[j], rr) : kInside ? f2_swap(x[s][j]) : x[s][(j + H) % V], ms[s][j]));
             }
         } else {
             f2 dot = 0;
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                f2 d[V];
+                f2 d[V], q[V];
                 values(slot, true, s, live ? db + go : nullptr, d);
+                partners(slot, true, s, q);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    y[s][j] = f2_fma(d[j], mc[s][j], f2_mul(kInside ? f2_swap(d[j]) : d[(j + H) % V], ms[s][j]));
+                    y[s][j] = f2_fma(d[j], mc[s][j], f2_mul(kCross ? q[j] : kInside ? f2_swap(d[j]) : d[(j + H) % V], ms[s][j]));
                     x[s][j] = f2_mul(x[s][j], rr);                            // xh
                     acc[s][j] = f2_fma(y[s][j], x[s][j], acc[s][j]);
                     y[s][j] = f2_mul(y[s][j], weight(s, j));
@@ -473,8 +536,10 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
         const bool in = tk < a.tokens;
         int64_t xo = (int64_t)tk * h.xt + (int64_t)first * h.xh, go = (int64_t)tk * h.dt + (int64_t)first * h.dh, oo = (int64_t)tk * h.ot + (int64_t)first * h.oh;
         for (uint32_t hd = first; hd - first < rounds * abreast; hd += abreast) {
+            if constexpr (kCross) __syncwarp();                               // (all lanes have done with that item)
             fetch(slot == 0 ? kRing - 1 : slot - 1);                          // into the place of the item before this one
             if constexpr (V > 1) asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+            if constexpr (kCross) __syncwarp();                               // (and what the other lanes brought is there)
             work(slot, in && hd < h.heads, xo, go, oo);
             slot = slot + 1 == kRing ? 0 : slot + 1;
             if constexpr (V == 1) { xo += abreast * h.xh; go += abreast * h.dh; }
@@ -509,14 +574,14 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
 // (Two copies of the walk: with the side a constant its strides are constants of the instruction, not loads by index.)
 // LANES: the lanes that share a head where the host picks a copy made for them (0: any; the sum over a head is then a
 // chain of branches, which take a tenth of the time).
-template <typename T, int V, int NS, bool BACK, bool INTER, int LANES>
+template <typename T, int V, int NS, bool BACK, int PAIRS, int LANES>
 __global__ void __launch_bounds__(kQkThreads, NS == 1 ? 4 : 1) qk_kernel(const __grid_constant__ QkArgs a)
 {
     let_next_start();
     wait_for_previous();
     extern __shared__ __align__(16) unsigned char smem[];
-    if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, INTER, LANES, 0>(a, blockIdx.x, smem);
-    else qk_walk<T, V, NS, BACK, INTER, LANES, 1>(a, blockIdx.x - a.ctas[0], smem);
+    if (blockIdx.x < a.ctas[0]) qk_walk<T, V, NS, BACK, PAIRS, LANES, 0>(a, blockIdx.x, smem);
+    else qk_walk<T, V, NS, BACK, PAIRS, LANES, 1>(a, blockIdx.x - a.ctas[0], smem);
 }
 
 struct QkSumArgs {
