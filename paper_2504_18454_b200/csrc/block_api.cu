@@ -304,19 +304,23 @@ int run_stage(const Stage& st, uint32_t K, int sms, cudaStream_t stream)
     return launch("operand copies", stage_kernel, dim3((unsigned)(want < cap ? want : cap), st.n, K), 256, 0, stream, st.a);
 }
 
-int encode(CUtensorMap* map, const Operand& o, bool mn)
+// box: columns and rows of one copy, its order in shared memory
+int encode(CUtensorMap* map, const Operand& o, uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle order)
 {
     const cuuint64_t dims[4] = {o.cols, o.rows, o.one ? 1u : o.K, o.parts};
     // a dimension of one element is never stepped over, but its stride has to be a valid one
     const cuuint64_t row = (cuuint64_t)o.r * 2, w = o.one ? row : (cuuint64_t)o.w * 2, part = o.parts > 1 ? (cuuint64_t)o.part * 2 : row;
     const cuuint64_t strides[3] = {row, w, part};
-    const cuuint32_t box[4] = {64, mn ? kTileK : 128u, 1, 1}, unit[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {box_cols, box_rows, 1, 1}, unit[4] = {1, 1, 1, 1};
     const CUresult rc = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.p), dims, strides, box, unit,
-                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                 CU_TENSOR_MAP_INTERLEAVE_NONE, order, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (rc == CUDA_SUCCESS) return PALSGD_OK;
     return palsgd_block_cuda_fail((int)rc, "cuTensorMapEncodeTiled");   // (the runtime's codes are the driver's)
 }
+
+int encode(CUtensorMap* map, const Operand& o, bool mn) { return encode(map, o, 64, mn ? kTileK : 128, CU_TENSOR_MAP_SWIZZLE_128B); }
+int encode_store(CUtensorMap* map, const Operand& o) { return encode(map, o, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B); }
 
 MatOut out_of(const palsgd_mat* m, uint64_t cols, size_t es)
 {
@@ -696,6 +700,7 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
     MatLaunch gated{};
     BLOCK_TRY(add_problem(gated, M, F, D, s->K, &ox, nullptr, false, &og, &ou, false, kTileN / 2));
     gated.p[0].out[0] = out_of(oh);
+    if (parts == 1) BLOCK_TRY(encode_store(&gated.store[0], oh));
     set_saved(gated, s, gate, up, gate_e, up_e);
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_GATED>(gated, s, dev, st));
@@ -769,7 +774,10 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     BLOCK_TRY(device_of(dev));
     MatLaunch hidden{};
     BLOCK_TRY(add_problem(hidden, M, F, D, s->K, &ody, nullptr, false, &od, nullptr, true, kTileN));
-    for (int i = 0; i < 3; ++i) hidden.p[0].out[i] = out_of(hid[i]);
+    for (int i = 0; i < 3; ++i) {
+        hidden.p[0].out[i] = out_of(hid[i]);
+        if (parts == 1) BLOCK_TRY(encode_store(&hidden.store[i], hid[i]));
+    }
     set_saved(hidden, s, gate, up, gate_e, up_e);
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s, dev, st));

@@ -28,8 +28,8 @@ constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr uint32_t kBarrierBytes = 256;
 constexpr uint32_t kPiece = 4;                                          // fp32: steps of kTileK between two roundings to binary32
 
-// Shared memory and warps of a kernel: 16 epilogue warps of 64 columns each (8 of 128 took three times as long in the
-// hidden pass: two warps a scheduler do not cover each other's latencies).  They pass their results (and, in the hidden
+// Shared memory and warps of a kernel: 16 epilogue warps of 64 columns each (8 of 128 took 59 us where these took 49
+// in the hidden pass: two warps a scheduler do not cover each other's latencies).  They pass their results (and, in the hidden
 // pass, gate and up) through blocks of 32 rows of 64 bytes in shared memory: 32 columns of bfloat16, 16 of fp32.
 template <typename T, int MODE>
 struct MatShape {
@@ -70,6 +70,7 @@ struct MatLaunch {
     int      save;
     MatOut   gate, up;            // saved (gate/up pass) or read (hidden pass)
     MatOut   gate_e, up_e;
+    CUtensorMap store[3];         // bfloat16: h (gate/up), or dg, du, h (hidden), as the copy engine writes blocks of them
     unsigned int* gave_up;
 };
 
@@ -135,6 +136,16 @@ __device__ __forceinline__ void tma_load(const CUtensorMap* map, uint32_t dst, u
     asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                  ::"r"(dst), "l"(map), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
+// A block of 32 x 32 bfloat16 (64-byte swizzle, which is the order of block_at<64>) to a matrix; what is outside is dropped.
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, uint32_t c0, uint32_t c1, uint32_t c2)
+{
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(0) : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }   // the blocks may be written again
+__device__ __forceinline__ void tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void block_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void mma_commit(uint32_t bar)                // to this barrier of both CTAs
 {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
@@ -323,30 +334,27 @@ __device__ __forceinline__ float next_part(float& v)
     return hi;
 }
 
-// A block of an operand of the next product -> workspace: bfloat16, or the three parts of 16 fp32 columns.
+// A block of 16 fp32 columns of an operand of the next product -> workspace, as its three parts.
 template <typename T>
 __device__ __forceinline__ void operand_out(uint32_t base, const MatOut& o, int64_t at, uint32_t rows, uint32_t room, uint32_t lane)
 {
-    if constexpr (sizeof(T) == 2) {
-        block_out<64, 2>(base, static_cast<unsigned char*>(o.p) + 2 * at, 2 * o.r, rows, room, true, lane);
-    } else {
-        const uint32_t piece = lane & 3;
-        bf16* p = static_cast<bf16*>(o.p) + at + (int64_t)(lane >> 2) * o.r + piece * 4;
+    static_assert(sizeof(T) == 4, "bfloat16 blocks go out by the copy engine");
+    const uint32_t piece = lane & 3;
+    bf16* p = static_cast<bf16*>(o.p) + at + (int64_t)(lane >> 2) * o.r + piece * 4;
 #pragma unroll 1
-        for (uint32_t row = lane >> 2; row < 32; row += 8) {
-            float v[4];
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(block_at<64>(base, row, piece)));
-            if (row < rows && piece * 4 < room) {         // (the workspace's rows hold a multiple of eight columns)
+    for (uint32_t row = lane >> 2; row < 32; row += 8) {
+        float v[4];
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(block_at<64>(base, row, piece)));
+        if (row < rows && piece * 4 < room) {             // (the workspace's rows hold a multiple of eight columns)
 #pragma unroll
-                for (int part = 0; part < 3; ++part) {
-                    float hi[4];
+            for (int part = 0; part < 3; ++part) {
+                float hi[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) hi[i] = next_part(v[i]);
-                    *reinterpret_cast<uint2*>(p + part * o.part) = make_uint2(f2_narrow(f2_of(hi[0], hi[1])), f2_narrow(f2_of(hi[2], hi[3])));
-                }
+                for (int i = 0; i < 4; ++i) hi[i] = next_part(v[i]);
+                *reinterpret_cast<uint2*>(p + part * o.part) = make_uint2(f2_narrow(f2_of(hi[0], hi[1])), f2_narrow(f2_of(hi[2], hi[3])));
             }
-            p += 8 * o.r;
         }
+        p += 8 * o.r;
     }
 }
 
@@ -578,7 +586,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
         // blocks of kCols columns, eight columns at a time in a loop (unrolled, they outgrow the instruction cache)
         constexpr uint32_t E = sizeof(T), kCols = 64 / E, kOcts = kCols / 8, kMine = MODE == MAT_GATED ? 32 : 64, kChunks = kMine / kCols;
         const uint32_t b0 = blocks + (warp - 4) * Shape::kBlocks * 2048, b1 = b0 + 2048;
-        const bool eight = a.save == PALSGD_SAVE_8BIT;
+        const bool eight = a.save == PALSGD_SAVE_8BIT, one = elect_one();
+        bool stored = false;                                              // gate/up: the block may still be read by the copy engine
         uint32_t ge = 0, ue = 0;                                          // hidden, 8 bits: exponents of the block under way
         // hidden: gate and up of block c of a tile into the warp's two blocks
         auto fetch = [&](const Tile& tl, uint32_t c) {
@@ -696,7 +705,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     block_out<64, E>(b0, static_cast<unsigned char*>(p.out[0].p) + E * to, E * p.out[0].r, rows, room, p.out[0].wide, lane);
                     __syncwarp();
                 } else if constexpr (MODE == MAT_GATED) {
-                    // gate, up and h pass through one block, one after another (tensor memory is read again for each)
+                    // gate, up and h pass through one block, one after another (tensor memory is read again for each); h goes
+                    // out by the copy engine, and the block is free again by the time the next tile is there
+                    if (E == 2 && stored) { tma_store_read(); stored = false; }
+                    __syncwarp();
                     if (a.save != PALSGD_SAVE_NONE) {
 #pragma unroll 1
                         for (uint32_t which = 0; which < 2; ++which) {
@@ -739,10 +751,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                         }
                         row_put<T>(b0, lane, j, h);
                     }
+                    if (E == 2) block_to_async();
                     if (c + 1 == kChunks) acc_read();
                     __syncwarp();
-                    operand_out<T>(b0, p.out[0], at, rows, room, lane);
-                    __syncwarp();
+                    if constexpr (E == 2) {
+                        if (one && rows && cols) {
+                            tma_store(&a.store[0], b0, n, m, tl.worker);
+                            tma_store_commit();
+                            stored = true;
+                        }
+                    } else {
+                        operand_out<T>(b0, p.out[0], at, rows, room, lane);
+                        __syncwarp();
+                    }
                 } else {
                     block_wait();
                     __syncwarp();
@@ -777,21 +798,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                         }
                     }
                     tmem_store_wait();
-                    __syncwarp();
-                    operand_out<T>(b0, p.out[0], at, rows, room, lane);
-                    operand_out<T>(b1, p.out[1], at, rows, room, lane);
-                    __syncwarp();
-                    {
-                        float h[16];                                      // 64 bytes of a row in either type
-                        tmem_load16(from, h);
+                    float h[16];                                          // 64 bytes of a row in either type
+                    tmem_load16(from, h);
+                    if constexpr (E == 2) {
+                        // dg and du leave by the copy engine (100 MB of dg, du and h: 49 us through the warps, 46 so)
+                        block_to_async();
+                        __syncwarp();
+                        if (one && rows && cols) {
+                            tma_store(&a.store[0], b0, n, m, tl.worker);
+                            tma_store(&a.store[1], b1, n, m, tl.worker);
+                            tma_store_commit();
+                        }
                         tmem_load_wait();
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            sts128(block_at<64>(b0, lane, j), make_uint4(__float_as_uint(h[4 * j]), __float_as_uint(h[4 * j + 1]), __float_as_uint(h[4 * j + 2]), __float_as_uint(h[4 * j + 3])));
+                        if (c + 1 == kChunks) acc_read();
+                        if (one) tma_store_read();
+                        __syncwarp();
+                    } else {
+                        tmem_load_wait();
+                        if (c + 1 == kChunks) acc_read();
+                        __syncwarp();
+                        operand_out<T>(b0, p.out[0], at, rows, room, lane);
+                        operand_out<T>(b1, p.out[1], at, rows, room, lane);
+                        __syncwarp();
                     }
-                    if (c + 1 == kChunks) acc_read();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        sts128(block_at<64>(b0, lane, j), make_uint4(__float_as_uint(h[4 * j]), __float_as_uint(h[4 * j + 1]), __float_as_uint(h[4 * j + 2]), __float_as_uint(h[4 * j + 3])));
+                    if (E == 2) block_to_async();
                     __syncwarp();
-                    operand_out<T>(b0, p.out[2], at, rows, room, lane);
+                    if constexpr (E == 2) {
+                        if (one && rows && cols) {
+                            tma_store(&a.store[2], b0, n, m, tl.worker);
+                            tma_store_commit();
+                            tma_store_read();
+                        }
+                    } else {
+                        operand_out<T>(b0, p.out[2], at, rows, room, lane);
+                    }
                     __syncwarp();
                     // the next block: of this tile, or the first of the warp's next tile
                     if (c + 1 < kChunks) fetch(tl, c + 1);
@@ -800,6 +843,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             }
         }
         if constexpr (MODE == MAT_HIDDEN) block_wait();
+        if (E == 2 && MODE != MAT_PLAIN && one) tma_store_done();
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
