@@ -289,9 +289,11 @@ Operand input_operand(Arena& ws, Stage& st, const palsgd_mat* m, const palsgd_ma
     Operand o = own_operand(ws, copies, rows, cols, kind == STAGE_SPLIT ? 3 : 1);
     o.K = K;
     o.one = copies == 1;
+    const int64_t unit = kind == STAGE_SPLIT ? 4 : 8;    // elements between the boundaries of wide loads
+    const bool wide = aligned(m->data, kind == STAGE_ACT8 ? 8 : 16) && m->row_stride % unit == 0 && w % unit == 0;
     StageItem& it = st.a.item[st.n++];
     it = StageItem{m->data, e ? static_cast<const uint8_t*>(e->data) : nullptr, w, m->row_stride, e ? e->worker_stride : 0, e ? e->row_stride : 0,
-                   static_cast<bf16*>(const_cast<void*>(o.p)), o.r, o.part, (uint32_t)rows, (uint32_t)cols, rows * (uint64_t)(o.r / 8), kind, copies};
+                   static_cast<bf16*>(const_cast<void*>(o.p)), o.r, o.part, (uint32_t)rows, (uint32_t)cols, rows * (uint64_t)(o.r / 8), divisor((uint32_t)(o.r / 8)), kind, wide, copies};
     return o;
 }
 

@@ -334,6 +334,40 @@ __device__ __forceinline__ float next_part(float& v)
     return hi;
 }
 
+// N fp32 values as their three bfloat16 parts: out(part, words of two).  Where all values are finite and none rounds past
+// the largest bfloat16, two at a time without a look at each (operand copies of an fp32 backward call: 18.3 -> 12.8 us).
+template <int N, typename Out>
+__device__ __forceinline__ void three_parts(float (&v)[N], Out&& out)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    if (top < 0x7F7F8000u) {
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+            uint32_t w[N / 2];
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                w[i] = f2_narrow(f2_of(v[2 * i], v[2 * i + 1]));
+                v[2 * i] = __fsub_rn(v[2 * i], __uint_as_float(w[i] << 16));
+                v[2 * i + 1] = __fsub_rn(v[2 * i + 1], __uint_as_float(w[i] & 0xFFFF0000u));
+            }
+            out(part, w);
+        }
+    } else {
+#pragma unroll 1
+        for (int part = 0; part < 3; ++part) {
+            uint32_t w[N / 2];
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const float lo = next_part(v[2 * i]), hi = next_part(v[2 * i + 1]);
+                w[i] = f2_narrow(f2_of(lo, hi));
+            }
+            out(part, w);
+        }
+    }
+}
+
 // A block of 16 fp32 columns of an operand of the next product -> workspace, as its three parts.
 template <typename T>
 __device__ __forceinline__ void operand_out(uint32_t base, const MatOut& o, int64_t at, uint32_t rows, uint32_t room, uint32_t lane)
@@ -346,13 +380,7 @@ __device__ __forceinline__ void operand_out(uint32_t base, const MatOut& o, int6
         float v[4];
         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(block_at<64>(base, row, piece)));
         if (row < rows && piece * 4 < room) {             // (the workspace's rows hold a multiple of eight columns)
-#pragma unroll
-            for (int part = 0; part < 3; ++part) {
-                float hi[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) hi[i] = next_part(v[i]);
-                *reinterpret_cast<uint2*>(p + part * o.part) = make_uint2(f2_narrow(f2_of(hi[0], hi[1])), f2_narrow(f2_of(hi[2], hi[3])));
-            }
+            three_parts<4>(v, [&](int part, const uint32_t (&w)[2]) { *reinterpret_cast<uint2*>(p + part * o.part) = make_uint2(w[0], w[1]); });
         }
         p += 8 * o.r;
     }
@@ -868,7 +896,9 @@ struct StageItem {
     int64_t  ld, part;            // row stride (multiple of 8) and part stride of dst; workers are rows * ld apart
     uint32_t rows, cols;
     uint64_t units;               // of 8 columns, one worker
+    Divisor  per_row;             // ld / 8
     int      kind;
+    int      wide;                // eight values of src start on a 16-byte (8 bits: 8-byte) boundary in every row
     uint32_t K;                   // workers to copy: 1 if all read one matrix
 };
 struct StageArgs { StageItem item[kMaxStaged]; };
@@ -878,12 +908,11 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
     let_next_start();
     wait_for_previous();
     const StageItem& it = a.item[blockIdx.y];
-    const uint32_t per = (uint32_t)(it.ld / 8);
     const int64_t k = blockIdx.z;
     if (k >= it.K) return;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < it.units; i += (uint64_t)gridDim.x * 256) {
-        const uint64_t row = it.units < 0x80000000ull ? (uint32_t)i / per : i / per;
-        const uint32_t c = (uint32_t)(i - row * per) * 8;
+        const uint64_t row = it.units < 0x80000000ull ? it.per_row.of((uint32_t)i) : i / it.per_row.d;
+        const uint32_t c = (uint32_t)(i - row * it.per_row.d) * 8;
         const int64_t from = k * it.w + (int64_t)row * it.r + c;
         float v[8];
         const uint32_t n = c < it.cols ? min(it.cols - c, 8u) : 0;
@@ -892,10 +921,15 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
             *reinterpret_cast<uint4*>(it.dst + (k * it.rows + (int64_t)row) * it.ld + c) = q;
             continue;
         } else if (it.kind == STAGE_ACT8) {
-            const uint4 q = get16(static_cast<const unsigned char*>(it.src) + from, n);
+            const unsigned char* p = static_cast<const unsigned char*>(it.src) + from;
+            uint2 q;
+            if (it.wide && n == 8) q = __ldg(reinterpret_cast<const uint2*>(p));
+            else { const uint4 t = get16(p, n); q = make_uint2(t.x, t.y); }
             const float s = act8_step(it.e[k * it.ew + (int64_t)row * it.er + c / 32]);
             act8_value4(q.x, s, v);
             act8_value4(q.y, s, v + 4);
+        } else if (it.wide && n == 8) {
+            Vec<float, 8>::load(static_cast<const float*>(it.src) + from, v);
         } else {
 #pragma unroll
             for (uint32_t j = 0; j < 2; ++j) {
@@ -905,13 +939,7 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
         }
         bf16* to = it.dst + (k * it.rows + (int64_t)row) * it.ld + c;
         if (it.kind == STAGE_SPLIT) {
-#pragma unroll
-            for (int part = 0; part < 3; ++part) {
-                float hi[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) hi[j] = next_part(v[j]);
-                Vec<bf16, 8>::store(to + part * it.part, hi);
-            }
+            three_parts<8>(v, [&](int part, const uint32_t (&w)[4]) { *reinterpret_cast<uint4*>(to + part * it.part) = make_uint4(w[0], w[1], w[2], w[3]); });
         } else {
             Vec<bf16, 8>::store(to, v);
         }
