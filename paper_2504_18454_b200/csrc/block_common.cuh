@@ -25,14 +25,6 @@ template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __flo
 
 // V consecutive values of T at p as floats: one 16-byte (or 32-byte, as two) access where V fills it, else one by one.
 template <typename T, int V> struct Vec;
-template <> struct Vec<float, 1> {
-    static __device__ __forceinline__ void load(const float* p, float* v) { v[0] = __ldg(p); }
-    static __device__ __forceinline__ void store(float* p, const float* v) { p[0] = v[0]; }
-};
-template <> struct Vec<bf16, 1> {
-    static __device__ __forceinline__ void load(const bf16* p, float* v) { v[0] = __bfloat162float(p[0]); }
-    static __device__ __forceinline__ void store(bf16* p, const float* v) { p[0] = __float2bfloat16_rn(v[0]); }
-};
 template <> struct Vec<float, 4> {
     static __device__ __forceinline__ void load(const float* p, float* v)
     {
@@ -49,13 +41,6 @@ template <> struct Vec<float, 8> {
     static __device__ __forceinline__ void store(float* p, const float* v) { Vec<float, 4>::store(p, v); Vec<float, 4>::store(p + 4, v + 4); }
 };
 template <> struct Vec<bf16, 8> {
-    static __device__ __forceinline__ void load(const bf16* p, float* v)
-    {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-    }
     static __device__ __forceinline__ void store(bf16* p, const float* v)
     {
         uint32_t w[4];
