@@ -371,7 +371,7 @@ struct Product {
 };
 
 // Cuts long inner axes into shares where a launch has too few tiles for the pairs of CTAs: the shares' binary32 sums go
-// to the workspace and one more small kernel joins them (kJoin: what that costs, in steps of 0.43 us; kStepBytes: the
+// to the workspace and one more small kernel joins them (kJoin: what that costs, in steps of about 0.35 us; kStepBytes: the
 // sums that are written and read again in a step's time).  Of a few cuts -- shares of the average load of a pair, or up to
 // three times that -- the one that should end first, if it ends before no cut at all.  (One worker, one token, 2048 x
 // 5632: the second product is 8 tiles of 88 steps, the forward call 68 us uncut and 48 us cut.)

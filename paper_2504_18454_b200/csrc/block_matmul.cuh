@@ -13,9 +13,10 @@
 // fp32 operands come as three bfloat16 parts each; the products of parts i, j with i + j <= 2 are summed as so many more
 // steps of the inner axis, the small ones first.
 //
-// What bounds it (bfloat16, one B200): 8 workers of 1024 tokens, 768 x 2048 -- gate/up pass 45 us (1145 TFLOP/s, tensor pipe
-// 65 % active: a step of 64 takes 0.29 us of matrix instructions and 0.43 us to bring), hidden pass 46 us (its epilogue: g, u
-// in, dg, du, h out), dx and the weight gradients 94 us (1370 TFLOP/s).  2 workers of 8192, 2048 x 5632, back to back: forward
+// What bounds it (bfloat16, one B200): 8 workers of 1024 tokens, 768 x 2048 -- gate/up pass 44 us (1170 TFLOP/s: 83
+// steps of 64 at 0.33 us, of which 0.29 are matrix instructions; the rest is the start, with operands from memory, and the last
+// tile's epilogue: 38 us if nothing is saved, 42 in full, 44 in 8 bits), hidden pass 46 us (its epilogue: g, u in, dg, du, h
+// out), dx and the weight gradients 94 us (1370 TFLOP/s).  2 workers of 8192, 2048 x 5632, back to back: forward
 // 0.88-0.92 ms, backward 1.9-2.04 ms, 1110-1290 TFLOP/s at the power limit, where a library product sustains 1385.
 // fp32: 8 workers of 500 tokens, 256 x 1024, backward 134-137 us.
 #pragma once
