@@ -542,15 +542,13 @@ bool heads_wide(const void* p, int64_t w, int64_t t, int64_t h, size_t es)
     return aligned(p, 16) && (w * es) % 16 == 0 && (t * es) % 16 == 0 && (h * es) % 16 == 0;
 }
 
-constexpr int kQkCtasPerSm = 4;                          // resident at the least, of the kernels that the usual sizes take
-
 struct QkPlan { QkArgs a; int V, NS, pairs; };
 
 // CTAs by the workers, and by q and k as their heads are.  Needs nothing of the operands: the workspace goes by it.
-void share_out(QkArgs& a, const palsgd_qk_shape* s)
+void share_out(QkArgs& a, const palsgd_qk_shape* s, bool back)
 {
     const uint32_t heads[2] = {s->heads_q, s->heads_k}, all = heads[0] + heads[1];
-    const uint64_t slots = (uint64_t)kQkCtasPerSm * sm_count() / s->K;
+    const uint64_t slots = (uint64_t)qk_ctas_per_sm(back) * sm_count() / s->K;
     for (int i = 0; i < 2; ++i) {
         uint64_t n = all ? slots * heads[i] / all : 0;
         const uint64_t most = ceil_div(s->tokens, kQkThreads / 32);
@@ -560,8 +558,7 @@ void share_out(QkArgs& a, const palsgd_qk_shape* s)
     }
 }
 
-
-QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos)
+QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos, bool back)
 {
     QkPlan p{};
     QkArgs& a = p.a;
@@ -570,7 +567,7 @@ QkPlan plan_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t,
     a.eps = (float)s->eps;
     a.table_wide = s->rotary_dim % 8 == 0 && aligned(cos_t, 16) && aligned(sin_t, 16);
     a.side[0].heads = s->heads_q; a.side[1].heads = s->heads_k;
-    share_out(a, s);
+    share_out(a, s, back);
     return p;
 }
 
@@ -600,7 +597,7 @@ void finish_qk(QkPlan& p, const palsgd_qk_shape* s, bool back)
         const uint32_t heads = a.side[i].heads;
         uint32_t n = 1;
         while (n < groups && n < heads &&
-               ((heads % (2 * n) == 0 && heads / (2 * n) >= 4) || s->tokens * s->K * n < (uint64_t)(kQkCtasPerSm * (kQkThreads / 32)) * sm_count() * groups))
+               ((heads % (2 * n) == 0 && heads / (2 * n) >= 4) || s->tokens * s->K * n < (uint64_t)(qk_ctas_per_sm(back) * (kQkThreads / 32)) * sm_count() * groups))
             n *= 2;
         a.abreast[i] = n;
     }
@@ -817,7 +814,7 @@ extern "C" int palsgd_qk_norm_rope_forward(const palsgd_qk_shape* s, const palsg
         if (heads[i]) BLOCK_TRY(check_mat(w[i], s->K, 1, s->head_dim, elem(s->precision), false));
     }
     if (s->tokens == 0 || (heads[0] | heads[1]) == 0) return PALSGD_OK;
-    QkPlan p = plan_qk(s, cos_table, sin_table, positions);
+    QkPlan p = plan_qk(s, cos_table, sin_table, positions, false);
     for (int i = 0; i < 2; ++i) {
         if (!heads[i]) continue;
         HeadsArg& h = p.a.side[i];
@@ -852,7 +849,7 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
         BLOCK_TRY(check_mat(dw[i], s->K, 1, s->head_dim, elem(s->precision), true));
     }
     BLOCK_TRY(check_workspace(workspace, workspace_bytes));
-    QkPlan p = plan_qk(s, cos_table, sin_table, positions);
+    QkPlan p = plan_qk(s, cos_table, sin_table, positions, true);
     Arena ws{static_cast<char*>(workspace), 0};
     float* part[2] = {nullptr, nullptr};
     for (int i = 0; i < 2; ++i)

@@ -166,6 +166,9 @@ __global__ void __launch_bounds__(256, LAYOUT == ACT8_LOOSE ? 4 : 6) act8_kernel
 // ------------------------------------------------------------------------------------------------ q/k norm + rotation
 
 constexpr uint32_t kQkThreads = 128;
+// CTAs of an SM: four forward (five spill and are 6 % slower, three 19 %); three backward, whose registers four do not hold
+// (8 workers, 2048 tokens, 12 + 12 heads of 64: 40.2 us with four, 32.9 with three; 2 of 32768, 16 + 4 of 128: 221 and 219)
+__host__ __device__ constexpr int qk_ctas_per_sm(bool back) { return back ? 3 : 4; }
 // items of a warp under way at a time, and a CTA's shared memory: the ring, or the warps' sums of the weight gradient
 __host__ __device__ constexpr int qk_ring(int V, int NS) { return V == 1 ? 1 : NS == 1 ? 4 : 2; }
 __host__ __device__ constexpr uint32_t qk_smem(int V, int NS, bool back, uint32_t head_dim)
@@ -577,7 +580,7 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
 // LANES: the lanes that share a head where the host picks a copy made for them (0: any; the sum over a head is then a
 // chain of branches, which take a tenth of the time).
 template <typename T, int V, int NS, bool BACK, int PAIRS, int LANES>
-__global__ void __launch_bounds__(kQkThreads, NS == 1 ? 4 : 1) qk_kernel(const __grid_constant__ QkArgs a)
+__global__ void __launch_bounds__(kQkThreads, NS == 1 ? qk_ctas_per_sm(BACK) : 1) qk_kernel(const __grid_constant__ QkArgs a)
 {
     let_next_start();
     wait_for_previous();
