@@ -277,7 +277,10 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
         const uint32_t slot = s * lanes + sub, split = PAIRS == QK_SPLIT ? a.pair_slots : 0;
         uint32_t v0, v1;
         if (PAIRS == QK_SPLIT && slot < split) { v0 = slot; v1 = slot + split; }
-        else { v0 = 2 * split + 2 * (slot - split); v1 = v0 + 1; }
+        // (the vectors of neighbouring lanes follow one another: interleaved in pairs, the two of a lane side by side, every
+        // access took half-filled sectors -- fp32 backward of 2 x 16384 tokens, 16 + 4 heads of 128: 303 us, so 150)
+        else if (PAIRS == QK_SPLIT || (PAIRS == QK_INTER && V > 1)) { v0 = split + slot; v1 = v0 + a.slots - split; }
+        else { v0 = 2 * slot; v1 = v0 + 1; }
         at[s][0] = slot < a.slots && v0 < n_vec ? v0 * V : ~0u;
         at[s][1] = slot < a.slots && v1 < n_vec ? v1 * V : ~0u;
 #pragma unroll
@@ -431,18 +434,40 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
                 continue;
             }
             float c[V], sn[V];
-            const uint32_t i = (s * lanes + sub) * V;                       // first pair of the slot
-            if (V > 1 && a.table_wide && i + V <= half && ok) {
-                if constexpr (V > 1) {
+            if constexpr (kInside && V > 1) {                                // pairs of two vectors, each of its own place
 #pragma unroll
-                    for (int j = 0; j < V; j += 4) { Vec<float, 4>::load(ct + i + j, c + j); Vec<float, 4>::load(st + i + j, sn + j); }
+                for (int p = 0; p < 2; ++p) {
+                    const uint32_t i = at[s][p] == ~0u ? half : at[s][p] / 2;
+                    if (a.table_wide && i + H <= half && ok) {
+                        if constexpr (H == 4) {
+                            Vec<float, 4>::load(ct + i, c + p * H); Vec<float, 4>::load(st + i, sn + p * H);
+                        } else {
+                            const float2 c2 = __ldg(reinterpret_cast<const float2*>(ct + i)), s2 = __ldg(reinterpret_cast<const float2*>(st + i));
+                            c[p * H] = c2.x; c[p * H + 1] = c2.y; sn[p * H] = s2.x; sn[p * H + 1] = s2.y;
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < H; ++j) {
+                            const bool on = i + j < half && ok;
+                            c[p * H + j] = on ? __ldg(ct + i + j) : 1.0f;
+                            sn[p * H + j] = on ? __ldg(st + i + j) : 0.0f;
+                        }
+                    }
                 }
             } else {
+                const uint32_t i = (s * lanes + sub) * V;                   // first pair of the slot
+                if (V > 1 && a.table_wide && i + V <= half && ok) {
+                    if constexpr (V > 1) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const bool on = i + j < half && ok;
-                    c[j] = on ? __ldg(ct + i + j) : 1.0f;
-                    sn[j] = on ? __ldg(st + i + j) : 0.0f;
+                        for (int j = 0; j < V; j += 4) { Vec<float, 4>::load(ct + i + j, c + j); Vec<float, 4>::load(st + i + j, sn + j); }
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const bool on = i + j < half && ok;
+                        c[j] = on ? __ldg(ct + i + j) : 1.0f;
+                        sn[j] = on ? __ldg(st + i + j) : 0.0f;
+                    }
                 }
             }
             if constexpr (kInside) {
