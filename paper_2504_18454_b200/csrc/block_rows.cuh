@@ -279,7 +279,7 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
         if (PAIRS == QK_SPLIT && slot < split) { v0 = slot; v1 = slot + split; }
         // (the vectors of neighbouring lanes follow one another: interleaved in pairs, the two of a lane side by side, every
         // access took half-filled sectors -- fp32 backward of 2 x 16384 tokens, 16 + 4 heads of 128: 303 us, so 150)
-        else if (PAIRS == QK_SPLIT || (PAIRS == QK_INTER && V > 1)) { v0 = split + slot; v1 = v0 + a.slots - split; }
+        else if (PAIRS != QK_INTER || V > 1) { v0 = split + slot; v1 = v0 + a.slots - split; }
         else { v0 = 2 * slot; v1 = v0 + 1; }
         at[s][0] = slot < a.slots && v0 < n_vec ? v0 * V : ~0u;
         at[s][1] = slot < a.slots && v1 < n_vec ? v1 * V : ~0u;
@@ -302,9 +302,9 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
 #pragma unroll
             for (int j = 0; j < 2 * V; ++j) {
                 const uint32_t e = at[s][j / V] == ~0u ? 0 : at[s][j / V] + j % V;
-                const uint32_t q = e < half ? e + half : e < a.rot ? e - half : e, v = q / V, sl = v / 2;
+                const uint32_t q = e < half ? e + half : e < a.rot ? e - half : e, v = q / V, p = v >= a.slots, sl = v - p * a.slots;
                 w_of[s][j] = wp[q];
-                lies[s][j] = ((sl / lanes) * 2 + (v & 1)) * 512 + (sl % lanes) * 16 + q % V * (uint32_t)sizeof(T) - sub * 16;
+                lies[s][j] = ((sl / lanes) * 2 + p) * 512 + (sl % lanes) * 16 + q % V * (uint32_t)sizeof(T) - sub * 16;
             }
     }
     const float inv_n = 1.0f / (float)a.head_dim;
