@@ -2,12 +2,21 @@
 
 They keep what the C ABI's backward calls ask for and nothing else; with `checkpoint8` the feed-forward block keeps its
 input, gate and up in 8 bits (8.25 bits a value), and its backward pass works on the values that those stand for.
+They are differentiable once: under create_graph=True their backward raises RuntimeError.
 """
 from __future__ import annotations
 
 import torch
 
 from . import block
+
+
+def _once(what: str) -> None:
+    """Their gradients carry no graph.  (torch's once_differentiable would not do: it raises only where the incoming
+    gradient needs one itself, and not for a derivative taken by the inputs.)"""
+    if torch.is_grad_enabled():
+        raise RuntimeError(f"{what} is differentiable once: its gradients carry no graph, so with create_graph=True a second "
+                           "derivative would lack its part")
 
 
 class _GatedFfn(torch.autograd.Function):
@@ -25,6 +34,7 @@ class _GatedFfn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
+        _once("gated_ffn")
         w_gate, w_up, w_down, *kept = ctx.saved_tensors
         if ctx.checkpoint8:
             kept = [block.Act8(kept[i], kept[i + 1], ctx.dtype) for i in (0, 2, 4)]
@@ -44,6 +54,7 @@ class _QkNormRope(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dq, dk):
+        _once("qk_norm_rope")
         q, k, *rest = ctx.saved_tensors
         dq, dk = (torch.zeros_like(t) if d is None else d if d.stride(-1) == 1 else d.contiguous()
                   for d, t in ((dq, q), (dk, k)))
