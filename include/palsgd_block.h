@@ -57,7 +57,7 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
 /*
  * Gated feed-forward block of worker k, x [tokens, d_model], w_gate and w_up [d_ff, d_model], w_down [d_model, d_ff]:
  *   g = x w_gate^T;  u = x w_up^T;  h = act(g) * u;  y = h w_down^T
- * act: SILU g/(1+e^-g);  GELU g Phi(g);  GELU_TANH g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)));  RELU g > 0 ? g : 0.
+ * act: SILU g/(1+e^-g);  GELU g Phi(g);  GELU_TANH g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)));  RELU max(g, 0).
  * g and u stay in binary32 up to h.  BF16: h is rounded to bfloat16 once, for the second product.
  *
  * `save` names what the forward call keeps for the backward call (and the form the backward call finds it in):
@@ -68,8 +68,9 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
  * Backward, at the saved g and u (the values that they stand for):
  *   dh = dy w_down;  du = dh act(g);  dg = dh u act'(g);  h = act(g) u
  *   dx = dg w_gate + du w_up;  dw_gate = dg^T x;  dw_up = du^T x;  dw_down = dy^T h
- * BF16: dg, du and h are rounded to bfloat16 once, for the products.  act'(0) of RELU is 0.  With save = 8BIT, x_e
- * may be given: x is then the int8 of an 8-bit checkpoint of x, x_e its exponents (x_e = NULL: x in the storage type).
+ * BF16: dg, du and h are rounded to bfloat16 once, for the products.  act'(0) of RELU is 0; a NaN in g gives NaN in act
+ * and act' of all four.  With save = 8BIT, x_e may be given: x is then the int8 of an 8-bit checkpoint of x, x_e its
+ * exponents (x_e = NULL: x in the storage type).
  * Outputs are overwritten.  tokens = 0: the weight gradients are zero.  dx may be NULL (first layer).
  *
  * FP32 products are formed on the tensor cores from three bfloat16 parts of each operand (24 bits together), all six

@@ -195,8 +195,9 @@ __device__ __forceinline__ float act(float g, float& slope)
         if constexpr (SLOPE) slope = fmaf(g * s * (1.0f - s), c * fmaf(0.134145f * g, g, 1.0f), s);
         return g * s;
     } else {
-        if constexpr (SLOPE) slope = g > 0.0f ? 1.0f : 0.0f;
-        return g > 0.0f ? g : 0.0f;
+        // (a NaN stays: what overflowed in a checkpoint has to reach the gradients)
+        if constexpr (SLOPE) slope = g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g;
+        return g <= 0.0f ? 0.0f : g;
     }
 }
 

@@ -1,0 +1,61 @@
+"""The block operators where values are not finite, sizes are empty, or work is long: against their 64-bit statements."""
+import pytest
+import torch
+
+import paper_2504_18454_b200 as P
+from _block_ref import ffn_backward64, ffn_forward64, within
+
+pytestmark = pytest.mark.gpu
+DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _ffn_inputs(K, M, D, F, dt, seed=1):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s, std: (torch.randn(*s, generator=gen, device="cuda") * std).to(dt)
+    return (r(K, M, D, std=1.0), r(K, F, D, std=D ** -0.5), r(K, F, D, std=D ** -0.5), r(K, D, F, std=F ** -0.5),
+            r(K, M, D, std=0.01))
+
+
+# ---------------------------------------------------------------------------------------------- NaN in the gate
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", range(4))
+def test_a_nan_of_the_gate_alone_reaches_the_result(dtype, kind):
+    x, wg, wu, wd, _ = _ffn_inputs(1, 40, 64, 96, DT[dtype])
+    wg[0, 5, 2] = float("nan")
+    y, (g, u) = P.ffn_forward(x, wg, wu, wd, activation=kind)
+    assert bool(g[..., 5].isnan().all()) and not bool(u.isnan().any()) and bool(y.isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("save", [P.SAVE_FULL, P.SAVE_8BIT])
+@pytest.mark.parametrize("kind", range(4))
+def test_what_overflowed_in_the_gate_stays_visible_backward(dtype, save, kind):
+    """One infinity: its whole group of a checkpoint reads back as NaN.  The gradients of its token and of its columns are
+    NaN, all others are as without it."""
+    K, M, D, F = 1, 40, 64, 96
+    x, wg, wu, wd, dy = _ffn_inputs(K, M, D, F, DT[dtype], seed=2)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    g, u = ((torch.randn(K, M, F, generator=gen, device="cuda") * 1.5).to(DT[dtype]) for _ in range(2))
+    cols = torch.zeros(F, dtype=torch.bool, device="cuda")
+    if save == P.SAVE_8BIT:
+        cols[32:64] = True
+        g[0, 7, 40] = float("inf")
+        saved = (P.act8_pack(g), P.act8_pack(u))
+        g, u = (P.act8_unpack(a, dtype=torch.float32) for a in saved)
+    else:
+        cols[40] = True
+        g[0, 7, 40] = float("nan")
+        saved = (g, u)
+    dx, dwg, dwu, dwd = P.ffn_backward(dy, x, wg, wu, wd, saved, activation=kind)
+    assert bool(dx[0, 7].isnan().all())
+    for t in (dwg[0, cols], dwu[0, cols], dwd[0][:, cols]):
+        assert bool(t.isnan().all())
+    want = ffn_backward64(dy, x, wg, wu, wd, g, u, kind, dtype == "bf16")
+    rows = torch.arange(M, device="cuda") != 7
+    keep = {"dx": (dx, lambda t: t[:, rows]), "dw_gate": (dwg, lambda t: t[:, ~cols]), "dw_up": (dwu, lambda t: t[:, ~cols]),
+            "dw_down": (dwd, lambda t: t[:, :, ~cols])}
+    for name, (t, cut) in keep.items():
+        v, e = want[name]
+        assert not bool(cut(t).isnan().any())
+        within(cut(t), cut(v), cut(e), name)
