@@ -123,7 +123,7 @@ int palsgd_block_status(void* stream);
  * float [table_rows, rotary_dim/2], contiguous; positions int32, one row per worker at pos_worker_stride (0: one row for
  * all).  w: rows of head_dim in the storage type, one per worker (row_stride unused).  A token whose position is
  * outside 0..table_rows-1 gets NaN outputs (and NaN gradients, dw included).
- * dw are overwritten; with tokens = 0 they are zero.  Workspace (backward only): as for the feed-forward block.
+ * dw are overwritten; with tokens = 0, or no heads, they are zero.  Workspace (backward only): as for the feed-forward block.
  * Errors: EINVAL (NULL, K, odd rotary_dim or rotary_dim > head_dim, head_dim = 0, eps negative or not finite,
  * overlapping outputs, small workspace); EUNSUPPORTED (head_dim > 512); EALIGN; ECUDA.
  */

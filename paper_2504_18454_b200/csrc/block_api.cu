@@ -844,9 +844,9 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
         BLOCK_TRY(check_heads(grad[i], s, heads[i], false));
         BLOCK_TRY(check_heads(in[i], s, heads[i], false));
         BLOCK_TRY(check_heads(out[i], s, heads[i], true));
-        if (!heads[i]) continue;
-        BLOCK_TRY(check_mat(w[i], s->K, 1, s->head_dim, elem(s->precision), false));
+        if (!heads[i] && (!dw[i] || !dw[i]->data)) { dw[i] = nullptr; continue; }
         BLOCK_TRY(check_mat(dw[i], s->K, 1, s->head_dim, elem(s->precision), true));
+        if (heads[i]) BLOCK_TRY(check_mat(w[i], s->K, 1, s->head_dim, elem(s->precision), false));
     }
     BLOCK_TRY(check_workspace(workspace, workspace_bytes));
     QkPlan p = plan_qk(s, cos_table, sin_table, positions, true);
@@ -856,23 +856,25 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
         if (heads[i]) part[i] = static_cast<float*>(ws.take((size_t)s->K * p.a.ctas[i] * s->head_dim * sizeof(float)));
     if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
     if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
-    if ((heads[0] | heads[1]) == 0) return PALSGD_OK;
     QkSumArgs sum{};
     for (int i = 0; i < 2; ++i) {
-        if (!heads[i]) continue;
+        if (dw[i]) { sum.dw[i] = dw[i]->data; sum.dww[i] = dw[i]->worker_stride; }
+        if (!heads[i]) continue;                         // no parts: a gradient that is given becomes zero
         HeadsArg& h = p.a.side[i];
         h.x = in[i]->data; h.xw = in[i]->worker_stride; h.xt = in[i]->token_stride; h.xh = in[i]->head_stride;
         h.d = grad[i]->data; h.dw = grad[i]->worker_stride; h.dt = grad[i]->token_stride; h.dh = grad[i]->head_stride;
         h.out = out[i]->data; h.ow = out[i]->worker_stride; h.ot = out[i]->token_stride; h.oh = out[i]->head_stride;
         h.w = w[i]->data; h.ww = w[i]->worker_stride;
         h.part = part[i];
-        sum.part[i] = part[i]; sum.dw[i] = dw[i]->data; sum.dww[i] = dw[i]->worker_stride; sum.heads[i] = heads[i];
+        sum.part[i] = part[i];
+        sum.parts[i] = s->tokens ? p.a.ctas[i] : 0;
     }
-    finish_qk(p, s, true);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    for (int i = 0; i < 2; ++i) sum.parts[i] = s->tokens ? p.a.ctas[i] : 0;
     sum.head_dim = s->head_dim;
     const dim3 grid((unsigned)ceil_div(s->head_dim, 32), 2, s->K);
-    if (s->tokens) BLOCK_TRY(run_qk<true>(p, s, st));
+    if (s->tokens && (heads[0] | heads[1])) {
+        finish_qk(p, s, true);
+        BLOCK_TRY(run_qk<true>(p, s, st));
+    }
     return launch("q/k weight gradient", s->precision == PALSGD_PREC_FP32 ? qk_sum_kernel<float> : qk_sum_kernel<bf16>, grid, 256, 0, st, sum);
 }

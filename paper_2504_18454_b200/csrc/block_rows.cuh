@@ -616,10 +616,9 @@ __global__ void __launch_bounds__(kQkThreads, NS == 1 ? qk_ctas_per_sm(BACK) : 1
 
 struct QkSumArgs {
     const float* part[2];
-    void*    dw[2];
+    void*    dw[2];               // may be NULL where the side has no heads
     int64_t  dww[2];
     uint32_t parts[2], head_dim;
-    uint32_t heads[2];
 };
 
 // The CTAs' partial sums of the weight gradients, joined in a fixed order: eight interleaved runs, then those.
@@ -630,7 +629,7 @@ __global__ void __launch_bounds__(256) qk_sum_kernel(const __grid_constant__ QkS
     let_next_start();
     wait_for_previous();
     const uint32_t side = blockIdx.y, k = blockIdx.z;
-    if (a.heads[side] == 0) return;
+    if (!a.dw[side]) return;
     const uint32_t i = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
     const uint32_t parts = a.parts[side];
     const float* p = a.part[side] + (uint64_t)k * parts * a.head_dim;

@@ -59,3 +59,39 @@ def test_what_overflowed_in_the_gate_stays_visible_backward(dtype, save, kind):
         v, e = want[name]
         assert not bool(cut(t).isnan().any())
         within(cut(t), cut(v), cut(e), name)
+
+
+# ---------------------------------------------------------------------------------------------- q/k: nothing to sum
+
+def _qk_inputs(K, M, HQ, HK, DH, R, dt, seed=1, rows=50):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s, m=0.0, std=1.0: (m + torch.randn(*s, generator=gen, device="cuda") * std).to(dt)
+    q, k = r(K, M, HQ, DH), r(K, M, HK, DH, std=3.0)
+    ang = torch.rand(rows, R // 2, generator=gen, device="cuda", dtype=torch.float64) * 6.3
+    pos = torch.randint(0, rows, (K, M), generator=gen, device="cuda", dtype=torch.int32)
+    return q, k, r(K, DH, m=1.0, std=0.2), r(K, DH, m=1.0, std=0.2), ang.cos().float(), ang.sin().float(), pos, r(K, M, HQ, DH, std=0.1), r(K, M, HK, DH, std=0.1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads", [(3, 0), (0, 2), (0, 0)], ids=str)
+@pytest.mark.parametrize("tokens", [0, 9])
+@pytest.mark.parametrize("DH", [40, 33])
+def test_the_weight_gradient_of_no_heads_is_zero(dtype, heads, tokens, DH):
+    K = 2
+    q, k, wq, wk, cos, sin, pos, dq, dk = _qk_inputs(K, tokens, *heads, DH, 8, DT[dtype])
+    dw = tuple(torch.full((K, DH + 8), 7.0, device="cuda", dtype=DT[dtype]) for _ in range(2))
+    inner = tuple(t[:, 3:3 + DH] for t in dw)
+    P.qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, out=(None, None, *inner))
+    for t, i, n in zip(dw, inner, heads):
+        assert bool((i == 0).all()) if n == 0 or tokens == 0 else not bool((i == 7).any())
+        assert bool((t[:, :3] == 7).all()) and bool((t[:, 3 + DH:] == 7).all())
+
+
+def test_autograd_gives_zero_for_the_weights_of_no_heads():
+    from paper_2504_18454_b200 import autograd as A
+    q, k, wq, wk, cos, sin, pos, dq, dk = _qk_inputs(2, 9, 3, 0, 40, 8, torch.float32)
+    junk = [torch.full((2, 40), float("nan"), device="cuda") for _ in range(64)]      # what a fresh tensor may lie over
+    del junk
+    wq.requires_grad_(), wk.requires_grad_()
+    A.qk_norm_rope(q, k, wq, wk, cos, sin, pos)[0].backward(dq)
+    assert bool((wk.grad == 0).all()) and bool((wq.grad != 0).any())
