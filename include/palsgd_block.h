@@ -80,7 +80,8 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
  *
  * Workspace: call with workspace = NULL to learn *workspace_bytes (nothing is enqueued; all other arguments as in the
  * call to come); then pass at least that many bytes, 256-byte aligned.  Contents need no preparation.  A workspace that
- * is too small is refused with EINVAL, and *workspace_bytes says what is needed.
+ * is too small is refused with EINVAL, and *workspace_bytes says what is needed: never 0, with tokens = 0 neither, so
+ * that a call to do the work cannot look like one that asks.
  * Errors: EINVAL (NULL, K = 0 or > 64, d_model or d_ff = 0, a size >= 2^31, bad enum, negative or overlapping strides,
  * small workspace); EALIGN; ECUDA.
  */

@@ -182,6 +182,8 @@ struct Arena {
         used += (bytes + 255) / 256 * 256;
         return p;
     }
+    // Never 0: a caller's buffer of no bytes may be NULL, and NULL asks for the size.
+    size_t need() const { return used ? used : 256; }
 };
 
 int check_workspace(const void* ws, const size_t* bytes)
@@ -690,8 +692,8 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
     }
     Product down{M, D, F, &oh, nullptr, &od, nullptr, false, false, y, 1, nullptr};
     if (M) take_shares(ws, &down, 1, s->K, parts);
-    if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
-    if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
+    if (!workspace) { *workspace_bytes = ws.need(); return PALSGD_OK; }
+    if (*workspace_bytes < ws.need()) { *workspace_bytes = ws.need(); return PALSGD_EINVAL; }
     if (M == 0) return PALSGD_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Device dev{};
@@ -756,8 +758,8 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     const int n_products = dx ? 4 : 3;
     for (int i = 0; i < n_products; ++i) products[i] = all[dx ? i : i + 1];
     if (M) take_shares(ws, products, n_products, s->K, parts);
-    if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
-    if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
+    if (!workspace) { *workspace_bytes = ws.need(); return PALSGD_OK; }
+    if (*workspace_bytes < ws.need()) { *workspace_bytes = ws.need(); return PALSGD_EINVAL; }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M == 0) {
         const palsgd_mat* w[3] = {dw_gate, dw_up, dw_down};
@@ -854,8 +856,8 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
     float* part[2] = {nullptr, nullptr};
     for (int i = 0; i < 2; ++i)
         if (heads[i]) part[i] = static_cast<float*>(ws.take((size_t)s->K * p.a.ctas[i] * s->head_dim * sizeof(float)));
-    if (!workspace) { *workspace_bytes = ws.used; return PALSGD_OK; }
-    if (*workspace_bytes < ws.used) { *workspace_bytes = ws.used; return PALSGD_EINVAL; }
+    if (!workspace) { *workspace_bytes = ws.need(); return PALSGD_OK; }
+    if (*workspace_bytes < ws.need()) { *workspace_bytes = ws.need(); return PALSGD_EINVAL; }
     QkSumArgs sum{};
     for (int i = 0; i < 2; ++i) {
         if (dw[i]) { sum.dw[i] = dw[i]->data; sum.dww[i] = dw[i]->worker_stride; }

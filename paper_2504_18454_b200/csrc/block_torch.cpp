@@ -158,8 +158,10 @@ void with_workspace(F&& call, PyObject* given, at::Device d, const char* where)
     if (given != Py_None) {
         ws = tensor(given, where, "workspace");
         if (ws.scalar_type() != at::kByte || ws.device() != d || !ws.is_contiguous()) refuse(where, "workspace must be a contiguous uint8 tensor on " + d.str());
+        // (an empty tensor's address is NULL, which would ask for the size once more and do nothing)
+        if ((size_t)ws.numel() < n) refuse(where, "workspace must have " + std::to_string(n) + " bytes, not " + std::to_string(ws.numel()));
     } else {
-        ws = fresh({(int64_t)(n ? n : 1)}, at::kByte, d);
+        ws = fresh({(int64_t)n}, at::kByte, d);
     }
     n = (size_t)ws.numel();
     int rc;

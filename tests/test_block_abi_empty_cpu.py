@@ -33,3 +33,26 @@ def test_a_weight_gradient_of_no_heads_is_checked_where_it_is_given(side):
     assert qk_backward(*heads, **{side: B.Mat(A * 9, 63, 0)})[0] == -1
     assert qk_backward(*heads, **{side: B.Mat(A * 9, -64, 0)})[0] == -1
     assert qk_backward(*heads, **{side: B.Mat(A * 9 + 1, 64, 0)})[0] == -2
+
+
+def ffn(back, tokens=0, ws=None, n=0):
+    D, F = 32, 64
+    s, m = B.FfnShape(2, 1, 0, 1, tokens, D, F), lambda i, r, c: B.Mat(A * i, r * c, c)
+    x, wg, wu, wd, y, g, u, dwg, dwu, dwd = (N(m(i + 1, *rc)) for i, rc in enumerate(
+        [(tokens, D), (F, D), (F, D), (D, F), (tokens, D), (tokens, F), (tokens, F), (F, D), (F, D), (D, F)]))
+    count = C.c_size_t(n)
+    if back:
+        rc = B.lib().palsgd_ffn_backward(N(s), y, x, None, wg, wu, wd, g, u, None, None, None, dwg, dwu, dwd, ws, N(count), None)
+    else:
+        rc = B.lib().palsgd_ffn_forward(N(s), x, wg, wu, wd, y, g, u, None, None, ws, N(count), None)
+    return rc, count.value
+
+
+@pytest.mark.parametrize("call", [lambda **k: ffn(False, **k), lambda **k: ffn(True, **k), lambda **k: qk_backward(0, 0, **k),
+                                  lambda **k: qk_backward(2, 1, tokens=0, **k)], ids=["forward", "backward", "no heads", "no tokens"])
+def test_a_call_with_nothing_to_do_still_asks_for_a_workspace(call):
+    """A caller who is told 0 bytes passes NULL for them, which would be taken for the question again: the weight gradients
+    of a backward call would stay as they were, with status OK."""
+    rc, need = call()
+    assert rc == 0 and need > 0
+    assert call(ws=A * 30, n=need - 1) == (-1, need)

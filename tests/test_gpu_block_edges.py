@@ -95,3 +95,35 @@ def test_autograd_gives_zero_for_the_weights_of_no_heads():
     wq.requires_grad_(), wk.requires_grad_()
     A.qk_norm_rope(q, k, wq, wk, cos, sin, pos)[0].backward(dq)
     assert bool((wk.grad == 0).all()) and bool((wq.grad != 0).any())
+
+
+# ---------------------------------------------------------------------------------------------- workspaces
+
+def test_an_empty_workspace_is_refused():
+    """Its address is NULL; a call that took that for the question how large it has to be would leave its outputs unwritten."""
+    x, wg, wu, wd, dy = _ffn_inputs(1, 40, 64, 96, torch.bfloat16)
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    _, saved = P.ffn_forward(x, wg, wu, wd)
+    q, k, wq, wk, cos, sin, pos, dq, dk = _qk_inputs(1, 9, 2, 1, 64, 64, torch.bfloat16)
+    for call in (lambda: P.ffn_forward(x, wg, wu, wd, workspace=none), lambda: P.ffn_backward(dy, x, wg, wu, wd, saved, workspace=none),
+                 lambda: P.qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, workspace=none)):
+        with pytest.raises(P.PalsgdError, match="workspace"):
+            call()
+
+
+def test_no_tokens_with_the_workspace_that_the_library_asks_for():
+    """The C calls as the header says: ask, allocate that much, call.  The weight gradients become zero."""
+    import ctypes as C
+    from paper_2504_18454_b200 import block as B
+    K, D, F = 2, 40, 24
+    dw = [torch.full((K, *s), 7.0, device="cuda", dtype=torch.bfloat16) for s in ((F, D), (F, D), (D, F))]
+    w = [torch.zeros_like(t) for t in dw]
+    mat = lambda t: C.byref(B.Mat(t.data_ptr(), t.stride(0), t.stride(1)))
+    empty = C.byref(B.Mat(None, 0, 0))
+    s, n = B.FfnShape(K, P.PREC_BF16_MASTER, 0, P.SAVE_FULL, 0, D, F), C.c_size_t(0)
+    call = lambda ws: B.lib().palsgd_ffn_backward(C.byref(s), empty, empty, None, *map(mat, w), empty, empty, None, None, None, *map(mat, dw),
+                                                  ws, C.byref(n), torch.cuda.current_stream().cuda_stream)
+    assert call(None) == 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    assert call(ws.data_ptr()) == 0
+    assert all(bool((t == 0).all()) for t in dw)
