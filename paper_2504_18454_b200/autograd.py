@@ -21,8 +21,8 @@ def _once(what: str) -> None:
 
 class _GatedFfn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_gate, w_up, w_down, activation, checkpoint8):
-        needs = any(ctx.needs_input_grad)
+    def forward(ctx, x, w_gate, w_up, w_down, activation, checkpoint8, recording):
+        needs = recording and any(ctx.needs_input_grad)  # (which stays true under no_grad)
         save = (block.SAVE_8BIT if checkpoint8 else block.SAVE_FULL) if needs else block.SAVE_NONE
         y, saved = block.ffn_forward(x, w_gate, w_up, w_down, activation=activation, save=save)
         if needs:
@@ -42,7 +42,7 @@ class _GatedFfn(torch.autograd.Function):
         dy = dy if dy.stride(-1) == 1 or dy.shape[-1] == 1 else dy.contiguous()
         dx, *dw = block.ffn_backward(dy, x, w_gate, w_up, w_down, (gate, up), activation=ctx.activation,
                                      need_dx=ctx.needs_input_grad[0])
-        return (dx, *dw, None, None)
+        return (dx, *dw, None, None, None)
 
 
 class _QkNormRope(torch.autograd.Function):
@@ -65,7 +65,7 @@ class _QkNormRope(torch.autograd.Function):
 def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
               activation: int = block.ACT_SILU, checkpoint8: bool = False) -> torch.Tensor:
     """`block.ffn_forward` with gradients for x and the three weights."""
-    return _GatedFfn.apply(x, w_gate, w_up, w_down, activation, checkpoint8)
+    return _GatedFfn.apply(x, w_gate, w_up, w_down, activation, checkpoint8, torch.is_grad_enabled())
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, w_q: torch.Tensor, w_k: torch.Tensor, cos: torch.Tensor,

@@ -70,3 +70,25 @@ def test_first_derivatives_do_not(plain):
     want = torch.autograd.grad(sum(t.square().sum() for t in _qk(*args, None, None, None, eps=0, interleaved=0)), args)
     for a, b in zip(got, want):
         assert torch.allclose(a, b, rtol=1e-12)
+
+
+@pytest.mark.parametrize("checkpoint8", [False, True])
+def test_nothing_is_kept_where_gradients_are_off(plain, monkeypatch, checkpoint8):
+    """Evaluation of a model whose parameters want gradients, under no_grad."""
+    saves = []
+
+    def forward(*a, save, **k):
+        saves.append(save)
+        return _ffn_forward(*a, save=save, **k)
+
+    def pack(x, **k):
+        raise AssertionError("a checkpoint that nothing will read")
+
+    monkeypatch.setattr(B, "ffn_forward", forward)
+    monkeypatch.setattr(B, "act8_pack", pack)
+    with torch.no_grad():
+        A.gated_ffn(*_ffn_args(), activation=B.ACT_RELU, checkpoint8=checkpoint8)
+    A.gated_ffn(*(t.detach() for t in _ffn_args()), activation=B.ACT_RELU, checkpoint8=checkpoint8)
+    assert saves == [B.SAVE_NONE, B.SAVE_NONE]
+    A.gated_ffn(*_ffn_args(), activation=B.ACT_RELU)
+    assert saves[2:] == [B.SAVE_FULL]
