@@ -338,6 +338,10 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
                                 if constexpr (BACK)
                                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + NS * 2 * 512), "l"(db + fd + at[s][p]) : "memory");
                             }
+                } else if constexpr (BACK) {                                 // not a head: zeros, which add nothing to the weight gradient
+#pragma unroll
+                    for (int i = 0; i < kVecs; ++i)                           // (an infinity of the item before it would: times 0 it is NaN)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(mine + (slot * kVecs + i) * 512), "r"(0) : "memory");
                 }
                 --left;
                 fh += abreast;
@@ -505,7 +509,7 @@ __device__ __forceinline__ void qk_walk(const QkArgs& a, const uint32_t cta, uns
 #pragma unroll
             for (int j = 0; j < V; ++j) sq = f2_fma(x[s][j], x[s][j], sq);
         }
-        // (a head that is not there: 0, so that what its place in the ring still holds adds nothing to the weight gradient)
+        // (a head that is not there reads zeros backward, and 0 for r: eps may be 0 and its position outside the table)
         const float mean = fmaf(over_head(sq), inv_n, a.eps), r = live ? rsqrtf(mean) + bad : 0.0f;
         const f2 rr = f2_of(r, r);
         f2 y[NS][V];

@@ -97,6 +97,26 @@ def test_autograd_gives_zero_for_the_weights_of_no_heads():
     assert bool((wk.grad == 0).all()) and bool((wq.grad != 0).any())
 
 
+# ---------------------------------------------------------------------------------------------- q/k: an infinite gradient
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size", [(1, 33, 64, 64), (1, 41, 64, 20), (1, 65, 32, 32), (1, 33, 33, 20), (40003, 3, 64, 64)], ids=str)
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_an_infinite_gradient_gives_an_infinite_weight_gradient(dtype, size, interleaved):
+    """Not NaN: heads (or tokens) that a warp's last group lacks, and whose place held an infinity before, add nothing.  The
+    gradient of one value is infinite in every head; it and its partner of the rotation have x > 0, so no infinities of
+    both signs meet."""
+    M, HQ, DH, R = size
+    q, k, wq, wk, cos, sin, pos, dq, dk = _qk_inputs(1, M, HQ, 1, DH, R, DT[dtype], seed=4)
+    cos.fill_(0.6), sin.fill_(0.8)
+    a, b = (2, 3) if interleaved else (2, 2 + R // 2)
+    dq[..., a], q[..., a], q[..., b] = float("inf"), 1.0, 1.0
+    _, _, dw, _ = P.qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, interleaved=interleaved)
+    assert float(dw[0, a]) == float("inf") and float(dw[0, b]) == float("-inf")
+    rest = [i for i in range(DH) if i not in (a, b)]
+    assert bool(dw[0, rest].isfinite().all())
+
+
 # ---------------------------------------------------------------------------------------------- workspaces
 
 def test_an_empty_workspace_is_refused():
