@@ -192,7 +192,10 @@ __device__ __forceinline__ float act(float g, float& slope)
         const float c = 1.5957691216057308f;                     // 2 sqrt(2/pi)
         const float z2 = c * g * fmaf(0.044715f * g, g, 1.0f);
         const float s = FAST ? __fdividef(1.0f, 1.0f + __expf(-z2)) : 1.0f / (1.0f + expf(-z2));
-        if constexpr (SLOPE) slope = fmaf(g * s * (1.0f - s), c * fmaf(0.134145f * g, g, 1.0f), s);
+        if constexpr (SLOPE) {                                   // (its square has to stay finite: 0 times an infinity is NaN)
+            const float m = fminf(fabsf(g), 1e9f);
+            slope = fmaf(g * s * (1.0f - s), c * fmaf(0.134145f * m, m, 1.0f), s);
+        }
         return g * s;
     } else {
         // (a NaN stays: what overflowed in a checkpoint has to reach the gradients)
@@ -228,8 +231,12 @@ __device__ __forceinline__ f2 act2(f2 g, f2& slope)
         const f2 gg = f2_mul(g, g);
         const f2 s = f2_logistic(f2_mul(f2_mul(g, f2_same(-1.4426950408889634f * c)), f2_fma(gg, f2_same(0.044715f), f2_same(1.0f))));
         const f2 a = f2_mul(g, s);
-        if constexpr (SLOPE)
-            slope = f2_fma(f2_mul(a, f2_fma(s, f2_same(-1.0f), f2_same(1.0f))), f2_fma(gg, f2_same(0.134145f * c), f2_same(c)), s);
+        if constexpr (SLOPE) {
+            float x, y;
+            f2_get(gg, x, y);
+            const f2 m = f2_of(fminf(x, 1e18f), fminf(y, 1e18f));
+            slope = f2_fma(f2_mul(a, f2_fma(s, f2_same(-1.0f), f2_same(1.0f))), f2_fma(m, f2_same(0.134145f * c), f2_same(c)), s);
+        }
         return a;
     } else {
         float x, y, sx = 0.0f, sy = 0.0f;

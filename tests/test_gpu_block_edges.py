@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2504_18454_b200 as P
-from _block_ref import ffn_backward64, ffn_forward64, within
+from _block_ref import act64, ffn_backward64, ffn_forward64, within
 
 pytestmark = pytest.mark.gpu
 DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
@@ -59,6 +59,23 @@ def test_what_overflowed_in_the_gate_stays_visible_backward(dtype, save, kind):
         v, e = want[name]
         assert not bool(cut(t).isnan().any())
         within(cut(t), cut(v), cut(e), name)
+
+
+# ---------------------------------------------------------------------------------------------- very large gates
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("save", [P.SAVE_FULL, P.SAVE_8BIT])
+@pytest.mark.parametrize("kind", range(4))
+def test_the_slope_of_very_large_gates(dtype, save, kind):
+    """act' is within 4e-8 of 1 or 0 there, up to the largest number (2^-20: 8 roundings of a number about 1).  With one value,
+    u = dy = w_down = w_gate = 1 and w_up = 0, dx is act'(g)."""
+    g = torch.tensor([s * v for v in (20.0, 1e3, 1e9, 1e10, 1e18, 2e19, 1e25, 3e38) for s in (1, -1)], device="cuda").to(DT[dtype])[None, :, None]
+    one = torch.ones(1, 1, 1, device="cuda", dtype=DT[dtype])
+    saved = (g, torch.ones_like(g))
+    if save == P.SAVE_8BIT:
+        saved = tuple(map(P.act8_pack, saved))
+    dx, *_ = P.ffn_backward(torch.ones_like(g), torch.ones_like(g), one, torch.zeros_like(one), one, saved, activation=kind)
+    within(dx, act64(kind, g)[1], 2.0 ** -20, "act'")
 
 
 # ---------------------------------------------------------------------------------------------- q/k: nothing to sum
