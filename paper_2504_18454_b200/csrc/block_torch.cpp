@@ -122,6 +122,14 @@ struct On {
 
 at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, at::Device d) { return at::empty(shape, at::TensorOptions().dtype(type).device(d)); }
 
+// The library wrote to these tensors: autograd is to see that, as of an in-place operation, where it has saved one of them.
+template <typename... T>
+void written(const T&... t)
+{
+    auto note = [](const at::Tensor& x) { if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version(); };
+    (note(t), ...);
+}
+
 int64_t integer(PyObject* o)
 {
     const int64_t v = PyLong_AsLongLong(o);
@@ -194,6 +202,7 @@ PyObject* act8_pack(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         auto m = [&](const at::Tensor& t) { return one ? palsgd_mat{t.data_ptr(), 0, t.stride(0)} : mat(t); };
         const palsgd_mat mx = m(x), mq = m(q), me = m(e);
         check(g_lib.act8_pack(prec, one ? 1u : (uint32_t)std::min<int64_t>(x.size(0), 65), x.size(-2), x.size(-1), &mx, &mq, &me, on.raw), where);
+        written(q, e);
         return pack(std::optional<at::Tensor>(q), std::optional<at::Tensor>(e));
     });
 }
@@ -219,6 +228,7 @@ PyObject* act8_unpack(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         auto m = [&](const at::Tensor& t) { return one ? palsgd_mat{t.data_ptr(), 0, t.stride(0)} : mat(t); };
         const palsgd_mat mx = m(x), mq = m(q), me = m(e);
         check(g_lib.act8_unpack(prec, one ? 1u : (uint32_t)std::min<int64_t>(q.size(0), 65), q.size(-2), q.size(-1), &mq, &me, &mx, on.raw), where);
+        written(x);
         return wrap(x);
     });
 }
@@ -287,6 +297,8 @@ PyObject* ffn_forward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         with_workspace([&](void* ws, size_t* n) {
             return g_lib.ffn_forward(&f.shape, &mx, &f.w_gate, &f.w_up, &f.w_down, &my, s.at(0), s.at(1), s.at(2), s.at(3), ws, n, on.raw);
         }, a[11], f.d, where);
+        written(y);
+        for (const auto& t : s.t) if (t) written(*t);
         return pack(std::optional<at::Tensor>(y), s.t[0], s.t[1], s.t[2], s.t[3]);
     });
 }
@@ -318,6 +330,7 @@ PyObject* ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
             return g_lib.ffn_backward(&f.shape, &mdy, &mx, xe ? &me : nullptr, &f.w_gate, &f.w_up, &f.w_down, s.at(0), s.at(1), s.at(2), s.at(3),
                                       out[0] ? &m[0] : nullptr, &m[1], &m[2], &m[3], ws, n, on.raw);
         }, a[17], f.d, where);
+        for (const auto& t : out) if (t) written(*t);
         return pack(out[0], out[1], out[2], out[3]);
     });
 }
@@ -374,6 +387,7 @@ PyObject* qk_forward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         fit(ok, where, "k_out", t.k.sizes(), t.type, t.d);
         const palsgd_heads hoq = heads(oq), hok = heads(ok);
         check(g_lib.qk_forward(&t.shape, &t.hq, &t.hk, &t.mq, &t.mk, t.c, t.s, t.p, &hoq, &hok, on.raw), where);
+        written(oq, ok);
         return pack(std::optional<at::Tensor>(oq), std::optional<at::Tensor>(ok));
     });
 }
@@ -400,6 +414,7 @@ PyObject* qk_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         with_workspace([&](void* ws, size_t* n) {
             return g_lib.qk_backward(&t.shape, &hgq, &hgk, &t.hq, &t.hk, &t.mq, &t.mk, t.c, t.s, t.p, &hdq, &hdk, &mdq, &mdk, ws, n, on.raw);
         }, a[15], t.d, where);
+        for (const auto& t : out) if (t) written(*t);
         return pack(out[0], out[1], out[2], out[3]);
     });
 }

@@ -164,3 +164,36 @@ def test_no_tokens_with_the_workspace_that_the_library_asks_for():
     ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
     assert call(ws.data_ptr()) == 0
     assert all(bool((t == 0).all()) for t in dw)
+
+
+# ---------------------------------------------------------------------------------------------- outputs that autograd has saved
+
+def test_writing_to_given_memory_raises_its_version():
+    x, wg, wu, wd, dy = _ffn_inputs(1, 40, 64, 96, torch.bfloat16)
+    q, k, wq, wk, cos, sin, pos, dq, dk = _qk_inputs(1, 9, 2, 1, 64, 64, torch.bfloat16)
+    _, saved = P.ffn_forward(x, wg, wu, wd)
+    px, (_, saved8) = P.act8_pack(x), P.ffn_forward(x, wg, wu, wd, save=P.SAVE_8BIT)
+    new = torch.empty_like
+    calls = [(lambda o: P.ffn_forward(x, wg, wu, wd, out=o[0], saved=tuple(o[1:])), [x, *saved]),
+             (lambda o: P.ffn_forward(x, wg, wu, wd, out=o[0], saved=(P.Act8(o[1], o[2], x.dtype), P.Act8(o[3], o[4], x.dtype)), save=P.SAVE_8BIT),
+              [x, saved8[0].q, saved8[0].exponent, saved8[1].q, saved8[1].exponent]),
+             (lambda o: P.ffn_backward(dy, x, wg, wu, wd, saved, out=tuple(o)), [x, wg, wu, wd]),
+             (lambda o: P.act8_pack(x, out=P.Act8(o[0], o[1], x.dtype)), [px.q, px.exponent]), (lambda o: P.act8_unpack(px, out=o[0]), [x]),
+             (lambda o: P.qk_norm_rope(q, k, wq, wk, cos, sin, pos, out=tuple(o)), [q, k]),
+             (lambda o: P.qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, out=tuple(o)), [q, k, wq, wk])]
+    for call, like in calls:
+        outs = [new(t) for t in like]
+        before = [t._version for t in outs]
+        call(outs)
+        assert all(t._version > v for t, v in zip(outs, before))
+        with torch.inference_mode():
+            call([new(t) for t in like])
+
+
+def test_autograd_sees_that_a_saved_tensor_was_written_to():
+    x, wg, wu, wd, _ = _ffn_inputs(1, 40, 64, 96, torch.bfloat16)
+    h = x.requires_grad_() * 2
+    z = h * h                                            # saves h
+    P.ffn_forward(x.detach(), wg, wu, wd, save=P.SAVE_NONE, out=h.detach())
+    with pytest.raises(RuntimeError, match="inplace"):
+        z.sum().backward()
