@@ -13,7 +13,10 @@
  *   - Every entry point returns a palsgd_status, never throws, never exits.  Arguments are checked before anything is
  *     enqueued.  `stream` is a cudaStream_t as void*.  Work is asynchronous; entry points keep no state between calls,
  *     so calls on distinct streams and host threads are independent as long as their outputs and workspaces are.
- *   - All buffers are DEVICE memory of the caller.  Nothing is allocated.  Inputs and outputs must not overlap.
+ *   - All buffers are DEVICE memory of the caller.  Nothing is allocated.  Outputs and the workspace must not overlap each
+ *     other or an input: EINVAL, told exactly from addresses, sizes and strides (interleaved layouts are no overlap), but
+ *     for layouts of unlike strides so entangled that the search would take long.  The one exception: a head matrix that
+ *     palsgd_qk_norm_rope_* writes may be exactly one that it reads (q_out = q; dq = dq_out or q): work in place.
  *   - `precision` fixes the storage type of activations, weights and gradients: PALSGD_PREC_FP32 = float,
  *     PALSGD_PREC_BF16_MASTER = bfloat16.  Sums, norms and activations are taken in binary32; each result is rounded
  *     once to the storage type.  What is rounded in between is stated at each call.
@@ -83,7 +86,7 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
  * is too small is refused with EINVAL, and *workspace_bytes says what is needed: never 0, with tokens = 0 neither, so
  * that a call to do the work cannot look like one that asks.
  * Errors: EINVAL (NULL, K = 0 or > 64, d_model or d_ff = 0, a size >= 2^31, bad enum, negative or overlapping strides,
- * small workspace); EALIGN; ECUDA.
+ * overlapping buffers, small workspace); EALIGN; ECUDA.
  */
 enum { PALSGD_ACT_SILU = 0, PALSGD_ACT_GELU = 1, PALSGD_ACT_GELU_TANH = 2, PALSGD_ACT_RELU = 3 };
 enum { PALSGD_SAVE_NONE = 0, PALSGD_SAVE_FULL = 1, PALSGD_SAVE_8BIT = 2 };
@@ -126,7 +129,7 @@ int palsgd_block_status(void* stream);
  * outside 0..table_rows-1 gets NaN outputs (and NaN gradients, dw included).
  * dw are overwritten; with tokens = 0, or no heads, they are zero.  Workspace (backward only): as for the feed-forward block.
  * Errors: EINVAL (NULL, K, odd rotary_dim or rotary_dim > head_dim, head_dim = 0, eps negative or not finite,
- * overlapping outputs, small workspace); EUNSUPPORTED (head_dim > 512); EALIGN; ECUDA.
+ * overlapping buffers, small workspace); EUNSUPPORTED (head_dim > 512); EALIGN; ECUDA.
  */
 typedef struct palsgd_heads {
     void*   data;

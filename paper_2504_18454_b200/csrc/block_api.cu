@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "block_host.h"
+#include "block_overlap.h"
 
 using namespace palsgd::block;
 
@@ -81,6 +82,12 @@ int check_mat(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, siz
     return PALSGD_OK;
 }
 
+Region region(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, size_t es)
+{
+    if (!m) return Region();
+    return Region(m->data, cols * es).axis(0, K, m->worker_stride * (int64_t)es).axis(1, rows, m->row_stride * (int64_t)es);
+}
+
 #define BLOCK_TRY(call) do { const int rc_ = (call); if (rc_ != PALSGD_OK) return rc_; } while (0)
 
 // A launch that may start up while the stream's previous kernel still runs (the kernels wait for it: block_common.cuh).
@@ -122,7 +129,11 @@ int check_act8(int32_t prec, uint32_t K, uint64_t rows, uint64_t cols, const pal
     BLOCK_TRY(check_mat(x, K, rows, cols, elem(prec), !pack));
     BLOCK_TRY(check_mat(q, K, rows, cols, 1, pack));
     BLOCK_TRY(check_mat(e, K, rows, ceil_div(cols, PALSGD_ACT8_GROUP), 1, pack));
-    return PALSGD_OK;
+    const Region rx = region(x, K, rows, cols, elem(prec)), rq = region(q, K, rows, cols, 1), re = region(e, K, rows, ceil_div(cols, PALSGD_ACT8_GROUP), 1);
+    Regions all;
+    if (pack) { all.reads(rx); all.writes(rq); all.writes(re); }
+    else { all.reads(rq); all.reads(re); all.writes(rx); }
+    return all.clash() ? PALSGD_EINVAL : PALSGD_OK;
 }
 
 template <typename T, bool PACK>
@@ -172,6 +183,19 @@ int check_saved(const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_
     return PALSGD_OK;
 }
 
+void add_saved(Regions& all, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e,
+               const palsgd_mat* up_e, bool output)
+{
+    if (s->save == PALSGD_SAVE_NONE) return;
+    const bool eight = s->save == PALSGD_SAVE_8BIT;
+    const palsgd_mat* m[4] = {gate, up, eight ? gate_e : nullptr, eight ? up_e : nullptr};
+    for (int i = 0; i < 4; ++i) {
+        const Region r = region(m[i], s->K, s->tokens, i < 2 ? s->d_ff : ceil_div(s->d_ff, PALSGD_ACT8_GROUP), i >= 2 || eight ? 1 : elem(s->precision));
+        if (output) all.writes(r);
+        else all.reads(r);
+    }
+}
+
 // Hands out 256-byte aligned pieces of the workspace; with base = nullptr it only counts.
 struct Arena {
     char* base;
@@ -190,6 +214,16 @@ int check_workspace(const void* ws, const size_t* bytes)
 {
     if (!bytes) return PALSGD_EINVAL;
     if (ws && !aligned(ws, 256)) return PALSGD_EALIGN;
+    return PALSGD_OK;
+}
+
+// The workspace's size is asked for or checked, and that nothing that the call writes overlaps.
+int settle(const Arena& ws, size_t* bytes, Regions& all)
+{
+    if (ws.base && *bytes < ws.need()) { *bytes = ws.need(); return PALSGD_EINVAL; }
+    all.writes(Region(ws.base, ws.used));
+    if (all.clash()) return PALSGD_EINVAL;
+    if (!ws.base) *bytes = ws.need();
     return PALSGD_OK;
 }
 
@@ -539,6 +573,22 @@ int check_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, c
     return PALSGD_OK;
 }
 
+Region region(const palsgd_heads* h, const palsgd_qk_shape* s, uint32_t heads)
+{
+    const int64_t es = (int64_t)elem(s->precision);
+    if (!h || heads == 0) return Region();
+    return Region(h->data, s->head_dim * (uint64_t)es).axis(0, s->K, h->worker_stride * es).axis(1, s->tokens, h->token_stride * es).axis(2, heads, h->head_stride * es);
+}
+
+// The tables and positions of a call
+void add_angles(Regions& all, const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, const int32_t* pos)
+{
+    if (s->rotary_dim == 0 || s->tokens == 0) return;
+    all.reads(Region(cos_t, s->table_rows * (s->rotary_dim / 2) * 4));
+    all.reads(Region(sin_t, s->table_rows * (s->rotary_dim / 2) * 4));
+    all.reads(Region(pos, s->tokens * 4).axis(0, s->K, s->pos_worker_stride * 4));
+}
+
 bool heads_wide(const void* p, int64_t w, int64_t t, int64_t h, size_t es)
 {
     return aligned(p, 16) && (w * es) % 16 == 0 && (t * es) % 16 == 0 && (h * es) % 16 == 0;
@@ -692,8 +742,13 @@ extern "C" int palsgd_ffn_forward(const palsgd_ffn_shape* s, const palsgd_mat* x
     }
     Product down{M, D, F, &oh, nullptr, &od, nullptr, false, false, y, 1, nullptr};
     if (M) take_shares(ws, &down, 1, s->K, parts);
-    if (!workspace) { *workspace_bytes = ws.need(); return PALSGD_OK; }
-    if (*workspace_bytes < ws.need()) { *workspace_bytes = ws.need(); return PALSGD_EINVAL; }
+    Regions all;
+    all.reads(region(x, s->K, M, D, es));
+    all.reads(region(w_gate, s->K, F, D, es)); all.reads(region(w_up, s->K, F, D, es)); all.reads(region(w_down, s->K, D, F, es));
+    all.writes(region(y, s->K, M, D, es));
+    add_saved(all, s, gate, up, gate_e, up_e, true);
+    BLOCK_TRY(settle(ws, workspace_bytes, all));
+    if (!workspace) return PALSGD_OK;
     if (M == 0) return PALSGD_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Device dev{};
@@ -758,8 +813,16 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     const int n_products = dx ? 4 : 3;
     for (int i = 0; i < n_products; ++i) products[i] = all[dx ? i : i + 1];
     if (M) take_shares(ws, products, n_products, s->K, parts);
-    if (!workspace) { *workspace_bytes = ws.need(); return PALSGD_OK; }
-    if (*workspace_bytes < ws.need()) { *workspace_bytes = ws.need(); return PALSGD_EINVAL; }
+    Regions mem;
+    mem.reads(region(dy, s->K, M, D, es));
+    mem.reads(region(x, s->K, M, D, x_e ? 1 : es));
+    mem.reads(region(x_e, s->K, M, ceil_div(D, PALSGD_ACT8_GROUP), 1));
+    mem.reads(region(w_gate, s->K, F, D, es)); mem.reads(region(w_up, s->K, F, D, es)); mem.reads(region(w_down, s->K, D, F, es));
+    add_saved(mem, s, gate, up, gate_e, up_e, false);
+    mem.writes(region(dx, s->K, M, D, es));
+    mem.writes(region(dw_gate, s->K, F, D, es)); mem.writes(region(dw_up, s->K, F, D, es)); mem.writes(region(dw_down, s->K, D, F, es));
+    BLOCK_TRY(settle(ws, workspace_bytes, mem));
+    if (!workspace) return PALSGD_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M == 0) {
         const palsgd_mat* w[3] = {dw_gate, dw_up, dw_down};
@@ -815,6 +878,13 @@ extern "C" int palsgd_qk_norm_rope_forward(const palsgd_qk_shape* s, const palsg
         BLOCK_TRY(check_heads(out[i], s, heads[i], true));
         if (heads[i]) BLOCK_TRY(check_mat(w[i], s->K, 1, s->head_dim, elem(s->precision), false));
     }
+    Regions all;
+    add_angles(all, s, cos_table, sin_table, positions);
+    for (int i = 0; i < 2; ++i) {
+        if (heads[i]) all.reads(region(w[i], s->K, 1, s->head_dim, elem(s->precision)));
+        all.writes(region(out[i], s, heads[i]), all.reads(region(in[i], s, heads[i])));
+    }
+    if (all.clash()) return PALSGD_EINVAL;
     if (s->tokens == 0 || (heads[0] | heads[1]) == 0) return PALSGD_OK;
     QkPlan p = plan_qk(s, cos_table, sin_table, positions, false);
     for (int i = 0; i < 2; ++i) {
@@ -856,8 +926,16 @@ extern "C" int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const pals
     float* part[2] = {nullptr, nullptr};
     for (int i = 0; i < 2; ++i)
         if (heads[i]) part[i] = static_cast<float*>(ws.take((size_t)s->K * p.a.ctas[i] * s->head_dim * sizeof(float)));
-    if (!workspace) { *workspace_bytes = ws.need(); return PALSGD_OK; }
-    if (*workspace_bytes < ws.need()) { *workspace_bytes = ws.need(); return PALSGD_EINVAL; }
+    Regions all;
+    add_angles(all, s, cos_table, sin_table, positions);
+    for (int i = 0; i < 2; ++i) {
+        if (heads[i]) all.reads(region(w[i], s->K, 1, s->head_dim, elem(s->precision)));
+        const int x = all.reads(region(in[i], s, heads[i])), d = all.reads(region(grad[i], s, heads[i]));
+        all.writes(region(out[i], s, heads[i]), x, d);
+        all.writes(region(dw[i], s->K, 1, s->head_dim, elem(s->precision)));
+    }
+    BLOCK_TRY(settle(ws, workspace_bytes, all));
+    if (!workspace) return PALSGD_OK;
     QkSumArgs sum{};
     for (int i = 0; i < 2; ++i) {
         if (dw[i]) { sum.dw[i] = dw[i]->data; sum.dww[i] = dw[i]->worker_stride; }

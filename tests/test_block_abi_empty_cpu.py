@@ -29,10 +29,10 @@ def test_a_weight_gradient_of_no_heads_is_checked_where_it_is_given(side):
     heads = (0, 2) if side == "dwq" else (2, 0)
     assert qk_backward(*heads)[0] == 0
     assert qk_backward(*heads, **{side: B.Mat(None, 64, 0)})[0] == 0
-    assert qk_backward(*heads, **{side: B.Mat(A * 9, 64, 0)})[0] == 0
-    assert qk_backward(*heads, **{side: B.Mat(A * 9, 63, 0)})[0] == -1
-    assert qk_backward(*heads, **{side: B.Mat(A * 9, -64, 0)})[0] == -1
-    assert qk_backward(*heads, **{side: B.Mat(A * 9 + 1, 64, 0)})[0] == -2
+    assert qk_backward(*heads, **{side: B.Mat(A * 11, 64, 0)})[0] == 0
+    assert qk_backward(*heads, **{side: B.Mat(A * 11, 63, 0)})[0] == -1
+    assert qk_backward(*heads, **{side: B.Mat(A * 11, -64, 0)})[0] == -1
+    assert qk_backward(*heads, **{side: B.Mat(A * 11 + 1, 64, 0)})[0] == -2
 
 
 def ffn(back, tokens=0, ws=None, n=0):

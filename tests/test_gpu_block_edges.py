@@ -197,3 +197,39 @@ def test_autograd_sees_that_a_saved_tensor_was_written_to():
     P.ffn_forward(x.detach(), wg, wu, wd, save=P.SAVE_NONE, out=h.detach())
     with pytest.raises(RuntimeError, match="inplace"):
         z.sum().backward()
+
+
+# ---------------------------------------------------------------------------------------------- overlap
+
+def test_overlapping_outputs_are_refused():
+    """dx written in the launch that reads dy would race; so would any other output over an input."""
+    x, wg, wu, wd, dy = _ffn_inputs(1, 40, 64, 96, torch.bfloat16)
+    _, saved = P.ffn_forward(x, wg, wu, wd)
+    q, k, wq, wk, cos, sin, pos, dq, dk = _qk_inputs(1, 9, 2, 2, 64, 64, torch.bfloat16)
+    p = P.act8_pack(x)
+    for call in (lambda: P.ffn_backward(dy, x, wg, wu, wd, saved, out=(dy, None, None, None)),
+                 lambda: P.ffn_backward(dy, x, wg, wu, wd, saved, out=(None, wg, None, None)),
+                 lambda: P.ffn_forward(x, wg, wu, wd, out=x), lambda: P.ffn_forward(x, wg, wu, wd, saved=(saved[0], saved[0])),
+                 lambda: P.act8_unpack(P.Act8(x.view(torch.int8)[..., :64], p.exponent, x.dtype), out=x),
+                 lambda: P.act8_pack(x, out=P.Act8(x.view(torch.int8)[..., :64], p.exponent, x.dtype)),
+                 lambda: P.qk_norm_rope(q, k, wq, wk, cos, sin, pos, out=(k, None)), lambda: P.qk_norm_rope(q, k, wq, wk, cos, sin, pos, out=(k, q)),
+                 lambda: P.qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, out=(dk, None, None, None))):
+        with pytest.raises(P.PalsgdError):
+            call()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size", [(2, 3001, 6, 2, 64, 64), (1, 700, 3, 3, 64, 20), (1, 300, 3, 1, 33, 20)], ids=str)
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_heads_in_place(dtype, size, interleaved):
+    """A head is read before it is written: q_out = q, and dq = dq_out or q, give the same bits."""
+    q, k, wq, wk, cos, sin, pos, dq, dk = _qk_inputs(*size, DT[dtype], seed=8)
+    kw = dict(interleaved=interleaved)
+    want = P.qk_norm_rope(q, k, wq, wk, cos, sin, pos, **kw)
+    back = P.qk_norm_rope_backward(dq, dk, q, k, wq, wk, cos, sin, pos, **kw)
+    a, b = q.clone(), k.clone()
+    P.qk_norm_rope(a, b, wq, wk, cos, sin, pos, out=(a, b), **kw)
+    assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+    a, b = dq.clone(), k.clone()
+    got = P.qk_norm_rope_backward(a, dk, q, b, wq, wk, cos, sin, pos, out=(a, b, None, None), **kw)
+    assert all(torch.equal(s, t) for s, t in zip(got, back))
