@@ -33,21 +33,24 @@ from .binding import (  # noqa: F401
     TUNE_OUTER_VARIANT,
     TUNE_OUTER_DYNAMIC,
 )
-from .block import (  # noqa: F401
-    Act8,
-    act8_pack,
-    act8_unpack,
-    block_status,
-    ffn_backward,
-    ffn_forward,
-    qk_norm_rope,
-    qk_norm_rope_backward,
-    ACT8_GROUP,
-    ACT_GELU,
-    ACT_GELU_TANH,
-    ACT_RELU,
-    ACT_SILU,
-    SAVE_8BIT,
-    SAVE_FULL,
-    SAVE_NONE,
+
+# The block operators take torch tensors: `block`, and torch with it, is imported where one of its names is first used.
+_BLOCK = (
+    "Act8", "act8_pack", "act8_unpack", "block_status", "ffn_backward", "ffn_forward", "qk_norm_rope",
+    "qk_norm_rope_backward", "ACT8_GROUP", "ACT_GELU", "ACT_GELU_TANH", "ACT_RELU", "ACT_SILU", "SAVE_8BIT", "SAVE_FULL",
+    "SAVE_NONE",
 )
+__all__ = [n for n in globals() if not n.startswith("_")] + ["block", *_BLOCK]
+
+
+def __getattr__(name):
+    if name != "block" and name not in _BLOCK:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from importlib import import_module
+    block = import_module(".block", __name__)
+    globals().update((n, getattr(block, n)) for n in _BLOCK)
+    return globals()[name]                               # (importing a submodule sets `block` itself)
+
+
+def __dir__():
+    return sorted({*globals(), *__all__})
