@@ -7,9 +7,11 @@ driver; anything that touches the GPU then returns PALSGD_ECUDA.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
+import sys
 from pathlib import Path
 
 HERE = Path(__file__).resolve().parent
@@ -42,7 +44,7 @@ def needs_build() -> bool:
 
 def build_extension(force: bool = False) -> Path:
     """_block.so: it is bound to the loaded libpalsgd.so at run time and links torch only."""
-    newest = max(p.stat().st_mtime for p in (EXT_SOURCE, HERE.parent / "include" / "palsgd_block.h", Path(__file__)))
+    newest = max(p.stat().st_mtime for p in (EXT_SOURCE, *(HERE.parent / "include").glob("*.h"), Path(__file__)))
     if not force and EXT.exists() and EXT.stat().st_mtime >= newest:
         return EXT
     import sysconfig
@@ -61,8 +63,7 @@ def build_extension(force: bool = False) -> Path:
     return EXT
 
 
-def build(force: bool = False, verbose: bool = False) -> Path:
-    build_extension(force)
+def build_library(force: bool = False, verbose: bool = False) -> Path:
     if not force and not needs_build():
         return LIB
     tmp = HERE / f"libpalsgd.{os.getpid()}.tmp.so"
@@ -75,6 +76,16 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     return LIB
 
 
+def build(force: bool = False, verbose: bool = False) -> Path:
+    """The library, then the block operators' binding where torch is installed: the library needs neither torch nor
+    Python's headers, and the binding raises ImportError where it is missing."""
+    build_library(force, verbose)
+    if importlib.util.find_spec("torch"):
+        build_extension(force)
+    else:
+        print("torch is not installed: the block operators' Python binding (_block.so) is not built", file=sys.stderr)
+    return LIB
+
+
 if __name__ == "__main__":
-    import sys
     print(build(force=True, verbose="-v" in sys.argv))
