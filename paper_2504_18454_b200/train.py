@@ -21,6 +21,7 @@ import torch
 from . import INNER_ADAMW, PREC_BF16_MASTER, PREC_FP32
 from .arena import ReplicaArena
 from .autograd import gated_ffn, qk_norm_rope
+from .block import block_status
 
 HEAD = 64
 
@@ -116,8 +117,10 @@ def run(K: int = 4, steps: int = 120, layers: int = 2, width: int = 256, hidden:
         losses = w.gradients(batch(K, per_worker, seq, vocab, gen))
         ctx.step(lr * min(1.0, (t + 1) / 10), 0.25 * p / lr, stream)      # a pull moves a quarter of the way
         history.append(losses)
-        if report and (t % 10 == 0 or t + 1 == steps):
-            report(t, float(losses.mean()))
+        if t % 10 == 0 or t + 1 == steps:
+            block_status(stream)                         # raises if a matrix kernel gave up: its results are not to be trained on
+            if report:
+                report(t, float(losses.mean()))
     return torch.stack(history).mean(1).tolist()
 
 

@@ -233,3 +233,22 @@ def test_heads_in_place(dtype, size, interleaved):
     a, b = dq.clone(), k.clone()
     got = P.qk_norm_rope_backward(a, dk, q, b, wq, wk, cos, sin, pos, out=(a, b, None, None), **kw)
     assert all(torch.equal(s, t) for s, t in zip(got, back))
+
+
+# ---------------------------------------------------------------------------------------------- a wait that gave up
+
+def test_training_ends_with_an_error_where_a_kernel_gave_up(monkeypatch):
+    """What palsgd_block_status reports of a bounded wait reaches whoever trains (the report itself is made on the host here)."""
+    from paper_2504_18454_b200 import train
+    seen = []
+
+    def status(stream=None):
+        seen.append(stream)
+        if len(seen) == 2:
+            raise P.PalsgdError(-3, "palsgd_block_status", "a matrix kernel's wait gave up")
+
+    monkeypatch.setattr(train, "block_status", status)
+    steps = []
+    with pytest.raises(P.PalsgdError, match="gave up"):
+        train.run(K=1, steps=40, layers=1, width=64, hidden=64, report=lambda t, v: steps.append(t))
+    assert len(seen) == 2 and steps == [0]
