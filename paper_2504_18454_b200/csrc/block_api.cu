@@ -670,7 +670,9 @@ int launch_qk(const QkPlan& p, const palsgd_qk_shape* s, cudaStream_t st)
             default: return run(qk_kernel<T, W, 1, BACK, PAIRS, 0>, W, 1);
         }
     }
-    if (p.V == W) return run(qk_kernel<T, W, 2, BACK, PAIRS, 32>, W, 2);
+    if constexpr (W == 4) {                              // (bfloat16: 512 values are 32 slots, one a lane)
+        if (p.V == W) return run(qk_kernel<T, W, 2, BACK, PAIRS, 32>, W, 2);
+    }
     if constexpr (PAIRS != QK_CROSS) {                   // (one value a vector is never across)
         if (p.NS <= 2) return run(qk_kernel<T, 1, 2, BACK, PAIRS, 0>, 1, 2);
         return run(qk_kernel<T, 1, 8, BACK, PAIRS, 32>, 1, 8);

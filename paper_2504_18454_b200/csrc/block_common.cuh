@@ -173,13 +173,13 @@ __device__ __forceinline__ void act8_value4(uint32_t w, float step, float* v)
 }
 
 // ---- gated activations
-// SLOPE: also act'(g).  FAST: exp and division to about 2 units in the last place of binary32, for results that are
-// rounded to bfloat16 anyway.
+// SLOPE: also act'(g).  FAST: the slope's exponential to about 2 units in the last place of binary32, for results that are
+// rounded to bfloat16 anyway (act2 has the other forms for those).
 template <int ACT, bool SLOPE, bool FAST>
 __device__ __forceinline__ float act(float g, float& slope)
 {
     if constexpr (ACT == PALSGD_ACT_SILU) {
-        const float s = FAST ? __fdividef(1.0f, 1.0f + __expf(-g)) : 1.0f / (1.0f + expf(-g));
+        const float s = 1.0f / (1.0f + expf(-g));
         const float a = g * s;
         if constexpr (SLOPE) slope = fmaf(a, 1.0f - s, s);
         return a;
@@ -191,7 +191,7 @@ __device__ __forceinline__ float act(float g, float& slope)
         // (1 + tanh z) / 2 = 1 / (1 + e^(-2z))
         const float c = 1.5957691216057308f;                     // 2 sqrt(2/pi)
         const float z2 = c * g * fmaf(0.044715f * g, g, 1.0f);
-        const float s = FAST ? __fdividef(1.0f, 1.0f + __expf(-z2)) : 1.0f / (1.0f + expf(-z2));
+        const float s = 1.0f / (1.0f + expf(-z2));
         if constexpr (SLOPE) {                                   // (its square has to stay finite: 0 times an infinity is NaN)
             const float m = fminf(fabsf(g), 1e9f);
             slope = fmaf(g * s * (1.0f - s), c * fmaf(0.134145f * m, m, 1.0f), s);
