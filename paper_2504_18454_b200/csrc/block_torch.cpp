@@ -130,11 +130,12 @@ void written(const T&... t)
     (note(t), ...);
 }
 
+// (beyond 32 bits, where the C call's arguments end: a value that none of them accepts)
 int64_t integer(PyObject* o)
 {
     const int64_t v = PyLong_AsLongLong(o);
     if (v == -1 && PyErr_Occurred()) throw python_error();
-    return v;
+    return v == (int32_t)v ? v : INT32_MIN;
 }
 
 PyObject* wrap(const std::optional<at::Tensor>& t)

@@ -252,3 +252,16 @@ def test_training_ends_with_an_error_where_a_kernel_gave_up(monkeypatch):
     with pytest.raises(P.PalsgdError, match="gave up"):
         train.run(K=1, steps=40, layers=1, width=64, hidden=64, report=lambda t, v: steps.append(t))
     assert len(seen) == 2 and steps == [0]
+
+
+# ---------------------------------------------------------------------------------------------- numbers of more than 32 bits
+
+def test_an_activation_or_saved_form_beyond_32_bits_is_refused():
+    """Not cut to its low half, which is a valid one."""
+    x, wg, wu, wd, dy = _ffn_inputs(1, 40, 64, 96, torch.bfloat16)
+    _, saved = P.ffn_forward(x, wg, wu, wd)
+    for n in (2 ** 32, 2 ** 32 + 1, -2 ** 32):
+        for call in (lambda: P.ffn_forward(x, wg, wu, wd, activation=n), lambda: P.ffn_forward(x, wg, wu, wd, save=n),
+                     lambda: P.ffn_backward(dy, x, wg, wu, wd, saved, activation=n)):
+            with pytest.raises(P.PalsgdError):
+                call()
