@@ -25,6 +25,8 @@
  *     workers read one matrix); the rows of an output may not overlap.  Buffers need only natural element alignment:
  *     matrices whose base is 16-byte aligned and whose strides are multiples of 16 bytes are read in place by the
  *     copy engines of the matrix kernels; any other is first copied, by one more kernel, into the workspace.
+ *     Unaligned rows are read by whole aligned 16-byte blocks that hold a byte of the row: up to 15 bytes before its
+ *     first and behind its last byte are read (and not used), never across a multiple of 16 bytes.
  */
 #ifndef PALSGD_BLOCK_H_
 #define PALSGD_BLOCK_H_
@@ -78,8 +80,8 @@ int palsgd_act8_unpack(int32_t precision, uint32_t K, uint64_t rows, uint64_t co
  *
  * FP32 products are formed on the tensor cores from three bfloat16 parts of each operand (24 bits together), all six
  * products of parts that reach above 2^-24 of the whole, summed in binary32 with a rounding to nearest every 256 terms.
- * An infinite operand gives NaN there where a product of binary32 would be infinite.  Results do not depend on timing:
- * the same call gives the same bits.
+ * An infinite operand gives NaN there where a product of binary32 would be infinite, and operands below about 2^-110 lose
+ * the bits of their parts below 2^-133.  Results do not depend on timing: the same call gives the same bits.
  *
  * Workspace: call with workspace = NULL to learn *workspace_bytes (nothing is enqueued; all other arguments as in the
  * call to come); then pass at least that many bytes, 256-byte aligned.  Contents need no preparation.  A workspace that
@@ -117,7 +119,7 @@ int palsgd_block_status(void* stream);
 /*
  * Norm of queries and keys for each head, with the position rotation in the same pass.  For worker k, token t, head h
  * of q (and, with its own weights, of k), x in R^head_dim:
- *   r = 1 / sqrt(mean(x^2) + eps);  n = x r w;   the first rotary_dim values of n are rotated by pairs (a, b):
+ *   r = 1 / sqrt(mean(x^2) + eps), eps as a float;  n = x r w;   the first rotary_dim values of n are rotated by pairs:
  *   (a, b) -> (a c_i - b s_i, b c_i + a s_i),  c_i = cos_table[pos][i], s_i = sin_table[pos][i], pos = positions[k][t]
  *   pair i is (i, i + rotary_dim/2), or (2i, 2i+1) with interleaved = 1;  0 <= i < rotary_dim/2.
  * Backward:  dn = the gradient rotated back;  xh = x r;

@@ -3,8 +3,10 @@
 Every call takes tensors whose first axis is the worker; a worker's weights may lie anywhere at a constant stride (a
 view of the rows of a packed ReplicaArena: `ReplicaArena.worker_tensor`).  The last axis is contiguous.  `stream` is a
 raw cudaStream_t; None is torch's current stream of the tensors' device.  Outputs and workspaces that the caller does
-not give are allocated for that stream.  Calls are asynchronous.  Arguments are checked and packed by the native module
-`_block` (csrc/block_torch.cpp); a refused one raises PalsgdError.
+not give are allocated for that stream; inputs that belong to another stream have to outlive the call there
+(`Tensor.record_stream`), as with torch's own operators.  Calls are asynchronous.  Arguments are checked and packed by the
+native module `_block` (csrc/block_torch.cpp); a refused one raises PalsgdError: outputs that overlap an input among them, but
+for a head matrix that the q/k operator writes in place.
 """
 from __future__ import annotations
 
