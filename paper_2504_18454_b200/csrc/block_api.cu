@@ -84,7 +84,7 @@ int check_mat(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, siz
 
 Region region(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, size_t es)
 {
-    if (!m) return Region();
+    if (!m) return Region(nullptr, 0);
     return Region(m->data, cols * es).axis(0, K, m->worker_stride * (int64_t)es).axis(1, rows, m->row_stride * (int64_t)es);
 }
 
@@ -576,7 +576,7 @@ int check_qk(const palsgd_qk_shape* s, const float* cos_t, const float* sin_t, c
 Region region(const palsgd_heads* h, const palsgd_qk_shape* s, uint32_t heads)
 {
     const int64_t es = (int64_t)elem(s->precision);
-    if (!h || heads == 0) return Region();
+    if (!h || heads == 0) return Region(nullptr, 0);
     return Region(h->data, s->head_dim * (uint64_t)es).axis(0, s->K, h->worker_stride * es).axis(1, s->tokens, h->token_stride * es).axis(2, heads, h->head_stride * es);
 }
 

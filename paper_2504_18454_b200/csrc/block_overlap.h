@@ -10,8 +10,8 @@ struct Region {
     uint64_t at, run;             // first byte; bytes of a run (0: nothing)
     uint64_t n[3], s[3];          // elements of an axis and its stride in bytes; an axis without steps has n = 1
 
-    Region() : at(0), run(0), n{1, 1, 1}, s{0, 0, 0} {}
-    Region(const void* p, uint64_t bytes) : Region() { at = reinterpret_cast<uintptr_t>(p); run = p ? bytes : 0; }
+    Region() = default;           // (not set: a call keeps two dozen of these and uses few)
+    Region(const void* p, uint64_t bytes) : at(reinterpret_cast<uintptr_t>(p)), run(p ? bytes : 0), n{1, 1, 1}, s{0, 0, 0} {}
     Region& axis(int i, uint64_t count, int64_t stride_bytes)
     {
         if (count == 0) run = 0;
