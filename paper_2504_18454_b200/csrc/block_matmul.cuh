@@ -17,8 +17,10 @@
 // steps of 64 at 0.33 us, of which 0.29 are matrix instructions; the rest is the start, with operands from memory, and the last
 // tile's epilogue: 38 us if nothing is saved, 42 in full, 44 in 8 bits), hidden pass 46 us (its epilogue: g, u in, dg, du, h
 // out), dx and the weight gradients 94 us (1370 TFLOP/s).  2 workers of 8192, 2048 x 5632, back to back: forward
-// 0.88-0.92 ms, backward 1.9-2.04 ms, 1110-1290 TFLOP/s at the power limit, where a library product sustains 1385.
-// fp32: 8 workers of 500 tokens, 256 x 1024, backward 134-137 us.
+// 0.84-0.97 ms, backward 2.04-2.16 ms, 1050-1350 TFLOP/s at the power limit, where a library product sustains 1385.
+// fp32: 8 workers of 500 tokens, 256 x 1024, backward 136-138 us, forward 69.
+// One token of one worker, 2048 x 5632: forward 48 us, backward 65, for 69 and 138 MB (10.6 and 21 us): the tokens are the
+// long side of every tile, which are then few and mostly zeros.
 #pragma once
 #include <cuda.h>
 

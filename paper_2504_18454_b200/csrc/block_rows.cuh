@@ -1,7 +1,7 @@
 // Row kernels of the block operators: 8-bit checkpoints, and the norm of queries and keys with the position rotation.
-// Both move every byte once.  Checkpoints run at the copy rate (pack and unpack of 32768 x 5632 bfloat16: 165-172 us, 6.5-6.8
+// Both move every byte once.  Checkpoints run at the copy rate (pack and unpack of 32768 x 5632 bfloat16: 168-173 us, 6.5-6.7
 // TB/s); norm and rotation at 70-85 % of it, held by the latencies and instructions of a reduction for each head (8 workers,
-// 2048 tokens, 12 + 12 heads of 64: forward 19.5-21.6 us, backward 32; 2 of 32768, 16 + 4 of 128: backward 185-195, 5.2-5.4 TB/s).
+// 2048 tokens, 12 + 12 heads of 64: forward 20.4-21.6 us, backward 33; 2 of 32768, 16 + 4 of 128: backward 190-199, 5.1-5.3 TB/s).
 #pragma once
 #include "block_common.cuh"
 
