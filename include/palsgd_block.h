@@ -8,6 +8,10 @@
  *   - activation checkpoints in 8 bits                                 palsgd_act8_pack / _unpack
  *   - the norm of queries and keys for each head with the position
  *     rotation in the same pass, forward and backward                  palsgd_qk_norm_rope_forward / _backward
+ *   - the matrix product with bias, activation and residual, forward
+ *     and backward                                                     palsgd_linear_forward / _backward
+ *   - the layer norm with the residual added, forward and backward     palsgd_layer_norm_forward / _backward
+ *   - the cross entropy over a vocabulary, forward and backward        palsgd_cross_entropy_forward / _backward
  *
  * General rules (as in palsgd.h unless stated here)
  *   - Every entry point returns a palsgd_status, never throws, never exits.  Arguments are checked before anything is
@@ -160,6 +164,90 @@ int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const palsgd_heads* d
                                  const int32_t* positions, const palsgd_heads* dq, const palsgd_heads* dk,
                                  const palsgd_mat* dw_q, const palsgd_mat* dw_k, void* workspace,
                                  size_t* workspace_bytes, void* stream);
+
+/*
+ * Matrix product with bias, activation and residual of worker k, x [tokens, d_in], w [d_out, d_in], b [d_out]:
+ *   z = x w^T + b;   y = act(z) + residual
+ * act: one of the four above, or NONE (z itself).  bias and residual [tokens, d_out] may be NULL.  z stays in binary32 up to y.
+ * `save` names what is kept of z for the backward call, as in the feed-forward block: NONE; FULL: pre, in the storage type;
+ * 8BIT: pre, pre_e, the 8-bit checkpoint taken from the binary32 values.  With act = NONE the backward call needs none of it, and
+ * save has to be NONE there and here.  b: rows of d_out in the storage type, one per worker (row_stride unused).
+ *
+ * Backward, at the saved z (the value that it stands for), x in the storage type or (x_e given, save = 8BIT) as a checkpoint:
+ *   dz = dy act'(z);   dx = dz w;   dw = dz^T x;   db = sum over tokens of dz;   the residual's gradient is dy itself
+ * BF16: dz is rounded to bfloat16 once, for the products; db sums the unrounded values.  dx and db may be NULL.  Outputs are
+ * overwritten.  tokens = 0: dw and db are zero.  Sums have a fixed order: the same call gives the same bits.
+ * FP32 products as in the feed-forward block; calls of at most 8 tokens sum in binary32 throughout.
+ * Workspace and errors as for the feed-forward block (d_in or d_out = 0: EINVAL).
+ */
+enum { PALSGD_ACT_NONE = 4 };
+
+typedef struct palsgd_linear_shape {
+    uint32_t K;
+    int32_t  precision, activation, save;
+    uint64_t tokens, d_in, d_out;
+} palsgd_linear_shape;
+
+int palsgd_linear_forward(const palsgd_linear_shape* s, const palsgd_mat* x, const palsgd_mat* w, const palsgd_mat* bias,
+                          const palsgd_mat* residual, const palsgd_mat* y, const palsgd_mat* pre, const palsgd_mat* pre_e,
+                          void* workspace, size_t* workspace_bytes, void* stream);
+int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd_mat* dy, const palsgd_mat* x, const palsgd_mat* x_e,
+                           const palsgd_mat* w, const palsgd_mat* pre, const palsgd_mat* pre_e, const palsgd_mat* dx,
+                           const palsgd_mat* dw, const palsgd_mat* db, void* workspace, size_t* workspace_bytes, void* stream);
+
+/*
+ * Layer norm of every token of worker k, x [tokens, width], w and b [width]:
+ *   h = x + residual (residual NULL: h = x);   m = mean(h);   r = 1 / sqrt(mean((h - m)^2) + eps), eps as a float
+ *   y = (h - m) r w + b
+ * h stays in binary32 up to y; total (given exactly where residual is) receives h in the storage type: the residual stream.
+ * mean, rstd: rows of `tokens` floats, one per worker (row_stride unused); either may be NULL.  w, b: rows of width in the
+ * storage type.
+ * Backward, x being the normed input (total, where there was a residual), at the given mean and rstd:
+ *   xh = (x - m) r;   g = dy w;   dx = r (g - mean(g) - xh mean(g xh)) + dtotal;   dw = sum over tokens of dy xh;   db = sum of dy
+ * dtotal (may be NULL): the gradient that reaches the residual stream past the norm; dx is then the gradient of x and of the
+ * residual alike.  Sums have a fixed order (bitwise repeatable).  dw and db are overwritten; with tokens = 0 they are zero.
+ * A row that holds an infinity or a NaN gives NaN.  Workspace (backward only): as for the feed-forward block.
+ * Errors: EINVAL (NULL, K, width = 0, a size >= 2^31, eps negative or not finite, residual without total or the reverse,
+ * overlapping buffers, small workspace); EUNSUPPORTED (width > 16384); EALIGN; ECUDA.
+ */
+typedef struct palsgd_norm_shape {
+    uint32_t K;
+    int32_t  precision;
+    uint64_t tokens, width;
+    double   eps;             /* forward */
+} palsgd_norm_shape;
+
+int palsgd_layer_norm_forward(const palsgd_norm_shape* s, const palsgd_mat* x, const palsgd_mat* residual, const palsgd_mat* w,
+                              const palsgd_mat* b, const palsgd_mat* y, const palsgd_mat* total, const palsgd_mat* mean,
+                              const palsgd_mat* rstd, void* stream);
+int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const palsgd_mat* dy, const palsgd_mat* x, const palsgd_mat* w,
+                               const palsgd_mat* mean, const palsgd_mat* rstd, const palsgd_mat* dtotal, const palsgd_mat* dx,
+                               const palsgd_mat* dw, const palsgd_mat* db, void* workspace, size_t* workspace_bytes, void* stream);
+
+/*
+ * Cross entropy of every token of worker k, logits [tokens, vocab], targets int32 (one row per worker at
+ * target_worker_stride; 0: one row for all):
+ *   lse = log(sum of e^z);   loss = lse - z_target
+ * loss, lse, dloss: rows of `tokens` floats, one per worker (row_stride unused).
+ *   target < 0: the token does not count: loss 0, gradient 0 whatever its logits are.   target >= vocab: loss and gradient NaN.
+ * Logits of -infinity take no part (a target of that logit: loss +infinity).  A row that holds NaN or +infinity, or nothing
+ * above -infinity, gives NaN in loss and gradient; its lse is NaN, or -infinity where nothing is above that.
+ * Backward, at the given lse:  dlogits = (e^(z - lse) - [target]) dloss.  dlogits may be exactly logits: work in place.
+ * Sums in binary32, in a fixed order; dlogits are rounded once to the storage type.
+ * Errors: EINVAL (NULL, K, vocab = 0, a size >= 2^31, overlapping buffers); EUNSUPPORTED (more than 2^31 - 1 rows, or parts of
+ * rows of 2048 16-byte pieces, of a worker); EALIGN; ECUDA.
+ */
+typedef struct palsgd_loss_shape {
+    uint32_t K;
+    int32_t  precision;
+    uint64_t tokens, vocab;
+    int64_t  target_worker_stride;
+} palsgd_loss_shape;
+
+int palsgd_cross_entropy_forward(const palsgd_loss_shape* s, const palsgd_mat* logits, const int32_t* targets,
+                                 const palsgd_mat* loss, const palsgd_mat* lse, void* stream);
+int palsgd_cross_entropy_backward(const palsgd_loss_shape* s, const palsgd_mat* dloss, const palsgd_mat* logits,
+                                  const int32_t* targets, const palsgd_mat* lse, const palsgd_mat* dlogits, void* stream);
 
 #ifdef __cplusplus
 }

@@ -37,7 +37,8 @@ from .binding import (  # noqa: F401
 # The block operators take torch tensors: `block`, and torch with it, is imported where one of its names is first used.
 _BLOCK = (
     "Act8", "act8_pack", "act8_unpack", "block_status", "ffn_backward", "ffn_forward", "qk_norm_rope",
-    "qk_norm_rope_backward", "ACT8_GROUP", "ACT_GELU", "ACT_GELU_TANH", "ACT_RELU", "ACT_SILU", "SAVE_8BIT", "SAVE_FULL",
+    "qk_norm_rope_backward", "linear_forward", "linear_backward", "layer_norm_forward", "layer_norm_backward",
+    "cross_entropy_forward", "cross_entropy_backward", "ACT_NONE", "ACT8_GROUP", "ACT_GELU", "ACT_GELU_TANH", "ACT_RELU", "ACT_SILU", "SAVE_8BIT", "SAVE_FULL",
     "SAVE_NONE",
 )
 __all__ = [n for n in globals() if not n.startswith("_")] + ["block", *_BLOCK]

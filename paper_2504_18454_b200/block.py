@@ -19,6 +19,7 @@ from .binding import PalsgdError
 from .binding import lib as _base_lib
 
 ACT_SILU, ACT_GELU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2, 3
+ACT_NONE = 4                                             # `linear_*` only
 SAVE_NONE, SAVE_FULL, SAVE_8BIT = 0, 1, 2
 ACT8_GROUP = 32
 EINVAL = -1
@@ -45,6 +46,20 @@ class QkShape(C.Structure):
                 ("pos_worker_stride", C.c_int64), ("eps", C.c_double)]
 
 
+class LinearShape(C.Structure):
+    _fields_ = [("K", C.c_uint32), ("precision", C.c_int32), ("activation", C.c_int32), ("save", C.c_int32),
+                ("tokens", C.c_uint64), ("d_in", C.c_uint64), ("d_out", C.c_uint64)]
+
+
+class NormShape(C.Structure):
+    _fields_ = [("K", C.c_uint32), ("precision", C.c_int32), ("tokens", C.c_uint64), ("width", C.c_uint64), ("eps", C.c_double)]
+
+
+class LossShape(C.Structure):
+    _fields_ = [("K", C.c_uint32), ("precision", C.c_int32), ("tokens", C.c_uint64), ("vocab", C.c_uint64),
+                ("target_worker_stride", C.c_int64)]
+
+
 class Act8(NamedTuple):
     """An 8-bit activation checkpoint: q * 2^(exponent - 127), one exponent per 32 values of the last axis."""
     q: torch.Tensor              # int8 (K, rows, cols) or (rows, cols)
@@ -65,10 +80,13 @@ def lib() -> C.CDLL:
         vp, u32, u64, i32 = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int32
         L.palsgd_act8_pack.argtypes = L.palsgd_act8_unpack.argtypes = [i32, u32, u64, u64] + [vp] * 4
         for n, args in (("ffn_forward", 13), ("ffn_backward", 18), ("qk_norm_rope_forward", 11),
-                        ("qk_norm_rope_backward", 17), ("block_status", 1)):
+                        ("qk_norm_rope_backward", 17), ("linear_forward", 11), ("linear_backward", 13),
+                        ("layer_norm_forward", 10), ("layer_norm_backward", 13), ("cross_entropy_forward", 6),
+                        ("cross_entropy_backward", 7), ("block_status", 1)):
             getattr(L, "palsgd_" + n).argtypes = [vp] * args
         for n in ("block_status", "act8_pack", "act8_unpack", "ffn_forward", "ffn_backward", "qk_norm_rope_forward",
-                  "qk_norm_rope_backward"):
+                  "qk_norm_rope_backward", "linear_forward", "linear_backward", "layer_norm_forward", "layer_norm_backward",
+                  "cross_entropy_forward", "cross_entropy_backward"):
             getattr(L, "palsgd_" + n).restype = C.c_int
         _ready = True
     return L
@@ -207,3 +225,97 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.T
         _refuse("palsgd_qk_norm_rope_backward", "out must be (dq, dk, dw_q, dw_k)")
     return native.qk_backward(q, k, w_q, w_k, cos, sin, positions, eps, 1 if interleaved else 0, dq_out, dk_out, *out,
                               workspace, stream)
+
+
+# ---------------------------------------------------------------------------------------------- linear
+
+def _plain_or_8bit(t: Optional[Saved]):
+    """(values or int8, exponents or None)"""
+    return (t.q, t.exponent) if isinstance(t, Act8) else (t, None)
+
+
+def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None, *, activation: int = ACT_NONE, save: int = SAVE_NONE,
+                   out: Optional[torch.Tensor] = None, saved: Optional[Saved] = None,
+                   workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> Tuple[torch.Tensor, Optional[Saved]]:
+    """palsgd_linear_forward: y = act(x w^T + bias) + residual for K workers.
+
+    x (K, tokens, d_in), w (K, d_out, d_in), bias (K, d_out), residual (K, tokens, d_out).  Returns y and what
+    `linear_backward` needs of an activation besides its arguments: the values before it as a tensor, as Act8, or None, by
+    `save` (with ACT_NONE nothing is needed).  `out`, `saved` and `workspace` give the memory to write to.
+    """
+    native = _native or _ext()
+    if saved is not None and save != SAVE_NONE and isinstance(saved, Act8) != (save == SAVE_8BIT):
+        _refuse("palsgd_linear_forward", "saved must be an Act8 with SAVE_8BIT, and a tensor with SAVE_FULL")
+    y, pre, pre_e = native.linear_forward(x, w, bias, residual, activation, save, out, *_plain_or_8bit(saved), workspace, stream)
+    return y, Act8(pre, pre_e, x.dtype) if save == SAVE_8BIT else pre
+
+
+def linear_backward(dy: torch.Tensor, x: Saved, w: torch.Tensor, saved: Optional[Saved] = None, *,
+                    activation: int = ACT_NONE, need_dx: bool = True, need_dbias: bool = True, out: Optional[Tuple] = None,
+                    workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None):
+    """palsgd_linear_backward: (dx, dw, dbias) from dy and what the forward call saved; the residual's gradient is dy.
+
+    With `saved` as Act8, x may be an Act8 too.  `out` = (dx, dw, dbias) gives the memory to write to (e.g. the workers'
+    gradient buffers); entries may be None.  need_dx, need_dbias = False leave those out (they come back as None).
+    """
+    where = "palsgd_linear_backward"
+    native = _native or _ext()
+    save = SAVE_NONE if saved is None else SAVE_8BIT if isinstance(saved, Act8) else SAVE_FULL
+    if isinstance(x, Act8) and save != SAVE_8BIT:
+        _refuse(where, "x may be an Act8 only where saved is")
+    out = (None,) * 3 if out is None else out
+    if len(out) != 3:
+        _refuse(where, "out must be (dx, dw, dbias)")
+    return native.linear_backward(dy, *_plain_or_8bit(x), w, *_plain_or_8bit(saved), activation, save, 1 if need_dx else 0,
+                                  1 if need_dbias else 0, *out, workspace, stream)
+
+
+# ---------------------------------------------------------------------------------------------- layer norm
+
+def layer_norm_forward(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, residual: Optional[torch.Tensor] = None, *,
+                       eps: float = 1e-5, stats: bool = True, out: Optional[Tuple] = None, stream: Optional[int] = None):
+    """palsgd_layer_norm_forward: the layer norm of x + residual with weights w, b (K, width), x (K, tokens, width).
+
+    Returns (y, total, mean, rstd): total is x + residual in x's type (x itself where there is no residual), mean and rstd
+    (K, tokens) float32 are what `layer_norm_backward` needs (None with stats = False).  `out` = (y, total, mean, rstd)
+    gives the memory to write to; entries may be None.
+    """
+    native = _native or _ext()
+    out = (None,) * 4 if out is None else out
+    if len(out) != 4:
+        _refuse("palsgd_layer_norm_forward", "out must be (y, total, mean, rstd)")
+    y, total, mean, rstd = native.norm_forward(x, w, b, residual, eps, 1 if stats else 0, *out, stream)
+    return y, x if total is None else total, mean, rstd
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        dtotal: Optional[torch.Tensor] = None, *, out: Optional[Tuple] = None,
+                        workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None):
+    """palsgd_layer_norm_backward: (dx, dw, db) from dy, the normed input x (the forward call's total), mean and rstd.
+    dtotal is the gradient that reaches x past the norm: it is added to dx.  `out` gives the memory to write to; entries may
+    be None."""
+    native = _native or _ext()
+    out = (None,) * 3 if out is None else out
+    if len(out) != 3:
+        _refuse("palsgd_layer_norm_backward", "out must be (dx, dw, db)")
+    return native.norm_backward(dy, x, w, mean, rstd, dtotal, *out, workspace, stream)
+
+
+# ---------------------------------------------------------------------------------------------- cross entropy
+
+def cross_entropy_forward(logits: torch.Tensor, targets: torch.Tensor, *, out: Optional[Tuple] = None,
+                          stream: Optional[int] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """palsgd_cross_entropy_forward: (loss, lse), both (K, tokens) float32, of logits (K, tokens, vocab) at targets
+    (K, tokens) int32.  A target below 0 does not count (loss 0); one beyond the vocabulary gives NaN."""
+    native = _native or _ext()
+    loss, lse = (None, None) if out is None else out
+    return native.loss_forward(logits, targets, loss, lse, stream)
+
+
+def cross_entropy_backward(dloss: torch.Tensor, logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, *,
+                           out: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> torch.Tensor:
+    """palsgd_cross_entropy_backward: the gradient of the logits from dloss (K, tokens) float32.  `out` may be the logits
+    themselves: work in place."""
+    native = _native or _ext()
+    return native.loss_backward(dloss, logits, targets, lse, out, stream)

@@ -19,7 +19,7 @@ CSRC = HERE / "csrc"
 LIB = HERE / "libpalsgd.so"
 EXT = HERE / "_block.so"
 EXT_SOURCE = CSRC / "block_torch.cpp"
-SOURCES = [CSRC / "palsgd_api.cu", CSRC / "palsgd_noalloc.cu", CSRC / "block_api.cu"]
+SOURCES = [CSRC / "palsgd_api.cu", CSRC / "palsgd_noalloc.cu", CSRC / "block_api.cu", CSRC / "block_norm_loss_api.cu"]
 DEPS = sorted(CSRC.glob("*.cu*")) + sorted(CSRC.glob("*.h")) + sorted((HERE.parent / "include").glob("*.h")) + [Path(__file__)]
 
 NVCC_FLAGS = [

@@ -1,5 +1,7 @@
 // Host side of the block operators (see include/palsgd_block.h): checks of arguments, workspaces, launches.
+#include "block_columns.cuh"
 #include "block_common.cuh"
+#include "block_linear.cuh"
 #include "block_matmul.cuh"
 #include "block_rows.cuh"
 
@@ -7,54 +9,13 @@
 
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
-#include "block_host.h"
-#include "block_overlap.h"
+#include "block_args.h"
 
 using namespace palsgd::block;
 
 namespace {
-
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
-inline size_t elem(int32_t prec) { return prec == PALSGD_PREC_BF16_MASTER ? 2 : 4; }
-inline bool prec_ok(int32_t p) { return p == PALSGD_PREC_FP32 || p == PALSGD_PREC_BF16_MASTER; }
-
-constexpr uint64_t kMaxSize = 0x7FFFFFFFull;             // rows, columns, tokens: 31 bits (offsets are 64-bit)
-constexpr int64_t kMaxStride = (int64_t)1 << 40;
-
-struct Axis { uint64_t n; int64_t stride; };
-
-// No two of n0*n1*n2 runs of `run` contiguous elements at these strides share an element (sufficient condition: sorted
-// by stride, each axis steps over all of the axes inside it).
-bool disjoint(Axis a, Axis b, Axis c, uint64_t run)
-{
-    Axis v[3] = {a, b, c};
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j + 1 < 3; ++j)
-            if (v[j].stride > v[j + 1].stride) { const Axis t = v[j]; v[j] = v[j + 1]; v[j + 1] = t; }
-    uint64_t span = run;
-    for (const Axis& x : v) {
-        if (x.n <= 1) continue;
-        if ((uint64_t)x.stride < span) return false;
-        span += (uint64_t)x.stride * (x.n - 1);
-    }
-    return true;
-}
-
-// A matrix argument with the strides of axes of at most one element, which nothing steps over, as zero.
-struct Mat {
-    palsgd_mat m{};
-    bool given;
-    Mat(const palsgd_mat* p, uint32_t K, uint64_t rows) : given(p != nullptr)
-    {
-        if (!p) return;
-        m = *p;
-        if (K <= 1) m.worker_stride = 0;
-        if (rows <= 1) m.row_stride = 0;
-    }
-    operator const palsgd_mat*() const { return given ? &m : nullptr; }
-};
 
 struct HeadsOf {
     palsgd_heads m{};
@@ -69,56 +30,6 @@ struct HeadsOf {
     }
     operator const palsgd_heads*() const { return given ? &m : nullptr; }
 };
-
-// A matrix argument: EINVAL / EALIGN / OK.  Nothing is asked of a matrix without elements.
-int check_mat(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, size_t es, bool output)
-{
-    if (!m) return PALSGD_EINVAL;
-    if (m->worker_stride < 0 || m->row_stride < 0 || m->worker_stride > kMaxStride || m->row_stride > kMaxStride) return PALSGD_EINVAL;
-    if (rows == 0 || cols == 0) return PALSGD_OK;
-    if (!m->data) return PALSGD_EINVAL;
-    if (!aligned(m->data, es)) return PALSGD_EALIGN;
-    if (output && !disjoint({K, m->worker_stride}, {rows, m->row_stride}, {1, 0}, cols)) return PALSGD_EINVAL;
-    return PALSGD_OK;
-}
-
-Region region(const palsgd_mat* m, uint32_t K, uint64_t rows, uint64_t cols, size_t es)
-{
-    if (!m) return Region(nullptr, 0);
-    return Region(m->data, cols * es).axis(0, K, m->worker_stride * (int64_t)es).axis(1, rows, m->row_stride * (int64_t)es);
-}
-
-#define BLOCK_TRY(call) do { const int rc_ = (call); if (rc_ != PALSGD_OK) return rc_; } while (0)
-
-// A launch that may start up while the stream's previous kernel still runs (the kernels wait for it: block_common.cuh).
-template <typename... A, typename... B>
-int launch(const char* what, void (*kernel)(A...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const B&... args)
-{
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t c{};
-    c.gridDim = grid; c.blockDim = dim3(threads); c.dynamicSmemBytes = smem; c.stream = st;
-    c.attrs = &early; c.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&c, kernel, args...);
-    if (e == cudaSuccess) return PALSGD_OK;
-    (void)cudaGetLastError();
-    return palsgd_block_cuda_fail((int)e, what);
-}
-
-int sm_count()
-{
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
-    return n;
-}
-
-Divisor divisor(uint32_t d)
-{
-    uint32_t s = 0;
-    while ((1ull << s) < d) ++s;
-    return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
-}
 
 // ------------------------------------------------------------------------------------------------ 8-bit checkpoints
 
@@ -196,37 +107,6 @@ void add_saved(Regions& all, const palsgd_ffn_shape* s, const palsgd_mat* gate, 
     }
 }
 
-// Hands out 256-byte aligned pieces of the workspace; with base = nullptr it only counts.
-struct Arena {
-    char* base;
-    size_t used;
-    void* take(size_t bytes)
-    {
-        void* p = base ? base + used : nullptr;
-        used += (bytes + 255) / 256 * 256;
-        return p;
-    }
-    // Never 0: a caller's buffer of no bytes may be NULL, and NULL asks for the size.
-    size_t need() const { return used ? used : 256; }
-};
-
-int check_workspace(const void* ws, const size_t* bytes)
-{
-    if (!bytes) return PALSGD_EINVAL;
-    if (ws && !aligned(ws, 256)) return PALSGD_EALIGN;
-    return PALSGD_OK;
-}
-
-// The workspace's size is asked for or checked, and that nothing that the call writes overlaps.
-int settle(const Arena& ws, size_t* bytes, Regions& all)
-{
-    if (ws.base && *bytes < ws.need()) { *bytes = ws.need(); return PALSGD_EINVAL; }
-    all.writes(Region(ws.base, ws.used));
-    if (all.clash()) return PALSGD_EINVAL;
-    if (!ws.base) *bytes = ws.need();
-    return PALSGD_OK;
-}
-
 // Set by a kernel whose wait gave up (see palsgd_block_status).
 __device__ unsigned int g_gave_up;
 
@@ -248,9 +128,11 @@ cudaError_t allow_smem() { return cudaFuncSetAttribute(mat_kernel<T, MODE, ACT>,
 template <typename T>
 cudaError_t allow_smem_all()
 {
-    const cudaError_t e[9] = {allow_smem<T, MAT_PLAIN, 0>(),
+    const cudaError_t e[14] = {allow_smem<T, MAT_PLAIN, 0>(),
                               allow_smem<T, MAT_GATED, 0>(), allow_smem<T, MAT_GATED, 1>(), allow_smem<T, MAT_GATED, 2>(), allow_smem<T, MAT_GATED, 3>(),
-                              allow_smem<T, MAT_HIDDEN, 0>(), allow_smem<T, MAT_HIDDEN, 1>(), allow_smem<T, MAT_HIDDEN, 2>(), allow_smem<T, MAT_HIDDEN, 3>()};
+                              allow_smem<T, MAT_HIDDEN, 0>(), allow_smem<T, MAT_HIDDEN, 1>(), allow_smem<T, MAT_HIDDEN, 2>(), allow_smem<T, MAT_HIDDEN, 3>(),
+                              allow_smem<T, MAT_LINEAR, 0>(), allow_smem<T, MAT_LINEAR, 1>(), allow_smem<T, MAT_LINEAR, 2>(), allow_smem<T, MAT_LINEAR, 3>(),
+                              allow_smem<T, MAT_LINEAR, PALSGD_ACT_NONE>()};
     for (cudaError_t r : e) if (r != cudaSuccess) return r;
     return cudaSuccess;
 }
@@ -462,6 +344,7 @@ int launch_mat(const MatLaunch& L, int act, uint32_t pairs, cudaStream_t st)
     if constexpr (MODE == MAT_PLAIN) {
         return launch_mat<T, MODE, 0>(L, pairs, st);
     } else {
+        if constexpr (MODE == MAT_LINEAR) if (act == PALSGD_ACT_NONE) return launch_mat<T, MODE, PALSGD_ACT_NONE>(L, pairs, st);
         switch (act) {
             case PALSGD_ACT_SILU: return launch_mat<T, MODE, PALSGD_ACT_SILU>(L, pairs, st);
             case PALSGD_ACT_GELU: return launch_mat<T, MODE, PALSGD_ACT_GELU>(L, pairs, st);
@@ -489,8 +372,9 @@ void take_shares(Arena& ws, Product* p, int n, uint32_t K, uint32_t parts)
         if (p[i].splits > 1) p[i].part = static_cast<const float*>(ws.take((size_t)p[i].splits * K * p[i].M * (size_t)p[i].ld() * sizeof(float)));
 }
 
-// The products of a call in one launch, the longer ones first, and the kernel that joins what was cut.
-int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, size_t es, uint32_t parts, cudaStream_t st)
+// The products of a call in one launch, the longer ones first, and the kernel that joins what was cut (unless the caller has
+// one of its own).
+int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, size_t es, uint32_t parts, cudaStream_t st, bool joined = true)
 {
     MatLaunch L{};
     JoinArgs join{};
@@ -504,6 +388,14 @@ int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, 
             for (int i = 0; i < 3; ++i) p[i] = p[i + 1];
             p[3] = x;
             heavy = 3;
+        }
+    }
+    if (n == 2) {                                        // the linear operator's dx and dw
+        heavy = 1;
+        if (p[0].length(parts) < p[1].length(parts)) {
+            const Product x = p[0];
+            p[0] = p[1];
+            p[1] = x;
         }
     }
     for (int i = 0; i < n; ++i) {
@@ -527,7 +419,7 @@ int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, 
     }
     if (heavy) L.lag = (uint32_t)(p[0].length(parts) / p[n - 1].length(parts));
     BLOCK_TRY(run_mat<MAT_PLAIN>(L, s, d, st));
-    if (joins == 0) return PALSGD_OK;
+    if (joins == 0 || !joined) return PALSGD_OK;
     const uint64_t want = ceil_div(units, 256), cap = 16ull * d.sms;
     const dim3 grid((unsigned)(want < cap ? want : cap), joins, s->K);
     return launch("joined shares", es == 4 ? join_kernel<float> : join_kernel<bf16>, grid, 256, 0, st, join);
@@ -541,6 +433,115 @@ void set_saved(MatLaunch& L, const palsgd_ffn_shape* s, const palsgd_mat* gate, 
     L.gate = out_of(gate, s->d_ff, es);
     L.up = out_of(up, s->d_ff, es);
     if (s->save == PALSGD_SAVE_8BIT) { L.gate_e = out_of(gate_e, 0, 1); L.up_e = out_of(up_e, 0, 1); }
+}
+
+// ------------------------------------------------------------------------------------------------ linear
+
+int check_linear(const palsgd_linear_shape* s)
+{
+    if (!s || s->K == 0 || s->K > PALSGD_MAX_WORKERS || !prec_ok(s->precision)) return PALSGD_EINVAL;
+    if (s->activation < PALSGD_ACT_SILU || s->activation > PALSGD_ACT_NONE) return PALSGD_EINVAL;
+    if (s->save < PALSGD_SAVE_NONE || s->save > PALSGD_SAVE_8BIT) return PALSGD_EINVAL;
+    if (s->activation == PALSGD_ACT_NONE && s->save != PALSGD_SAVE_NONE) return PALSGD_EINVAL;
+    if (s->d_in == 0 || s->d_out == 0 || s->d_in > kMaxSize || s->d_out > kMaxSize || s->tokens > kMaxSize) return PALSGD_EINVAL;
+    return PALSGD_OK;
+}
+
+// What is saved of z: its matrices are checked, and put on the list of what the call reads or writes.
+int check_pre(const palsgd_linear_shape* s, const palsgd_mat* pre, const palsgd_mat* pre_e, bool output, Regions& all)
+{
+    if (s->save == PALSGD_SAVE_NONE) return PALSGD_OK;
+    const bool eight = s->save == PALSGD_SAVE_8BIT;
+    const size_t es = eight ? 1 : elem(s->precision);
+    const uint64_t groups = ceil_div(s->d_out, PALSGD_ACT8_GROUP);
+    BLOCK_TRY(check_mat(pre, s->K, s->tokens, s->d_out, es, output));
+    if (eight) BLOCK_TRY(check_mat(pre_e, s->K, s->tokens, groups, 1, output));
+    const Region r = region(pre, s->K, s->tokens, s->d_out, es), e = region(eight ? pre_e : nullptr, s->K, s->tokens, groups, 1);
+    if (output) { all.writes(r); all.writes(e); }
+    else { all.reads(r); all.reads(e); }
+    return PALSGD_OK;
+}
+
+// The shape as the matrix kernels' launches take it
+palsgd_ffn_shape products_of(const palsgd_linear_shape* s)
+{
+    return palsgd_ffn_shape{s->K, s->precision, s->activation, s->save, s->tokens, s->d_in, s->d_out};
+}
+
+LinearEnd end_of(const palsgd_linear_shape* s, const palsgd_mat* bias, const palsgd_mat* residual, const palsgd_mat* y, const palsgd_mat* pre, const palsgd_mat* pre_e)
+{
+    const size_t es = elem(s->precision);
+    LinearEnd e{};
+    if (bias) e.bias = out_of(bias, s->d_out, es);
+    if (residual) e.residual = out_of(residual, s->d_out, es);
+    e.y = out_of(y, s->d_out, es);
+    e.save = s->save;
+    if (s->save != PALSGD_SAVE_NONE) e.pre = out_of(pre, s->d_out, s->save == PALSGD_SAVE_8BIT ? 1 : es);
+    if (s->save == PALSGD_SAVE_8BIT) e.pre_e = out_of(pre_e, 0, 1);
+    return e;
+}
+
+// f(the activation as a constant)
+template <typename F>
+int with_act(int act, F&& f)
+{
+    switch (act) {
+        case PALSGD_ACT_SILU: return f(std::integral_constant<int, PALSGD_ACT_SILU>{});
+        case PALSGD_ACT_GELU: return f(std::integral_constant<int, PALSGD_ACT_GELU>{});
+        case PALSGD_ACT_GELU_TANH: return f(std::integral_constant<int, PALSGD_ACT_GELU_TANH>{});
+        case PALSGD_ACT_RELU: return f(std::integral_constant<int, PALSGD_ACT_RELU>{});
+        default: return f(std::integral_constant<int, PALSGD_ACT_NONE>{});
+    }
+}
+
+// Up to eight tokens.  The inner axis is cut into slices for the CTA's warps while there are fewer CTAs than the device
+// holds at a time and a slice keeps a step of its own; an 8-bit checkpoint's group is 32 columns of one CTA.
+template <typename T>
+int run_few(const palsgd_linear_shape* s, const palsgd_mat* x, const palsgd_mat* w, const LinearEnd& end, cudaStream_t st)
+{
+    constexpr uint32_t kStep = 32 * 16 / sizeof(T);
+    FewArgs a{x->data, w->data, x->worker_stride, x->row_stride, w->worker_stride, w->row_stride, (uint32_t)s->tokens, (uint32_t)s->d_out, (uint32_t)s->d_in, 8, 0, s->activation, end};
+    const uint64_t steps = ceil_div(s->d_in, kStep);
+    const uint32_t full = 4 * (uint32_t)sm_count();
+    while (s->save != PALSGD_SAVE_8BIT && a.groups > 1 && steps >= 2 * (8 / a.groups) && s->K * ceil_div(s->d_out, a.groups * kFewRows) < full) a.groups /= 2;
+    a.slice = (uint32_t)(ceil_div(steps, 8 / a.groups) * kStep);
+    const bool wide = s->d_in * sizeof(T) % 16 == 0 && out_of(x, 0, sizeof(T)).wide && out_of(w, 0, sizeof(T)).wide;
+    const dim3 grid((unsigned)ceil_div(s->d_out, a.groups * kFewRows), s->K);
+    auto go = [&](auto mt) { return launch("linear, few tokens", wide ? few_kernel<T, mt, true> : few_kernel<T, mt, false>, grid, 256, 0, st, a); };
+    return a.M <= 1 ? go(std::integral_constant<int, 1>{}) : a.M <= 2 ? go(std::integral_constant<int, 2>{})
+         : a.M <= 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 8>{});
+}
+
+template <typename T>
+int run_linear_join(const palsgd_linear_shape* s, const Product& p, const LinearEnd& end, int sms, cudaStream_t st)
+{
+    const uint32_t per_row = (uint32_t)ceil_div(p.N, 32) * 4;
+    const int64_t w = p.ld() * (int64_t)p.M;
+    const LinearJoinArgs a{p.part, w, w * s->K, p.splits, (uint32_t)p.ld(), (uint32_t)p.M, (uint32_t)p.N, p.M * per_row, divisor(per_row), end};
+    const uint64_t want = ceil_div(a.units, 256), cap = 16ull * sms;
+    return with_act(s->activation, [&](auto act) {
+        return launch("linear, joined shares", linear_join_kernel<T, act>, dim3((unsigned)(want < cap ? want : cap), s->K), 256, 0, st, a);
+    });
+}
+
+// Row CTAs of the gradient before the activation: enough to fill the device, with at least 32 rows each.
+uint32_t slope_rows(const palsgd_linear_shape* s)
+{
+    const uint64_t strips = ceil_div(s->d_out, 256) * s->K, want = ceil_div(6ull * sm_count(), strips);
+    const uint64_t rows = ceil_div(ceil_div(s->tokens, want), 32) * 32;
+    const uint64_t least = ceil_div(s->tokens, 65535);   // (the grid's second axis)
+    return (uint32_t)(rows > least ? rows : least);
+}
+
+template <typename T>
+int run_slope(const palsgd_linear_shape* s, const SlopeArgs& a, cudaStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(s->d_out, 256), (unsigned)ceil_div(s->tokens, a.rows), s->K);
+    return with_act(s->activation, [&](auto act) {
+        if constexpr (act != PALSGD_ACT_NONE)
+            if (s->save == PALSGD_SAVE_8BIT) return launch("linear, gradient before the activation", slope_kernel<T, act, true>, grid, 256, 0, st, a);
+        return launch("linear, gradient before the activation", slope_kernel<T, act, false>, grid, 256, 0, st, a);
+    });
 }
 
 // ------------------------------------------------------------------------------------------------ q/k norm + rotation
@@ -848,6 +849,148 @@ extern "C" int palsgd_ffn_backward(const palsgd_ffn_shape* s, const palsgd_mat* 
     BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     BLOCK_TRY(run_mat<MAT_HIDDEN>(hidden, s, dev, st));
     return run_products(products, n_products, s, dev, es, parts, st);
+}
+
+extern "C" int palsgd_linear_forward(const palsgd_linear_shape* s, const palsgd_mat* x_, const palsgd_mat* w_, const palsgd_mat* bias_,
+                                     const palsgd_mat* residual_, const palsgd_mat* y_, const palsgd_mat* pre_, const palsgd_mat* pre_e_,
+                                     void* workspace, size_t* workspace_bytes, void* stream)
+{
+    BLOCK_TRY(check_linear(s));
+    const uint64_t M = s->tokens, D = s->d_in, N = s->d_out;
+    const size_t es = elem(s->precision);
+    const Mat x(x_, s->K, M), w(w_, s->K, N), bias(bias_, s->K, 1), residual(residual_, s->K, M), y(y_, s->K, M), pre(pre_, s->K, M), pre_e(pre_e_, s->K, M);
+    BLOCK_TRY(check_mat(x, s->K, M, D, es, false));
+    BLOCK_TRY(check_mat(w, s->K, N, D, es, false));
+    if (bias.given) BLOCK_TRY(check_mat(bias, s->K, 1, N, es, false));
+    if (residual.given) BLOCK_TRY(check_mat(residual, s->K, M, N, es, false));
+    BLOCK_TRY(check_mat(y, s->K, M, N, es, true));
+    BLOCK_TRY(check_workspace(workspace, workspace_bytes));
+    Regions all;
+    all.reads(region(x, s->K, M, D, es)); all.reads(region(w, s->K, N, D, es));
+    all.reads(region(bias, s->K, 1, N, es)); all.reads(region(residual, s->K, M, N, es));
+    all.writes(region(y, s->K, M, N, es));
+    BLOCK_TRY(check_pre(s, pre, pre_e, true, all));
+    Arena ws{static_cast<char*>(workspace), 0};
+    Stage stage;
+    const uint32_t parts = s->precision == PALSGD_PREC_FP32 ? 3 : 1;
+    const bool few = M <= kFewTokens;
+    Operand ox, ow;
+    Product product{M, N, D, &ox, nullptr, &ow, nullptr, false, false, y, 1, nullptr};
+    if (!few) {
+        ox = input_operand(ws, stage, x, nullptr, s->precision, s->K, M, D);
+        ow = input_operand(ws, stage, w, nullptr, s->precision, s->K, N, D);
+        take_shares(ws, &product, 1, s->K, parts);
+    }
+    BLOCK_TRY(settle(ws, workspace_bytes, all));
+    if (!workspace || M == 0) return PALSGD_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const LinearEnd end = end_of(s, bias, residual, y, pre, pre_e);
+    if (few) return es == 4 ? run_few<float>(s, x, w, end, st) : run_few<bf16>(s, x, w, end, st);
+    Device dev{};
+    BLOCK_TRY(device_of(dev));
+    const palsgd_ffn_shape f = products_of(s);
+    if (product.splits > 1) {
+        BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
+        BLOCK_TRY(run_products(&product, 1, &f, dev, es, parts, st, false));
+        return es == 4 ? run_linear_join<float>(s, product, end, dev.sms, st) : run_linear_join<bf16>(s, product, end, dev.sms, st);
+    }
+    MatLaunch L{};
+    BLOCK_TRY(add_problem(L, M, N, D, s->K, &ox, nullptr, false, &ow, nullptr, false, kTileN));
+    L.p[0].out[0] = end.y;
+    L.save = s->save;
+    L.gate = end.pre; L.gate_e = end.pre_e; L.bias = end.bias; L.residual = end.residual;
+    BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
+    return run_mat<MAT_LINEAR>(L, &f, dev, st);
+}
+
+extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd_mat* dy_, const palsgd_mat* x_, const palsgd_mat* x_e_,
+                                      const palsgd_mat* w_, const palsgd_mat* pre_, const palsgd_mat* pre_e_, const palsgd_mat* dx_,
+                                      const palsgd_mat* dw_, const palsgd_mat* db_, void* workspace, size_t* workspace_bytes, void* stream)
+{
+    BLOCK_TRY(check_linear(s));
+    const uint64_t M = s->tokens, D = s->d_in, N = s->d_out;
+    const size_t es = elem(s->precision);
+    const Mat dy(dy_, s->K, M), x(x_, s->K, M), x_e(x_e_, s->K, M), w(w_, s->K, N), pre(pre_, s->K, M), pre_e(pre_e_, s->K, M);
+    const Mat dx(dx_, s->K, M), dw(dw_, s->K, N), db(db_, s->K, 1);
+    const bool bent = s->activation != PALSGD_ACT_NONE;
+    if (bent && s->save == PALSGD_SAVE_NONE) return PALSGD_EINVAL;
+    if (x_e.given && s->save != PALSGD_SAVE_8BIT) return PALSGD_EINVAL;
+    BLOCK_TRY(check_mat(dy, s->K, M, N, es, false));
+    BLOCK_TRY(check_mat(x, s->K, M, D, x_e.given ? 1 : es, false));
+    if (x_e.given) BLOCK_TRY(check_mat(x_e, s->K, M, ceil_div(D, PALSGD_ACT8_GROUP), 1, false));
+    BLOCK_TRY(check_mat(w, s->K, N, D, es, false));
+    if (dx.given) BLOCK_TRY(check_mat(dx, s->K, M, D, es, true));
+    BLOCK_TRY(check_mat(dw, s->K, N, D, es, true));
+    if (db.given) BLOCK_TRY(check_mat(db, s->K, 1, N, es, true));
+    BLOCK_TRY(check_workspace(workspace, workspace_bytes));
+    Regions all;
+    all.reads(region(dy, s->K, M, N, es));
+    all.reads(region(x, s->K, M, D, x_e.given ? 1 : es));
+    all.reads(region(x_e, s->K, M, ceil_div(D, PALSGD_ACT8_GROUP), 1));
+    all.reads(region(w, s->K, N, D, es));
+    BLOCK_TRY(check_pre(s, pre, pre_e, false, all));
+    all.writes(region(dx, s->K, M, D, es)); all.writes(region(dw, s->K, N, D, es)); all.writes(region(db, s->K, 1, N, es));
+    Arena ws{static_cast<char*>(workspace), 0};
+    Stage stage;
+    const uint32_t parts = s->precision == PALSGD_PREC_FP32 ? 3 : 1;
+    Operand odz, ox, ow;
+    SlopeArgs slope{};
+    bool pass = false;                                   // dz is formed, or summed, by a pass of its own
+    Product products[2];
+    int n_products = 0;
+    if (M) {
+        // dy is read in place where it is dz and the copy engine can; else the pass writes the operand
+        Stage in_place;
+        Arena none{nullptr, 0};
+        odz = input_operand(none, in_place, dy, nullptr, s->precision, s->K, M, N);
+        const bool write = bent || in_place.n;
+        if (write) {
+            odz = own_operand(ws, s->K, M, N, parts);
+            slope.dst = static_cast<bf16*>(const_cast<void*>(odz.p));
+            slope.dstw = odz.w; slope.ld = odz.r; slope.dst_part = odz.part;
+        }
+        pass = write || db.given;
+        slope.rows = slope_rows(s);
+        if (db.given) slope.part = static_cast<float*>(ws.take((size_t)s->K * ceil_div(M, slope.rows) * N * sizeof(float)));
+        ox = input_operand(ws, stage, x, x_e, s->precision, s->K, M, D);
+        if (dx.given) {
+            ow = input_operand(ws, stage, w, nullptr, s->precision, s->K, N, D);
+            products[n_products++] = Product{M, D, N, &odz, nullptr, &ow, nullptr, false, true, dx, 1, nullptr};
+        }
+        products[n_products++] = Product{N, D, M, &odz, nullptr, &ox, nullptr, true, true, dw, 1, nullptr};
+        take_shares(ws, products, n_products, s->K, parts);
+    }
+    BLOCK_TRY(settle(ws, workspace_bytes, all));
+    if (!workspace) return PALSGD_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (M == 0) {
+        ZeroArgs z{};
+        z.p[0] = dw.m.data; z.w[0] = dw.m.worker_stride; z.r[0] = dw.m.row_stride; z.rows[0] = (uint32_t)N; z.cols[0] = (uint32_t)D;
+        z.p[1] = db.m.data; z.w[1] = db.m.worker_stride; z.rows[1] = db.given; z.cols[1] = (uint32_t)N;
+        const dim3 grid((unsigned)N < 1024u ? (unsigned)N : 1024u, 2, s->K);
+        return launch("zero weight gradients", es == 4 ? zero_kernel<float> : zero_kernel<bf16>, grid, 256, 0, st, z);
+    }
+    Device dev{};
+    BLOCK_TRY(device_of(dev));
+    BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
+    if (pass) {
+        slope.dy = dy.m.data; slope.dw = dy.m.worker_stride; slope.dr = dy.m.row_stride;
+        slope.dy_wide = out_of(dy, N, es).wide;
+        if (bent) {
+            const bool eight = s->save == PALSGD_SAVE_8BIT;
+            slope.pre = pre.m.data; slope.pw = pre.m.worker_stride; slope.pr = pre.m.row_stride;
+            slope.pre_wide = eight ? aligned(pre.m.data, 8) && pre.m.worker_stride % 8 == 0 && pre.m.row_stride % 8 == 0 : out_of(pre, N, es).wide;
+            if (eight) { slope.pre_e = static_cast<const uint8_t*>(pre_e.m.data); slope.ew = pre_e.m.worker_stride; slope.er = pre_e.m.row_stride; }
+        }
+        slope.M = (uint32_t)M; slope.N = (uint32_t)N;
+        BLOCK_TRY(es == 4 ? run_slope<float>(s, slope, st) : run_slope<bf16>(s, slope, st));
+    }
+    if (db.given) {
+        ColumnSumArgs c{slope.part, {db.m.data, nullptr}, {db.m.worker_stride, 0}, (uint32_t)ceil_div(M, slope.rows), (uint32_t)N, (uint32_t)N};
+        BLOCK_TRY(launch("linear, bias gradient", es == 4 ? column_sum_kernel<float> : column_sum_kernel<bf16>, dim3((unsigned)ceil_div(N, 32), s->K), 256, 0, st, c));
+    }
+    const palsgd_ffn_shape f = products_of(s);
+    return run_products(products, n_products, &f, dev, es, parts, st);
 }
 
 extern "C" int palsgd_block_status(void* stream)

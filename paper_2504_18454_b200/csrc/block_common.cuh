@@ -82,11 +82,9 @@ __device__ __forceinline__ uint32_t f2_narrow(f2 v)
 // Reads are of whole aligned 16-byte blocks that hold a byte of the row, shifted into place; such a block lies inside the
 // row's allocation, which starts and ends on a multiple of 16 bytes.  Writes are as wide as the address allows; ELEM: the
 // size of the elements, on a multiple of which the address lies.
-__device__ __forceinline__ uint4 get16(const unsigned char* p, uint32_t bytes)
+__device__ __forceinline__ uint4 shift16(const uint4& a, const uint4& b, uint32_t o, uint32_t bytes)    // from byte o of a on
 {
-    const uint32_t o = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15, s = 8 * (o & 3);
-    const uint4* base = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
-    const uint4 a = bytes ? __ldg(base) : make_uint4(0, 0, 0, 0), b = bytes && o + bytes > 16 ? __ldg(base + 1) : make_uint4(0, 0, 0, 0);
+    const uint32_t s = 8 * (o & 3);
     uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
     for (int i = 0; i < 6; ++i) w[i] = o & 8 ? w[i + 2] : w[i];
@@ -98,6 +96,13 @@ __device__ __forceinline__ uint4 get16(const unsigned char* p, uint32_t bytes)
     for (uint32_t i = 0; i < 4; ++i)                      // what lies behind the row's end is not of it
         if (4 * i + 4 > bytes) w[i] = 4 * i >= bytes ? 0u : w[i] & ((1u << (8 * (bytes & 3))) - 1u);
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 get16(const unsigned char* p, uint32_t bytes)
+{
+    const uint32_t o = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15;
+    const uint4* base = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+    const uint4 a = bytes ? __ldg(base) : make_uint4(0, 0, 0, 0), b = bytes && o + bytes > 16 ? __ldg(base + 1) : make_uint4(0, 0, 0, 0);
+    return shift16(a, b, o, bytes);
 }
 template <int ELEM>
 __device__ __forceinline__ void put16(unsigned char* p, uint32_t bytes, const uint4& v)
@@ -178,7 +183,10 @@ __device__ __forceinline__ void act8_value4(uint32_t w, float step, float* v)
 template <int ACT, bool SLOPE, bool FAST>
 __device__ __forceinline__ float act(float g, float& slope)
 {
-    if constexpr (ACT == PALSGD_ACT_SILU) {
+    if constexpr (ACT == PALSGD_ACT_NONE) {
+        if constexpr (SLOPE) slope = 1.0f;
+        return g;
+    } else if constexpr (ACT == PALSGD_ACT_SILU) {
         const float s = 1.0f / (1.0f + expf(-g));
         const float a = g * s;
         if constexpr (SLOPE) slope = fmaf(a, 1.0f - s, s);
@@ -244,6 +252,43 @@ __device__ __forceinline__ f2 act2(f2 g, f2& slope)
         const float ax = act<ACT, SLOPE, true>(x, sx), ay = act<ACT, SLOPE, true>(y, sy);
         if constexpr (SLOPE) slope = f2_of(sx, sy);
         return f2_of(ax, ay);
+    }
+}
+
+// ---- eight values of a row at any address, the first `n` of them inside it (the others read as 0, and are not written).
+// wide: eight values of every row start on a 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ void row8_load(const T* p, uint32_t n, bool wide, f2 (&v)[4])
+{
+    const unsigned char* b = reinterpret_cast<const unsigned char*>(p);
+    if constexpr (sizeof(T) == 2) {
+        const uint4 q = wide && n >= 8 ? __ldg(reinterpret_cast<const uint4*>(p)) : get16(b, 2 * min(n, 8u));
+        v[0] = f2_wide(q.x); v[1] = f2_wide(q.y); v[2] = f2_wide(q.z); v[3] = f2_wide(q.w);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            const uint4 q = wide && n >= 8 ? __ldg(reinterpret_cast<const uint4*>(p) + i) : get16(b + 16 * i, n > 4 * i ? 4 * min(n - 4 * i, 4u) : 0);
+            v[2 * i] = f2_of(__uint_as_float(q.x), __uint_as_float(q.y)); v[2 * i + 1] = f2_of(__uint_as_float(q.z), __uint_as_float(q.w));
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void row8_store(T* p, uint32_t n, bool wide, const f2 (&v)[4])
+{
+    unsigned char* b = reinterpret_cast<unsigned char*>(p);
+    if constexpr (sizeof(T) == 2) {
+        const uint4 q = make_uint4(f2_narrow(v[0]), f2_narrow(v[1]), f2_narrow(v[2]), f2_narrow(v[3]));
+        if (wide && n >= 8) *reinterpret_cast<uint4*>(p) = q;
+        else put16<2>(b, 2 * min(n, 8u), q);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            float x, y, z, w;
+            f2_get(v[2 * i], x, y); f2_get(v[2 * i + 1], z, w);
+            const uint4 q = make_uint4(__float_as_uint(x), __float_as_uint(y), __float_as_uint(z), __float_as_uint(w));
+            if (wide && n >= 8) reinterpret_cast<uint4*>(p)[i] = q;
+            else put16<4>(b + 16 * i, n > 4 * i ? 4 * min(n - 4 * i, 4u) : 0, q);
+        }
     }
 }
 

@@ -1,0 +1,324 @@
+// Kernels of the matrix product with bias, activation and residual beside the matrix kernel: calls of few tokens, the
+// epilogue of products whose inner axis was cut into shares, and the gradient before the activation with its column sums.
+#pragma once
+#include "block_matmul.cuh"
+
+namespace palsgd {
+namespace block {
+
+struct LinearEnd {                // what follows the sums
+    MatOut bias, residual, y, pre, pre_e;                               // p may be NULL but for y's
+    int save;
+};
+
+// ---------------------------------------------------------------------------------------------- few tokens
+//
+// Up to eight tokens: bound by reading the weights once.  A warp takes four rows of w over its slice of the inner axis, in
+// pieces of 16 bytes a lane, and multiplies each with all of the tokens in binary32 (the tokens come from the caches).  A CTA's
+// eight warps are `rows` row groups by slices; slices are joined in shared memory in order, and one thread finishes each
+// value.  (The matrix kernel's tile of one token multiplies 255 rows of zeros, and a few outputs give it too few tiles.)
+constexpr uint32_t kFewTokens = 8, kFewRows = 4;
+
+struct FewArgs {
+    const void *x, *w;
+    int64_t  xw, xr, ww, wr;
+    uint32_t M, N, D;
+    uint32_t groups;              // row groups of a CTA: 8 / groups slices of the inner axis
+    uint32_t slice;               // values of a slice: a multiple of a warp's step
+    int      act;
+    LinearEnd end;
+};
+
+template <typename T>
+__device__ __forceinline__ float few_act(int kind, float z)             // one value a thread: no copies of the kernel by activation
+{
+    float slope;
+    switch (kind) {
+        case PALSGD_ACT_SILU: return act<PALSGD_ACT_SILU, false, sizeof(T) == 2>(z, slope);
+        case PALSGD_ACT_GELU: return act<PALSGD_ACT_GELU, false, sizeof(T) == 2>(z, slope);
+        case PALSGD_ACT_GELU_TANH: return act<PALSGD_ACT_GELU_TANH, false, sizeof(T) == 2>(z, slope);
+        case PALSGD_ACT_RELU: return act<PALSGD_ACT_RELU, false, sizeof(T) == 2>(z, slope);
+        default: return z;
+    }
+}
+
+template <typename T, int MT, bool WIDE>
+__global__ void __launch_bounds__(256, MT >= 4 ? 2 : 3) few_kernel(const __grid_constant__ FewArgs a)
+{
+    constexpr int V = 16 / (int)sizeof(T), H = V / 2, C = kFewRows * MT;
+    constexpr uint32_t kStep = 32 * V;
+    __shared__ float sums[8][C];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp % a.groups, slice = warp / a.groups;
+    const int64_t k = blockIdx.y;
+    const uint32_t n0 = blockIdx.x * a.groups * kFewRows;
+    let_next_start();
+    wait_for_previous();
+    const T *x = static_cast<const T*>(a.x) + k * a.xw, *w[kFewRows];
+#pragma unroll
+    for (uint32_t r = 0; r < kFewRows; ++r)               // (rows past the end: the last one, and their sums are not used)
+        w[r] = static_cast<const T*>(a.w) + k * a.ww + (int64_t)min(n0 + group * kFewRows + r, a.N - 1) * a.wr;
+    f2 acc[kFewRows][MT];
+#pragma unroll
+    for (uint32_t r = 0; r < kFewRows; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[r][m] = 0;
+    auto piece = [&](const T* row, uint32_t c) {
+        if constexpr (WIDE) return c < a.D ? __ldg(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+        else return get16(reinterpret_cast<const unsigned char*>(row + c), c < a.D ? min(a.D - c, (uint32_t)V) * (uint32_t)sizeof(T) : 0);
+    };
+    auto widen = [](const uint4& q, f2 (&v)[H]) {
+        if constexpr (sizeof(T) == 2) {
+            v[0] = f2_wide(q.x); v[1] = f2_wide(q.y); v[2] = f2_wide(q.z); v[3] = f2_wide(q.w);
+        } else {
+            v[0] = f2_of(__uint_as_float(q.x), __uint_as_float(q.y)); v[1] = f2_of(__uint_as_float(q.z), __uint_as_float(q.w));
+        }
+    };
+    const uint32_t last = min(a.D, (slice + 1) * a.slice);
+    constexpr int U = MT == 8 ? 1 : 2;                    // steps whose weights are under way together
+    for (uint32_t c0 = slice * a.slice; c0 < last; c0 += U * kStep) {
+        uint4 q[U][kFewRows];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (uint32_t r = 0; r < kFewRows; ++r) q[u][r] = c0 + u * kStep < last ? piece(w[r], c0 + u * kStep + lane * V) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t c = c0 + u * kStep + lane * V;
+            f2 wv[kFewRows][H];
+#pragma unroll
+            for (uint32_t r = 0; r < kFewRows; ++r) widen(q[u][r], wv[r]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                f2 xv[H];
+                widen((uint32_t)m < a.M && c0 + u * kStep < last ? piece(x + (int64_t)m * a.xr, c) : make_uint4(0, 0, 0, 0), xv);
+#pragma unroll
+                for (uint32_t r = 0; r < kFewRows; ++r)
+#pragma unroll
+                    for (int i = 0; i < H; ++i) acc[r][m] = f2_fma(wv[r][i], xv[i], acc[r][m]);
+            }
+        }
+    }
+    // the lanes' sums: every step halves the values that a lane keeps, until it has one; then the rest of the lanes are added
+    float v[C];
+#pragma unroll
+    for (uint32_t r = 0; r < kFewRows; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float p, q;
+            f2_get(acc[r][m], p, q);
+            v[r * MT + m] = p + q;
+        }
+    int d = 16;
+#pragma unroll
+    for (int h = C / 2; h >= 1; h /= 2, d /= 2)
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const bool upper = lane & d;
+            const float send = upper ? v[i] : v[i + h], keep = upper ? v[i + h] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, d);
+        }
+    for (; d; d /= 2) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], d);
+    if (lane % (32 / C) == 0) sums[warp][lane / (32 / C)] = v[0];
+    __syncthreads();
+    // one thread for each value: column of the CTA's, token
+    const uint32_t cols = a.groups * kFewRows, col = threadIdx.x % cols, m = threadIdx.x / cols, n = n0 + col;
+    const bool on = m < a.M && n < a.N;
+    const LinearEnd& e = a.end;
+    float z = 0.0f;
+    if (on) {
+        const uint32_t at = (col % kFewRows) * MT + m;
+        z = sums[col / kFewRows][at];
+        for (uint32_t s = 1; s < 8 / a.groups; ++s) z += sums[s * a.groups + col / kFewRows][at];
+        if (e.bias.p) z += to_f(static_cast<const T*>(e.bias.p)[k * e.bias.w + n]);
+    }
+    if (e.save == PALSGD_SAVE_8BIT) {                     // 32 columns a CTA: a warp holds a group of one token
+        float top = fabsf(z);
+#pragma unroll
+        for (int s = 16; s; s >>= 1) top = act8_max(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+        const uint32_t E = act8_exponent(top);
+        if (on) {
+            static_cast<int8_t*>(e.pre.p)[k * e.pre.w + (int64_t)m * e.pre.r + n] = (int8_t)act8_quant4(z, z, z, z, act8_inverse(E));
+            if (lane == 0) static_cast<uint8_t*>(e.pre_e.p)[k * e.pre_e.w + (int64_t)m * e.pre_e.r + n / 32] = (uint8_t)E;
+        }
+    } else if (e.save == PALSGD_SAVE_FULL && on) {
+        static_cast<T*>(e.pre.p)[k * e.pre.w + (int64_t)m * e.pre.r + n] = from_f<T>(z);
+    }
+    if (!on) return;
+    float y = few_act<T>(a.act, z);
+    if (e.residual.p) y += to_f(static_cast<const T*>(e.residual.p)[k * e.residual.w + (int64_t)m * e.residual.r + n]);
+    static_cast<T*>(e.y.p)[k * e.y.w + (int64_t)m * e.y.r + n] = from_f<T>(y);
+}
+
+// ---------------------------------------------------------------------------------------------- shares
+
+// The shares' sums of a product joined in a fixed order, and what follows them.  A thread has eight columns; four threads of
+// a warp, 32 (the rows' units are whole groups).
+struct LinearJoinArgs {
+    const float* part;            // [splits][K][M][ld]
+    int64_t  w, share;            // strides of a worker and of a share
+    uint32_t splits, ld, M, N;
+    uint64_t units;               // of one worker
+    Divisor  per_row;             // 4 ceil(N / 32)
+    LinearEnd end;
+};
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant__ LinearJoinArgs a)
+{
+    let_next_start();
+    wait_for_previous();
+    const int64_t k = blockIdx.y;
+    const LinearEnd& e = a.end;
+    const uint64_t last = (a.units + 255) / 256 * 256;    // (whole warps: a group's threads look at one another)
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < last; i += (uint64_t)gridDim.x * 256) {
+        const bool on = i < a.units;
+        const uint64_t row = !on ? 0 : a.units < 0x80000000ull ? a.per_row.of((uint32_t)i) : i / a.per_row.d;
+        const uint32_t c = on ? (uint32_t)(i - row * a.per_row.d) * 8 : 0, n = on && c < a.N ? min(a.N - c, 8u) : 0;
+        f2 z[4] = {0, 0, 0, 0};
+        if (n) {                                          // (the shares' rows hold a multiple of eight columns)
+            const float* p = a.part + k * a.w + (int64_t)row * a.ld + c;
+            row8_load(p, 8, true, z);
+            for (uint32_t s = 1; s < a.splits; ++s) {
+                f2 v[4];
+                row8_load(p + s * a.share, 8, true, v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] = f2_add(z[j], v[j]);
+            }
+            if (e.bias.p) {
+                f2 b[4];
+                row8_load(static_cast<const T*>(e.bias.p) + k * e.bias.w + c, n, e.bias.wide, b);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] = f2_add(z[j], b[j]);
+            }
+        }
+        if (e.save == PALSGD_SAVE_8BIT) {
+            float v[8], top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f2_get(z[j], v[2 * j], v[2 * j + 1]);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) if (j < n) top = act8_max(top, v[j]);
+            top = act8_max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = act8_max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const uint32_t E = act8_exponent(top);
+            const float inv = act8_inverse(E);
+            if (n) {
+                unsigned char* q = static_cast<unsigned char*>(e.pre.p) + k * e.pre.w + (int64_t)row * e.pre.r + c;
+                const uint2 t = make_uint2(act8_quant4(v[0], v[1], v[2], v[3], inv), act8_quant4(v[4], v[5], v[6], v[7], inv));
+                if (e.pre.wide && n == 8) *reinterpret_cast<uint2*>(q) = t;
+                else put16<1>(q, n, make_uint4(t.x, t.y, 0, 0));
+                if (c % 32 == 0) static_cast<uint8_t*>(e.pre_e.p)[k * e.pre_e.w + (int64_t)row * e.pre_e.r + c / 32] = (uint8_t)E;
+            }
+        } else if (e.save == PALSGD_SAVE_FULL && n) {
+            row8_store(static_cast<T*>(e.pre.p) + k * e.pre.w + (int64_t)row * e.pre.r + c, n, e.pre.wide, z);
+        }
+        if (n == 0) continue;
+        f2 unused;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = act_pair<T, ACT, false>(z[j], unused);
+        if (e.residual.p) {
+            f2 r[4];
+            row8_load(static_cast<const T*>(e.residual.p) + k * e.residual.w + (int64_t)row * e.residual.r + c, n, e.residual.wide, r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = f2_add(z[j], r[j]);
+        }
+        row8_store(static_cast<T*>(e.y.p) + k * e.y.w + (int64_t)row * e.y.r + c, n, e.y.wide, z);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- gradient before the activation
+
+// dz = dy act'(z) as the products' operand (bfloat16, or fp32 in three parts; dst NULL: dy itself is the operand), and its
+// sums over a CTA's rows, unrounded, to the CTA's row of `part` (NULL: none wanted).  A CTA has 256 columns -- a lane eight of
+// them -- and its warps take the rows in turn.
+struct SlopeArgs {
+    const void *dy, *pre;         // pre: NULL without an activation
+    const uint8_t* pre_e;         // 8 bits
+    int64_t  dw, dr, pw, pr, ew, er;
+    bf16*    dst;
+    int64_t  dstw, ld, dst_part;  // worker, row and part strides
+    float*   part;                // [K][row CTAs][N]
+    uint32_t M, N, rows;          // rows of a CTA
+    int      dy_wide, pre_wide;
+};
+
+template <typename T, int ACT, bool EIGHT>
+__global__ void __launch_bounds__(256, 2) slope_kernel(const __grid_constant__ SlopeArgs a)
+{
+    constexpr int U = 4;                                  // rows of a warp under way
+    __shared__ float sums[8][257];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 256 + lane * 8;
+    const int64_t k = blockIdx.z;
+    const uint32_t n = c < a.N ? min(a.N - c, 8u) : 0, room = a.dst && c < a.ld ? 8u : 0u;    // (the operand's rows hold a multiple of eight columns)
+    const uint32_t first = blockIdx.y * a.rows, last = min(a.M, first + a.rows);
+    let_next_start();
+    wait_for_previous();
+    f2 sum[4] = {0, 0, 0, 0};
+    for (uint32_t r0 = first + warp; r0 < last; r0 += 8 * U) {
+        f2 d[U][4], z[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = r0 + 8 * u;
+            const uint32_t m = r0 + 8 * u < last ? n : 0;
+            row8_load(static_cast<const T*>(a.dy) + k * a.dw + r * a.dr + c, m, a.dy_wide, d[u]);
+            if constexpr (ACT != PALSGD_ACT_NONE) {
+                if constexpr (EIGHT) {
+                    const unsigned char* p = static_cast<const unsigned char*>(a.pre) + k * a.pw + r * a.pr + c;
+                    uint2 q;
+                    if (a.pre_wide && m == 8) q = __ldg(reinterpret_cast<const uint2*>(p));
+                    else { const uint4 t = get16(p, m); q = make_uint2(t.x, t.y); }
+                    const float s = act8_step(m ? a.pre_e[k * a.ew + r * a.er + c / 32] : 127u);
+                    float v[8];
+                    act8_value4(q.x, s, v);
+                    act8_value4(q.y, s, v + 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[u][i] = f2_of(v[2 * i], v[2 * i + 1]);
+                } else {
+                    row8_load(static_cast<const T*>(a.pre) + k * a.pw + r * a.pr + c, m, a.pre_wide, z[u]);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (r0 + 8 * u >= last) break;
+            if constexpr (ACT != PALSGD_ACT_NONE) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f2 slope;
+                    act_pair<T, ACT, true>(z[u][i], slope);
+                    d[u][i] = f2_mul(d[u][i], slope);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = f2_add(sum[i], d[u][i]);
+            if (room) {
+                bf16* to = a.dst + k * a.dstw + (int64_t)(r0 + 8 * u) * a.ld + c;
+                if constexpr (sizeof(T) == 2) {
+                    *reinterpret_cast<uint4*>(to) = make_uint4(f2_narrow(d[u][0]), f2_narrow(d[u][1]), f2_narrow(d[u][2]), f2_narrow(d[u][3]));
+                } else {
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f2_get(d[u][i], v[2 * i], v[2 * i + 1]);
+                    three_parts<8>(v, [&](int part, const uint32_t (&w)[4]) { *reinterpret_cast<uint4*>(to + part * a.dst_part) = make_uint4(w[0], w[1], w[2], w[3]); });
+                }
+            }
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x, y;
+        f2_get(sum[i], x, y);
+        sums[warp][lane * 8 + 2 * i] = x;
+        sums[warp][lane * 8 + 2 * i + 1] = y;
+    }
+    __syncthreads();
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x;
+    if (at >= a.N) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
+    a.part[((uint64_t)k * gridDim.y + blockIdx.y) * a.N + at] = t;
+}
+
+}  // namespace block
+}  // namespace palsgd

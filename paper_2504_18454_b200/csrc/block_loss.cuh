@@ -1,0 +1,222 @@
+// Row kernels of the block operators: cross entropy over a vocabulary, forward and backward.
+//
+// Forward: one pass over the logits.  A lane keeps the largest value that it has seen and the sum of e^(z - largest), for two
+// pieces of 16 bytes at a time; lanes, then warps, join theirs.  Rows are read by the aligned 16-byte pieces that hold their
+// values (a vocabulary of odd size starts every row at another offset), what is outside masked.
+// Backward: e^(z - lse) from what the forward call left, one read and one write a value.
+// Bound by memory.
+#pragma once
+#include "block_common.cuh"
+
+namespace palsgd {
+namespace block {
+
+struct LossArgs {
+    const void*    z;
+    const int32_t* target;
+    const float*   dloss;         // backward
+    float *loss, *lse;            // lse: written (forward), read (backward)
+    void*          dz;            // backward; may be z
+    int64_t  zw, zr, tw, lw, sw, gw, dw, dr;         // worker and row strides, elements
+    uint64_t rows;
+    uint32_t vocab, warps;        // of a team that has a row
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// A largest value and the sum of e^(z - largest).  No value yet, or none above -infinity: the sum is zero or NaN.
+struct Soft { float top, sum; };
+__device__ __forceinline__ float soft_scale(float from, float to)       // e^(from - to); 0 for from = -infinity, whatever to is
+{
+    return from == -INFINITY ? 0.0f : fast_exp2((from - to) * kLog2e);
+}
+__device__ __forceinline__ Soft soft_join(Soft a, Soft b)
+{
+    const float top = fmaxf(a.top, b.top);
+    // (a side without a value counts for nothing; one that holds a NaN keeps it)
+    return Soft{top, fmaf(a.sum, soft_scale(a.top, top), b.sum * soft_scale(b.top, top))};
+}
+
+// 16 bytes as floats
+template <typename T>
+__device__ __forceinline__ void floats_of(const uint4& p, float (&v)[16 / sizeof(T)])
+{
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+        else v[i] = __uint_as_float(w[i]);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(1024) loss_forward_kernel(const __grid_constant__ LossArgs a)
+{
+    constexpr int V = 16 / (int)sizeof(T), P = 4;         // pieces of a lane under way
+    __shared__ Soft places[32];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
+    const uint32_t size = a.warps * 32, me = threadIdx.x - team * size;
+    const int64_t k = blockIdx.y;
+    let_next_start();
+    wait_for_previous();
+    const uint64_t row = (uint64_t)blockIdx.x * teams + team;
+    if (row >= a.rows) return;                            // (a whole team: its barrier is its own)
+    const T* z = static_cast<const T*>(a.z) + k * a.zw + (int64_t)row * a.zr;
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(z) & 15) / (uint32_t)sizeof(T);      // values of the first piece that are not the row's
+    const uint4* p = reinterpret_cast<const uint4*>(z - off);
+    const uint32_t end = off + a.vocab, pieces = (end + V - 1) / V;
+    Soft s{-INFINITY, 0.0f};
+    for (uint32_t i = me; i < pieces; i += size * P) {
+        uint4 q[P];
+#pragma unroll
+        for (int j = 0; j < P; ++j) q[j] = i + j * size < pieces ? __ldg(p + i + j * size) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint32_t at = i + j * size;
+            if (at >= pieces) break;
+            float v[V];
+            floats_of<T>(q[j], v);
+            if (at == 0 || (at + 1) * V > end) {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (at * V + e < off || at * V + e >= end) v[e] = -INFINITY;
+            }
+            float top = v[0];
+#pragma unroll
+            for (int e = 1; e < V; ++e) top = fmaxf(top, v[e]);
+            if (!(top <= s.top)) {                        // (or all of them NaN)
+                s.sum *= soft_scale(s.top, top);
+                s.top = top;
+            }
+            const float ref = s.top == -INFINITY ? 0.0f : s.top;
+            const f2 scale = f2_same(kLog2e), shift = f2_same(-ref);
+            f2 sum = 0;
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                float x, y;
+                f2_get(f2_mul(f2_add(f2_of(v[e], v[e + 1]), shift), scale), x, y);
+                sum = f2_add(sum, f2_of(fast_exp2(x), fast_exp2(y)));
+            }
+            float x, y;
+            f2_get(sum, x, y);
+            s.sum += x + y;
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+        s = soft_join(s, Soft{__shfl_xor_sync(0xFFFFFFFFu, s.top, d), __shfl_xor_sync(0xFFFFFFFFu, s.sum, d)});
+    if (a.warps > 1) {
+        if (lane == 0) places[warp] = s;
+        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(size) : "memory");
+        if (me != 0) return;
+        s = places[warp];
+        for (uint32_t j = 1; j < a.warps; ++j) s = soft_join(s, places[warp + j]);
+    } else if (me != 0) {
+        return;
+    }
+    const float log_sum = logf(s.sum);
+    const int32_t t = a.target[k * a.tw + (int64_t)row];
+    a.lse[k * a.sw + (int64_t)row] = s.top == -INFINITY && s.sum == 0.0f ? -INFINITY : s.top + log_sum;
+    float loss = 0.0f;
+    if (t >= 0) loss = (uint32_t)t < a.vocab ? (s.top - to_f(z[t])) + log_sum : __uint_as_float(0x7FFFFFFFu);
+    if (a.loss) a.loss[k * a.lw + (int64_t)row] = loss;
+}
+
+// dz = (e^(z - lse) - [target]) dloss of a part of a row: `pieces` of 16 bytes a lane, from where the row's copy in memory
+// lets it.  Rows of z and dz that start alike are walked by aligned pieces, the ragged ends one value at a time; others at
+// any address.
+constexpr uint32_t kLossPieces = 8;                       // of a lane
+
+struct LossGrid { Divisor parts; uint32_t units; };       // parts of a row; parts of all rows of a worker
+
+template <typename T>
+__global__ void __launch_bounds__(256) loss_backward_kernel(const __grid_constant__ LossArgs a, const __grid_constant__ LossGrid g)
+{
+    constexpr int V = 16 / (int)sizeof(T), P = 4;
+    const uint32_t warp = threadIdx.x >> 5, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
+    const uint32_t size = a.warps * 32, me = threadIdx.x - team * size;
+    const int64_t k = blockIdx.y;
+    let_next_start();
+    wait_for_previous();
+    const uint32_t unit = blockIdx.x * teams + team;
+    if (unit >= g.units) return;
+    const uint32_t row = g.parts.of(unit), part = unit - row * g.parts.d;
+    const T* z = static_cast<const T*>(a.z) + k * a.zw + (int64_t)row * a.zr;
+    T* dz = static_cast<T*>(a.dz) + k * a.dw + (int64_t)row * a.dr;
+    const int32_t t = a.target[k * a.tw + row];
+    const bool bad = t >= 0 && (uint32_t)t >= a.vocab;
+    const float d = bad ? __uint_as_float(0x7FFFFFFFu) : t < 0 ? 0.0f : a.dloss[k * a.gw + row];
+    const float lse = a.lse[k * a.sw + row];
+    auto gradient = [&](uint4& q, int64_t c) {            // the piece whose first value is the row's c-th
+        float v[V];
+        floats_of<T>(q, v);
+        if (t < 0) {
+            q = make_uint4(0, 0, 0, 0);
+            return;
+        }
+        if constexpr (sizeof(T) == 2) {
+            const f2 shift = f2_same(-lse * kLog2e), scale = f2_same(kLog2e), dd = f2_same(d);
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float x, y;
+                f2_get(f2_fma(f2_of(v[2 * i], v[2 * i + 1]), scale, shift), x, y);
+                x = fast_exp2(x); y = fast_exp2(y);
+                if (c + 2 * i == t) x -= 1.0f;
+                if (c + 2 * i + 1 == t) y -= 1.0f;
+                w[i] = f2_narrow(f2_mul(f2_of(x, y), dd));
+            }
+            q = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = expf(v[i] - lse);
+                if (c + i == t) v[i] -= 1.0f;
+                v[i] *= d;
+            }
+            q = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        }
+    };
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(z) & 15) / (uint32_t)sizeof(T);
+    const bool alike = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+    const uint32_t begin = part * size * kLossPieces;
+    if (alike) {
+        const uint32_t end = off + a.vocab, pieces = (end + V - 1) / V, last = min(pieces, begin + size * kLossPieces);
+        const uint4* from = reinterpret_cast<const uint4*>(z - off);
+        uint4* to = reinterpret_cast<uint4*>(dz - off);
+        for (uint32_t i = begin + me; i < last; i += size * P) {
+            uint4 q[P];
+#pragma unroll
+            for (int j = 0; j < P; ++j) if (i + j * size < last) q[j] = from[i + j * size];
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const uint32_t at = i + j * size;
+                if (at >= last) break;
+                gradient(q[j], (int64_t)at * V - off);
+                if (at * V >= off && (at + 1) * V <= end) {
+                    to[at] = q[j];
+                } else {                                  // the neighbours' values in the piece stay
+                    const uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const uint32_t c = at * V + e;
+                        if (c < off || c >= end) continue;
+                        if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(to)[c] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+                        else reinterpret_cast<uint32_t*>(to)[c] = w[e];
+                    }
+                }
+            }
+        }
+    } else {
+        const uint32_t pieces = (a.vocab + V - 1) / V, last = min(pieces, begin + size * kLossPieces);
+        for (uint32_t i = begin + me; i < last; i += size) {
+            const uint32_t n = min(a.vocab - i * V, (uint32_t)V) * (uint32_t)sizeof(T);
+            uint4 q = get16(reinterpret_cast<const unsigned char*>(z + (uint64_t)i * V), n);
+            gradient(q, (int64_t)i * V);
+            put16<(int)sizeof(T)>(reinterpret_cast<unsigned char*>(dz + (uint64_t)i * V), n, q);
+        }
+    }
+}
+
+}  // namespace block
+}  // namespace palsgd

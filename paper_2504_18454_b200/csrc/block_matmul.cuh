@@ -29,7 +29,7 @@
 namespace palsgd {
 namespace block {
 
-enum { MAT_PLAIN = 0, MAT_GATED = 1, MAT_HIDDEN = 2 };
+enum { MAT_PLAIN = 0, MAT_GATED = 1, MAT_HIDDEN = 2, MAT_LINEAR = 3 };
 
 constexpr uint32_t kTileM = 256, kTileN = 256, kTileK = 64;
 constexpr uint32_t kOperandBytes = 128 * kTileK * 2;                    // a CTA's half of an operand's tile
@@ -45,8 +45,8 @@ struct MatShape {
     static constexpr bool kWide = sizeof(T) == 4;
     static constexpr uint32_t kEpilogue = 16;
     static constexpr uint32_t kThreads = 128 + 32 * kEpilogue;
-    static constexpr uint32_t kBlocks = MODE == MAT_HIDDEN ? 2 : 1;       // a warp's
-    static constexpr uint32_t kStages = MODE == MAT_HIDDEN ? 5 : 6;
+    static constexpr uint32_t kBlocks = MODE == MAT_HIDDEN || MODE == MAT_LINEAR ? 2 : 1;       // a warp's
+    static constexpr uint32_t kStages = kBlocks == 2 ? 5 : 6;
     static constexpr uint32_t kSmem = kStages * kStageBytes + kEpilogue * kBlocks * 2048 + kBarrierBytes + 1024;   // 1024: to start on a swizzle atom
     static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
@@ -70,7 +70,7 @@ struct alignas(64) MatProblem {
     uint32_t splits;              // shares of the inner axis (plain): above one, out[0] takes each share's binary32 sums
     uint8_t  n_seg, a_parts, b_parts, a_mn, b_mn;
     uint8_t  a_one[2], b_one[2];  // all workers read one matrix
-    MatOut   out[3];              // plain: the product; gate/up: h; hidden: dg, du, h
+    MatOut   out[3];              // plain: the product; gate/up: h; hidden: dg, du, h; linear: y
 };
 
 struct MatLaunch {
@@ -79,6 +79,7 @@ struct MatLaunch {
     int      save;
     MatOut   gate, up;            // saved (gate/up pass) or read (hidden pass)
     MatOut   gate_e, up_e;
+    MatOut   bias, residual;      // linear (gate: what is saved); p may be NULL
     CUtensorMap store[3];         // bfloat16: h (gate/up), or dg, du, h (hidden), as the copy engine writes blocks of them
     unsigned int* gave_up;
 };
@@ -644,6 +645,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 block_in<E, 4>(b1, static_cast<const unsigned char*>(a.up.p) + E * uo, E * a.up.r, rows, cols, a.up.wide, lane);
             }
         };
+        // linear: the residual of block c of a tile into the warp's second block
+        auto fetch_residual = [&](const Tile& tl, uint32_t c) {
+            const uint32_t m = tl.m0 + rank * 128 + quad * 32, n = tl.n0 + part * kMine + c * kCols;
+            const uint32_t M = tl.p->M, N = tl.p->N;
+            const int64_t at = (int64_t)tl.worker * a.residual.w + (int64_t)m * a.residual.r + n;
+            block_in<E, 4>(b1, static_cast<const unsigned char*>(a.residual.p) + E * at, E * a.residual.r, m < M ? min(M - m, 32u) : 0, n < N ? N - n : 0, a.residual.wide, lane);
+        };
+        if constexpr (MODE == MAT_LINEAR) if (a.residual.p) fetch_residual(tile_at<MODE>(a, Order(a, pair, pairs).now()), 0);
         if constexpr (MODE == MAT_HIDDEN) fetch(tile_at<MODE>(a, Order(a, pair, pairs).now()), 0);
         for (Order o(a, pair, pairs); o.now() < a.tiles; o.next()) {
             const Tile tl = tile_at<MODE>(a, o.now());
@@ -702,6 +711,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     }
                 }
             }
+            // linear: z = the sum + bias of eight columns, from the tile's column j on
+            auto linear_z = [&](uint32_t j, f2 (&z)[4]) {
+                float v[8];
+                tmem_load8(src + j, v);
+                f2 b[4] = {0, 0, 0, 0};
+                const uint32_t n = tl.n0 + part * kMine + j;
+                if (a.bias.p && n < p.N) row8_load(static_cast<const T*>(a.bias.p) + w * a.bias.w + n, p.N - n, a.bias.wide, b);
+                tmem_load_wait();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = f2_add(f2_of(v[2 * i], v[2 * i + 1]), b[i]);
+            };
+            float inv[2] = {0.0f, 0.0f};                                  // 8 bits: one over the steps of the warp's two groups
+            if constexpr (MODE == MAT_LINEAR) {
+                if (eight) {
+#pragma unroll
+                    for (uint32_t g = 0; g < 2; ++g) {
+                        const uint32_t n = tl.n0 + part * kMine + 32 * g;
+                        float top = 0.0f;
+#pragma unroll 1
+                        for (uint32_t j = 0; j < 32; j += 8) {
+                            f2 z[4];
+                            linear_z(32 * g + j, z);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float x, y;
+                                f2_get(z[i], x, y);
+                                top = act8_max(act8_max(top, x), y);
+                            }
+                        }
+                        const uint32_t e = act8_exponent(top);
+                        inv[g] = act8_inverse(e);
+                        if (lane < rows && n < p.N) static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * a.gate_e.r + n / 32] = (uint8_t)e;
+                    }
+                }
+            }
 #pragma unroll 1
             for (uint32_t c = 0; c < kChunks; ++c) {
                 const uint32_t from = src + c * kCols, n = tl.n0 + part * kMine + c * kCols;
@@ -740,6 +784,54 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     __syncwarp();
                     const int64_t to = E == 4 && p.splits > 1 ? at + (int64_t)tl.split * p.out[0].part : at;
                     block_out<64, E>(b0, static_cast<unsigned char*>(p.out[0].p) + E * to, E * p.out[0].r, rows, room, p.out[0].wide, lane);
+                    __syncwarp();
+                } else if constexpr (MODE == MAT_LINEAR) {
+                    // what is saved, then y, pass through one block (the sums are read again for each); the residual comes
+                    // into the other one while the products of the tile, or the work on the block before, still run
+                    if (a.save != PALSGD_SAVE_NONE) {
+#pragma unroll 1
+                        for (uint32_t j = 0; j < kOcts; ++j) {
+                            f2 z[4];
+                            linear_z(c * kCols + 8 * j, z);
+                            if (eight) {
+                                float v[8];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) f2_get(z[i], v[2 * i], v[2 * i + 1]);
+                                row_put_act8<T>(b0, lane, j, c * kCols >= 32 ? inv[1] : inv[0], v);
+                            } else {
+                                row_put<T>(b0, lane, j, z);
+                            }
+                        }
+                        __syncwarp();
+                        const int64_t to = w * a.gate.w + (int64_t)m * a.gate.r + n;
+                        if (eight) block_out<kCols, 1>(b0, static_cast<unsigned char*>(a.gate.p) + to, a.gate.r, rows, cols, a.gate.wide, lane);
+                        else block_out<64, E>(b0, static_cast<unsigned char*>(a.gate.p) + E * to, E * a.gate.r, rows, cols, a.gate.wide, lane);
+                        __syncwarp();
+                    }
+                    if (a.residual.p) {
+                        block_wait();
+                        __syncwarp();
+                    }
+#pragma unroll 1
+                    for (uint32_t j = 0; j < kOcts; ++j) {
+                        f2 z[4], r[4], unused;
+                        linear_z(c * kCols + 8 * j, z);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z[i] = act_pair<T, ACT, false>(z[i], unused);
+                        if (a.residual.p) {
+                            row_get<T>(b1, lane, j, r);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) z[i] = f2_add(z[i], r[i]);
+                        }
+                        row_put<T>(b0, lane, j, z);
+                    }
+                    if (c + 1 == kChunks) acc_read();
+                    __syncwarp();
+                    if (a.residual.p) {
+                        if (c + 1 < kChunks) fetch_residual(tl, c + 1);
+                        else if (o.then() < a.tiles) fetch_residual(tile_at<MODE>(a, o.then()), 0);
+                    }
+                    block_out<64, E>(b0, static_cast<unsigned char*>(p.out[0].p) + E * at, E * p.out[0].r, rows, cols, p.out[0].wide, lane);
                     __syncwarp();
                 } else if constexpr (MODE == MAT_GATED) {
                     // gate, up and h pass through one block, one after another (tensor memory is read again for each); h goes
@@ -879,8 +971,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 }
             }
         }
-        if constexpr (MODE == MAT_HIDDEN) block_wait();
-        if (E == 2 && MODE != MAT_PLAIN && one) tma_store_done();
+        if constexpr (MODE == MAT_HIDDEN || MODE == MAT_LINEAR) block_wait();
+        if (E == 2 && (MODE == MAT_GATED || MODE == MAT_HIDDEN) && one) tma_store_done();
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

@@ -1,0 +1,394 @@
+// Row kernels of the block operators: layer norm forward and backward.
+//
+// A team of W warps has a row at a time in its registers: mean, then the mean square around it (two passes over registers: a
+// row whose mean is large against its spread loses nothing), then the result, in one pass over memory.  A team walks rows
+// with the next one under way; its columns of w (and b), and in the backward pass its sums of dw and db, stay in registers
+// over all of its rows.  The sums go to one row of the workspace for each CTA and are joined in a fixed order.
+// Bound by memory: every byte is moved once.
+#pragma once
+#include "block_common.cuh"
+
+namespace palsgd {
+namespace block {
+
+struct NormArgs {
+    const void *x, *r;            // forward: input and what is added to it (may be NULL); backward: the sum, and the gradient past the norm
+    const void *w, *b, *dy;
+    void *y, *total;              // backward: y is dx
+    float *mean, *rstd;           // forward: may be NULL
+    float* part;                  // backward: [K][CTAs][2][width]
+    int64_t xw, xr, rw, rr, dw, dr, yw, yr, tw, tr, ww, bw, mw, sw;      // worker and row strides, elements
+    uint64_t rows;
+    uint32_t width, warps;        // warps of a team
+    float    eps;
+};
+
+// A piece is 16 bytes of a row, V values.
+template <typename T> constexpr int kPieceValues = 16 / (int)sizeof(T);
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ uint4 piece_load(const T* row, uint32_t c, uint32_t width)
+{
+    if constexpr (WIDE) {
+        return c < width ? __ldg(reinterpret_cast<const uint4*>(row + c)) : make_uint4(0, 0, 0, 0);
+    } else {
+        const uint32_t n = c < width ? min(width - c, (uint32_t)kPieceValues<T>) : 0;
+        return get16(reinterpret_cast<const unsigned char*>(row + c), n * (uint32_t)sizeof(T));
+    }
+}
+
+// Pieces on their way: every lane copies its own pieces of the rows to come into places of its own in shared memory,
+// asynchronously, and reads them there: no barrier, and registers for one row only.  (The next row in registers took 200 of
+// them a lane in the backward pass, which left eight warps an SM and 24 KB under way.)  Rows at any address come as the
+// aligned 16-byte blocks that hold a byte of them: a lane's piece lies in its block and the next lane's.
+template <typename T, bool WIDE>
+struct Ring {
+    static constexpr uint32_t kPlaces = WIDE ? 32 : 33;   // of 16 bytes: a warp's for one piece a lane
+    uint32_t base, step;
+    __device__ __forceinline__ explicit Ring(const void* raw)
+    {
+        const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        base = (uint32_t)__cvta_generic_to_shared(raw) + (warp * kPlaces + lane) * 16;
+        step = (blockDim.x >> 5) * kPlaces * 16;
+    }
+    static __device__ __forceinline__ void copy(uint32_t to, const void* from, bool on)
+    {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16u : 0u) : "memory");
+    }
+    // piece c of a row into place i
+    __device__ __forceinline__ void fetch(uint32_t i, const T* row, uint32_t c, uint32_t width) const
+    {
+        const uint32_t to = base + i * step;
+        if constexpr (WIDE) {
+            copy(to, row + (c < width ? c : 0), c < width);
+        } else {
+            const uintptr_t start = reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15, end = reinterpret_cast<uintptr_t>(row + width);
+            const uintptr_t block = reinterpret_cast<uintptr_t>(row + c) & ~(uintptr_t)15;
+            copy(to, reinterpret_cast<const void*>(block < end ? block : start), block < end);
+            if ((threadIdx.x & 31) == 31) copy(to + 16, reinterpret_cast<const void*>(block + 16 < end ? block + 16 : start), block + 16 < end);
+        }
+    }
+    __device__ __forceinline__ uint4 get(uint32_t i, const T* row, uint32_t c, uint32_t width) const
+    {
+        uint4 v;
+        lds(base + i * step, v);
+        if constexpr (!WIDE) {
+            uint4 u;
+            lds(base + i * step + 16, u);
+            const uint32_t n = c < width ? min(width - c, (uint32_t)kPieceValues<T>) * (uint32_t)sizeof(T) : 0;
+            v = shift16(v, u, (uint32_t)reinterpret_cast<uintptr_t>(row + c) & 15, n);
+        }
+        return v;
+    }
+    static __device__ __forceinline__ void lds(uint32_t at, uint4& v)
+    {
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    }
+    static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    // All but the last AHEAD rows are there.  (A lane's copies are complete for it alone: the others look behind the barrier.)
+    template <int AHEAD>
+    static __device__ __forceinline__ void wait()
+    {
+        asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+        if constexpr (!WIDE) __syncwarp();
+    }
+    // Every lane has read what the next copies write over.
+    static __device__ __forceinline__ void left() { if constexpr (!WIDE) __syncwarp(); }
+};
+// Rows under way: as many as find room beside the SM's other CTAs, four at most.
+template <typename T, bool WIDE>
+constexpr __host__ __device__ uint32_t norm_stage_bytes(int pieces, int warps) { return (uint32_t)pieces * warps * Ring<T, WIDE>::kPlaces * 16; }
+template <typename T, bool WIDE>
+constexpr __host__ __device__ uint32_t norm_stages(int pieces, int warps, int ctas)
+{
+    const uint32_t n = (227 * 1024 / ctas - 2048) / norm_stage_bytes<T, WIDE>(pieces, warps);
+    return n > 4 ? 4 : n;
+}
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ void piece_store(T* row, uint32_t c, uint32_t width, const uint4& v)
+{
+    if (c >= width) return;
+    if constexpr (WIDE) *reinterpret_cast<uint4*>(row + c) = v;
+    else put16<(int)sizeof(T)>(reinterpret_cast<unsigned char*>(row + c), min(width - c, (uint32_t)kPieceValues<T>) * (uint32_t)sizeof(T), v);
+}
+// A piece as V / 2 pairs of floats, and back
+template <typename T>
+__device__ __forceinline__ void piece_wide(const uint4& p, f2 (&v)[kPieceValues<T> / 2])
+{
+    if constexpr (sizeof(T) == 2) {
+        v[0] = f2_wide(p.x); v[1] = f2_wide(p.y); v[2] = f2_wide(p.z); v[3] = f2_wide(p.w);
+    } else {
+        v[0] = f2_of(__uint_as_float(p.x), __uint_as_float(p.y)); v[1] = f2_of(__uint_as_float(p.z), __uint_as_float(p.w));
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint4 piece_narrow(const f2 (&v)[kPieceValues<T> / 2])
+{
+    if constexpr (sizeof(T) == 2) {
+        return make_uint4(f2_narrow(v[0]), f2_narrow(v[1]), f2_narrow(v[2]), f2_narrow(v[3]));
+    } else {
+        float a, b, c, d;
+        f2_get(v[0], a, b); f2_get(v[1], c, d);
+        return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+    }
+}
+__device__ __forceinline__ float f2_total(f2 v) { float a, b; f2_get(v, a, b); return a + b; }
+// The pair at column c with what lies behind the row's end as zero
+template <bool WIDE>
+__device__ __forceinline__ f2 inside(f2 v, uint32_t c, uint32_t width)
+{
+    if (c + 1 < width) return v;
+    if (WIDE || c >= width) return 0;
+    float a, b;
+    f2_get(v, a, b);
+    return f2_of(a, 0.0f);
+}
+
+constexpr uint32_t kNormMostWarps = 32;                                 // of a team
+
+// Sums of N values over a team, the same bits in all of its lanes.  `turn` alternates between calls: the places of one call
+// are read while the next one's are written.
+template <int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], uint32_t warps, uint32_t team, float* places, uint32_t& turn)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+    if (warps == 1) return;
+    const uint32_t warp = threadIdx.x >> 5, first = team * warps;
+    float* p = places + turn * (2 * kNormMostWarps);
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i * kNormMostWarps + warp] = v[i];
+    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float s = p[i * kNormMostWarps + first];
+        for (uint32_t j = 1; j < warps; ++j) s += p[i * kNormMostWarps + first + j];
+        v[i] = s;
+    }
+}
+
+// WARPS: of a CTA, 8 or as many as one team needs beyond that.  N: pieces a lane.  ADD: there is an addend (forward), a
+// gradient that comes past the norm (backward).
+template <typename T, int N, bool WIDE, bool ADD, int WARPS, int CTAS>
+__global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __grid_constant__ NormArgs a)
+{
+    constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 2 * N : N, S = norm_stages<T, WIDE>(Q, WARPS, CTAS);    // Q: pieces of a lane for a row
+    __shared__ float places[4 * kNormMostWarps];
+    extern __shared__ __align__(16) unsigned char ring_raw[];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
+    const uint32_t first = ((warp - team * a.warps) * 32 + lane) * V, step = a.warps * 32 * V, width = a.width;
+    const Ring<T, WIDE> ring(ring_raw);
+    const int64_t k = blockIdx.y;
+    const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
+    const T *w = static_cast<const T*>(a.w) + k * a.ww, *b = static_cast<const T*>(a.b) + k * a.bw;
+    const uint64_t rows_step = (uint64_t)gridDim.x * teams;
+    uint64_t row = (uint64_t)blockIdx.x * teams + team, ahead = row;
+    uint32_t turn = 0, put = 0, got = 0;
+
+    let_next_start();
+    wait_for_previous();
+    auto fetch = [&]() {
+        if (ahead < a.rows) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                ring.fetch(put * Q + i, x + (int64_t)ahead * a.xr, first + i * step, width);
+                if constexpr (ADD) ring.fetch(put * Q + N + i, r + (int64_t)ahead * a.rr, first + i * step, width);
+            }
+            ahead += rows_step;
+        }
+        ring.commit();
+        put = put + 1 == S ? 0 : put + 1;
+    };
+#pragma unroll 1
+    for (int i = 0; i < S - 1; ++i) fetch();
+    uint4 wp[N], bp[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        wp[i] = piece_load<T, WIDE>(w, first + i * step, width);
+        bp[i] = piece_load<T, WIDE>(b, first + i * step, width);
+    }
+    for (; row < a.rows; row += rows_step) {
+        ring.left();
+        fetch();                                          // into the place that the row before this one has left
+        ring.template wait<S - 1>();
+        f2 h[N][H], sum = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            piece_wide<T>(ring.get(got * Q + i, x + (int64_t)row * a.xr, first + i * step, width), h[i]);
+            if constexpr (ADD) {
+                f2 t[H];
+                piece_wide<T>(ring.get(got * Q + N + i, r + (int64_t)row * a.rr, first + i * step, width), t);
+#pragma unroll
+                for (int j = 0; j < H; ++j) h[i][j] = f2_add(h[i][j], t[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < H; ++j) sum = f2_add(sum, h[i][j]);      // (behind the row's end: zeros)
+        }
+        got = got + 1 == S ? 0 : got + 1;
+        if constexpr (ADD) {
+            T* total = static_cast<T*>(a.total) + k * a.tw + (int64_t)row * a.tr;
+#pragma unroll
+            for (int i = 0; i < N; ++i) piece_store<T, WIDE>(total, first + i * step, width, piece_narrow<T>(h[i]));
+        }
+        float s[1] = {f2_total(sum)};
+        team_sum<1>(s, a.warps, team, places, turn);
+        const float mean = s[0] / (float)width;
+        sum = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                h[i][j] = f2_add(h[i][j], f2_same(-mean));
+                const f2 c = inside<WIDE>(h[i][j], first + i * step + 2 * j, width);
+                sum = f2_fma(c, c, sum);
+            }
+        s[0] = f2_total(sum);
+        team_sum<1>(s, a.warps, team, places, turn);
+        const float rstd = 1.0f / sqrtf(s[0] / (float)width + a.eps);
+        T* y = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            f2 wv[H], bv[H];
+            piece_wide<T>(wp[i], wv);
+            piece_wide<T>(bp[i], bv);
+#pragma unroll
+            for (int j = 0; j < H; ++j) bv[j] = f2_fma(f2_mul(h[i][j], f2_same(rstd)), wv[j], bv[j]);
+            piece_store<T, WIDE>(y, first + i * step, width, piece_narrow<T>(bv));
+        }
+        if (first == 0) {
+            if (a.mean) a.mean[k * a.mw + (int64_t)row] = mean;
+            if (a.rstd) a.rstd[k * a.sw + (int64_t)row] = rstd;
+        }
+    }
+}
+
+// dx = rstd (g - mean g - xh mean(g xh)) (+ what comes past the norm), g = dy w, xh = (x - mean) rstd; the CTA's sums of
+// dy xh and dy go to its row of `part`.
+template <typename T, int N, bool WIDE, bool ADD, int WARPS, int CTAS>
+__global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a)
+{
+    constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 3 * N : 2 * N, S = norm_stages<T, WIDE>(Q, WARPS, CTAS);
+    __shared__ float places[4 * kNormMostWarps];
+    extern __shared__ __align__(16) unsigned char ring_raw[];            // the ring; at the end [2][width] floats, where a CTA has more than one team
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
+    const uint32_t first = ((warp - team * a.warps) * 32 + lane) * V, step = a.warps * 32 * V, width = a.width;
+    const Ring<T, WIDE> ring(ring_raw);
+    const int64_t k = blockIdx.y;
+    const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
+    const T *w = static_cast<const T*>(a.w) + k * a.ww, *dy = static_cast<const T*>(a.dy) + k * a.dw;
+    const uint64_t rows_step = (uint64_t)gridDim.x * teams;
+    uint64_t row = (uint64_t)blockIdx.x * teams + team, ahead = row;
+    uint32_t turn = 0, put = 0, got = 0;
+
+    let_next_start();
+    wait_for_previous();
+    auto fetch = [&]() {
+        if (ahead < a.rows) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                ring.fetch(put * Q + i, x + (int64_t)ahead * a.xr, first + i * step, width);
+                ring.fetch(put * Q + N + i, dy + (int64_t)ahead * a.dr, first + i * step, width);
+                if constexpr (ADD) ring.fetch(put * Q + 2 * N + i, r + (int64_t)ahead * a.rr, first + i * step, width);
+            }
+            ahead += rows_step;
+        }
+        ring.commit();
+        put = put + 1 == S ? 0 : put + 1;
+    };
+#pragma unroll 1
+    for (int i = 0; i < S - 1; ++i) fetch();
+    uint4 wp[N];
+    f2 dw[N][H], db[N][H];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        wp[i] = piece_load<T, WIDE>(w, first + i * step, width);
+#pragma unroll
+        for (int j = 0; j < H; ++j) dw[i][j] = db[i][j] = 0;
+    }
+    float mean = 0.0f, rstd = 0.0f;
+    auto stats = [&](uint64_t at) {
+        if (at >= a.rows) return;
+        mean = __ldg(a.mean + k * a.mw + (int64_t)at);
+        rstd = __ldg(a.rstd + k * a.sw + (int64_t)at);
+    };
+    stats(row);
+    for (; row < a.rows; row += rows_step) {
+        const float rs = rstd, mean_now = mean;
+        stats(row + rows_step);
+        ring.left();
+        fetch();
+        ring.template wait<S - 1>();
+        f2 xh[N][H], g[N][H], sg = 0, sx = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            f2 d[H], wv[H];
+            piece_wide<T>(ring.get(got * Q + i, x + (int64_t)row * a.xr, first + i * step, width), xh[i]);
+            piece_wide<T>(ring.get(got * Q + N + i, dy + (int64_t)row * a.dr, first + i * step, width), d);
+            piece_wide<T>(wp[i], wv);
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                // (behind the row's end d is zero: xh must be finite there)
+                xh[i][j] = inside<WIDE>(f2_mul(f2_add(xh[i][j], f2_same(-mean_now)), f2_same(rs)), first + i * step + 2 * j, width);
+                g[i][j] = f2_mul(d[j], wv[j]);
+                dw[i][j] = f2_fma(d[j], xh[i][j], dw[i][j]);
+                db[i][j] = f2_add(db[i][j], d[j]);
+                sg = f2_add(sg, g[i][j]);
+                sx = f2_fma(g[i][j], xh[i][j], sx);
+            }
+        }
+        float s[2] = {f2_total(sg), f2_total(sx)};
+        team_sum<2>(s, a.warps, team, places, turn);
+        const f2 mg = f2_same(-s[0] / (float)width), mx = f2_same(-s[1] / (float)width);
+        T* dx = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            f2 t[H];
+            if constexpr (ADD) piece_wide<T>(ring.get(got * Q + 2 * N + i, r + (int64_t)row * a.rr, first + i * step, width), t);
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                const f2 v = f2_add(f2_fma(xh[i][j], mx, g[i][j]), mg);
+                t[j] = ADD ? f2_fma(v, f2_same(rs), t[j]) : f2_mul(v, f2_same(rs));
+            }
+            piece_store<T, WIDE>(dx, first + i * step, width, piece_narrow<T>(t));
+        }
+        got = got + 1 == S ? 0 : got + 1;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();                                      // the ring's place is free
+    float* const joined = reinterpret_cast<float*>(ring_raw);
+    // the teams' sums, one team after another
+    float* part = a.part + ((uint64_t)k * gridDim.x + blockIdx.x) * 2 * width;
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                const uint32_t c = first + i * step + 2 * j;
+                float u, v, p, q;
+                f2_get(dw[i][j], u, v);
+                f2_get(db[i][j], p, q);
+                if (c < width) f(c, u, p);
+                if (c + 1 < width) f(c + 1, v, q);
+            }
+    };
+    if (teams == 1) {
+        each([&](uint32_t c, float u, float p) { part[c] = u; part[width + c] = p; });
+        return;
+    }
+    for (uint32_t t = 0; t < teams; ++t) {
+        if (t == team) {
+            if (t == 0) each([&](uint32_t c, float u, float p) { joined[c] = u; joined[width + c] = p; });
+            else each([&](uint32_t c, float u, float p) { joined[c] += u; joined[width + c] += p; });
+        }
+        __syncthreads();
+    }
+    for (uint32_t c = threadIdx.x; c < 2 * width; c += blockDim.x) part[c] = joined[c];
+}
+
+}  // namespace block
+}  // namespace palsgd

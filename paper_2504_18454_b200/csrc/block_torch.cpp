@@ -25,6 +25,12 @@ struct Library {
     decltype(&palsgd_ffn_backward) ffn_backward;
     decltype(&palsgd_qk_norm_rope_forward) qk_forward;
     decltype(&palsgd_qk_norm_rope_backward) qk_backward;
+    decltype(&palsgd_linear_forward) linear_forward;
+    decltype(&palsgd_linear_backward) linear_backward;
+    decltype(&palsgd_layer_norm_forward) norm_forward;
+    decltype(&palsgd_layer_norm_backward) norm_backward;
+    decltype(&palsgd_cross_entropy_forward) loss_forward;
+    decltype(&palsgd_cross_entropy_backward) loss_backward;
     decltype(&palsgd_last_cuda_error) last_cuda_error;
 } g_lib;
 PyObject* g_error = nullptr;
@@ -420,6 +426,257 @@ PyObject* qk_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     });
 }
 
+// ---------------------------------------------------------------------------------------------- linear
+
+uint32_t workers(int64_t K) { return (uint32_t)std::min<int64_t>(K, 65); }       // (more than there may be are as good as 65)
+const palsgd_mat* at(const std::optional<at::Tensor>& t, const palsgd_mat& m) { return t ? &m : nullptr; }
+palsgd_mat mat(const std::optional<at::Tensor>& t) { return t ? mat(*t) : palsgd_mat{}; }
+
+struct Linear {
+    int64_t K, M, D, N;
+    at::ScalarType type;
+    at::Device d;
+    palsgd_linear_shape shape;
+    palsgd_mat w;
+};
+
+// x (its last axis: d_in) or dy (d_out), and the weights
+Linear linear(const char* where, const at::Tensor& t, const char* name, bool back, PyObject* weight, int64_t act, int64_t save)
+{
+    const at::Device d = on_cuda(t, where, name, 3);
+    const at::Tensor& w = tensor(weight, where, "w");
+    Linear f{t.size(0), t.size(1), 0, 0, t.scalar_type(), d, {}, {}};
+    const int prec = precision(f.type, where, name);
+    fit(t, where, name, t.sizes(), f.type, d);
+    f.D = back ? (w.dim() == 3 ? w.size(2) : 0) : t.size(2);
+    f.N = back ? t.size(2) : (w.dim() == 3 ? w.size(1) : 0);
+    fit(w, where, "w", {f.K, f.N, f.D}, f.type, d);
+    f.w = mat(w);
+    f.shape = palsgd_linear_shape{workers(f.K), prec, (int32_t)act, (int32_t)save, (uint64_t)f.M, (uint64_t)f.D, (uint64_t)f.N};
+    return f;
+}
+
+// (x, w, bias, residual, activation, save, out, pre, pre_e, workspace, stream) -> (y, pre, pre_e)
+PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 11, [&] {
+        const char* where = "palsgd_linear_forward";
+        const at::Tensor& x = tensor(a[0], where, "x");
+        const Linear f = linear(where, x, "x", false, a[1], integer(a[4]), integer(a[5]));
+        const int64_t ys[3] = {f.K, f.M, f.N}, es[3] = {f.K, f.M, groups(f.N)};
+        const std::optional<at::Tensor> bias = maybe(a[2], where, "bias"), residual = maybe(a[3], where, "residual");
+        if (bias) fit(*bias, where, "bias", {f.K, f.N}, f.type, f.d);
+        if (residual) fit(*residual, where, "residual", ys, f.type, f.d);
+        const On on(f.d, a[10]);
+        const at::Tensor y = a[6] == Py_None ? fresh(ys, f.type, f.d) : tensor(a[6], where, "out");
+        fit(y, where, "out", ys, f.type, f.d);
+        std::optional<at::Tensor> pre, pre_e;
+        const bool eight = f.shape.save == PALSGD_SAVE_8BIT;
+        if (f.shape.save == PALSGD_SAVE_FULL || eight) {
+            const at::ScalarType type = eight ? at::kChar : f.type;
+            pre = a[7] == Py_None ? fresh(ys, type, f.d) : tensor(a[7], where, eight ? "saved.q" : "saved");
+            fit(*pre, where, eight ? "saved.q" : "saved", ys, type, f.d);
+        }
+        if (eight) {
+            pre_e = a[8] == Py_None ? fresh(es, at::kByte, f.d) : tensor(a[8], where, "saved.exponent");
+            fit(*pre_e, where, "saved.exponent", es, at::kByte, f.d);
+        }
+        const palsgd_mat mx = mat(x), my = mat(y), mb = mat(bias), mr = mat(residual), mp = mat(pre), me = mat(pre_e);
+        with_workspace([&](void* ws, size_t* n) {
+            return g_lib.linear_forward(&f.shape, &mx, &f.w, at(bias, mb), at(residual, mr), &my, at(pre, mp), at(pre_e, me), ws, n, on.raw);
+        }, a[9], f.d, where);
+        written(y);
+        if (pre) written(*pre);
+        if (pre_e) written(*pre_e);
+        return pack(std::optional<at::Tensor>(y), pre, pre_e);
+    });
+}
+
+// (dy, x, x_e, w, pre, pre_e, activation, save, need_dx, need_db, dx, dw, db, workspace, stream) -> (dx, dw, db)
+PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 15, [&] {
+        const char* where = "palsgd_linear_backward";
+        const at::Tensor& dy = tensor(a[0], where, "dy");
+        const Linear f = linear(where, dy, "dy", true, a[3], integer(a[6]), integer(a[7]));
+        const at::Tensor& x = tensor(a[1], where, "x");
+        const std::optional<at::Tensor> xe = maybe(a[2], where, "x.exponent"), pre = maybe(a[4], where, "saved"), pre_e = maybe(a[5], where, "saved.exponent");
+        const int64_t xs[3] = {f.K, f.M, f.D}, ys[3] = {f.K, f.M, f.N};
+        const bool eight = f.shape.save == PALSGD_SAVE_8BIT;
+        fit(x, where, xe ? "x.q" : "x", xs, xe ? at::kChar : f.type, f.d);
+        if (xe) fit(*xe, where, "x.exponent", {f.K, f.M, groups(f.D)}, at::kByte, f.d);
+        if (pre) fit(*pre, where, eight ? "saved.q" : "saved", ys, eight ? at::kChar : f.type, f.d);
+        if (pre_e) fit(*pre_e, where, "saved.exponent", {f.K, f.M, groups(f.N)}, at::kByte, f.d);
+        const On on(f.d, a[14]);
+        static const char* names[3] = {"dx", "dw", "db"};
+        const int64_t ws3[3] = {f.K, f.N, f.D}, bs[2] = {f.K, f.N};
+        const at::IntArrayRef want[3] = {xs, ws3, bs};
+        const bool need[3] = {integer(a[8]) != 0, true, integer(a[9]) != 0};
+        std::optional<at::Tensor> out[3];
+        palsgd_mat m[3];
+        for (int i = 0; i < 3; ++i) {
+            if (!need[i]) continue;
+            out[i] = a[10 + i] == Py_None ? fresh(want[i], f.type, f.d) : tensor(a[10 + i], where, names[i]);
+            fit(*out[i], where, names[i], want[i], f.type, f.d);
+            m[i] = mat(*out[i]);
+        }
+        const palsgd_mat mdy = mat(dy), mx = mat(x), me = mat(xe), mp = mat(pre), mpe = mat(pre_e);
+        with_workspace([&](void* ws, size_t* n) {
+            return g_lib.linear_backward(&f.shape, &mdy, &mx, at(xe, me), &f.w, at(pre, mp), at(pre_e, mpe), at(out[0], m[0]), &m[1], at(out[2], m[2]), ws, n, on.raw);
+        }, a[13], f.d, where);
+        for (const auto& t : out) if (t) written(*t);
+        return pack(out[0], out[1], out[2]);
+    });
+}
+
+// ---------------------------------------------------------------------------------------------- layer norm
+
+struct Norm {
+    int64_t K, M, D;
+    at::ScalarType type;
+    at::Device d;
+    palsgd_norm_shape shape;
+    palsgd_mat w;
+};
+Norm norm(const char* where, const at::Tensor& x, const char* name, PyObject* weight, double eps)
+{
+    const at::Device d = on_cuda(x, where, name, 3);
+    Norm f{x.size(0), x.size(1), x.size(2), x.scalar_type(), d, {}, {}};
+    const int prec = precision(f.type, where, name);
+    fit(x, where, name, x.sizes(), f.type, d);
+    const at::Tensor& w = tensor(weight, where, "w");
+    fit(w, where, "w", {f.K, f.D}, f.type, d);
+    f.w = mat(w);
+    f.shape = palsgd_norm_shape{workers(f.K), prec, (uint64_t)f.M, (uint64_t)f.D, eps};
+    return f;
+}
+
+// (x, w, b, residual, eps, need_stats, y, total, mean, rstd, stream) -> (y, total, mean, rstd)
+PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 11, [&] {
+        const char* where = "palsgd_layer_norm_forward";
+        const double eps = PyFloat_AsDouble(a[4]);
+        if (eps == -1.0 && PyErr_Occurred()) throw python_error();
+        const at::Tensor& x = tensor(a[0], where, "x");
+        const Norm f = norm(where, x, "x", a[1], eps);
+        const at::Tensor& b = tensor(a[2], where, "b");
+        fit(b, where, "b", {f.K, f.D}, f.type, f.d);
+        const std::optional<at::Tensor> residual = maybe(a[3], where, "residual");
+        if (residual) fit(*residual, where, "residual", x.sizes(), f.type, f.d);
+        const On on(f.d, a[10]);
+        const at::Tensor y = a[6] == Py_None ? fresh(x.sizes(), f.type, f.d) : tensor(a[6], where, "y");
+        fit(y, where, "y", x.sizes(), f.type, f.d);
+        std::optional<at::Tensor> total, mean, rstd;
+        if (residual) {
+            total = a[7] == Py_None ? fresh(x.sizes(), f.type, f.d) : tensor(a[7], where, "total");
+            fit(*total, where, "total", x.sizes(), f.type, f.d);
+        }
+        const int64_t rows[2] = {f.K, f.M};
+        if (integer(a[5])) {
+            mean = a[8] == Py_None ? fresh(rows, at::kFloat, f.d) : tensor(a[8], where, "mean");
+            rstd = a[9] == Py_None ? fresh(rows, at::kFloat, f.d) : tensor(a[9], where, "rstd");
+            fit(*mean, where, "mean", rows, at::kFloat, f.d);
+            fit(*rstd, where, "rstd", rows, at::kFloat, f.d);
+        }
+        const palsgd_mat mx = mat(x), mb = mat(b), my = mat(y), mr = mat(residual), mt = mat(total), mm = mat(mean), ms = mat(rstd);
+        check(g_lib.norm_forward(&f.shape, &mx, at(residual, mr), &f.w, &mb, &my, at(total, mt), at(mean, mm), at(rstd, ms), on.raw), where);
+        written(y);
+        for (const auto* t : {&total, &mean, &rstd}) if (*t) written(**t);
+        return pack(std::optional<at::Tensor>(y), total, mean, rstd);
+    });
+}
+
+// (dy, x, w, mean, rstd, dtotal, dx, dw, db, workspace, stream) -> (dx, dw, db)
+PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 11, [&] {
+        const char* where = "palsgd_layer_norm_backward";
+        const at::Tensor& dy = tensor(a[0], where, "dy");
+        const Norm f = norm(where, dy, "dy", a[2], 0.0);
+        const at::Tensor &x = tensor(a[1], where, "x"), &mean = tensor(a[3], where, "mean"), &rstd = tensor(a[4], where, "rstd");
+        const int64_t rows[2] = {f.K, f.M}, cols[2] = {f.K, f.D};
+        fit(x, where, "x", dy.sizes(), f.type, f.d);
+        fit(mean, where, "mean", rows, at::kFloat, f.d);
+        fit(rstd, where, "rstd", rows, at::kFloat, f.d);
+        const std::optional<at::Tensor> past = maybe(a[5], where, "dtotal");
+        if (past) fit(*past, where, "dtotal", dy.sizes(), f.type, f.d);
+        const On on(f.d, a[10]);
+        static const char* names[3] = {"dx", "dw", "db"};
+        const at::IntArrayRef want[3] = {dy.sizes(), cols, cols};
+        std::optional<at::Tensor> out[3];
+        palsgd_mat m[3];
+        for (int i = 0; i < 3; ++i) {
+            out[i] = a[6 + i] == Py_None ? fresh(want[i], f.type, f.d) : tensor(a[6 + i], where, names[i]);
+            fit(*out[i], where, names[i], want[i], f.type, f.d);
+            m[i] = mat(*out[i]);
+        }
+        const palsgd_mat mdy = mat(dy), mx = mat(x), mm = mat(mean), ms = mat(rstd), mp = mat(past);
+        with_workspace([&](void* ws, size_t* n) {
+            return g_lib.norm_backward(&f.shape, &mdy, &mx, &f.w, &mm, &ms, at(past, mp), &m[0], &m[1], &m[2], ws, n, on.raw);
+        }, a[9], f.d, where);
+        for (const auto& t : out) written(*t);
+        return pack(out[0], out[1], out[2]);
+    });
+}
+
+// ---------------------------------------------------------------------------------------------- cross entropy
+
+struct Loss {
+    int64_t rows[2];
+    at::Device d;
+    palsgd_loss_shape shape;
+    palsgd_mat logits;
+    const int32_t* targets;
+};
+Loss loss(const char* where, const at::Tensor& z, PyObject* targets)
+{
+    const at::Device d = on_cuda(z, where, "logits", 3);
+    const int prec = precision(z.scalar_type(), where, "logits");
+    fit(z, where, "logits", z.sizes(), z.scalar_type(), d);
+    const at::Tensor& t = tensor(targets, where, "targets");
+    fit(t, where, "targets", {z.size(0), z.size(1)}, at::kInt, d);
+    return Loss{{z.size(0), z.size(1)}, d, palsgd_loss_shape{workers(z.size(0)), prec, (uint64_t)z.size(1), (uint64_t)z.size(2), z.size(0) > 1 ? t.stride(0) : 0},
+                mat(z), t.data_ptr<int32_t>()};
+}
+
+// (logits, targets, loss, lse, stream) -> (loss, lse)
+PyObject* loss_forward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 5, [&] {
+        const char* where = "palsgd_cross_entropy_forward";
+        const Loss f = loss(where, tensor(a[0], where, "logits"), a[1]);
+        const On on(f.d, a[4]);
+        const at::Tensor out = a[2] == Py_None ? fresh(f.rows, at::kFloat, f.d) : tensor(a[2], where, "loss");
+        const at::Tensor lse = a[3] == Py_None ? fresh(f.rows, at::kFloat, f.d) : tensor(a[3], where, "lse");
+        fit(out, where, "loss", f.rows, at::kFloat, f.d);
+        fit(lse, where, "lse", f.rows, at::kFloat, f.d);
+        const palsgd_mat mo = mat(out), ml = mat(lse);
+        check(g_lib.loss_forward(&f.shape, &f.logits, f.targets, &mo, &ml, on.raw), where);
+        written(out, lse);
+        return pack(std::optional<at::Tensor>(out), std::optional<at::Tensor>(lse));
+    });
+}
+
+// (dloss, logits, targets, lse, out, stream) -> dlogits
+PyObject* loss_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 6, [&] {
+        const char* where = "palsgd_cross_entropy_backward";
+        const at::Tensor &dloss = tensor(a[0], where, "dloss"), &z = tensor(a[1], where, "logits"), &lse = tensor(a[3], where, "lse");
+        const Loss f = loss(where, z, a[2]);
+        fit(dloss, where, "dloss", f.rows, at::kFloat, f.d);
+        fit(lse, where, "lse", f.rows, at::kFloat, f.d);
+        const On on(f.d, a[5]);
+        const at::Tensor dz = a[4] == Py_None ? fresh(z.sizes(), z.scalar_type(), f.d) : tensor(a[4], where, "out");
+        fit(dz, where, "out", z.sizes(), z.scalar_type(), f.d);
+        const palsgd_mat md = mat(dloss), ml = mat(lse), mz = mat(dz);
+        check(g_lib.loss_backward(&f.shape, &md, &f.logits, f.targets, &ml, &mz, on.raw), where);
+        written(dz);
+        return wrap(dz);
+    });
+}
+
 // (handle of the loaded library, exception class)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -430,6 +687,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
         {"palsgd_act8_pack", (void**)&g_lib.act8_pack}, {"palsgd_act8_unpack", (void**)&g_lib.act8_unpack},
         {"palsgd_ffn_forward", (void**)&g_lib.ffn_forward}, {"palsgd_ffn_backward", (void**)&g_lib.ffn_backward},
         {"palsgd_qk_norm_rope_forward", (void**)&g_lib.qk_forward}, {"palsgd_qk_norm_rope_backward", (void**)&g_lib.qk_backward},
+        {"palsgd_linear_forward", (void**)&g_lib.linear_forward}, {"palsgd_linear_backward", (void**)&g_lib.linear_backward},
+        {"palsgd_layer_norm_forward", (void**)&g_lib.norm_forward}, {"palsgd_layer_norm_backward", (void**)&g_lib.norm_backward},
+        {"palsgd_cross_entropy_forward", (void**)&g_lib.loss_forward}, {"palsgd_cross_entropy_backward", (void**)&g_lib.loss_backward},
         {"palsgd_last_cuda_error", (void**)&g_lib.last_cuda_error}};
     for (const auto& f : all)
         if (!(*f.to = dlsym(lib, f.name))) { PyErr_Format(PyExc_ImportError, "the library has no %s", f.name); return nullptr; }
@@ -439,7 +699,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 }
 
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(act8_pack), ENTRY(act8_unpack), ENTRY(ffn_forward), ENTRY(ffn_backward), ENTRY(qk_forward), ENTRY(qk_backward), ENTRY(bind),
+PyMethodDef methods[] = {ENTRY(act8_pack), ENTRY(act8_unpack), ENTRY(ffn_forward), ENTRY(ffn_backward), ENTRY(qk_forward), ENTRY(qk_backward),
+                         ENTRY(linear_forward), ENTRY(linear_backward), ENTRY(norm_forward), ENTRY(norm_backward), ENTRY(loss_forward), ENTRY(loss_backward), ENTRY(bind),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
