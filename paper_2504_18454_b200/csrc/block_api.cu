@@ -524,19 +524,29 @@ int run_linear_join(const palsgd_linear_shape* s, const Product& p, const Linear
     });
 }
 
-// Row CTAs of the gradient before the activation: enough to fill the device, with at least 32 rows each.
+// Lanes side by side in the pass before the activation, and rows of a CTA: enough CTAs to run at a time, with at least four
+// turns of their lanes each; all rows where that is less than the kernel that joins what several CTAs leave takes to launch.
+uint32_t slope_lanes(const palsgd_linear_shape* s)
+{
+    uint32_t lanes = 2;
+    while (lanes < 32 && lanes * 8 < s->d_out) lanes *= 2;
+    return lanes;
+}
 uint32_t slope_rows(const palsgd_linear_shape* s)
 {
-    const uint64_t strips = ceil_div(s->d_out, 256) * s->K, want = ceil_div(6ull * sm_count(), strips);
-    const uint64_t rows = ceil_div(ceil_div(s->tokens, want), 32) * 32;
-    const uint64_t least = ceil_div(s->tokens, 65535);   // (the grid's second axis)
-    return (uint32_t)(rows > least ? rows : least);
+    const uint32_t lanes = slope_lanes(s);
+    const uint64_t strips = ceil_div(s->d_out, lanes * 8) * s->K, want = ceil_div(3ull * sm_count(), strips), turn = 8 * (32 / lanes), least = 4 * turn;
+    if (s->tokens <= 2 * least) return (uint32_t)s->tokens;
+    uint64_t rows = ceil_div(s->tokens, want);
+    if (rows < least) rows = least;
+    const uint64_t grid = ceil_div(s->tokens, 65535);    // (the grid's second axis)
+    return (uint32_t)ceil_div(rows > grid ? rows : grid, turn) * (uint32_t)turn;
 }
 
 template <typename T>
 int run_slope(const palsgd_linear_shape* s, const SlopeArgs& a, cudaStream_t st)
 {
-    const dim3 grid((unsigned)ceil_div(s->d_out, 256), (unsigned)ceil_div(s->tokens, a.rows), s->K);
+    const dim3 grid((unsigned)ceil_div(s->d_out, a.lanes * 8), (unsigned)ceil_div(s->tokens, a.rows), s->K);
     return with_act(s->activation, [&](auto act) {
         if constexpr (act != PALSGD_ACT_NONE)
             if (s->save == PALSGD_SAVE_8BIT) return launch("linear, gradient before the activation", slope_kernel<T, act, true>, grid, 256, 0, st, a);
@@ -951,7 +961,9 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
         }
         pass = write || db.given;
         slope.rows = slope_rows(s);
-        if (db.given) slope.part = static_cast<float*>(ws.take((size_t)s->K * ceil_div(M, slope.rows) * N * sizeof(float)));
+        slope.lanes = slope_lanes(s);
+        if (db.given && slope.rows >= M) { slope.db = db.m.data; slope.dbw = db.m.worker_stride; }
+        else if (db.given) slope.part = static_cast<float*>(ws.take((size_t)s->K * ceil_div(M, slope.rows) * N * sizeof(float)));
         ox = input_operand(ws, stage, x, x_e, s->precision, s->K, M, D);
         if (dx.given) {
             ow = input_operand(ws, stage, w, nullptr, s->precision, s->K, N, D);
@@ -985,7 +997,7 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
         slope.M = (uint32_t)M; slope.N = (uint32_t)N;
         BLOCK_TRY(es == 4 ? run_slope<float>(s, slope, st) : run_slope<bf16>(s, slope, st));
     }
-    if (db.given) {
+    if (slope.part) {
         ColumnSumArgs c{slope.part, {db.m.data, nullptr}, {db.m.worker_stride, 0}, (uint32_t)ceil_div(M, slope.rows), (uint32_t)N, (uint32_t)N};
         BLOCK_TRY(launch("linear, bias gradient", es == 4 ? column_sum_kernel<float> : column_sum_kernel<bf16>, dim3((unsigned)ceil_div(N, 32), s->K), 256, 0, st, c));
     }

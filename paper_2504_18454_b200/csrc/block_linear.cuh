@@ -228,37 +228,43 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
 // ---------------------------------------------------------------------------------------------- gradient before the activation
 
 // dz = dy act'(z) as the products' operand (bfloat16, or fp32 in three parts; dst NULL: dy itself is the operand), and its
-// sums over a CTA's rows, unrounded, to the CTA's row of `part` (NULL: none wanted).  A CTA has 256 columns -- a lane eight of
-// them -- and its warps take the rows in turn.
+// sums over a CTA's rows, unrounded, to the CTA's row of `part` -- or, where one CTA has all rows, the gradient of the bias
+// itself.  `lanes` lanes have a row side by side, eight columns each, and a warp 32 / lanes rows.
 struct SlopeArgs {
     const void *dy, *pre;         // pre: NULL without an activation
     const uint8_t* pre_e;         // 8 bits
     int64_t  dw, dr, pw, pr, ew, er;
     bf16*    dst;
     int64_t  dstw, ld, dst_part;  // worker, row and part strides
-    float*   part;                // [K][row CTAs][N]
+    float*   part;                // [K][row CTAs][N]; NULL: none wanted, or `db` is written
+    void*    db;
+    int64_t  dbw;
     uint32_t M, N, rows;          // rows of a CTA
+    uint32_t lanes;
     int      dy_wide, pre_wide;
 };
 
 template <typename T, int ACT, bool EIGHT>
-__global__ void __launch_bounds__(256, 2) slope_kernel(const __grid_constant__ SlopeArgs a)
+__global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ SlopeArgs a)
 {
-    constexpr int U = 4;                                  // rows of a warp under way
-    __shared__ float sums[8][257];
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 256 + lane * 8;
+    constexpr int U = 2;                                  // rows of a lane under way
+    __shared__ float sums[8][256];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, abreast = 32 / a.lanes;
+    const uint32_t local = (lane % a.lanes) * 8, c = blockIdx.x * a.lanes * 8 + local;
     const int64_t k = blockIdx.z;
-    const uint32_t n = c < a.N ? min(a.N - c, 8u) : 0, room = a.dst && c < a.ld ? 8u : 0u;    // (the operand's rows hold a multiple of eight columns)
-    const uint32_t first = blockIdx.y * a.rows, last = min(a.M, first + a.rows);
+    const uint32_t n = c < a.N ? min(a.N - c, 8u) : 0;
+    const bool room = a.dst && c < a.ld;                  // (the operand's rows hold a multiple of eight columns)
+    const uint32_t first = blockIdx.y * a.rows, last = min(a.M, first + a.rows), step = 8 * abreast;
     let_next_start();
     wait_for_previous();
     f2 sum[4] = {0, 0, 0, 0};
-    for (uint32_t r0 = first + warp; r0 < last; r0 += 8 * U) {
+#pragma unroll 1
+    for (uint32_t r0 = first + warp * abreast + lane / a.lanes; r0 < last; r0 += U * step) {
         f2 d[U][4], z[U][4];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t r = r0 + 8 * u;
-            const uint32_t m = r0 + 8 * u < last ? n : 0;
+            const int64_t r = r0 + u * step;
+            const uint32_t m = r0 + u * step < last ? n : 0;
             row8_load(static_cast<const T*>(a.dy) + k * a.dw + r * a.dr + c, m, a.dy_wide, d[u]);
             if constexpr (ACT != PALSGD_ACT_NONE) {
                 if constexpr (EIGHT) {
@@ -279,19 +285,19 @@ __global__ void __launch_bounds__(256, 2) slope_kernel(const __grid_constant__ S
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (r0 + 8 * u >= last) break;
+            if (r0 + u * step >= last) break;
             if constexpr (ACT != PALSGD_ACT_NONE) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     f2 slope;
                     act_pair<T, ACT, true>(z[u][i], slope);
-                    d[u][i] = f2_mul(d[u][i], slope);
+                    d[u][i] = f2_mul(d[u][i], slope);     // (what lies behind the row's end is used nowhere)
                 }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = f2_add(sum[i], d[u][i]);
             if (room) {
-                bf16* to = a.dst + k * a.dstw + (int64_t)(r0 + 8 * u) * a.ld + c;
+                bf16* to = a.dst + k * a.dstw + (int64_t)(r0 + u * step) * a.ld + c;
                 if constexpr (sizeof(T) == 2) {
                     *reinterpret_cast<uint4*>(to) = make_uint4(f2_narrow(d[u][0]), f2_narrow(d[u][1]), f2_narrow(d[u][2]), f2_narrow(d[u][3]));
                 } else {
@@ -303,21 +309,27 @@ __global__ void __launch_bounds__(256, 2) slope_kernel(const __grid_constant__ S
             }
         }
     }
-    if (!a.part) return;
+    if (!a.part && !a.db) return;
+    for (uint32_t d = a.lanes; d < 32; d *= 2)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float x, y;
-        f2_get(sum[i], x, y);
-        sums[warp][lane * 8 + 2 * i] = x;
-        sums[warp][lane * 8 + 2 * i + 1] = y;
+        for (int i = 0; i < 4; ++i) sum[i] = f2_add(sum[i], __shfl_xor_sync(0xFFFFFFFFu, sum[i], d));
+    if (lane < a.lanes) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x, y;
+            f2_get(sum[i], x, y);
+            sums[warp][local + 2 * i] = x;
+            sums[warp][local + 2 * i + 1] = y;
+        }
     }
     __syncthreads();
-    const uint32_t at = blockIdx.x * 256 + threadIdx.x;
-    if (at >= a.N) return;
+    const uint32_t at = blockIdx.x * a.lanes * 8 + threadIdx.x;
+    if (threadIdx.x >= a.lanes * 8 || at >= a.N) return;
     float t = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
-    a.part[((uint64_t)k * gridDim.y + blockIdx.y) * a.N + at] = t;
+    if (a.part) a.part[((uint64_t)k * gridDim.y + blockIdx.y) * a.N + at] = t;
+    else static_cast<T*>(a.db)[k * a.dbw + at] = from_f<T>(t);
 }
 
 }  // namespace block

@@ -462,8 +462,10 @@ __device__ __forceinline__ uint32_t pairs_of(const MatProblem& p) { return p.a_p
 // all their parts) are a sum of their own, and the sums are joined in registers with rounding to nearest -- the tensor
 // cores cut off what an addition does not hold, which over long sums adds up (measured over 4096 steps of the inner axis
 // in one sum: 4.4e-6 of the result's norm; in pieces of 4: 2.4e-7, of 8: 4.8e-7, where the whole is 2 % faster).
-template <typename T, typename F>
-__device__ __forceinline__ bool for_pieces(const Tile& tl, F&& f)
+// `cut`: whether sums are cut into pieces.  (Of bfloat16 products, those that go into an 8-bit checkpoint are: how many of
+// its values land on the other side of a rounding goes by the sums' error.)
+template <typename F>
+__device__ __forceinline__ bool for_pieces(const Tile& tl, bool cut, F&& f)
 {
     const MatProblem& p = *tl.p;
     const uint32_t steps = (p.Kd + kTileK - 1) / kTileK, all = p.n_seg * steps;
@@ -475,9 +477,9 @@ __device__ __forceinline__ bool for_pieces(const Tile& tl, F&& f)
     for (bool first = true; g < last; first = false) {
         const uint32_t seg = g >= steps, k = g - seg * steps;
         uint32_t n = min(steps - k, last - g);
-        if (sizeof(T) == 4) n = min(n, kPiece);
+        if (cut) n = min(n, kPiece);
         g += n;
-        if (!f(seg, k, k + n, sizeof(T) == 4 || first, sizeof(T) == 4 || g == last)) return false;
+        if (!f(seg, k, k + n, cut || first, cut || g == last)) return false;
     }
     return true;
 }
@@ -494,6 +496,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
     const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16, tmem_at = acc_empty + 16;
     const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+    const bool cut = Shape::kWide || (MODE == MAT_LINEAR && a.save == PALSGD_SAVE_8BIT);
 
     let_next_start();
     if (threadIdx.x == 0) {
@@ -529,7 +533,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 const uint32_t mn = is_b ? (MODE == MAT_GATED ? tl.n0 : tl.n0 + rank * 128) : tl.m0 + rank * 128;
                 const bool across = is_b ? p.b_mn : p.a_mn;
                 const int parts_a = p.a_parts, parts_b = p.b_parts;
-                ok = for_pieces<T>(tl, [&](uint32_t seg, uint32_t from, uint32_t to, bool, bool) {
+                ok = for_pieces(tl, cut, [&](uint32_t seg, uint32_t from, uint32_t to, bool, bool) {
                     const uint32_t i = is_b && MODE == MAT_GATED ? rank : seg;
                     const CUtensorMap* const map = is_b ? &p.B[i] : &p.A[i];
                     const uint32_t w = (is_b ? p.b_one[i] : p.a_one[i]) ? 0 : tl.worker;
@@ -578,7 +582,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((kTileN / 8) << 17) | ((kTileM / 16) << 24);
                 const uint64_t da = operand_desc(base, p.a_mn), db = operand_desc(base + kOperandBytes, p.b_mn);
                 const uint32_t sa = p.a_mn ? 2048 / 16 : 32 / 16, sb = p.b_mn ? 2048 / 16 : 32 / 16;
-                ok = for_pieces<T>(tl, [&](uint32_t, uint32_t from, uint32_t to, bool begins, bool ends) {
+                ok = for_pieces(tl, cut, [&](uint32_t, uint32_t from, uint32_t to, bool begins, bool ends) {
                     const uint32_t acc = it & 1, d = tmem + acc * kTileN;
                     if (begins) {
                         if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_empty + 8 * acc, (it >> 1 & 1) ^ 1, a.gave_up))) return false;
@@ -660,15 +664,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             const uint32_t m = tl.m0 + rank * 128 + quad * 32, rows = m < p.M ? min(p.M - m, 32u) : 0;
             const int64_t w = tl.worker;
             uint32_t src = tmem + (it & 1) * kTileN + (quad << 21) + part * kMine;
-            if constexpr (!Shape::kWide) {
+            // (a warp whose rows or columns are all outside has nothing to do but to let the sums go)
+            const bool idle = (MODE == MAT_PLAIN || MODE == MAT_LINEAR) && (rows == 0 || tl.n0 + part * kMine >= p.N);
+            if (!cut) {
                 if (!acc_wait()) break;
-            } else {
-                // fp32: the pieces' sums joined in registers, and put back for what follows
+            } else if (MODE != MAT_GATED && MODE != MAT_HIDDEN && idle) {
+                bool ok = true;
+                uint32_t pieces = 0;
+                for_pieces(tl, true, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
+                while (ok && --pieces) {
+                    ok = acc_wait();
+                    if (ok) acc_read();
+                }
+                if (!ok || !acc_wait()) break;
+            } else if constexpr (Shape::kWide || MODE == MAT_LINEAR) {
+                // the pieces' sums joined in registers, and put back for what follows
                 float sum[64];
 #pragma unroll
                 for (int i = 0; i < 64; ++i) sum[i] = 0.0f;
                 uint32_t pieces = 0;
-                for_pieces<T>(tl, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
+                for_pieces(tl, true, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
                 bool ok = true;
                 for (;;) {
                     src = tmem + (it & 1) * kTileN + (quad << 21) + part * kMine;
@@ -689,7 +704,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 for (int q = 0; q < 8; ++q) tmem_store8(src + (MODE == MAT_GATED && q >= 4 ? kTileN / 2 + (q - 4) * 8 : q * 8), sum + 8 * q);
                 tmem_store_wait();
             }
-            float gi = 0.0f, ui = 0.0f;                                   // gate/up, 8 bits: one over the steps of the groups
+            float gi = 0.0f, ui = 0.0f, inv = 0.0f;                       // 8 bits: one over the steps of the groups (gate/up; linear)
             if constexpr (MODE == MAT_GATED) {
                 const uint32_t n = tl.n0 + part * kMine;
                 if (eight) {
@@ -711,41 +726,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     }
                 }
             }
-            // linear: z = the sum + bias of eight columns, from the tile's column j on
-            auto linear_z = [&](uint32_t j, f2 (&z)[4]) {
-                float v[8];
-                tmem_load8(src + j, v);
-                f2 b[4] = {0, 0, 0, 0};
+            if (idle) {
+                acc_read();
+                if constexpr (MODE == MAT_LINEAR) if (a.residual.p && o.then() < a.tiles) fetch_residual(tile_at<MODE>(a, o.then()), 0);
+                continue;
+            }
+            // linear: z = the sums + bias of 16 columns, from the tile's column j on
+            auto linear_z = [&](uint32_t j, f2* z) {
+                float v[16];
+                tmem_load16(src + j, v);
                 const uint32_t n = tl.n0 + part * kMine + j;
-                if (a.bias.p && n < p.N) row8_load(static_cast<const T*>(a.bias.p) + w * a.bias.w + n, p.N - n, a.bias.wide, b);
-                tmem_load_wait();
+                f2 b[8];
+                if (a.bias.p) {
+                    const T* at = static_cast<const T*>(a.bias.p) + w * a.bias.w + n;
+                    if (n + 16 <= p.N && a.bias.wide) {
+                        row8_load(at, 8, true, *reinterpret_cast<f2(*)[4]>(b));
+                        row8_load(at + 8, 8, true, *reinterpret_cast<f2(*)[4]>(b + 4));
+                    } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[i] = f2_add(f2_of(v[2 * i], v[2 * i + 1]), b[i]);
-            };
-            float inv[2] = {0.0f, 0.0f};                                  // 8 bits: one over the steps of the warp's two groups
-            if constexpr (MODE == MAT_LINEAR) {
-                if (eight) {
-#pragma unroll
-                    for (uint32_t g = 0; g < 2; ++g) {
-                        const uint32_t n = tl.n0 + part * kMine + 32 * g;
-                        float top = 0.0f;
-#pragma unroll 1
-                        for (uint32_t j = 0; j < 32; j += 8) {
-                            f2 z[4];
-                            linear_z(32 * g + j, z);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                float x, y;
-                                f2_get(z[i], x, y);
-                                top = act8_max(act8_max(top, x), y);
-                            }
-                        }
-                        const uint32_t e = act8_exponent(top);
-                        inv[g] = act8_inverse(e);
-                        if (lane < rows && n < p.N) static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * a.gate_e.r + n / 32] = (uint8_t)e;
+                        for (uint32_t i = 0; i < 8; ++i)
+                            b[i] = f2_of(n + 2 * i < p.N ? to_f(at[2 * i]) : 0.0f, n + 2 * i + 1 < p.N ? to_f(at[2 * i + 1]) : 0.0f);
                     }
                 }
-            }
+                tmem_load_wait();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    z[i] = f2_of(v[2 * i], v[2 * i + 1]);
+                    if (a.bias.p) z[i] = f2_add(z[i], b[i]);
+                }
+            };
+            auto linear_top = [](float top, const f2* z) {                // the largest magnitude of 16 columns and `top`
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float x, y;
+                    f2_get(z[i], x, y);
+                    top = act8_max(act8_max(top, x), y);
+                }
+                return top;
+            };
 #pragma unroll 1
             for (uint32_t c = 0; c < kChunks; ++c) {
                 const uint32_t from = src + c * kCols, n = tl.n0 + part * kMine + c * kCols;
@@ -786,46 +804,57 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     block_out<64, E>(b0, static_cast<unsigned char*>(p.out[0].p) + E * to, E * p.out[0].r, rows, room, p.out[0].wide, lane);
                     __syncwarp();
                 } else if constexpr (MODE == MAT_LINEAR) {
-                    // what is saved, then y, pass through one block (the sums are read again for each); the residual comes
-                    // into the other one while the products of the tile, or the work on the block before, still run
+                    // z of the block in registers; what is saved, then y, pass through one block; the residual comes into the
+                    // other one while the products of the tile, or the work on the block before, still run
+                    f2 z[kCols / 2];
+#pragma unroll
+                    for (uint32_t j = 0; j < kCols; j += 16) linear_z(c * kCols + j, z + j / 2);
                     if (a.save != PALSGD_SAVE_NONE) {
-#pragma unroll 1
-                        for (uint32_t j = 0; j < kOcts; ++j) {
-                            f2 z[4];
-                            linear_z(c * kCols + 8 * j, z);
-                            if (eight) {
+                        if (eight) {
+                            if (E == 2 || c % 2 == 0) {                   // a group of 32 columns begins
+                                float top = linear_top(0.0f, z);
+                                if constexpr (E == 2) {
+                                    top = linear_top(top, z + 8);
+                                } else {
+                                    f2 more[8];
+                                    linear_z((c + 1) * kCols, more);
+                                    top = linear_top(top, more);
+                                }
+                                const uint32_t e = act8_exponent(top);
+                                inv = act8_inverse(e);
+                                if (lane < rows && cols) static_cast<uint8_t*>(a.gate_e.p)[w * a.gate_e.w + (int64_t)(m + lane) * a.gate_e.r + n / 32] = (uint8_t)e;
+                            }
+#pragma unroll
+                            for (uint32_t j = 0; j < kOcts; ++j) {
                                 float v[8];
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) f2_get(z[i], v[2 * i], v[2 * i + 1]);
-                                row_put_act8<T>(b0, lane, j, c * kCols >= 32 ? inv[1] : inv[0], v);
-                            } else {
-                                row_put<T>(b0, lane, j, z);
+                                for (int i = 0; i < 4; ++i) f2_get(z[4 * j + i], v[2 * i], v[2 * i + 1]);
+                                row_put_act8<T>(b0, lane, j, inv, v);
                             }
+                        } else {
+#pragma unroll
+                            for (uint32_t j = 0; j < kOcts; ++j) row_put<T>(b0, lane, j, *reinterpret_cast<f2(*)[4]>(z + 4 * j));
                         }
                         __syncwarp();
                         const int64_t to = w * a.gate.w + (int64_t)m * a.gate.r + n;
                         if (eight) block_out<kCols, 1>(b0, static_cast<unsigned char*>(a.gate.p) + to, a.gate.r, rows, cols, a.gate.wide, lane);
                         else block_out<64, E>(b0, static_cast<unsigned char*>(a.gate.p) + E * to, E * a.gate.r, rows, cols, a.gate.wide, lane);
-                        __syncwarp();
                     }
-                    if (a.residual.p) {
-                        block_wait();
-                        __syncwarp();
-                    }
-#pragma unroll 1
-                    for (uint32_t j = 0; j < kOcts; ++j) {
-                        f2 z[4], r[4], unused;
-                        linear_z(c * kCols + 8 * j, z);
+                    if (c + 1 == kChunks) acc_read();
+                    if (a.residual.p) block_wait();
+                    __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) z[i] = act_pair<T, ACT, false>(z[i], unused);
+                    for (uint32_t j = 0; j < kOcts; ++j) {
+                        f2 r[4], unused;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z[4 * j + i] = act_pair<T, ACT, false>(z[4 * j + i], unused);
                         if (a.residual.p) {
                             row_get<T>(b1, lane, j, r);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) z[i] = f2_add(z[i], r[i]);
+                            for (int i = 0; i < 4; ++i) z[4 * j + i] = f2_add(z[4 * j + i], r[i]);
                         }
-                        row_put<T>(b0, lane, j, z);
+                        row_put<T>(b0, lane, j, *reinterpret_cast<f2(*)[4]>(z + 4 * j));
                     }
-                    if (c + 1 == kChunks) acc_read();
                     __syncwarp();
                     if (a.residual.p) {
                         if (c + 1 < kChunks) fetch_residual(tl, c + 1);

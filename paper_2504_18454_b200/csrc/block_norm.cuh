@@ -1,9 +1,10 @@
 // Row kernels of the block operators: layer norm forward and backward.
 //
-// A team of W warps has a row at a time in its registers: mean, then the mean square around it (two passes over registers: a
-// row whose mean is large against its spread loses nothing), then the result, in one pass over memory.  A team walks rows
-// with the next one under way; its columns of w (and b), and in the backward pass its sums of dw and db, stay in registers
-// over all of its rows.  The sums go to one row of the workspace for each CTA and are joined in a fixed order.
+// A team of lanes -- 4 to 32 of a warp, or up to 32 warps -- has a row at a time in its registers: mean, then the mean square
+// around it (two passes over registers: a row whose mean is large against its spread loses nothing), then the result, in one
+// pass over memory.  A team walks rows with the next ones under way; its columns of w (and b), and in the backward pass its
+// sums of dw and db, stay in registers over all of its rows.  The sums go to one row of the workspace for each CTA and are
+// joined in a fixed order; where one CTA has all of a worker's rows it writes the gradients itself.
 // Bound by memory: every byte is moved once.
 #pragma once
 #include "block_common.cuh"
@@ -16,10 +17,12 @@ struct NormArgs {
     const void *w, *b, *dy;
     void *y, *total;              // backward: y is dx
     float *mean, *rstd;           // forward: may be NULL
-    float* part;                  // backward: [K][CTAs][2][width]
+    float* part;                  // backward: [K][CTAs][2][width]; NULL: the gradients themselves are written
+    void  *dw_out, *db_out;
+    int64_t dwo, dbo;
     int64_t xw, xr, rw, rr, dw, dr, yw, yr, tw, tr, ww, bw, mw, sw;      // worker and row strides, elements
     uint64_t rows;
-    uint32_t width, warps;        // warps of a team
+    uint32_t width, lanes;        // lanes of a team: 4 .. 1024
     float    eps;
 };
 
@@ -40,15 +43,18 @@ __device__ __forceinline__ uint4 piece_load(const T* row, uint32_t c, uint32_t w
 // Pieces on their way: every lane copies its own pieces of the rows to come into places of its own in shared memory,
 // asynchronously, and reads them there: no barrier, and registers for one row only.  (The next row in registers took 200 of
 // them a lane in the backward pass, which left eight warps an SM and 24 KB under way.)  Rows at any address come as the
-// aligned 16-byte blocks that hold a byte of them: a lane's piece lies in its block and the next lane's.
-template <typename T, bool WIDE>
+// aligned 16-byte blocks that hold a byte of them: a lane's piece lies in its block and the next lane's (the team's last lane
+// of a warp fetches one more).
+template <typename T, bool WIDE, int N>
 struct Ring {
-    static constexpr uint32_t kPlaces = WIDE ? 32 : 33;   // of 16 bytes: a warp's for one piece a lane
+    static constexpr uint32_t kPlaces = WIDE ? 32 : N == 1 ? 40 : 33;    // of 16 bytes: a warp's for one piece a lane
     uint32_t base, step;
-    __device__ __forceinline__ explicit Ring(const void* raw)
+    bool     last;                // the team's last lane of the warp
+    __device__ __forceinline__ Ring(const void* raw, uint32_t lanes)
     {
-        const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        base = (uint32_t)__cvta_generic_to_shared(raw) + (warp * kPlaces + lane) * 16;
+        const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, of_warp = min(lanes, 32u);
+        last = lane % of_warp == of_warp - 1;
+        base = (uint32_t)__cvta_generic_to_shared(raw) + (warp * kPlaces + lane + (WIDE ? 0 : lane / of_warp)) * 16;
         step = (blockDim.x >> 5) * kPlaces * 16;
     }
     static __device__ __forceinline__ void copy(uint32_t to, const void* from, bool on)
@@ -65,7 +71,7 @@ struct Ring {
             const uintptr_t start = reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15, end = reinterpret_cast<uintptr_t>(row + width);
             const uintptr_t block = reinterpret_cast<uintptr_t>(row + c) & ~(uintptr_t)15;
             copy(to, reinterpret_cast<const void*>(block < end ? block : start), block < end);
-            if ((threadIdx.x & 31) == 31) copy(to + 16, reinterpret_cast<const void*>(block + 16 < end ? block + 16 : start), block + 16 < end);
+            if (last) copy(to + 16, reinterpret_cast<const void*>(block + 16 < end ? block + 16 : start), block + 16 < end);
         }
     }
     __device__ __forceinline__ uint4 get(uint32_t i, const T* row, uint32_t c, uint32_t width) const
@@ -96,12 +102,12 @@ struct Ring {
     static __device__ __forceinline__ void left() { if constexpr (!WIDE) __syncwarp(); }
 };
 // Rows under way: as many as find room beside the SM's other CTAs, four at most.
-template <typename T, bool WIDE>
-constexpr __host__ __device__ uint32_t norm_stage_bytes(int pieces, int warps) { return (uint32_t)pieces * warps * Ring<T, WIDE>::kPlaces * 16; }
-template <typename T, bool WIDE>
-constexpr __host__ __device__ uint32_t norm_stages(int pieces, int warps, int ctas)
+template <typename T, bool WIDE, int N>
+constexpr __host__ __device__ uint32_t norm_stage_bytes(int arrays, int warps) { return (uint32_t)(arrays * N) * warps * Ring<T, WIDE, N>::kPlaces * 16; }
+template <typename T, bool WIDE, int N>
+constexpr __host__ __device__ uint32_t norm_stages(int arrays, int warps, int ctas)
 {
-    const uint32_t n = (227 * 1024 / ctas - 2048) / norm_stage_bytes<T, WIDE>(pieces, warps);
+    const uint32_t n = (227 * 1024 / ctas - 2048) / norm_stage_bytes<T, WIDE, N>(arrays, warps);
     return n > 4 ? 4 : n;
 }
 
@@ -150,20 +156,19 @@ constexpr uint32_t kNormMostWarps = 32;                                 // of a 
 // Sums of N values over a team, the same bits in all of its lanes.  `turn` alternates between calls: the places of one call
 // are read while the next one's are written.
 template <int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], uint32_t warps, uint32_t team, float* places, uint32_t& turn)
+__device__ __forceinline__ void team_sum(float (&v)[N], uint32_t lanes, uint32_t team, float* places, uint32_t& turn)
 {
-#pragma unroll
-    for (int d = 16; d; d >>= 1)
+    for (uint32_t d = min(lanes, 32u) / 2; d; d >>= 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
-    if (warps == 1) return;
-    const uint32_t warp = threadIdx.x >> 5, first = team * warps;
+    if (lanes <= 32) return;
+    const uint32_t warps = lanes / 32, warp = threadIdx.x >> 5, first = team * warps;
     float* p = places + turn * (2 * kNormMostWarps);
     turn ^= 1;
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
         for (int i = 0; i < N; ++i) p[i * kNormMostWarps + warp] = v[i];
-    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
+    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(lanes) : "memory");
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float s = p[i * kNormMostWarps + first];
@@ -177,12 +182,13 @@ __device__ __forceinline__ void team_sum(float (&v)[N], uint32_t warps, uint32_t
 template <typename T, int N, bool WIDE, bool ADD, int WARPS, int CTAS>
 __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 2 * N : N, S = norm_stages<T, WIDE>(Q, WARPS, CTAS);    // Q: pieces of a lane for a row
+    constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 2 * N : N, S = norm_stages<T, WIDE, N>(Q / N, WARPS, CTAS);    // Q: pieces of a lane for a row
     __shared__ float places[4 * kNormMostWarps];
     extern __shared__ __align__(16) unsigned char ring_raw[];
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
-    const uint32_t first = ((warp - team * a.warps) * 32 + lane) * V, step = a.warps * 32 * V, width = a.width;
-    const Ring<T, WIDE> ring(ring_raw);
+    const uint32_t team = threadIdx.x / a.lanes, teams = blockDim.x / a.lanes;
+    const uint32_t first = (threadIdx.x - team * a.lanes) * V, step = a.lanes * V, width = a.width;
+    const uint32_t beside = a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
+    const Ring<T, WIDE, N> ring(ring_raw, a.lanes);
     const int64_t k = blockIdx.y;
     const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
     const T *w = static_cast<const T*>(a.w) + k * a.ww, *b = static_cast<const T*>(a.b) + k * a.bw;
@@ -212,7 +218,8 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
         wp[i] = piece_load<T, WIDE>(w, first + i * step, width);
         bp[i] = piece_load<T, WIDE>(b, first + i * step, width);
     }
-    for (; row < a.rows; row += rows_step) {
+    for (; row - beside < a.rows; row += rows_step) {
+        const bool on = row < a.rows;
         ring.left();
         fetch();                                          // into the place that the row before this one has left
         ring.template wait<S - 1>();
@@ -233,10 +240,10 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
         if constexpr (ADD) {
             T* total = static_cast<T*>(a.total) + k * a.tw + (int64_t)row * a.tr;
 #pragma unroll
-            for (int i = 0; i < N; ++i) piece_store<T, WIDE>(total, first + i * step, width, piece_narrow<T>(h[i]));
+            for (int i = 0; i < N; ++i) piece_store<T, WIDE>(total, first + i * step, on ? width : 0, piece_narrow<T>(h[i]));
         }
         float s[1] = {f2_total(sum)};
-        team_sum<1>(s, a.warps, team, places, turn);
+        team_sum<1>(s, a.lanes, team, places, turn);
         const float mean = s[0] / (float)width;
         sum = 0;
 #pragma unroll
@@ -248,7 +255,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
                 sum = f2_fma(c, c, sum);
             }
         s[0] = f2_total(sum);
-        team_sum<1>(s, a.warps, team, places, turn);
+        team_sum<1>(s, a.lanes, team, places, turn);
         const float rstd = 1.0f / sqrtf(s[0] / (float)width + a.eps);
         T* y = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
 #pragma unroll
@@ -258,9 +265,9 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
             piece_wide<T>(bp[i], bv);
 #pragma unroll
             for (int j = 0; j < H; ++j) bv[j] = f2_fma(f2_mul(h[i][j], f2_same(rstd)), wv[j], bv[j]);
-            piece_store<T, WIDE>(y, first + i * step, width, piece_narrow<T>(bv));
+            piece_store<T, WIDE>(y, first + i * step, on ? width : 0, piece_narrow<T>(bv));
         }
-        if (first == 0) {
+        if (first == 0 && on) {
             if (a.mean) a.mean[k * a.mw + (int64_t)row] = mean;
             if (a.rstd) a.rstd[k * a.sw + (int64_t)row] = rstd;
         }
@@ -272,12 +279,14 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
 template <typename T, int N, bool WIDE, bool ADD, int WARPS, int CTAS>
 __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 3 * N : 2 * N, S = norm_stages<T, WIDE>(Q, WARPS, CTAS);
+    constexpr bool kKeep = WARPS == 8;                    // the wide kernel forms xh and g twice: they would not fit its registers
+    constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 3 * N : 2 * N, S = norm_stages<T, WIDE, N>(Q / N, WARPS, CTAS);
     __shared__ float places[4 * kNormMostWarps];
     extern __shared__ __align__(16) unsigned char ring_raw[];            // the ring; at the end [2][width] floats, where a CTA has more than one team
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
-    const uint32_t first = ((warp - team * a.warps) * 32 + lane) * V, step = a.warps * 32 * V, width = a.width;
-    const Ring<T, WIDE> ring(ring_raw);
+    const uint32_t team = threadIdx.x / a.lanes, teams = blockDim.x / a.lanes;
+    const uint32_t first = (threadIdx.x - team * a.lanes) * V, step = a.lanes * V, width = a.width;
+    const uint32_t beside = a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
+    const Ring<T, WIDE, N> ring(ring_raw, a.lanes);
     const int64_t k = blockIdx.y;
     const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
     const T *w = static_cast<const T*>(a.w) + k * a.ww, *dy = static_cast<const T*>(a.dy) + k * a.dw;
@@ -287,16 +296,17 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
 
     let_next_start();
     wait_for_previous();
-    auto fetch = [&]() {
-        if (ahead < a.rows) {
+    auto fetch = [&]() {                                  // (behind the last row: zeros, for the sums of dw and db of a warp's other teams)
+        const bool more = ahead < a.rows;
+        const int64_t at = more ? (int64_t)ahead : 0;
+        const uint32_t some = more ? width : 0;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                ring.fetch(put * Q + i, x + (int64_t)ahead * a.xr, first + i * step, width);
-                ring.fetch(put * Q + N + i, dy + (int64_t)ahead * a.dr, first + i * step, width);
-                if constexpr (ADD) ring.fetch(put * Q + 2 * N + i, r + (int64_t)ahead * a.rr, first + i * step, width);
-            }
-            ahead += rows_step;
+        for (int i = 0; i < N; ++i) {
+            ring.fetch(put * Q + i, x + at * a.xr, first + i * step, some);
+            ring.fetch(put * Q + N + i, dy + at * a.dr, first + i * step, some);
+            if constexpr (ADD) ring.fetch(put * Q + 2 * N + i, r + at * a.rr, first + i * step, some);
         }
+        ahead += rows_step;
         ring.commit();
         put = put + 1 == S ? 0 : put + 1;
     };
@@ -317,52 +327,66 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
         rstd = __ldg(a.rstd + k * a.sw + (int64_t)at);
     };
     stats(row);
-    for (; row < a.rows; row += rows_step) {
+    for (; row - beside < a.rows; row += rows_step) {
+        const bool on = row < a.rows;
         const float rs = rstd, mean_now = mean;
         stats(row + rows_step);
         ring.left();
         fetch();
         ring.template wait<S - 1>();
-        f2 xh[N][H], g[N][H], sg = 0, sx = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            f2 d[H], wv[H];
-            piece_wide<T>(ring.get(got * Q + i, x + (int64_t)row * a.xr, first + i * step, width), xh[i]);
-            piece_wide<T>(ring.get(got * Q + N + i, dy + (int64_t)row * a.dr, first + i * step, width), d);
+        const uint32_t some = on ? width : 0;
+        // a piece's xh, d and g = d w.  (Behind the row's end d is zero, and xh has to be finite.)
+        auto load = [&](int i, f2 (&xh)[H], f2 (&d)[H], f2 (&g)[H]) {
+            f2 wv[H];
+            piece_wide<T>(ring.get(got * Q + i, x + (int64_t)row * a.xr, first + i * step, some), xh);
+            piece_wide<T>(ring.get(got * Q + N + i, dy + (int64_t)row * a.dr, first + i * step, some), d);
             piece_wide<T>(wp[i], wv);
 #pragma unroll
             for (int j = 0; j < H; ++j) {
-                // (behind the row's end d is zero: xh must be finite there)
-                xh[i][j] = inside<WIDE>(f2_mul(f2_add(xh[i][j], f2_same(-mean_now)), f2_same(rs)), first + i * step + 2 * j, width);
-                g[i][j] = f2_mul(d[j], wv[j]);
-                dw[i][j] = f2_fma(d[j], xh[i][j], dw[i][j]);
+                xh[j] = inside<WIDE>(f2_mul(f2_add(xh[j], f2_same(-mean_now)), f2_same(rs)), first + i * step + 2 * j, some);
+                g[j] = f2_mul(d[j], wv[j]);
+            }
+        };
+        f2 xh[kKeep ? N : 1][H], g[kKeep ? N : 1][H], sg = 0, sx = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            f2 (&xi)[H] = xh[kKeep ? i : 0], (&gi)[H] = g[kKeep ? i : 0], d[H];
+            load(i, xi, d, gi);
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                dw[i][j] = f2_fma(d[j], xi[j], dw[i][j]);
                 db[i][j] = f2_add(db[i][j], d[j]);
-                sg = f2_add(sg, g[i][j]);
-                sx = f2_fma(g[i][j], xh[i][j], sx);
+                sg = f2_add(sg, gi[j]);
+                sx = f2_fma(gi[j], xi[j], sx);
             }
         }
         float s[2] = {f2_total(sg), f2_total(sx)};
-        team_sum<2>(s, a.warps, team, places, turn);
+        team_sum<2>(s, a.lanes, team, places, turn);
         const f2 mg = f2_same(-s[0] / (float)width), mx = f2_same(-s[1] / (float)width);
         T* dx = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            f2 t[H];
-            if constexpr (ADD) piece_wide<T>(ring.get(got * Q + 2 * N + i, r + (int64_t)row * a.rr, first + i * step, width), t);
+            f2 t[H], (&xi)[H] = xh[kKeep ? i : 0], (&gi)[H] = g[kKeep ? i : 0];
+            if constexpr (!kKeep) load(i, xi, t, gi);
+            if constexpr (ADD) piece_wide<T>(ring.get(got * Q + 2 * N + i, r + (int64_t)row * a.rr, first + i * step, some), t);
 #pragma unroll
             for (int j = 0; j < H; ++j) {
-                const f2 v = f2_add(f2_fma(xh[i][j], mx, g[i][j]), mg);
+                const f2 v = f2_add(f2_fma(xi[j], mx, gi[j]), mg);
                 t[j] = ADD ? f2_fma(v, f2_same(rs), t[j]) : f2_mul(v, f2_same(rs));
             }
-            piece_store<T, WIDE>(dx, first + i * step, width, piece_narrow<T>(t));
+            piece_store<T, WIDE>(dx, first + i * step, some, piece_narrow<T>(t));
         }
         got = got + 1 == S ? 0 : got + 1;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                      // the ring's place is free
     float* const joined = reinterpret_cast<float*>(ring_raw);
-    // the teams' sums, one team after another
-    float* part = a.part + ((uint64_t)k * gridDim.x + blockIdx.x) * 2 * width;
+    float* const part = a.part ? a.part + ((uint64_t)k * gridDim.x + blockIdx.x) * 2 * width : nullptr;
+    auto put_sum = [&](uint32_t which, uint32_t c, float v) {
+        if (part) part[which * width + c] = v;
+        else if (which) static_cast<T*>(a.db_out)[k * a.dbo + c] = from_f<T>(v);
+        else static_cast<T*>(a.dw_out)[k * a.dwo + c] = from_f<T>(v);
+    };
     auto each = [&](auto&& f) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -376,18 +400,28 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
                 if (c + 1 < width) f(c + 1, v, q);
             }
     };
+    // the teams of a warp, then those of the CTA, one after another
+    for (uint32_t d = a.lanes; d < 32; d *= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                dw[i][j] = f2_add(dw[i][j], __shfl_xor_sync(0xFFFFFFFFu, dw[i][j], d));
+                db[i][j] = f2_add(db[i][j], __shfl_xor_sync(0xFFFFFFFFu, db[i][j], d));
+            }
     if (teams == 1) {
-        each([&](uint32_t c, float u, float p) { part[c] = u; part[width + c] = p; });
+        each([&](uint32_t c, float u, float p) { put_sum(0, c, u); put_sum(1, c, p); });
         return;
     }
-    for (uint32_t t = 0; t < teams; ++t) {
-        if (t == team) {
+    const uint32_t turns = a.lanes <= 32 ? WARPS : teams, mine = a.lanes <= 32 ? threadIdx.x >> 5 : team;
+    for (uint32_t t = 0; t < turns; ++t) {
+        if (t == mine && beside == 0) {
             if (t == 0) each([&](uint32_t c, float u, float p) { joined[c] = u; joined[width + c] = p; });
             else each([&](uint32_t c, float u, float p) { joined[c] += u; joined[width + c] += p; });
         }
         __syncthreads();
     }
-    for (uint32_t c = threadIdx.x; c < 2 * width; c += blockDim.x) part[c] = joined[c];
+    for (uint32_t c = threadIdx.x; c < width; c += blockDim.x) { put_sum(0, c, joined[c]); put_sum(1, c, joined[width + c]); }
 }
 
 }  // namespace block

@@ -30,27 +30,28 @@ bool norm_wide(const palsgd_mat* m, size_t es)
     return !m || (aligned(m->data, 16) && (m->worker_stride * es) % 16 == 0 && (m->row_stride * es) % 16 == 0);
 }
 
-// Warps of a team, pieces a lane: the fewest warps of up to 8 whose lanes hold a row in `most` pieces each; beyond that 16 or
-// 32, with two pieces a lane of bfloat16 and four of fp32 (16 values: what 1024 threads have the registers for).
-struct Team { uint32_t warps, pieces; };
+// Lanes of a team, pieces a lane: the fewest lanes of up to 8 warps that hold a row in `most` pieces each, narrow rows in one
+// piece a lane (several rows a warp); beyond that 16 or 32 warps, with two pieces a lane of bfloat16 and four of fp32 (16
+// values: what 1024 threads have the registers for).
+struct Team { uint32_t lanes, pieces; };
 Team team_of(uint64_t width, size_t es, uint32_t most)
 {
     const uint64_t pieces = ceil_div(width * es, 16);
-    Team t{1, 0};
-    while (t.warps < 8 && pieces > (uint64_t)t.warps * 32 * most) t.warps *= 2;
-    if (pieces > 256ull * most) t.warps = pieces > 512 * es ? 32 : 16;
-    t.pieces = (uint32_t)ceil_div(pieces, t.warps * 32);
+    Team t{pieces <= 32 ? 4u : 32u, 0};
+    while (t.lanes < 256 && pieces > (uint64_t)t.lanes * (pieces <= 32 ? 1 : most)) t.lanes *= 2;
+    if (pieces > 256ull * most) t.lanes = pieces > 512 * es ? 1024 : 512;
+    t.pieces = (uint32_t)ceil_div(pieces, t.lanes);
     return t;
 }
+uint64_t teams_of(Team t) { return t.lanes <= 256 ? 256 / t.lanes : 1; }
 
 // CTAs of a worker: as many as run at a time, each team with as many rows as any other (but for the last turn).
 uint32_t norm_ctas(const palsgd_norm_shape* s, Team t, uint32_t per_sm)
 {
-    const uint64_t teams = t.warps <= 8 ? 8 / t.warps : 1;
-    uint64_t most = (uint64_t)per_sm * sm_count() / s->K;
+    uint64_t most = (uint64_t)(t.lanes > 256 ? 1 : per_sm) * sm_count() / s->K;
     if (most == 0) most = 1;
-    const uint64_t turns = ceil_div(s->tokens, most * teams);
-    const uint64_t n = turns ? ceil_div(s->tokens, turns * teams) : 1;
+    const uint64_t turns = ceil_div(s->tokens, most * teams_of(t));
+    const uint64_t n = turns ? ceil_div(s->tokens, turns * teams_of(t)) : 1;
     return (uint32_t)(n ? n : 1);
 }
 
@@ -65,12 +66,12 @@ int launch_norm(const NormArgs& a, dim3 grid, cudaStream_t st)
     void (*kernel)(NormArgs);
     if constexpr (BACK) kernel = norm_backward_kernel<T, N, WIDE, ADD, WARPS, kCtas>;
     else kernel = norm_forward_kernel<T, N, WIDE, ADD, WARPS, kCtas>;
-    const unsigned threads = WARPS == 8 ? 256 : a.warps * 32;
-    constexpr int kPieces = N * (BACK ? ADD ? 3 : 2 : ADD ? 2 : 1);
-    constexpr uint32_t kStage = norm_stage_bytes<T, WIDE>(kPieces, WARPS), kStages = norm_stages<T, WIDE>(kPieces, WARPS, kCtas);
+    const unsigned threads = WARPS == 8 ? 256 : a.lanes;
+    constexpr int kArrays = BACK ? ADD ? 3 : 2 : ADD ? 2 : 1;
+    constexpr uint32_t kStage = norm_stage_bytes<T, WIDE, N>(kArrays, WARPS), kStages = norm_stages<T, WIDE, N>(kArrays, WARPS, kCtas);
     static_assert(kStages >= 1, "room for a row");
     static_assert(!BACK || WARPS > 8 || kStage * kStages >= 2 * sizeof(float) * (WARPS / 2) * 32 * N * kPieceValues<T>, "room for the sums of two teams or more");
-    const size_t smem = WARPS == 8 ? kStage * kStages : kStage / WARPS * a.warps * kStages;
+    const size_t smem = WARPS == 8 ? kStage * kStages : kStage / (WARPS * 32) * threads * kStages;
     BLOCK_TRY(allow_smem(reinterpret_cast<const void*>(kernel), smem));
     return launch(BACK ? "layer norm backward" : "layer norm", kernel, grid, threads, smem, st, a);
 }
@@ -78,7 +79,7 @@ int launch_norm(const NormArgs& a, dim3 grid, cudaStream_t st)
 template <typename T, bool BACK, bool WIDE, bool ADD>
 int launch_norm(const NormArgs& a, Team t, dim3 grid, cudaStream_t st)
 {
-    if (t.warps > 8) return launch_norm<T, BACK, (int)sizeof(T), WIDE, ADD, 32>(a, grid, st);
+    if (t.lanes > 256) return launch_norm<T, BACK, (int)sizeof(T), WIDE, ADD, 32>(a, grid, st);
     if (t.pieces == 1) return launch_norm<T, BACK, 1, WIDE, ADD, 8>(a, grid, st);
     if constexpr (norm_most<BACK>() == 2) {
         return launch_norm<T, BACK, 2, WIDE, ADD, 8>(a, grid, st);
@@ -153,8 +154,8 @@ extern "C" int palsgd_layer_norm_forward(const palsgd_norm_shape* s, const palsg
     a.rows = M; a.width = (uint32_t)D; a.eps = (float)s->eps;
     const bool wide = (D * es) % 16 == 0 && norm_wide(x, es) && norm_wide(r, es) && norm_wide(w, es) && norm_wide(b, es) && norm_wide(y, es) && norm_wide(total, es);
     const Team t = team_of(D, es, norm_most<false>());
-    a.warps = t.warps;
-    const dim3 grid(norm_ctas(s, t, t.warps > 8 ? 1 : norm_ctas_per_sm<false>()), s->K);
+    a.lanes = t.lanes;
+    const dim3 grid(norm_ctas(s, t, norm_ctas_per_sm<false>()), s->K);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return es == 4 ? launch_norm<float, false>(a, t, wide, r.given, grid, st) : launch_norm<bf16, false>(a, t, wide, r.given, grid, st);
 }
@@ -180,9 +181,10 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     BLOCK_TRY(check_mat(db, s->K, 1, D, es, true));
     BLOCK_TRY(check_workspace(workspace, workspace_bytes));
     const Team t = team_of(D, es, norm_most<true>());
-    const uint32_t ctas = norm_ctas(s, t, t.warps > 8 ? 1 : norm_ctas_per_sm<true>());
+    // (four rows a team: as long as the launch of the kernel that joins what several CTAs leave)
+    const uint32_t ctas = s->tokens <= 4 * teams_of(t) ? 1 : norm_ctas(s, t, norm_ctas_per_sm<true>());
     Arena ws{static_cast<char*>(workspace), 0};
-    float* part = static_cast<float*>(ws.take((size_t)s->K * ctas * 2 * D * sizeof(float)));
+    float* part = ctas > 1 ? static_cast<float*>(ws.take((size_t)s->K * ctas * 2 * D * sizeof(float))) : nullptr;
     Regions all;
     all.reads(region(dy, s->K, M, D, es)); all.reads(region(x, s->K, M, D, es)); all.reads(region(w, s->K, 1, D, es));
     all.reads(region(mean, s->K, 1, M, 4)); all.reads(region(rstd, s->K, 1, M, 4)); all.reads(region(past, s->K, M, D, es));
@@ -198,11 +200,13 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     a.mean = static_cast<float*>(mean.m.data); a.mw = mean.m.worker_stride;
     a.rstd = static_cast<float*>(rstd.m.data); a.sw = rstd.m.worker_stride;
     a.part = part;
-    a.rows = M; a.width = (uint32_t)D; a.warps = t.warps;
+    a.dw_out = dw.m.data; a.dwo = dw.m.worker_stride; a.db_out = db.m.data; a.dbo = db.m.worker_stride;
+    a.rows = M; a.width = (uint32_t)D; a.lanes = t.lanes;
     const bool wide = (D * es) % 16 == 0 && norm_wide(dy, es) && norm_wide(x, es) && norm_wide(w, es) && norm_wide(past, es) && norm_wide(dx, es);
     const dim3 grid(ctas, s->K);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     BLOCK_TRY((es == 4 ? launch_norm<float, true>(a, t, wide, past.given, grid, st) : launch_norm<bf16, true>(a, t, wide, past.given, grid, st)));
+    if (!part) return PALSGD_OK;
     ColumnSumArgs c{part, {dw.m.data, db.m.data}, {dw.m.worker_stride, db.m.worker_stride}, ctas, (uint32_t)(2 * D), (uint32_t)D};
     const dim3 columns((unsigned)ceil_div(2 * D, 32), s->K);
     return launch("layer norm weight gradients", es == 4 ? column_sum_kernel<float> : column_sum_kernel<bf16>, columns, 256, 0, st, c);
