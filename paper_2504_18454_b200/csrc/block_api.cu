@@ -374,9 +374,10 @@ void take_shares(Arena& ws, Product* p, int n, uint32_t K, uint32_t parts)
 
 // The products of a call in one launch, the longer ones first, and the kernel that joins what was cut (unless the caller has
 // one of its own).
-int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, size_t es, uint32_t parts, cudaStream_t st, bool joined = true)
+int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, size_t es, uint32_t parts, cudaStream_t st, bool joined = true, const MatSums* sums = nullptr)
 {
     MatLaunch L{};
+    if (sums) L.sums = *sums;
     JoinArgs join{};
     uint32_t joins = 0;
     uint64_t units = 0;
@@ -494,7 +495,18 @@ int with_act(int act, F&& f)
     }
 }
 
-// Up to eight tokens.  The inner axis is cut into slices for the CTA's warps while there are fewer CTAs than the device
+// Whether a call goes to the kernel of few tokens: up to eight, or so little work that the matrix kernel would take longer to
+// start than this one takes in all.  (Measured at 256 x 683, fp32, 4 x 17 tokens: matrix kernel 29 us; see kFewWork.)
+constexpr uint64_t kFewWorkBf16 = 60000000, kFewWorkFp32 = 200000000;   // multiplications, tokens in whole eights
+bool few_tokens(const palsgd_linear_shape* s)
+{
+    const uint64_t tiles = ceil_div(s->tokens, kFewTokens);
+    if (tiles <= 1) return true;
+    if (tiles > 65535 || s->d_in > (1u << 20) || s->d_out > (1u << 20) || s->tokens > (1u << 16)) return false;     // (no product below overflows)
+    return tiles * kFewTokens * s->K * s->d_in * s->d_out <= (s->precision == PALSGD_PREC_FP32 ? kFewWorkFp32 : kFewWorkBf16);
+}
+
+// Few tokens.  The inner axis is cut into slices for the CTA's warps while there are fewer CTAs than the device
 // holds at a time and a slice keeps a step of its own; an 8-bit checkpoint's group is 32 columns of one CTA.
 template <typename T>
 int run_few(const palsgd_linear_shape* s, const palsgd_mat* x, const palsgd_mat* w, const LinearEnd& end, cudaStream_t st)
@@ -503,10 +515,10 @@ int run_few(const palsgd_linear_shape* s, const palsgd_mat* x, const palsgd_mat*
     FewArgs a{x->data, w->data, x->worker_stride, x->row_stride, w->worker_stride, w->row_stride, (uint32_t)s->tokens, (uint32_t)s->d_out, (uint32_t)s->d_in, 8, 0, s->activation, end};
     const uint64_t steps = ceil_div(s->d_in, kStep);
     const uint32_t full = 4 * (uint32_t)sm_count();
-    while (s->save != PALSGD_SAVE_8BIT && a.groups > 1 && steps >= 2 * (8 / a.groups) && s->K * ceil_div(s->d_out, a.groups * kFewRows) < full) a.groups /= 2;
+    while (s->save != PALSGD_SAVE_8BIT && a.groups > 1 && steps >= 2 * (8 / a.groups) && s->K * ceil_div(s->tokens, kFewTokens) * ceil_div(s->d_out, a.groups * kFewRows) < full) a.groups /= 2;
     a.slice = (uint32_t)(ceil_div(steps, 8 / a.groups) * kStep);
     const bool wide = s->d_in * sizeof(T) % 16 == 0 && out_of(x, 0, sizeof(T)).wide && out_of(w, 0, sizeof(T)).wide;
-    const dim3 grid((unsigned)ceil_div(s->d_out, a.groups * kFewRows), s->K);
+    const dim3 grid((unsigned)ceil_div(s->d_out, a.groups * kFewRows), s->K, (unsigned)ceil_div(s->tokens, kFewTokens));
     auto go = [&](auto mt) { return launch("linear, few tokens", wide ? few_kernel<T, mt, true> : few_kernel<T, mt, false>, grid, 256, 0, st, a); };
     return a.M <= 1 ? go(std::integral_constant<int, 1>{}) : a.M <= 2 ? go(std::integral_constant<int, 2>{})
          : a.M <= 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 8>{});
@@ -535,7 +547,7 @@ uint32_t slope_lanes(const palsgd_linear_shape* s)
 uint32_t slope_rows(const palsgd_linear_shape* s)
 {
     const uint32_t lanes = slope_lanes(s);
-    const uint64_t strips = ceil_div(s->d_out, lanes * 8) * s->K, want = ceil_div(3ull * sm_count(), strips), turn = 8 * (32 / lanes), least = 4 * turn;
+    const uint64_t strips = ceil_div(s->d_out, lanes * 8) * s->K, run = 3ull * sm_count() / strips, want = run ? run : 1, turn = 8 * (32 / lanes), least = 4 * turn;
     if (s->tokens <= 2 * least) return (uint32_t)s->tokens;
     uint64_t rows = ceil_div(s->tokens, want);
     if (rows < least) rows = least;
@@ -544,13 +556,23 @@ uint32_t slope_rows(const palsgd_linear_shape* s)
 }
 
 template <typename T>
-int run_slope(const palsgd_linear_shape* s, const SlopeArgs& a, cudaStream_t st)
+int run_slope(const palsgd_linear_shape* s, SlopeArgs& a, const Stage& copies, int sms, cudaStream_t st)
 {
-    const dim3 grid((unsigned)ceil_div(s->d_out, a.lanes * 8), (unsigned)ceil_div(s->tokens, a.rows), s->K);
+    a.strips = (uint32_t)ceil_div(s->d_out, a.lanes * 8);
+    const uint64_t ctas = a.strips * ceil_div(s->tokens, a.rows);
+    if (ctas > 0x3FFFFFFFull) return PALSGD_EUNSUPPORTED;
+    uint32_t all = a.ctas = (uint32_t)ctas;
+    for (uint32_t i = 0; i < kMaxStaged; ++i) {
+        a.first_copy[i] = all;
+        const uint64_t want = i < copies.n ? ceil_div(copies.a.item[i].units, 512) : 0, cap = 8ull * sms;
+        all += (uint32_t)(want < cap ? want : cap);
+    }
+    a.first_copy[kMaxStaged] = all;
+    const dim3 grid(all, s->K);
     return with_act(s->activation, [&](auto act) {
         if constexpr (act != PALSGD_ACT_NONE)
-            if (s->save == PALSGD_SAVE_8BIT) return launch("linear, gradient before the activation", slope_kernel<T, act, true>, grid, 256, 0, st, a);
-        return launch("linear, gradient before the activation", slope_kernel<T, act, false>, grid, 256, 0, st, a);
+            if (s->save == PALSGD_SAVE_8BIT) return launch("linear, gradient before the activation", slope_kernel<T, act, true>, grid, 256, 0, st, a, copies.a);
+        return launch("linear, gradient before the activation", slope_kernel<T, act, false>, grid, 256, 0, st, a, copies.a);
     });
 }
 
@@ -883,7 +905,7 @@ extern "C" int palsgd_linear_forward(const palsgd_linear_shape* s, const palsgd_
     Arena ws{static_cast<char*>(workspace), 0};
     Stage stage;
     const uint32_t parts = s->precision == PALSGD_PREC_FP32 ? 3 : 1;
-    const bool few = M <= kFewTokens;
+    const bool few = few_tokens(s);
     Operand ox, ow;
     Product product{M, N, D, &ox, nullptr, &ow, nullptr, false, false, y, 1, nullptr};
     if (!few) {
@@ -962,8 +984,9 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
         pass = write || db.given;
         slope.rows = slope_rows(s);
         slope.lanes = slope_lanes(s);
+        slope.part_ld = (uint32_t)N;
         if (db.given && slope.rows >= M) { slope.db = db.m.data; slope.dbw = db.m.worker_stride; }
-        else if (db.given) slope.part = static_cast<float*>(ws.take((size_t)s->K * ceil_div(M, slope.rows) * N * sizeof(float)));
+        else if (db.given) slope.part = static_cast<float*>(ws.take((size_t)s->K * ceil_div(M, slope.rows) * slope.part_ld * sizeof(float)));
         ox = input_operand(ws, stage, x, x_e, s->precision, s->K, M, D);
         if (dx.given) {
             ow = input_operand(ws, stage, w, nullptr, s->precision, s->K, N, D);
@@ -984,7 +1007,6 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
     }
     Device dev{};
     BLOCK_TRY(device_of(dev));
-    BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     if (pass) {
         slope.dy = dy.m.data; slope.dw = dy.m.worker_stride; slope.dr = dy.m.row_stride;
         slope.dy_wide = out_of(dy, N, es).wide;
@@ -995,14 +1017,13 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
             if (eight) { slope.pre_e = static_cast<const uint8_t*>(pre_e.m.data); slope.ew = pre_e.m.worker_stride; slope.er = pre_e.m.row_stride; }
         }
         slope.M = (uint32_t)M; slope.N = (uint32_t)N;
-        BLOCK_TRY(es == 4 ? run_slope<float>(s, slope, st) : run_slope<bf16>(s, slope, st));
-    }
-    if (slope.part) {
-        ColumnSumArgs c{slope.part, {db.m.data, nullptr}, {db.m.worker_stride, 0}, (uint32_t)ceil_div(M, slope.rows), (uint32_t)N, (uint32_t)N};
-        BLOCK_TRY(launch("linear, bias gradient", es == 4 ? column_sum_kernel<float> : column_sum_kernel<bf16>, dim3((unsigned)ceil_div(N, 32), s->K), 256, 0, st, c));
+        BLOCK_TRY(es == 4 ? run_slope<float>(s, slope, stage, dev.sms, st) : run_slope<bf16>(s, slope, stage, dev.sms, st));
+    } else {
+        BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     }
     const palsgd_ffn_shape f = products_of(s);
-    return run_products(products, n_products, &f, dev, es, parts, st);
+    const MatSums sums{slope.part, db.m.data, db.m.worker_stride, slope.part ? (uint32_t)ceil_div(M, slope.rows) : 0, (uint32_t)N, slope.part_ld, s->K};
+    return run_products(products, n_products, &f, dev, es, parts, st, true, &sums);
 }
 
 extern "C" int palsgd_block_status(void* stream)

@@ -5,38 +5,40 @@
 namespace palsgd {
 namespace block {
 
-// Rows of binary32 sums [K][parts][cols], joined in a fixed order: the columns of up to two results lie behind one another.
+// Rows of binary32 sums [K][parts][ld], ld a multiple of four, joined in a fixed order: a thread has four columns and every
+// eighth row.  The columns of two results lie behind one another.
 struct ColumnSumArgs {
     const float* part;
-    void*    out[2];              // columns 0 .. split-1, and the rest; may be NULL
+    void*    out[2];              // columns 0 .. split-1, and the rest
     int64_t  ow[2];               // worker strides
-    uint32_t parts, cols, split;
+    uint32_t parts, cols, ld, split;
 };
 template <typename T>
 __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ ColumnSumArgs a)
 {
-    __shared__ float run[8][32];
+    __shared__ float4 run[8][32];
     let_next_start();
     wait_for_previous();
-    const uint32_t k = blockIdx.y, lane = threadIdx.x & 31, r = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
-    const float* p = a.part + (uint64_t)k * a.parts * a.cols;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (i < a.cols) {
-        uint32_t b = r;
-        for (; b + 24 < a.parts; b += 32)
-#pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) v[j] += p[(uint64_t)(b + 8 * j) * a.cols + i];
-        for (; b < a.parts; b += 8) v[0] += p[(uint64_t)b * a.cols + i];
+    const uint32_t k = blockIdx.y, lane = threadIdx.x & 31, r = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * 4;
+    const float* p = a.part + (uint64_t)k * a.parts * a.ld + c;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (c < a.cols) {
+#pragma unroll 4
+        for (uint32_t b = r; b < a.parts; b += 8) {
+            const float4 t = __ldg(reinterpret_cast<const float4*>(p + (uint64_t)b * a.ld));
+            v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+        }
     }
-    run[r][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+    run[r][lane] = v;
     __syncthreads();
-    if (r == 0 && i < a.cols) {
-        float t = 0.0f;
+    if (threadIdx.x >= 128) return;
+    const uint32_t i = blockIdx.x * 128 + threadIdx.x;
+    if (i >= a.cols) return;
+    float t = 0.0f;
 #pragma unroll
-        for (int b = 0; b < 8; ++b) t += run[b][lane];
-        const uint32_t which = i >= a.split;
-        if (a.out[which]) static_cast<T*>(a.out[which])[(int64_t)k * a.ow[which] + i - (which ? a.split : 0)] = from_f<T>(t);
-    }
+    for (int b = 0; b < 8; ++b) t += reinterpret_cast<const float*>(run[b])[threadIdx.x];
+    const uint32_t which = i >= a.split;
+    static_cast<T*>(a.out[which])[(int64_t)k * a.ow[which] + i - (which ? a.split : 0)] = from_f<T>(t);
 }
 
 }  // namespace block

@@ -13,7 +13,7 @@ struct LinearEnd {                // what follows the sums
 
 // ---------------------------------------------------------------------------------------------- few tokens
 //
-// Up to eight tokens: bound by reading the weights once.  A warp takes four rows of w over its slice of the inner axis, in
+// Up to eight tokens at a time: bound by reading the weights once (for more tokens, by the multiplications: small calls).  A warp takes four rows of w over its slice of the inner axis, in
 // pieces of 16 bytes a lane, and multiplies each with all of the tokens in binary32 (the tokens come from the caches).  A CTA's
 // eight warps are `rows` row groups by slices; slices are joined in shared memory in order, and one thread finishes each
 // value.  (The matrix kernel's tile of one token multiplies 255 rows of zeros, and a few outputs give it too few tiles.)
@@ -50,10 +50,10 @@ __global__ void __launch_bounds__(256, MT >= 4 ? 2 : 3) few_kernel(const __grid_
     __shared__ float sums[8][C];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp % a.groups, slice = warp / a.groups;
     const int64_t k = blockIdx.y;
-    const uint32_t n0 = blockIdx.x * a.groups * kFewRows;
+    const uint32_t n0 = blockIdx.x * a.groups * kFewRows, m0 = blockIdx.z * MT, M = min(a.M - m0, (uint32_t)MT);
     let_next_start();
     wait_for_previous();
-    const T *x = static_cast<const T*>(a.x) + k * a.xw, *w[kFewRows];
+    const T *x = static_cast<const T*>(a.x) + k * a.xw + (int64_t)m0 * a.xr, *w[kFewRows];
 #pragma unroll
     for (uint32_t r = 0; r < kFewRows; ++r)               // (rows past the end: the last one, and their sums are not used)
         w[r] = static_cast<const T*>(a.w) + k * a.ww + (int64_t)min(n0 + group * kFewRows + r, a.N - 1) * a.wr;
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(256, MT >= 4 ? 2 : 3) few_kernel(const __grid_
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 f2 xv[H];
-                widen((uint32_t)m < a.M && c0 + u * kStep < last ? piece(x + (int64_t)m * a.xr, c) : make_uint4(0, 0, 0, 0), xv);
+                widen((uint32_t)m < M && c0 + u * kStep < last ? piece(x + (int64_t)m * a.xr, c) : make_uint4(0, 0, 0, 0), xv);
 #pragma unroll
                 for (uint32_t r = 0; r < kFewRows; ++r)
 #pragma unroll
@@ -121,12 +121,12 @@ __global__ void __launch_bounds__(256, MT >= 4 ? 2 : 3) few_kernel(const __grid_
     if (lane % (32 / C) == 0) sums[warp][lane / (32 / C)] = v[0];
     __syncthreads();
     // one thread for each value: column of the CTA's, token
-    const uint32_t cols = a.groups * kFewRows, col = threadIdx.x % cols, m = threadIdx.x / cols, n = n0 + col;
-    const bool on = m < a.M && n < a.N;
+    const uint32_t cols = a.groups * kFewRows, col = threadIdx.x % cols, t = threadIdx.x / cols, m = m0 + t, n = n0 + col;
+    const bool on = t < M && n < a.N;
     const LinearEnd& e = a.end;
     float z = 0.0f;
     if (on) {
-        const uint32_t at = (col % kFewRows) * MT + m;
+        const uint32_t at = (col % kFewRows) * MT + t;
         z = sums[col / kFewRows][at];
         for (uint32_t s = 1; s < 8 / a.groups; ++s) z += sums[s * a.groups + col / kFewRows][at];
         if (e.bias.p) z += to_f(static_cast<const T*>(e.bias.p)[k * e.bias.w + n]);
@@ -229,81 +229,116 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
 
 // dz = dy act'(z) as the products' operand (bfloat16, or fp32 in three parts; dst NULL: dy itself is the operand), and its
 // sums over a CTA's rows, unrounded, to the CTA's row of `part` -- or, where one CTA has all rows, the gradient of the bias
-// itself.  `lanes` lanes have a row side by side, eight columns each, and a warp 32 / lanes rows.
+// itself.  `lanes` lanes have a row side by side, eight columns each, and a warp 32 / lanes rows.  Bound by memory; a lane has
+// as many rows under way as it has registers for.  The copies of other operands ride along in CTAs of their own.
 struct SlopeArgs {
     const void *dy, *pre;         // pre: NULL without an activation
     const uint8_t* pre_e;         // 8 bits
     int64_t  dw, dr, pw, pr, ew, er;
     bf16*    dst;
     int64_t  dstw, ld, dst_part;  // worker, row and part strides
-    float*   part;                // [K][row CTAs][N]; NULL: none wanted, or `db` is written
+    float*   part;                // [K][row CTAs][part_ld]; NULL: none wanted, or `db` is written
     void*    db;
     int64_t  dbw;
     uint32_t M, N, rows;          // rows of a CTA
-    uint32_t lanes;
+    uint32_t lanes, strips, ctas, part_ld;               // CTAs across, CTAs of a worker
     int      dy_wide, pre_wide;
+    uint32_t first_copy[kMaxStaged + 1];                  // CTAs of the copies, behind those
+};
+
+// Eight values of a row as they lie in memory
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16> {
+    uint4 q;
+    __device__ __forceinline__ void load(const bf16* p, uint32_t n, bool wide) { q = wide && n == 8 ? __ldg(reinterpret_cast<const uint4*>(p)) : get16(reinterpret_cast<const unsigned char*>(p), 2 * n); }
+    __device__ __forceinline__ void get(f2 (&v)[4]) const { v[0] = f2_wide(q.x); v[1] = f2_wide(q.y); v[2] = f2_wide(q.z); v[3] = f2_wide(q.w); }
+};
+template <> struct Raw8<float> {
+    f2 r[4];
+    __device__ __forceinline__ void load(const float* p, uint32_t n, bool wide) { row8_load(p, n, wide, r); }
+    __device__ __forceinline__ void get(f2 (&v)[4]) const { v[0] = r[0]; v[1] = r[1]; v[2] = r[2]; v[3] = r[3]; }
+};
+struct RawAct8 {
+    uint2    q;
+    uint32_t e;
+    __device__ __forceinline__ void load(const unsigned char* p, const uint8_t* exponent, uint32_t n, bool wide)
+    {
+        if (wide && n == 8) { q = __ldg(reinterpret_cast<const uint2*>(p)); }
+        else { const uint4 t = get16(p, n); q = make_uint2(t.x, t.y); }
+        e = n ? *exponent : 127u;
+    }
+    __device__ __forceinline__ void get(f2 (&v)[4]) const
+    {
+        const float s = act8_step(e);
+        float f[8];
+        act8_value4(q.x, s, f);
+        act8_value4(q.y, s, f + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = f2_of(f[2 * i], f[2 * i + 1]);
+    }
 };
 
 template <typename T, int ACT, bool EIGHT>
-__global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ SlopeArgs a)
+__global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ SlopeArgs a, const __grid_constant__ StageArgs copies)
 {
-    constexpr int U = 2;                                  // rows of a lane under way
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;             // rows of a lane under way
     __shared__ float sums[8][256];
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, abreast = 32 / a.lanes;
-    const uint32_t local = (lane % a.lanes) * 8, c = blockIdx.x * a.lanes * 8 + local;
-    const int64_t k = blockIdx.z;
-    const uint32_t n = c < a.N ? min(a.N - c, 8u) : 0;
-    const bool room = a.dst && c < a.ld;                  // (the operand's rows hold a multiple of eight columns)
-    const uint32_t first = blockIdx.y * a.rows, last = min(a.M, first + a.rows), step = 8 * abreast;
+    const int64_t k = blockIdx.y;
     let_next_start();
     wait_for_previous();
+    if (blockIdx.x >= a.ctas) {
+        uint32_t i = 0;
+        while (blockIdx.x >= a.first_copy[i + 1]) ++i;
+        stage_item(copies.item[i], k, blockIdx.x - a.first_copy[i], a.first_copy[i + 1] - a.first_copy[i]);
+        return;
+    }
+    const uint32_t chunk = blockIdx.x / a.strips, strip = blockIdx.x - chunk * a.strips;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, abreast = 32 / a.lanes;
+    const uint32_t local = (lane % a.lanes) * 8, c = strip * a.lanes * 8 + local;
+    const uint32_t n = c < a.N ? min(a.N - c, 8u) : 0;
+    const bool room = a.dst && c < a.ld;                  // (the operand's rows hold a multiple of eight columns)
+    const uint32_t first = chunk * a.rows, last = min(a.M, first + a.rows), step = 8 * abreast;
     f2 sum[4] = {0, 0, 0, 0};
 #pragma unroll 1
     for (uint32_t r0 = first + warp * abreast + lane / a.lanes; r0 < last; r0 += U * step) {
-        f2 d[U][4], z[U][4];
+        Raw8<T> dr[U];
+        Raw8<T> zr[U];
+        RawAct8 qr[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t r = r0 + u * step;
             const uint32_t m = r0 + u * step < last ? n : 0;
-            row8_load(static_cast<const T*>(a.dy) + k * a.dw + r * a.dr + c, m, a.dy_wide, d[u]);
+            dr[u].load(static_cast<const T*>(a.dy) + k * a.dw + r * a.dr + c, m, a.dy_wide);
             if constexpr (ACT != PALSGD_ACT_NONE) {
-                if constexpr (EIGHT) {
-                    const unsigned char* p = static_cast<const unsigned char*>(a.pre) + k * a.pw + r * a.pr + c;
-                    uint2 q;
-                    if (a.pre_wide && m == 8) q = __ldg(reinterpret_cast<const uint2*>(p));
-                    else { const uint4 t = get16(p, m); q = make_uint2(t.x, t.y); }
-                    const float s = act8_step(m ? a.pre_e[k * a.ew + r * a.er + c / 32] : 127u);
-                    float v[8];
-                    act8_value4(q.x, s, v);
-                    act8_value4(q.y, s, v + 4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[u][i] = f2_of(v[2 * i], v[2 * i + 1]);
-                } else {
-                    row8_load(static_cast<const T*>(a.pre) + k * a.pw + r * a.pr + c, m, a.pre_wide, z[u]);
-                }
+                if constexpr (EIGHT) qr[u].load(static_cast<const unsigned char*>(a.pre) + k * a.pw + r * a.pr + c, a.pre_e + k * a.ew + r * a.er + c / 32, m, a.pre_wide);
+                else zr[u].load(static_cast<const T*>(a.pre) + k * a.pw + r * a.pr + c, m, a.pre_wide);
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (r0 + u * step >= last) break;
+            f2 d[4], z[4];
+            dr[u].get(d);
             if constexpr (ACT != PALSGD_ACT_NONE) {
+                if constexpr (EIGHT) qr[u].get(z);
+                else zr[u].get(z);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     f2 slope;
-                    act_pair<T, ACT, true>(z[u][i], slope);
-                    d[u][i] = f2_mul(d[u][i], slope);     // (what lies behind the row's end is used nowhere)
+                    act_pair<T, ACT, true>(z[i], slope);
+                    d[i] = f2_mul(d[i], slope);           // (what lies behind the row's end is used nowhere)
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = f2_add(sum[i], d[u][i]);
+            for (int i = 0; i < 4; ++i) sum[i] = f2_add(sum[i], d[i]);
             if (room) {
                 bf16* to = a.dst + k * a.dstw + (int64_t)(r0 + u * step) * a.ld + c;
                 if constexpr (sizeof(T) == 2) {
-                    *reinterpret_cast<uint4*>(to) = make_uint4(f2_narrow(d[u][0]), f2_narrow(d[u][1]), f2_narrow(d[u][2]), f2_narrow(d[u][3]));
+                    *reinterpret_cast<uint4*>(to) = make_uint4(f2_narrow(d[0]), f2_narrow(d[1]), f2_narrow(d[2]), f2_narrow(d[3]));
                 } else {
                     float v[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) f2_get(d[u][i], v[2 * i], v[2 * i + 1]);
+                    for (int i = 0; i < 4; ++i) f2_get(d[i], v[2 * i], v[2 * i + 1]);
                     three_parts<8>(v, [&](int part, const uint32_t (&w)[4]) { *reinterpret_cast<uint4*>(to + part * a.dst_part) = make_uint4(w[0], w[1], w[2], w[3]); });
                 }
             }
@@ -323,12 +358,12 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ S
         }
     }
     __syncthreads();
-    const uint32_t at = blockIdx.x * a.lanes * 8 + threadIdx.x;
+    const uint32_t at = strip * a.lanes * 8 + threadIdx.x;
     if (threadIdx.x >= a.lanes * 8 || at >= a.N) return;
     float t = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
-    if (a.part) a.part[((uint64_t)k * gridDim.y + blockIdx.y) * a.N + at] = t;
+    if (a.part) a.part[((uint64_t)k * (a.ctas / a.strips) + chunk) * a.part_ld + at] = t;
     else static_cast<T*>(a.db)[k * a.dbw + at] = from_f<T>(t);
 }
 

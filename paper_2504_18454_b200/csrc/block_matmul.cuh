@@ -73,8 +73,17 @@ struct alignas(64) MatProblem {
     MatOut   out[3];              // plain: the product; gate/up: h; hidden: dg, du, h; linear: y
 };
 
+// Rows of binary32 sums [K][parts][ld] that other CTAs have left, joined in a fixed order beside the products.
+struct MatSums {
+    const float* part;            // NULL: none
+    void*    out;
+    int64_t  w;                   // worker stride of out
+    uint32_t parts, cols, ld, K;
+};
+
 struct MatLaunch {
     MatProblem p[kMaxProblems];
+    MatSums  sums;                // plain
     uint32_t n_problems, tiles, heavy, lag;   // see Order
     int      save;
     MatOut   gate, up;            // saved (gate/up pass) or read (hidden pass)
@@ -610,6 +619,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 });
             }
         }
+    } else if (warp == 2) {
+        // plain: the sums of a bias gradient, 32 columns at a time (a kernel of its own for them took 4 us)
+        if constexpr (MODE == MAT_PLAIN) {
+            const MatSums& q = a.sums;
+            const uint32_t groups = (q.cols + 31) / 32, all = q.part ? groups * q.K : 0;
+            for (uint32_t g = blockIdx.x; g < all; g += gridDim.x) {
+                const uint32_t k = g / groups, c = (g - k * groups) * 32 + lane;
+                if (c >= q.cols) continue;
+                const float* at = q.part + (uint64_t)k * q.parts * q.ld + c;
+                float v[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) v[i] = 0.0f;
+                for (uint32_t r = 0; r < q.parts; r += 8)
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) if (r + i < q.parts) v[i] += at[(uint64_t)(r + i) * q.ld];
+                static_cast<T*>(q.out)[(int64_t)k * q.w + c] = from_f<T>(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+            }
+            __syncwarp();
+        }
     } else if (warp >= 4) {
         const uint32_t quad = warp & 3, part = (warp - 4) >> 2;           // tensor memory rows of 32; share of the columns
         uint32_t it = 0;
@@ -664,6 +692,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             const uint32_t m = tl.m0 + rank * 128 + quad * 32, rows = m < p.M ? min(p.M - m, 32u) : 0;
             const int64_t w = tl.worker;
             uint32_t src = tmem + (it & 1) * kTileN + (quad << 21) + part * kMine;
+            float bias[2] = {0.0f, 0.0f};                                 // linear: of the warp's columns lane and lane + 32
+            if constexpr (MODE == MAT_LINEAR) {
+                if (a.bias.p) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 2; ++i) {
+                        const uint32_t n = tl.n0 + part * kMine + 32 * i + lane;
+                        if (n < p.N) bias[i] = to_f(static_cast<const T*>(a.bias.p)[w * a.bias.w + n]);
+                    }
+                }
+            }
             // (a warp whose rows or columns are all outside has nothing to do but to let the sums go)
             const bool idle = (MODE == MAT_PLAIN || MODE == MAT_LINEAR) && (rows == 0 || tl.n0 + part * kMine >= p.N);
             if (!cut) {
@@ -731,33 +769,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 if constexpr (MODE == MAT_LINEAR) if (a.residual.p && o.then() < a.tiles) fetch_residual(tile_at<MODE>(a, o.then()), 0);
                 continue;
             }
-            // linear: z = the sums + bias of 16 columns, from the tile's column j on
-            auto linear_z = [&](uint32_t j, f2* z) {
-                float v[16];
-                tmem_load16(src + j, v);
-                const uint32_t n = tl.n0 + part * kMine + j;
-                f2 b[8];
-                if (a.bias.p) {
-                    const T* at = static_cast<const T*>(a.bias.p) + w * a.bias.w + n;
-                    if (n + 16 <= p.N && a.bias.wide) {
-                        row8_load(at, 8, true, *reinterpret_cast<f2(*)[4]>(b));
-                        row8_load(at + 8, 8, true, *reinterpret_cast<f2(*)[4]>(b + 4));
-                    } else {
+            // linear: z = the sums + bias of a block, from the tile's column j on.  (The lanes hold a bias each: loaded where it is
+            // needed, its latency stood in every block's way.)
+            auto linear_z = [&](uint32_t j, f2 (&z)[kCols / 2]) {
+                float v[kCols];
 #pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i)
-                            b[i] = f2_of(n + 2 * i < p.N ? to_f(at[2 * i]) : 0.0f, n + 2 * i + 1 < p.N ? to_f(at[2 * i + 1]) : 0.0f);
-                    }
-                }
+                for (uint32_t i = 0; i < kCols; i += 16) tmem_load16(src + j + i, *reinterpret_cast<float(*)[16]>(v + i));
+                const float mine = j < 32 ? bias[0] : bias[1];
                 tmem_load_wait();
+                if (a.bias.p) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    z[i] = f2_of(v[2 * i], v[2 * i + 1]);
-                    if (a.bias.p) z[i] = f2_add(z[i], b[i]);
+                    for (uint32_t i = 0; i < kCols; ++i) v[i] += __shfl_sync(0xFFFFFFFFu, mine, (j & 31) + i);
                 }
-            };
-            auto linear_top = [](float top, const f2* z) {                // the largest magnitude of 16 columns and `top`
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (uint32_t i = 0; i < kCols / 2; ++i) z[i] = f2_of(v[2 * i], v[2 * i + 1]);
+            };
+            auto linear_top = [](float top, const f2 (&z)[kCols / 2]) {   // the largest magnitude of a block and `top`
+#pragma unroll
+                for (uint32_t i = 0; i < kCols / 2; ++i) {
                     float x, y;
                     f2_get(z[i], x, y);
                     top = act8_max(act8_max(top, x), y);
@@ -807,16 +836,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     // z of the block in registers; what is saved, then y, pass through one block; the residual comes into the
                     // other one while the products of the tile, or the work on the block before, still run
                     f2 z[kCols / 2];
-#pragma unroll
-                    for (uint32_t j = 0; j < kCols; j += 16) linear_z(c * kCols + j, z + j / 2);
+                    linear_z(c * kCols, z);
                     if (a.save != PALSGD_SAVE_NONE) {
                         if (eight) {
                             if (E == 2 || c % 2 == 0) {                   // a group of 32 columns begins
                                 float top = linear_top(0.0f, z);
-                                if constexpr (E == 2) {
-                                    top = linear_top(top, z + 8);
-                                } else {
-                                    f2 more[8];
+                                if constexpr (E == 4) {
+                                    f2 more[kCols / 2];
                                     linear_z((c + 1) * kCols, more);
                                     top = linear_top(top, more);
                                 }
@@ -1033,14 +1059,11 @@ struct StageItem {
 };
 struct StageArgs { StageItem item[kMaxStaged]; };
 
-__global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ StageArgs a)
+// Block `block` of the `blocks` that copy worker k's part of an item.
+__device__ __forceinline__ void stage_item(const StageItem& it, int64_t k, uint32_t block, uint32_t blocks)
 {
-    let_next_start();
-    wait_for_previous();
-    const StageItem& it = a.item[blockIdx.y];
-    const int64_t k = blockIdx.z;
     if (k >= it.K) return;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < it.units; i += (uint64_t)gridDim.x * 256) {
+    for (uint64_t i = (uint64_t)block * 256 + threadIdx.x; i < it.units; i += (uint64_t)blocks * 256) {
         const uint64_t row = it.units < 0x80000000ull ? it.per_row.of((uint32_t)i) : i / it.per_row.d;
         const uint32_t c = (uint32_t)(i - row * it.per_row.d) * 8;
         const int64_t from = k * it.w + (int64_t)row * it.r + c;
@@ -1074,6 +1097,13 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
             Vec<bf16, 8>::store(to, v);
         }
     }
+}
+
+__global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ StageArgs a)
+{
+    let_next_start();
+    wait_for_previous();
+    stage_item(a.item[blockIdx.y], blockIdx.z, blockIdx.x, gridDim.x);
 }
 
 // The shares' sums of a product, joined in a fixed order.

@@ -17,12 +17,13 @@ struct NormArgs {
     const void *w, *b, *dy;
     void *y, *total;              // backward: y is dx
     float *mean, *rstd;           // forward: may be NULL
-    float* part;                  // backward: [K][CTAs][2][width]; NULL: the gradients themselves are written
+    float* part;                  // backward: [K][CTAs][part_ld >= 2 width]; NULL: the gradients themselves are written
     void  *dw_out, *db_out;
     int64_t dwo, dbo;
     int64_t xw, xr, rw, rr, dw, dr, yw, yr, tw, tr, ww, bw, mw, sw;      // worker and row strides, elements
     uint64_t rows;
     uint32_t width, lanes;        // lanes of a team: 4 .. 1024
+    uint32_t part_ld;             // a row of `part`
     float    eps;
 };
 
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
     extern __shared__ __align__(16) unsigned char ring_raw[];
     const uint32_t team = threadIdx.x / a.lanes, teams = blockDim.x / a.lanes;
     const uint32_t first = (threadIdx.x - team * a.lanes) * V, step = a.lanes * V, width = a.width;
-    const uint32_t beside = a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
+    const uint32_t beside = N == 1 && a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
     const Ring<T, WIDE, N> ring(ring_raw, a.lanes);
     const int64_t k = blockIdx.y;
     const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
         bp[i] = piece_load<T, WIDE>(b, first + i * step, width);
     }
     for (; row - beside < a.rows; row += rows_step) {
-        const bool on = row < a.rows;
+        const bool on = N > 1 || row < a.rows;            // (narrow rows: one piece a lane)
         ring.left();
         fetch();                                          // into the place that the row before this one has left
         ring.template wait<S - 1>();
@@ -251,8 +252,8 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
 #pragma unroll
             for (int j = 0; j < H; ++j) {
                 h[i][j] = f2_add(h[i][j], f2_same(-mean));
-                const f2 c = inside<WIDE>(h[i][j], first + i * step + 2 * j, width);
-                sum = f2_fma(c, c, sum);
+                if (first + i * step + V > width) h[i][j] = inside<WIDE>(h[i][j], first + i * step + 2 * j, width);
+                sum = f2_fma(h[i][j], h[i][j], sum);
             }
         s[0] = f2_total(sum);
         team_sum<1>(s, a.lanes, team, places, turn);
@@ -279,13 +280,13 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
 template <typename T, int N, bool WIDE, bool ADD, int WARPS, int CTAS>
 __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr bool kKeep = WARPS == 8;                    // the wide kernel forms xh and g twice: they would not fit its registers
+    constexpr bool kKeep = WARPS < 32;                    // the widest kernel forms xh and g twice: they would not fit its registers
     constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 3 * N : 2 * N, S = norm_stages<T, WIDE, N>(Q / N, WARPS, CTAS);
     __shared__ float places[4 * kNormMostWarps];
     extern __shared__ __align__(16) unsigned char ring_raw[];            // the ring; at the end [2][width] floats, where a CTA has more than one team
     const uint32_t team = threadIdx.x / a.lanes, teams = blockDim.x / a.lanes;
     const uint32_t first = (threadIdx.x - team * a.lanes) * V, step = a.lanes * V, width = a.width;
-    const uint32_t beside = a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
+    const uint32_t beside = N == 1 && a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
     const Ring<T, WIDE, N> ring(ring_raw, a.lanes);
     const int64_t k = blockIdx.y;
     const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
     };
     stats(row);
     for (; row - beside < a.rows; row += rows_step) {
-        const bool on = row < a.rows;
+        const bool on = N > 1 || row < a.rows;            // (narrow rows: one piece a lane)
         const float rs = rstd, mean_now = mean;
         stats(row + rows_step);
         ring.left();
@@ -343,7 +344,8 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
             piece_wide<T>(wp[i], wv);
 #pragma unroll
             for (int j = 0; j < H; ++j) {
-                xh[j] = inside<WIDE>(f2_mul(f2_add(xh[j], f2_same(-mean_now)), f2_same(rs)), first + i * step + 2 * j, some);
+                xh[j] = f2_mul(f2_add(xh[j], f2_same(-mean_now)), f2_same(rs));
+                if (first + i * step + V > some) xh[j] = inside<WIDE>(xh[j], first + i * step + 2 * j, some);
                 g[j] = f2_mul(d[j], wv[j]);
             }
         };
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                      // the ring's place is free
     float* const joined = reinterpret_cast<float*>(ring_raw);
-    float* const part = a.part ? a.part + ((uint64_t)k * gridDim.x + blockIdx.x) * 2 * width : nullptr;
+    float* const part = a.part ? a.part + ((uint64_t)k * gridDim.x + blockIdx.x) * a.part_ld : nullptr;
     auto put_sum = [&](uint32_t which, uint32_t c, float v) {
         if (part) part[which * width + c] = v;
         else if (which) static_cast<T*>(a.db_out)[k * a.dbo + c] = from_f<T>(v);

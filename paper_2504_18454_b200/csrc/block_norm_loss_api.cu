@@ -56,22 +56,22 @@ uint32_t norm_ctas(const palsgd_norm_shape* s, Team t, uint32_t per_sm)
 }
 
 // CTAs an SM that the kernel's registers are fitted to; the ring of a lane, 16 bytes a place.
-template <bool BACK> constexpr uint32_t norm_ctas_per_sm() { return BACK ? 2 : 3; }
+template <bool BACK> constexpr uint32_t norm_ctas_per_sm(uint32_t pieces) { return BACK || pieces > 2 ? 2 : 3; }
 template <bool BACK> constexpr uint32_t norm_most() { return BACK ? 2 : 3; }        // pieces a lane
 
 template <typename T, bool BACK, int N, bool WIDE, bool ADD, int WARPS>
 int launch_norm(const NormArgs& a, dim3 grid, cudaStream_t st)
 {
-    constexpr int kCtas = WARPS > 8 ? 1 : (int)norm_ctas_per_sm<BACK>();
+    constexpr int kCtas = WARPS > 8 ? 1 : (int)norm_ctas_per_sm<BACK>(N);
     void (*kernel)(NormArgs);
     if constexpr (BACK) kernel = norm_backward_kernel<T, N, WIDE, ADD, WARPS, kCtas>;
     else kernel = norm_forward_kernel<T, N, WIDE, ADD, WARPS, kCtas>;
-    const unsigned threads = WARPS == 8 ? 256 : a.lanes;
+    const unsigned threads = WARPS == 8 ? 256 : WARPS * 32;
     constexpr int kArrays = BACK ? ADD ? 3 : 2 : ADD ? 2 : 1;
     constexpr uint32_t kStage = norm_stage_bytes<T, WIDE, N>(kArrays, WARPS), kStages = norm_stages<T, WIDE, N>(kArrays, WARPS, kCtas);
     static_assert(kStages >= 1, "room for a row");
     static_assert(!BACK || WARPS > 8 || kStage * kStages >= 2 * sizeof(float) * (WARPS / 2) * 32 * N * kPieceValues<T>, "room for the sums of two teams or more");
-    const size_t smem = WARPS == 8 ? kStage * kStages : kStage / (WARPS * 32) * threads * kStages;
+    const size_t smem = (size_t)kStage * kStages;
     BLOCK_TRY(allow_smem(reinterpret_cast<const void*>(kernel), smem));
     return launch(BACK ? "layer norm backward" : "layer norm", kernel, grid, threads, smem, st, a);
 }
@@ -79,7 +79,8 @@ int launch_norm(const NormArgs& a, dim3 grid, cudaStream_t st)
 template <typename T, bool BACK, bool WIDE, bool ADD>
 int launch_norm(const NormArgs& a, Team t, dim3 grid, cudaStream_t st)
 {
-    if (t.lanes > 256) return launch_norm<T, BACK, (int)sizeof(T), WIDE, ADD, 32>(a, grid, st);
+    if (t.lanes == 512) return launch_norm<T, BACK, (int)sizeof(T), WIDE, ADD, 16>(a, grid, st);
+    if (t.lanes == 1024) return launch_norm<T, BACK, (int)sizeof(T), WIDE, ADD, 32>(a, grid, st);
     if (t.pieces == 1) return launch_norm<T, BACK, 1, WIDE, ADD, 8>(a, grid, st);
     if constexpr (norm_most<BACK>() == 2) {
         return launch_norm<T, BACK, 2, WIDE, ADD, 8>(a, grid, st);
@@ -155,7 +156,7 @@ extern "C" int palsgd_layer_norm_forward(const palsgd_norm_shape* s, const palsg
     const bool wide = (D * es) % 16 == 0 && norm_wide(x, es) && norm_wide(r, es) && norm_wide(w, es) && norm_wide(b, es) && norm_wide(y, es) && norm_wide(total, es);
     const Team t = team_of(D, es, norm_most<false>());
     a.lanes = t.lanes;
-    const dim3 grid(norm_ctas(s, t, norm_ctas_per_sm<false>()), s->K);
+    const dim3 grid(norm_ctas(s, t, norm_ctas_per_sm<false>(t.pieces)), s->K);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return es == 4 ? launch_norm<float, false>(a, t, wide, r.given, grid, st) : launch_norm<bf16, false>(a, t, wide, r.given, grid, st);
 }
@@ -182,9 +183,10 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     BLOCK_TRY(check_workspace(workspace, workspace_bytes));
     const Team t = team_of(D, es, norm_most<true>());
     // (four rows a team: as long as the launch of the kernel that joins what several CTAs leave)
-    const uint32_t ctas = s->tokens <= 4 * teams_of(t) ? 1 : norm_ctas(s, t, norm_ctas_per_sm<true>());
+    const uint32_t ctas = s->tokens <= 4 * teams_of(t) ? 1 : norm_ctas(s, t, norm_ctas_per_sm<true>(t.pieces));
     Arena ws{static_cast<char*>(workspace), 0};
-    float* part = ctas > 1 ? static_cast<float*>(ws.take((size_t)s->K * ctas * 2 * D * sizeof(float))) : nullptr;
+    const uint32_t part_ld = (uint32_t)ceil_div(2 * D, 4) * 4;
+    float* part = ctas > 1 ? static_cast<float*>(ws.take((size_t)s->K * ctas * part_ld * sizeof(float))) : nullptr;
     Regions all;
     all.reads(region(dy, s->K, M, D, es)); all.reads(region(x, s->K, M, D, es)); all.reads(region(w, s->K, 1, D, es));
     all.reads(region(mean, s->K, 1, M, 4)); all.reads(region(rstd, s->K, 1, M, 4)); all.reads(region(past, s->K, M, D, es));
@@ -199,7 +201,7 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     a.y = dx.m.data; a.yw = dx.m.worker_stride; a.yr = dx.m.row_stride;
     a.mean = static_cast<float*>(mean.m.data); a.mw = mean.m.worker_stride;
     a.rstd = static_cast<float*>(rstd.m.data); a.sw = rstd.m.worker_stride;
-    a.part = part;
+    a.part = part; a.part_ld = part_ld;
     a.dw_out = dw.m.data; a.dwo = dw.m.worker_stride; a.db_out = db.m.data; a.dbo = db.m.worker_stride;
     a.rows = M; a.width = (uint32_t)D; a.lanes = t.lanes;
     const bool wide = (D * es) % 16 == 0 && norm_wide(dy, es) && norm_wide(x, es) && norm_wide(w, es) && norm_wide(past, es) && norm_wide(dx, es);
@@ -207,8 +209,8 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     BLOCK_TRY((es == 4 ? launch_norm<float, true>(a, t, wide, past.given, grid, st) : launch_norm<bf16, true>(a, t, wide, past.given, grid, st)));
     if (!part) return PALSGD_OK;
-    ColumnSumArgs c{part, {dw.m.data, db.m.data}, {dw.m.worker_stride, db.m.worker_stride}, ctas, (uint32_t)(2 * D), (uint32_t)D};
-    const dim3 columns((unsigned)ceil_div(2 * D, 32), s->K);
+    ColumnSumArgs c{part, {dw.m.data, db.m.data}, {dw.m.worker_stride, db.m.worker_stride}, ctas, (uint32_t)(2 * D), part_ld, (uint32_t)D};
+    const dim3 columns((unsigned)ceil_div(2 * D, 128), s->K);
     return launch("layer norm weight gradients", es == 4 ? column_sum_kernel<float> : column_sum_kernel<bf16>, columns, 256, 0, st, c);
 }
 
