@@ -372,6 +372,19 @@ void take_shares(Arena& ws, Product* p, int n, uint32_t K, uint32_t parts)
         if (p[i].splits > 1) p[i].part = static_cast<const float*>(ws.take((size_t)p[i].splits * K * p[i].M * (size_t)p[i].ld() * sizeof(float)));
 }
 
+JoinItem join_of(const float* part, uint32_t splits, uint32_t K, uint64_t M, uint64_t N, int64_t ld, const MatOut& out)
+{
+    const int64_t w = ld * (int64_t)M;
+    return JoinItem{part, w, w * K, splits, (uint32_t)ld, (uint32_t)M, (uint32_t)N, M * (uint64_t)(ld / 8), divisor((uint32_t)(ld / 8)), out};
+}
+
+int run_join(const JoinArgs& join, uint32_t joins, uint64_t units, uint32_t K, size_t es, int sms, cudaStream_t st)
+{
+    const uint64_t want = ceil_div(units, 256), cap = 16ull * sms;
+    const dim3 grid((unsigned)(want < cap ? want : cap), joins, K);
+    return launch("joined shares", es == 4 ? join_kernel<float> : join_kernel<bf16>, grid, 256, 0, st, join);
+}
+
 // The products of a call in one launch, the longer ones first, and the kernel that joins what was cut (unless the caller has
 // one of its own).
 int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, size_t es, uint32_t parts, cudaStream_t st, bool joined = true, const MatSums* sums = nullptr)
@@ -406,7 +419,7 @@ int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, 
         if (p[i].splits > 1) {
             JoinItem& j = join.item[joins++];
             const int64_t ld = p[i].ld(), w = ld * (int64_t)p[i].M;
-            j = JoinItem{p[i].part, w, w * s->K, p[i].splits, (uint32_t)ld, (uint32_t)p[i].M, (uint32_t)p[i].N, p[i].M * (uint64_t)(ld / 8), divisor((uint32_t)(ld / 8)), q.out[0]};
+            j = join_of(p[i].part, p[i].splits, s->K, p[i].M, p[i].N, ld, q.out[0]);
             if (j.units > units) units = j.units;
             q.out[0] = MatOut{const_cast<float*>(p[i].part), w, ld, w * s->K, 1, (uint32_t)ld};
             q.splits = p[i].splits;
@@ -420,10 +433,7 @@ int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, 
     }
     if (heavy) L.lag = (uint32_t)(p[0].length(parts) / p[n - 1].length(parts));
     BLOCK_TRY(run_mat<MAT_PLAIN>(L, s, d, st));
-    if (joins == 0 || !joined) return PALSGD_OK;
-    const uint64_t want = ceil_div(units, 256), cap = 16ull * d.sms;
-    const dim3 grid((unsigned)(want < cap ? want : cap), joins, s->K);
-    return launch("joined shares", es == 4 ? join_kernel<float> : join_kernel<bf16>, grid, 256, 0, st, join);
+    return joins == 0 || !joined ? PALSGD_OK : run_join(join, joins, units, s->K, es, d.sms, st);
 }
 
 void set_saved(MatLaunch& L, const palsgd_ffn_shape* s, const palsgd_mat* gate, const palsgd_mat* up, const palsgd_mat* gate_e, const palsgd_mat* up_e)
@@ -534,6 +544,51 @@ int run_linear_join(const palsgd_linear_shape* s, const Product& p, const Linear
     return with_act(s->activation, [&](auto act) {
         return launch("linear, joined shares", linear_join_kernel<T, act>, dim3((unsigned)(want < cap ? want : cap), s->K), 256, 0, st, a);
     });
+}
+
+// A backward call of few tokens: lanes side by side in a row, and rows of a CTA -- 16 turns of its lanes, more where the device
+// could not run all CTAs at a time, as many as there is room for at most.
+uint32_t few_lanes(const palsgd_linear_shape* s)
+{
+    uint32_t lanes = 1;
+    while (lanes < 256 && lanes * 4 < s->d_in) lanes *= 2;
+    return lanes;
+}
+uint32_t few_rows(const palsgd_linear_shape* s)
+{
+    const uint64_t lanes = few_lanes(s), strips = ceil_div(s->d_in, lanes * 4) * s->K, least = 16 * (256 / lanes);
+    uint64_t rows = ceil_div(s->d_out * strips, 3ull * sm_count());
+    const uint64_t grid = ceil_div(s->d_out, 65535);     // (the grid's second axis)
+    if (rows < least) rows = least;
+    if (rows > kFewBackRows) rows = kFewBackRows;
+    return (uint32_t)(rows > grid ? rows : grid);
+}
+
+// Whether a backward call goes to the kernel of few tokens.  fp32: always (7 workers, 2 tokens, 736 x 2688: 30 us, the matrix kernel
+// on operands in three parts 90).  bfloat16: where the matrix kernel's launches take longer than its work (one token, 2048 x 5632:
+// 16.6 us, and 21; 3 x 4 tokens, 3320 x 1680: 28.7, and 25.3).  The rows of a CTA have to find room, and the columns of all
+// tokens 31 bits.
+constexpr uint64_t kFewBackWork = 32000000;              // multiplications
+bool few_backward(const palsgd_linear_shape* s)
+{
+    if (s->tokens == 0 || s->tokens > kFewTokens || s->d_in > (1u << 24) || few_rows(s) > kFewBackRows) return false;
+    return s->precision == PALSGD_PREC_FP32 || s->tokens * s->K * s->d_in * s->d_out <= kFewBackWork;
+}
+
+int wide4(const palsgd_mat* m, size_t es)               // four values of every row start on a multiple of their size
+{
+    return aligned(m->data, 4 * es) && m->worker_stride % 4 == 0 && m->row_stride % 4 == 0;
+}
+
+template <typename T>
+int run_few_backward(const palsgd_linear_shape* s, FewBackArgs& a, cudaStream_t st)
+{
+    a.M = (uint32_t)s->tokens; a.N = (uint32_t)s->d_out; a.D = (uint32_t)s->d_in; a.act = s->activation;
+    a.lanes = few_lanes(s);
+    a.rows = few_rows(s);
+    const dim3 grid((unsigned)ceil_div(s->d_in, a.lanes * 4), (unsigned)ceil_div(s->d_out, a.rows), s->K);
+    return launch("linear backward, few tokens", a.M <= 1 ? few_backward_kernel<T, 1> : a.M <= 2 ? few_backward_kernel<T, 2> : a.M <= 4 ? few_backward_kernel<T, 4> : few_backward_kernel<T, 8>,
+                  grid, 256, 0, st, a);
 }
 
 // Lanes side by side in the pass before the activation, and rows of a CTA: enough CTAs to run at a time, with at least four
@@ -970,7 +1025,13 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
     bool pass = false;                                   // dz is formed, or summed, by a pass of its own
     Product products[2];
     int n_products = 0;
-    if (M) {
+    const bool few = few_backward(s);
+    const int64_t few_ld = (int64_t)ceil_div(D, 8) * 8;
+    const uint32_t shares = few && dx.given ? (uint32_t)ceil_div(N, few_rows(s)) : 1;
+    float* sums_of_dx = nullptr;
+    if (few) {
+        if (shares > 1) sums_of_dx = static_cast<float*>(ws.take((size_t)shares * s->K * M * few_ld * sizeof(float)));
+    } else if (M) {
         // dy is read in place where it is dz and the copy engine can; else the pass writes the operand
         Stage in_place;
         Arena none{nullptr, 0};
@@ -1004,6 +1065,27 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
         z.p[1] = db.m.data; z.w[1] = db.m.worker_stride; z.rows[1] = db.given; z.cols[1] = (uint32_t)N;
         const dim3 grid((unsigned)N < 1024u ? (unsigned)N : 1024u, 2, s->K);
         return launch("zero weight gradients", es == 4 ? zero_kernel<float> : zero_kernel<bf16>, grid, 256, 0, st, z);
+    }
+    if (few) {
+        FewBackArgs a{};
+        a.dy = dy.m.data; a.dyw = dy.m.worker_stride; a.dyr = dy.m.row_stride;
+        a.x = x.m.data; a.xw = x.m.worker_stride; a.xr = x.m.row_stride; a.x_wide = wide4(x, x_e.given ? 1 : es);
+        if (x_e.given) { a.x_e = static_cast<const uint8_t*>(x_e.m.data); a.xew = x_e.m.worker_stride; a.xer = x_e.m.row_stride; }
+        a.w = w.m.data; a.ww = w.m.worker_stride; a.wr = w.m.row_stride; a.w_wide = wide4(w, es);
+        if (bent) {
+            a.eight = s->save == PALSGD_SAVE_8BIT;
+            a.pre = pre.m.data; a.pw = pre.m.worker_stride; a.pr = pre.m.row_stride;
+            if (a.eight) { a.pre_e = static_cast<const uint8_t*>(pre_e.m.data); a.pew = pre_e.m.worker_stride; a.per = pre_e.m.row_stride; }
+        }
+        const MatOut out = dx.given ? out_of(dx, D, es) : MatOut{};
+        a.dx = shares > 1 ? MatOut{sums_of_dx, few_ld * (int64_t)M * shares, few_ld, few_ld * (int64_t)M, 1, (uint32_t)few_ld} : out;
+        a.dw = out_of(dw, D, es); a.dw.wide = wide4(dw, es);
+        if (db.given) { a.db = db.m.data; a.dbw = db.m.worker_stride; }
+        BLOCK_TRY(es == 4 ? run_few_backward<float>(s, a, st) : run_few_backward<bf16>(s, a, st));
+        if (shares == 1) return PALSGD_OK;
+        const uint32_t cols = (uint32_t)(few_ld * (int64_t)M);
+        const ColumnSumArgs c{sums_of_dx, {dx.m.data, nullptr}, {dx.m.worker_stride, 0}, shares, cols, cols, cols, (uint32_t)few_ld, (uint32_t)D, dx.m.row_stride};
+        return launch("linear, joined sums", es == 4 ? column_sum_kernel<float> : column_sum_kernel<bf16>, dim3((unsigned)ceil_div(cols, 128), s->K), 256, 0, st, c);
     }
     Device dev{};
     BLOCK_TRY(device_of(dev));

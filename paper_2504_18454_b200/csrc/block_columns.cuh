@@ -6,12 +6,14 @@ namespace palsgd {
 namespace block {
 
 // Rows of binary32 sums [K][parts][ld], ld a multiple of four, joined in a fixed order: a thread has four columns and every
-// eighth row.  The columns of two results lie behind one another.
+// eighth row.  The columns of two results lie behind one another, or those of one are the rows of a matrix.
 struct ColumnSumArgs {
     const float* part;
     void*    out[2];              // columns 0 .. split-1, and the rest
     int64_t  ow[2];               // worker strides
     uint32_t parts, cols, ld, split;
+    uint32_t wrap, inside;        // columns of a row of out[0] in `part`, and in out[0]
+    int64_t  row;                 // out[0]'s row stride
 };
 template <typename T>
 __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ ColumnSumArgs a)
@@ -37,8 +39,12 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__
     float t = 0.0f;
 #pragma unroll
     for (int b = 0; b < 8; ++b) t += reinterpret_cast<const float*>(run[b])[threadIdx.x];
-    const uint32_t which = i >= a.split;
-    static_cast<T*>(a.out[which])[(int64_t)k * a.ow[which] + i - (which ? a.split : 0)] = from_f<T>(t);
+    if (i >= a.split) {
+        static_cast<T*>(a.out[1])[(int64_t)k * a.ow[1] + i - a.split] = from_f<T>(t);
+    } else {
+        const uint32_t m = i / a.wrap, c = i - m * a.wrap;
+        if (c < a.inside) static_cast<T*>(a.out[0])[(int64_t)k * a.ow[0] + m * a.row + c] = from_f<T>(t);
+    }
 }
 
 }  // namespace block

@@ -367,5 +367,200 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ S
     else static_cast<T*>(a.db)[k * a.dbw + at] = from_f<T>(t);
 }
 
+// ---------------------------------------------------------------------------------------------- few tokens, backward
+//
+// Up to eight tokens: bound by reading w and writing dw once.  A lane has four columns; it keeps them of every token's x and of
+// its sums of dx in registers and walks rows of w: dw's row is a sum over the tokens, dx's sums grow by the row.  Lanes that the
+// columns leave over take rows side by side.  A CTA has `rows` rows, whose dz it forms once, in shared memory; the CTAs' sums of
+// dx are joined in a fixed order.  All in binary32.
+struct FewBackArgs {
+    const void *dy, *pre, *x, *w;
+    const uint8_t *pre_e, *x_e;   // 8 bits: of pre, of x
+    int64_t  dyw, dyr, pw, pr, pew, per, xw, xr, xew, xer, ww, wr;
+    MatOut   dx, dw;              // dx: p may be NULL; binary32 sums where there is more than one row CTA
+    void*    db;
+    int64_t  dbw;
+    uint32_t M, N, D, rows, lanes;                       // lanes side by side in a row: 1 .. 256
+    int      act, eight, x_wide, w_wide;                  // wide: four values start on a boundary of four
+};
+
+// Four values of a row, the first n of them inside it
+__device__ __forceinline__ void load4(const float* p, uint32_t n, bool wide, float (&v)[4])
+{
+    if (wide && n >= 4) {
+        const float4 q = __ldg(reinterpret_cast<const float4*>(p));
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) v[i] = i < n ? __ldg(p + i) : 0.0f;
+    }
+}
+__device__ __forceinline__ void load4(const bf16* p, uint32_t n, bool wide, float (&v)[4])
+{
+    if (wide && n >= 4) {
+        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+        v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) v[i] = i < n ? to_f(__ldg(p + i)) : 0.0f;
+    }
+}
+// ... of an 8-bit checkpoint (they lie in one group)
+__device__ __forceinline__ void load4(const int8_t* p, const uint8_t* e, uint32_t n, bool wide, float (&v)[4])
+{
+    if (n == 0) {
+        v[0] = v[1] = v[2] = v[3] = 0.0f;
+        return;
+    }
+    const float s = act8_step(*e);
+    if (wide && n >= 4) {
+        act8_value4(__ldg(reinterpret_cast<const uint32_t*>(p)), s, v);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) v[i] = i < n ? (float)__ldg(p + i) * s : 0.0f;
+    }
+}
+__device__ __forceinline__ void store4(float* p, uint32_t n, bool wide, const float (&v)[4])
+{
+    if (wide && n >= 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) if (i < n) p[i] = v[i];
+}
+__device__ __forceinline__ void store4(bf16* p, uint32_t n, bool wide, const float (&v)[4])
+{
+    if (wide && n >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(f2_narrow(f2_of(v[0], v[1])), f2_narrow(f2_of(v[2], v[3])));
+    else
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) if (i < n) p[i] = from_f<bf16>(v[i]);
+}
+
+template <typename T>
+__device__ __forceinline__ float few_slope(int kind, float z)
+{
+    float slope = 1.0f;
+    switch (kind) {
+        case PALSGD_ACT_SILU: act<PALSGD_ACT_SILU, true, sizeof(T) == 2>(z, slope); break;
+        case PALSGD_ACT_GELU: act<PALSGD_ACT_GELU, true, sizeof(T) == 2>(z, slope); break;
+        case PALSGD_ACT_GELU_TANH: act<PALSGD_ACT_GELU_TANH, true, sizeof(T) == 2>(z, slope); break;
+        case PALSGD_ACT_RELU: act<PALSGD_ACT_RELU, true, sizeof(T) == 2>(z, slope); break;
+        default: break;
+    }
+    return slope;
+}
+
+// Four values as they lie in memory
+template <typename T> struct Raw4;
+template <> struct Raw4<bf16> {
+    uint2 q;
+    __device__ __forceinline__ void load(const bf16* p, uint32_t n, bool wide)
+    {
+        if (wide && n >= 4) { q = __ldg(reinterpret_cast<const uint2*>(p)); return; }
+        uint32_t h[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) h[i] = i < n ? __ldg(reinterpret_cast<const unsigned short*>(p) + i) : 0;
+        q = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+    }
+    __device__ __forceinline__ void get(f2& a, f2& b) const { a = f2_wide(q.x); b = f2_wide(q.y); }
+};
+template <> struct Raw4<float> {
+    float v[4];
+    __device__ __forceinline__ void load(const float* p, uint32_t n, bool wide) { load4(p, n, wide, v); }
+    __device__ __forceinline__ void get(f2& a, f2& b) const { a = f2_of(v[0], v[1]); b = f2_of(v[2], v[3]); }
+};
+
+constexpr uint32_t kFewBackRows = 256;                    // of a CTA, at most
+
+template <typename T, int MT>
+__global__ void __launch_bounds__(256, MT == 8 ? 2 : 3) few_backward_kernel(const __grid_constant__ FewBackArgs a)
+{
+    constexpr int U = sizeof(T) == 2 && MT < 8 ? 4 : 2;   // rows of w at a time; as many more under way
+    __shared__ __align__(16) float dz[kFewBackRows][MT];
+    __shared__ float joined[256][4 * MT + 1];
+    const uint32_t tid = threadIdx.x, side = 256 / a.lanes, group = tid / a.lanes, d = (blockIdx.x * a.lanes + tid % a.lanes) * 4;
+    const uint32_t n0 = blockIdx.y * a.rows, rows = min(a.rows, a.N - n0), in = d < a.D ? min(a.D - d, 4u) : 0;
+    const int64_t k = blockIdx.z;
+    let_next_start();
+    wait_for_previous();
+    const T* w = static_cast<const T*>(a.w) + k * a.ww + (int64_t)n0 * a.wr + d;
+    T* dw = static_cast<T*>(a.dw.p) + k * a.dw.w + (int64_t)n0 * a.dw.r + d;
+    Raw4<T> raw[U], next[U];
+    auto fetch = [&](uint32_t r0, Raw4<T> (&to)[U]) {
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) to[u].load(w + (int64_t)(r0 + u * side) * a.wr, a.dx.p && r0 + u * side < rows ? in : 0, a.w_wide);
+    };
+    fetch(group, raw);
+    f2 x[MT][2], acc[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        float v[4];
+        const uint32_t there = (uint32_t)m < a.M ? in : 0;
+        if (a.x_e) load4(static_cast<const int8_t*>(a.x) + k * a.xw + m * a.xr + d, a.x_e + k * a.xew + m * a.xer + d / 32, there, a.x_wide, v);
+        else load4(static_cast<const T*>(a.x) + k * a.xw + m * a.xr + d, there, a.x_wide, v);
+        x[m][0] = f2_of(v[0], v[1]); x[m][1] = f2_of(v[2], v[3]);
+        acc[m][0] = acc[m][1] = 0;
+    }
+    for (uint32_t i = tid; i < rows * MT; i += 256) {
+        const uint32_t m = i / rows, r = i - m * rows, n = n0 + r;       // (lanes side by side: columns)
+        float v = 0.0f;
+        if (m < a.M) {
+            v = to_f(static_cast<const T*>(a.dy)[k * a.dyw + m * a.dyr + n]);
+            if (a.act != PALSGD_ACT_NONE) {
+                float z;
+                if (a.eight) z = (float)static_cast<const int8_t*>(a.pre)[k * a.pw + m * a.pr + n] * act8_step(a.pre_e[k * a.pew + m * a.per + n / 32]);
+                else z = to_f(static_cast<const T*>(a.pre)[k * a.pw + m * a.pr + n]);
+                v *= few_slope<T>(a.act, z);
+            }
+        }
+        dz[r][m] = v;
+    }
+    __syncthreads();
+    if (a.db && blockIdx.x == 0 && tid < rows) {
+        float t = 0.0f;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) t += dz[tid][m];
+        static_cast<T*>(a.db)[k * a.dbw + n0 + tid] = from_f<T>(t);
+    }
+    for (uint32_t r0 = group; r0 < rows; r0 += U * side) {
+        fetch(r0 + U * side, next);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t r = r0 + u * side;
+            if (r >= rows) break;
+            f2 w0, w1, s0 = 0, s1 = 0;
+            raw[u].get(w0, w1);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const f2 g = f2_same(dz[r][m]);
+                s0 = f2_fma(g, x[m][0], s0); s1 = f2_fma(g, x[m][1], s1);
+                acc[m][0] = f2_fma(g, w0, acc[m][0]); acc[m][1] = f2_fma(g, w1, acc[m][1]);
+            }
+            float o[4];
+            f2_get(s0, o[0], o[1]); f2_get(s1, o[2], o[3]);
+            store4(dw + (int64_t)r * a.dw.r, in, a.dw.wide, o);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) raw[u] = next[u];
+    }
+    if (!a.dx.p) return;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        f2_get(acc[m][0], joined[tid][4 * m], joined[tid][4 * m + 1]);
+        f2_get(acc[m][1], joined[tid][4 * m + 2], joined[tid][4 * m + 3]);
+    }
+    __syncthreads();
+    // the side-by-side rows' sums, in order: a thread for each token and column
+    for (uint32_t i = tid; i < a.lanes * 4 * a.M; i += 256) {
+        const uint32_t m = i / (a.lanes * 4), c = i - m * a.lanes * 4, at = blockIdx.x * a.lanes * 4 + c;
+        float t = 0.0f;
+        for (uint32_t g = 0; g < side; ++g) t += joined[g * a.lanes + c / 4][4 * m + c % 4];
+        if (at >= a.D) continue;
+        const int64_t to = k * a.dx.w + m * a.dx.r + at;
+        if (gridDim.y > 1) static_cast<float*>(a.dx.p)[blockIdx.y * a.dx.part + to] = t;
+        else static_cast<T*>(a.dx.p)[to] = from_f<T>(t);
+    }
+}
+
 }  // namespace block
 }  // namespace palsgd

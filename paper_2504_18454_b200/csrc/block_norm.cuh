@@ -336,7 +336,8 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
         fetch();
         ring.template wait<S - 1>();
         const uint32_t some = on ? width : 0;
-        // a piece's xh, d and g = d w.  (Behind the row's end d is zero, and xh has to be finite.)
+        // a piece's xh, d and g = d w.  (Behind the row's end d is zero, and xh has to be finite where it goes into the sums
+        // of columns that are there: a piece cut by the end, and a team without a row.)
         auto load = [&](int i, f2 (&xh)[H], f2 (&d)[H], f2 (&g)[H]) {
             f2 wv[H];
             piece_wide<T>(ring.get(got * Q + i, x + (int64_t)row * a.xr, first + i * step, some), xh);
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
 #pragma unroll
             for (int j = 0; j < H; ++j) {
                 xh[j] = f2_mul(f2_add(xh[j], f2_same(-mean_now)), f2_same(rs));
-                if (first + i * step + V > some) xh[j] = inside<WIDE>(xh[j], first + i * step + 2 * j, some);
+                if ((!WIDE || N == 1) && first + i * step + V > some) xh[j] = inside<WIDE>(xh[j], first + i * step + 2 * j, some);
                 g[j] = f2_mul(d[j], wv[j]);
             }
         };

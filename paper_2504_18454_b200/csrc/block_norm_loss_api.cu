@@ -209,7 +209,7 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     BLOCK_TRY((es == 4 ? launch_norm<float, true>(a, t, wide, past.given, grid, st) : launch_norm<bf16, true>(a, t, wide, past.given, grid, st)));
     if (!part) return PALSGD_OK;
-    ColumnSumArgs c{part, {dw.m.data, db.m.data}, {dw.m.worker_stride, db.m.worker_stride}, ctas, (uint32_t)(2 * D), part_ld, (uint32_t)D};
+    ColumnSumArgs c{part, {dw.m.data, db.m.data}, {dw.m.worker_stride, db.m.worker_stride}, ctas, (uint32_t)(2 * D), part_ld, (uint32_t)D, (uint32_t)D, (uint32_t)D, 0};
     const dim3 columns((unsigned)ceil_div(2 * D, 128), s->K);
     return launch("layer norm weight gradients", es == 4 ? column_sum_kernel<float> : column_sum_kernel<bf16>, columns, 256, 0, st, c);
 }

@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
 # K, tokens, d_in, d_out: one token, odd everything, few tokens, one tile, just past a tile, several tiles, a long inner axis
 SIZES = [(1, 1, 1, 1), (1, 1, 64, 128), (2, 3, 7, 5), (1, 8, 2056, 40), (3, 5, 513, 33), (2, 9, 24, 33), (3, 129, 65, 257), (1, 128, 64, 256),
-         (4, 17, 256, 683), (2, 300, 264, 520), (1, 40, 4104, 72), (1, 1000, 40, 48), (2, 257, 136, 1000)]
+         (4, 17, 256, 683), (2, 300, 264, 520), (1, 40, 4104, 72), (1, 1000, 40, 48), (2, 257, 136, 1000), (1, 16, 40, 1500), (2, 17, 300, 1025), (3, 512, 100, 70), (1, 40, 9000, 1030),
+         (2, 700, 600, 601)]
 
 
 def _inputs(K, M, D, N, dt, seed=1):
@@ -101,11 +102,12 @@ def test_every_activation_over_its_range(dtype, kind, M):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("odd", [False, True])
-@pytest.mark.parametrize("M", [6, 70])
-def test_strided_operands_and_untouched_surroundings(dtype, odd, M):
+@pytest.mark.parametrize("M,D", [(6, 72), (70, 72), (2100, 264)])
+@pytest.mark.parametrize("form", [P.SAVE_FULL, P.SAVE_8BIT])
+def test_strided_operands_and_untouched_surroundings(dtype, odd, M, D, form):
     """Weights and gradients as views of packed rows (odd: not 16-byte aligned), activations inside wider rows, outputs inside
     sentinels."""
-    dt, (K, D, N) = DT[dtype], (3, 72, 136)
+    dt, (K, N) = DT[dtype], (3, 136)
     x, w, b, r, dy, z = _inputs(K, M, D, N, dt, seed=4)
     shift, row = 1 if odd else 8, N * D + N + 64
 
@@ -120,13 +122,21 @@ def test_strided_operands_and_untouched_surroundings(dtype, odd, M):
     inner = lambda t, n: t[:, :, shift:shift + n]
     xb, rb, yb, zb, dyb, dxb = wide(D), wide(N), wide(N), wide(N), wide(N), wide(D)
     inner(xb, D).copy_(x), inner(rb, N).copy_(r), inner(dyb, N).copy_(dy)
-    y, saved = P.linear_forward(inner(xb, D), vw, vb, inner(rb, N), activation=P.ACT_GELU, save=P.SAVE_FULL, out=inner(yb, N), saved=inner(zb, N))
+    saved, bytes_ = inner(zb, N), None
+    if form == P.SAVE_8BIT:
+        bytes_ = torch.full((2, K, M, N + 16), 99, device="cuda", dtype=torch.uint8)
+        saved = P.Act8(bytes_[0, :, :, shift:shift + N].view(torch.int8), bytes_[1, :, :, shift:shift + (N + 31) // 32], dt)
+    _, saved = P.linear_forward(inner(xb, D), vw, vb, inner(rb, N), activation=P.ACT_GELU, save=form, out=inner(yb, N), saved=saved)
     want = linear64(x, w, b, r, P.ACT_GELU, dtype == "bf16")
     within(inner(yb, N), *want["y"], "y")
-    check_saved(inner(zb, N), want["z"], dt, N)
+    check_saved(saved, want["z"], dt, N)
     ag, gw, gb = arena()
-    P.linear_backward(inner(dyb, N), inner(xb, D), vw, inner(zb, N), activation=P.ACT_GELU, out=(inner(dxb, D), gw, gb))
-    ref = linear_backward64(dy, x, w, inner(zb, N), P.ACT_GELU, dtype == "bf16")
+    P.linear_backward(inner(dyb, N), inner(xb, D), vw, saved, activation=P.ACT_GELU, out=(inner(dxb, D), gw, gb))
+    z = P.act8_unpack(saved, dtype=torch.float32) if bytes_ is not None else saved
+    ref = linear_backward64(dy, x, w, z, P.ACT_GELU, dtype == "bf16")
+    if bytes_ is not None:
+        for t, n in ((bytes_[0], N), (bytes_[1], (N + 31) // 32)):
+            assert bool((t[:, :, :shift] == 99).all()) and bool((t[:, :, shift + n:] == 99).all())
     for t, name in zip((inner(dxb, D), gw, gb), ("dx", "dw", "db")):
         within(t, *ref[name], name)
     for t, n in ((xb, D), (rb, N), (yb, N), (zb, N), (dyb, N), (dxb, D)):
@@ -136,7 +146,7 @@ def test_strided_operands_and_untouched_surroundings(dtype, odd, M):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("M", [5, 70])
+@pytest.mark.parametrize("M", [5, 70, 10000])
 def test_broadcast_inputs(dtype, M):
     """All workers read one weight, one bias and one input; every token reads one row of the residual."""
     K, D, N = 3, 72, 104
@@ -149,8 +159,9 @@ def test_broadcast_inputs(dtype, M):
         within(t, *want[name], name)
 
 
-def test_what_is_not_asked_for_is_left_out():
-    x, w, _, _, dy, _ = _inputs(2, 33, 40, 48, torch.bfloat16)
+@pytest.mark.parametrize("M", [33, 600])
+def test_what_is_not_asked_for_is_left_out(M):
+    x, w, _, _, dy, _ = _inputs(2, M, 40, 48, torch.bfloat16)
     full = P.linear_backward(dy, x, w)
     dx, dw, db = P.linear_backward(dy, x, w, need_dx=False, need_dbias=False)
     assert dx is None and db is None and torch.equal(dw, full[1])
@@ -168,7 +179,7 @@ def test_no_tokens(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("M", [4, 50])
+@pytest.mark.parametrize("M", [4, 50, 12000])
 def test_infinities_and_nan_stay_where_they_are(dtype, M):
     """A NaN in one input row reaches that row alone, one in the bias its column, one in the residual its place."""
     x, w, b, r, _, _ = _inputs(1, M, 72, 264, DT[dtype], seed=8)
