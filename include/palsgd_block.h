@@ -234,8 +234,8 @@ int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const palsgd_mat* dy,
  * above -infinity, gives NaN in loss and gradient; its lse is NaN, or -infinity where nothing is above that.
  * Backward, at the given lse:  dlogits = (e^(z - lse) - [target]) dloss.  dlogits may be exactly logits: work in place.
  * Sums in binary32, in a fixed order; dlogits are rounded once to the storage type.
- * Errors: EINVAL (NULL, K, vocab = 0, a size >= 2^31, overlapping buffers); EUNSUPPORTED (more than 2^31 - 1 rows, or parts of
- * rows of 2048 16-byte pieces, of a worker); EALIGN; ECUDA.
+ * Errors: EINVAL (NULL, K, vocab = 0, a size >= 2^31, overlapping buffers); EUNSUPPORTED (backward: more than 2^31 - 1
+ * parts of rows of up to 2048 16-byte pieces, of a worker); EALIGN; ECUDA.
  */
 typedef struct palsgd_loss_shape {
     uint32_t K;

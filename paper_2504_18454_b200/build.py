@@ -58,7 +58,7 @@ def build_extension(force: bool = False) -> Path:
         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
         f"-I{home}/include", f"-I{home}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}",
         f"-I{cuda}/include", str(EXT_SOURCE), "-o", str(tmp),
-        f"-L{home}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+        f"-L{home}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
     os.replace(tmp, EXT)
     return EXT
 

@@ -591,8 +591,8 @@ int run_few_backward(const palsgd_linear_shape* s, FewBackArgs& a, cudaStream_t 
                   grid, 256, 0, st, a);
 }
 
-// Lanes side by side in the pass before the activation, and rows of a CTA: enough CTAs to run at a time, with at least four
-// turns of their lanes each; all rows where that is less than the kernel that joins what several CTAs leave takes to launch.
+// Lanes side by side in the pass before the activation, and rows of a CTA: as many CTAs as run at a time, down to one turn of
+// their lanes each (their sums are joined beside the products, in a launch that comes anyway).
 uint32_t slope_lanes(const palsgd_linear_shape* s)
 {
     uint32_t lanes = 2;
@@ -602,12 +602,8 @@ uint32_t slope_lanes(const palsgd_linear_shape* s)
 uint32_t slope_rows(const palsgd_linear_shape* s)
 {
     const uint32_t lanes = slope_lanes(s);
-    const uint64_t strips = ceil_div(s->d_out, lanes * 8) * s->K, run = 3ull * sm_count() / strips, want = run ? run : 1, turn = 8 * (32 / lanes), least = 4 * turn;
-    if (s->tokens <= 2 * least) return (uint32_t)s->tokens;
-    uint64_t rows = ceil_div(s->tokens, want);
-    if (rows < least) rows = least;
-    const uint64_t grid = ceil_div(s->tokens, 65535);    // (the grid's second axis)
-    return (uint32_t)ceil_div(rows > grid ? rows : grid, turn) * (uint32_t)turn;
+    const uint64_t strips = ceil_div(s->d_out, lanes * 8) * s->K, run = 3ull * sm_count() / strips, turn = 8 * (32 / lanes);
+    return (uint32_t)ceil_div(ceil_div(s->tokens, run ? run : 1), turn) * (uint32_t)turn;
 }
 
 template <typename T>

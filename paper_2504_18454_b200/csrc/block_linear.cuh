@@ -178,11 +178,15 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
         if (n) {                                          // (the shares' rows hold a multiple of eight columns)
             const float* p = a.part + k * a.w + (int64_t)row * a.ld + c;
             row8_load(p, 8, true, z);
-            for (uint32_t s = 1; s < a.splits; ++s) {
-                f2 v[4];
-                row8_load(p + s * a.share, 8, true, v);
+            for (uint32_t s = 1; s < a.splits; s += 4) {  // (four loads under way; the order of the sums is fixed)
+                f2 v[4][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) z[j] = f2_add(z[j], v[j]);
+                for (uint32_t u = 0; u < 4; ++u) if (s + u < a.splits) row8_load(p + (s + u) * a.share, 8, true, v[u]);
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u)
+                    if (s + u < a.splits)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) z[j] = f2_add(z[j], v[u][j]);
             }
             if (e.bias.p) {
                 f2 b[4];
@@ -214,7 +218,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
         if (n == 0) continue;
         f2 unused;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = act_pair<T, ACT, false>(z[j], unused);
+        for (int j = 0; j < 4; ++j) z[j] = linear_act<T, ACT, false>(z[j], unused);
         if (e.residual.p) {
             f2 r[4];
             row8_load(static_cast<const T*>(e.residual.p) + k * e.residual.w + (int64_t)row * e.residual.r + c, n, e.residual.wide, r);
@@ -325,7 +329,7 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ S
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     f2 slope;
-                    act_pair<T, ACT, true>(z[i], slope);
+                    linear_act<T, ACT, true>(z[i], slope);
                     d[i] = f2_mul(d[i], slope);           // (what lies behind the row's end is used nowhere)
                 }
             }

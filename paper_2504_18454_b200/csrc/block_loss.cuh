@@ -1,7 +1,7 @@
 // Row kernels of the block operators: cross entropy over a vocabulary, forward and backward.
 //
-// Forward: one pass over the logits.  A lane keeps the largest value that it has seen and the sum of e^(z - largest), for two
-// pieces of 16 bytes at a time; lanes, then warps, join theirs.  Rows are read by the aligned 16-byte pieces that hold their
+// Forward: one pass over the logits.  A lane keeps the largest value that it has seen and the sum of e^(z - largest), with the
+// next pieces of 16 bytes -- of the next row, at a row's end -- under way; lanes, then warps, join theirs.  Rows are read by the aligned 16-byte pieces that hold their
 // values (a vocabulary of odd size starts every row at another offset), what is outside masked.
 // Backward: e^(z - lse) from what the forward call left, one read and one write a value.
 // Bound by memory.
@@ -52,34 +52,56 @@ __device__ __forceinline__ void floats_of(const uint4& p, float (&v)[16 / sizeof
 template <typename T>
 __global__ void __launch_bounds__(1024) loss_forward_kernel(const __grid_constant__ LossArgs a)
 {
-    constexpr int V = 16 / (int)sizeof(T), P = 4;         // pieces of a lane under way
-    __shared__ Soft places[32];
+    constexpr int V = 16 / (int)sizeof(T), P = 4;         // pieces of a lane at a time; as many more under way
+    __shared__ Soft places[2][32];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
     const uint32_t size = a.warps * 32, me = threadIdx.x - team * size;
     const int64_t k = blockIdx.y;
+    const uint64_t rows_step = (uint64_t)gridDim.x * teams;
     let_next_start();
     wait_for_previous();
-    const uint64_t row = (uint64_t)blockIdx.x * teams + team;
-    if (row >= a.rows) return;                            // (a whole team: its barrier is its own)
-    const T* z = static_cast<const T*>(a.z) + k * a.zw + (int64_t)row * a.zr;
-    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(z) & 15) / (uint32_t)sizeof(T);      // values of the first piece that are not the row's
-    const uint4* p = reinterpret_cast<const uint4*>(z - off);
-    const uint32_t end = off + a.vocab, pieces = (end + V - 1) / V;
-    Soft s{-INFINITY, 0.0f};
-    for (uint32_t i = me; i < pieces; i += size * P) {
-        uint4 q[P];
+    // a row, and what a team has come to in it
+    struct Place {
+        const uint4* p;
+        const T*     z;
+        uint64_t     row;
+        uint32_t     off, end, pieces, i;                 // values of the first piece that are not the row's; the last one's end
+    } now, next;
+    auto enter = [&](uint64_t row) {
+        Place at;
+        at.row = row;
+        at.z = static_cast<const T*>(a.z) + k * a.zw + (int64_t)row * a.zr;
+        at.off = (uint32_t)(reinterpret_cast<uintptr_t>(at.z) & 15) / (uint32_t)sizeof(T);
+        at.p = reinterpret_cast<const uint4*>(at.z - at.off);
+        at.end = at.off + a.vocab;
+        at.pieces = (at.end + V - 1) / V;
+        at.i = me;
+        return at;
+    };
+    auto fetch = [&](const Place& at, uint4 (&q)[P]) {
 #pragma unroll
-        for (int j = 0; j < P; ++j) q[j] = i + j * size < pieces ? __ldg(p + i + j * size) : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < P; ++j) q[j] = at.row < a.rows && at.i + j * size < at.pieces ? __ldg(at.p + at.i + j * size) : make_uint4(0, 0, 0, 0);
+    };
+    now = enter((uint64_t)blockIdx.x * teams + team);
+    uint4 q[P], ahead[P];
+    fetch(now, q);
+    Soft s{-INFINITY, 0.0f};
+    for (uint32_t turn = 0; now.row < a.rows;) {
+        // (the row ends at the same time for all lanes of the team)
+        const bool ends = now.i - me + size * P >= now.pieces;
+        if (ends) next = enter(now.row + rows_step);
+        else { next = now; next.i += size * P; }
+        fetch(next, ahead);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t at = i + j * size;
-            if (at >= pieces) break;
+            const uint32_t at = now.i + j * size;
+            if (at >= now.pieces) break;
             float v[V];
             floats_of<T>(q[j], v);
-            if (at == 0 || (at + 1) * V > end) {
+            if (at == 0 || (at + 1) * V > now.end) {
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    if (at * V + e < off || at * V + e >= end) v[e] = -INFINITY;
+                    if (at * V + e < now.off || at * V + e >= now.end) v[e] = -INFINITY;
             }
             float top = v[0];
 #pragma unroll
@@ -101,25 +123,33 @@ __global__ void __launch_bounds__(1024) loss_forward_kernel(const __grid_constan
             f2_get(sum, x, y);
             s.sum += x + y;
         }
-    }
+        if (ends) {
 #pragma unroll
-    for (int d = 16; d; d >>= 1)
-        s = soft_join(s, Soft{__shfl_xor_sync(0xFFFFFFFFu, s.top, d), __shfl_xor_sync(0xFFFFFFFFu, s.sum, d)});
-    if (a.warps > 1) {
-        if (lane == 0) places[warp] = s;
-        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(size) : "memory");
-        if (me != 0) return;
-        s = places[warp];
-        for (uint32_t j = 1; j < a.warps; ++j) s = soft_join(s, places[warp + j]);
-    } else if (me != 0) {
-        return;
+            for (int d = 16; d; d >>= 1)
+                s = soft_join(s, Soft{__shfl_xor_sync(0xFFFFFFFFu, s.top, d), __shfl_xor_sync(0xFFFFFFFFu, s.sum, d)});
+            if (a.warps > 1) {                            // (the places of one row are read while the next one's are written)
+                if (lane == 0) places[turn][warp] = s;
+                asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(size) : "memory");
+                if (me == 0) {
+                    s = places[turn][warp];
+                    for (uint32_t j = 1; j < a.warps; ++j) s = soft_join(s, places[turn][warp + j]);
+                }
+                turn ^= 1;
+            }
+            if (me == 0) {
+                const float log_sum = logf(s.sum);
+                const int32_t t = a.target[k * a.tw + (int64_t)now.row];
+                a.lse[k * a.sw + (int64_t)now.row] = s.top == -INFINITY && s.sum == 0.0f ? -INFINITY : s.top + log_sum;
+                float loss = 0.0f;
+                if (t >= 0) loss = (uint32_t)t < a.vocab ? (s.top - to_f(now.z[t])) + log_sum : __uint_as_float(0x7FFFFFFFu);
+                a.loss[k * a.lw + (int64_t)now.row] = loss;
+            }
+            s = Soft{-INFINITY, 0.0f};
+        }
+        now = next;
+#pragma unroll
+        for (int j = 0; j < P; ++j) q[j] = ahead[j];
     }
-    const float log_sum = logf(s.sum);
-    const int32_t t = a.target[k * a.tw + (int64_t)row];
-    a.lse[k * a.sw + (int64_t)row] = s.top == -INFINITY && s.sum == 0.0f ? -INFINITY : s.top + log_sum;
-    float loss = 0.0f;
-    if (t >= 0) loss = (uint32_t)t < a.vocab ? (s.top - to_f(z[t])) + log_sum : __uint_as_float(0x7FFFFFFFu);
-    if (a.loss) a.loss[k * a.lw + (int64_t)row] = loss;
 }
 
 // dz = (e^(z - lse) - [target]) dloss of a part of a row: `pieces` of 16 bytes a lane, from where the row's copy in memory

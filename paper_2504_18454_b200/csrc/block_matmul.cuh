@@ -253,7 +253,7 @@ template <int ROW, int E>
 __device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
     constexpr uint32_t kPieces = ROW / 16;
-    if (rows == 32 && cols >= ROW / E && wide) {          // the same for the whole warp
+    if (rows && cols >= ROW / E && wide) {                // the same for the whole warp
         const uint32_t piece = lane % kPieces, row = lane / kPieces;
         unsigned char* p = to + (int64_t)row * row_bytes + piece * 16;
         const int64_t step = row_bytes * (32 / kPieces);
@@ -261,7 +261,10 @@ __device__ __forceinline__ void block_out(uint32_t base, unsigned char* to, int6
 #pragma unroll
         for (uint32_t i = 0; i < kPieces; ++i) lds128(block_at<ROW>(base, i * (32 / kPieces) + row, piece), v[i]);
 #pragma unroll
-        for (uint32_t i = 0; i < kPieces; ++i) { *reinterpret_cast<uint4*>(p) = v[i]; p += step; }
+        for (uint32_t i = 0; i < kPieces; ++i) {
+            if (i * (32 / kPieces) + row < rows) *reinterpret_cast<uint4*>(p) = v[i];
+            p += step;
+        }
     } else if (rows && cols) {
         block_out_edge<ROW, E>(base, to, row_bytes, rows, min(cols, (uint32_t)(ROW / E)), lane);
     }
@@ -282,13 +285,14 @@ template <int E, int PIECES>
 __device__ __forceinline__ void block_in(uint32_t base, const unsigned char* from, int64_t row_bytes, uint32_t rows, uint32_t cols, bool wide, uint32_t lane)
 {
     constexpr uint32_t kFirst = 4 - PIECES;
-    if (rows == 32 && cols >= PIECES * 16 / E && wide) {
+    if (rows && cols >= PIECES * 16 / E && wide) {
         const uint32_t piece = lane % PIECES, row = lane / PIECES;
         const unsigned char* p = from + (int64_t)row * row_bytes + piece * 16;
         const int64_t step = row_bytes * (32 / PIECES);
 #pragma unroll
         for (uint32_t i = 0; i < PIECES; ++i) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(block_at<64>(base, i * (32 / PIECES) + row, kFirst + piece)), "l"(p) : "memory");
+            const bool on = i * (32 / PIECES) + row < rows;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(block_at<64>(base, i * (32 / PIECES) + row, kFirst + piece)), "l"(on ? p : from), "r"(on ? 16u : 0u) : "memory");
             p += step;
         }
     } else if (rows && cols) {                            // (a block that is all outside is not read)
@@ -417,6 +421,37 @@ __device__ __forceinline__ f2 act_pair(f2 g, f2& slope)
         const float ax = act<ACT, SLOPE, false>(x, sx), ay = act<ACT, SLOPE, false>(y, sy);
         if constexpr (SLOPE) slope = f2_of(sx, sy);
         return f2_of(ax, ay);
+    }
+}
+
+// The same for the linear operator: GELU of a pair that is rounded to bfloat16 by the rational approximation of erf with one
+// exponential (Abramowitz and Stegun 7.1.26, off by at most 1.5e-7), which is also the slope's.  (erff for each value took the
+// pass before the activation from 9 us to 27: 5 workers of 4449 tokens, 144 columns.)
+template <typename T, int ACT, bool SLOPE>
+__device__ __forceinline__ f2 linear_act(f2 g, f2& slope)
+{
+    if constexpr (sizeof(T) == 2 && ACT == PALSGD_ACT_GELU) {
+        float x, y;
+        f2_get(g, x, y);
+        const float ax = fabsf(x), ay = fabsf(y);
+        f2 t = f2_fma(f2_of(ax, ay), f2_same(0.3275911f * 0.70710678118654752f), f2_same(1.0f));
+        float tx, ty, ex, ey;
+        f2_get(t, tx, ty);
+        t = f2_of(fast_inverse(tx), fast_inverse(ty));
+        f2_get(f2_mul(f2_mul(g, g), f2_same(-0.5f * 1.4426950408889634f)), ex, ey);
+        const f2 e = f2_of(fast_exp2(ex), fast_exp2(ey));                // e^(-g^2 / 2)
+        f2 p = f2_fma(t, f2_same(1.061405429f), f2_same(-1.453152027f));
+        p = f2_fma(p, t, f2_same(1.421413741f));
+        p = f2_fma(p, t, f2_same(-0.284496736f));
+        p = f2_fma(p, t, f2_same(0.254829592f));
+        float qx, qy;
+        f2_get(f2_mul(f2_mul(f2_mul(p, t), e), f2_same(0.5f)), qx, qy);  // Phi(-|g|)
+        const f2 cdf = f2_of(x > 0.0f ? 1.0f - qx : qx, y > 0.0f ? 1.0f - qy : qy);
+        // (a gate beyond 10^19: its square's exponential is 0, and so is what it multiplies)
+        if constexpr (SLOPE) slope = f2_fma(f2_mul(f2_of(fminf(fmaxf(x, -1e4f), 1e4f), fminf(fmaxf(y, -1e4f), 1e4f)), f2_same(0.39894228040143268f)), e, cdf);
+        return f2_mul(g, cdf);
+    } else {
+        return act_pair<T, ACT, SLOPE>(g, slope);
     }
 }
 
@@ -873,7 +908,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     for (uint32_t j = 0; j < kOcts; ++j) {
                         f2 r[4], unused;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) z[4 * j + i] = act_pair<T, ACT, false>(z[4 * j + i], unused);
+                        for (int i = 0; i < 4; ++i) z[4 * j + i] = linear_act<T, ACT, false>(z[4 * j + i], unused);
                         if (a.residual.p) {
                             row_get<T>(b1, lane, j, r);
 #pragma unroll
@@ -1131,11 +1166,15 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinA
         const float* p = it.part + k * it.w + (int64_t)row * it.ld + c;
         float sum[8];
         Vec<float, 8>::load(p, sum);
-        for (uint32_t s = 1; s < it.splits; ++s) {
-            float v[8];
-            Vec<float, 8>::load(p + s * it.share, v);
+        for (uint32_t s = 1; s < it.splits; s += 4) {     // (four loads under way; the order of the sums stays)
+            float v[4][8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += v[j];
+            for (uint32_t u = 0; u < 4; ++u) if (s + u < it.splits) Vec<float, 8>::load(p + (s + u) * it.share, v[u]);
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u)
+                if (s + u < it.splits)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
         }
         T* to = static_cast<T*>(it.out.p) + k * it.out.w + (int64_t)row * it.out.r + c;
         const uint32_t n = min(it.N - c, 8u);

@@ -240,9 +240,9 @@ extern "C" int palsgd_cross_entropy_forward(const palsgd_loss_shape* s, const pa
     a.warps = 1;
     while (a.warps < (least == 1 ? 32u : 8u) && pieces >= least * a.warps * 64) a.warps *= 2;
     const uint64_t teams = a.warps <= 8 ? 8 / a.warps : 1;
-    const uint64_t ctas = ceil_div(M, teams);
-    if (ctas > 0x7FFFFFFFull) return PALSGD_EUNSUPPORTED;
-    return launch("cross entropy", es == 4 ? loss_forward_kernel<float> : loss_forward_kernel<bf16>, dim3((unsigned)ctas, s->K), (unsigned)(teams * a.warps * 32), 0,
+    // as many CTAs as run at a time, each team with as many rows as any other (but for the last turn)
+    const uint64_t run = (a.warps <= 8 ? 4ull : 1ull) * sm_count() / s->K, turns = ceil_div(M, (run ? run : 1) * teams);
+    return launch("cross entropy", es == 4 ? loss_forward_kernel<float> : loss_forward_kernel<bf16>, dim3((unsigned)ceil_div(M, turns * teams), s->K), (unsigned)(teams * a.warps * 32), 0,
                   static_cast<cudaStream_t>(stream), a);
 }
 
