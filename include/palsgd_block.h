@@ -173,11 +173,12 @@ int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const palsgd_heads* d
  * 8BIT: pre, pre_e, the 8-bit checkpoint taken from the binary32 values.  With act = NONE the backward call needs none of it, and
  * save has to be NONE there and here.  b: rows of d_out in the storage type, one per worker (row_stride unused).
  *
- * Backward, at the saved z (the value that it stands for), x in the storage type or (x_e given, save = 8BIT) as a checkpoint:
+ * Backward, at the saved z (the value that it stands for), x in the storage type or, where x_e is given, as a checkpoint:
  *   dz = dy act'(z);   dx = dz w;   dw = dz^T x;   db = sum over tokens of dz;   the residual's gradient is dy itself
  * BF16: dz is rounded to bfloat16 once, for the products; db sums the unrounded values.  dx and db may be NULL.  Outputs are
  * overwritten.  tokens = 0: dw and db are zero.  Sums have a fixed order: the same call gives the same bits.
- * FP32 products as in the feed-forward block; calls of at most 8 tokens sum in binary32 throughout.
+ * FP32 products as in the feed-forward block; small calls sum in binary32 multiply-adds throughout, and keep dz in binary32.
+ * BF16 GELU is off by at most 1.5e-7 (1 + |z|) before it is rounded, the other activations by a few units of binary32.
  * Workspace and errors as for the feed-forward block (d_in or d_out = 0: EINVAL).
  */
 enum { PALSGD_ACT_NONE = 4 };

@@ -1,10 +1,13 @@
 """The block operators as functions that torch's autograd can differentiate.
 
 They keep what the C ABI's backward calls ask for and nothing else; with `checkpoint8` the feed-forward block keeps its
-input, gate and up in 8 bits (8.25 bits a value), and its backward pass works on the values that those stand for.
+input, gate and up in 8 bits (8.25 bits a value), the linear operator its input and what goes into its activation, and their
+backward passes work on the values that those stand for.
 They are differentiable once: under create_graph=True their backward raises RuntimeError.
 """
 from __future__ import annotations
+
+from typing import Optional
 
 import torch
 
@@ -62,6 +65,74 @@ class _QkNormRope(torch.autograd.Function):
         return (*grads, None, None, None, None, None)
 
 
+def _rows(d: torch.Tensor) -> torch.Tensor:
+    """An incoming gradient as the C ABI takes it: the last axis contiguous (that of a sum is expanded)."""
+    return d if d.stride(-1) == 1 or d.shape[-1] == 1 else d.contiguous()
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, residual, activation, checkpoint8, recording):
+        needs = recording and any(ctx.needs_input_grad[:3])  # (the residual's gradient is the incoming one)
+        bent = activation != block.ACT_NONE
+        save = (block.SAVE_8BIT if checkpoint8 else block.SAVE_FULL) if needs and bent else block.SAVE_NONE
+        y, pre = block.linear_forward(x, w, bias, residual, activation=activation, save=save)
+        if needs:
+            ctx.activation, ctx.dtype, ctx.eight_x, ctx.eight_pre = activation, x.dtype, checkpoint8, checkpoint8 and bent
+            kept = [*block.act8_pack(x)[:2]] if checkpoint8 else [x]
+            if bent:
+                kept += [pre.q, pre.exponent] if checkpoint8 else [pre]
+            ctx.save_for_backward(w, *kept)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        _once("linear")
+        dy, need = _rows(dy), ctx.needs_input_grad
+        if not any(need[:3]):
+            return None, None, None, dy, None, None, None
+        w, *kept = ctx.saved_tensors
+        x = block.Act8(kept.pop(0), kept.pop(0), ctx.dtype) if ctx.eight_x else kept.pop(0)
+        pre = None if not kept else block.Act8(*kept, ctx.dtype) if ctx.eight_pre else kept[0]
+        dx, dw, db = block.linear_backward(dy, x, w, pre, activation=ctx.activation, need_dx=need[0], need_dbias=need[2])
+        return dx, dw if need[1] else None, db, dy if need[3] else None, None, None, None
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, b, residual, eps, recording):
+        needs = recording and any(ctx.needs_input_grad)
+        y, total, mean, rstd = block.layer_norm_forward(x, w, b, residual, eps=eps, stats=needs)
+        ctx.added = residual is not None
+        ctx.set_materialize_grads(False)
+        if needs:
+            ctx.save_for_backward(total, w, mean, rstd)
+        return (y, total) if ctx.added else y
+
+    @staticmethod
+    def backward(ctx, dy, dtotal=None):
+        _once("layer_norm")
+        x, w, mean, rstd = ctx.saved_tensors
+        dy = torch.zeros_like(x) if dy is None else _rows(dy)
+        dx, dw, db = block.layer_norm_backward(dy, x, w, mean, rstd, None if dtotal is None else _rows(dtotal))
+        return dx, dw, db, dx if ctx.added else None, None, None
+
+
+class _CrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, in_place):
+        loss, lse = block.cross_entropy_forward(logits, targets)
+        ctx.in_place = in_place
+        ctx.save_for_backward(logits, targets, lse)
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        _once("cross_entropy")
+        logits, targets, lse = ctx.saved_tensors
+        return block.cross_entropy_backward(_rows(dloss), logits, targets, lse, out=logits if ctx.in_place else None), None, None
+
+
 def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
               activation: int = block.ACT_SILU, checkpoint8: bool = False) -> torch.Tensor:
     """`block.ffn_forward` with gradients for x and the three weights."""
@@ -72,3 +143,21 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, w_q: torch.Tensor, w_k: torch
                  sin: torch.Tensor, positions: torch.Tensor, *, eps: float = 1e-6, interleaved: bool = False):
     """`block.qk_norm_rope` with gradients for q, k and the two norm weights."""
     return _QkNormRope.apply(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, *,
+           activation: int = block.ACT_NONE, checkpoint8: bool = False) -> torch.Tensor:
+    """`block.linear_forward` with gradients for x, w, bias and residual."""
+    return _Linear.apply(x, w, bias, residual, activation, checkpoint8, torch.is_grad_enabled())
+
+
+def layer_norm(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-5):
+    """`block.layer_norm_forward` with gradients for x, w, b and residual: y, or (y, x + residual) where there is a residual."""
+    return _LayerNorm.apply(x, w, b, residual, eps, torch.is_grad_enabled())
+
+
+def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, *, in_place: bool = False) -> torch.Tensor:
+    """`block.cross_entropy_forward`'s losses (K, tokens) with a gradient for the logits.  in_place: the backward pass writes the
+    gradient over the logits, which nothing may need any more (autograd tells where it does; a product's backward pass does not
+    need its result)."""
+    return _CrossEntropy.apply(logits, targets, in_place)

@@ -256,14 +256,12 @@ def linear_backward(dy: torch.Tensor, x: Saved, w: torch.Tensor, saved: Optional
                     workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None):
     """palsgd_linear_backward: (dx, dw, dbias) from dy and what the forward call saved; the residual's gradient is dy.
 
-    With `saved` as Act8, x may be an Act8 too.  `out` = (dx, dw, dbias) gives the memory to write to (e.g. the workers'
+    x may be an Act8.  `out` = (dx, dw, dbias) gives the memory to write to (e.g. the workers'
     gradient buffers); entries may be None.  need_dx, need_dbias = False leave those out (they come back as None).
     """
     where = "palsgd_linear_backward"
     native = _native or _ext()
     save = SAVE_NONE if saved is None else SAVE_8BIT if isinstance(saved, Act8) else SAVE_FULL
-    if isinstance(x, Act8) and save != SAVE_8BIT:
-        _refuse(where, "x may be an Act8 only where saved is")
     out = (None,) * 3 if out is None else out
     if len(out) != 3:
         _refuse(where, "out must be (dx, dw, dbias)")

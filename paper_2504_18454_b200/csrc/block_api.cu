@@ -997,7 +997,6 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
     const Mat dx(dx_, s->K, M), dw(dw_, s->K, N), db(db_, s->K, 1);
     const bool bent = s->activation != PALSGD_ACT_NONE;
     if (bent && s->save == PALSGD_SAVE_NONE) return PALSGD_EINVAL;
-    if (x_e.given && s->save != PALSGD_SAVE_8BIT) return PALSGD_EINVAL;
     BLOCK_TRY(check_mat(dy, s->K, M, N, es, false));
     BLOCK_TRY(check_mat(x, s->K, M, D, x_e.given ? 1 : es, false));
     if (x_e.given) BLOCK_TRY(check_mat(x_e, s->K, M, ceil_div(D, PALSGD_ACT8_GROUP), 1, false));

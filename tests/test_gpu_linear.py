@@ -79,6 +79,12 @@ def test_backward(dtype, size, save):
     want = linear_backward64(dy, x, w, z, kind, dtype == "bf16")
     for t, name in zip(got, ("dx", "dw", "db")):
         within(t, *want[name], name)
+    if save == P.SAVE_NONE:                                # the input in 8 bits, no activation
+        x8 = P.act8_pack(x)
+        got = P.linear_backward(dy, x8, w)
+        want = linear_backward64(dy, P.act8_unpack(x8, dtype=torch.float32), w, z, kind, dtype == "bf16")
+        for t, name in zip(got, ("dx", "dw", "db")):
+            within(t, *want[name], name)
     if save == P.SAVE_8BIT:                                # the input in the storage type beside an 8-bit z
         within(P.linear_backward(dy, x.to(DT[dtype]), w, saved, activation=kind)[1], *want["dw"], "dw")
 
