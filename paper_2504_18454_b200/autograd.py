@@ -3,7 +3,9 @@
 They keep what the C ABI's backward calls ask for and nothing else; with `checkpoint8` the feed-forward block keeps its
 input, gate and up in 8 bits (8.25 bits a value), the linear operator its input and what goes into its activation, and their
 backward passes work on the values that those stand for.
-They are differentiable once: under create_graph=True their backward raises RuntimeError.
+They are differentiable once: under create_graph=True their backward raises RuntimeError.  As with torch's own functions, no
+eager graph of the same leaves may be alive while a backward pass is captured (the engine would make the capture wait for that
+graph's stream: an error, and no graph).
 """
 from __future__ import annotations
 

@@ -220,7 +220,7 @@ int run_stage(const Stage& st, uint32_t K, int sms, cudaStream_t stream)
     if (st.n == 0) return PALSGD_OK;
     uint64_t most = 1;
     for (uint32_t i = 0; i < st.n; ++i) most = st.a.item[i].units > most ? st.a.item[i].units : most;
-    const uint64_t want = ceil_div(most, 256), cap = 32ull * sms;
+    const uint64_t want = ceil_div(most, 1024), cap = 8ull * sms;
     return launch("operand copies", stage_kernel, dim3((unsigned)(want < cap ? want : cap), st.n, K), 256, 0, stream, st.a);
 }
 
@@ -615,7 +615,7 @@ int run_slope(const palsgd_linear_shape* s, SlopeArgs& a, const Stage& copies, i
     uint32_t all = a.ctas = (uint32_t)ctas;
     for (uint32_t i = 0; i < kMaxStaged; ++i) {
         a.first_copy[i] = all;
-        const uint64_t want = i < copies.n ? ceil_div(copies.a.item[i].units, 512) : 0, cap = 8ull * sms;
+        const uint64_t want = i < copies.n ? ceil_div(copies.a.item[i].units, 1024) : 0, cap = 8ull * sms;
         all += (uint32_t)(want < cap ? want : cap);
     }
     a.first_copy[kMaxStaged] = all;

@@ -751,7 +751,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 }
                 if (!ok || !acc_wait()) break;
             } else if constexpr (Shape::kWide || MODE == MAT_LINEAR) {
-                // the pieces' sums joined in registers, and put back for what follows
+                // the pieces' sums joined in registers, and put back for what follows (kept there through the epilogue, they spill:
+                // linear in 8 bits, 1024 tokens, 768 x 2048: 43 us, and 57)
                 float sum[64];
 #pragma unroll
                 for (int i = 0; i < 64; ++i) sum[i] = 0.0f;
@@ -808,9 +809,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             // needed, its latency stood in every block's way.)
             auto linear_z = [&](uint32_t j, f2 (&z)[kCols / 2]) {
                 float v[kCols];
+                const float mine = j < 32 ? bias[0] : bias[1];
 #pragma unroll
                 for (uint32_t i = 0; i < kCols; i += 16) tmem_load16(src + j + i, *reinterpret_cast<float(*)[16]>(v + i));
-                const float mine = j < 32 ? bias[0] : bias[1];
                 tmem_load_wait();
                 if (a.bias.p) {
 #pragma unroll
@@ -1094,42 +1095,58 @@ struct StageItem {
 };
 struct StageArgs { StageItem item[kMaxStaged]; };
 
-// Block `block` of the `blocks` that copy worker k's part of an item.
+// Block `block` of the `blocks` that copy worker k's part of an item: a thread has four units under way.
 __device__ __forceinline__ void stage_item(const StageItem& it, int64_t k, uint32_t block, uint32_t blocks)
 {
+    constexpr uint32_t U = 4;
     if (k >= it.K) return;
-    for (uint64_t i = (uint64_t)block * 256 + threadIdx.x; i < it.units; i += (uint64_t)blocks * 256) {
-        const uint64_t row = it.units < 0x80000000ull ? it.per_row.of((uint32_t)i) : i / it.per_row.d;
-        const uint32_t c = (uint32_t)(i - row * it.per_row.d) * 8;
-        const int64_t from = k * it.w + (int64_t)row * it.r + c;
-        float v[8];
-        const uint32_t n = c < it.cols ? min(it.cols - c, 8u) : 0;
-        if (it.kind == STAGE_BF16) {
-            const uint4 q = get16(static_cast<const unsigned char*>(it.src) + 2 * from, 2 * n);
-            *reinterpret_cast<uint4*>(it.dst + (k * it.rows + (int64_t)row) * it.ld + c) = q;
-            continue;
-        } else if (it.kind == STAGE_ACT8) {
-            const unsigned char* p = static_cast<const unsigned char*>(it.src) + from;
-            uint2 q;
-            if (it.wide && n == 8) q = __ldg(reinterpret_cast<const uint2*>(p));
-            else { const uint4 t = get16(p, n); q = make_uint2(t.x, t.y); }
-            const float s = act8_step(it.e[k * it.ew + (int64_t)row * it.er + c / 32]);
-            act8_value4(q.x, s, v);
-            act8_value4(q.y, s, v + 4);
-        } else if (it.wide && n == 8) {
-            Vec<float, 8>::load(static_cast<const float*>(it.src) + from, v);
-        } else {
+    for (uint64_t i0 = (uint64_t)block * (256 * U) + threadIdx.x; i0 < it.units; i0 += (uint64_t)blocks * (256 * U)) {
+        uint4 q[U][2];                                    // as they lie in memory; 8 bits: the exponent behind them
+        int64_t to[U];
 #pragma unroll
-            for (uint32_t j = 0; j < 2; ++j) {
-                const uint4 q = get16(static_cast<const unsigned char*>(it.src) + 4 * (from + 4 * j), n > 4 * j ? 4 * min(n - 4 * j, 4u) : 0);
-                v[4 * j] = __uint_as_float(q.x); v[4 * j + 1] = __uint_as_float(q.y); v[4 * j + 2] = __uint_as_float(q.z); v[4 * j + 3] = __uint_as_float(q.w);
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint64_t i = i0 + u * 256;
+            to[u] = -1;
+            if (i >= it.units) continue;
+            const uint64_t row = it.units < 0x80000000ull ? it.per_row.of((uint32_t)i) : i / it.per_row.d;
+            const uint32_t c = (uint32_t)(i - row * it.per_row.d) * 8, n = c < it.cols ? min(it.cols - c, 8u) : 0;
+            const int64_t from = k * it.w + (int64_t)row * it.r + c;
+            to[u] = (k * it.rows + (int64_t)row) * it.ld + c;
+            if (it.kind == STAGE_BF16) {
+                q[u][0] = get16(static_cast<const unsigned char*>(it.src) + 2 * from, 2 * n);
+            } else if (it.kind == STAGE_ACT8) {
+                const unsigned char* p = static_cast<const unsigned char*>(it.src) + from;
+                if (it.wide && n == 8) { const uint2 t = __ldg(reinterpret_cast<const uint2*>(p)); q[u][0] = make_uint4(t.x, t.y, 0, 0); }
+                else q[u][0] = get16(p, n);
+                q[u][1].x = it.e[k * it.ew + (int64_t)row * it.er + c / 32];
+            } else {
+                const float* p = static_cast<const float*>(it.src) + from;
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j)
+                    q[u][j] = it.wide && n == 8 ? __ldg(reinterpret_cast<const uint4*>(p) + j)
+                                                : get16(reinterpret_cast<const unsigned char*>(p + 4 * j), n > 4 * j ? 4 * min(n - 4 * j, 4u) : 0);
             }
         }
-        bf16* to = it.dst + (k * it.rows + (int64_t)row) * it.ld + c;
-        if (it.kind == STAGE_SPLIT) {
-            three_parts<8>(v, [&](int part, const uint32_t (&w)[4]) { *reinterpret_cast<uint4*>(to + part * it.part) = make_uint4(w[0], w[1], w[2], w[3]); });
-        } else {
-            Vec<bf16, 8>::store(to, v);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            if (to[u] < 0) continue;
+            if (it.kind == STAGE_BF16) {
+                *reinterpret_cast<uint4*>(it.dst + to[u]) = q[u][0];
+            } else if (it.kind == STAGE_ACT8) {
+                float v[8];
+                const float s = act8_step(q[u][1].x);
+                act8_value4(q[u][0].x, s, v);
+                act8_value4(q[u][0].y, s, v + 4);
+                Vec<bf16, 8>::store(it.dst + to[u], v);
+            } else {
+                float v[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j) {
+                    v[4 * j] = __uint_as_float(q[u][j].x); v[4 * j + 1] = __uint_as_float(q[u][j].y);
+                    v[4 * j + 2] = __uint_as_float(q[u][j].z); v[4 * j + 3] = __uint_as_float(q[u][j].w);
+                }
+                three_parts<8>(v, [&](int part, const uint32_t (&w)[4]) { *reinterpret_cast<uint4*>(it.dst + to[u] + part * it.part) = make_uint4(w[0], w[1], w[2], w[3]); });
+            }
         }
     }
 }

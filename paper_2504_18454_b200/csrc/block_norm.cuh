@@ -297,17 +297,19 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
 
     let_next_start();
     wait_for_previous();
-    auto fetch = [&]() {                                  // (behind the last row: zeros, for the sums of dw and db of a warp's other teams)
+    auto fetch = [&]() {
         const bool more = ahead < a.rows;
-        const int64_t at = more ? (int64_t)ahead : 0;
-        const uint32_t some = more ? width : 0;
+        if (more || N == 1) {                             // (narrow rows, behind the last one: zeros, for the sums of a warp's other teams)
+            const int64_t at = more ? (int64_t)ahead : 0;
+            const uint32_t some = N > 1 || more ? width : 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            ring.fetch(put * Q + i, x + at * a.xr, first + i * step, some);
-            ring.fetch(put * Q + N + i, dy + at * a.dr, first + i * step, some);
-            if constexpr (ADD) ring.fetch(put * Q + 2 * N + i, r + at * a.rr, first + i * step, some);
+            for (int i = 0; i < N; ++i) {
+                ring.fetch(put * Q + i, x + at * a.xr, first + i * step, some);
+                ring.fetch(put * Q + N + i, dy + at * a.dr, first + i * step, some);
+                if constexpr (ADD) ring.fetch(put * Q + 2 * N + i, r + at * a.rr, first + i * step, some);
+            }
+            ahead += rows_step;
         }
-        ahead += rows_step;
         ring.commit();
         put = put + 1 == S ? 0 : put + 1;
     };

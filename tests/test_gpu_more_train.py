@@ -131,7 +131,7 @@ def test_a_captured_step_of_the_autograd_functions():
 
     def step():
         loss = A.cross_entropy(A.linear(A.layer_norm(x, lw, lb), w, b, activation=P.ACT_SILU), t).mean()
-        return (loss, *torch.autograd.grad(loss, leaves))
+        return (loss.detach(), *torch.autograd.grad(loss, leaves))
 
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
