@@ -159,9 +159,16 @@ constexpr uint32_t kNormMostWarps = 32;                                 // of a 
 template <int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], uint32_t lanes, uint32_t team, float* places, uint32_t& turn)
 {
-    for (uint32_t d = min(lanes, 32u) / 2; d; d >>= 1)
+    if (lanes >= 32) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+        for (int d = 16; d; d >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+    } else {
+        for (uint32_t d = lanes / 2; d; d >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+    }
     if (lanes <= 32) return;
     const uint32_t warps = lanes / 32, warp = threadIdx.x >> 5, first = team * warps;
     float* p = places + turn * (2 * kNormMostWarps);
@@ -172,10 +179,30 @@ __device__ __forceinline__ void team_sum(float (&v)[N], uint32_t lanes, uint32_t
     asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(lanes) : "memory");
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        float s = p[i * kNormMostWarps + first];
-        for (uint32_t j = 1; j < warps; ++j) s += p[i * kNormMostWarps + first + j];
-        v[i] = s;
+        const float* q = p + i * kNormMostWarps + first;
+        if (warps == 2) {
+            const float2 t = *reinterpret_cast<const float2*>(q);
+            v[i] = t.x + t.y;
+        } else {                                          // (a team's first warp is a multiple of its warps)
+            float s = 0.0f;
+            for (uint32_t j = 0; j < warps; j += 4) {
+                const float4 t = *reinterpret_cast<const float4*>(q + j);
+                s += (t.x + t.y) + (t.z + t.w);
+            }
+            v[i] = s;
+        }
     }
+}
+
+// 1 / sqrt(v) to about a unit in the last place: the unit's approximation and one step of Newton's method.  (0 and infinity
+// stay what they are: the step would make a NaN of them.)
+__device__ __forceinline__ float inverse_root(float v)
+{
+    float r;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    const float e = fmaf(-v * r, r, 1.0f);
+    const float better = fmaf(0.5f * r, e, r);
+    return v > 1e-37f && v < 1e37f ? better : 1.0f / sqrtf(v);
 }
 
 // WARPS: of a CTA, 8 or as many as one team needs beyond that.  N: pieces a lane.  ADD: there is an addend (forward), a
@@ -184,18 +211,24 @@ template <typename T, int N, bool WIDE, bool ADD, int WARPS, int CTAS>
 __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 2 * N : N, S = norm_stages<T, WIDE, N>(Q / N, WARPS, CTAS);    // Q: pieces of a lane for a row
-    __shared__ float places[4 * kNormMostWarps];
+    __shared__ __align__(16) float places[4 * kNormMostWarps];
     extern __shared__ __align__(16) unsigned char ring_raw[];
     const uint32_t team = threadIdx.x / a.lanes, teams = blockDim.x / a.lanes;
     const uint32_t first = (threadIdx.x - team * a.lanes) * V, step = a.lanes * V, width = a.width;
     const uint32_t beside = N == 1 && a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
     const Ring<T, WIDE, N> ring(ring_raw, a.lanes);
     const int64_t k = blockIdx.y;
-    const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
     const T *w = static_cast<const T*>(a.w) + k * a.ww, *b = static_cast<const T*>(a.b) + k * a.bw;
     const uint64_t rows_step = (uint64_t)gridDim.x * teams;
     uint64_t row = (uint64_t)blockIdx.x * teams + team, ahead = row;
     uint32_t turn = 0, put = 0, got = 0;
+    // the rows that a team is at, and comes to next
+    const T *x = static_cast<const T*>(a.x) + k * a.xw + (int64_t)row * a.xr, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw + (int64_t)row * a.rr : 0);
+    const T *x_next = x, *r_next = r;
+    T* y = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
+    T* total = static_cast<T*>(a.total) + (ADD ? k * a.tw + (int64_t)row * a.tr : 0);
+    const int64_t x_step = (int64_t)rows_step * a.xr, r_step = (int64_t)rows_step * a.rr, y_step = (int64_t)rows_step * a.yr, t_step = (int64_t)rows_step * a.tr;
+    const float inv_width = 1.0f / (float)width;
 
     let_next_start();
     wait_for_previous();
@@ -203,10 +236,12 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
         if (ahead < a.rows) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                ring.fetch(put * Q + i, x + (int64_t)ahead * a.xr, first + i * step, width);
-                if constexpr (ADD) ring.fetch(put * Q + N + i, r + (int64_t)ahead * a.rr, first + i * step, width);
+                ring.fetch(put * Q + i, x_next, first + i * step, width);
+                if constexpr (ADD) ring.fetch(put * Q + N + i, r_next, first + i * step, width);
             }
             ahead += rows_step;
+            x_next += x_step;
+            if constexpr (ADD) r_next += r_step;
         }
         ring.commit();
         put = put + 1 == S ? 0 : put + 1;
@@ -227,10 +262,10 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
         f2 h[N][H], sum = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            piece_wide<T>(ring.get(got * Q + i, x + (int64_t)row * a.xr, first + i * step, width), h[i]);
+            piece_wide<T>(ring.get(got * Q + i, x, first + i * step, width), h[i]);
             if constexpr (ADD) {
                 f2 t[H];
-                piece_wide<T>(ring.get(got * Q + N + i, r + (int64_t)row * a.rr, first + i * step, width), t);
+                piece_wide<T>(ring.get(got * Q + N + i, r, first + i * step, width), t);
 #pragma unroll
                 for (int j = 0; j < H; ++j) h[i][j] = f2_add(h[i][j], t[j]);
             }
@@ -239,26 +274,29 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
         }
         got = got + 1 == S ? 0 : got + 1;
         if constexpr (ADD) {
-            T* total = static_cast<T*>(a.total) + k * a.tw + (int64_t)row * a.tr;
 #pragma unroll
             for (int i = 0; i < N; ++i) piece_store<T, WIDE>(total, first + i * step, on ? width : 0, piece_narrow<T>(h[i]));
+            total += t_step;
         }
         float s[1] = {f2_total(sum)};
         team_sum<1>(s, a.lanes, team, places, turn);
-        const float mean = s[0] / (float)width;
+        const float mean = s[0] * inv_width;
         sum = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int i = 0; i < N; ++i) {
+            const uint32_t c = first + i * step;
+            const f2 shift = f2_same(c < width ? -mean : 0.0f);          // (a piece behind the row's end stays zero)
 #pragma unroll
-            for (int j = 0; j < H; ++j) {
-                h[i][j] = f2_add(h[i][j], f2_same(-mean));
-                if (first + i * step + V > width) h[i][j] = inside<WIDE>(h[i][j], first + i * step + 2 * j, width);
-                sum = f2_fma(h[i][j], h[i][j], sum);
-            }
+            for (int j = 0; j < H; ++j) h[i][j] = f2_add(h[i][j], shift);
+            if (!WIDE && c + V > width)
+#pragma unroll
+                for (int j = 0; j < H; ++j) h[i][j] = inside<WIDE>(h[i][j], c + 2 * j, width);
+#pragma unroll
+            for (int j = 0; j < H; ++j) sum = f2_fma(h[i][j], h[i][j], sum);
+        }
         s[0] = f2_total(sum);
         team_sum<1>(s, a.lanes, team, places, turn);
-        const float rstd = 1.0f / sqrtf(s[0] / (float)width + a.eps);
-        T* y = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
+        const float rstd = inverse_root(fmaf(s[0], inv_width, a.eps));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             f2 wv[H], bv[H];
@@ -272,6 +310,9 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_forward_kernel(const __
             if (a.mean) a.mean[k * a.mw + (int64_t)row] = mean;
             if (a.rstd) a.rstd[k * a.sw + (int64_t)row] = rstd;
         }
+        if constexpr (!WIDE) x += x_step;                 // (of an aligned row nothing but its place in shared memory counts)
+        if constexpr (!WIDE && ADD) r += r_step;
+        y += y_step;
     }
 }
 
@@ -282,33 +323,42 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
 {
     constexpr bool kKeep = WARPS < 32;                    // the widest kernel forms xh and g twice: they would not fit its registers
     constexpr int V = kPieceValues<T>, H = V / 2, Q = ADD ? 3 * N : 2 * N, S = norm_stages<T, WIDE, N>(Q / N, WARPS, CTAS);
-    __shared__ float places[4 * kNormMostWarps];
+    __shared__ __align__(16) float places[4 * kNormMostWarps];
     extern __shared__ __align__(16) unsigned char ring_raw[];            // the ring; at the end [2][width] floats, where a CTA has more than one team
     const uint32_t team = threadIdx.x / a.lanes, teams = blockDim.x / a.lanes;
     const uint32_t first = (threadIdx.x - team * a.lanes) * V, step = a.lanes * V, width = a.width;
     const uint32_t beside = N == 1 && a.lanes < 32 ? team % (32 / a.lanes) : 0;    // teams of the warp before this one: a warp's teams go on together
     const Ring<T, WIDE, N> ring(ring_raw, a.lanes);
     const int64_t k = blockIdx.y;
-    const T *x = static_cast<const T*>(a.x) + k * a.xw, *r = static_cast<const T*>(a.r) + (ADD ? k * a.rw : 0);
-    const T *w = static_cast<const T*>(a.w) + k * a.ww, *dy = static_cast<const T*>(a.dy) + k * a.dw;
+    const T* w = static_cast<const T*>(a.w) + k * a.ww;
     const uint64_t rows_step = (uint64_t)gridDim.x * teams;
     uint64_t row = (uint64_t)blockIdx.x * teams + team, ahead = row;
     uint32_t turn = 0, put = 0, got = 0;
+    const T* x = static_cast<const T*>(a.x) + k * a.xw + (int64_t)row * a.xr;
+    const T* dy = static_cast<const T*>(a.dy) + k * a.dw + (int64_t)row * a.dr;
+    const T* r = static_cast<const T*>(a.r) + (ADD ? k * a.rw + (int64_t)row * a.rr : 0);
+    const T *x_next = x, *dy_next = dy, *r_next = r;
+    T* dx = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
+    const int64_t x_step = (int64_t)rows_step * a.xr, d_step = (int64_t)rows_step * a.dr, r_step = (int64_t)rows_step * a.rr, y_step = (int64_t)rows_step * a.yr;
+    const float inv_width = 1.0f / (float)width;
 
     let_next_start();
     wait_for_previous();
     auto fetch = [&]() {
         const bool more = ahead < a.rows;
         if (more || N == 1) {                             // (narrow rows, behind the last one: zeros, for the sums of a warp's other teams)
-            const int64_t at = more ? (int64_t)ahead : 0;
             const uint32_t some = N > 1 || more ? width : 0;
+            if (N == 1 && !more) { x_next = static_cast<const T*>(a.x); dy_next = static_cast<const T*>(a.dy); r_next = static_cast<const T*>(a.r); }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                ring.fetch(put * Q + i, x + at * a.xr, first + i * step, some);
-                ring.fetch(put * Q + N + i, dy + at * a.dr, first + i * step, some);
-                if constexpr (ADD) ring.fetch(put * Q + 2 * N + i, r + at * a.rr, first + i * step, some);
+                ring.fetch(put * Q + i, x_next, first + i * step, some);
+                ring.fetch(put * Q + N + i, dy_next, first + i * step, some);
+                if constexpr (ADD) ring.fetch(put * Q + 2 * N + i, r_next, first + i * step, some);
             }
             ahead += rows_step;
+            x_next += x_step;
+            dy_next += d_step;
+            if constexpr (ADD) r_next += r_step;
         }
         ring.commit();
         put = put + 1 == S ? 0 : put + 1;
@@ -324,10 +374,11 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
         for (int j = 0; j < H; ++j) dw[i][j] = db[i][j] = 0;
     }
     float mean = 0.0f, rstd = 0.0f;
+    const float *means = a.mean + k * a.mw, *rstds = a.rstd + k * a.sw;
     auto stats = [&](uint64_t at) {
         if (at >= a.rows) return;
-        mean = __ldg(a.mean + k * a.mw + (int64_t)at);
-        rstd = __ldg(a.rstd + k * a.sw + (int64_t)at);
+        mean = __ldg(means + at);
+        rstd = __ldg(rstds + at);
     };
     stats(row);
     for (; row - beside < a.rows; row += rows_step) {
@@ -342,8 +393,8 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
         // of columns that are there: a piece cut by the end, and a team without a row.)
         auto load = [&](int i, f2 (&xh)[H], f2 (&d)[H], f2 (&g)[H]) {
             f2 wv[H];
-            piece_wide<T>(ring.get(got * Q + i, x + (int64_t)row * a.xr, first + i * step, some), xh);
-            piece_wide<T>(ring.get(got * Q + N + i, dy + (int64_t)row * a.dr, first + i * step, some), d);
+            piece_wide<T>(ring.get(got * Q + i, x, first + i * step, some), xh);
+            piece_wide<T>(ring.get(got * Q + N + i, dy, first + i * step, some), d);
             piece_wide<T>(wp[i], wv);
 #pragma unroll
             for (int j = 0; j < H; ++j) {
@@ -367,13 +418,12 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
         }
         float s[2] = {f2_total(sg), f2_total(sx)};
         team_sum<2>(s, a.lanes, team, places, turn);
-        const f2 mg = f2_same(-s[0] / (float)width), mx = f2_same(-s[1] / (float)width);
-        T* dx = static_cast<T*>(a.y) + k * a.yw + (int64_t)row * a.yr;
+        const f2 mg = f2_same(-s[0] * inv_width), mx = f2_same(-s[1] * inv_width);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             f2 t[H], (&xi)[H] = xh[kKeep ? i : 0], (&gi)[H] = g[kKeep ? i : 0];
             if constexpr (!kKeep) load(i, xi, t, gi);
-            if constexpr (ADD) piece_wide<T>(ring.get(got * Q + 2 * N + i, r + (int64_t)row * a.rr, first + i * step, some), t);
+            if constexpr (ADD) piece_wide<T>(ring.get(got * Q + 2 * N + i, r, first + i * step, some), t);
 #pragma unroll
             for (int j = 0; j < H; ++j) {
                 const f2 v = f2_add(f2_fma(xi[j], mx, gi[j]), mg);
@@ -382,6 +432,9 @@ __global__ void __launch_bounds__(32 * WARPS, CTAS) norm_backward_kernel(const _
             piece_store<T, WIDE>(dx, first + i * step, some, piece_narrow<T>(t));
         }
         got = got + 1 == S ? 0 : got + 1;
+        if constexpr (!WIDE) { x += x_step; dy += d_step; }
+        if constexpr (!WIDE && ADD) r += r_step;
+        dx += y_step;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                      // the ring's place is free
