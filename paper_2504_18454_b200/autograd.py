@@ -123,6 +123,8 @@ class _LayerNorm(torch.autograd.Function):
 class _CrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, in_place):
+        if in_place and logits.is_leaf and logits.requires_grad:
+            raise RuntimeError("cross_entropy: the gradient of a leaf's logits cannot take their place")
         loss, lse = block.cross_entropy_forward(logits, targets)
         ctx.in_place = in_place
         ctx.save_for_backward(logits, targets, lse)

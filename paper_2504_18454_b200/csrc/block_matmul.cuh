@@ -425,8 +425,8 @@ __device__ __forceinline__ f2 act_pair(f2 g, f2& slope)
 }
 
 // The same for the linear operator: GELU of a pair that is rounded to bfloat16 by the rational approximation of erf with one
-// exponential (Abramowitz and Stegun 7.1.26, off by at most 1.5e-7), which is also the slope's.  (erff for each value took the
-// pass before the activation from 9 us to 27: 5 workers of 4449 tokens, 144 columns.)
+// exponential (Abramowitz and Stegun 7.1.26, off by at most 1.5e-7), which is also the slope's.  (With erff for each value
+// the pass before the activation took 27 us, so 20: 5 workers of 4449 tokens, 144 columns.)
 template <typename T, int ACT, bool SLOPE>
 __device__ __forceinline__ f2 linear_act(f2 g, f2& slope)
 {
@@ -449,6 +449,35 @@ __device__ __forceinline__ f2 linear_act(f2 g, f2& slope)
         const f2 cdf = f2_of(x > 0.0f ? 1.0f - qx : qx, y > 0.0f ? 1.0f - qy : qy);
         // (a gate beyond 10^19: its square's exponential is 0, and so is what it multiplies)
         if constexpr (SLOPE) slope = f2_fma(f2_mul(f2_of(fminf(fmaxf(x, -1e4f), 1e4f), fminf(fmaxf(y, -1e4f), 1e4f)), f2_same(0.39894228040143268f)), e, cdf);
+        return f2_mul(g, cdf);
+    } else if constexpr (sizeof(T) == 4 && ACT == PALSGD_ACT_GELU) {
+        // fp32: the Chebyshev form of erfc that is off by at most 1.2e-7 of itself everywhere (Numerical Recipes, 6.2):
+        // Phi(-|g|) = erfc(z) / 2, z = |g| / sqrt(2), erfc(z) = t e^(-z^2 + P(t)), t = 1 / (1 + z / 2)
+        float x, y, tx, ty, ex, ey;
+        f2_get(g, x, y);
+        const f2 z = f2_of(fabsf(x) * 0.70710678118654752f, fabsf(y) * 0.70710678118654752f);
+        f2_get(f2_fma(z, f2_same(0.5f), f2_same(1.0f)), tx, ty);
+        const f2 t = f2_of(fast_inverse(tx), fast_inverse(ty));
+        f2 p = f2_fma(t, f2_same(0.17087277f), f2_same(-0.82215223f));
+        p = f2_fma(p, t, f2_same(1.48851587f));
+        p = f2_fma(p, t, f2_same(-1.13520398f));
+        p = f2_fma(p, t, f2_same(0.27886807f));
+        p = f2_fma(p, t, f2_same(-0.18628806f));
+        p = f2_fma(p, t, f2_same(0.09678418f));
+        p = f2_fma(p, t, f2_same(0.37409196f));
+        p = f2_fma(p, t, f2_same(1.00002368f));
+        p = f2_fma(p, t, f2_same(-1.26551223f));
+        const f2 zz = f2_mul(z, z);
+        f2_get(f2_mul(f2_add(p, f2_neg(zz)), f2_same(1.4426950408889634f)), ex, ey);
+        float qx, qy;
+        f2_get(f2_mul(f2_mul(t, f2_same(0.5f)), f2_of(fast_exp2(ex), fast_exp2(ey))), qx, qy);
+        const f2 cdf = f2_of(x > 0.0f ? 1.0f - qx : qx, y > 0.0f ? 1.0f - qy : qy);
+        if constexpr (SLOPE) {
+            float wx, wy;
+            f2_get(f2_mul(zz, f2_same(-1.4426950408889634f)), wx, wy);
+            slope = f2_fma(f2_mul(f2_of(fminf(fmaxf(x, -1e4f), 1e4f), fminf(fmaxf(y, -1e4f), 1e4f)), f2_same(0.39894228040143268f)),
+                           f2_of(fast_exp2(wx), fast_exp2(wy)), cdf);
+        }
         return f2_mul(g, cdf);
     } else {
         return act_pair<T, ACT, SLOPE>(g, slope);

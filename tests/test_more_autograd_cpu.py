@@ -115,6 +115,8 @@ def test_in_place_the_gradient_takes_the_logits_memory(plain):
     loss = A.cross_entropy(logits, TARGETS, in_place=True).sum()
     assert torch.allclose(torch.autograd.grad(loss, z, retain_graph=True)[0], want)
     assert not torch.equal(logits, z * 2)
+    with pytest.raises(RuntimeError, match="leaf"):
+        A.cross_entropy(z, TARGETS, in_place=True)
 
 
 def test_the_model_of_the_trainer_has_the_tensors_of_the_gptneo_lists():
