@@ -505,15 +505,20 @@ int with_act(int act, F&& f)
     }
 }
 
-// Whether a call goes to the kernel of few tokens: up to eight, or so little work that the matrix kernel would take longer to
-// start than this one takes in all.  (Measured at 256 x 683, fp32, 4 x 17 tokens: matrix kernel 29 us; see kFewWork.)
-constexpr uint64_t kFewWorkBf16 = 60000000, kFewWorkFp32 = 200000000;   // multiplications, tokens in whole eights
+// Whether a call goes to the kernel of few tokens, by what the two take.  That kernel: some 4 us and one for each 8.6 million
+// multiplications, tokens in whole eights (less for up to four tokens, where reading the weights is what it does).
+// bfloat16: the matrix kernel takes 11.5 us for any small call (768 x 2048: 16 tokens 5.3 us here; 8 workers of 8 tokens 16.1, and
+// 14.2 there; 2048 x 5632: 4 tokens 8.9 and 17.0, 8 workers of 4 tokens 44.0 and 43.6, of 8 tokens 90 and 43).
+// fp32: there the operands are rewritten in three parts first, 22 us and 3.3 for each million weights (8 x 32 tokens, 768 x 2048:
+// 48.5 us here, 67 there; 8 x 64 tokens: 95 and 69; one token, 2048 x 5632: 7.2 and 67).
+constexpr uint64_t kFewWorkBf16 = 80000000, kFewWorkFp32 = 150000000, kFewPerWeight = 28;
 bool few_tokens(const palsgd_linear_shape* s)
 {
-    const uint64_t tiles = ceil_div(s->tokens, kFewTokens);
-    if (tiles <= 1) return true;
+    const uint64_t tiles = ceil_div(s->tokens, kFewTokens), few = s->precision == PALSGD_PREC_FP32 ? kFewTokens : 4;
+    if (s->tokens <= few) return true;
     if (tiles > 65535 || s->d_in > (1u << 20) || s->d_out > (1u << 20) || s->tokens > (1u << 16)) return false;     // (no product below overflows)
-    return tiles * kFewTokens * s->K * s->d_in * s->d_out <= (s->precision == PALSGD_PREC_FP32 ? kFewWorkFp32 : kFewWorkBf16);
+    const uint64_t weights = s->K * s->d_in * s->d_out, work = tiles * kFewTokens * weights;
+    return s->precision == PALSGD_PREC_FP32 ? work <= kFewWorkFp32 + kFewPerWeight * weights : work <= kFewWorkBf16;
 }
 
 // Few tokens.  The inner axis is cut into slices for the CTA's warps while there are fewer CTAs than the device

@@ -11,7 +11,7 @@ DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
 # K, tokens, d_in, d_out: one token, odd everything, few tokens, one tile, just past a tile, several tiles, a long inner axis
 SIZES = [(1, 1, 1, 1), (1, 1, 64, 128), (2, 3, 7, 5), (1, 8, 2056, 40), (3, 5, 513, 33), (2, 9, 24, 33), (3, 129, 65, 257), (1, 128, 64, 256),
          (4, 17, 256, 683), (2, 300, 264, 520), (1, 40, 4104, 72), (1, 1000, 40, 48), (2, 257, 136, 1000), (1, 16, 40, 1500), (2, 17, 300, 1025), (3, 512, 100, 70), (1, 40, 9000, 1030),
-         (2, 700, 600, 601)]
+         (2, 700, 600, 601), (1, 100, 9000, 265)]
 
 
 def _inputs(K, M, D, N, dt, seed=1):
@@ -52,10 +52,10 @@ def test_forward(dtype, size, save):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("bias", [False, True])
 @pytest.mark.parametrize("residual", [False, True])
-@pytest.mark.parametrize("M", [3, 40, 700])
+@pytest.mark.parametrize("M", [3, 40, 130, 700])
 def test_every_part_of_the_epilogue(dtype, bias, residual, M):
-    """One call of few tokens, one whose inner axis is cut into shares, one of whole tiles."""
-    x, w, b, r, _, _ = _inputs(2, M, 520 if M != 40 else 4096, 264, DT[dtype], seed=5)
+    """A call of few tokens, two whose inner axis is cut into shares (in fp32 the longer one), one of whole tiles."""
+    x, w, b, r, _, _ = _inputs(2, M, 4096 if M in (40, 130) else 520, 264, DT[dtype], seed=5)
     b, r = b if bias else None, r if residual else None
     for kind in (NONE, P.ACT_RELU):
         y, _ = P.linear_forward(x, w, b, r, activation=kind)

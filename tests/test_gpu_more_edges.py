@@ -266,3 +266,36 @@ def test_python_refusals():
             call()
             pytest.fail(f"call {i} was not refused")
     torch.cuda.synchronize()
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    """Nothing has been set up on the device before: every operator's first call is inside a capture."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2504_18454_b200 as P
+x, w, lw = (torch.ones(*s, device="cuda", dtype=torch.bfloat16) for s in ((2, 2100, 64), (2, 600, 64), (2, 64)))
+t, d = torch.zeros(2, 2100, device="cuda", dtype=torch.int32), torch.ones(2, 2100, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    n, total, mean, rstd = P.layer_norm_forward(x, lw, lw, x)
+    y, z = P.linear_forward(x, w, activation=P.ACT_SILU, save=P.SAVE_8BIT)
+    few, _ = P.linear_forward(x[:, :3], w)
+    grads = P.linear_backward(y, x, w, z, activation=P.ACT_SILU)
+    few_grads = P.linear_backward(y[:, :3], x[:, :3], w)
+    norm_grads = P.layer_norm_backward(x, total, lw, mean, rstd)
+    loss, lse = P.cross_entropy_forward(y, t)
+    dz = P.cross_entropy_backward(d, y, t, lse)
+g.replay()
+torch.cuda.synchronize()
+assert bool((n == 1).all()) and bool((total == 2).all()) and bool((few == 64).all()) and bool((y == 64).all())
+assert bool((few_grads[1] == 192).all()) and bool((norm_grads[2] == 2096).all())
+assert abs(float(loss[0, 0]) - 6.3969) < 1e-3
+P.block_status()
+print("done")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "done" in r.stdout, r.stderr[-2000:]
