@@ -128,7 +128,7 @@ cudaError_t allow_smem() { return cudaFuncSetAttribute(mat_kernel<T, MODE, ACT>,
 template <typename T>
 cudaError_t allow_smem_all()
 {
-    const cudaError_t e[14] = {allow_smem<T, MAT_PLAIN, 0>(),
+    const cudaError_t e[16] = {allow_smem<T, MAT_PLAIN, 0>(), allow_smem<T, MAT_SUMS, 0>(), allow_smem<bf16, MAT_ROWS, 0>(),
                               allow_smem<T, MAT_GATED, 0>(), allow_smem<T, MAT_GATED, 1>(), allow_smem<T, MAT_GATED, 2>(), allow_smem<T, MAT_GATED, 3>(),
                               allow_smem<T, MAT_HIDDEN, 0>(), allow_smem<T, MAT_HIDDEN, 1>(), allow_smem<T, MAT_HIDDEN, 2>(), allow_smem<T, MAT_HIDDEN, 3>(),
                               allow_smem<T, MAT_LINEAR, 0>(), allow_smem<T, MAT_LINEAR, 1>(), allow_smem<T, MAT_LINEAR, 2>(), allow_smem<T, MAT_LINEAR, 3>(),
@@ -220,7 +220,7 @@ int run_stage(const Stage& st, uint32_t K, int sms, cudaStream_t stream)
     if (st.n == 0) return PALSGD_OK;
     uint64_t most = 1;
     for (uint32_t i = 0; i < st.n; ++i) most = st.a.item[i].units > most ? st.a.item[i].units : most;
-    const uint64_t want = ceil_div(most, 1024), cap = 8ull * sms;
+    const uint64_t want = ceil_div(most, 256), cap = 32ull * sms;
     return launch("operand copies", stage_kernel, dim3((unsigned)(want < cap ? want : cap), st.n, K), 256, 0, stream, st.a);
 }
 
@@ -341,7 +341,7 @@ int launch_mat(const MatLaunch& L, uint32_t pairs, cudaStream_t st)
 template <typename T, int MODE>
 int launch_mat(const MatLaunch& L, int act, uint32_t pairs, cudaStream_t st)
 {
-    if constexpr (MODE == MAT_PLAIN) {
+    if constexpr (mat_plain(MODE)) {
         return launch_mat<T, MODE, 0>(L, pairs, st);
     } else {
         if constexpr (MODE == MAT_LINEAR) if (act == PALSGD_ACT_NONE) return launch_mat<T, MODE, PALSGD_ACT_NONE>(L, pairs, st);
@@ -360,7 +360,8 @@ int run_mat(MatLaunch& L, const palsgd_ffn_shape* s, const Device& d, cudaStream
     if (L.tiles == 0) return PALSGD_OK;
     L.gave_up = d.gave_up;
     const uint32_t pairs = (uint32_t)(d.sms / 2) < L.tiles ? (uint32_t)(d.sms / 2) : L.tiles;
-    return s->precision == PALSGD_PREC_FP32 ? launch_mat<float, MODE>(L, s->activation, pairs, st) : launch_mat<bf16, MODE>(L, s->activation, pairs, st);
+    if constexpr (MODE != MAT_ROWS) if (s->precision == PALSGD_PREC_FP32) return launch_mat<float, MODE>(L, s->activation, pairs, st);
+    return launch_mat<bf16, MODE>(L, s->activation, pairs, st);
 }
 
 // Decides on the shares and takes the workspace for their sums (the same decision in both calls of an entry point: it
@@ -432,7 +433,9 @@ int run_products(Product* p, int n, const palsgd_ffn_shape* s, const Device& d, 
         if (i + 1 == heavy) L.heavy = L.tiles;
     }
     if (heavy) L.lag = (uint32_t)(p[0].length(parts) / p[n - 1].length(parts));
-    BLOCK_TRY(run_mat<MAT_PLAIN>(L, s, d, st));
+    if (sums && sums->part) BLOCK_TRY(run_mat<MAT_SUMS>(L, s, d, st));
+    else if (sums && sums->rows) BLOCK_TRY(run_mat<MAT_ROWS>(L, s, d, st));
+    else BLOCK_TRY(run_mat<MAT_PLAIN>(L, s, d, st));
     return joins == 0 || !joined ? PALSGD_OK : run_join(join, joins, units, s->K, es, d.sms, st);
 }
 
@@ -596,6 +599,22 @@ int run_few_backward(const palsgd_linear_shape* s, FewBackArgs& a, cudaStream_t 
                   grid, 256, 0, st, a);
 }
 
+// Whether the bias gradient of a dy that is read in place is summed beside the products, by the matrix kernel's spare warps:
+// where their turns (of 64 rows, about four steps of the products long) end before the products do.  (The backward
+// call with a pass of its own over dy and so: 8 workers of 1024 tokens, 2048 -> 768, 45.4 and 42.8 us; 2 of 8192 tokens,
+// 5632 -> 2048, 540 and 518, 2048 -> 6144, 695 and 665.)
+bool sums_beside(const Product* p, int n, const palsgd_linear_shape* s, uint32_t parts)
+{
+    uint64_t tiles = 0, work = 0;
+    for (int i = 0; i < n; ++i) {
+        tiles += p[i].tiles(s->K) * p[i].splits;
+        work += p[i].tiles(s->K) * p[i].splits * p[i].length(parts);
+    }
+    const uint64_t most = (uint64_t)sm_count() / 2, pairs = tiles < most ? tiles : most;
+    const uint64_t turns = ceil_div(s->K * ceil_div(s->d_out, kSumsCols), 2 * pairs) * ceil_div(s->tokens, kSumsRows);
+    return s->precision == PALSGD_PREC_BF16_MASTER && 4 * turns <= work / pairs;
+}
+
 // Lanes side by side in the pass before the activation, and rows of a CTA: as many CTAs as run at a time, down to one turn of
 // their lanes each (their sums are joined beside the products, in a launch that comes anyway).
 uint32_t slope_lanes(const palsgd_linear_shape* s)
@@ -620,7 +639,7 @@ int run_slope(const palsgd_linear_shape* s, SlopeArgs& a, const Stage& copies, i
     uint32_t all = a.ctas = (uint32_t)ctas;
     for (uint32_t i = 0; i < kMaxStaged; ++i) {
         a.first_copy[i] = all;
-        const uint64_t want = i < copies.n ? ceil_div(copies.a.item[i].units, 1024) : 0, cap = 8ull * sms;
+        const uint64_t want = i < copies.n ? ceil_div(copies.a.item[i].units, 512) : 0, cap = 4ull * sms;
         all += (uint32_t)(want < cap ? want : cap);
     }
     a.first_copy[kMaxStaged] = all;
@@ -1022,7 +1041,7 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
     const uint32_t parts = s->precision == PALSGD_PREC_FP32 ? 3 : 1;
     Operand odz, ox, ow;
     SlopeArgs slope{};
-    bool pass = false;                                   // dz is formed, or summed, by a pass of its own
+    bool pass = false, beside = false;                   // dz is formed, or summed, by a pass of its own; db beside the products
     Product products[2];
     int n_products = 0;
     const bool few = few_backward(s);
@@ -1042,12 +1061,9 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
             slope.dst = static_cast<bf16*>(const_cast<void*>(odz.p));
             slope.dstw = odz.w; slope.ld = odz.r; slope.dst_part = odz.part;
         }
-        pass = write || db.given;
         slope.rows = slope_rows(s);
         slope.lanes = slope_lanes(s);
         slope.part_ld = (uint32_t)N;
-        if (db.given && slope.rows >= M) { slope.db = db.m.data; slope.dbw = db.m.worker_stride; }
-        else if (db.given) slope.part = static_cast<float*>(ws.take((size_t)s->K * ceil_div(M, slope.rows) * slope.part_ld * sizeof(float)));
         ox = input_operand(ws, stage, x, x_e, s->precision, s->K, M, D);
         if (dx.given) {
             ow = input_operand(ws, stage, w, nullptr, s->precision, s->K, N, D);
@@ -1055,6 +1071,10 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
         }
         products[n_products++] = Product{N, D, M, &odz, nullptr, &ox, nullptr, true, true, dw, 1, nullptr};
         take_shares(ws, products, n_products, s->K, parts);
+        beside = db.given && !write && sums_beside(products, n_products, s, parts);
+        pass = write || (db.given && !beside);
+        if (pass && db.given && slope.rows >= M) { slope.db = db.m.data; slope.dbw = db.m.worker_stride; }
+        else if (pass && db.given) slope.part = static_cast<float*>(ws.take((size_t)s->K * ceil_div(M, slope.rows) * slope.part_ld * sizeof(float)));
     }
     BLOCK_TRY(settle(ws, workspace_bytes, all));
     if (!workspace) return PALSGD_OK;
@@ -1104,7 +1124,8 @@ extern "C" int palsgd_linear_backward(const palsgd_linear_shape* s, const palsgd
         BLOCK_TRY(run_stage(stage, s->K, dev.sms, st));
     }
     const palsgd_ffn_shape f = products_of(s);
-    const MatSums sums{slope.part, db.m.data, db.m.worker_stride, slope.part ? (uint32_t)ceil_div(M, slope.rows) : 0, (uint32_t)N, slope.part_ld, s->K};
+    const MatSums sums{slope.part, beside ? dy.m.data : nullptr, dy.m.worker_stride, dy.m.row_stride, db.m.data, db.m.worker_stride,
+                       beside ? (uint32_t)M : slope.part ? (uint32_t)ceil_div(M, slope.rows) : 0, (uint32_t)N, slope.part_ld, s->K};
     return run_products(products, n_products, &f, dev, es, parts, st, true, &sums);
 }
 

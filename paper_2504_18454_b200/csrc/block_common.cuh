@@ -92,11 +92,9 @@ __device__ __forceinline__ uint4 shift16(const uint4& a, const uint4& b, uint32_
     for (int i = 0; i < 5; ++i) w[i] = o & 4 ? w[i + 1] : w[i];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], s);
-    if (bytes < 16) {
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)                  // what lies behind the row's end is not of it
-            if (4 * i + 4 > bytes) w[i] = 4 * i >= bytes ? 0u : w[i] & ((1u << (8 * (bytes & 3))) - 1u);
-    }
+    for (uint32_t i = 0; i < 4; ++i)                      // what lies behind the row's end is not of it
+        if (4 * i + 4 > bytes) w[i] = 4 * i >= bytes ? 0u : w[i] & ((1u << (8 * (bytes & 3))) - 1u);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ uint4 get16(const unsigned char* p, uint32_t bytes)

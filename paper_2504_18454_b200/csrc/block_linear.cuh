@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ S
     if (blockIdx.x >= a.ctas) {
         uint32_t i = 0;
         while (blockIdx.x >= a.first_copy[i + 1]) ++i;
-        stage_item(copies.item[i], k, blockIdx.x - a.first_copy[i], a.first_copy[i + 1] - a.first_copy[i]);
+        stage_item<4>(copies.item[i], k, blockIdx.x - a.first_copy[i], a.first_copy[i + 1] - a.first_copy[i]);
         return;
     }
     const uint32_t chunk = blockIdx.x / a.strips, strip = blockIdx.x - chunk * a.strips;

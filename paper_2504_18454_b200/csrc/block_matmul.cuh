@@ -29,7 +29,9 @@
 namespace palsgd {
 namespace block {
 
-enum { MAT_PLAIN = 0, MAT_GATED = 1, MAT_HIDDEN = 2, MAT_LINEAR = 3 };
+// MAT_SUMS, MAT_ROWS: plain, with column sums beside the products, of partial sums or of a matrix
+enum { MAT_PLAIN = 0, MAT_GATED = 1, MAT_HIDDEN = 2, MAT_LINEAR = 3, MAT_SUMS = 4, MAT_ROWS = 5 };
+constexpr __host__ __device__ bool mat_plain(int mode) { return mode == MAT_PLAIN || mode == MAT_SUMS || mode == MAT_ROWS; }
 
 constexpr uint32_t kTileM = 256, kTileN = 256, kTileK = 64;
 constexpr uint32_t kOperandBytes = 128 * kTileK * 2;                    // a CTA's half of an operand's tile
@@ -73,17 +75,21 @@ struct alignas(64) MatProblem {
     MatOut   out[3];              // plain: the product; gate/up: h; hidden: dg, du, h; linear: y
 };
 
-// Rows of binary32 sums [K][parts][ld] that other CTAs have left, joined in a fixed order beside the products.
+// Column sums beside the products, in a fixed order: of rows of binary32 sums [K][parts][ld] that other CTAs have left, or of
+// a matrix itself (bfloat16, rows on 16-byte boundaries).
 struct MatSums {
     const float* part;            // NULL: none
+    const void*  rows;            // NULL: none
+    int64_t  rows_w, rows_r;
     void*    out;
     int64_t  w;                   // worker stride of out
-    uint32_t parts, cols, ld, K;
+    uint32_t parts, cols, ld, K;  // parts: rows of either
 };
+constexpr uint32_t kSumsCols = 64, kSumsRows = 64;        // of a matrix: columns of a warp, rows under way
 
 struct MatLaunch {
     MatProblem p[kMaxProblems];
-    MatSums  sums;                // plain
+    MatSums  sums;                // sums, rows
     uint32_t n_problems, tiles, heavy, lag;   // see Order
     int      save;
     MatOut   gate, up;            // saved (gate/up pass) or read (hidden pass)
@@ -523,7 +529,7 @@ __device__ __forceinline__ Tile tile_at(const MatLaunch& a, uint32_t t)
     uint32_t i = 0;
     while (i + 1 < a.n_problems && t >= a.p[i].tiles) { t -= a.p[i].tiles; ++i; }
     const MatProblem& p = a.p[i];
-    const uint32_t w = p.per_worker.of(t), i_w = t - w * p.per_worker.d, s = MODE == MAT_PLAIN ? p.per_split.of(i_w) : 0, r = i_w - s * p.per_split.d;
+    const uint32_t w = p.per_worker.of(t), i_w = t - w * p.per_worker.d, s = mat_plain(MODE) ? p.per_split.of(i_w) : 0, r = i_w - s * p.per_split.d;
     const uint32_t n = p.tiles_m.of(r), m = r - n * p.tiles_m.d;
     return Tile{w, m * kTileM, n * (MODE == MAT_GATED ? kTileN / 2 : kTileN), s, &p};
 }
@@ -684,11 +690,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             }
         }
     } else if (warp == 2) {
-        // plain: the sums of a bias gradient, 32 columns at a time (a kernel of its own for them took 4 us)
-        if constexpr (MODE == MAT_PLAIN) {
-            const MatSums& q = a.sums;
-            const uint32_t groups = (q.cols + 31) / 32, all = q.part ? groups * q.K : 0;
-            for (uint32_t g = blockIdx.x; g < all; g += gridDim.x) {
+        // the sums of a bias gradient (a kernel of its own for them took 4 us, a pass over dy 6; with the code for both in the plain
+        // kernel, calls without them took 8 % longer)
+        const MatSums& q = a.sums;
+        if constexpr (MODE == MAT_SUMS) {
+            const uint32_t groups = (q.cols + 31) / 32;
+            for (uint32_t g = blockIdx.x; g < groups * q.K; g += gridDim.x) {
                 const uint32_t k = g / groups, c = (g - k * groups) * 32 + lane;
                 if (c >= q.cols) continue;
                 const float* at = q.part + (uint64_t)k * q.parts * q.ld + c;
@@ -700,8 +707,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                     for (uint32_t i = 0; i < 8; ++i) if (r + i < q.parts) v[i] += at[(uint64_t)(r + i) * q.ld];
                 static_cast<T*>(q.out)[(int64_t)k * q.w + c] = from_f<T>(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
             }
-            __syncwarp();
+        } else if constexpr (MODE == MAT_ROWS) {
+            // eight lanes have a row's 64 columns, four rows side by side, sixteen of each under way
+            const uint32_t groups = (q.cols + kSumsCols - 1) / kSumsCols;
+            for (uint32_t g = blockIdx.x; g < groups * q.K; g += gridDim.x) {
+                const uint32_t k = g / groups, c = (g - k * groups) * kSumsCols + (lane & 7) * 8;
+                const bf16* at = static_cast<const bf16*>(q.rows) + (int64_t)k * q.rows_w + c;
+                const bool on = c < q.cols;
+                f2 sum[4] = {0, 0, 0, 0};
+                for (uint32_t r0 = lane >> 3; r0 < q.parts; r0 += kSumsRows) {
+                    uint4 v[kSumsRows / 4];
+#pragma unroll
+                    for (uint32_t i = 0; i < kSumsRows / 4; ++i) {
+                        const uint32_t r = r0 + 4 * i;
+                        v[i] = !on || r >= q.parts ? make_uint4(0, 0, 0, 0)
+                             : c + 8 <= q.cols ? __ldg(reinterpret_cast<const uint4*>(at + (int64_t)r * q.rows_r))
+                                               : get16(reinterpret_cast<const unsigned char*>(at + (int64_t)r * q.rows_r), 2 * (q.cols - c));
+                    }
+#pragma unroll
+                    for (uint32_t i = 0; i < kSumsRows / 4; ++i) {
+                        sum[0] = f2_add(sum[0], f2_wide(v[i].x)); sum[1] = f2_add(sum[1], f2_wide(v[i].y));
+                        sum[2] = f2_add(sum[2], f2_wide(v[i].z)); sum[3] = f2_add(sum[3], f2_wide(v[i].w));
+                    }
+                }
+#pragma unroll
+                for (int d = 8; d < 32; d *= 2)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = f2_add(sum[i], __shfl_xor_sync(0xFFFFFFFFu, sum[i], d));
+                if (lane < 8 && on) {
+                    float f[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f2_get(sum[i], f[2 * i], f[2 * i + 1]);
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) if (c + i < q.cols) static_cast<T*>(q.out)[(int64_t)k * q.w + c + i] = from_f<T>(f[i]);
+                }
+            }
         }
+        __syncwarp();
     } else if (warp >= 4) {
         const uint32_t quad = warp & 3, part = (warp - 4) >> 2;           // tensor memory rows of 32; share of the columns
         uint32_t it = 0;
@@ -767,7 +809,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 }
             }
             // (a warp whose rows or columns are all outside has nothing to do but to let the sums go)
-            const bool idle = (MODE == MAT_PLAIN || MODE == MAT_LINEAR) && (rows == 0 || tl.n0 + part * kMine >= p.N);
+            const bool idle = (mat_plain(MODE) || MODE == MAT_LINEAR) && (rows == 0 || tl.n0 + part * kMine >= p.N);
             if (!cut) {
                 if (!acc_wait()) break;
             } else if (MODE != MAT_GATED && MODE != MAT_HIDDEN && idle) {
@@ -863,7 +905,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
                 const uint32_t from = src + c * kCols, n = tl.n0 + part * kMine + c * kCols;
                 const uint32_t cols = n < p.N ? p.N - n : 0, room = n < p.out[0].cols ? p.out[0].cols - n : 0;
                 const int64_t at = w * p.out[0].w + (int64_t)m * p.out[0].r + n;
-                if constexpr (MODE == MAT_PLAIN) {
+                if constexpr (mat_plain(MODE)) {
                     if (E == 2 && p.splits > 1) {                         // binary32 sums of a share: 16 columns a block
                         float* to = static_cast<float*>(p.out[0].p) + (int64_t)tl.split * p.out[0].part + at;
 #pragma unroll 1
@@ -1124,17 +1166,20 @@ struct StageItem {
 };
 struct StageArgs { StageItem item[kMaxStaged]; };
 
-// Block `block` of the `blocks` that copy worker k's part of an item: a thread has four units under way.
+// Block `block` of the `blocks` that copy worker k's part of an item: a thread has U units under way (one where the grid
+// holds a thread a unit: with four, a feed-forward backward call of 4 workers of 500 tokens, 333 x 1001, took 10.4 us for
+// its copies instead of 6.9).
+template <uint32_t U>
 __device__ __forceinline__ void stage_item(const StageItem& it, int64_t k, uint32_t block, uint32_t blocks)
 {
-    constexpr uint32_t U = 4;
     if (k >= it.K) return;
-    for (uint64_t i0 = (uint64_t)block * (256 * U) + threadIdx.x; i0 < it.units; i0 += (uint64_t)blocks * (256 * U)) {
+    const uint64_t step = (uint64_t)blocks * 256;
+    for (uint64_t i0 = (uint64_t)block * 256 + threadIdx.x; i0 < it.units; i0 += U * step) {
         uint4 q[U][2];                                    // as they lie in memory; 8 bits: the exponent behind them
         int64_t to[U];
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
-            const uint64_t i = i0 + u * 256;
+            const uint64_t i = i0 + u * step;
             to[u] = -1;
             if (i >= it.units) continue;
             const uint64_t row = it.units < 0x80000000ull ? it.per_row.of((uint32_t)i) : i / it.per_row.d;
@@ -1184,7 +1229,7 @@ __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ Stag
 {
     let_next_start();
     wait_for_previous();
-    stage_item(a.item[blockIdx.y], blockIdx.z, blockIdx.x, gridDim.x);
+    stage_item<1>(a.item[blockIdx.y], blockIdx.z, blockIdx.x, gridDim.x);
 }
 
 // The shares' sums of a product, joined in a fixed order.

@@ -224,3 +224,24 @@ def test_several_tiles_of_a_pair(dtype, size, save):
     ref = linear_backward64(dy, x, w, z, P.ACT_SILU, dtype == "bf16")
     for t, name in zip(P.linear_backward(dy, x, w, saved, activation=P.ACT_SILU), ("dx", "dw", "db")):
         within(t, *ref[name], name)
+
+
+@pytest.mark.parametrize("size", [(1, 200, 7600, 2501), (3, 130, 6500, 1001), (1, 70, 4100, 9601), (2, 64, 9000, 1032)], ids=str)
+@pytest.mark.parametrize("need_dx", [False, True])
+def test_bias_gradients_beside_many_tiles(size, need_dx):
+    """Calls whose products take long enough for the sums of dy to run beside them: odd columns, ragged rows, more groups of columns
+    than CTAs."""
+    K, M, D, N = size
+    pad = (N + 7) // 8 * 8 + 8
+    dy = torch.full((K, M, pad), float("nan"), dtype=torch.bfloat16, device="cuda")[..., :N]
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    r = lambda *s, std=1.0: (torch.randn(*s, generator=gen, device="cuda") * std).bfloat16()
+    dy.copy_(r(K, M, N))
+    x, w = r(K, M, D), r(K, N, D, std=N ** -0.5)
+    dx, dw, db = P.linear_backward(dy, x, w, need_dx=need_dx)
+    ref = linear_backward64(dy, x, w, None, P.ACT_NONE, True)
+    assert (dx is not None) == need_dx
+    for a, name in ((dx, "dx"), (dw, "dw"), (db, "db")):
+        if a is not None:
+            within(a, *ref[name], name)
+    assert all(torch.equal(a, b) for a, b in zip((dw, db), P.linear_backward(dy, x, w, need_dx=need_dx)[1:]))
