@@ -536,15 +536,24 @@ __device__ __forceinline__ Tile tile_at(const MatLaunch& a, uint32_t t)
 
 __device__ __forceinline__ uint32_t pairs_of(const MatProblem& p) { return p.a_parts == 1 ? p.b_parts : p.b_parts == 1 ? p.a_parts : 6; }
 
+// bfloat16 products that go into an 8-bit checkpoint: steps of a piece.  How many of its values land on the other side of a
+// rounding goes by the sums' error.  A third of a short inner axis keeps it at that of binary32 multiply-adds (4 workers of
+// 3000 tokens, 256 -> 600: 22 of 7.2 million values, with one piece 49, with multiply-adds 13; 18.4 us, with one piece
+// 18.1; 512 -> 600: 44, with two pieces 51, with multiply-adds 37; 22.2 us, with two 20.0).
+__device__ __forceinline__ uint32_t piece_of(uint32_t inner)
+{
+    const uint32_t third = (inner + 3 * kTileK - 1) / (3 * kTileK);
+    return third < 2 ? 2 : third < kPiece ? third : kPiece;
+}
+
 // The inner axis of a tile -- its share of all segments' steps -- in pieces of one segment each:
 // f(segment, first step, end, begins a sum, ends it).  bfloat16: the pieces of a tile are one sum.  fp32: kPiece steps (with
 // all their parts) are a sum of their own, and the sums are joined in registers with rounding to nearest -- the tensor
 // cores cut off what an addition does not hold, which over long sums adds up (measured over 4096 steps of the inner axis
 // in one sum: 4.4e-6 of the result's norm; in pieces of 4: 2.4e-7, of 8: 4.8e-7, where the whole is 2 % faster).
-// `cut`: whether sums are cut into pieces.  (Of bfloat16 products, those that go into an 8-bit checkpoint are: how many of
-// its values land on the other side of a rounding goes by the sums' error.)
+// `cut`: steps of a piece, 0: sums are not cut.
 template <typename F>
-__device__ __forceinline__ bool for_pieces(const Tile& tl, bool cut, F&& f)
+__device__ __forceinline__ bool for_pieces(const Tile& tl, uint32_t cut, F&& f)
 {
     const MatProblem& p = *tl.p;
     const uint32_t steps = (p.Kd + kTileK - 1) / kTileK, all = p.n_seg * steps;
@@ -556,7 +565,7 @@ __device__ __forceinline__ bool for_pieces(const Tile& tl, bool cut, F&& f)
     for (bool first = true; g < last; first = false) {
         const uint32_t seg = g >= steps, k = g - seg * steps;
         uint32_t n = min(steps - k, last - g);
-        if (cut) n = min(n, kPiece);
+        if (cut) n = min(n, cut);
         g += n;
         if (!f(seg, k, k + n, cut || first, cut || g == last)) return false;
     }
@@ -576,7 +585,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
     const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, rank = cluster_rank();
     const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
-    const bool cut = Shape::kWide || (MODE == MAT_LINEAR && a.save == PALSGD_SAVE_8BIT);
+    const uint32_t cut = Shape::kWide ? kPiece : MODE == MAT_LINEAR && a.save == PALSGD_SAVE_8BIT ? piece_of(a.p[0].Kd) : 0;
 
     let_next_start();
     if (threadIdx.x == 0) {
@@ -815,7 +824,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
             } else if (MODE != MAT_GATED && MODE != MAT_HIDDEN && idle) {
                 bool ok = true;
                 uint32_t pieces = 0;
-                for_pieces(tl, true, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
+                for_pieces(tl, cut, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
                 while (ok && --pieces) {
                     ok = acc_wait();
                     if (ok) acc_read();
@@ -828,7 +837,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MatShape<T, MODE>::k
 #pragma unroll
                 for (int i = 0; i < 64; ++i) sum[i] = 0.0f;
                 uint32_t pieces = 0;
-                for_pieces(tl, true, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
+                for_pieces(tl, cut, [&](uint32_t, uint32_t, uint32_t, bool, bool) { ++pieces; return true; });
                 bool ok = true;
                 for (;;) {
                     src = tmem + (it & 1) * kTileN + (quad << 21) + part * kMine;
@@ -1168,7 +1177,7 @@ struct StageArgs { StageItem item[kMaxStaged]; };
 
 // Block `block` of the `blocks` that copy worker k's part of an item: a thread has U units under way (one where the grid
 // holds a thread a unit: with four, a feed-forward backward call of 4 workers of 500 tokens, 333 x 1001, took 10.4 us for
-// its copies instead of 6.9).
+// its copies instead of 7.3).
 template <uint32_t U>
 __device__ __forceinline__ void stage_item(const StageItem& it, int64_t k, uint32_t block, uint32_t blocks)
 {
