@@ -293,7 +293,9 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const __grid_constant__ S
     if (blockIdx.x >= a.ctas) {
         uint32_t i = 0;
         while (blockIdx.x >= a.first_copy[i + 1]) ++i;
-        stage_item<4>(copies.item[i], k, blockIdx.x - a.first_copy[i], a.first_copy[i + 1] - a.first_copy[i]);
+        const uint32_t block = blockIdx.x - a.first_copy[i], blocks = a.first_copy[i + 1] - a.first_copy[i];
+        if (copies.item[i].kind == STAGE_BF16) stage_item<2>(copies.item[i], k, block, blocks);   // (rows off the boundaries: two reads a unit)
+        else stage_item<4>(copies.item[i], k, block, blocks);
         return;
     }
     const uint32_t chunk = blockIdx.x / a.strips, strip = blockIdx.x - chunk * a.strips;
