@@ -255,6 +255,8 @@ __device__ __forceinline__ f2 act2(f2 g, f2& slope)
     }
 }
 
+__device__ __forceinline__ float f2_total(f2 v) { float a, b; f2_get(v, a, b); return a + b; }
+
 // ---- eight values of a row at any address, the first `n` of them inside it (the others read as 0, and are not written).
 // wide: eight values of every row start on a 16-byte boundary.
 template <typename T>

@@ -15,8 +15,8 @@ struct LinearEnd {                // what follows the sums
 //
 // Up to eight tokens at a time: bound by reading the weights once (for more tokens, by the multiplications: small calls).  A warp takes four rows of w over its slice of the inner axis, in
 // pieces of 16 bytes a lane, and multiplies each with all of the tokens in binary32 (the tokens come from the caches).  A CTA's
-// eight warps are `rows` row groups by slices; slices are joined in shared memory in order, and one thread finishes each
-// value.  (The matrix kernel's tile of one token multiplies 255 rows of zeros, and a few outputs give it too few tiles.)
+// eight warps are `groups` row groups by slices; slices are joined in shared memory in order, and one thread finishes each
+// value.  (bfloat16, 8 workers of one token, 2048 -> 5632: 36 us for 185 MB, 28 at the rate of a copy.  The matrix kernel's tile of one token multiplies 255 rows of zeros, and a few outputs give it too few tiles.)
 constexpr uint32_t kFewTokens = 8, kFewRows = 4;
 
 struct FewArgs {
@@ -234,7 +234,8 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
 // dz = dy act'(z) as the products' operand (bfloat16, or fp32 in three parts; dst NULL: dy itself is the operand), and its
 // sums over a CTA's rows, unrounded, to the CTA's row of `part` -- or, where one CTA has all rows, the gradient of the bias
 // itself.  `lanes` lanes have a row side by side, eight columns each, and a warp 32 / lanes rows.  Bound by memory; a lane has
-// as many rows under way as it has registers for.  The copies of other operands ride along in CTAs of their own.
+// as many rows under way as it has registers for (bfloat16, tanh GELU, 2 x 4096 tokens, 5632 columns: 50 us for 277 MB, 42 at the
+// rate of a copy).  The copies of other operands ride along in CTAs of their own.
 struct SlopeArgs {
     const void *dy, *pre;         // pre: NULL without an activation
     const uint8_t* pre_e;         // 8 bits
