@@ -223,12 +223,14 @@ __global__ void __launch_bounds__(256) loss_backward_kernel(const __grid_constan
             return;
         }
         if constexpr (sizeof(T) == 2) {
-            const f2 shift = f2_same(-lse * kLog2e), scale = f2_same(kLog2e), dd = f2_same(d);
+            // (first the difference, exact or rounded once, then its scale: as multiply-add with lse log2(e), that product's rounding,
+            // and its overflow, does not cancel where z is near lse)
+            const f2 shift = f2_same(-lse), scale = f2_same(kLog2e), dd = f2_same(d);
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float x, y;
-                f2_get(f2_fma(f2_of(v[2 * i], v[2 * i + 1]), scale, shift), x, y);
+                f2_get(f2_mul(f2_add(f2_of(v[2 * i], v[2 * i + 1]), shift), scale), x, y);
                 x = fast_exp2(x); y = fast_exp2(y);
                 if (c + 2 * i == t) x -= 1.0f;
                 if (c + 2 * i + 1 == t) y -= 1.0f;
