@@ -134,7 +134,9 @@ class _CrossEntropy(torch.autograd.Function):
     def backward(ctx, dloss):
         _once("cross_entropy")
         logits, targets, lse = ctx.saved_tensors
-        return block.cross_entropy_backward(_rows(dloss), logits, targets, lse, out=logits if ctx.in_place else None), None, None
+        # (detached: the same memory and version, without the logits' own place in the graph)
+        out = logits.detach() if ctx.in_place else None
+        return block.cross_entropy_backward(_rows(dloss), logits, targets, lse, out=out), None, None
 
 
 def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
