@@ -120,11 +120,24 @@ class _LayerNorm(torch.autograd.Function):
         return dx, dw, db, dx if ctx.added else None, None, None
 
 
+def _leaf_memory(t: torch.Tensor) -> bool:
+    """Whether t is a leaf that takes a gradient, or a view of one.  (A leaf may itself be a view, of an arena's buffer, so that
+    the base that a view names need not be the leaf: its gradient's way is followed for as long as it goes to one tensor.)"""
+    if t.is_leaf or not t.requires_grad:
+        return t.requires_grad
+    node, further = None, [t.grad_fn]
+    while len(further) == 1:
+        node, = further
+        further = [f for f, _ in node.next_functions if f is not None]
+    leaf = getattr(node, "variable", None)
+    return leaf is not None and t.numel() > 0 and leaf.untyped_storage().data_ptr() == t.untyped_storage().data_ptr()
+
+
 class _CrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, in_place):
-        if in_place and logits.is_leaf and logits.requires_grad:
-            raise RuntimeError("cross_entropy: the gradient of a leaf's logits cannot take their place")
+        if in_place and _leaf_memory(logits):
+            raise RuntimeError("cross_entropy: the gradient of a leaf's logits cannot take their place, nor that of a view of a leaf")
         loss, lse = block.cross_entropy_forward(logits, targets)
         ctx.in_place = in_place
         ctx.save_for_backward(logits, targets, lse)
@@ -165,5 +178,5 @@ def layer_norm(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, residual: Opti
 def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, *, in_place: bool = False) -> torch.Tensor:
     """`block.cross_entropy_forward`'s losses (K, tokens) with a gradient for the logits.  in_place: the backward pass writes the
     gradient over the logits, which nothing may need any more (autograd tells where it does; a product's backward pass does not
-    need its result)."""
+    need its result) and which may be neither a leaf nor a view of one."""
     return _CrossEntropy.apply(logits, targets, in_place)

@@ -40,3 +40,28 @@ def test_the_gradient_is_a_tensor_of_its_own_in_the_logits_memory():
     assert g.data_ptr() == logits.data_ptr() and torch.allclose(g, want)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):       # the logits are gone
         torch.autograd.grad(loss, logits)
+
+
+@pytest.mark.parametrize("own", [True, False])
+@pytest.mark.parametrize("view", [lambda p: p.view(2, 5, 6), lambda p: p.view(1, 10, 6)[:, 2:].view(2, 4, 6), lambda p: p.view(2, 5, 6)[:, :, 1:], lambda p: p.view(5, 2, 6).transpose(0, 1)])
+def test_a_view_of_a_leaf_is_refused(view, own):
+    """The gradient would be written over the parameter, be it a tensor of its own or (as an arena's) a view of a buffer."""
+    p = torch.empty(60, dtype=torch.float64) if own else torch.empty(2, 90, dtype=torch.float64)[1, 30:]
+    p = p.copy_(_leaf().detach().view(60)).detach().requires_grad_()
+    before = p.detach().clone()
+    z = view(p)
+    with pytest.raises(RuntimeError, match="leaf"):
+        A.cross_entropy(z, TARGETS[:, :z.shape[1]].clamp_max(4), in_place=True)
+    A.cross_entropy(z, TARGETS[:, :z.shape[1]].clamp_max(4)).sum().backward()
+    assert torch.equal(p, before) and p.grad is not None and p.grad.data_ptr() != p.data_ptr()
+
+
+def test_a_view_of_a_result_is_not():
+    z = _leaf()
+    want, = torch.autograd.grad(A.cross_entropy(z * 2, TARGETS).sum(), z)
+    logits = (z * 2).view(10, 6).view(2, 5, 6)
+    got, = torch.autograd.grad(A.cross_entropy(logits, TARGETS, in_place=True).sum(), z)
+    assert torch.allclose(got, want)
+    bent = z.exp().clamp_max(50.0)                         # one input all the way down to the leaf, but memory of its own
+    A.cross_entropy(bent, TARGETS, in_place=True).sum().backward()
+    assert z.grad is not None
