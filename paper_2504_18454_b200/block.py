@@ -305,10 +305,13 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, mean
 def cross_entropy_forward(logits: torch.Tensor, targets: torch.Tensor, *, out: Optional[Tuple] = None,
                           stream: Optional[int] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """palsgd_cross_entropy_forward: (loss, lse), both (K, tokens) float32, of logits (K, tokens, vocab) at targets
-    (K, tokens) int32.  A target below 0 does not count (loss 0); one beyond the vocabulary gives NaN."""
+    (K, tokens) int32.  A target below 0 does not count (loss 0); one beyond the vocabulary gives NaN.  `out` = (loss, lse) gives the
+    memory to write to; entries may be None."""
     native = _native or _ext()
-    loss, lse = (None, None) if out is None else out
-    return native.loss_forward(logits, targets, loss, lse, stream)
+    out = (None,) * 2 if out is None else out
+    if len(out) != 2:
+        _refuse("palsgd_cross_entropy_forward", "out must be (loss, lse)")
+    return native.loss_forward(logits, targets, *out, stream)
 
 
 def cross_entropy_backward(dloss: torch.Tensor, logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, *,
