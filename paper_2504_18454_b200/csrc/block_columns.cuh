@@ -1,4 +1,5 @@
-// Sums over tokens of the block operators' weight gradients: CTAs leave binary32 rows in the workspace, joined here.
+// Sums over tokens of the block operators' weight gradients: CTAs leave binary32 rows in the workspace, joined here; zeros where there
+// are no tokens.
 #pragma once
 #include "block_common.cuh"
 
@@ -45,6 +46,20 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__
         const uint32_t m = i / a.wrap, c = i - m * a.wrap;
         if (c < a.inside) static_cast<T*>(a.out[0])[(int64_t)k * a.ow[0] + m * a.row + c] = from_f<T>(t);
     }
+}
+
+// Weight gradients of no tokens: up to three matrices of zeros.
+struct ZeroArgs { void* p[3]; int64_t w[3], r[3]; uint32_t rows[3], cols[3]; };
+
+template <typename T>
+__global__ void __launch_bounds__(256) zero_kernel(const __grid_constant__ ZeroArgs a)
+{
+    let_next_start();
+    wait_for_previous();
+    const uint32_t i = blockIdx.y;
+    T* p = static_cast<T*>(a.p[i]) + (int64_t)blockIdx.z * a.w[i];
+    for (uint32_t r = blockIdx.x; r < a.rows[i]; r += gridDim.x)
+        for (uint32_t c = threadIdx.x; c < a.cols[i]; c += 256) p[(int64_t)r * a.r[i] + c] = from_f<T>(0.0f);
 }
 
 }  // namespace block

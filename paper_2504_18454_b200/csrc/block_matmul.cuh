@@ -1339,18 +1339,5 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinA
     }
 }
 
-struct ZeroArgs { void* p[3]; int64_t w[3], r[3]; uint32_t rows[3], cols[3]; };
-
-template <typename T>
-__global__ void __launch_bounds__(256) zero_kernel(const __grid_constant__ ZeroArgs a)
-{
-    let_next_start();
-    wait_for_previous();
-    const uint32_t i = blockIdx.y;
-    T* p = static_cast<T*>(a.p[i]) + (int64_t)blockIdx.z * a.w[i];
-    for (uint32_t r = blockIdx.x; r < a.rows[i]; r += gridDim.x)
-        for (uint32_t c = threadIdx.x; c < a.cols[i]; c += 256) p[(int64_t)r * a.r[i] + c] = from_f<T>(0.0f);
-}
-
 }  // namespace block
 }  // namespace palsgd

@@ -193,6 +193,15 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     all.writes(region(dx, s->K, M, D, es)); all.writes(region(dw, s->K, 1, D, es)); all.writes(region(db, s->K, 1, D, es));
     BLOCK_TRY(settle(ws, workspace_bytes, all));
     if (!workspace) return PALSGD_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (M == 0) {                                         // (addresses of matrices without rows may be anything)
+        ZeroArgs z{};
+        z.p[0] = dw.m.data; z.w[0] = dw.m.worker_stride;
+        z.p[1] = db.m.data; z.w[1] = db.m.worker_stride;
+        z.rows[0] = z.rows[1] = 1;
+        z.cols[0] = z.cols[1] = (uint32_t)D;
+        return launch("zero weight gradients", es == 4 ? zero_kernel<float> : zero_kernel<bf16>, dim3(1, 2, s->K), 256, 0, st, z);
+    }
     NormArgs a{};
     a.x = x.m.data; a.xw = x.m.worker_stride; a.xr = x.m.row_stride;
     a.r = past.m.data; a.rw = past.m.worker_stride; a.rr = past.m.row_stride;
@@ -206,7 +215,6 @@ extern "C" int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const pals
     a.rows = M; a.width = (uint32_t)D; a.lanes = t.lanes;
     const bool wide = (D * es) % 16 == 0 && norm_wide(dy, es) && norm_wide(x, es) && norm_wide(w, es) && norm_wide(past, es) && norm_wide(dx, es);
     const dim3 grid(ctas, s->K);
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
     BLOCK_TRY((es == 4 ? launch_norm<float, true>(a, t, wide, past.given, grid, st) : launch_norm<bf16, true>(a, t, wide, past.given, grid, st)));
     if (!part) return PALSGD_OK;
     ColumnSumArgs c{part, {dw.m.data, db.m.data}, {dw.m.worker_stride, db.m.worker_stride}, ctas, (uint32_t)(2 * D), part_ld, (uint32_t)D, (uint32_t)D, (uint32_t)D, 0};
