@@ -234,6 +234,9 @@ int palsgd_layer_norm_backward(const palsgd_norm_shape* s, const palsgd_mat* dy,
  * Logits of -infinity take no part (a target of that logit: loss +infinity).  A row that holds NaN or +infinity, or nothing
  * above -infinity, gives NaN in loss and gradient; its lse is NaN, or -infinity where nothing is above that.
  * Backward, at the given lse:  dlogits = (e^(z - lse) - [target]) dloss.  dlogits may be exactly logits: work in place.
+ * The given lse is rounded to binary32, which the exponential feels as 2^-24 |lse| of itself.  From |lse| = 1024 on, one within 2^-22 of
+ * itself of the row's own is taken as the row's own before rounding, formed again from the row (1 / vocab for a row of nothing but the
+ * type's lowest value); rows of such an lse take five to seven times as long as others.
  * Sums in binary32, in a fixed order; dlogits are rounded once to the storage type.
  * Errors: EINVAL (NULL, K, vocab = 0, a size >= 2^31, overlapping buffers); EUNSUPPORTED (backward: more than 2^31 - 1
  * parts of rows of up to 2048 16-byte pieces, of a worker); EALIGN; ECUDA.

@@ -317,6 +317,6 @@ def cross_entropy_forward(logits: torch.Tensor, targets: torch.Tensor, *, out: O
 def cross_entropy_backward(dloss: torch.Tensor, logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, *,
                            out: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> torch.Tensor:
     """palsgd_cross_entropy_backward: the gradient of the logits from dloss (K, tokens) float32.  `out` may be the logits
-    themselves: work in place."""
+    themselves: work in place.  (Of a large lse that is the row's own, the part that its rounding took is formed again.)"""
     native = _native or _ext()
     return native.loss_backward(dloss, logits, targets, lse, out, stream)

@@ -4,8 +4,8 @@
 // 16 bytes at a time with the next four -- of the next row, at a row's end -- under way; lanes, then warps, join theirs.  Rows are
 // read by the aligned 16-byte pieces that hold their values (a vocabulary of odd size starts every row at another offset), what
 // is outside set to -infinity.
-// Backward: e^(z - lse) from what the forward call left, one read and one write a value.
-// Backward bound by memory (bfloat16, 8 x 512 rows of 50257: 126 us, 823 MB at the rate of a copy), forward in fp32 too (8 x 512 rows
+// Backward: e^(z - lse) from what the forward call left, one read and one write a value (rows of a large lse are read twice).
+// Backward bound by memory (bfloat16, 8 x 512 rows of 50257: 128 us, 823 MB at 98 % of the rate of a copy), forward in fp32 too (8 x 512 rows
 // of 32768: 82 us, as a copy), in bfloat16 by its instructions and exponentials (8 x 512 rows of 50257: 88 us, 63 at the rate of a
 // copy; with one largest value a piece instead of four pieces 91).
 #pragma once
@@ -195,10 +195,33 @@ __global__ void __launch_bounds__(1024) loss_forward_kernel(const __grid_constan
 // any address.
 constexpr uint32_t kLossPieces = 8;                       // of a lane
 
+// From here on binary32 holds lse to 2^-14 at best, and nothing of the sum where a row has nothing but the type's lowest value.  An
+// lse that is the row's own, to its rounding, then gives way to the row's largest value and sum, formed again; any other is taken as
+// it is.  One warp has the row: all of it is read before its gradient is written over it.  (By the whole team, its barriers left room
+// for fewer CTAs: bfloat16, 8 x 512 x 50257, near rows 149 us, so 128, without far rows in the kernel 126.5; all rows far 833.)
+constexpr float kFarLse = 1024.0f;
+template <typename T>
+__device__ __noinline__ void loss_far_row(const T* z, T* dz, uint32_t vocab, int32_t t, float d, float lse, uint32_t lane)
+{
+    Soft s{-INFINITY, 0.0f};
+    for (uint32_t c = lane; c < vocab; c += 32) s = soft_join(s, Soft{to_f(z[c]), 1.0f});
+#pragma unroll
+    for (int b = 16; b; b >>= 1)
+        s = soft_join(s, Soft{__shfl_xor_sync(0xFFFFFFFFu, s.top, b), __shfl_xor_sync(0xFFFFFFFFu, s.sum, b)});
+    float rest = logf(s.sum);
+    if (fabsf((s.top + rest) - lse) <= 0x1p-22f * fabsf(lse)) lse = s.top;
+    else rest = 0.0f;
+    for (uint32_t c = lane; c < vocab; c += 32) {
+        float p = expf((to_f(z[c]) - lse) - rest);
+        if (c == (uint32_t)t) p -= 1.0f;
+        dz[c] = from_f<T>(p * d);
+    }
+}
+
 struct LossGrid { Divisor parts; uint32_t units; };       // parts of a row; parts of all rows of a worker
 
 template <typename T>
-__global__ void __launch_bounds__(256) loss_backward_kernel(const __grid_constant__ LossArgs a, const __grid_constant__ LossGrid g)
+__global__ void __launch_bounds__(256, 6) loss_backward_kernel(const __grid_constant__ LossArgs a, const __grid_constant__ LossGrid g)
 {
     constexpr int V = 16 / (int)sizeof(T), P = 4;
     const uint32_t warp = threadIdx.x >> 5, team = warp / a.warps, teams = (blockDim.x >> 5) / a.warps;
@@ -215,6 +238,10 @@ __global__ void __launch_bounds__(256) loss_backward_kernel(const __grid_constan
     const bool bad = t >= 0 && (uint32_t)t >= a.vocab;
     const float d = bad ? __uint_as_float(0x7FFFFFFFu) : t < 0 ? 0.0f : a.dloss[k * a.gw + row];
     const float lse = a.lse[k * a.sw + row];
+    if (fabsf(lse) >= kFarLse && fabsf(lse) < INFINITY && t >= 0) {
+        if (part == 0 && me < 32) loss_far_row(z, dz, a.vocab, t, d, lse, me);
+        return;
+    }
     auto gradient = [&](uint4& q, int64_t c) {            // the piece whose first value is the row's c-th
         float v[V];
         floats_of<T>(q, v);
