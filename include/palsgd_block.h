@@ -178,7 +178,9 @@ int palsgd_qk_norm_rope_backward(const palsgd_qk_shape* s, const palsgd_heads* d
  * BF16: dz is rounded to bfloat16 once, for the products; db sums the unrounded values.  dx and db may be NULL.  Outputs are
  * overwritten.  tokens = 0: dw and db are zero.  Sums have a fixed order: the same call gives the same bits.
  * FP32 products as in the feed-forward block; small calls sum in binary32 multiply-adds throughout, and keep dz in binary32.
- * BF16 GELU is off by at most 1.5e-7 (1 + |z|) before it is rounded, the other activations by a few units of binary32.
+ * An activation and its slope are off by at most 2^-21 (1 + |z|) each before they are rounded, in either type.  Far below zero that is
+ * more than they are, and calls of few and of many tokens differ there: GELU of the former is 0 below about -5.6, of the latter e^(-z^2 / 2)
+ * small, in fp32 to some 100 units in its last place.
  * Workspace and errors as for the feed-forward block (d_in or d_out = 0: EINVAL).
  */
 enum { PALSGD_ACT_NONE = 4 };

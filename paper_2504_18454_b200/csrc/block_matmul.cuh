@@ -483,8 +483,9 @@ __device__ __forceinline__ f2 act_pair(f2 g, f2& slope)
 }
 
 // The same for the linear operator: GELU of a pair that is rounded to bfloat16 by the rational approximation of erf with one
-// exponential (Abramowitz and Stegun 7.1.26, off by at most 1.5e-7), which is also the slope's.  (With erff for each value
-// the pass before the activation took 27 us, so 20: 5 workers of 4449 tokens, 144 columns.)
+// exponential (Abramowitz and Stegun 7.1.26, erf off by at most 1.5e-7; with the roundings of its evaluation y by some 2 and the slope by some 5
+// units of 2^-24 (1 + |g|)), which is also the slope's.  (With erff for each value the pass before the activation took 27 us, so 20: 5
+// workers of 4449 tokens, 144 columns.)
 template <typename T, int ACT, bool SLOPE>
 __device__ __forceinline__ f2 linear_act(f2 g, f2& slope)
 {
@@ -509,7 +510,8 @@ __device__ __forceinline__ f2 linear_act(f2 g, f2& slope)
         if constexpr (SLOPE) slope = f2_fma(f2_mul(f2_of(fminf(fmaxf(x, -1e4f), 1e4f), fminf(fmaxf(y, -1e4f), 1e4f)), f2_same(0.39894228040143268f)), e, cdf);
         return f2_mul(g, cdf);
     } else if constexpr (sizeof(T) == 4 && ACT == PALSGD_ACT_GELU) {
-        // fp32: the Chebyshev form of erfc that is off by at most 1.2e-7 of itself everywhere (Numerical Recipes, 6.2):
+        // fp32: the Chebyshev form of erfc that is off by at most 1.2e-7 of itself everywhere (Numerical Recipes, 6.2), as evaluated here by
+        // that and about the roundings of the exponent, |E| units in the last place of e^E:
         // Phi(-|g|) = erfc(z) / 2, z = |g| / sqrt(2), erfc(z) = t e^(-z^2 + P(t)), t = 1 / (1 + z / 2)
         float x, y, tx, ty, ex, ey;
         f2_get(g, x, y);
