@@ -591,9 +591,11 @@ __device__ __forceinline__ Tile tile_at(const MatLaunch& a, uint32_t t)
 __device__ __forceinline__ uint32_t pairs_of(const MatProblem& p) { return p.a_parts == 1 ? p.b_parts : p.b_parts == 1 ? p.a_parts : 6; }
 
 // bfloat16 products that go into an 8-bit checkpoint: steps of a piece.  How many of its values land on the other side of a
-// rounding goes by the sums' error.  A third of a short inner axis keeps it at that of binary32 multiply-adds (4 workers of
-// 3000 tokens, 256 -> 600: 22 of 7.2 million values, with one piece 49, with multiply-adds 13; 18.4 us, with one piece
-// 18.1; 512 -> 600: 44, with two pieces 51, with multiply-adds 37; 22.2 us, with two 20.0).
+// rounding goes by the sums' error.  Pieces of 128 to 256 terms, three of a short inner axis where they have that many, keep it at that of
+// binary32 multiply-adds (4 workers of 3000 tokens, 256 -> 600, two pieces: 22 of 7.2 million values, with one piece 49, with multiply-adds
+// 13; 18.4 us, with one piece 18.1; 512 -> 600, three pieces: 44, with two 51, with multiply-adds 37; 22.2 us, with two 20.0).  Of a launch
+// of few tiles, cut into shares, a share is one sum, not cut again (one worker, 512 tokens, 5632 -> 768: 20 of 1.6 million values, a product
+// in binary32 27; 1024 tokens, 8192 -> 512: 59 of 2.1 million, and 55).
 __device__ __forceinline__ uint32_t piece_of(uint32_t inner)
 {
     const uint32_t third = (inner + 3 * kTileK - 1) / (3 * kTileK);
