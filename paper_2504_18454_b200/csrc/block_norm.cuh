@@ -2,12 +2,13 @@
 //
 // A team of lanes -- 4 to 32 of a warp, or up to 32 warps -- has a row at a time in its registers: mean, then the mean square
 // around it (two passes over registers: a row whose mean is large against its spread loses what the mean is rounded by, not
-// the digits that a difference of squares would), then the result, in one pass over memory.  A team walks rows with the next ones under way; its columns of w (and b), and in the backward pass its
-// sums of dw and db, stay in registers over all of its rows.  The sums go to one row of the workspace for each CTA and are
-// joined in a fixed order; where one CTA has all of a worker's rows it writes the gradients itself.
-// Bound by memory: every byte is moved once.  (bfloat16, 2 x 16384 rows of 2048, with an addend: forward 100 us, backward 92 and 8 for
-// the join of its sums; 537 MB each, 82 us at the rate of a copy.  fp32: 196 and, with the join, 163, 164 at that rate.  Rows of 2001: 192 and 215, bound by the instructions that shift
-// pieces into place.)
+// the digits that a difference of squares would), then the result, in one pass over memory.  A team walks rows with the next
+// ones under way; its columns of w (and b), and in the backward pass its sums of dw and db, stay in registers over all of its
+// rows.  The sums go to one row of the workspace for each CTA and are joined in a fixed order; where one CTA has all of a
+// worker's rows it writes the gradients itself.
+// Bound by memory: every byte is moved once.  (bfloat16, 2 x 16384 rows of 2048, with an addend: forward 100 us, backward 92 and
+// 8 for the join of its sums; 537 MB each, 82 us at the rate of a copy.  fp32: forward 196, backward with the join 163, 164 at that
+// rate.  bfloat16, rows of 2001: 192 and 215, bound by the instructions that shift pieces into place.)
 #pragma once
 #include "block_common.cuh"
 
